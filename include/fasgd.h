@@ -503,9 +503,184 @@ FASGD_API int fasgd_sim_quadratic_loss(int64_t P, const float* theta, const floa
                                        const float* star, double* scratch, double* loss,
                                        void* stream);
 
+/*
+ * Client operators: what a client computes between a fetch and a push, besides
+ * its matrix products, when its model is a deep residual network (the paper's
+ * clients only say "compute a gradient", Sec. 2.1; no counterpart there).
+ * Activations are fp32, bf16 or fp16; parameters and their gradients are fp32,
+ * the server's type, and need 4-byte alignment only, so that they may be views
+ * into the flat vectors that are pulled and pushed.  Draws come from the same
+ * generator as the server's, keyed by (seed, client, n), so a client's step can
+ * be replayed.  No handle is needed.  The calls run on `stream` (a cudaStream_t,
+ * NULL = legacy default), on the current device, allocate nothing, can be
+ * captured, and give the same bits whenever they are given the same arguments.
+ *
+ * Arguments come in a struct; set what is not used to zero.  Matrices are rows
+ * of `cols` consecutive values, ld values from one row to the next (ld >= cols;
+ * not looked at where there are fewer than two rows); base and rows need the
+ * alignment of their type only.  16-byte aligned bases with rows that follow
+ * each other without a gap, or with cols and ld multiples of 8, take the fast
+ * kernels.  An output must not share memory with another argument, except as
+ * fasgd_dropout says.  Everything computed is held in fp32 and rounded once,
+ * where it is stored.  A call with rows = 0 reads nothing and writes zeros to
+ * the gradients of parameters.  Limits: rows <= 2^40, cols <= FASGD_COLS_MAX
+ * (fasgd_dropout: 2^40).
+ * Errors: EINVAL (text via fasgd_last_error(NULL)), ECUDA.
+ */
+enum fasgd_dtype { FASGD_F32 = 0, FASGD_BF16 = 1, FASGD_F16 = 2 };
+enum fasgd_norm { FASGD_RMS_NORM = 0, FASGD_LAYER_NORM = 1 };
+#define FASGD_COLS_MAX ((int64_t)1 << 20)
+
+/*
+ * fasgd_dropout -- out = residual + m x / (1 - rate), residual NULL: without it.
+ * The mask m is never stored: element r * cols + c (of the matrix, not of its
+ * memory) is draw i = index mod 8 of octet q = index div 8, the 16-bit half
+ * (i mod 2) of word (i div 2) of Philox4x32-10 at counter (q, client + 3 * 2^30,
+ * n, (n >> 32) + ((q >> 32) << 16)), key = seed.  It is kept (m = 1) iff the
+ * draw >= cut = floor(65536 rate + 1/2): the rate is rounded to a multiple of
+ * 2^-16, and kept values are scaled by 65536 / (65536 - cut), which that rate
+ * makes unbiased.  A dropped element contributes 0 whatever it holds, NaN
+ * included.  The gradient is the same call on the output's gradient, without
+ * the residual.  0 <= rate <= 1; 0 <= client < 2^30; n < 2^48; rows * cols < 2^51.
+ * out may be x or residual itself (same base and ld).
+ */
+typedef struct fasgd_dropout_args {
+    int64_t rows, cols;
+    const void* x;
+    int64_t ld_x;
+    const void* residual;
+    int64_t ld_residual;
+    void* out;
+    int64_t ld_out;
+    double rate;
+    uint64_t seed, n;
+    int32_t client;
+    int32_t dtype;              /* enum fasgd_dtype */
+} fasgd_dropout_args;
+FASGD_API int fasgd_dropout(const fasgd_dropout_args* a, void* stream);
+
+/*
+ * fasgd_join -- where a block's output y meets the residual stream x: the norm
+ * after the block, dropout, gate and residual scale, and the norm before the
+ * next block, in one pass:
+ *   t = N(y; post, post_bias)              (t = y where post is NULL)
+ *   u = dropout(t; rate, seed, client, n)  (exactly fasgd_dropout's mask)
+ *   h = carry x + branch gate u            (gate NULL: 1;  y NULL: h = x)
+ *   z = N(h; pre, pre_bias)                (where pre is not NULL)
+ * FASGD_RMS_NORM: N(t; w, b) = that w + b with that = t / sqrt(mean t^2 + eps);
+ * FASGD_LAYER_NORM: that = (t - mean t) / sqrt(mean (t - mean t)^2 + eps); a NULL
+ * bias is 0.  z is formed from the unrounded h.
+ * gate: groups x cols values without gaps, of type gate_dtype (FASGD_F32 or
+ * dtype); row r takes gate row r div (rows / groups) -- one learned vector
+ * (groups = 1), or one computed for each sequence or token.  groups divides
+ * rows, groups >= 1.
+ * Without y: post, gate, h and dy are NULL, pre is given (the first norm of a
+ * network).  h is written iff y is given, z iff pre is.  stats: fp32[4 rows],
+ * 16-byte aligned (mean and 1/sqrt of y, then of h), for the gradient; may be
+ * NULL.  eps > 0, finite; carry and branch finite.  0 <= rate <= 1 as above.
+ *
+ * fasgd_join_grad -- given the gradients dh (of h; NULL: zero) and dz (of z,
+ * where pre is given), those of x, y and the parameters.  It reads x, y and
+ * stats of the forward call (h is formed again, unrounded) and the same
+ * parameters and draws; h and z are not looked at.  dx is written, and dy iff y
+ * is given; dpost, dpost_bias, dpre, dpre_bias (fp32[cols]) and dgate (as gate)
+ * where not NULL.  Sums over rows are fp32 in a fixed order.  workspace:
+ * 16-byte aligned device memory of at least fasgd_join_workspace() bytes.
+ *
+ * fasgd_join_workspace -- that size, for the rows, cols, groups, dtype and
+ * pointers of a fasgd_join_grad call on the current device (the pointers' NULLs
+ * and alignments count, not what they point to); -1 on a bad argument.
+ */
+typedef struct fasgd_join_args {
+    int64_t rows, cols, groups;
+    const void* x;
+    int64_t ld_x;
+    const void* y;
+    int64_t ld_y;
+    void* h;
+    int64_t ld_h;
+    void* z;
+    int64_t ld_z;
+    const float* post;
+    const float* post_bias;
+    const void* gate;
+    const float* pre;
+    const float* pre_bias;
+    float* stats;
+    const void* dh;
+    int64_t ld_dh;
+    const void* dz;
+    int64_t ld_dz;
+    void* dx;
+    int64_t ld_dx;
+    void* dy;
+    int64_t ld_dy;
+    float* dpost;
+    float* dpost_bias;
+    void* dgate;
+    float* dpre;
+    float* dpre_bias;
+    void* workspace;
+    int64_t workspace_bytes;
+    double rate;
+    uint64_t seed, n;
+    int32_t client;
+    int32_t dtype;              /* enum fasgd_dtype: x, y, h, z and their gradients */
+    int32_t gate_dtype;         /* FASGD_F32, or dtype */
+    int32_t norm;               /* enum fasgd_norm */
+    float eps, carry, branch;
+    float reserved;             /* 0 */
+} fasgd_join_args;
+FASGD_API int fasgd_join(const fasgd_join_args* a, void* stream);
+FASGD_API int fasgd_join_grad(const fasgd_join_args* a, void* stream);
+FASGD_API int64_t fasgd_join_workspace(const fasgd_join_args* a);
+
+/*
+ * fasgd_balance -- a router's balance and z losses over rows = tokens and cols =
+ * experts (<= FASGD_EXPERTS_MAX), its per-expert counts, and the gradient of the
+ * logits, in one pass over the logits.
+ * p = softmax(logits row); lse = its log-sum-exp.  The rows form `groups` equal
+ * groups of consecutive rows (groups = 1: the whole batch; else one per
+ * sequence; groups divides rows).  valid: uint8[rows], 0 marks a row that does
+ * not take part, whatever it holds (its gradient is 0); NULL: all do.  chosen:
+ * int32[rows x top], without gaps: the experts each row was sent to; an entry
+ * outside [0, cols) is an assignment that was dropped.  With N_g valid rows in
+ * group g, G' groups that have any, N valid rows in all:
+ *   counts[g, e] = entries equal to e in the valid rows of g       (int32)
+ *   balance = 1/G' sum_g cols sum_e (counts[g,e] / (top N_g)) (1/N_g sum_t p_te)
+ *   z       = 1/N sum_t lse_t^2
+ *   loss[0..2] = balance_scale balance + z_scale z, balance, z     (fp32)
+ *   dlogits = upstream * d loss[0] / d logits                      (of logits' type)
+ * with the counts held constant, as they are by nature.  No valid row: all 0.
+ * A row whose logits are all -inf has p = 0 and lse = 0.  upstream: device float
+ * or NULL (1).  loss and dlogits may each be NULL; counts is always written.
+ * rows * top < 2^31.  workspace: 16-byte aligned device memory of at least
+ * fasgd_balance_workspace() bytes, which the shape alone fixes (-1 on a bad one).
+ */
+#define FASGD_EXPERTS_MAX 1024
+typedef struct fasgd_balance_args {
+    int64_t rows, cols, groups, top;
+    const void* logits;
+    int64_t ld_logits;
+    const int32_t* chosen;
+    const uint8_t* valid;
+    const float* upstream;
+    void* dlogits;
+    int64_t ld_dlogits;
+    int32_t* counts;
+    float* loss;
+    void* workspace;
+    int64_t workspace_bytes;
+    float balance_scale, z_scale;
+    int32_t dtype;              /* enum fasgd_dtype */
+    int32_t reserved;           /* 0 */
+} fasgd_balance_args;
+FASGD_API int fasgd_balance(const fasgd_balance_args* a, void* stream);
+FASGD_API int64_t fasgd_balance_workspace(const fasgd_balance_args* a);
+
 /* Text of the last failure on h, or, when h is NULL, of the last failed call
  * made without a handle (fasgd_create, bfasgd_fetch_apply, fasgd_sim_*,
- * bfasgd_select_compact_noalloc). */
+ * bfasgd_select_compact_noalloc, the client operators). */
 FASGD_API const char* fasgd_last_error(const fasgd_t* h);
 
 #ifdef __cplusplus

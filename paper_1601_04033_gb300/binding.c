@@ -20,7 +20,8 @@
 
 enum { F_PUSH, F_PUSH_HOST, F_PUSH_SPARSE, F_APPLY, F_SELECT, F_FETCH, F_FETCH_APPLY, F_PUSH_MESSAGE,
        F_FETCH_MESSAGE, F_PUSH_BUDGET, F_FETCH_BUDGET, F_PULL, F_TIMESTAMP, F_PENDING, F_SIM_GRAD,
-       F_SIM_LOSS, F_COUNT };
+       F_SIM_LOSS, F_DROPOUT, F_JOIN, F_JOIN_GRAD, F_JOIN_WORKSPACE, F_BALANCE, F_BALANCE_WORKSPACE,
+       F_COUNT };
 
 static PyObject* slow[F_COUNT];   /* the ctypes functions (install) */
 
@@ -99,6 +100,14 @@ ENTRY(fasgd_sim_quadratic_loss, F_SIM_LOSS, 7, 0x7e,
       fasgd_sim_quadratic_loss(I64(0), PTR(const float, 1), PTR(const float, 2), PTR(const float, 3),
                                PTR(double, 4), PTR(double, 5), PTR(void, 6)))
 
+ENTRY(fasgd_dropout, F_DROPOUT, 2, 0x3, fasgd_dropout(PTR(const fasgd_dropout_args, 0), PTR(void, 1)))
+ENTRY(fasgd_join, F_JOIN, 2, 0x3, fasgd_join(PTR(const fasgd_join_args, 0), PTR(void, 1)))
+ENTRY(fasgd_join_grad, F_JOIN_GRAD, 2, 0x3, fasgd_join_grad(PTR(const fasgd_join_args, 0), PTR(void, 1)))
+ENTRY(fasgd_join_workspace, F_JOIN_WORKSPACE, 1, 0x1, fasgd_join_workspace(PTR(const fasgd_join_args, 0)))
+ENTRY(fasgd_balance, F_BALANCE, 2, 0x3, fasgd_balance(PTR(const fasgd_balance_args, 0), PTR(void, 1)))
+ENTRY(fasgd_balance_workspace, F_BALANCE_WORKSPACE, 1, 0x1,
+      fasgd_balance_workspace(PTR(const fasgd_balance_args, 0)))
+
 /* fasgd_pull(h, params) -> (status, T) */
 static PyObject* py_fasgd_pull(PyObject* self, PyObject* const* args, Py_ssize_t nargs,
                                PyObject* kwnames) {
@@ -131,7 +140,8 @@ static const char* const names[F_COUNT] = {
     "fasgd_push", "fasgd_push_host", "fasgd_push_sparse", "fasgd_apply_pending", "bfasgd_select_compact",
     "bfasgd_fetch_compact", "bfasgd_fetch_apply", "bfasgd_push_message", "bfasgd_fetch_message",
     "bfasgd_push_budget", "bfasgd_fetch_budget", "fasgd_pull", "fasgd_timestamp", "fasgd_pending",
-    "fasgd_sim_quadratic_grad", "fasgd_sim_quadratic_loss"};
+    "fasgd_sim_quadratic_grad", "fasgd_sim_quadratic_loss", "fasgd_dropout", "fasgd_join",
+    "fasgd_join_grad", "fasgd_join_workspace", "fasgd_balance", "fasgd_balance_workspace"};
 
 /* install(namespace): keeps the ctypes functions of these names for the calls
  * this module does not take, and returns the names.  A namespace that holds one
@@ -176,7 +186,9 @@ static PyMethodDef methods[] = {
     METHOD(bfasgd_select_compact), METHOD(bfasgd_fetch_compact), METHOD(bfasgd_fetch_apply),
     METHOD(bfasgd_push_message), METHOD(bfasgd_fetch_message), METHOD(bfasgd_push_budget),
     METHOD(bfasgd_fetch_budget), METHOD(fasgd_pull), METHOD(fasgd_timestamp), METHOD(fasgd_pending),
-    METHOD(fasgd_sim_quadratic_grad), METHOD(fasgd_sim_quadratic_loss),
+    METHOD(fasgd_sim_quadratic_grad), METHOD(fasgd_sim_quadratic_loss), METHOD(fasgd_dropout),
+    METHOD(fasgd_join), METHOD(fasgd_join_grad), METHOD(fasgd_join_workspace), METHOD(fasgd_balance),
+    METHOD(fasgd_balance_workspace),
     {"install", py_install, METH_O, NULL}, {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, methods,

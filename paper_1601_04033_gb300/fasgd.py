@@ -67,8 +67,38 @@ SIGNATURES = {
     "fasgd_sim_quadratic_loss": (_i32, [_i64, _p, _p, _p, _p, _p, _p]),
     "bfasgd_select_compact_noalloc": (_i32, [_i64, _p, _p, _f32, _f32, _u64, _i32, _u64,
                                              _p, _p, _p, _p]),
+    "fasgd_dropout": (_i32, [_p, _p]),
+    "fasgd_join": (_i32, [_p, _p]),
+    "fasgd_join_grad": (_i32, [_p, _p]),
+    "fasgd_join_workspace": (_i64, [_p]),
+    "fasgd_balance": (_i32, [_p, _p]),
+    "fasgd_balance_workspace": (_i64, [_p]),
     "fasgd_last_error": (ctypes.c_char_p, [_p]),
 }
+
+F32, BF16, F16 = 0, 1, 2
+RMS_NORM, LAYER_NORM = 0, 1
+COLS_MAX, EXPERTS_MAX = 1 << 20, 1024
+
+
+def _struct(name, fields):
+    """A ctypes structure from "name:type" words (pointers as p, as in the C header)."""
+    kinds = {"p": _p, "i32": _i32, "i64": _i64, "u64": _u64, "f32": _f32, "f64": ctypes.c_double}
+    pairs = [f.split(":") for f in fields.split()]
+    return type(name, (ctypes.Structure,), {"_fields_": [(n, kinds[k]) for n, k in pairs]})
+
+
+# The argument structs of the client operators, field by field as in the header.
+DropoutArgs = _struct("DropoutArgs", "rows:i64 cols:i64 x:p ld_x:i64 residual:p ld_residual:i64 out:p "
+                      "ld_out:i64 rate:f64 seed:u64 n:u64 client:i32 dtype:i32")
+JoinArgs = _struct("JoinArgs", "rows:i64 cols:i64 groups:i64 x:p ld_x:i64 y:p ld_y:i64 h:p ld_h:i64 z:p "
+                   "ld_z:i64 post:p post_bias:p gate:p pre:p pre_bias:p stats:p dh:p ld_dh:i64 dz:p "
+                   "ld_dz:i64 dx:p ld_dx:i64 dy:p ld_dy:i64 dpost:p dpost_bias:p dgate:p dpre:p "
+                   "dpre_bias:p workspace:p workspace_bytes:i64 rate:f64 seed:u64 n:u64 client:i32 "
+                   "dtype:i32 gate_dtype:i32 norm:i32 eps:f32 carry:f32 branch:f32 reserved:f32")
+BalanceArgs = _struct("BalanceArgs", "rows:i64 cols:i64 groups:i64 top:i64 logits:p ld_logits:i64 chosen:p "
+                      "valid:p upstream:p dlogits:p ld_dlogits:i64 counts:p loss:p workspace:p "
+                      "workspace_bytes:i64 balance_scale:f32 z_scale:f32 dtype:i32 reserved:i32")
 
 NOALLOC_PMAX = 1 << 24
 BFASGD_TMAX = 4096
@@ -250,6 +280,30 @@ def bfasgd_select_compact_noalloc(P, grad, v, c, eps_b, seed, client, push_no, i
                                   n_dev, stream):
     return LIB.bfasgd_select_compact_noalloc(P, grad, v, c, eps_b, seed, client, push_no, idx,
                                              val, n_dev, stream)
+
+
+def fasgd_dropout(a, stream):
+    return LIB.fasgd_dropout(a, stream)
+
+
+def fasgd_join(a, stream):
+    return LIB.fasgd_join(a, stream)
+
+
+def fasgd_join_grad(a, stream):
+    return LIB.fasgd_join_grad(a, stream)
+
+
+def fasgd_join_workspace(a):
+    return LIB.fasgd_join_workspace(a)
+
+
+def fasgd_balance(a, stream):
+    return LIB.fasgd_balance(a, stream)
+
+
+def fasgd_balance_workspace(a):
+    return LIB.fasgd_balance_workspace(a)
 
 
 def fasgd_last_error(h) -> str:
