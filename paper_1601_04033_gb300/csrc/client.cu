@@ -210,9 +210,9 @@ int64_t lay_out(fasgd::JoinArgs& a, const fasgd::JoinPlan& plan, char* base) {
         at += up16(bytes);
         return p;
     };
-    a.params = reinterpret_cast<float*>(take(16 * plan.parts * a.cols));
+    a.params = reinterpret_cast<float*>(take(20 * plan.parts * a.cols));
     a.gates = reinterpret_cast<float*>(
-        take(a.out_gate != nullptr && plan.splits > 1 ? 4 * a.groups * plan.splits * a.cols : 0));
+        take(a.out_gate != nullptr && a.groups > 1 && plan.splits > 1 ? 4 * a.groups * plan.splits * a.cols : 0));
     a.row_means = reinterpret_cast<float2*>(take(8 * plan.row_means));
     return at;
 }

@@ -48,8 +48,8 @@ struct JoinArgs {
     void *dx, *dy;
     int64_t ld_dh, ld_dz, ld_dx, ld_dy;
     float2* row_means;       // per row: mean q hhat, mean q (the plain form only)
-    float* params;           // partial sums [parts][4][cols]: post, post_bias, pre, pre_bias
-    float* gates;            // partial sums [groups * splits][cols] of the gate's gradient
+    float* params;           // partial sums [parts][5][cols]: post, post_bias, pre, pre_bias, a single gate
+    float* gates;            // partial sums [groups * splits][cols] of the groups' gates (splits > 1)
     int64_t parts, splits;   // splits: units that each group's rows fall into; parts: blocks that take the units
     float* out_param[4];     // final gradients, each may be null
     void* out_gate;
@@ -76,10 +76,8 @@ struct BalanceArgs {
 cudaError_t launch_dropout(const DropoutArgs& a, int dtype, int num_sms, cudaStream_t stream);
 cudaError_t launch_join(const JoinArgs& a, int dtype, int num_sms, cudaStream_t stream);
 cudaError_t launch_join_grad(const JoinArgs& a, int dtype, int num_sms, cudaStream_t stream);
-// Whether the fast kernels take these arguments; parts, splits and row_means'
-// length of a gradient call.
+// parts, splits and row_means' length of a gradient call.
 struct JoinPlan {
-    bool fast;
     int64_t parts, splits, row_means;
 };
 JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms);

@@ -7,6 +7,7 @@
 // reading h would and keeps h's rounding out of the parameters' gradients.
 
 #include "join.cuh"
+#include "octet.cuh"
 #include "pdl.cuh"
 
 namespace fasgd {
@@ -115,7 +116,7 @@ __global__ void __launch_bounds__(kThreads) grad_columns_any_kernel(const __grid
     for (int64_t block = blockIdx.x; block < tiles * a.parts; block += gridDim.x) {
         const int64_t part = block / tiles, c = (block - part * tiles) * kThreads + threadIdx.x;
         if (c >= a.cols) continue;
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        float s[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
         for (int64_t unit = part; unit < a.groups * a.splits; unit += a.parts) {
             const int64_t group = unit / a.splits;
             const float gate = gate_at<T>(a, group, c);
@@ -134,26 +135,262 @@ __global__ void __launch_bounds__(kThreads) grad_columns_any_kernel(const __grid
                 s[2] += p.dz * p.hhat;
                 s[3] += p.dz;
             }
-            if (a.out_gate == nullptr) continue;
+            s[4] += g;
+            if (a.out_gate == nullptr || a.groups == 1) continue;
             if (a.splits > 1)
                 a.gates[unit * a.cols + c] = g;
             else
                 store_gate<T>(a, group * a.cols + c, g);
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (a.out_param[k] != nullptr) a.params[(part * 4 + k) * a.cols + c] = s[k];
+        for (int k = 0; k < 5; ++k)
+            if (k < 4 ? a.out_param[k] != nullptr : a.out_gate != nullptr && a.groups == 1) a.params[(part * 5 + k) * a.cols + c] = s[k];
     }
 }
 
 // The gate's gradients that grad_finish_kernel has to write: a unit that is a
-// whole group has written its own.
+// whole group has written its own.  A single gate is the fifth of the vectors.
 __host__ __device__ __forceinline__ int64_t gates_left(const JoinArgs& a) {
-    return a.out_gate != nullptr && (a.splits > 1 || a.rows == 0) ? a.groups : 0;
+    return a.out_gate != nullptr && a.groups > 1 && (a.splits > 1 || a.rows == 0) ? a.groups : 0;
+}
+
+// Rows in octets.  TPR threads hold a row, an octet each; every thread keeps its
+// columns' sums over the rows it takes in registers.  One reduction a row is
+// enough: with e = m scale branch gate post (so q2 = e dH) and w = dh + r_h q,
+//   sum q2 yhat = S(e yhat w) - r_h (mean q S(e yhat) + mean(q hhat) S(e yhat hhat)),
+// and the same without yhat for mean q2, so all sums are of what is known before
+// mean q is.  Units as in the plain form, for the threads of one row ("sub") at a
+// time; where cols is no multiple of 8 a unit's rows agree modulo 8 (octet.cuh).
+struct Unit {
+    int64_t row, step, rows;     // first row, from row to row, one past the last
+    __device__ Unit(const JoinArgs& a, int64_t unit) {
+        if (a.groups == 1) {
+            row = unit;
+            rows = a.rows;
+        } else {
+            const int64_t group = unit / a.splits, start = group * a.group_rows;
+            int64_t at = unit - group * a.splits;
+            if (a.cols & 7) at = (at & ~(int64_t)7) + ((at - start) & 7);
+            row = start + at;
+            rows = start + a.group_rows;
+        }
+        step = a.splits;
+    }
+};
+
+template <class T, int TPR, int STAGES, bool LAYER>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1) grad_rows_kernel(const __grid_constant__ JoinArgs a) {
+    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR, kP = kPieces<T>;
+    constexpr int kSums = LAYER ? 8 : 3;
+    extern __shared__ uint4 ring[];                  // [STAGES][x, y, dh, dz][kP][kBlock]
+    __shared__ __align__(16) float red[kSubs * 2 * kSums * (TPR < 32 ? 1 : TPR / 32)];
+    const int sub = threadIdx.x / TPR, lane = threadIdx.x % TPR;
+    const int64_t units = a.groups * a.splits, subs = (int64_t)gridDim.x * kSubs;
+    const int64_t mine = (int64_t)blockIdx.x * kSubs + sub;
+    const bool has_y = a.y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
+    const bool has_dh = a.dh != nullptr, gates = a.groups > 1;
+    RowSums<TPR, kSums> sums(red, sub);
+    pdl_wait();
+    pdl_trigger();
+
+    // All rows that this sub takes begin at the same place in an octet.
+    const int shift = mine < units ? (int)((Unit(a, mine).row * a.cols) & 7) : 0;
+    const Columns c(lane, shift, (int32_t)a.cols);
+    const Oct post = load_vector(a.post, c, 1.f), pre = load_vector(a.pre, c, 0.f);
+    Oct post_bias, gate;
+    if (LAYER) post_bias = load_vector(a.post_bias, c, 0.f);
+    Oct d_post = {}, d_post_bias = {}, d_gate = {}, d_pre = {}, d_pre_bias = {};
+
+    const int64_t end = (a.rows - 1) * a.cols + a.cols;     // where cols is no multiple of 8: rows follow without a gap
+    const bool ragged = (a.cols & 7) != 0;
+    const auto fetch = [&](int64_t r, int64_t rows, int stage) {
+        if (r < rows && c.any()) {
+            uint4* slot = ring + stage * 4 * kP * kBlock + threadIdx.x;
+            const int64_t left = ragged ? end - r * a.cols - c.c0 : kOctet;
+            copy_octet<T>(slot, kBlock, static_cast<const T*>(a.x) + r * a.ld_x, c, left);
+            if (has_y) copy_octet<T>(slot + kP * kBlock, kBlock, static_cast<const T*>(a.y) + r * a.ld_y, c, left);
+            if (has_dh)
+                copy_octet<T>(slot + 2 * kP * kBlock, kBlock, static_cast<const T*>(a.dh) + r * a.ld_dh, c, left);
+            if (has_pre)
+                copy_octet<T>(slot + 3 * kP * kBlock, kBlock, static_cast<const T*>(a.dz) + r * a.ld_dz, c, left);
+        }
+        copy_commit();
+    };
+
+    // Subs that share a warp or (units = subs) nothing: a warp's subs go on together.
+    const int64_t last_unit = units + (TPR < 32 ? sub % (32 / TPR) : 0);
+    for (int64_t unit = mine; unit < last_unit; unit += subs) {
+        Unit u(a, unit < units ? unit : 0);
+        if (unit >= units) u.rows = 0;
+        int64_t turns = u.row < u.rows ? (u.rows - u.row + u.step - 1) / u.step : 0;
+        if constexpr (TPR < 32) {
+#pragma unroll
+            for (int off = 16; off >= TPR; off >>= 1) {
+                const int64_t other = __shfl_xor_sync(0xffffffffu, turns, off);
+                turns = other > turns ? other : turns;
+            }
+        }
+        if (gates || unit == mine) {
+            gate = load_gate<T>(a, gates && unit < units ? unit / a.splits : 0, c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) gate.v[i] = mul2(gate.v[i], f2(a.branch));
+        }
+        if (gates) d_gate = Oct{};
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) fetch(u.row + s * u.step, u.rows, s);
+        int stage = 0;
+        int64_t r = u.row;
+        float4 st = r < u.rows ? a.stats[r] : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int64_t turn = 0; turn < turns; ++turn, r += u.step) {
+            const bool live = TPR >= 32 || r < u.rows;
+            // The next row's statistics, ahead of its turn.
+            const float4 next = r + u.step < u.rows ? a.stats[r + u.step] : make_float4(0.f, 0.f, 0.f, 0.f);
+            copy_wait<STAGES - 2>();
+            const uint4* slot = ring + stage * 4 * kP * kBlock + threadIdx.x;
+            Oct hhat = take_octet<T>(slot, kBlock, c), yhat = {}, w = {}, q = {}, e, uu;
+            if (has_y) yhat = take_octet<T>(slot + kP * kBlock, kBlock, c);
+            if (has_dh) w = take_octet<T>(slot + 2 * kP * kBlock, kBlock, c);
+            if (has_pre) q = take_octet<T>(slot + 3 * kP * kBlock, kBlock, c);
+            fetch(r + (STAGES - 1) * u.step, u.rows, stage == 0 ? STAGES - 1 : stage - 1);
+            stage = stage == STAGES - 1 ? 0 : stage + 1;
+            if (TPR < 32 && !live) {       // a row past the end: nothing of it may reach the sums
+                hhat = yhat = w = q = Oct{};
+            }
+            uint32_t bits = 0xffu;
+            if (a.drop.cut != 0 && c.any()) bits = kept_bits(a.drop, ((live ? r : 0) * a.cols + c.c0) >> 3);
+            float2 s2[kSums];
+#pragma unroll
+            for (int k = 0; k < kSums; ++k) s2[k] = f2(0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (has_y) {
+                    if (LAYER) yhat.v[i] = add2(yhat.v[i], f2(-st.x));
+                    yhat.v[i] = mul2(yhat.v[i], f2(st.y));
+                    float2 t = mul2(yhat.v[i], post.v[i]);
+                    if (LAYER) t = add2(t, post_bias.v[i]);
+                    float2 factor = gate.v[i];
+                    if (a.drop.cut != 0) {
+                        t = select2(bits, i, mul2(t, f2(a.drop.scale)));
+                        factor = select2(bits, i, mul2(factor, f2(a.drop.scale)));
+                    }
+                    hhat.v[i] = fma2(gate.v[i], t, mul2(hhat.v[i], f2(a.carry)));
+                    uu.v[i] = t;
+                    e.v[i] = factor;
+                }
+                if (has_pre) {
+                    if (LAYER) hhat.v[i] = add2(hhat.v[i], f2(-st.z));
+                    hhat.v[i] = mul2(hhat.v[i], f2(st.w));
+                    d_pre.v[i] = fma2(q.v[i], hhat.v[i], d_pre.v[i]);
+                    if (LAYER) d_pre_bias.v[i] = add2(d_pre_bias.v[i], q.v[i]);
+                    q.v[i] = mul2(q.v[i], pre.v[i]);
+                    s2[0] = fma2(q.v[i], hhat.v[i], s2[0]);
+                    if (LAYER) s2[3] = add2(s2[3], q.v[i]);
+                    w.v[i] = fma2(q.v[i], f2(st.w), w.v[i]);
+                }
+                if (has_post) {
+                    const float2 ep = mul2(e.v[i], post.v[i]), ey = mul2(ep, yhat.v[i]);
+                    s2[1] = fma2(ey, w.v[i], s2[1]);
+                    if (has_pre) s2[2] = fma2(ey, hhat.v[i], s2[2]);
+                    if (LAYER) {
+                        s2[4] = add2(s2[4], ey);
+                        s2[5] = fma2(ep, w.v[i], s2[5]);
+                        if (has_pre) s2[6] = fma2(ep, hhat.v[i], s2[6]);
+                        s2[7] = add2(s2[7], ep);
+                    }
+                }
+            }
+            float m1 = 0.f, m0 = 0.f, k1 = 0.f, k0 = 0.f;    // r_h times the means of q hhat and q; the means of q2 yhat and q2
+            if (has_pre || has_post) {
+                float s[kSums];
+#pragma unroll
+                for (int k = 0; k < kSums; ++k) s[k] = s2[k].x + s2[k].y;
+                sums(s);
+                if (has_pre) {
+                    m1 = s[0] * a.inv_cols * st.w;
+                    if (LAYER) m0 = s[3] * a.inv_cols * st.w;
+                }
+                if (LAYER) {
+                    k1 = (s[1] - m0 * s[4] - m1 * s[2]) * a.inv_cols;
+                    k0 = (s[5] - m0 * s[7] - m1 * s[6]) * a.inv_cols;
+                } else {
+                    k1 = (s[1] - m1 * s[2]) * a.inv_cols;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float2 d = w.v[i];
+                if (has_pre) {
+                    d = fma2(hhat.v[i], f2(-m1), d);
+                    if (LAYER) d = add2(d, f2(-m0));
+                }
+                if (has_y) {
+                    hhat.v[i] = mul2(d, f2(a.carry));
+                    d_gate.v[i] = fma2(d, uu.v[i], d_gate.v[i]);
+                    float2 dt = mul2(e.v[i], d);
+                    if (a.drop.cut != 0) dt = select2(bits, i, dt);
+                    if (has_post) {
+                        d_post.v[i] = fma2(dt, yhat.v[i], d_post.v[i]);
+                        if (LAYER) d_post_bias.v[i] = add2(d_post_bias.v[i], dt);
+                        dt = fma2(dt, post.v[i], mul2(yhat.v[i], f2(-k1)));
+                        if (LAYER) dt = add2(dt, f2(-k0));
+                        dt = mul2(dt, f2(st.y));
+                    }
+                    yhat.v[i] = dt;
+                } else {
+                    hhat.v[i] = d;
+                }
+            }
+            if (live) {
+                store_octet(static_cast<T*>(a.dx) + r * a.ld_dx, c, hhat);
+                if (has_y) store_octet(static_cast<T*>(a.dy) + r * a.ld_dy, c, yhat);
+            }
+            st = next;
+        }
+        copy_wait<0>();
+        if (gates && a.out_gate != nullptr && unit < units) {
+            const int64_t at = a.splits > 1 ? unit * a.cols : unit / a.splits * a.cols;
+#pragma unroll
+            for (int i = 0; i < kOctet; ++i)
+                if (c.in >> i & 1) {
+                    const float g = a.branch * element(d_gate, i);
+                    if (a.splits > 1)
+                        a.gates[at + c.c0 + i] = g;
+                    else
+                        store_gate<T>(a, at + c.c0 + i, g);
+                }
+        }
+    }
+
+    // The block's sums: its subs' in turn, joined in shared memory.
+    float* joint = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+        if (k == 4 ? gates || a.out_gate == nullptr : a.out_param[k] == nullptr) continue;
+        Oct& o = k == 0 ? d_post : k == 1 ? d_post_bias : k == 2 ? d_pre : k == 3 ? d_pre_bias : d_gate;
+        float* out = a.params + (blockIdx.x * 5 + k) * a.cols;
+        const float factor = k == 4 ? a.branch : 1.f;
+        if constexpr (kSubs == 1) {
+#pragma unroll
+            for (int i = 0; i < kOctet; ++i)
+                if (c.in >> i & 1) out[c.c0 + i] = factor * element(o, i);
+        } else {
+            for (int s = 0; s < kSubs; ++s) {
+                __syncthreads();
+                if (s == sub && mine < units) {
+#pragma unroll
+                    for (int i = 0; i < kOctet; ++i)
+                        if (c.in >> i & 1)
+                            joint[c.c0 + i] = s == 0 ? element(o, i) : joint[c.c0 + i] + element(o, i);
+                }
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < (int)a.cols; i += kBlock) out[i] = factor * joint[i];
+        }
+    }
 }
 
 // Joins the partial sums: a block takes 32 columns of one vector (the four
-// parameters' gradients, then the gate's, group by group); eight lanes of rows
+// parameters' gradients and a single gate's, then the groups' gates'); eight lanes of rows
 // take every eighth partial sum, then are added in order.
 template <class T>
 __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_constant__ JoinArgs a) {
@@ -161,13 +398,13 @@ __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_cons
     pdl_wait();
     pdl_trigger();
     const int64_t tiles = (a.cols + 31) / 32;
-    const int64_t vectors = 4 + gates_left(a);
+    const int64_t vectors = 5 + gates_left(a);
     const int lane = threadIdx.x & 31, slot = threadIdx.x >> 5;
     for (int64_t u = blockIdx.x; u < tiles * vectors; u += gridDim.x) {
         const int64_t vec = u / tiles, c = (u - vec * tiles) * 32 + lane;
-        if (vec < 4 && a.out_param[vec] == nullptr) continue;
-        const float* src = vec < 4 ? a.params + vec * a.cols : a.gates + (vec - 4) * a.splits * a.cols;
-        const int64_t step = vec < 4 ? 4 * a.cols : a.cols, count = vec < 4 ? a.parts : a.rows > 0 ? a.splits : 0;
+        if (vec < 4 ? a.out_param[vec] == nullptr : vec == 4 && (a.out_gate == nullptr || a.groups > 1)) continue;
+        const float* src = vec < 5 ? a.params + vec * a.cols : a.gates + (vec - 5) * a.splits * a.cols;
+        const int64_t step = vec < 5 ? 5 * a.cols : a.cols, count = vec < 5 ? a.parts : a.rows > 0 ? a.splits : 0;
         float s = 0.f;
         if (c < a.cols)
             for (int64_t i = slot; i < count; i += kThreads / 32) s += src[i * step + c];
@@ -180,7 +417,7 @@ __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_cons
             if (vec < 4)
                 a.out_param[vec][c] = s;
             else
-                store_gate<T>(a, (vec - 4) * a.cols + c, s);
+                store_gate<T>(a, (vec == 4 ? 0 : vec - 5) * a.cols + c, s);
         }
         __syncthreads();
     }
@@ -188,10 +425,52 @@ __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_cons
 
 int64_t at_most(int64_t n, int64_t cap) { return n < cap ? (n < 1 ? 1 : n) : cap; }
 
+// The threads of a row of the fast kernels (0: the plain form), and its blocks'.
+int threads_per_row(const JoinArgs& a) {
+    const int64_t octets = row_octets(a.cols);
+    const void* p[] = {a.x, a.y, a.dh, a.dz, a.dx, a.dy};
+    const int64_t ld[] = {a.ld_x, a.ld_y, a.ld_dh, a.ld_dz, a.ld_dx, a.ld_dy};
+    for (int i = 0; i < 6; ++i) {
+        if (!octet_matrix(p[i], ld[i], a.rows, a.cols)) return 0;
+        if (a.cols % 8 != 0 && a.rows > 1 && p[i] != nullptr && ld[i] != a.cols) return 0;
+    }
+    // A group's rows fall into eight classes where cols is no multiple of 8: short
+    // groups would leave more sums than rows.
+    if (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64) return 0;
+    for (int t : {8, 32, 64, 128, 256, 512})
+        if (octets <= t) return t;
+    return 0;
+}
+int blocks_per_sm(int threads) { return threads <= 256 ? 2 : 1; }
+
+template <class T, int TPR, bool LAYER>
+cudaError_t launch_rows(const JoinArgs& a, cudaStream_t stream) {
+    constexpr int kBlock = TPR < 256 ? 256 : TPR;
+    constexpr int kStages = sizeof(T) == 4 ? 3 : 4;
+    constexpr size_t kSmem = (size_t)kStages * 4 * kPieces<T> * kBlock * 16;
+    const cudaError_t st = cudaFuncSetAttribute(grad_rows_kernel<T, TPR, kStages, LAYER>,
+                                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    if (st != cudaSuccess) return st;
+    return launch_pdl(grad_rows_kernel<T, TPR, kStages, LAYER>, (unsigned)a.parts, kBlock, kSmem, stream, a);
+}
+template <class T, bool LAYER>
+cudaError_t launch_octets(const JoinArgs& a, int threads, cudaStream_t stream) {
+    switch (threads) {
+        case 8: return launch_rows<T, 8, LAYER>(a, stream);
+        case 32: return launch_rows<T, 32, LAYER>(a, stream);
+        case 64: return launch_rows<T, 64, LAYER>(a, stream);
+        case 128: return launch_rows<T, 128, LAYER>(a, stream);
+        case 256: return launch_rows<T, 256, LAYER>(a, stream);
+        default: return launch_rows<T, 512, LAYER>(a, stream);
+    }
+}
+
 template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     cudaError_t st = cudaSuccess;
-    if (a.rows > 0) {
+    if (const int threads = a.rows > 0 ? threads_per_row(a) : 0) {
+        st = a.layer ? launch_octets<T, true>(a, threads, stream) : launch_octets<T, false>(a, threads, stream);
+    } else if (a.rows > 0) {
         st = launch_pdl(grad_rows_any_kernel<T>, (unsigned)at_most(a.rows, (int64_t)num_sms * 8), kThreads, 0,
                         stream, a);
         const int64_t tiles = (a.cols + kThreads - 1) / kThreads;
@@ -199,7 +478,7 @@ cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
             st = launch_pdl(grad_columns_any_kernel<T>, (unsigned)at_most(tiles * a.parts, (int64_t)num_sms * 16),
                             kThreads, 0, stream, a);
     }
-    const int64_t vectors = 4 + gates_left(a);
+    const int64_t vectors = 5 + gates_left(a);
     if (st == cudaSuccess)
         st = launch_pdl(grad_finish_kernel<T>,
                         (unsigned)at_most((a.cols + 31) / 32 * vectors, (int64_t)num_sms * 64), kThreads, 0,
@@ -212,11 +491,27 @@ cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
 JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms) {
     (void)dtype;
     JoinPlan p;
-    p.fast = false;
-    p.splits = (2 * (int64_t)num_sms + a.groups - 1) / a.groups;
-    if (p.splits > a.group_rows) p.splits = a.group_rows;
-    if (p.splits < 1) p.splits = 1;
-    p.parts = a.rows > 0 ? at_most(a.groups * p.splits, 2 * (int64_t)num_sms) : 0;
+    p.parts = p.splits = p.row_means = 0;
+    if (a.rows == 0) return p;
+    if (const int threads = threads_per_row(a)) {
+        const int block_subs = threads < 256 ? 256 / threads : 1;
+        const int64_t most = (int64_t)num_sms * blocks_per_sm(threads) / 8 * 8 * block_subs;
+        if (a.groups == 1) {
+            p.splits = at_most(a.rows, most);
+        } else {
+            // Four units for each sub, but no fewer than eight rows to a unit: each
+            // leaves a row's worth of fp32 sums.
+            p.splits = at_most((4 * most + a.groups - 1) / a.groups, at_most(a.group_rows / 8, a.group_rows));
+            if (a.cols % 8 != 0) p.splits = (p.splits + 7) / 8 * 8;
+        }
+        const int64_t units = a.groups * p.splits;
+        p.parts = (at_most(units, most) + block_subs - 1) / block_subs;
+        if (a.groups == 1) p.splits = p.parts * block_subs;
+        return p;
+    }
+    const int64_t most = 2 * (int64_t)num_sms;
+    p.splits = at_most((most + a.groups - 1) / a.groups, a.group_rows);
+    p.parts = at_most(a.groups * p.splits, most);
     p.row_means = a.rows;
     return p;
 }
