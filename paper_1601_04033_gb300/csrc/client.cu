@@ -100,6 +100,7 @@ int fill_draws(const char* call, fasgd::DropArgs& d, double rate, uint64_t seed,
     d.n_lo = (uint32_t)n;
     d.n_hi = (uint32_t)(n >> 32);
     d.cut = (uint32_t)std::floor(rate * 65536.0 + 0.5);
+    d.last = d.cut == 0 ? 0u : d.cut >= 65536u ? ~0u : (d.cut << 16) - 1u;
     d.scale = d.cut < 65536u ? 65536.0f / (float)(65536u - d.cut) : 0.0f;
     return FASGD_OK;
 }
@@ -157,8 +158,8 @@ int fill_join(const char* call, const fasgd_join_args& u, fasgd::JoinArgs& a) {
     a.layer = u.norm == FASGD_LAYER_NORM;
     a.gate_f32 = u.gate_dtype == FASGD_F32;
     a.eps = u.eps;
-    a.carry = u.carry;
-    a.branch = u.branch;
+    a.carry = u.y != nullptr ? u.carry : 1.f;      // h = x
+    a.branch = u.y != nullptr ? u.branch : 0.f;
     a.inv_cols = 1.0f / (float)u.cols;
     return FASGD_OK;
 }

@@ -20,6 +20,7 @@ struct DropArgs {
     uint32_t round_key0[10], round_key1[10];
     uint32_t client_word, n_lo, n_hi;
     uint32_t cut;       // dropped iff half < cut; 0: nothing is, 65536: everything is
+    uint32_t last;      // (cut << 16) - 1, or 0 for cut = 0 (octet.cuh)
     float scale;        // 65536 / (65536 - cut)
 };
 

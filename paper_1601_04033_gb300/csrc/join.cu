@@ -71,183 +71,158 @@ __global__ void __launch_bounds__(kThreads) join_any_kernel(const __grid_constan
     }
 }
 
-// Rows in octets: TPR threads hold a row, NV octets each, between its statistics,
-// so x and y are read once; blocks stay and take every gridDim-th row, the next
-// STAGES - 1 of them on their way into shared memory.
-template <class T, int TPR, int NV, int STAGES, bool LAYER>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) join_rows_kernel(const __grid_constant__ JoinArgs a) {
-    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR;
-    constexpr int kSlots = 2 * NV * kPieces<T>;      // 16-byte places of a stage, each kBlock wide
-    extern __shared__ uint4 ring[];
-    __shared__ __align__(16) float red[kSubs * 2 * (TPR < 32 ? 1 : TPR / 32)];
+// Rows in octets: TPR threads hold a row between its statistics, an octet each
+// (or as many in each of the C blocks of a cluster), so x and y are read once;
+// blocks stay and take every gridDim-th row, the next STAGES - 1 of them on their
+// way into shared memory.
+template <class T, int TPR, int C, int STAGES, bool LAYER>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? (LAYER ? 3 : 4) : TPR == 512 ? 2 : 1)
+    join_rows_kernel(const __grid_constant__ JoinArgs a) {
+    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR, kP = kPieces<T>;
+    using Sums = RowSums<TPR, 1, C>;
+    extern __shared__ uint4 ring[];                  // [STAGES][x, y][kP][kBlock]
+    __shared__ __align__(16) float red[kSubs * Sums::kPlaces];
     const int sub = threadIdx.x / TPR, lane = threadIdx.x % TPR;
-    const int32_t cols = (int32_t)a.cols;
-    const int64_t step = (int64_t)gridDim.x * kSubs, first = (int64_t)blockIdx.x * kSubs + sub;
+    const int64_t step = (int64_t)(gridDim.x / C) * kSubs, first = (int64_t)(blockIdx.x / C) * kSubs + sub;
     // Where a warp holds several rows, it goes on until the first of them is past the end.
-    const int64_t last = a.rows + (TPR < 32 ? sub % (32 / TPR) : 0);
-    const int shift = (int)((first * a.cols) & 7);
-    Columns c[NV] = {{lane, shift, cols}};
-#pragma unroll
-    for (int v = 1; v < NV; ++v) c[v] = Columns(lane + v * TPR, shift, cols);
-    RowSums<TPR, 1> sums(red, sub);
-    const T* x = static_cast<const T*>(a.x);
-    const T* y = static_cast<const T*>(a.y);
-    const bool has_y = y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
-    const int64_t end_x = (a.rows - 1) * a.ld_x + a.cols, end_y = (a.rows - 1) * a.ld_y + a.cols;
+    const int64_t end = a.rows + (TPR < 32 ? sub % (32 / TPR) : 0);
+    const bool ragged = (a.cols & 7) != 0;
+    const Columns c(lane + (C > 1 ? (int)cluster_rank() * TPR : 0), ragged ? (int)((first * a.cols) & 7) : 0,
+                    (int32_t)a.cols);
+    Sums sums(red, sub);
+    const bool has_y = a.y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
     pdl_wait();
     pdl_trigger();
 
-    const auto fetch = [&](int64_t r, int stage) {
-        if (r < a.rows) {
-            uint4* slot = ring + stage * kSlots * kBlock + threadIdx.x;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-                if (c[v].any()) {
-                    copy_octet<T>(slot + v * kPieces<T> * kBlock, kBlock, x + r * a.ld_x, c[v],
-                                  end_x - r * a.ld_x - c[v].c0);
-                    if (has_y)
-                        copy_octet<T>(slot + (NV + v) * kPieces<T> * kBlock, kBlock, y + r * a.ld_y, c[v],
-                                      end_y - r * a.ld_y - c[v].c0);
-                }
+    const T* x = static_cast<const T*>(a.x) + first * a.ld_x + c.c0;      // of the next row to fetch
+    const T* y = static_cast<const T*>(a.y) + first * a.ld_y + c.c0;
+    int64_t fetched = first, left = (a.rows - first) * a.cols - c.c0;       // (used where rows leave no gaps)
+    const auto fetch = [&](uint4* slot) {
+        if (fetched < a.rows && c.any()) {
+            const bool whole = !ragged || left >= kOctet;
+            copy_octet<T>(slot, kBlock, x, whole, left);
+            if (has_y) copy_octet<T>(slot + kP * kBlock, kBlock, y, whole, left);
         }
         copy_commit();
+        fetched += step;
+        left -= step * a.cols;
+        x += step * a.ld_x;
+        y += step * a.ld_y;
     };
+    constexpr int kStage = 2 * kP * kBlock;
+    uint4* const mine = ring + threadIdx.x;
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) fetch(first + s * step, s);
+    for (int s = 0; s < STAGES - 1; ++s) fetch(mine + s * kStage);
 
-    Oct post[NV], post_bias[NV], gate[NV], pre[NV], pre_bias[NV];
+    // u = yhat (post scale) + post_bias scale.
+    Oct post = load_vector(a.post, c, 1.f), post_bias, gate, pre = load_vector(a.pre, c, 0.f), pre_bias;
     const bool gates = a.groups > 1;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        post[v] = load_vector(a.post, c[v], 1.f);
-        if (LAYER) post_bias[v] = load_vector(a.post_bias, c[v], 0.f);
-        if (!gates) {
-            gate[v] = load_gate<T>(a, 0, c[v]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) gate[v].v[i] = mul2(gate[v].v[i], f2(a.branch));
-        }
-        pre[v] = load_vector(a.pre, c[v], 0.f);
-        if (LAYER) pre_bias[v] = load_vector(a.pre_bias, c[v], 0.f);
+    if (LAYER) {
+        post_bias = load_vector(a.post_bias, c, 0.f);
+        pre_bias = load_vector(a.pre_bias, c, 0.f);
     }
+    if (!gates) gate = load_gate<T>(a, 0, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        post.v[i] = mul2(post.v[i], f2(a.drop.scale));
+        if (LAYER) post_bias.v[i] = mul2(post_bias.v[i], f2(a.drop.scale));
+        if (!gates) gate.v[i] = mul2(gate.v[i], f2(a.branch));
+    }
+    T* hp = static_cast<T*>(a.h) + first * a.ld_h + c.c0;
+    T* zp = static_cast<T*>(a.z) + first * a.ld_z + c.c0;
+
+    const auto centre = [&](Oct& o) {      // the row's mean, taken off; 0 where there is no column
+        const float2 p = add2(add2(o.v[0], o.v[1]), add2(o.v[2], o.v[3]));
+        float s[1] = {p.x + p.y};
+        sums(s);
+        const float mean = s[0] * a.inv_cols;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.v[i] = add2(o.v[i], f2(-mean));
+        mask(o, c);
+        return mean;
+    };
+    const auto inverse = [&](const Oct& o) {
+        const float2 p = fma2(o.v[0], o.v[0], mul2(o.v[1], o.v[1]));
+        const float2 q = fma2(o.v[2], o.v[2], mul2(o.v[3], o.v[3]));
+        float s[1] = {(p.x + q.x) + (p.y + q.y)};
+        sums(s);
+        return rsqrtf(fmaf(s[0], a.inv_cols, a.eps));
+    };
 
     int stage = 0;
-    for (int64_t r = first; r < last; r += step) {
+    for (int64_t r = first; r < end; r += step) {
         const bool live = TPR >= 32 || r < a.rows;
         copy_wait<STAGES - 2>();
-        const uint4* slot = ring + stage * kSlots * kBlock + threadIdx.x;
-        Oct h[NV], t[NV];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            h[v] = take_octet<T>(slot + v * kPieces<T> * kBlock, kBlock, c[v]);
-            if (has_y) t[v] = take_octet<T>(slot + (NV + v) * kPieces<T> * kBlock, kBlock, c[v]);
-        }
-        fetch(r + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+        const uint4* slot = mine + stage * kStage;
+        Oct h = take_octet<T>(slot, kBlock, c), t = {};
+        if (has_y) t = take_octet<T>(slot + kP * kBlock, kBlock, c);
+        fetch(mine + (stage == 0 ? STAGES - 1 : stage - 1) * kStage);
         stage = stage == STAGES - 1 ? 0 : stage + 1;
         float4 st = {0.f, 1.f, 0.f, 1.f};
-        float s[1];
-        const auto centre = [&](Oct (&o)[NV]) {      // the row's mean, taken off; 0 where there is no column
-            float2 p = f2(0.f);
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p = add2(p, o[v].v[i]);
-            s[0] = p.x + p.y;
-            sums(s);
-            const float mean = s[0] * a.inv_cols;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[v].v[i] = add2(o[v].v[i], f2(-mean));
-                if (!c[v].any()) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[v].v[i] = f2(0.f);
-                } else {
-                    mask(o[v], c[v]);
-                }
-            }
-            return mean;
-        };
-        const auto inverse = [&](const Oct (&o)[NV]) {
-            float2 p = f2(0.f);
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p = fma2(o[v].v[i], o[v].v[i], p);
-            s[0] = p.x + p.y;
-            sums(s);
-            return rsqrtf(fmaf(s[0], a.inv_cols, a.eps));
-        };
         if (has_y) {
+            const Philox4 draws = octet_draws(a.drop, c.any(), (r * a.cols + c.c0) >> 3);
+            if (gates) {
+                gate = load_gate<T>(a, (live ? r : 0) / a.group_rows, c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) gate.v[i] = mul2(gate.v[i], f2(a.branch));
+            }
             if (has_post) {
                 if (LAYER) st.x = centre(t);
                 st.y = inverse(t);
             }
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                if (gates) {
-                    gate[v] = load_gate<T>(a, (live ? r : 0) / a.group_rows, c[v]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) gate[v].v[i] = mul2(gate[v].v[i], f2(a.branch));
-                }
-                uint32_t bits = 0xffu;
-                if (a.drop.cut != 0 && c[v].any()) bits = kept_bits(a.drop, (r * a.cols + c[v].c0) >> 3);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float2 u = mul2(mul2(t[v].v[i], f2(st.y)), post[v].v[i]);
-                    if (LAYER) u = add2(u, post_bias[v].v[i]);
-                    if (a.drop.cut != 0) u = select2(bits, i, mul2(u, f2(a.drop.scale)));
-                    h[v].v[i] = fma2(gate[v].v[i], u, mul2(h[v].v[i], f2(a.carry)));
-                }
-                if (live) store_octet(static_cast<T*>(a.h) + r * a.ld_h, c[v], h[v]);
+            for (int i = 0; i < 4; ++i) {
+                float2 u = mul2(t.v[i], f2(st.y));
+                u = LAYER ? fma2(u, post.v[i], post_bias.v[i]) : mul2(u, post.v[i]);
+                u = keep2(draws, i, a.drop.last, u);
+                h.v[i] = fma2(gate.v[i], u, mul2(h.v[i], f2(a.carry)));
             }
+            if (live) store_octet(hp, c, h);
         }
         if (has_pre) {
             if (LAYER) st.z = centre(h);
             st.w = inverse(h);
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    h[v].v[i] = mul2(mul2(h[v].v[i], f2(st.w)), pre[v].v[i]);
-                    if (LAYER) h[v].v[i] = add2(h[v].v[i], pre_bias[v].v[i]);
-                }
-                if (live) store_octet(static_cast<T*>(a.z) + r * a.ld_z, c[v], h[v]);
+            for (int i = 0; i < 4; ++i) {
+                h.v[i] = mul2(h.v[i], f2(st.w));
+                h.v[i] = LAYER ? fma2(h.v[i], pre.v[i], pre_bias.v[i]) : mul2(h.v[i], pre.v[i]);
             }
+            if (live) store_octet(zp, c, h);
         }
-        if (lane == 0 && live && a.stats != nullptr) a.stats[r] = st;
+        if (lane == 0 && live && a.stats != nullptr && (C == 1 || cluster_rank() == 0)) a.stats[r] = st;
+        hp += step * a.ld_h;
+        zp += step * a.ld_z;
     }
 }
 
-template <class T, int TPR, int NV, int STAGES, bool LAYER>
-cudaError_t launch_rows(const JoinArgs& a, int num_sms, int per_sm, cudaStream_t stream) {
-    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR;
-    constexpr size_t kSmem = (size_t)STAGES * 2 * NV * kPieces<T> * kBlock * 16;
+template <class T, int TPR, int C, bool LAYER>
+cudaError_t launch_rows(const JoinArgs& a, int num_sms, cudaStream_t stream) {
+    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR, kStages = 3;
+    const int per_sm = TPR <= 256 ? (LAYER ? 3 : 4) : TPR == 512 ? 2 : 1;
+    constexpr size_t kSmem = (size_t)kStages * 2 * kPieces<T> * kBlock * 16;
     int64_t grid = (a.rows + kSubs - 1) / kSubs;
-    // Past one row each, blocks step by a multiple of 8 rows (octet.cuh).
-    const int64_t cap = (int64_t)num_sms * per_sm / 8 * 8;
+    // Past one row each, they step by a multiple of 8 rows (octet.cuh).
+    const int64_t cap = (int64_t)num_sms * per_sm / C / 8 * 8;
     if (grid > cap) grid = cap;
-    if (kSmem > 40 * 1024) {    // beyond 48 KB with the kernel's own: asked for
-        const cudaError_t st = cudaFuncSetAttribute(join_rows_kernel<T, TPR, NV, STAGES, LAYER>,
-                                                    cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
-        if (st != cudaSuccess) return st;
-    }
-    return launch_pdl(join_rows_kernel<T, TPR, NV, STAGES, LAYER>, (unsigned)grid, kBlock, kSmem, stream, a);
+    return launch_rows_kernel<C>(join_rows_kernel<T, TPR, C, kStages, LAYER>, grid * C, kBlock, kSmem, stream, a);
 }
 
 template <class T, bool LAYER>
 cudaError_t launch_octets(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     const int64_t octets = row_octets(a.cols);
-    if (octets <= 8) return launch_rows<T, 8, 1, 3, LAYER>(a, num_sms, 4, stream);
-    if (octets <= 32) return launch_rows<T, 32, 1, 3, LAYER>(a, num_sms, 4, stream);
-    if (octets <= 64) return launch_rows<T, 64, 1, 3, LAYER>(a, num_sms, 4, stream);
-    if (octets <= 128) return launch_rows<T, 128, 1, 3, LAYER>(a, num_sms, 4, stream);
-    if (octets <= 256) return launch_rows<T, 256, 1, 3, LAYER>(a, num_sms, 4, stream);
-    if (octets <= 512) return launch_rows<T, 512, 1, 3, LAYER>(a, num_sms, 2, stream);
-    return launch_rows<T, 1024, 1, 3, LAYER>(a, num_sms, 1, stream);
+    if (octets <= 8) return launch_rows<T, 8, 1, LAYER>(a, num_sms, stream);
+    if (octets <= 32) return launch_rows<T, 32, 1, LAYER>(a, num_sms, stream);
+    if (octets <= 64) return launch_rows<T, 64, 1, LAYER>(a, num_sms, stream);
+    if (octets <= 128) return launch_rows<T, 128, 1, LAYER>(a, num_sms, stream);
+    if (octets <= 256) return launch_rows<T, 256, 1, LAYER>(a, num_sms, stream);
+    if (octets <= 512) return launch_rows<T, 512, 1, LAYER>(a, num_sms, stream);
+    if (octets <= 1024) return launch_rows<T, 512, 2, LAYER>(a, num_sms, stream);
+    if (octets <= 2048) return launch_rows<T, 512, 4, LAYER>(a, num_sms, stream);
+    return launch_rows<T, 512, 8, LAYER>(a, num_sms, stream);
 }
 
 bool in_octets(const JoinArgs& a) {
-    return row_octets(a.cols) <= 1024 && octet_matrix(a.x, a.ld_x, a.rows, a.cols) &&
+    return row_octets(a.cols) <= 4096 && octet_matrix(a.x, a.ld_x, a.rows, a.cols) &&
            octet_matrix(a.y, a.ld_y, a.rows, a.cols) && octet_matrix(a.h, a.ld_h, a.rows, a.cols) &&
            octet_matrix(a.z, a.ld_z, a.rows, a.cols) &&
            (a.cols % 8 == 0 || a.rows < 2 ||

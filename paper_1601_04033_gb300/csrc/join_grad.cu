@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kThreads) grad_rows_any_kernel(const __grid_co
             const float d = d_stream(a, p, st, m);
             static_cast<T*>(a.dx)[r * a.ld_dx + c] = from_f32<T>(a.y != nullptr ? a.carry * d : d);
             if (a.y == nullptr) continue;
-            const float dt = p.b.keep ? a.branch * gate * d * a.drop.scale : 0.f;
+            const float dt = p.b.keep ? a.branch * gate * a.drop.scale * d : 0.f * d;
             if (a.post == nullptr) {
                 static_cast<T*>(a.dy)[r * a.ld_dy + c] = from_f32<T>(dt);
             } else {
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) grad_rows_any_kernel(const __grid_co
                 const float gate = gate_at<T>(a, group, c);
                 const Point p = point_at<T>(a, r, c, st, gate);
                 const float d = d_stream(a, p, st, m);
-                const float dt = p.b.keep ? a.branch * gate * d * a.drop.scale : 0.f;
+                const float dt = p.b.keep ? a.branch * gate * a.drop.scale * d : 0.f * d;
                 static_cast<T*>(a.dy)[r * a.ld_dy + c] =
                     from_f32<T>(st.y * (dt * a.post[c] - m0 - p.b.yhat * m1));
             }
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads) grad_columns_any_kernel(const __grid
                 const float d = d_stream(a, p, st, a.row_means[r]);
                 g += a.branch * d * p.b.u;
                 if (a.post != nullptr) {
-                    const float dt = p.b.keep ? a.branch * gate * d * a.drop.scale : 0.f;
+                    const float dt = p.b.keep ? a.branch * gate * a.drop.scale * d : 0.f * d;
                     s[0] += dt * p.b.yhat;
                     s[1] += dt;
                 }
@@ -178,46 +178,43 @@ struct Unit {
     }
 };
 
-template <class T, int TPR, int STAGES, bool LAYER>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1) grad_rows_kernel(const __grid_constant__ JoinArgs a) {
+template <class T, int TPR, int C, int STAGES, bool LAYER>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1)
+    grad_rows_kernel(const __grid_constant__ JoinArgs a) {
     constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR, kP = kPieces<T>;
     constexpr int kSums = LAYER ? 8 : 3;
+    using Sums = RowSums<TPR, kSums, C>;
     extern __shared__ uint4 ring[];                  // [STAGES][x, y, dh, dz][kP][kBlock]
-    __shared__ __align__(16) float red[kSubs * 2 * kSums * (TPR < 32 ? 1 : TPR / 32)];
+    __shared__ __align__(16) float red[kSubs * Sums::kPlaces];
     const int sub = threadIdx.x / TPR, lane = threadIdx.x % TPR;
-    const int64_t units = a.groups * a.splits, subs = (int64_t)gridDim.x * kSubs;
-    const int64_t mine = (int64_t)blockIdx.x * kSubs + sub;
+    const int64_t units = a.groups * a.splits, subs = (int64_t)(gridDim.x / C) * kSubs;
+    const int64_t mine = (int64_t)(blockIdx.x / C) * kSubs + sub;
     const bool has_y = a.y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
-    const bool has_dh = a.dh != nullptr, gates = a.groups > 1;
-    RowSums<TPR, kSums> sums(red, sub);
+    const bool has_dh = a.dh != nullptr, gates = a.groups > 1, ragged = (a.cols & 7) != 0;
+    Sums sums(red, sub);
     pdl_wait();
     pdl_trigger();
 
     // All rows that this sub takes begin at the same place in an octet.
-    const int shift = mine < units ? (int)((Unit(a, mine).row * a.cols) & 7) : 0;
-    const Columns c(lane, shift, (int32_t)a.cols);
-    const Oct post = load_vector(a.post, c, 1.f), pre = load_vector(a.pre, c, 0.f);
-    Oct post_bias, gate;
+    const Columns c(lane + (C > 1 ? (int)cluster_rank() * TPR : 0),
+                    ragged && mine < units ? (int)((Unit(a, mine).row * a.cols) & 7) : 0, (int32_t)a.cols);
+    const float scale = a.drop.scale;
+    // As the forward kernel has them, so that h comes out in the same bits.
+    Oct post = load_vector(a.post, c, 1.f), post_bias, gate;
+    const Oct pre = load_vector(a.pre, c, 0.f);
     if (LAYER) post_bias = load_vector(a.post_bias, c, 0.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        post.v[i] = mul2(post.v[i], f2(scale));
+        if (LAYER) post_bias.v[i] = mul2(post_bias.v[i], f2(scale));
+    }
+    // Sums over the rows: those of the norm after the block without `scale`, the
+    // gate's without `branch`.
     Oct d_post = {}, d_post_bias = {}, d_gate = {}, d_pre = {}, d_pre_bias = {};
+    constexpr int kStage = 4 * kP * kBlock;
+    uint4* const own = ring + threadIdx.x;
 
-    const int64_t end = (a.rows - 1) * a.cols + a.cols;     // where cols is no multiple of 8: rows follow without a gap
-    const bool ragged = (a.cols & 7) != 0;
-    const auto fetch = [&](int64_t r, int64_t rows, int stage) {
-        if (r < rows && c.any()) {
-            uint4* slot = ring + stage * 4 * kP * kBlock + threadIdx.x;
-            const int64_t left = ragged ? end - r * a.cols - c.c0 : kOctet;
-            copy_octet<T>(slot, kBlock, static_cast<const T*>(a.x) + r * a.ld_x, c, left);
-            if (has_y) copy_octet<T>(slot + kP * kBlock, kBlock, static_cast<const T*>(a.y) + r * a.ld_y, c, left);
-            if (has_dh)
-                copy_octet<T>(slot + 2 * kP * kBlock, kBlock, static_cast<const T*>(a.dh) + r * a.ld_dh, c, left);
-            if (has_pre)
-                copy_octet<T>(slot + 3 * kP * kBlock, kBlock, static_cast<const T*>(a.dz) + r * a.ld_dz, c, left);
-        }
-        copy_commit();
-    };
-
-    // Subs that share a warp or (units = subs) nothing: a warp's subs go on together.
+    // Where a warp holds several rows, it goes on until the first of them is done.
     const int64_t last_unit = units + (TPR < 32 ? sub % (32 / TPR) : 0);
     for (int64_t unit = mine; unit < last_unit; unit += subs) {
         Unit u(a, unit < units ? unit : 0);
@@ -236,115 +233,119 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1) gra
             for (int i = 0; i < 4; ++i) gate.v[i] = mul2(gate.v[i], f2(a.branch));
         }
         if (gates) d_gate = Oct{};
+
+        int64_t r = u.row, fetched = r, left = (a.rows - r) * a.cols - c.c0;
+        const T* x = static_cast<const T*>(a.x) + r * a.ld_x + c.c0;       // of the next row to fetch
+        const T* y = static_cast<const T*>(a.y) + r * a.ld_y + c.c0;
+        const T* dh = static_cast<const T*>(a.dh) + r * a.ld_dh + c.c0;
+        const T* dz = static_cast<const T*>(a.dz) + r * a.ld_dz + c.c0;
+        const auto fetch = [&](uint4* slot) {
+            if (fetched < u.rows && c.any()) {
+                const bool whole = !ragged || left >= kOctet;
+                copy_octet<T>(slot, kBlock, x, whole, left);
+                if (has_y) copy_octet<T>(slot + kP * kBlock, kBlock, y, whole, left);
+                if (has_dh) copy_octet<T>(slot + 2 * kP * kBlock, kBlock, dh, whole, left);
+                if (has_pre) copy_octet<T>(slot + 3 * kP * kBlock, kBlock, dz, whole, left);
+            }
+            copy_commit();
+            fetched += u.step;
+            left -= u.step * a.cols;
+            x += u.step * a.ld_x;
+            y += u.step * a.ld_y;
+            dh += u.step * a.ld_dh;
+            dz += u.step * a.ld_dz;
+        };
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) fetch(u.row + s * u.step, u.rows, s);
+        for (int s = 0; s < STAGES - 1; ++s) fetch(own + s * kStage);
+        T* dxp = static_cast<T*>(a.dx) + r * a.ld_dx + c.c0;
+        T* dyp = static_cast<T*>(a.dy) + r * a.ld_dy + c.c0;
         int stage = 0;
-        int64_t r = u.row;
         float4 st = r < u.rows ? a.stats[r] : make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int64_t turn = 0; turn < turns; ++turn, r += u.step) {
+        for (int64_t turn = 0; turn < turns; ++turn) {
             const bool live = TPR >= 32 || r < u.rows;
             // The next row's statistics, ahead of its turn.
             const float4 next = r + u.step < u.rows ? a.stats[r + u.step] : make_float4(0.f, 0.f, 0.f, 0.f);
+            const Philox4 draws = octet_draws(a.drop, c.any(), (r * a.cols + c.c0) >> 3);
             copy_wait<STAGES - 2>();
-            const uint4* slot = ring + stage * 4 * kP * kBlock + threadIdx.x;
+            const uint4* slot = own + stage * kStage;
             Oct hhat = take_octet<T>(slot, kBlock, c), yhat = {}, w = {}, q = {}, e, uu;
             if (has_y) yhat = take_octet<T>(slot + kP * kBlock, kBlock, c);
             if (has_dh) w = take_octet<T>(slot + 2 * kP * kBlock, kBlock, c);
             if (has_pre) q = take_octet<T>(slot + 3 * kP * kBlock, kBlock, c);
-            fetch(r + (STAGES - 1) * u.step, u.rows, stage == 0 ? STAGES - 1 : stage - 1);
+            fetch(own + (stage == 0 ? STAGES - 1 : stage - 1) * kStage);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
-            if (TPR < 32 && !live) {       // a row past the end: nothing of it may reach the sums
-                hhat = yhat = w = q = Oct{};
-            }
-            uint32_t bits = 0xffu;
-            if (a.drop.cut != 0 && c.any()) bits = kept_bits(a.drop, ((live ? r : 0) * a.cols + c.c0) >> 3);
-            float2 s2[kSums];
-#pragma unroll
-            for (int k = 0; k < kSums; ++k) s2[k] = f2(0.f);
+            if (TPR < 32 && !live) hhat = yhat = w = q = Oct{};      // a row past the end
+            // u; e = what dH is multiplied by in dt / scale.
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (has_y) {
-                    if (LAYER) yhat.v[i] = add2(yhat.v[i], f2(-st.x));
-                    yhat.v[i] = mul2(yhat.v[i], f2(st.y));
-                    float2 t = mul2(yhat.v[i], post.v[i]);
-                    if (LAYER) t = add2(t, post_bias.v[i]);
-                    float2 factor = gate.v[i];
-                    if (a.drop.cut != 0) {
-                        t = select2(bits, i, mul2(t, f2(a.drop.scale)));
-                        factor = select2(bits, i, mul2(factor, f2(a.drop.scale)));
-                    }
-                    hhat.v[i] = fma2(gate.v[i], t, mul2(hhat.v[i], f2(a.carry)));
-                    uu.v[i] = t;
-                    e.v[i] = factor;
-                }
-                if (has_pre) {
-                    if (LAYER) hhat.v[i] = add2(hhat.v[i], f2(-st.z));
-                    hhat.v[i] = mul2(hhat.v[i], f2(st.w));
-                    d_pre.v[i] = fma2(q.v[i], hhat.v[i], d_pre.v[i]);
-                    if (LAYER) d_pre_bias.v[i] = add2(d_pre_bias.v[i], q.v[i]);
-                    q.v[i] = mul2(q.v[i], pre.v[i]);
-                    s2[0] = fma2(q.v[i], hhat.v[i], s2[0]);
-                    if (LAYER) s2[3] = add2(s2[3], q.v[i]);
-                    w.v[i] = fma2(q.v[i], f2(st.w), w.v[i]);
-                }
-                if (has_post) {
-                    const float2 ep = mul2(e.v[i], post.v[i]), ey = mul2(ep, yhat.v[i]);
-                    s2[1] = fma2(ey, w.v[i], s2[1]);
-                    if (has_pre) s2[2] = fma2(ey, hhat.v[i], s2[2]);
-                    if (LAYER) {
-                        s2[4] = add2(s2[4], ey);
-                        s2[5] = fma2(ep, w.v[i], s2[5]);
-                        if (has_pre) s2[6] = fma2(ep, hhat.v[i], s2[6]);
-                        s2[7] = add2(s2[7], ep);
-                    }
-                }
+                if (LAYER) yhat.v[i] = add2(yhat.v[i], f2(-st.x));
+                yhat.v[i] = mul2(yhat.v[i], f2(st.y));
+                uu.v[i] = LAYER ? fma2(yhat.v[i], post.v[i], post_bias.v[i]) : mul2(yhat.v[i], post.v[i]);
+                uu.v[i] = keep2(draws, i, a.drop.last, uu.v[i]);
+                e.v[i] = keep2(draws, i, a.drop.last, gate.v[i]);
+                hhat.v[i] = fma2(gate.v[i], uu.v[i], mul2(hhat.v[i], f2(a.carry)));
+                hhat.v[i] = LAYER ? mul2(add2(hhat.v[i], f2(-st.z)), f2(st.w)) : mul2(hhat.v[i], f2(st.w));
             }
-            float m1 = 0.f, m0 = 0.f, k1 = 0.f, k0 = 0.f;    // r_h times the means of q hhat and q; the means of q2 yhat and q2
-            if (has_pre || has_post) {
-                float s[kSums];
+            if (!has_pre) hhat = Oct{};        // (h may be infinite)
+            float2 s2[8];
 #pragma unroll
-                for (int k = 0; k < kSums; ++k) s[k] = s2[k].x + s2[k].y;
-                sums(s);
-                if (has_pre) {
-                    m1 = s[0] * a.inv_cols * st.w;
-                    if (LAYER) m0 = s[3] * a.inv_cols * st.w;
-                }
+            for (int k = 0; k < 8; ++k) s2[k] = f2(0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                d_pre.v[i] = fma2(q.v[i], hhat.v[i], d_pre.v[i]);
+                if (LAYER) d_pre_bias.v[i] = add2(d_pre_bias.v[i], q.v[i]);
+                q.v[i] = mul2(q.v[i], pre.v[i]);
+                w.v[i] = fma2(q.v[i], f2(st.w), w.v[i]);
+                const float2 ep = mul2(e.v[i], post.v[i]), ey = mul2(ep, yhat.v[i]);
+                s2[0] = fma2(q.v[i], hhat.v[i], s2[0]);
+                s2[1] = fma2(ey, w.v[i], s2[1]);
+                s2[2] = fma2(ey, hhat.v[i], s2[2]);
                 if (LAYER) {
-                    k1 = (s[1] - m0 * s[4] - m1 * s[2]) * a.inv_cols;
-                    k0 = (s[5] - m0 * s[7] - m1 * s[6]) * a.inv_cols;
-                } else {
-                    k1 = (s[1] - m1 * s[2]) * a.inv_cols;
+                    s2[3] = add2(s2[3], q.v[i]);
+                    s2[4] = add2(s2[4], ey);
+                    s2[5] = fma2(ep, w.v[i], s2[5]);
+                    s2[6] = fma2(ep, hhat.v[i], s2[6]);
+                    s2[7] = add2(s2[7], ep);
                 }
             }
+            float s[kSums];
+#pragma unroll
+            for (int k = 0; k < kSums; ++k) s[k] = s2[k].x + s2[k].y;
+            sums(s);
+            // r_h times the means of q hhat and of q; the means of q2 yhat and of q2.
+            const float m1 = s[0] * a.inv_cols * st.w, m0 = LAYER ? s[3] * a.inv_cols * st.w : 0.f;
+            const float k1 = (LAYER ? s[1] - m0 * s[4] - m1 * s[2] : s[1] - m1 * s[2]) * a.inv_cols;
+            const float k0 = LAYER ? (s[5] - m0 * s[7] - m1 * s[6]) * a.inv_cols : 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float2 d = w.v[i];
-                if (has_pre) {
-                    d = fma2(hhat.v[i], f2(-m1), d);
-                    if (LAYER) d = add2(d, f2(-m0));
+                float2 d = fma2(hhat.v[i], f2(-m1), w.v[i]);
+                if (LAYER) d = add2(d, f2(-m0));
+                hhat.v[i] = mul2(d, f2(a.carry));
+                d_gate.v[i] = fma2(d, uu.v[i], d_gate.v[i]);
+                w.v[i] = mul2(e.v[i], d);
+            }
+            if (has_post) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    d_post.v[i] = fma2(w.v[i], yhat.v[i], d_post.v[i]);
+                    if (LAYER) d_post_bias.v[i] = add2(d_post_bias.v[i], w.v[i]);
+                    w.v[i] = mul2(w.v[i], post.v[i]);
+                    if (LAYER) w.v[i] = add2(w.v[i], f2(-k0));
+                    w.v[i] = mul2(fma2(yhat.v[i], f2(-k1), w.v[i]), f2(st.y));
                 }
-                if (has_y) {
-                    hhat.v[i] = mul2(d, f2(a.carry));
-                    d_gate.v[i] = fma2(d, uu.v[i], d_gate.v[i]);
-                    float2 dt = mul2(e.v[i], d);
-                    if (a.drop.cut != 0) dt = select2(bits, i, dt);
-                    if (has_post) {
-                        d_post.v[i] = fma2(dt, yhat.v[i], d_post.v[i]);
-                        if (LAYER) d_post_bias.v[i] = add2(d_post_bias.v[i], dt);
-                        dt = fma2(dt, post.v[i], mul2(yhat.v[i], f2(-k1)));
-                        if (LAYER) dt = add2(dt, f2(-k0));
-                        dt = mul2(dt, f2(st.y));
-                    }
-                    yhat.v[i] = dt;
-                } else {
-                    hhat.v[i] = d;
-                }
+            }
+            if (!has_post) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w.v[i] = mul2(w.v[i], f2(scale));
             }
             if (live) {
-                store_octet(static_cast<T*>(a.dx) + r * a.ld_dx, c, hhat);
-                if (has_y) store_octet(static_cast<T*>(a.dy) + r * a.ld_dy, c, yhat);
+                store_octet(dxp, c, hhat);
+                if (has_y) store_octet(dyp, c, w);
             }
             st = next;
+            r += u.step;
+            dxp += u.step * a.ld_dx;
+            dyp += u.step * a.ld_dy;
         }
         copy_wait<0>();
         if (gates && a.out_gate != nullptr && unit < units) {
@@ -367,8 +368,8 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1) gra
     for (int k = 0; k < 5; ++k) {
         if (k == 4 ? gates || a.out_gate == nullptr : a.out_param[k] == nullptr) continue;
         Oct& o = k == 0 ? d_post : k == 1 ? d_post_bias : k == 2 ? d_pre : k == 3 ? d_pre_bias : d_gate;
-        float* out = a.params + (blockIdx.x * 5 + k) * a.cols;
-        const float factor = k == 4 ? a.branch : 1.f;
+        float* out = a.params + ((int64_t)(blockIdx.x / C) * 5 + k) * a.cols;
+        const float factor = k == 4 ? a.branch : k < 2 ? a.drop.scale : 1.f;
         if constexpr (kSubs == 1) {
 #pragma unroll
             for (int i = 0; i < kOctet; ++i)
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_cons
 
 int64_t at_most(int64_t n, int64_t cap) { return n < cap ? (n < 1 ? 1 : n) : cap; }
 
-// The threads of a row of the fast kernels (0: the plain form), and its blocks'.
+// The threads of a row of the fast kernels, in blocks of at most 512 (0: the plain form).
 int threads_per_row(const JoinArgs& a) {
     const int64_t octets = row_octets(a.cols);
     const void* p[] = {a.x, a.y, a.dh, a.dz, a.dx, a.dy};
@@ -437,31 +438,31 @@ int threads_per_row(const JoinArgs& a) {
     // A group's rows fall into eight classes where cols is no multiple of 8: short
     // groups would leave more sums than rows.
     if (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64) return 0;
-    for (int t : {8, 32, 64, 128, 256, 512})
+    for (int t : {8, 32, 64, 128, 256, 512, 1024, 2048, 4096})
         if (octets <= t) return t;
     return 0;
 }
 int blocks_per_sm(int threads) { return threads <= 256 ? 2 : 1; }
 
-template <class T, int TPR, bool LAYER>
+template <class T, int TPR, int C, bool LAYER>
 cudaError_t launch_rows(const JoinArgs& a, cudaStream_t stream) {
     constexpr int kBlock = TPR < 256 ? 256 : TPR;
     constexpr int kStages = sizeof(T) == 4 ? 3 : 4;
     constexpr size_t kSmem = (size_t)kStages * 4 * kPieces<T> * kBlock * 16;
-    const cudaError_t st = cudaFuncSetAttribute(grad_rows_kernel<T, TPR, kStages, LAYER>,
-                                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
-    if (st != cudaSuccess) return st;
-    return launch_pdl(grad_rows_kernel<T, TPR, kStages, LAYER>, (unsigned)a.parts, kBlock, kSmem, stream, a);
+    return launch_rows_kernel<C>(grad_rows_kernel<T, TPR, C, kStages, LAYER>, a.parts * C, kBlock, kSmem, stream, a);
 }
 template <class T, bool LAYER>
 cudaError_t launch_octets(const JoinArgs& a, int threads, cudaStream_t stream) {
     switch (threads) {
-        case 8: return launch_rows<T, 8, LAYER>(a, stream);
-        case 32: return launch_rows<T, 32, LAYER>(a, stream);
-        case 64: return launch_rows<T, 64, LAYER>(a, stream);
-        case 128: return launch_rows<T, 128, LAYER>(a, stream);
-        case 256: return launch_rows<T, 256, LAYER>(a, stream);
-        default: return launch_rows<T, 512, LAYER>(a, stream);
+        case 8: return launch_rows<T, 8, 1, LAYER>(a, stream);
+        case 32: return launch_rows<T, 32, 1, LAYER>(a, stream);
+        case 64: return launch_rows<T, 64, 1, LAYER>(a, stream);
+        case 128: return launch_rows<T, 128, 1, LAYER>(a, stream);
+        case 256: return launch_rows<T, 256, 1, LAYER>(a, stream);
+        case 512: return launch_rows<T, 512, 1, LAYER>(a, stream);
+        case 1024: return launch_rows<T, 512, 2, LAYER>(a, stream);
+        case 2048: return launch_rows<T, 512, 4, LAYER>(a, stream);
+        default: return launch_rows<T, 512, 8, LAYER>(a, stream);
     }
 }
 
@@ -495,7 +496,8 @@ JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms) {
     if (a.rows == 0) return p;
     if (const int threads = threads_per_row(a)) {
         const int block_subs = threads < 256 ? 256 / threads : 1;
-        const int64_t most = (int64_t)num_sms * blocks_per_sm(threads) / 8 * 8 * block_subs;
+        const int cluster = threads > 512 ? threads / 512 : 1;
+        const int64_t most = (int64_t)num_sms * blocks_per_sm(threads) / cluster / 8 * 8 * block_subs;
         if (a.groups == 1) {
             p.splits = at_most(a.rows, most);
         } else {

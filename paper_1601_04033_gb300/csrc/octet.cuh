@@ -132,21 +132,16 @@ __device__ __forceinline__ Oct load_gate(const JoinArgs& a, int64_t group, const
     return o;
 }
 
-// Which elements of octet q are kept, a bit each.  A half is kept iff >= cut;
-// shifted to the top of its word that is > (cut << 16) - 1 (cut 65536: never).
-__device__ __forceinline__ uint32_t kept_bits(const DropArgs& d, int64_t q) {
-    const Philox4 r = draw_octet(d, q);
-    const uint32_t last = (d.cut << 16) - 1u;
-    uint32_t bits = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        bits |= (r.x[w] << 16) > last ? 1u << (2 * w) : 0u;
-        bits |= r.x[w] > last ? 2u << (2 * w) : 0u;
-    }
-    return bits;
+// The draws of octet q; where nothing is dropped, words that keep everything.
+__device__ __forceinline__ Philox4 octet_draws(const DropArgs& d, bool any, int64_t q) {
+    Philox4 r = {{~0u, ~0u, ~0u, ~0u}};
+    if (d.cut != 0 && any) r = draw_octet(d, q);
+    return r;
 }
-__device__ __forceinline__ float2 select2(uint32_t bits, int pair, float2 v) {
-    return make_float2((bits >> (2 * pair) & 1) ? v.x : 0.f, (bits >> (2 * pair + 1) & 1) ? v.y : 0.f);
+// Pair i of an octet, 0 where dropped.  A half is kept iff >= cut; shifted to the
+// top of its word that is > last = (cut << 16) - 1 (cut 65536: never; cut 0: last = 0).
+__device__ __forceinline__ float2 keep2(const Philox4& r, int i, uint32_t last, float2 v) {
+    return make_float2((r.x[i] << 16) > last ? v.x : 0.f, r.x[i] > last ? v.y : 0.f);
 }
 
 // ---- loads into shared memory -------------------------------------------------
@@ -162,17 +157,20 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// Octet c of a row that begins at `row`, of which the matrix holds `left` values
-// from the octet's start on (what lies behind its end is not read; zeros).
+// An octet from p on, of which the matrix holds `left` values (what lies behind
+// its end is not read: zeros); whole: it holds all of them.
 template <class T>
-__device__ __forceinline__ void copy_octet(uint4* slot, int stride, const T* row, const Columns& c, int64_t left) {
-    const T* p = row + c.c0;
+__device__ __forceinline__ void copy_octet(uint4* slot, int stride, const T* p, bool whole, int64_t left) {
+    constexpr int kPer = 16 / (int)sizeof(T);
 #pragma unroll
     for (int k = 0; k < kPieces<T>; ++k) {
-        constexpr int kPer = 16 / (int)sizeof(T);
-        const int64_t l = left - k * kPer;
-        const int n = l >= kPer ? kPer : l > 0 ? (int)l : 0;
-        copy_async16(slot + k * stride, n > 0 ? p + k * kPer : p, n * (int)sizeof(T));
+        if (whole) {
+            copy_async16(slot + k * stride, p + k * kPer, 16);
+        } else {
+            const int64_t l = left - k * kPer;
+            const int n = l >= kPer ? kPer : l > 0 ? (int)l : 0;
+            copy_async16(slot + k * stride, n > 0 ? p + k * kPer : p, n * (int)sizeof(T));
+        }
     }
 }
 template <class T>
@@ -184,54 +182,108 @@ __device__ __forceinline__ Oct take_octet(const uint4* slot, int stride, const C
     mask(o, c);
     return o;
 }
+// An octet to p on (the place of its first column, which may not be one).
 template <class T>
-__device__ __forceinline__ void store_octet(T* row, const Columns& c, Oct& o) {
+__device__ __forceinline__ void store_octet(T* p, const Columns& c, Oct& o) {
     if (c.whole()) {
         uint4 raw[kPieces<T>];
         pack<T>(o, raw);
 #pragma unroll
-        for (int k = 0; k < kPieces<T>; ++k) reinterpret_cast<uint4*>(row + c.c0)[k] = raw[k];
+        for (int k = 0; k < kPieces<T>; ++k) reinterpret_cast<uint4*>(p)[k] = raw[k];
         return;
     }
 #pragma unroll
     for (int i = 0; i < kOctet; ++i)
-        if (c.in >> i & 1) row[c.c0 + i] = from_f32<T>(element(o, i));
+        if (c.in >> i & 1) p[i] = from_f32<T>(element(o, i));
 }
 
-// Sums of N values over the TPR threads of a row, every thread ending with them.
-// Rows of more than a warp meet at a barrier of their own; `red` has two places
-// that are used in turn, so that one barrier a sum is enough.
-template <int TPR, int N>
+// Sums of N values over the TPR threads of a row in each of C blocks of a cluster,
+// every thread ending with them.  In a warp the values are halved among the lanes
+// as they are added (four values: 6 shuffles, not 20).  Warps meet at a barrier of
+// their row's own, or the cluster's, having left their sums in its blocks' `red`,
+// which has two places that are used in turn: one barrier for each use is enough.
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void store_to_block(float* p, uint32_t rank, float v) {
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(there)
+                 : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+}
+constexpr int pow2_above(int n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }
+template <int TPR, int N, int C>
 struct RowSums {
-    static constexpr int kWarps = TPR / 32;
-    float* red;          // [2][N][kWarps] of this row's threads
+    static constexpr int kWarps = TPR < 32 ? 1 : TPR / 32 * C;     // that hold a part of a row
+    static constexpr int kN = pow2_above(N), kLanes = 32 / kN;     // lanes that end with one value
+    static constexpr int kPlaces = 2 * kN * kWarps;                // floats of `red` for each row of a block
+    float* red;
     int barrier, turn;
-    __device__ RowSums(float* smem, int sub) : red(smem + sub * 2 * N * kWarps), barrier(1 + sub), turn(0) {}
-    template <int M>
-    __device__ __forceinline__ void operator()(float (&v)[M]) {
-        static_assert(M <= N, "places");
+    __device__ RowSums(float* smem, int sub) : red(smem + sub * kPlaces), barrier(1 + sub), turn(0) {
+        if (C > 1) cluster_barrier();      // every block of the cluster has begun
+    }
+    __device__ __forceinline__ void operator()(float (&in)[N]) {
+        if constexpr (TPR < 32) {
 #pragma unroll
-        for (int i = 0; i < M; ++i) {
+            for (int i = 0; i < N; ++i) {
 #pragma unroll
-            for (int off = (TPR < 32 ? TPR : 32) / 2; off > 0; off >>= 1)
-                v[i] += __shfl_xor_sync(0xffffffffu, v[i], off);
-        }
-        if constexpr (TPR > 32) {
-            float* at = red + turn * N * kWarps;
-            turn ^= 1;
-            const int warp = (threadIdx.x % TPR) >> 5;
-            if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-                for (int i = 0; i < M; ++i) at[i * kWarps + warp] = v[i];
+                for (int off = TPR / 2; off > 0; off >>= 1) in[i] += __shfl_xor_sync(0xffffffffu, in[i], off);
             }
-            asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(TPR) : "memory");
+        } else {
+            const int lane = threadIdx.x & 31;
+            float v[kN];
 #pragma unroll
-            for (int i = 0; i < M; ++i) {
+            for (int i = 0; i < kN; ++i) v[i] = i < N ? in[i] : 0.f;
+            // A lane keeps the half of the values that its bits name.
+#pragma unroll
+            for (int n = kN / 2, off = 16; off > 0; off >>= 1, n >>= 1) {
+                if (n >= 1) {
+                    const bool upper = lane & off;
+#pragma unroll
+                    for (int i = 0; i < (n >= 1 ? n : 1); ++i) {
+                        const float mine = upper ? v[i + n] : v[i], other = upper ? v[i] : v[i + n];
+                        v[i] = mine + __shfl_xor_sync(0xffffffffu, other, off);
+                    }
+                } else {
+                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+                }
+            }
+            if constexpr (kWarps > 1) {
+                float* at = red + turn * kN * kWarps;
+                turn ^= 1;
+                const int warp = (threadIdx.x % TPR) >> 5;
+                if (lane % kLanes == 0) {
+                    float* place = at + lane / kLanes * kWarps + warp;
+                    if constexpr (C == 1) {
+                        *place = v[0];
+                    } else {
+                        place += cluster_rank() * (TPR / 32);
+#pragma unroll
+                        for (int k = 0; k < C; ++k) store_to_block(place, k, v[0]);
+                    }
+                }
+                __syncwarp();
+                if constexpr (C == 1)
+                    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(TPR) : "memory");
+                else
+                    cluster_barrier();
                 float s = 0.f;
+                const float* from = at + lane / kLanes * kWarps;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) s += at[i * kWarps + w];
-                v[i] = s;
+                for (int w = 0; w < kWarps; w += kLanes)
+                    if (kWarps % kLanes == 0 || w + lane % kLanes < kWarps) s += from[w + lane % kLanes];
+#pragma unroll
+                for (int off = kLanes / 2; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+                v[0] = s;
             }
+#pragma unroll
+            for (int i = 0; i < N; ++i) in[i] = kN == 1 ? v[0] : __shfl_sync(0xffffffffu, v[0], i * kLanes);
         }
     }
 };
@@ -242,6 +294,30 @@ inline int64_t row_octets(int64_t cols) {
     for (int r = 0; r < 8; ++r) most = r * cols % 8 > most ? r * cols % 8 : most;
     return (most + cols + 7) / 8;
 }
+// Programmatic dependent launch (pdl.cuh), of clusters where C > 1.
+template <int C, class Args>
+cudaError_t launch_rows_kernel(void (*kernel)(Args), int64_t grid, int block, size_t smem, cudaStream_t stream,
+                               const Args& args) {
+    if (smem > 40 * 1024) {          // with the kernel's own, what passes 48 KB is to be asked for
+        const cudaError_t st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (st != cudaSuccess) return st;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = C;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = C > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args);
+}
+
 // Whether a matrix (an absent one: yes) can be moved in octets.
 inline bool octet_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols) {
     if (p == nullptr) return true;
