@@ -71,48 +71,62 @@ __global__ void __launch_bounds__(kThreads) join_any_kernel(const __grid_constan
     }
 }
 
-// Rows in octets: TPR threads hold a row between its statistics, an octet each
-// (or as many in each of the C blocks of a cluster), so x and y are read once;
-// blocks stay and take every gridDim-th row, the next STAGES - 1 of them on their
-// way into shared memory.
-template <class T, int TPR, int C, int STAGES, bool LAYER>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? (LAYER ? 3 : 4) : TPR == 512 ? 2 : 1)
-    join_rows_kernel(const __grid_constant__ JoinArgs a) {
-    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR, kP = kPieces<T>;
-    using Sums = RowSums<TPR, 1, C>;
-    extern __shared__ uint4 ring[];                  // [STAGES][x, y][kP][kBlock]
-    __shared__ __align__(16) float red[kSubs * Sums::kPlaces];
-    const int sub = threadIdx.x / TPR, lane = threadIdx.x % TPR;
-    const int64_t step = (int64_t)(gridDim.x / C) * kSubs, first = (int64_t)(blockIdx.x / C) * kSubs + sub;
-    // Where a warp holds several rows, it goes on until the first of them is past the end.
-    const int64_t end = a.rows + (TPR < 32 ? sub % (32 / TPR) : 0);
-    const bool ragged = (a.cols & 7) != 0;
-    const Columns c(lane + (C > 1 ? (int)cluster_rank() * TPR : 0), ragged ? (int)((first * a.cols) & 7) : 0,
-                    (int32_t)a.cols);
-    Sums sums(red, sub);
+// Rows in octets (octet.cuh): a row's threads hold it between its statistics, an
+// octet each, so x and y are read once; blocks stay and take NR rows at a time, so
+// that two rows share each barrier, the next STAGES - 1 turns' on their way into
+// shared memory.
+// From one of a block's rows to the next: bytes in each matrix, octets of draws.
+struct RowSteps {
+    int64_t rows, x, y, h, z, octets;
+};
+constexpr int kForwardStages = 3;
+constexpr int kForwardThreads = 512;      // of an SM
+template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP>
+__global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : kForwardThreads / 512)
+    join_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ RowSteps s, int blocks) {
+    constexpr int kP = kPieces<T>, STAGES = kForwardStages;
+    extern __shared__ uint4 ring[];                  // [STAGES][warp][NR][x, y][kP][lane]
+    __shared__ __align__(16) float red[RowSums<TPR, NR>::kPlaces];
+    const RowThreads<TPR> th(blocks);
+    constexpr int kRows = TPR == 8 ? kWarpRows : 1;
+    const int64_t step = s.rows, ahead = (int64_t)(blockIdx.x / blocks) * kRows;
+    const int64_t first = ahead + th.sub;
+    // Rows first, first + step, ...: `rows` of them, in `turns` turns (a warp's as many).
+    const int64_t rows = first < a.rows ? (a.rows - first + step - 1) / step : 0;
+    const int64_t turns = ahead < a.rows ? ((a.rows - ahead + step - 1) / step + NR - 1) / NR : 0;
+    const Columns c(th.octet(), RAGGED ? (int)((first * a.cols) & 7) : 0, (int32_t)a.cols);
+    RowSums<TPR, NR> sums(th, red);
     const bool has_y = a.y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
+    constexpr int kSlots = 2 * NR * kP * kLane;      // of a warp's stage
+    uint4* const mine = ring + (threadIdx.x >> 5) * kSlots + (threadIdx.x & 31);
+    const int stage_size = kSlots * th.warps;
+    if (!c.any())
+        for (int i = 0; i < STAGES; ++i)
+            for (int k = 0; k < kSlots; k += kLane) mine[i * stage_size + k] = make_uint4(0, 0, 0, 0);
     pdl_wait();
     pdl_trigger();
 
     const T* x = static_cast<const T*>(a.x) + first * a.ld_x + c.c0;      // of the next row to fetch
     const T* y = static_cast<const T*>(a.y) + first * a.ld_y + c.c0;
-    int64_t fetched = first, left = (a.rows - first) * a.cols - c.c0;       // (used where rows leave no gaps)
+    int64_t unfetched = c.any() ? rows : 0;
+    // The matrix ends inside this thread's octet of its last row.
+    const bool clipped = RAGGED && c.c0 + kOctet > a.cols && first + (rows - 1) * step == a.rows - 1;
     const auto fetch = [&](uint4* slot) {
-        if (fetched < a.rows && c.any()) {
-            const bool whole = !ragged || left >= kOctet;
-            copy_octet<T>(slot, kBlock, x, whole, left);
-            if (has_y) copy_octet<T>(slot + kP * kBlock, kBlock, y, whole, left);
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            if (unfetched > 0) {
+                const bool whole = !RAGGED || !clipped || unfetched > 1;
+                copy_octet<T>(slot + 2 * j * kP * kLane, x, whole, a.cols - c.c0);
+                if (has_y) copy_octet<T>(slot + (2 * j + 1) * kP * kLane, y, whole, a.cols - c.c0);
+            }
+            --unfetched;
+            x = on(x, s.x);
+            y = on(y, s.y);
         }
         copy_commit();
-        fetched += step;
-        left -= step * a.cols;
-        x += step * a.ld_x;
-        y += step * a.ld_y;
     };
-    constexpr int kStage = 2 * kP * kBlock;
-    uint4* const mine = ring + threadIdx.x;
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) fetch(mine + s * kStage);
+    for (int k = 0; k < STAGES - 1; ++k) fetch(mine + k * stage_size);
 
     // u = yhat (post scale) + post_bias scale.
     Oct post = load_vector(a.post, c, 1.f), post_bias, gate, pre = load_vector(a.pre, c, 0.f), pre_bias;
@@ -124,116 +138,155 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? (LAYER ? 3
     if (!gates) gate = load_gate<T>(a, 0, c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        post.v[i] = mul2(post.v[i], f2(a.drop.scale));
-        if (LAYER) post_bias.v[i] = mul2(post_bias.v[i], f2(a.drop.scale));
+        if (DROP) post.v[i] = mul2(post.v[i], f2(a.drop.scale));
+        if (DROP && LAYER) post_bias.v[i] = mul2(post_bias.v[i], f2(a.drop.scale));
         if (!gates) gate.v[i] = mul2(gate.v[i], f2(a.branch));
     }
     T* hp = static_cast<T*>(a.h) + first * a.ld_h + c.c0;
     T* zp = static_cast<T*>(a.z) + first * a.ld_z + c.c0;
 
-    const auto centre = [&](Oct& o) {      // the row's mean, taken off; 0 where there is no column
-        const float2 p = add2(add2(o.v[0], o.v[1]), add2(o.v[2], o.v[3]));
-        float s[1] = {p.x + p.y};
-        sums(s);
-        const float mean = s[0] * a.inv_cols;
+    const auto centre = [&](Oct (&o)[NR], float (&mean)[NR]) {      // the rows' means, taken off
+        float v[NR];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o.v[i] = add2(o.v[i], f2(-mean));
-        mask(o, c);
-        return mean;
+        for (int j = 0; j < NR; ++j) {
+            const float2 p = add2(add2(o[j].v[0], o[j].v[1]), add2(o[j].v[2], o[j].v[3]));
+            v[j] = p.x + p.y;
+        }
+        sums(v);
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            mean[j] = v[j] * a.inv_cols;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[j].v[i] = add2(o[j].v[i], f2(-mean[j]));
+            mask(o[j], c);           // 0 where there is no column
+        }
     };
-    const auto inverse = [&](const Oct& o) {
-        const float2 p = fma2(o.v[0], o.v[0], mul2(o.v[1], o.v[1]));
-        const float2 q = fma2(o.v[2], o.v[2], mul2(o.v[3], o.v[3]));
-        float s[1] = {(p.x + q.x) + (p.y + q.y)};
-        sums(s);
-        return rsqrtf(fmaf(s[0], a.inv_cols, a.eps));
+    const auto inverse = [&](const Oct (&o)[NR], float (&rstd)[NR]) {
+        float v[NR];
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            const float2 p = fma2(o[j].v[0], o[j].v[0], mul2(o[j].v[1], o[j].v[1]));
+            const float2 q = fma2(o[j].v[2], o[j].v[2], mul2(o[j].v[3], o[j].v[3]));
+            v[j] = (p.x + q.x) + (p.y + q.y);
+        }
+        sums(v);
+#pragma unroll
+        for (int j = 0; j < NR; ++j) rstd[j] = rsqrtf(fmaf(v[j], a.inv_cols, a.eps));
     };
 
+    int64_t q = (first * a.cols + c.c0) >> 3;         // the row's octet of draws
     int stage = 0;
-    for (int64_t r = first; r < end; r += step) {
-        const bool live = TPR >= 32 || r < a.rows;
+    for (int64_t turn = 0, left = rows; turn < turns; ++turn, left -= NR) {
         copy_wait<STAGES - 2>();
-        const uint4* slot = mine + stage * kStage;
-        Oct h = take_octet<T>(slot, kBlock, c), t = {};
-        if (has_y) t = take_octet<T>(slot + kP * kBlock, kBlock, c);
-        fetch(mine + (stage == 0 ? STAGES - 1 : stage - 1) * kStage);
+        const uint4* slot = mine + stage * stage_size;
+        Oct h[NR], t[NR];
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            h[j] = take_octet<T, RAGGED>(slot + 2 * j * kP * kLane, c);
+            if (has_y) t[j] = take_octet<T, RAGGED>(slot + (2 * j + 1) * kP * kLane, c);
+        }
+        fetch(mine + (stage == 0 ? STAGES - 1 : stage - 1) * stage_size);
         stage = stage == STAGES - 1 ? 0 : stage + 1;
-        float4 st = {0.f, 1.f, 0.f, 1.f};
+        float mean_y[NR], rstd_y[NR], mean_h[NR], rstd_h[NR];
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            mean_y[j] = mean_h[j] = 0.f;
+            rstd_y[j] = rstd_h[j] = 1.f;
+        }
         if (has_y) {
-            const Philox4 draws = octet_draws(a.drop, c.any(), (r * a.cols + c.c0) >> 3);
-            if (gates) {
-                gate = load_gate<T>(a, (live ? r : 0) / a.group_rows, c);
+            Philox4 draws[NR];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) gate.v[i] = mul2(gate.v[i], f2(a.branch));
-            }
+            for (int j = 0; j < NR; ++j)
+                if (DROP) draws[j] = draw_octet(a.drop, q + j * s.octets);
             if (has_post) {
-                if (LAYER) st.x = centre(t);
-                st.y = inverse(t);
+                if (LAYER) centre(t, mean_y);
+                inverse(t, rstd_y);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float2 u = mul2(t.v[i], f2(st.y));
-                u = LAYER ? fma2(u, post.v[i], post_bias.v[i]) : mul2(u, post.v[i]);
-                u = keep2(draws, i, a.drop.last, u);
-                h.v[i] = fma2(gate.v[i], u, mul2(h.v[i], f2(a.carry)));
+            for (int j = 0; j < NR; ++j) {
+                if (gates) {
+                    const int64_t r = first + (turn * NR + j) * step;
+                    gate = load_gate<T>(a, (left > j ? r : 0) / a.group_rows, c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) gate.v[i] = mul2(gate.v[i], f2(a.branch));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float2 u = mul2(t[j].v[i], f2(rstd_y[j]));
+                    u = LAYER ? fma2(u, post.v[i], post_bias.v[i]) : mul2(u, post.v[i]);
+                    if (DROP) u = keep2(draws[j], i, a.drop.last, u);
+                    h[j].v[i] = fma2(gate.v[i], u, mul2(h[j].v[i], f2(a.carry)));
+                }
+                if (left > j) store_octet<T, RAGGED>(hp, c, h[j]);
+                hp = on(hp, s.h);
             }
-            if (live) store_octet(hp, c, h);
         }
         if (has_pre) {
-            if (LAYER) st.z = centre(h);
-            st.w = inverse(h);
+            if (LAYER) centre(h, mean_h);
+            inverse(h, rstd_h);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                h.v[i] = mul2(h.v[i], f2(st.w));
-                h.v[i] = LAYER ? fma2(h.v[i], pre.v[i], pre_bias.v[i]) : mul2(h.v[i], pre.v[i]);
+            for (int j = 0; j < NR; ++j) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    h[j].v[i] = mul2(h[j].v[i], f2(rstd_h[j]));
+                    h[j].v[i] = LAYER ? fma2(h[j].v[i], pre.v[i], pre_bias.v[i]) : mul2(h[j].v[i], pre.v[i]);
+                }
+                if (left > j) store_octet<T, RAGGED>(zp, c, h[j]);
+                zp = on(zp, s.z);
             }
-            if (live) store_octet(zp, c, h);
         }
-        if (lane == 0 && live && a.stats != nullptr && (C == 1 || cluster_rank() == 0)) a.stats[r] = st;
-        hp += step * a.ld_h;
-        zp += step * a.ld_z;
+        if (th.octet() == 0 && a.stats != nullptr) {
+#pragma unroll
+            for (int j = 0; j < NR; ++j)
+                if (left > j)
+                    a.stats[first + (turn * NR + j) * step] = make_float4(mean_y[j], rstd_y[j], mean_h[j], rstd_h[j]);
+        }
+        q += NR * s.octets;
     }
 }
 
-template <class T, int TPR, int C, bool LAYER>
-cudaError_t launch_rows(const JoinArgs& a, int num_sms, cudaStream_t stream) {
-    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR, kStages = 3;
-    const int per_sm = TPR <= 256 ? (LAYER ? 3 : 4) : TPR == 512 ? 2 : 1;
-    constexpr size_t kSmem = (size_t)kStages * 2 * kPieces<T> * kBlock * 16;
-    int64_t grid = (a.rows + kSubs - 1) / kSubs;
+constexpr int kForwardRows = 2;      // rows a turn
+template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
+cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
+    constexpr int NR = kForwardRows;
+    const size_t smem = (size_t)kForwardStages * 2 * NR * kPieces<T> * s.threads * 16;
+    int64_t grid = (a.rows + s.rows - 1) / s.rows;
     // Past one row each, they step by a multiple of 8 rows (octet.cuh).
-    const int64_t cap = (int64_t)num_sms * per_sm / C / 8 * 8;
+    const int64_t cap = (int64_t)num_sms * (kForwardThreads / s.threads) / s.blocks / 8 * 8;
     if (grid > cap) grid = cap;
-    return launch_rows_kernel<C>(join_rows_kernel<T, TPR, C, kStages, LAYER>, grid * C, kBlock, kSmem, stream, a);
+    const int64_t rows = grid * s.rows, bytes = rows * (int64_t)sizeof(T);
+    const RowSteps steps = {rows, bytes * a.ld_x, bytes * a.ld_y, bytes * a.ld_h, bytes * a.ld_z, rows * a.cols / 8};
+    return launch_rows_kernel(join_rows_kernel<T, TPR, NR, LAYER, RAGGED, DROP>, grid * s.blocks, s.threads, smem,
+                              s.blocks, stream, a, steps, s.blocks);
 }
-
+template <class T, bool LAYER, bool RAGGED, bool DROP>
+cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
+    if (s.rows > 1) return launch_rows<T, 8, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
+    return launch_rows<T, 0, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
+}
 template <class T, bool LAYER>
-cudaError_t launch_octets(const JoinArgs& a, int num_sms, cudaStream_t stream) {
-    const int64_t octets = row_octets(a.cols);
-    if (octets <= 8) return launch_rows<T, 8, 1, LAYER>(a, num_sms, stream);
-    if (octets <= 32) return launch_rows<T, 32, 1, LAYER>(a, num_sms, stream);
-    if (octets <= 64) return launch_rows<T, 64, 1, LAYER>(a, num_sms, stream);
-    if (octets <= 128) return launch_rows<T, 128, 1, LAYER>(a, num_sms, stream);
-    if (octets <= 256) return launch_rows<T, 256, 1, LAYER>(a, num_sms, stream);
-    if (octets <= 512) return launch_rows<T, 512, 1, LAYER>(a, num_sms, stream);
-    if (octets <= 1024) return launch_rows<T, 512, 2, LAYER>(a, num_sms, stream);
-    if (octets <= 2048) return launch_rows<T, 512, 4, LAYER>(a, num_sms, stream);
-    return launch_rows<T, 512, 8, LAYER>(a, num_sms, stream);
+cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
+    const bool drop = a.drop.cut != 0;
+    if (a.cols % 8 == 0)
+        return drop ? launch_octets<T, LAYER, false, true>(a, s, num_sms, stream)
+                    : launch_octets<T, LAYER, false, false>(a, s, num_sms, stream);
+    return drop ? launch_octets<T, LAYER, true, true>(a, s, num_sms, stream)
+                : launch_octets<T, LAYER, true, false>(a, s, num_sms, stream);
 }
 
 bool in_octets(const JoinArgs& a) {
-    return row_octets(a.cols) <= 4096 && octet_matrix(a.x, a.ld_x, a.rows, a.cols) &&
-           octet_matrix(a.y, a.ld_y, a.rows, a.cols) && octet_matrix(a.h, a.ld_h, a.rows, a.cols) &&
-           octet_matrix(a.z, a.ld_z, a.rows, a.cols) &&
-           (a.cols % 8 == 0 || a.rows < 2 ||
-            (a.ld_x == a.cols && (a.y == nullptr || a.ld_y == a.cols) && (a.h == nullptr || a.ld_h == a.cols) &&
-             (a.z == nullptr || a.ld_z == a.cols)));
+    const void* p[] = {a.x, a.y, a.h, a.z};
+    const int64_t ld[] = {a.ld_x, a.ld_y, a.ld_h, a.ld_z};
+    for (int i = 0; i < 4; ++i)
+        if (!octet_matrix(p[i], ld[i], a.rows, a.cols)) return false;
+    return true;
 }
 
 template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
-    if (in_octets(a))
-        return a.layer ? launch_octets<T, true>(a, num_sms, stream) : launch_octets<T, false>(a, num_sms, stream);
+    const RowShape s(row_octets(a.cols), 512);
+    if (s.fits() && in_octets(a))
+        return a.layer ? launch_octets<T, true>(a, s, num_sms, stream) : launch_octets<T, false>(a, s, num_sms, stream);
     const int64_t grid = a.rows < (int64_t)num_sms * 8 ? a.rows : (int64_t)num_sms * 8;
     return launch_pdl(join_any_kernel<T>, (unsigned)grid, kThreads, 0, stream, a);
 }

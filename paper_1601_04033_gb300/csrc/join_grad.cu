@@ -178,26 +178,41 @@ struct Unit {
     }
 };
 
-template <class T, int TPR, int C, int STAGES, bool LAYER>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1)
-    grad_rows_kernel(const __grid_constant__ JoinArgs a) {
-    constexpr int kBlock = TPR < 256 ? 256 : TPR, kSubs = kBlock / TPR, kP = kPieces<T>;
-    constexpr int kSums = LAYER ? 8 : 3;
-    using Sums = RowSums<TPR, kSums, C>;
-    extern __shared__ uint4 ring[];                  // [STAGES][x, y, dh, dz][kP][kBlock]
-    __shared__ __align__(16) float red[kSubs * Sums::kPlaces];
-    const int sub = threadIdx.x / TPR, lane = threadIdx.x % TPR;
-    const int64_t units = a.groups * a.splits, subs = (int64_t)(gridDim.x / C) * kSubs;
-    const int64_t mine = (int64_t)(blockIdx.x / C) * kSubs + sub;
+// From one of a unit's rows to the next: bytes in each matrix, octets of draws.
+struct GradSteps {
+    int64_t x, y, dh, dz, dx, dy, stats, octets;
+};
+template <class T>
+constexpr int kGradStages = sizeof(T) == 4 ? 3 : 4;
+template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
+__global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
+    grad_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ GradSteps s, int blocks) {
+    constexpr int kP = kPieces<T>, kSums = LAYER ? 8 : 3, STAGES = kGradStages<T>;
+    extern __shared__ uint4 ring[];                  // [STAGES][warp][x, y, dh, dz][kP][lane], then [STAGES][warp][row of a warp]
+    __shared__ __align__(16) float red[RowSums<TPR, kSums>::kPlaces];
+    const RowThreads<TPR> th(blocks);
+    constexpr int kRows = TPR == 8 ? kWarpRows : 1;
+    const int width = blockDim.x;
+    const int64_t units = a.groups * a.splits, subs = (int64_t)(gridDim.x / blocks) * kRows;
+    const int64_t ahead = (int64_t)(blockIdx.x / blocks) * kRows, mine = ahead + th.sub;
     const bool has_y = a.y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
-    const bool has_dh = a.dh != nullptr, gates = a.groups > 1, ragged = (a.cols & 7) != 0;
-    Sums sums(red, sub);
+    const bool has_dh = a.dh != nullptr, gates = a.groups > 1;
+    RowSums<TPR, kSums> sums(th, red);
+    // All rows that this sub takes begin at the same place in an octet.
+    const Columns c(th.octet(), RAGGED && mine < units ? (int)((Unit(a, mine).row * a.cols) & 7) : 0,
+                    (int32_t)a.cols);
+    constexpr int kSlots = 4 * kP * kLane;           // of a warp's stage
+    uint4* const own = ring + (threadIdx.x >> 5) * kSlots + (threadIdx.x & 31);
+    const int stage_size = kSlots * th.warps;
+    // The rows' statistics, copied ahead by one lane of theirs in each warp.
+    uint4* const own_stats = ring + STAGES * stage_size + (threadIdx.x >> 5) * kWarpRows + (TPR == 8 ? th.sub : 0);
+    const bool asks = (threadIdx.x & (TPR == 8 ? 7 : 31)) == 0;
+    if (!c.any())
+        for (int i = 0; i < STAGES; ++i)
+            for (int k = 0; k < kSlots; k += kLane) own[i * stage_size + k] = make_uint4(0, 0, 0, 0);
     pdl_wait();
     pdl_trigger();
 
-    // All rows that this sub takes begin at the same place in an octet.
-    const Columns c(lane + (C > 1 ? (int)cluster_rank() * TPR : 0),
-                    ragged && mine < units ? (int)((Unit(a, mine).row * a.cols) & 7) : 0, (int32_t)a.cols);
     const float scale = a.drop.scale;
     // As the forward kernel has them, so that h comes out in the same bits.
     Oct post = load_vector(a.post, c, 1.f), post_bias, gate;
@@ -205,24 +220,23 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1)
     if (LAYER) post_bias = load_vector(a.post_bias, c, 0.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        post.v[i] = mul2(post.v[i], f2(scale));
-        if (LAYER) post_bias.v[i] = mul2(post_bias.v[i], f2(scale));
+        if (DROP) post.v[i] = mul2(post.v[i], f2(scale));
+        if (DROP && LAYER) post_bias.v[i] = mul2(post_bias.v[i], f2(scale));
     }
     // Sums over the rows: those of the norm after the block without `scale`, the
     // gate's without `branch`.
     Oct d_post = {}, d_post_bias = {}, d_gate = {}, d_pre = {}, d_pre_bias = {};
-    constexpr int kStage = 4 * kP * kBlock;
-    uint4* const own = ring + threadIdx.x;
 
     // Where a warp holds several rows, it goes on until the first of them is done.
-    const int64_t last_unit = units + (TPR < 32 ? sub % (32 / TPR) : 0);
-    for (int64_t unit = mine; unit < last_unit; unit += subs) {
+    for (int64_t ahead_unit = ahead; ahead_unit < units; ahead_unit += subs) {
+        const int64_t unit = ahead_unit + th.sub;
         Unit u(a, unit < units ? unit : 0);
         if (unit >= units) u.rows = 0;
         int64_t turns = u.row < u.rows ? (u.rows - u.row + u.step - 1) / u.step : 0;
-        if constexpr (TPR < 32) {
+        const int64_t rows = turns;
+        if constexpr (TPR == 8) {
 #pragma unroll
-            for (int off = 16; off >= TPR; off >>= 1) {
+            for (int off = 16; off >= 8; off >>= 1) {
                 const int64_t other = __shfl_xor_sync(0xffffffffu, turns, off);
                 turns = other > turns ? other : turns;
             }
@@ -234,55 +248,68 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1)
         }
         if (gates) d_gate = Oct{};
 
-        int64_t r = u.row, fetched = r, left = (a.rows - r) * a.cols - c.c0;
-        const T* x = static_cast<const T*>(a.x) + r * a.ld_x + c.c0;       // of the next row to fetch
-        const T* y = static_cast<const T*>(a.y) + r * a.ld_y + c.c0;
-        const T* dh = static_cast<const T*>(a.dh) + r * a.ld_dh + c.c0;
-        const T* dz = static_cast<const T*>(a.dz) + r * a.ld_dz + c.c0;
-        const auto fetch = [&](uint4* slot) {
-            if (fetched < u.rows && c.any()) {
-                const bool whole = !ragged || left >= kOctet;
-                copy_octet<T>(slot, kBlock, x, whole, left);
-                if (has_y) copy_octet<T>(slot + kP * kBlock, kBlock, y, whole, left);
-                if (has_dh) copy_octet<T>(slot + 2 * kP * kBlock, kBlock, dh, whole, left);
-                if (has_pre) copy_octet<T>(slot + 3 * kP * kBlock, kBlock, dz, whole, left);
+        const int64_t r0 = u.row;
+        const T* x = static_cast<const T*>(a.x) + r0 * a.ld_x + c.c0;       // of the next row to fetch
+        const T* y = static_cast<const T*>(a.y) + r0 * a.ld_y + c.c0;
+        const T* dh = static_cast<const T*>(a.dh) + r0 * a.ld_dh + c.c0;
+        const T* dz = static_cast<const T*>(a.dz) + r0 * a.ld_dz + c.c0;
+        const float4* stats = a.stats + r0;
+        int64_t unfetched = rows;
+        // The matrix ends inside this thread's octet of its last row.
+        const bool clipped = RAGGED && c.c0 + kOctet > a.cols && r0 + (rows - 1) * u.step == a.rows - 1;
+        const auto fetch = [&](int stage) {
+            uint4* slot = own + stage * stage_size;
+            if (unfetched > 0 && asks) copy_async16(own_stats + stage * kWarpRows * th.warps, stats, 16);
+            if (unfetched > 0 && c.any()) {
+                const bool whole = !RAGGED || !clipped || unfetched > 1;
+                const int64_t left = a.cols - c.c0;
+                copy_octet<T>(slot, x, whole, left);
+                if (has_y) copy_octet<T>(slot + kP * kLane, y, whole, left);
+                if (has_dh) copy_octet<T>(slot + 2 * kP * kLane, dh, whole, left);
+                if (has_pre) copy_octet<T>(slot + 3 * kP * kLane, dz, whole, left);
             }
             copy_commit();
-            fetched += u.step;
-            left -= u.step * a.cols;
-            x += u.step * a.ld_x;
-            y += u.step * a.ld_y;
-            dh += u.step * a.ld_dh;
-            dz += u.step * a.ld_dz;
+            --unfetched;
+            x = on(x, s.x);
+            y = on(y, s.y);
+            dh = on(dh, s.dh);
+            dz = on(dz, s.dz);
+            stats = on(stats, s.stats);
         };
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) fetch(own + s * kStage);
-        T* dxp = static_cast<T*>(a.dx) + r * a.ld_dx + c.c0;
-        T* dyp = static_cast<T*>(a.dy) + r * a.ld_dy + c.c0;
+        for (int k = 0; k < STAGES - 1; ++k) fetch(k);
+        T* dxp = static_cast<T*>(a.dx) + r0 * a.ld_dx + c.c0;
+        T* dyp = static_cast<T*>(a.dy) + r0 * a.ld_dy + c.c0;
+        int64_t oct = (r0 * a.cols + c.c0) >> 3;         // the row's octet of draws
         int stage = 0;
-        float4 st = r < u.rows ? a.stats[r] : make_float4(0.f, 0.f, 0.f, 0.f);
         for (int64_t turn = 0; turn < turns; ++turn) {
-            const bool live = TPR >= 32 || r < u.rows;
-            // The next row's statistics, ahead of its turn.
-            const float4 next = r + u.step < u.rows ? a.stats[r + u.step] : make_float4(0.f, 0.f, 0.f, 0.f);
-            const Philox4 draws = octet_draws(a.drop, c.any(), (r * a.cols + c.c0) >> 3);
+            const bool live = TPR != 8 || turn < rows;
+            Philox4 draws;
+            if (DROP) draws = draw_octet(a.drop, oct);
+            oct += s.octets;
             copy_wait<STAGES - 2>();
-            const uint4* slot = own + stage * kStage;
-            Oct hhat = take_octet<T>(slot, kBlock, c), yhat = {}, w = {}, q = {}, e, uu;
-            if (has_y) yhat = take_octet<T>(slot + kP * kBlock, kBlock, c);
-            if (has_dh) w = take_octet<T>(slot + 2 * kP * kBlock, kBlock, c);
-            if (has_pre) q = take_octet<T>(slot + 3 * kP * kBlock, kBlock, c);
-            fetch(own + (stage == 0 ? STAGES - 1 : stage - 1) * kStage);
+            __syncwarp();
+            const float4 st = *reinterpret_cast<const float4*>(own_stats + stage * kWarpRows * th.warps);
+            const uint4* slot = own + stage * stage_size;
+            Oct hhat = take_octet<T, RAGGED>(slot, c), yhat = {}, w = {}, q = {}, e, uu;
+            if (has_y) yhat = take_octet<T, RAGGED>(slot + kP * kLane, c);
+            if (has_dh) w = take_octet<T, RAGGED>(slot + 2 * kP * kLane, c);
+            if (has_pre) q = take_octet<T, RAGGED>(slot + 3 * kP * kLane, c);
+            __syncwarp();     // every lane has read the statistics that the next copy replaces
+            fetch(stage == 0 ? STAGES - 1 : stage - 1);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
-            if (TPR < 32 && !live) hhat = yhat = w = q = Oct{};      // a row past the end
+            if (!live) hhat = yhat = w = q = Oct{};      // a row past the end
             // u; e = what dH is multiplied by in dt / scale.
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (LAYER) yhat.v[i] = add2(yhat.v[i], f2(-st.x));
                 yhat.v[i] = mul2(yhat.v[i], f2(st.y));
                 uu.v[i] = LAYER ? fma2(yhat.v[i], post.v[i], post_bias.v[i]) : mul2(yhat.v[i], post.v[i]);
-                uu.v[i] = keep2(draws, i, a.drop.last, uu.v[i]);
-                e.v[i] = keep2(draws, i, a.drop.last, gate.v[i]);
+                e.v[i] = gate.v[i];
+                if (DROP) {
+                    uu.v[i] = keep2(draws, i, a.drop.last, uu.v[i]);
+                    e.v[i] = keep2(draws, i, a.drop.last, e.v[i]);
+                }
                 hhat.v[i] = fma2(gate.v[i], uu.v[i], mul2(hhat.v[i], f2(a.carry)));
                 hhat.v[i] = LAYER ? mul2(add2(hhat.v[i], f2(-st.z)), f2(st.w)) : mul2(hhat.v[i], f2(st.w));
             }
@@ -308,14 +335,14 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1)
                     s2[7] = add2(s2[7], ep);
                 }
             }
-            float s[kSums];
+            float v[kSums];
 #pragma unroll
-            for (int k = 0; k < kSums; ++k) s[k] = s2[k].x + s2[k].y;
-            sums(s);
+            for (int k = 0; k < kSums; ++k) v[k] = s2[k].x + s2[k].y;
+            sums(v);
             // r_h times the means of q hhat and of q; the means of q2 yhat and of q2.
-            const float m1 = s[0] * a.inv_cols * st.w, m0 = LAYER ? s[3] * a.inv_cols * st.w : 0.f;
-            const float k1 = (LAYER ? s[1] - m0 * s[4] - m1 * s[2] : s[1] - m1 * s[2]) * a.inv_cols;
-            const float k0 = LAYER ? (s[5] - m0 * s[7] - m1 * s[6]) * a.inv_cols : 0.f;
+            const float m1 = v[0] * a.inv_cols * st.w, m0 = LAYER ? v[3] * a.inv_cols * st.w : 0.f;
+            const float k1 = (LAYER ? v[1] - m0 * v[4] - m1 * v[2] : v[1] - m1 * v[2]) * a.inv_cols;
+            const float k0 = LAYER ? (v[5] - m0 * v[7] - m1 * v[6]) * a.inv_cols : 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float2 d = fma2(hhat.v[i], f2(-m1), w.v[i]);
@@ -334,18 +361,16 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1)
                     w.v[i] = mul2(fma2(yhat.v[i], f2(-k1), w.v[i]), f2(st.y));
                 }
             }
-            if (!has_post) {
+            if (DROP && !has_post) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w.v[i] = mul2(w.v[i], f2(scale));
             }
             if (live) {
-                store_octet(dxp, c, hhat);
-                if (has_y) store_octet(dyp, c, w);
+                store_octet<T, RAGGED>(dxp, c, hhat);
+                if (has_y) store_octet<T, RAGGED>(dyp, c, w);
             }
-            st = next;
-            r += u.step;
-            dxp += u.step * a.ld_dx;
-            dyp += u.step * a.ld_dy;
+            dxp = on(dxp, s.dx);
+            dyp = on(dyp, s.dy);
         }
         copy_wait<0>();
         if (gates && a.out_gate != nullptr && unit < units) {
@@ -362,30 +387,30 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 ? 2 : 1)
         }
     }
 
-    // The block's sums: its subs' in turn, joined in shared memory.
+    // The block's sums: four rows' are joined in shared memory, in turn.
     float* joint = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int k = 0; k < 5; ++k) {
         if (k == 4 ? gates || a.out_gate == nullptr : a.out_param[k] == nullptr) continue;
         Oct& o = k == 0 ? d_post : k == 1 ? d_post_bias : k == 2 ? d_pre : k == 3 ? d_pre_bias : d_gate;
-        float* out = a.params + ((int64_t)(blockIdx.x / C) * 5 + k) * a.cols;
+        float* out = a.params + ((int64_t)(blockIdx.x / blocks) * 5 + k) * a.cols;
         const float factor = k == 4 ? a.branch : k < 2 ? a.drop.scale : 1.f;
-        if constexpr (kSubs == 1) {
+        if constexpr (TPR == 0) {
 #pragma unroll
             for (int i = 0; i < kOctet; ++i)
                 if (c.in >> i & 1) out[c.c0 + i] = factor * element(o, i);
         } else {
-            for (int s = 0; s < kSubs; ++s) {
-                __syncthreads();
-                if (s == sub && mine < units) {
+            for (int row = 0; row < kRows; ++row) {
+                __syncwarp();
+                if (row == th.sub && mine < units) {
 #pragma unroll
                     for (int i = 0; i < kOctet; ++i)
                         if (c.in >> i & 1)
-                            joint[c.c0 + i] = s == 0 ? element(o, i) : joint[c.c0 + i] + element(o, i);
+                            joint[c.c0 + i] = row == 0 ? element(o, i) : joint[c.c0 + i] + element(o, i);
                 }
             }
-            __syncthreads();
-            for (int i = threadIdx.x; i < (int)a.cols; i += kBlock) out[i] = factor * joint[i];
+            __syncwarp();
+            for (int i = threadIdx.x; i < (int)a.cols; i += width) out[i] = factor * joint[i];
         }
     }
 }
@@ -426,51 +451,46 @@ __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_cons
 
 int64_t at_most(int64_t n, int64_t cap) { return n < cap ? (n < 1 ? 1 : n) : cap; }
 
-// The threads of a row of the fast kernels, in blocks of at most 512 (0: the plain form).
-int threads_per_row(const JoinArgs& a) {
-    const int64_t octets = row_octets(a.cols);
+constexpr int kGradThreads = 512;       // of a row in one block, and in an SM (128 registers each)
+bool in_octets(const JoinArgs& a) {
     const void* p[] = {a.x, a.y, a.dh, a.dz, a.dx, a.dy};
     const int64_t ld[] = {a.ld_x, a.ld_y, a.ld_dh, a.ld_dz, a.ld_dx, a.ld_dy};
-    for (int i = 0; i < 6; ++i) {
-        if (!octet_matrix(p[i], ld[i], a.rows, a.cols)) return 0;
-        if (a.cols % 8 != 0 && a.rows > 1 && p[i] != nullptr && ld[i] != a.cols) return 0;
-    }
+    for (int i = 0; i < 6; ++i)
+        if (!octet_matrix(p[i], ld[i], a.rows, a.cols)) return false;
     // A group's rows fall into eight classes where cols is no multiple of 8: short
     // groups would leave more sums than rows.
-    if (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64) return 0;
-    for (int t : {8, 32, 64, 128, 256, 512, 1024, 2048, 4096})
-        if (octets <= t) return t;
-    return 0;
+    if (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64) return false;
+    return RowShape(row_octets(a.cols), kGradThreads).fits();
 }
-int blocks_per_sm(int threads) { return threads <= 256 ? 2 : 1; }
 
-template <class T, int TPR, int C, bool LAYER>
-cudaError_t launch_rows(const JoinArgs& a, cudaStream_t stream) {
-    constexpr int kBlock = TPR < 256 ? 256 : TPR;
-    constexpr int kStages = sizeof(T) == 4 ? 3 : 4;
-    constexpr size_t kSmem = (size_t)kStages * 4 * kPieces<T> * kBlock * 16;
-    return launch_rows_kernel<C>(grad_rows_kernel<T, TPR, C, kStages, LAYER>, a.parts * C, kBlock, kSmem, stream, a);
+template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
+cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {
+    const size_t smem = (size_t)kGradStages<T> * (4 * kPieces<T> * s.threads + s.threads / 32 * kWarpRows) * 16;
+    const int64_t step = a.splits, bytes = step * (int64_t)sizeof(T);
+    const GradSteps steps = {bytes * a.ld_x,  bytes * a.ld_y,  bytes * a.ld_dh, bytes * a.ld_dz,
+                             bytes * a.ld_dx, bytes * a.ld_dy, step * 16,       step * a.cols / 8};
+    return launch_rows_kernel(grad_rows_kernel<T, TPR, LAYER, RAGGED, DROP>, a.parts * s.blocks, s.threads, smem,
+                              s.blocks, stream, a, steps, s.blocks);
+}
+template <class T, bool LAYER, bool RAGGED, bool DROP>
+cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {
+    if (s.rows > 1) return launch_rows<T, 8, LAYER, RAGGED, DROP>(a, s, stream);
+    return launch_rows<T, 0, LAYER, RAGGED, DROP>(a, s, stream);
 }
 template <class T, bool LAYER>
-cudaError_t launch_octets(const JoinArgs& a, int threads, cudaStream_t stream) {
-    switch (threads) {
-        case 8: return launch_rows<T, 8, 1, LAYER>(a, stream);
-        case 32: return launch_rows<T, 32, 1, LAYER>(a, stream);
-        case 64: return launch_rows<T, 64, 1, LAYER>(a, stream);
-        case 128: return launch_rows<T, 128, 1, LAYER>(a, stream);
-        case 256: return launch_rows<T, 256, 1, LAYER>(a, stream);
-        case 512: return launch_rows<T, 512, 1, LAYER>(a, stream);
-        case 1024: return launch_rows<T, 512, 2, LAYER>(a, stream);
-        case 2048: return launch_rows<T, 512, 4, LAYER>(a, stream);
-        default: return launch_rows<T, 512, 8, LAYER>(a, stream);
-    }
+cudaError_t launch_octets(const JoinArgs& a, cudaStream_t stream) {
+    const RowShape s(row_octets(a.cols), kGradThreads);
+    const bool drop = a.drop.cut != 0;
+    if (a.cols % 8 == 0)
+        return drop ? launch_octets<T, LAYER, false, true>(a, s, stream) : launch_octets<T, LAYER, false, false>(a, s, stream);
+    return drop ? launch_octets<T, LAYER, true, true>(a, s, stream) : launch_octets<T, LAYER, true, false>(a, s, stream);
 }
 
 template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     cudaError_t st = cudaSuccess;
-    if (const int threads = a.rows > 0 ? threads_per_row(a) : 0) {
-        st = a.layer ? launch_octets<T, true>(a, threads, stream) : launch_octets<T, false>(a, threads, stream);
+    if (a.rows > 0 && in_octets(a)) {
+        st = a.layer ? launch_octets<T, true>(a, stream) : launch_octets<T, false>(a, stream);
     } else if (a.rows > 0) {
         st = launch_pdl(grad_rows_any_kernel<T>, (unsigned)at_most(a.rows, (int64_t)num_sms * 8), kThreads, 0,
                         stream, a);
@@ -494,10 +514,10 @@ JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms) {
     JoinPlan p;
     p.parts = p.splits = p.row_means = 0;
     if (a.rows == 0) return p;
-    if (const int threads = threads_per_row(a)) {
-        const int block_subs = threads < 256 ? 256 / threads : 1;
-        const int cluster = threads > 512 ? threads / 512 : 1;
-        const int64_t most = (int64_t)num_sms * blocks_per_sm(threads) / cluster / 8 * 8 * block_subs;
+    if (in_octets(a)) {
+        const RowShape s(row_octets(a.cols), kGradThreads);
+        const int64_t block_subs = s.rows, per_sm = kGradThreads / s.threads;
+        const int64_t most = (int64_t)num_sms * per_sm / s.blocks / 8 * 8 * block_subs;
         if (a.groups == 1) {
             p.splits = at_most(a.rows, most);
         } else {

@@ -132,21 +132,17 @@ __device__ __forceinline__ Oct load_gate(const JoinArgs& a, int64_t group, const
     return o;
 }
 
-// The draws of octet q; where nothing is dropped, words that keep everything.
-__device__ __forceinline__ Philox4 octet_draws(const DropArgs& d, bool any, int64_t q) {
-    Philox4 r = {{~0u, ~0u, ~0u, ~0u}};
-    if (d.cut != 0 && any) r = draw_octet(d, q);
-    return r;
-}
 // Pair i of an octet, 0 where dropped.  A half is kept iff >= cut; shifted to the
-// top of its word that is > last = (cut << 16) - 1 (cut 65536: never; cut 0: last = 0).
+// top of its word that is > last = (cut << 16) - 1 (cut 65536: never).
 __device__ __forceinline__ float2 keep2(const Philox4& r, int i, uint32_t last, float2 v) {
     return make_float2((r.x[i] << 16) > last ? v.x : 0.f, r.x[i] > last ? v.y : 0.f);
 }
 
 // ---- loads into shared memory -------------------------------------------------
 // Each thread copies its own octets ahead, into places that it alone reads, so
-// the pipeline needs no barrier and no wait that could run out.
+// the pipeline needs no barrier and no wait that could run out.  A warp's places
+// lie together: 16 bytes of each of its lanes, kLane apart, then the next 16.
+constexpr int kLane = 32;
 __device__ __forceinline__ void copy_async16(void* smem, const void* global, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)),
                  "l"(global), "r"(bytes)
@@ -160,48 +156,54 @@ __device__ __forceinline__ void copy_wait() {
 // An octet from p on, of which the matrix holds `left` values (what lies behind
 // its end is not read: zeros); whole: it holds all of them.
 template <class T>
-__device__ __forceinline__ void copy_octet(uint4* slot, int stride, const T* p, bool whole, int64_t left) {
+__device__ __forceinline__ void copy_octet(uint4* slot, const T* p, bool whole, int64_t left) {
     constexpr int kPer = 16 / (int)sizeof(T);
 #pragma unroll
     for (int k = 0; k < kPieces<T>; ++k) {
         if (whole) {
-            copy_async16(slot + k * stride, p + k * kPer, 16);
+            copy_async16(slot + k * kLane, p + k * kPer, 16);
         } else {
             const int64_t l = left - k * kPer;
             const int n = l >= kPer ? kPer : l > 0 ? (int)l : 0;
-            copy_async16(slot + k * stride, n > 0 ? p + k * kPer : p, n * (int)sizeof(T));
+            copy_async16(slot + k * kLane, n > 0 ? p + k * kPer : p, n * (int)sizeof(T));
         }
     }
 }
-template <class T>
-__device__ __forceinline__ Oct take_octet(const uint4* slot, int stride, const Columns& c) {
+template <class T, bool RAGGED>
+__device__ __forceinline__ Oct take_octet(const uint4* slot, const Columns& c) {
     uint4 raw[kPieces<T>];
 #pragma unroll
-    for (int k = 0; k < kPieces<T>; ++k) raw[k] = slot[k * stride];
+    for (int k = 0; k < kPieces<T>; ++k) raw[k] = slot[k * kLane];
     Oct o = unpack<T>(raw);
-    mask(o, c);
+    if (RAGGED) mask(o, c);
     return o;
 }
-// An octet to p on (the place of its first column, which may not be one).
+// p, `bytes` on.
 template <class T>
+__device__ __forceinline__ T* on(T* p, int64_t bytes) {
+    return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes);
+}
+// An octet to p on (the place of its first column, which may not be one).
+template <class T, bool RAGGED>
 __device__ __forceinline__ void store_octet(T* p, const Columns& c, Oct& o) {
-    if (c.whole()) {
+    if (RAGGED ? c.whole() : c.any()) {
         uint4 raw[kPieces<T>];
         pack<T>(o, raw);
 #pragma unroll
         for (int k = 0; k < kPieces<T>; ++k) reinterpret_cast<uint4*>(p)[k] = raw[k];
         return;
     }
+    if (RAGGED) {
 #pragma unroll
-    for (int i = 0; i < kOctet; ++i)
-        if (c.in >> i & 1) p[i] = from_f32<T>(element(o, i));
+        for (int i = 0; i < kOctet; ++i)
+            if (c.in >> i & 1) p[i] = from_f32<T>(element(o, i));
+    }
 }
 
-// Sums of N values over the TPR threads of a row in each of C blocks of a cluster,
-// every thread ending with them.  In a warp the values are halved among the lanes
+// Sums of N values over the threads of a row, every thread ending with them.  In a warp the values are halved among the lanes
 // as they are added (four values: 6 shuffles, not 20).  Warps meet at a barrier of
-// their row's own, or the cluster's, having left their sums in its blocks' `red`,
-// which has two places that are used in turn: one barrier for each use is enough.
+// the block, or the cluster, having left their sums in its blocks' `red`, which
+// has two places that are used in turn: one barrier for each use is enough.
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -218,22 +220,46 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }
 constexpr int pow2_above(int n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }
-template <int TPR, int N, int C>
+constexpr int kRowWarps = 16;       // of a block, that hold a row; times a cluster's blocks
+constexpr int kCluster = 8;
+
+// The threads of a row: a block's (TPR = 0, whole warps), or those of each block
+// of a cluster; or TPR = 8 of a block of one warp, which then holds four rows.
+template <int TPR>
+struct RowThreads {
+    int warps, sub, lane;           // in this block: of a row, which row's, which of them
+    int rank, blocks;               // in the row's cluster
+    __device__ explicit RowThreads(int blocks_) : warps(1), sub(0), lane(threadIdx.x), rank(0), blocks(1) {
+        if constexpr (TPR == 8) {
+            sub = threadIdx.x >> 3;
+            lane = threadIdx.x & 7;
+        } else {
+            warps = blockDim.x >> 5;
+            blocks = blocks_;
+            if (blocks > 1) rank = (int)cluster_rank();
+        }
+    }
+    __device__ int octet() const { return rank * (int)blockDim.x + lane; }
+};
+constexpr int kWarpRows = 4;       // of TPR = 8
+
+template <int TPR, int N>
 struct RowSums {
-    static constexpr int kWarps = TPR < 32 ? 1 : TPR / 32 * C;     // that hold a part of a row
     static constexpr int kN = pow2_above(N), kLanes = 32 / kN;     // lanes that end with one value
-    static constexpr int kPlaces = 2 * kN * kWarps;                // floats of `red` for each row of a block
+    // Floats of shared memory: two places for each warp of a cluster.
+    static constexpr int kPlaces = TPR ? 1 : 2 * kN * kRowWarps * kCluster;
+    const RowThreads<TPR>& th;
     float* red;
-    int barrier, turn;
-    __device__ RowSums(float* smem, int sub) : red(smem + sub * kPlaces), barrier(1 + sub), turn(0) {
-        if (C > 1) cluster_barrier();      // every block of the cluster has begun
+    int warps, turn;
+    __device__ RowSums(const RowThreads<TPR>& th_, float* smem) : th(th_), red(smem), warps(th_.warps * th_.blocks), turn(0) {
+        if (TPR == 0 && th.blocks > 1) cluster_barrier();      // every block of the cluster has begun
     }
     __device__ __forceinline__ void operator()(float (&in)[N]) {
-        if constexpr (TPR < 32) {
+        if constexpr (TPR == 8) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
 #pragma unroll
-                for (int off = TPR / 2; off > 0; off >>= 1) in[i] += __shfl_xor_sync(0xffffffffu, in[i], off);
+                for (int off = 4; off > 0; off >>= 1) in[i] += __shfl_xor_sync(0xffffffffu, in[i], off);
             }
         } else {
             const int lane = threadIdx.x & 31;
@@ -254,30 +280,28 @@ struct RowSums {
                     v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
                 }
             }
-            if constexpr (kWarps > 1) {
-                float* at = red + turn * kN * kWarps;
+            if (warps > 1) {
+                float* at = red + turn * kN * warps;
                 turn ^= 1;
-                const int warp = (threadIdx.x % TPR) >> 5;
-                if (lane % kLanes == 0) {
-                    float* place = at + lane / kLanes * kWarps + warp;
-                    if constexpr (C == 1) {
-                        *place = v[0];
-                    } else {
-                        place += cluster_rank() * (TPR / 32);
-#pragma unroll
-                        for (int k = 0; k < C; ++k) store_to_block(place, k, v[0]);
-                    }
-                }
-                __syncwarp();
-                if constexpr (C == 1)
-                    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(TPR) : "memory");
-                else
+                float* place = at + lane / kLanes * warps + th.rank * th.warps + (threadIdx.x >> 5);
+                if (th.blocks == 1) {
+                    if (lane % kLanes == 0) *place = v[0];
+                    __syncthreads();
+                } else {
+                    if (lane % kLanes == 0)
+                        for (int k = 0; k < th.blocks; ++k) store_to_block(place, k, v[0]);
+                    __syncwarp();
                     cluster_barrier();
+                }
                 float s = 0.f;
-                const float* from = at + lane / kLanes * kWarps;
-#pragma unroll
-                for (int w = 0; w < kWarps; w += kLanes)
-                    if (kWarps % kLanes == 0 || w + lane % kLanes < kWarps) s += from[w + lane % kLanes];
+                const float* from = at + lane / kLanes * warps;
+                const int w = lane % kLanes;
+                if (warps <= 2 * kLanes) {
+                    if (w < warps) s = from[w];
+                    if (w + kLanes < warps) s += from[w + kLanes];
+                } else {
+                    for (int i = w; i < warps; i += kLanes) s += from[i];
+                }
 #pragma unroll
                 for (int off = kLanes / 2; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
                 v[0] = s;
@@ -288,17 +312,33 @@ struct RowSums {
     }
 };
 
+// How rows of so many octets lie in threads: `threads` of a block, which holds
+// `rows` rows, or its part of one that `blocks` blocks of a cluster hold.
+struct RowShape {
+    int threads, rows, blocks;
+    RowShape(int64_t octets, int most) : rows(1), blocks(1) {           // most: threads of a row in one block
+        if (octets <= 8) {
+            threads = 32;
+            rows = kWarpRows;
+            return;
+        }
+        while ((octets + blocks - 1) / blocks > most) blocks *= 2;
+        threads = (int)((octets + 32 * blocks - 1) / (32 * blocks) * 32);
+    }
+    bool fits() const { return blocks <= kCluster && threads <= 32 * kRowWarps; }
+};
+
 // Octets that a row of `cols` values touches at most.
 inline int64_t row_octets(int64_t cols) {
     int64_t most = 0;              // the largest r * cols mod 8
     for (int r = 0; r < 8; ++r) most = r * cols % 8 > most ? r * cols % 8 : most;
     return (most + cols + 7) / 8;
 }
-// Programmatic dependent launch (pdl.cuh), of clusters where C > 1.
-template <int C, class Args>
-cudaError_t launch_rows_kernel(void (*kernel)(Args), int64_t grid, int block, size_t smem, cudaStream_t stream,
-                               const Args& args) {
-    if (smem > 40 * 1024) {          // with the kernel's own, what passes 48 KB is to be asked for
+// Programmatic dependent launch (pdl.cuh), of clusters of `cluster` blocks.
+template <class... Args>
+cudaError_t launch_rows_kernel(void (*kernel)(Args...), int64_t grid, int block, size_t smem, int cluster,
+                               cudaStream_t stream, Args... args) {
+    if (smem > 32 * 1024) {          // with the kernel's own, what passes 48 KB is to be asked for
         const cudaError_t st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (st != cudaSuccess) return st;
     }
@@ -311,18 +351,18 @@ cudaError_t launch_rows_kernel(void (*kernel)(Args), int64_t grid, int block, si
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = C;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = C > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args);
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 // Whether a matrix (an absent one: yes) can be moved in octets.
 inline bool octet_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols) {
     if (p == nullptr) return true;
     if (reinterpret_cast<uintptr_t>(p) & 15) return false;
-    return rows < 2 || ld == cols || (cols % 8 == 0 && ld % 8 == 0);
+    return rows < 2 || (cols % 8 == 0 ? ld % 8 == 0 : ld == cols);
 }
 
 }  // namespace
