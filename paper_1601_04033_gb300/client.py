@@ -49,15 +49,22 @@ def _dtype(t) -> int:
     return d
 
 
-def _rows(t, like=None):
+# A small call is bound by the host, so tensors are asked as few questions as
+# will do (each costs 0.06 to 0.2 us, a new tensor 1.4 us).
+def _stream(t) -> int:
+    """torch's current stream, which is to be on t's device."""
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("CUDA tensors on the current device are expected")
+    return _f._current_stream() if _raw_stream is None else _raw_stream(t.get_device())
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _rows(t):
     """(address, rows, cols, ld) of a matrix [..., cols] whose rows are evenly spaced."""
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
-        raise ValueError(f"{tuple(t.shape)} {t.dtype} given with {tuple(like.shape)} {like.dtype}")
-    if not t.is_cuda:
-        raise ValueError("CUDA tensors are expected")
-    dim = t.dim()
-    if dim != 2:
-        if dim == 0:
+    if t.dim() != 2:
+        if t.dim() == 0:
             raise ValueError("a matrix [..., cols] is expected")
         try:
             t = t.view(-1, t.shape[-1])
@@ -67,12 +74,26 @@ def _rows(t, like=None):
     step, one = t.stride()
     if one != 1 and cols > 1:
         raise ValueError("the values of a row must be contiguous")
+    if not t.is_cuda:
+        raise ValueError("CUDA tensors are expected")
     return t.data_ptr() or _NOWHERE, rows, cols, step
 
 
+def _like(t, like):
+    """(address, ld) of a matrix of like's shape and type."""
+    if t.shape != like.shape or t.dtype is not like.dtype:
+        raise ValueError(f"{tuple(t.shape)} {t.dtype} given with {tuple(like.shape)} {like.dtype}")
+    p, _, _, step = _rows(t)
+    return p, step
+
+
+def _new(like, cols):
+    """A new matrix of like's shape and type, without gaps: (tensor, address, ld)."""
+    t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    return t, t.data_ptr() or _NOWHERE, cols
+
+
 def _vector(t, cols: int, name: str):
-    if t is None:
-        return None
     if t.dtype is not torch.float32 or t.numel() != cols or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name} must be {cols} contiguous fp32 values on the GPU")
     return t.data_ptr()
@@ -82,15 +103,17 @@ def dropout(x, draws: Draws, *, residual=None, out=None):
     """residual + dropout(x) (fasgd_dropout), in a new tensor or in `out`, which may
     be x or residual.  The gradient of x is dropout(gradient, draws)."""
     a = _f.DropoutArgs()
-    a.x, a.rows, a.cols, a.ld_x = _rows(x)
+    a.x, a.rows, cols, a.ld_x = _rows(x)
+    a.cols = cols
     a.dtype = _dtype(x)
     if residual is not None:
-        a.residual, _, _, a.ld_residual = _rows(residual, x)
+        a.residual, a.ld_residual = _like(residual, x)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    a.out, _, _, a.ld_out = _rows(out, x)
+        out, a.out, a.ld_out = _new(x, cols)
+    else:
+        a.out, a.ld_out = _like(out, x)
     a.rate, a.seed, a.client, a.n = draws
-    _check(_f.fasgd_dropout(ctypes.addressof(a), _f._current_stream()))
+    _check(_f.fasgd_dropout(ctypes.addressof(a), _stream(x)))
     return out
 
 
@@ -105,41 +128,51 @@ def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=
     """fasgd_join: h = carry x + branch gate dropout(N(y; post)), z = N(h; pre).
     gate: fp32 [cols], or [groups, cols] of fp32 or x's type, groups dividing the
     rows.  h, z: where to write them (new tensors if None)."""
-    a = _f.JoinArgs()
-    a.x, a.rows, cols, a.ld_x = _rows(x)
+    j = Joined()
+    a = j.args = _f.JoinArgs()
+    a.x, rows, cols, a.ld_x = _rows(x)
+    a.rows = rows
     a.cols = cols
     a.groups = 1
     a.dtype = _dtype(x)
     a.norm = _NORMS[norm]
-    a.eps, a.carry, a.branch = eps, carry, branch
+    a.eps = eps
+    a.carry = carry
+    a.branch = branch
     if draws is not None:
         a.rate, a.seed, a.client, a.n = draws
     if y is not None:
-        a.y, _, _, a.ld_y = _rows(y, x)
+        a.y, a.ld_y = _like(y, x)
         if h is None:
-            h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        a.h, _, _, a.ld_h = _rows(h, x)
+            h, a.h, a.ld_h = _new(x, cols)
+        else:
+            a.h, a.ld_h = _like(h, x)
     elif h is not None:
         raise ValueError("h goes with y")
     if pre is not None:
+        a.pre = _vector(pre, cols, "pre")
         if z is None:
-            z = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        a.z, _, _, a.ld_z = _rows(z, x)
+            z, a.z, a.ld_z = _new(x, cols)
+        else:
+            a.z, a.ld_z = _like(z, x)
     elif z is not None:
         raise ValueError("z goes with pre")
-    a.post, a.post_bias = _vector(post, cols, "post"), _vector(post_bias, cols, "post_bias")
-    a.pre, a.pre_bias = _vector(pre, cols, "pre"), _vector(pre_bias, cols, "pre_bias")
+    if post is not None:
+        a.post = _vector(post, cols, "post")
+    if post_bias is not None:
+        a.post_bias = _vector(post_bias, cols, "post_bias")
+    if pre_bias is not None:
+        a.pre_bias = _vector(pre_bias, cols, "pre_bias")
     if gate is not None:
         if gate.dim() == 2:
             a.groups = gate.shape[0]
         if gate.shape[-1] != cols or gate.dim() > 2 or not gate.is_contiguous() or not gate.is_cuda:
             raise ValueError("gate must be contiguous [cols] or [groups, cols] on the GPU")
         a.gate, a.gate_dtype = gate.data_ptr(), _dtype(gate)
-    stats = torch.empty(4 * a.rows, dtype=torch.float32, device=x.device)
-    a.stats = stats.data_ptr() or _NOWHERE
-    _check(_f.fasgd_join(ctypes.addressof(a), _f._current_stream()))
-    j = Joined()
-    j.h, j.z, j.args, j.x, j.y, j.stats = h, z, a, x, y, stats
+    j.stats = torch.empty(4 * rows, dtype=torch.float32, device=x.device)
+    a.stats = j.stats.data_ptr() or _NOWHERE
+    _check(_f.fasgd_join(ctypes.addressof(a), _stream(x)))
+    j.h, j.z, j.x, j.y = h, z, x, y
     j.parameters = (post, post_bias, gate, pre, pre_bias)
     return j
 
@@ -154,50 +187,59 @@ class JoinGrads(NamedTuple):
     pre_bias: object = None
 
 
-def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads = JoinGrads()) -> JoinGrads:
+def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinGrads:
     """fasgd_join_grad: the gradients of ``join``'s x, y and parameters from those
     of its h (None: zero) and z.  x, y, the parameters and the stream's order are
     to be as they were.  into: where to write them (new tensors where None)."""
     a, x = _f.JoinArgs.from_buffer_copy(j.args), j.x
+    cols = a.cols
+    dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias = into if into is not None else _NO_GRADS
     post, post_bias, gate, pre, pre_bias = j.parameters
     if dh is not None:
-        a.dh, _, _, a.ld_dh = _rows(dh, x)
+        a.dh, a.ld_dh = _like(dh, x)
     if dz is not None:
-        a.dz, _, _, a.ld_dz = _rows(dz, x)
-
-    dx = into.x if into.x is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    a.dx, _, _, a.ld_dx = _rows(dx, x)
-    dy = None
-    if j.y is not None:
-        dy = into.y if into.y is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        a.dy, _, _, a.ld_dy = _rows(dy, x)
-    cols = a.cols
-
-    def vector(of, name):
-        if of is None:
-            return None, None
-        t = getattr(into, name)
-        if t is None:
-            t = torch.empty_like(of)
-            return t, t.data_ptr()
-        return t, _vector(t, cols, name)
-
-    dpost, a.dpost = vector(post, "post")
-    dpost_bias, a.dpost_bias = vector(post_bias, "post_bias")
-    dpre, a.dpre = vector(pre, "pre")
-    dpre_bias, a.dpre_bias = vector(pre_bias, "pre_bias")
-    dgate = None
+        a.dz, a.ld_dz = _like(dz, x)
+    if dx is None:
+        dx, a.dx, a.ld_dx = _new(x, cols)
+    else:
+        a.dx, a.ld_dx = _like(dx, x)
+    if j.y is None:
+        dy = None
+    elif dy is None:
+        dy, a.dy, a.ld_dy = _new(x, cols)
+    else:
+        a.dy, a.ld_dy = _like(dy, x)
+    if post is not None:
+        dpost, a.dpost = _grad_vector(dpost, post, cols)
+    if post_bias is not None:
+        dpost_bias, a.dpost_bias = _grad_vector(dpost_bias, post_bias, cols)
+    if pre is not None:
+        dpre, a.dpre = _grad_vector(dpre, pre, cols)
+    if pre_bias is not None:
+        dpre_bias, a.dpre_bias = _grad_vector(dpre_bias, pre_bias, cols)
     if gate is not None:
-        dgate = into.gate if into.gate is not None else torch.empty_like(gate)
-        if dgate.shape != gate.shape or dgate.dtype != gate.dtype or not dgate.is_contiguous():
+        if dgate is None:
+            dgate = torch.empty_like(gate)
+        elif dgate.shape != gate.shape or dgate.dtype is not gate.dtype or not dgate.is_contiguous():
             raise ValueError("the gate's gradient must be as the gate")
         a.dgate = dgate.data_ptr()
     at = ctypes.addressof(a)
     size = _check(_f.fasgd_join_workspace(at))
     space = torch.empty(size, dtype=torch.uint8, device=x.device)
-    a.workspace, a.workspace_bytes = space.data_ptr(), size
-    _check(_f.fasgd_join_grad(at, _f._current_stream()))
+    a.workspace = space.data_ptr()
+    a.workspace_bytes = size
+    _check(_f.fasgd_join_grad(at, _stream(x)))
     return JoinGrads(dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias)
+
+
+_NO_GRADS = JoinGrads()
+
+
+def _grad_vector(t, of, cols):
+    if t is None:
+        t = torch.empty_like(of)
+        return t, t.data_ptr()
+    return t, _vector(t, cols, "a parameter's gradient")
 
 
 class Balance(NamedTuple):
@@ -211,11 +253,14 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
     (grad) the gradient of the logits, times `upstream` (a device fp32 value) if
     given.  chosen: int32 [..., top]; valid: bool or uint8, one per row."""
     a = _f.BalanceArgs()
-    a.logits, rows, a.cols, a.ld_logits = _rows(logits)
-    a.rows, a.groups, a.top, a.dtype = rows, groups, chosen.shape[-1], _dtype(logits)
-    a.balance_scale, a.z_scale = balance, z
+    a.logits, rows, cols, a.ld_logits = _rows(logits)
+    a.rows, a.cols, a.groups, top = rows, cols, groups, chosen.shape[-1]
+    a.top = top
+    a.dtype = _dtype(logits)
+    a.balance_scale = balance
+    a.z_scale = z
     if chosen.dtype is not torch.int32 or not chosen.is_contiguous() or not chosen.is_cuda or \
-            chosen.numel() != rows * a.top:
+            chosen.numel() != rows * top:
         raise ValueError("chosen must be contiguous int32 [..., top] on the GPU, a row for each of logits")
     a.chosen = chosen.data_ptr() or _NOWHERE
     if valid is not None:
@@ -225,18 +270,20 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
         a.valid = valid.data_ptr()
     if upstream is not None:
         a.upstream = _vector(upstream, 1, "upstream")
-    dlogits = None
-    if grad:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        a.dlogits, _, _, a.ld_dlogits = _rows(dlogits)
-    counts = torch.empty((groups, a.cols), dtype=torch.int32, device=logits.device)
-    loss = torch.empty(3, dtype=torch.float32, device=logits.device)
-    a.counts, a.loss = counts.data_ptr(), loss.data_ptr()
     at = ctypes.addressof(a)
     size = _check(_f.fasgd_balance_workspace(at))
-    space = torch.empty(size, dtype=torch.uint8, device=logits.device)
-    a.workspace, a.workspace_bytes = space.data_ptr(), size
-    _check(_f.fasgd_balance(at, _f._current_stream()))
+    dlogits = None
+    if grad:
+        dlogits, a.dlogits, a.ld_dlogits = _new(logits, cols)
+    device = logits.device
+    counts = torch.empty((groups, cols), dtype=torch.int32, device=device)
+    loss = torch.empty(3, dtype=torch.float32, device=device)
+    space = torch.empty(size, dtype=torch.uint8, device=device)
+    a.counts = counts.data_ptr()
+    a.loss = loss.data_ptr()
+    a.workspace = space.data_ptr()
+    a.workspace_bytes = size
+    _check(_f.fasgd_balance(at, _stream(logits)))
     return Balance(loss, counts, dlogits)
 
 

@@ -98,26 +98,27 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : kForwardT
     RowSums<TPR, NR> sums(th, red);
     const bool has_y = a.y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
     constexpr int kSlots = 2 * NR * kP * kLane;      // of a warp's stage
-    uint4* const mine = ring + (threadIdx.x >> 5) * kSlots + (threadIdx.x & 31);
+    uint4* const mine = ring + (threadIdx.x >> 5) * kSlots;
     const int stage_size = kSlots * th.warps;
     if (!c.any())
         for (int i = 0; i < STAGES; ++i)
-            for (int k = 0; k < kSlots; k += kLane) mine[i * stage_size + k] = make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < kSlots; k += kLane) mine[i * stage_size + k + (threadIdx.x & 31)] = make_uint4(0, 0, 0, 0);
+    __syncwarp();
     pdl_wait();
     pdl_trigger();
 
-    const T* x = static_cast<const T*>(a.x) + first * a.ld_x + c.c0;      // of the next row to fetch
-    const T* y = static_cast<const T*>(a.y) + first * a.ld_y + c.c0;
-    int64_t unfetched = c.any() ? rows : 0;
-    // The matrix ends inside this thread's octet of its last row.
-    const bool clipped = RAGGED && c.c0 + kOctet > a.cols && first + (rows - 1) * step == a.rows - 1;
+    const CopyLane<T, TPR == 8 ? 8 : 32> lane(c, (int32_t)a.cols);
+    const T* x = static_cast<const T*>(a.x) + first * a.ld_x + lane.col;      // of the next row to fetch
+    const T* y = static_cast<const T*>(a.y) + first * a.ld_y + lane.col;
+    int64_t unfetched = rows;
+    const bool clipped = RAGGED && first + (rows - 1) * step == a.rows - 1;   // the matrix ends with the last row
     const auto fetch = [&](uint4* slot) {
 #pragma unroll
         for (int j = 0; j < NR; ++j) {
             if (unfetched > 0) {
-                const bool whole = !RAGGED || !clipped || unfetched > 1;
-                copy_octet<T>(slot + 2 * j * kP * kLane, x, whole, a.cols - c.c0);
-                if (has_y) copy_octet<T>(slot + (2 * j + 1) * kP * kLane, y, whole, a.cols - c.c0);
+                const bool clip = clipped && unfetched == 1;
+                lane.copy(slot + 2 * j * kP * kLane, x, clip);
+                if (has_y) lane.copy(slot + (2 * j + 1) * kP * kLane, y, clip);
             }
             --unfetched;
             x = on(x, s.x);
@@ -178,6 +179,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : kForwardT
     int stage = 0;
     for (int64_t turn = 0, left = rows; turn < turns; ++turn, left -= NR) {
         copy_wait<STAGES - 2>();
+        __syncwarp();
         const uint4* slot = mine + stage * stage_size;
         Oct h[NR], t[NR];
 #pragma unroll
@@ -274,18 +276,18 @@ cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cud
                 : launch_octets<T, LAYER, true, false>(a, s, num_sms, stream);
 }
 
-bool in_octets(const JoinArgs& a) {
+bool in_octets(const JoinArgs& a, int size) {
     const void* p[] = {a.x, a.y, a.h, a.z};
     const int64_t ld[] = {a.ld_x, a.ld_y, a.ld_h, a.ld_z};
     for (int i = 0; i < 4; ++i)
-        if (!octet_matrix(p[i], ld[i], a.rows, a.cols)) return false;
+        if (!octet_matrix(p[i], ld[i], a.rows, a.cols, size)) return false;
     return true;
 }
 
 template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     const RowShape s(row_octets(a.cols), 512);
-    if (s.fits() && in_octets(a))
+    if (s.fits() && in_octets(a, (int)sizeof(T)))
         return a.layer ? launch_octets<T, true>(a, s, num_sms, stream) : launch_octets<T, false>(a, s, num_sms, stream);
     const int64_t grid = a.rows < (int64_t)num_sms * 8 ? a.rows : (int64_t)num_sms * 8;
     return launch_pdl(join_any_kernel<T>, (unsigned)grid, kThreads, 0, stream, a);

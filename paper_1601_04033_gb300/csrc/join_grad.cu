@@ -202,14 +202,16 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     const Columns c(th.octet(), RAGGED && mine < units ? (int)((Unit(a, mine).row * a.cols) & 7) : 0,
                     (int32_t)a.cols);
     constexpr int kSlots = 4 * kP * kLane;           // of a warp's stage
-    uint4* const own = ring + (threadIdx.x >> 5) * kSlots + (threadIdx.x & 31);
+    uint4* const own = ring + (threadIdx.x >> 5) * kSlots;
     const int stage_size = kSlots * th.warps;
     // The rows' statistics, copied ahead by one lane of theirs in each warp.
     uint4* const own_stats = ring + STAGES * stage_size + (threadIdx.x >> 5) * kWarpRows + (TPR == 8 ? th.sub : 0);
     const bool asks = (threadIdx.x & (TPR == 8 ? 7 : 31)) == 0;
     if (!c.any())
         for (int i = 0; i < STAGES; ++i)
-            for (int k = 0; k < kSlots; k += kLane) own[i * stage_size + k] = make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < kSlots; k += kLane) own[i * stage_size + k + (threadIdx.x & 31)] = make_uint4(0, 0, 0, 0);
+    __syncwarp();
+    const CopyLane<T, TPR == 8 ? 8 : 32> lane(c, (int32_t)a.cols);
     pdl_wait();
     pdl_trigger();
 
@@ -249,24 +251,22 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
         if (gates) d_gate = Oct{};
 
         const int64_t r0 = u.row;
-        const T* x = static_cast<const T*>(a.x) + r0 * a.ld_x + c.c0;       // of the next row to fetch
-        const T* y = static_cast<const T*>(a.y) + r0 * a.ld_y + c.c0;
-        const T* dh = static_cast<const T*>(a.dh) + r0 * a.ld_dh + c.c0;
-        const T* dz = static_cast<const T*>(a.dz) + r0 * a.ld_dz + c.c0;
+        const T* x = static_cast<const T*>(a.x) + r0 * a.ld_x + lane.col;       // of the next row to fetch
+        const T* y = static_cast<const T*>(a.y) + r0 * a.ld_y + lane.col;
+        const T* dh = static_cast<const T*>(a.dh) + r0 * a.ld_dh + lane.col;
+        const T* dz = static_cast<const T*>(a.dz) + r0 * a.ld_dz + lane.col;
         const float4* stats = a.stats + r0;
         int64_t unfetched = rows;
-        // The matrix ends inside this thread's octet of its last row.
-        const bool clipped = RAGGED && c.c0 + kOctet > a.cols && r0 + (rows - 1) * u.step == a.rows - 1;
+        const bool clipped = RAGGED && r0 + (rows - 1) * u.step == a.rows - 1;   // the matrix ends with the last row
         const auto fetch = [&](int stage) {
             uint4* slot = own + stage * stage_size;
-            if (unfetched > 0 && asks) copy_async16(own_stats + stage * kWarpRows * th.warps, stats, 16);
-            if (unfetched > 0 && c.any()) {
-                const bool whole = !RAGGED || !clipped || unfetched > 1;
-                const int64_t left = a.cols - c.c0;
-                copy_octet<T>(slot, x, whole, left);
-                if (has_y) copy_octet<T>(slot + kP * kLane, y, whole, left);
-                if (has_dh) copy_octet<T>(slot + 2 * kP * kLane, dh, whole, left);
-                if (has_pre) copy_octet<T>(slot + 3 * kP * kLane, dz, whole, left);
+            if (unfetched > 0) {
+                const bool clip = clipped && unfetched == 1;
+                if (asks) copy_async16(own_stats + stage * kWarpRows * th.warps, stats, 16);
+                lane.copy(slot, x, clip);
+                if (has_y) lane.copy(slot + kP * kLane, y, clip);
+                if (has_dh) lane.copy(slot + 2 * kP * kLane, dh, clip);
+                if (has_pre) lane.copy(slot + 3 * kP * kLane, dz, clip);
             }
             copy_commit();
             --unfetched;
@@ -295,7 +295,6 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             if (has_y) yhat = take_octet<T, RAGGED>(slot + kP * kLane, c);
             if (has_dh) w = take_octet<T, RAGGED>(slot + 2 * kP * kLane, c);
             if (has_pre) q = take_octet<T, RAGGED>(slot + 3 * kP * kLane, c);
-            __syncwarp();     // every lane has read the statistics that the next copy replaces
             fetch(stage == 0 ? STAGES - 1 : stage - 1);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
             if (!live) hhat = yhat = w = q = Oct{};      // a row past the end
@@ -452,11 +451,11 @@ __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_cons
 int64_t at_most(int64_t n, int64_t cap) { return n < cap ? (n < 1 ? 1 : n) : cap; }
 
 constexpr int kGradThreads = 512;       // of a row in one block, and in an SM (128 registers each)
-bool in_octets(const JoinArgs& a) {
+bool in_octets(const JoinArgs& a, int size) {
     const void* p[] = {a.x, a.y, a.dh, a.dz, a.dx, a.dy};
     const int64_t ld[] = {a.ld_x, a.ld_y, a.ld_dh, a.ld_dz, a.ld_dx, a.ld_dy};
     for (int i = 0; i < 6; ++i)
-        if (!octet_matrix(p[i], ld[i], a.rows, a.cols)) return false;
+        if (!octet_matrix(p[i], ld[i], a.rows, a.cols, size)) return false;
     // A group's rows fall into eight classes where cols is no multiple of 8: short
     // groups would leave more sums than rows.
     if (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64) return false;
@@ -489,7 +488,7 @@ cudaError_t launch_octets(const JoinArgs& a, cudaStream_t stream) {
 template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     cudaError_t st = cudaSuccess;
-    if (a.rows > 0 && in_octets(a)) {
+    if (a.rows > 0 && in_octets(a, (int)sizeof(T))) {
         st = a.layer ? launch_octets<T, true>(a, stream) : launch_octets<T, false>(a, stream);
     } else if (a.rows > 0) {
         st = launch_pdl(grad_rows_any_kernel<T>, (unsigned)at_most(a.rows, (int64_t)num_sms * 8), kThreads, 0,
@@ -510,11 +509,10 @@ cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
 }  // namespace
 
 JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms) {
-    (void)dtype;
     JoinPlan p;
     p.parts = p.splits = p.row_means = 0;
     if (a.rows == 0) return p;
-    if (in_octets(a)) {
+    if (in_octets(a, dtype == FASGD_F32 ? 4 : 2)) {
         const RowShape s(row_octets(a.cols), kGradThreads);
         const int64_t block_subs = s.rows, per_sm = kGradThreads / s.threads;
         const int64_t most = (int64_t)num_sms * per_sm / s.blocks / 8 * 8 * block_subs;

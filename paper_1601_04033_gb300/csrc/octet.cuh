@@ -139,10 +139,12 @@ __device__ __forceinline__ float2 keep2(const Philox4& r, int i, uint32_t last, 
 }
 
 // ---- loads into shared memory -------------------------------------------------
-// Each thread copies its own octets ahead, into places that it alone reads, so
-// the pipeline needs no barrier and no wait that could run out.  A warp's places
-// lie together: 16 bytes of each of its lanes, kLane apart, then the next 16.
-constexpr int kLane = 32;
+// A warp copies its own octets ahead, into places that it alone reads, so the
+// pipeline needs no barrier of the block and no wait that could run out.  Of an
+// fp32 octet's two pieces a lane copies those that make a warp's copies contiguous
+// (each owner's own would touch every 32-byte sector twice); so a lane reads what
+// others copied, after the wait and a __syncwarp.
+constexpr int kLane = 32;          // 16-byte places of one piece of a warp's octets
 __device__ __forceinline__ void copy_async16(void* smem, const void* global, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)),
                  "l"(global), "r"(bytes)
@@ -153,27 +155,44 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// An octet from p on, of which the matrix holds `left` values (what lies behind
-// its end is not read: zeros); whole: it holds all of them.
-template <class T>
-__device__ __forceinline__ void copy_octet(uint4* slot, const T* p, bool whole, int64_t left) {
-    constexpr int kPer = 16 / (int)sizeof(T);
+// The pieces that a lane copies of a row that W lanes of its warp hold, the first
+// of them from column c0 on: from column col + k * kStep on, if bit k of `in`.
+template <class T, int W>
+struct CopyLane {
+    static constexpr int kPer = 16 / (int)sizeof(T), kStep = W * kPer;
+    int32_t col, cols;
+    uint32_t in;
+    int place;          // of its piece 0 in shared memory
+    __device__ CopyLane(const Columns& c, int32_t cols_) : cols(cols_), in(0) {
+        const int lane = threadIdx.x & 31, of_row = lane % W;
+        col = __shfl_sync(0xffffffffu, c.c0, 0, W) + of_row * kPer;
+        place = kPieces<T> == 1 ? lane : (of_row & 1) * kLane + lane - of_row + (of_row >> 1);
 #pragma unroll
-    for (int k = 0; k < kPieces<T>; ++k) {
-        if (whole) {
-            copy_async16(slot + k * kLane, p + k * kPer, 16);
-        } else {
-            const int64_t l = left - k * kPer;
-            const int n = l >= kPer ? kPer : l > 0 ? (int)l : 0;
-            copy_async16(slot + k * kLane, n > 0 ? p + k * kPer : p, n * (int)sizeof(T));
+        for (int k = 0; k < kPieces<T>; ++k)
+            if (col + k * kStep + kPer > 0 && col + k * kStep < cols) in |= 1u << k;
+    }
+    // p: the row's first value, `col` on.  clip: the matrix ends with this row, so
+    // what lies behind it is not read (zeros).
+    __device__ __forceinline__ void copy(uint4* slot, const T* p, bool clip) const {
+#pragma unroll
+        for (int k = 0; k < kPieces<T>; ++k) {
+            if (!(in >> k & 1)) continue;
+            uint4* to = slot + place + k * (W / 2);
+            if (!clip) {
+                copy_async16(to, p + k * kStep, 16);
+            } else {
+                const int left = cols - col - k * kStep;
+                copy_async16(to, p + k * kStep, (left < kPer ? left : kPer) * (int)sizeof(T));
+            }
         }
     }
-}
+};
+// slot: the warp's place of a matrix.
 template <class T, bool RAGGED>
 __device__ __forceinline__ Oct take_octet(const uint4* slot, const Columns& c) {
     uint4 raw[kPieces<T>];
 #pragma unroll
-    for (int k = 0; k < kPieces<T>; ++k) raw[k] = slot[k * kLane];
+    for (int k = 0; k < kPieces<T>; ++k) raw[k] = slot[k * kLane + (threadIdx.x & 31)];
     Oct o = unpack<T>(raw);
     if (RAGGED) mask(o, c);
     return o;
@@ -183,14 +202,28 @@ template <class T>
 __device__ __forceinline__ T* on(T* p, int64_t bytes) {
     return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes);
 }
+// A whole octet in one instruction: an fp32 one as 32 bytes.
+__device__ __forceinline__ void store_pieces(void* p, const uint4 (&r)[1]) { *static_cast<uint4*>(p) = r[0]; }
+__device__ __forceinline__ void store_pieces(void* p, const uint4 (&r)[2]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0].x), "r"(r[0].y),
+                 "r"(r[0].z), "r"(r[0].w), "r"(r[1].x), "r"(r[1].y), "r"(r[1].z), "r"(r[1].w)
+                 : "memory");
+}
+__device__ __forceinline__ void load_pieces(const void* p, uint4 (&r)[1]) { r[0] = *static_cast<const uint4*>(p); }
+__device__ __forceinline__ void load_pieces(const void* p, uint4 (&r)[2]) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0].x), "=r"(r[0].y), "=r"(r[0].z), "=r"(r[0].w), "=r"(r[1].x), "=r"(r[1].y), "=r"(r[1].z),
+                   "=r"(r[1].w)
+                 : "l"(p)
+                 : "memory");
+}
 // An octet to p on (the place of its first column, which may not be one).
 template <class T, bool RAGGED>
 __device__ __forceinline__ void store_octet(T* p, const Columns& c, Oct& o) {
     if (RAGGED ? c.whole() : c.any()) {
         uint4 raw[kPieces<T>];
         pack<T>(o, raw);
-#pragma unroll
-        for (int k = 0; k < kPieces<T>; ++k) reinterpret_cast<uint4*>(p)[k] = raw[k];
+        store_pieces(p, raw);
         return;
     }
     if (RAGGED) {
@@ -359,9 +392,9 @@ cudaError_t launch_rows_kernel(void (*kernel)(Args...), int64_t grid, int block,
 }
 
 // Whether a matrix (an absent one: yes) can be moved in octets.
-inline bool octet_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols) {
+inline bool octet_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols, int size) {
     if (p == nullptr) return true;
-    if (reinterpret_cast<uintptr_t>(p) & 15) return false;
+    if (reinterpret_cast<uintptr_t>(p) % (kOctet * size)) return false;
     return rows < 2 || (cols % 8 == 0 ? ld % 8 == 0 : ld == cols);
 }
 
