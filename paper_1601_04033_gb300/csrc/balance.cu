@@ -5,51 +5,86 @@
 // So once the assignments are counted, the losses and the gradient take one pass
 // over the logits, and a row leaves two numbers, not cols probabilities, to sum.
 
-#include "client.cuh"
+#include "octet.cuh"
 #include "pdl.cuh"
 
 namespace fasgd {
 namespace {
 
 constexpr int kCountThreads = 512;
+constexpr int kCountCluster = 8;        // blocks that count one split together
 constexpr int kThreads = 256;
 
-// Counts of one split of one group's rows, in shared memory (integers: the order
-// of the additions does not show).
-__global__ void __launch_bounds__(kCountThreads) balance_count_kernel(const __grid_constant__ BalanceArgs a) {
-    __shared__ int32_t hist[FASGD_EXPERTS_MAX];
-    __shared__ int32_t rows_valid;
+// Adds the assignments of rows r0 .. r1 to `hist`, and the rows that take part to
+// `rows_valid`, both in shared memory (integers: no order shows).  U entries a
+// thread are asked for before the first is counted.
+__device__ __forceinline__ void count_rows(const BalanceArgs& a, int64_t r0, int64_t r1, int32_t* hist,
+                                           int32_t* rows_valid) {
+    constexpr int U = 8;
+    const uint32_t top = (uint32_t)a.top, cols = (uint32_t)a.cols, threads = blockDim.x;
+    if (a.valid != nullptr) {
+        int32_t v = 0;
+        for (int64_t r = r0 + threadIdx.x; r < r1; r += threads) v += a.valid[r] != 0;
+        v = __reduce_add_sync(0xffffffffu, v);
+        if ((threadIdx.x & 31) == 0 && v != 0) atomicAdd(rows_valid, v);
+    }
+    const int64_t i1 = r1 * a.top;
+    for (int64_t i = r0 * a.top + threadIdx.x; i < i1; i += (int64_t)threads * U) {
+        int32_t e[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t k = i + (int64_t)u * threads;
+            e[u] = k < i1 ? a.chosen[k] : -1;
+            if (a.valid != nullptr && k < i1 && a.valid[(uint32_t)k / top] == 0) e[u] = -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if ((uint32_t)e[u] < cols) atomicAdd(&hist[e[u]], 1);
+    }
+}
+
+// Counts of one split of one group's rows: a block's where a group is one split,
+// else a cluster's, whose blocks add up their counts, a share of the experts each.
+__global__ void __launch_bounds__(kCountThreads)
+    balance_count_kernel(const __grid_constant__ BalanceArgs a, int blocks) {
+    __shared__ int32_t hist[FASGD_EXPERTS_MAX + 1];      // and the rows that take part
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
-    const int64_t per = (a.group_rows + a.splits - 1) / a.splits;
-    const int cols = (int)a.cols;
-    const uint32_t top = (uint32_t)a.top;
-    for (int64_t unit = blockIdx.x; unit < a.groups * a.splits; unit += gridDim.x) {
-        const int64_t group = unit / a.splits, split = unit - group * a.splits;
-        const int64_t from = split * per < a.group_rows ? split * per : a.group_rows;
+    const int cols = (int)a.cols, rank = blocks > 1 ? (int)cluster_rank() : 0;
+    const int64_t pieces = a.splits * blocks, per = (a.group_rows + pieces - 1) / pieces;
+    // Every block of a cluster takes as many turns.
+    for (int64_t unit = blockIdx.x / blocks; unit < a.groups * a.splits; unit += gridDim.x / blocks) {
+        const int64_t group = unit / a.splits, piece = (unit - group * a.splits) * blocks + rank;
+        const int64_t from = piece * per < a.group_rows ? piece * per : a.group_rows;
         const int64_t to = from + per < a.group_rows ? from + per : a.group_rows;
-        const int64_t r0 = group * a.group_rows + from, r1 = group * a.group_rows + to;
-        for (int e = threadIdx.x; e < cols; e += kCountThreads) hist[e] = 0;
-        if (threadIdx.x == 0) rows_valid = 0;
+        for (int e = threadIdx.x; e <= cols; e += kCountThreads) hist[e] = 0;
         __syncthreads();
-        if (a.valid != nullptr) {
-            int32_t v = 0;
-            for (int64_t r = r0 + threadIdx.x; r < r1; r += kCountThreads) v += a.valid[r] != 0;
-            v = __reduce_add_sync(0xffffffffu, v);
-            if ((threadIdx.x & 31) == 0 && v != 0) atomicAdd(&rows_valid, v);
-        }
-        const uint32_t i1 = (uint32_t)(r1 * a.top);
-        for (uint32_t i = (uint32_t)(r0 * a.top) + threadIdx.x; i < i1; i += kCountThreads) {
-            const int32_t e = a.chosen[i];
-            if ((uint32_t)e < (uint32_t)cols && (a.valid == nullptr || a.valid[i / top] != 0))
-                atomicAdd(&hist[e], 1);
-        }
+        if (a.valid == nullptr && threadIdx.x == 0) hist[cols] = (int32_t)(to - from);
+        count_rows(a, group * a.group_rows + from, group * a.group_rows + to, hist, &hist[cols]);
         __syncthreads();
         int32_t* out = a.splits > 1 ? a.part_counts + unit * cols : a.counts + group * cols;
-        for (int e = threadIdx.x; e < cols; e += kCountThreads) out[e] = hist[e];
-        if (threadIdx.x == 0) a.part_valid[unit] = a.valid != nullptr ? rows_valid : (int32_t)(r1 - r0);
-        __syncthreads();
+        if (blocks == 1) {
+            for (int e = threadIdx.x; e <= cols; e += kCountThreads)
+                *(e < cols ? out + e : a.part_valid + unit) = hist[e];
+            __syncthreads();
+            continue;
+        }
+        cluster_barrier();
+        for (int e = rank * kCountThreads + threadIdx.x; e <= cols; e += blocks * kCountThreads) {
+            int32_t s = 0;
+            for (int k = 0; k < blocks; ++k) {
+                uint32_t there;
+                int32_t v;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                             : "=r"(there)
+                             : "r"((uint32_t)__cvta_generic_to_shared(&hist[e])), "r"(k));
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
+                s += v;
+            }
+            *(e < cols ? out + e : a.part_valid + unit) = s;
+        }
+        cluster_barrier();       // before a block's counts are cleared, or it ends
     }
 }
 
@@ -65,20 +100,15 @@ __device__ __forceinline__ float block_sum(float v, float* smem) {
     return v;
 }
 
-// A unit is `unit_rows` consecutive rows of one group; a block takes every
-// gridDim-th unit, a warp a row at a time.
-template <class T>
-__global__ void __launch_bounds__(kThreads)
-    balance_any_kernel(const __grid_constant__ BalanceArgs a, int64_t unit_rows) {
-    __shared__ float f[FASGD_EXPERTS_MAX];
-    __shared__ float smem[kThreads / 32];
-    __shared__ bool last;
-    constexpr int kWarps = kThreads / 32;
-    pdl_wait();
-    pdl_trigger();
-    const int cols = (int)a.cols, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    // N and G'.
-    float live = (float)a.groups, rows_all = (float)a.rows;
+// What every block of the pass knows: N and G' (as floats), and the factors made
+// of them.
+struct Totals {
+    float rows, live, zscale, up;
+};
+__device__ __forceinline__ Totals totals(const BalanceArgs& a, float* smem) {
+    Totals t;
+    t.rows = (float)a.rows;
+    t.live = (float)a.groups;
     if (a.valid != nullptr) {
         float n = 0.f, g1 = 0.f;
         for (int64_t g = threadIdx.x; g < a.groups; g += kThreads) {
@@ -87,83 +117,53 @@ __global__ void __launch_bounds__(kThreads)
             n += (float)v;
             g1 += v > 0 ? 1.f : 0.f;
         }
-        rows_all = block_sum(n, smem);
-        live = block_sum(g1, smem);
+        t.rows = block_sum(n, smem);
+        t.live = block_sum(g1, smem);
     }
-    const float up = a.upstream != nullptr ? *a.upstream : 1.f;
-    const float zscale = rows_all > 0.f ? 2.f * a.z_scale / rows_all : 0.f;
-    const int64_t units_per_group = (a.group_rows + unit_rows - 1) / unit_rows;
-    float sum_dot = 0.f, sum_z = 0.f;
-    for (int64_t unit = blockIdx.x; unit < a.groups * units_per_group; unit += gridDim.x) {
-        const int64_t group = unit / units_per_group, part = unit - group * units_per_group;
-        int32_t n = 0;
-        for (int64_t s = 0; s < a.splits; ++s) n += a.part_valid[group * a.splits + s];
-        const float inv_n = n > 0 ? 1.f / (float)n : 0.f;
-        __syncthreads();
-        for (int e = threadIdx.x; e < cols; e += kThreads) {
-            int32_t c = 0;
-            if (a.splits > 1) {
-                for (int64_t s = 0; s < a.splits; ++s) c += a.part_counts[(group * a.splits + s) * cols + e];
-                if (part == 0) a.counts[group * cols + e] = c;
-            } else {
-                c = a.counts[group * cols + e];
-            }
-            f[e] = (float)c * (inv_n / (float)a.top);
+    t.up = a.upstream != nullptr ? *a.upstream : 1.f;
+    t.zscale = t.rows > 0.f ? 2.f * a.z_scale / t.rows : 0.f;
+    return t;
+}
+// The group's f = counts / (top N_g) in shared memory (and its counts, where it has
+// to add them up and `write` says so); returns 1 / N_g, or 0.
+__device__ __forceinline__ float group_shares(const BalanceArgs& a, int64_t group, bool write, float* f) {
+    const int cols = (int)a.cols;
+    int32_t n = 0;
+    for (int64_t s = 0; s < a.splits; ++s) n += a.part_valid[group * a.splits + s];
+    const float inv_n = n > 0 ? 1.f / (float)n : 0.f;
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols; e += kThreads) {
+        int32_t c = 0;
+        if (a.splits > 1) {
+            for (int64_t s = 0; s < a.splits; ++s) c += a.part_counts[(group * a.splits + s) * cols + e];
+            if (write) a.counts[group * cols + e] = c;
+        } else {
+            c = a.counts[group * cols + e];
         }
-        __syncthreads();
-        const float scale = live > 0.f ? a.balance_scale * (float)cols / live * inv_n : 0.f;
-        const int64_t end = (part + 1) * unit_rows < a.group_rows ? (part + 1) * unit_rows : a.group_rows;
-        float unit_dot = 0.f;
-        for (int64_t i = part * unit_rows + warp; i < end; i += kWarps) {
-            const int64_t r = group * a.group_rows + i;
-            const T* x = static_cast<const T*>(a.logits) + r * a.ld_logits;
-            T* d = static_cast<T*>(a.dlogits) + r * a.ld_dlogits;
-            if (a.valid != nullptr && a.valid[r] == 0) {
-                if (a.dlogits != nullptr)
-                    for (int e = lane; e < cols; e += 32) d[e] = from_f32<T>(0.f);
-                continue;
-            }
-            float top = -INFINITY;
-            for (int e = lane; e < cols; e += 32) top = fmaxf(top, to_f32(x[e]));
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            float sum = 0.f, dot = 0.f;
-            for (int e = lane; e < cols; e += 32) {
-                const float p = expf(to_f32(x[e]) - top);
-                sum += p;
-                dot += f[e] * p;
-            }
-            sum = warp_sum(sum);
-            dot = warp_sum(dot);
-            bool nan_row = false;
-            for (int e = lane; e < cols; e += 32) nan_row |= isnan(to_f32(x[e]));
-            nan_row = __any_sync(0xffffffffu, nan_row);
-            const bool empty = top == -INFINITY && !nan_row;   // no expert is open to this row
-            const float inv = empty ? 0.f : 1.f / sum, lse = empty ? 0.f : top + logf(sum);
-            dot = empty ? 0.f : dot * inv;
-            unit_dot += dot;
-            sum_z += lse * lse;
-            if (a.dlogits != nullptr)
-                for (int e = lane; e < cols; e += 32) {
-                    const float p = empty ? 0.f : expf(to_f32(x[e]) - top) * inv;
-                    d[e] = from_f32<T>(up * p * (scale * (f[e] - dot) + zscale * lse));
-                }
-        }
-        sum_dot += unit_dot * inv_n;
+        f[e] = (float)c * (inv_n / (float)a.top);
     }
-    if (a.loss == nullptr) return;
-    // The warps' sums (equal in all lanes), then the blocks', in order.
     __syncthreads();
-    if (lane == 0) smem[warp] = sum_dot;
-    __syncthreads();
-    float dot = 0.f, z = 0.f;
-    if (threadIdx.x == 0)
-        for (int w = 0; w < kWarps; ++w) dot += smem[w];
-    __syncthreads();
-    if (lane == 0) smem[warp] = sum_z;
-    __syncthreads();
+    return inv_n;
+}
+// The losses of sums over all rows.
+__device__ __forceinline__ void store_loss(const BalanceArgs& a, const Totals& t, float dot, float z) {
+    const float balance = t.live > 0.f ? (float)a.cols / t.live * dot : 0.f;
+    z = t.rows > 0.f ? z / t.rows : 0.f;
+    a.loss[0] = a.balance_scale * balance + a.z_scale * z;
+    a.loss[1] = balance;
+    a.loss[2] = z;
+}
+// The losses of the blocks' sums: the block that leaves its own last adds them up,
+// in the blocks' order.
+__device__ __forceinline__ void join_loss(const BalanceArgs& a, const Totals& t, float dot, float z, float* smem) {
+    __shared__ bool last;
+    dot = block_sum(dot, smem);
+    z = block_sum(z, smem);
+    if (gridDim.x == 1) {
+        if (threadIdx.x == 0) store_loss(a, t, dot, z);
+        return;
+    }
     if (threadIdx.x == 0) {
-        for (int w = 0; w < kWarps; ++w) z += smem[w];
         a.part_loss[blockIdx.x] = make_float2(dot, z);
         __threadfence();
         last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
@@ -179,13 +179,200 @@ __global__ void __launch_bounds__(kThreads)
     }
     dot = block_sum(dot, smem);
     z = block_sum(z, smem);
-    if (threadIdx.x == 0) {
-        const float balance = live > 0.f ? (float)cols / live * dot : 0.f;
-        z = rows_all > 0.f ? z / rows_all : 0.f;
-        a.loss[0] = a.balance_scale * balance + a.z_scale * z;
-        a.loss[1] = balance;
-        a.loss[2] = z;
+    if (threadIdx.x == 0) store_loss(a, t, dot, z);
+}
+
+// Any width, stride and alignment.  A unit is `unit_rows` consecutive rows of one
+// group; a block takes every gridDim-th unit, a warp a row at a time.
+template <class T>
+__global__ void __launch_bounds__(kThreads)
+    balance_any_kernel(const __grid_constant__ BalanceArgs a, int64_t unit_rows) {
+    __shared__ float f[FASGD_EXPERTS_MAX];
+    __shared__ float smem[kThreads / 32];
+    constexpr int kWarps = kThreads / 32;
+    pdl_wait();
+    pdl_trigger();
+    const int cols = (int)a.cols, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Totals t = totals(a, smem);
+    const int64_t units_per_group = (a.group_rows + unit_rows - 1) / unit_rows;
+    float sum_dot = 0.f, sum_z = 0.f;
+    for (int64_t unit = blockIdx.x; unit < a.groups * units_per_group; unit += gridDim.x) {
+        const int64_t group = unit / units_per_group, part = unit - group * units_per_group;
+        const float inv_n = group_shares(a, group, part == 0, f);
+        const float scale = t.live > 0.f ? a.balance_scale * (float)cols / t.live * inv_n : 0.f;
+        const int64_t end = (part + 1) * unit_rows < a.group_rows ? (part + 1) * unit_rows : a.group_rows;
+        float unit_dot = 0.f;
+        for (int64_t i = part * unit_rows + warp; i < end; i += kWarps) {
+            const int64_t r = group * a.group_rows + i;
+            const T* x = static_cast<const T*>(a.logits) + r * a.ld_logits;
+            T* d = static_cast<T*>(a.dlogits) + r * a.ld_dlogits;
+            if (a.valid != nullptr && a.valid[r] == 0) {
+                if (a.dlogits != nullptr)
+                    for (int e = lane; e < cols; e += 32) d[e] = from_f32<T>(0.f);
+                continue;
+            }
+            float top = -INFINITY;
+            for (int e = lane; e < cols; e += 32) top = fmaxf(top, to_f32(x[e]));
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            if (top == -INFINITY) top = 0.f;         // no expert is open to this row: sum = 0 (or NaN)
+            float sum = 0.f, dot = 0.f;
+            for (int e = lane; e < cols; e += 32) {
+                const float p = __expf(to_f32(x[e]) - top);
+                sum += p;
+                dot += f[e] * p;
+            }
+            sum = warp_sum(sum);
+            dot = warp_sum(dot);
+            const float inv = sum == 0.f ? 0.f : 1.f / sum, lse = sum == 0.f ? 0.f : top + logf(sum);
+            dot *= inv;
+            unit_dot += dot;
+            sum_z += lse * lse;
+            const float k = t.up * inv, c = t.zscale * lse - scale * dot;
+            if (a.dlogits != nullptr)
+                for (int e = lane; e < cols; e += 32)
+                    d[e] = from_f32<T>(__expf(to_f32(x[e]) - top) * k * fmaf(scale, f[e], c));
+        }
+        sum_dot += unit_dot * inv_n;
     }
+    if (a.loss != nullptr) join_loss(a, t, lane == 0 ? sum_dot : 0.f, lane == 0 ? sum_z : 0.f, smem);
+}
+
+// Rows in octets (octet.cuh): LPR lanes hold a row, NV octets each, from its one
+// read to its gradient; 256 / LPR rows a block at a time (a multiple of 8), the
+// next ones' logits asked for before this one's are used.  ONE: a single block,
+// which counts for itself.
+template <class T, int LPR, int NV, bool RAGGED, bool ONE>
+__global__ void __launch_bounds__(kThreads)
+    balance_rows_kernel(const __grid_constant__ BalanceArgs a, int64_t unit_rows) {
+    constexpr int kSlots = kThreads / LPR, kP = kPieces<T>;
+    __shared__ float f[FASGD_EXPERTS_MAX];
+    __shared__ float smem[kThreads / 32];
+    const int slot = threadIdx.x / LPR, lane = threadIdx.x % LPR;
+    const int32_t cols = (int32_t)a.cols;
+    pdl_wait();
+    pdl_trigger();
+    Totals t;
+    if constexpr (ONE) {
+        int32_t* hist = reinterpret_cast<int32_t*>(f);
+        __shared__ int32_t rows_valid;
+        for (int e = threadIdx.x; e < cols; e += kThreads) hist[e] = 0;
+        if (threadIdx.x == 0) rows_valid = a.valid != nullptr ? 0 : (int32_t)a.rows;
+        __syncthreads();
+        count_rows(a, 0, a.rows, hist, &rows_valid);
+        __syncthreads();
+        for (int e = threadIdx.x; e < cols; e += kThreads) {
+            const int32_t c = hist[e];
+            a.counts[e] = c;
+            f[e] = rows_valid > 0 ? (float)c * (1.f / (float)rows_valid / (float)a.top) : 0.f;
+        }
+        t.rows = (float)rows_valid;
+        t.live = rows_valid > 0 ? 1.f : 0.f;
+        t.up = a.upstream != nullptr ? *a.upstream : 1.f;
+        t.zscale = t.rows > 0.f ? 2.f * a.z_scale / t.rows : 0.f;
+        __syncthreads();
+    } else {
+        t = totals(a, smem);
+    }
+    const int64_t units_per_group = (a.group_rows + unit_rows - 1) / unit_rows;
+    float sum_dot = 0.f, sum_z = 0.f;
+    for (int64_t unit = blockIdx.x; unit < a.groups * units_per_group; unit += gridDim.x) {
+        const int64_t group = unit / units_per_group, part = unit - group * units_per_group;
+        const float inv_n = ONE ? (t.rows > 0.f ? 1.f / t.rows : 0.f) : group_shares(a, group, part == 0, f);
+        const float scale = t.live > 0.f ? a.balance_scale * (float)cols / t.live * inv_n : 0.f;
+        const int64_t base = group * a.group_rows + part * unit_rows;
+        const int64_t rows = a.group_rows - part * unit_rows < unit_rows ? a.group_rows - part * unit_rows : unit_rows;
+        const int shift = RAGGED ? (int)(((base + slot) * a.cols) & 7) : 0;
+        Oct share[NV];
+        uint4 raw[NV][kP];
+        const T* x = static_cast<const T*>(a.logits) + (base + slot) * a.ld_logits;
+        T* d = static_cast<T*>(a.dlogits) + (base + slot) * a.ld_dlogits;
+        // The matrix's last row may end inside its last octet: that one is read value by value.
+        const auto fetch = [&](int64_t i) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const Columns c(lane + v * LPR, shift, cols);
+                if (i >= rows || !c.any()) continue;
+                if (!RAGGED || c.c0 + kOctet <= cols || base + i < a.rows - 1) {
+                    load_pieces(x + c.c0, raw[v]);
+                } else {
+                    Oct o = {};
+#pragma unroll
+                    for (int k = 0; k < kOctet; ++k)
+                        if (c.in >> k & 1) element(o, k) = to_f32(x[c.c0 + k]);
+                    pack<T>(o, raw[v]);
+                }
+            }
+            x += kSlots * a.ld_logits;
+        };
+        fetch(slot);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) share[v] = load_vector(f, Columns(lane + v * LPR, shift, cols), 0.f);
+        float unit_dot = 0.f;
+        // A warp goes on until the first of its rows is past the end.
+        for (int64_t i = slot, ahead = slot - slot % (32 / LPR); ahead < rows; i += kSlots, ahead += kSlots) {
+            Oct e[NV];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const Columns c(lane + v * LPR, shift, cols);
+                e[v] = unpack<T>(raw[v]);
+                if (RAGGED ? !c.whole() : !c.any()) {
+#pragma unroll
+                    for (int k = 0; k < kOctet; ++k)
+                        if (!(c.in >> k & 1)) element(e[v], k) = -INFINITY;
+                }
+            }
+            fetch(i + kSlots);
+            const bool live = i < rows && (a.valid == nullptr || a.valid[base + i] != 0);
+            float top = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(e[v].v[k].x, e[v].v[k].y));
+#pragma unroll
+            for (int off = LPR / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            if (top == -INFINITY) top = 0.f;         // no expert is open to this row: sum = 0 (or NaN)
+            float2 s2 = f2(0.f), d2 = f2(0.f);
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float2& p = e[v].v[k];
+                    p = add2(p, f2(-top));
+                    p = make_float2(__expf(p.x), __expf(p.y));
+                    s2 = add2(s2, p);
+                    d2 = fma2(share[v].v[k], p, d2);
+                }
+            float sum = s2.x + s2.y, dot = d2.x + d2.y;
+#pragma unroll
+            for (int off = LPR / 2; off > 0; off >>= 1) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                dot += __shfl_xor_sync(0xffffffffu, dot, off);
+            }
+            const float inv = sum == 0.f ? 0.f : 1.f / sum, lse = sum == 0.f ? 0.f : top + logf(sum);
+            dot *= inv;
+            if (live) {
+                unit_dot += dot;
+                sum_z += lse * lse;
+            }
+            if (a.dlogits != nullptr) {
+                const float k1 = t.up * inv, c1 = t.zscale * lse - scale * dot;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const Columns c(lane + v * LPR, shift, cols);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float2 g = mul2(mul2(e[v].v[k], f2(k1)), fma2(f2(scale), share[v].v[k], f2(c1)));
+                        e[v].v[k] = live ? g : f2(0.f);
+                    }
+                    if (i < rows) store_octet<T, RAGGED>(d + c.c0, c, e[v]);
+                }
+                d += kSlots * a.ld_dlogits;
+            }
+        }
+        sum_dot += unit_dot * inv_n;
+    }
+    if (a.loss != nullptr) join_loss(a, t, lane == 0 ? sum_dot : 0.f, lane == 0 ? sum_z : 0.f, smem);
 }
 
 __global__ void balance_nothing_kernel(const __grid_constant__ BalanceArgs a) {
@@ -197,12 +384,67 @@ __global__ void balance_nothing_kernel(const __grid_constant__ BalanceArgs a) {
     if (t < 3 && a.loss != nullptr) a.loss[t] = 0.f;
 }
 
+// Whether one block does it all, `slots` rows at a time, in one launch: four turns
+// of one group, whose assignments it counts in as few.
+bool balance_alone(const BalanceArgs& a, int slots) {
+    return a.groups == 1 && a.rows <= 4 * slots && a.rows * a.top <= 4 * 8 * kThreads;
+}
+// `unit_rows` rows of a group to a unit: at most `cap` units where the groups allow it.
+int64_t rows_of_units(const BalanceArgs& a, int64_t cap, int64_t multiple) {
+    int64_t rows = (a.rows + cap - 1) / cap;
+    rows = (rows + multiple - 1) / multiple * multiple;
+    return rows < a.group_rows ? rows : a.group_rows;
+}
+template <class T, int LPR, int NV, bool RAGGED>
+cudaError_t launch_rows(const BalanceArgs& a, int num_sms, cudaStream_t stream) {
+    constexpr int kSlots = kThreads / LPR;
+    if (balance_alone(a, kSlots))
+        return launch_pdl(balance_rows_kernel<T, LPR, NV, RAGGED, true>, 1, kThreads, 0, stream, a, a.rows);
+    const int64_t cap = (int64_t)num_sms * (NV > 2 ? 2 : 4);
+    const int64_t unit_rows = rows_of_units(a, cap, kSlots);
+    const int64_t units = a.groups * ((a.group_rows + unit_rows - 1) / unit_rows);
+    return launch_pdl(balance_rows_kernel<T, LPR, NV, RAGGED, false>, (unsigned)(units < cap ? units : cap), kThreads,
+                      0, stream, a, unit_rows);
+}
+template <class T, bool RAGGED>
+cudaError_t launch_octets(const BalanceArgs& a, int64_t octets, int num_sms, cudaStream_t stream) {
+    if (octets <= 1) return launch_rows<T, 1, 1, RAGGED>(a, num_sms, stream);
+    if (octets <= 2) return launch_rows<T, 1, 2, RAGGED>(a, num_sms, stream);
+    if (octets <= 4) return launch_rows<T, 2, 2, RAGGED>(a, num_sms, stream);
+    if (octets <= 8) return launch_rows<T, 4, 2, RAGGED>(a, num_sms, stream);
+    if (octets <= 16) return launch_rows<T, 8, 2, RAGGED>(a, num_sms, stream);
+    if (octets <= 32) return launch_rows<T, 16, 2, RAGGED>(a, num_sms, stream);
+    if (octets <= 64) return launch_rows<T, 32, 2, RAGGED>(a, num_sms, stream);
+    return launch_rows<T, 32, 4, RAGGED>(a, num_sms, stream);
+}
+constexpr int64_t kOctetsMost = 128;
+
+int lanes_per_row(int64_t octets) {
+    int lanes = 1;
+    while (lanes * 2 < octets && lanes < 32) lanes *= 2;
+    return lanes;
+}
+bool in_octets(const BalanceArgs& a, int size) {
+    return row_octets(a.cols) <= kOctetsMost && octet_matrix(a.logits, a.ld_logits, a.rows, a.cols, size) &&
+           octet_matrix(a.dlogits, a.ld_dlogits, a.rows, a.cols, size);
+}
+
 template <class T>
 cudaError_t launch(const BalanceArgs& a, int num_sms, cudaStream_t stream) {
+    const int64_t octets = row_octets(a.cols);
+    const bool fast = in_octets(a, (int)sizeof(T));
+    if (!(fast && balance_alone(a, kThreads / lanes_per_row(octets)))) {
+        const int blocks = a.splits > 1 ? kCountCluster : 1;
+        const int64_t units = a.groups * a.splits, cap = (int64_t)num_sms * 4 / blocks;
+        const cudaError_t st = launch_rows_kernel(balance_count_kernel, (units < cap ? units : cap) * blocks,
+                                                  kCountThreads, 0, blocks, stream, a, blocks);
+        if (st != cudaSuccess) return st;
+    }
+    if (fast)
+        return a.cols % kOctet != 0 ? launch_octets<T, true>(a, octets, num_sms, stream)
+                                    : launch_octets<T, false>(a, octets, num_sms, stream);
     const int64_t cap = (int64_t)num_sms * 8 < kBalanceParts ? (int64_t)num_sms * 8 : kBalanceParts;
-    int64_t unit_rows = (a.rows + cap - 1) / cap;
-    unit_rows = (unit_rows + 7) / 8 * 8;
-    if (unit_rows > a.group_rows) unit_rows = a.group_rows;
+    const int64_t unit_rows = rows_of_units(a, cap, 8);
     const int64_t units = a.groups * ((a.group_rows + unit_rows - 1) / unit_rows);
     return launch_pdl(balance_any_kernel<T>, (unsigned)(units < cap ? units : cap), kThreads, 0, stream, a,
                       unit_rows);
@@ -210,20 +452,17 @@ cudaError_t launch(const BalanceArgs& a, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
-// Parts of each group in the counting: 32,768 assignments each, 64 at most (every
-// block of the pass adds up its group's).
+// Parts of each group in the counting, 16 at most (every block of the pass adds up
+// its group's): one for up to 16,384 assignments, which a block counts, else one
+// for each 131,072, which a cluster does.
 int64_t balance_splits(int64_t rows, int64_t groups, int64_t top) {
     if (groups < 1) return 1;
-    const int64_t n = rows / groups * top, s = (n + 32767) / 32768;
-    return s < 1 ? 1 : s > 64 ? 64 : s;
+    const int64_t n = rows / groups * top, s = (n + 131071) / 131072 + 1;
+    return n <= 16384 ? 1 : s > 16 ? 16 : s;
 }
 
 cudaError_t launch_balance(const BalanceArgs& a, int dtype, int num_sms, cudaStream_t stream) {
     if (a.rows == 0) return launch_pdl(balance_nothing_kernel, 32, kThreads, 0, stream, a);
-    const int64_t units = a.groups * a.splits, cap = (int64_t)num_sms * 4;
-    const cudaError_t st = launch_pdl(balance_count_kernel, (unsigned)(units < cap ? units : cap),
-                                      kCountThreads, 0, stream, a);
-    if (st != cudaSuccess) return st;
     if (dtype == FASGD_F32) return launch<float>(a, num_sms, stream);
     if (dtype == FASGD_BF16) return launch<__nv_bfloat16>(a, num_sms, stream);
     return launch<__half>(a, num_sms, stream);

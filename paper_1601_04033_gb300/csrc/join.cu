@@ -101,8 +101,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : kForwardT
     uint4* const mine = ring + (threadIdx.x >> 5) * kSlots;
     const int stage_size = kSlots * th.warps;
     if (!c.any())
-        for (int i = 0; i < STAGES; ++i)
-            for (int k = 0; k < kSlots; k += kLane) mine[i * stage_size + k + (threadIdx.x & 31)] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < STAGES; ++i) clear_octets<T>(mine + i * stage_size, 2 * NR);
     __syncwarp();
     pdl_wait();
     pdl_trigger();

@@ -208,8 +208,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     uint4* const own_stats = ring + STAGES * stage_size + (threadIdx.x >> 5) * kWarpRows + (TPR == 8 ? th.sub : 0);
     const bool asks = (threadIdx.x & (TPR == 8 ? 7 : 31)) == 0;
     if (!c.any())
-        for (int i = 0; i < STAGES; ++i)
-            for (int k = 0; k < kSlots; k += kLane) own[i * stage_size + k + (threadIdx.x & 31)] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < STAGES; ++i) clear_octets<T>(own + i * stage_size, 4);
     __syncwarp();
     const CopyLane<T, TPR == 8 ? 8 : 32> lane(c, (int32_t)a.cols);
     pdl_wait();

@@ -166,7 +166,10 @@ struct CopyLane {
     __device__ CopyLane(const Columns& c, int32_t cols_) : cols(cols_), in(0) {
         const int lane = threadIdx.x & 31, of_row = lane % W;
         col = __shfl_sync(0xffffffffu, c.c0, 0, W) + of_row * kPer;
-        place = kPieces<T> == 1 ? lane : (of_row & 1) * kLane + lane - of_row + (of_row >> 1);
+        // Its octet's lane owns it; the second pieces lie four places off, so that the
+        // copies of eight neighbours fall into all banks.
+        const int owner = lane - of_row + (of_row >> 1);
+        place = kPieces<T> == 1 ? lane : (of_row & 1) ? kLane + (owner ^ 4) : owner;
 #pragma unroll
         for (int k = 0; k < kPieces<T>; ++k)
             if (col + k * kStep + kPer > 0 && col + k * kStep < cols) in |= 1u << k;
@@ -177,7 +180,7 @@ struct CopyLane {
 #pragma unroll
         for (int k = 0; k < kPieces<T>; ++k) {
             if (!(in >> k & 1)) continue;
-            uint4* to = slot + place + k * (W / 2);
+            uint4* to = slot + (W == 8 ? place ^ (4 * k) : place + k * (W / 2));
             if (!clip) {
                 copy_async16(to, p + k * kStep, 16);
             } else {
@@ -187,12 +190,18 @@ struct CopyLane {
         }
     }
 };
+// Zeros in the places of an octet that nobody copies, of `count` matrices.
+template <class T>
+__device__ __forceinline__ void clear_octets(uint4* slot, int count) {
+    for (int i = 0; i < count * kPieces<T>; ++i)
+        slot[i * kLane + ((threadIdx.x & 31) ^ (4 * (i % kPieces<T>)))] = make_uint4(0, 0, 0, 0);
+}
 // slot: the warp's place of a matrix.
 template <class T, bool RAGGED>
 __device__ __forceinline__ Oct take_octet(const uint4* slot, const Columns& c) {
     uint4 raw[kPieces<T>];
 #pragma unroll
-    for (int k = 0; k < kPieces<T>; ++k) raw[k] = slot[k * kLane + (threadIdx.x & 31)];
+    for (int k = 0; k < kPieces<T>; ++k) raw[k] = slot[k * kLane + ((threadIdx.x & 31) ^ (4 * k))];
     Oct o = unpack<T>(raw);
     if (RAGGED) mask(o, c);
     return o;
