@@ -79,41 +79,88 @@ def _rows(t):
     return t.data_ptr() or _NOWHERE, rows, cols, step
 
 
-def _like(t, like):
-    """(address, ld) of a matrix of like's shape and type."""
-    if t.shape != like.shape or t.dtype is not like.dtype:
-        raise ValueError(f"{tuple(t.shape)} {t.dtype} given with {tuple(like.shape)} {like.dtype}")
-    p, _, _, step = _rows(t)
-    return p, step
+# The tensors of a call go into its argument struct by kind: the first matrix,
+# which fixes rows, cols and dtype; matrices of its shape and type; fp32 vectors of
+# cols values; and a gate, [cols] or [groups, cols] of fp32 or the first's type.
+_FIRST, _LIKE, _VECTOR, _GATE = range(4)
 
 
-def _new(like, cols):
-    """A new matrix of like's shape and type, without gaps: (tensor, address, ld)."""
-    t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
-    return t, t.data_ptr() or _NOWHERE, cols
+class _Spec:
+    """Where a struct's tensors go: "kind pointer" words in the order of intake's."""
+
+    def __init__(self, struct, **kinds):
+        def off(name):
+            f = getattr(struct, name, None)
+            return 0xFFFF if f is None else f.offset
+        self.fields = [(kind, name) for name, kind in kinds.items()]
+        words = [off("rows"), off("cols"), off("dtype"), off("groups") if struct is _f.JoinArgs else 0xFFFF,
+                 off("gate_dtype")]
+        for kind, name in self.fields:
+            words += [kind, off(name), off("ld_" + name)]
+        self.words = b"".join(w.to_bytes(2, "little") for w in words)
 
 
-def _vector(t, cols: int, name: str):
-    if t.dtype is not torch.float32 or t.numel() != cols or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name} must be {cols} contiguous fp32 values on the GPU")
-    return t.data_ptr()
+def _intake(a, spec, *tensors):
+    """Each tensor that is not None into struct a (its pointer, its ld, and what
+    the first and the gate fix); ValueError where one is not what its kind says."""
+    cols = None
+    if hasattr(a, "gate_dtype"):
+        a.groups = 1
+    for (kind, name), t in zip(spec.fields, tensors):
+        if t is None:
+            continue
+        p, rows, width, step = _rows(t)
+        if kind == _FIRST:
+            first, cols = t, width
+            a.rows, a.cols, a.dtype = rows, width, _dtype(t)
+        elif kind == _LIKE:
+            if cols is not None and (t.shape != first.shape or t.dtype is not first.dtype):
+                raise ValueError("matrices of one shape and type are expected")
+        elif kind == _VECTOR:
+            if t.dtype is not torch.float32 or t.numel() != (a.cols if cols is None else cols) or not t.is_contiguous():
+                raise ValueError("parameters are contiguous fp32 vectors of cols values")
+        else:
+            if width != cols or t.dim() > 2 or not t.is_contiguous():
+                raise ValueError("a gate is contiguous, [cols] or [groups, cols]")
+            if t.dim() == 2:
+                a.groups = rows
+            a.gate_dtype = _dtype(t)
+        setattr(a, name, p)
+        if kind <= _LIKE:
+            setattr(a, "ld_" + name, step)
+
+
+if getattr(_f._binding, "intake", None) is not None:
+    _f._binding.intake_types(torch.float32, torch.bfloat16, torch.float16)
+    _fast_intake = _f._binding.intake
+
+    def _take(a, at, spec, *tensors):
+        _fast_intake(at, spec.words, *tensors)
+else:
+    def _take(a, at, spec, *tensors):
+        _intake(a, spec, *tensors)
+
+
+def _new(like):
+    """A new matrix of like's shape and type, without gaps."""
+    if like.is_contiguous():
+        return torch.empty_like(like)
+    return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+
+
+_DROPOUT = _Spec(_f.DropoutArgs, x=_FIRST, out=_LIKE, residual=_LIKE)
 
 
 def dropout(x, draws: Draws, *, residual=None, out=None):
     """residual + dropout(x) (fasgd_dropout), in a new tensor or in `out`, which may
     be x or residual.  The gradient of x is dropout(gradient, draws)."""
     a = _f.DropoutArgs()
-    a.x, a.rows, cols, a.ld_x = _rows(x)
-    a.cols = cols
-    a.dtype = _dtype(x)
-    if residual is not None:
-        a.residual, a.ld_residual = _like(residual, x)
+    at = ctypes.addressof(a)
     if out is None:
-        out, a.out, a.ld_out = _new(x, cols)
-    else:
-        a.out, a.ld_out = _like(out, x)
+        out = _new(x)
+    _take(a, at, _DROPOUT, x, out, residual)
     a.rate, a.seed, a.client, a.n = draws
-    _check(_f.fasgd_dropout(ctypes.addressof(a), _stream(x)))
+    _check(_f.fasgd_dropout(at, _stream(x)))
     return out
 
 
@@ -123,55 +170,34 @@ class Joined:
     __slots__ = ("h", "z", "args", "x", "y", "parameters", "stats")
 
 
+_JOIN = _Spec(_f.JoinArgs, x=_FIRST, y=_LIKE, h=_LIKE, z=_LIKE, post=_VECTOR, post_bias=_VECTOR, gate=_GATE,
+              pre=_VECTOR, pre_bias=_VECTOR)
+
+
 def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=None, norm="rms",
          eps=1e-6, carry=1.0, branch=1.0, draws: Draws | None = None, h=None, z=None) -> Joined:
     """fasgd_join: h = carry x + branch gate dropout(N(y; post)), z = N(h; pre).
     gate: fp32 [cols], or [groups, cols] of fp32 or x's type, groups dividing the
     rows.  h, z: where to write them (new tensors if None)."""
+    if (h is not None and y is None) or (z is not None and pre is None):
+        raise ValueError("h goes with y, z with pre")
+    if y is not None and h is None:
+        h = _new(x)
+    if pre is not None and z is None:
+        z = _new(x)
     j = Joined()
     a = j.args = _f.JoinArgs()
-    a.x, rows, cols, a.ld_x = _rows(x)
-    a.rows = rows
-    a.cols = cols
-    a.groups = 1
-    a.dtype = _dtype(x)
+    at = ctypes.addressof(a)
+    _take(a, at, _JOIN, x, y, h, z, post, post_bias, gate, pre, pre_bias)
     a.norm = _NORMS[norm]
     a.eps = eps
     a.carry = carry
     a.branch = branch
     if draws is not None:
         a.rate, a.seed, a.client, a.n = draws
-    if y is not None:
-        a.y, a.ld_y = _like(y, x)
-        if h is None:
-            h, a.h, a.ld_h = _new(x, cols)
-        else:
-            a.h, a.ld_h = _like(h, x)
-    elif h is not None:
-        raise ValueError("h goes with y")
-    if pre is not None:
-        a.pre = _vector(pre, cols, "pre")
-        if z is None:
-            z, a.z, a.ld_z = _new(x, cols)
-        else:
-            a.z, a.ld_z = _like(z, x)
-    elif z is not None:
-        raise ValueError("z goes with pre")
-    if post is not None:
-        a.post = _vector(post, cols, "post")
-    if post_bias is not None:
-        a.post_bias = _vector(post_bias, cols, "post_bias")
-    if pre_bias is not None:
-        a.pre_bias = _vector(pre_bias, cols, "pre_bias")
-    if gate is not None:
-        if gate.dim() == 2:
-            a.groups = gate.shape[0]
-        if gate.shape[-1] != cols or gate.dim() > 2 or not gate.is_contiguous() or not gate.is_cuda:
-            raise ValueError("gate must be contiguous [cols] or [groups, cols] on the GPU")
-        a.gate, a.gate_dtype = gate.data_ptr(), _dtype(gate)
-    j.stats = torch.empty(4 * rows, dtype=torch.float32, device=x.device)
+    j.stats = torch.empty(4 * a.rows, dtype=torch.float32, device=x.device)
     a.stats = j.stats.data_ptr() or _NOWHERE
-    _check(_f.fasgd_join(ctypes.addressof(a), _stream(x)))
+    _check(_f.fasgd_join(at, _stream(x)))
     j.h, j.z, j.x, j.y = h, z, x, y
     j.parameters = (post, post_bias, gate, pre, pre_bias)
     return j
@@ -192,38 +218,32 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
     of its h (None: zero) and z.  x, y, the parameters and the stream's order are
     to be as they were.  into: where to write them (new tensors where None)."""
     a, x = _f.JoinArgs.from_buffer_copy(j.args), j.x
-    cols = a.cols
+    at = ctypes.addressof(a)
     dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias = into if into is not None else _NO_GRADS
     post, post_bias, gate, pre, pre_bias = j.parameters
-    if dh is not None:
-        a.dh, a.ld_dh = _like(dh, x)
-    if dz is not None:
-        a.dz, a.ld_dz = _like(dz, x)
     if dx is None:
-        dx, a.dx, a.ld_dx = _new(x, cols)
-    else:
-        a.dx, a.ld_dx = _like(dx, x)
+        dx = _new(x)
     if j.y is None:
         dy = None
     elif dy is None:
-        dy, a.dy, a.ld_dy = _new(x, cols)
-    else:
-        a.dy, a.ld_dy = _like(dy, x)
-    if post is not None:
-        dpost, a.dpost = _grad_vector(dpost, post, cols)
-    if post_bias is not None:
-        dpost_bias, a.dpost_bias = _grad_vector(dpost_bias, post_bias, cols)
-    if pre is not None:
-        dpre, a.dpre = _grad_vector(dpre, pre, cols)
-    if pre_bias is not None:
-        dpre_bias, a.dpre_bias = _grad_vector(dpre_bias, pre_bias, cols)
+        dy = _new(x)
+    if post is not None and dpost is None:
+        dpost = torch.empty_like(post)
+    if post_bias is not None and dpost_bias is None:
+        dpost_bias = torch.empty_like(post_bias)
+    if pre is not None and dpre is None:
+        dpre = torch.empty_like(pre)
+    if pre_bias is not None and dpre_bias is None:
+        dpre_bias = torch.empty_like(pre_bias)
     if gate is not None:
         if dgate is None:
             dgate = torch.empty_like(gate)
         elif dgate.shape != gate.shape or dgate.dtype is not gate.dtype or not dgate.is_contiguous():
             raise ValueError("the gate's gradient must be as the gate")
         a.dgate = dgate.data_ptr()
-    at = ctypes.addressof(a)
+    groups = a.groups
+    _take(a, at, _JOIN_GRAD, x, dh, dz, dx, dy, dpost, dpost_bias, dpre, dpre_bias)
+    a.groups = groups
     size = _check(_f.fasgd_join_workspace(at))
     space = torch.empty(size, dtype=torch.uint8, device=x.device)
     a.workspace = space.data_ptr()
@@ -233,13 +253,8 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
 
 
 _NO_GRADS = JoinGrads()
-
-
-def _grad_vector(t, of, cols):
-    if t is None:
-        t = torch.empty_like(of)
-        return t, t.data_ptr()
-    return t, _vector(t, cols, "a parameter's gradient")
+_JOIN_GRAD = _Spec(_f.JoinArgs, x=_FIRST, dh=_LIKE, dz=_LIKE, dx=_LIKE, dy=_LIKE, dpost=_VECTOR, dpost_bias=_VECTOR,
+                   dpre=_VECTOR, dpre_bias=_VECTOR)
 
 
 class Balance(NamedTuple):
@@ -248,15 +263,20 @@ class Balance(NamedTuple):
     dlogits: object    # as logits, or None
 
 
+_BALANCE = _Spec(_f.BalanceArgs, logits=_FIRST, dlogits=_LIKE)
+
+
 def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstream=None, grad=True) -> Balance:
     """fasgd_balance: a router's balance and z losses, its per-expert counts, and
     (grad) the gradient of the logits, times `upstream` (a device fp32 value) if
     given.  chosen: int32 [..., top]; valid: bool or uint8, one per row."""
     a = _f.BalanceArgs()
-    a.logits, rows, cols, a.ld_logits = _rows(logits)
-    a.rows, a.cols, a.groups, top = rows, cols, groups, chosen.shape[-1]
-    a.top = top
-    a.dtype = _dtype(logits)
+    at = ctypes.addressof(a)
+    dlogits = _new(logits) if grad else None
+    _take(a, at, _BALANCE, logits, dlogits)
+    rows = a.rows
+    a.groups = groups
+    a.top = top = chosen.shape[-1]
     a.balance_scale = balance
     a.z_scale = z
     if chosen.dtype is not torch.int32 or not chosen.is_contiguous() or not chosen.is_cuda or \
@@ -269,14 +289,12 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
             raise ValueError("valid must be contiguous bool or uint8 on the GPU, one for each row")
         a.valid = valid.data_ptr()
     if upstream is not None:
-        a.upstream = _vector(upstream, 1, "upstream")
-    at = ctypes.addressof(a)
+        if upstream.dtype is not torch.float32 or upstream.numel() != 1 or not upstream.is_cuda:
+            raise ValueError("upstream must be one fp32 value on the GPU")
+        a.upstream = upstream.data_ptr()
     size = _check(_f.fasgd_balance_workspace(at))
-    dlogits = None
-    if grad:
-        dlogits, a.dlogits, a.ld_dlogits = _new(logits, cols)
     device = logits.device
-    counts = torch.empty((groups, cols), dtype=torch.int32, device=device)
+    counts = torch.empty((groups, a.cols), dtype=torch.int32, device=device)
     loss = torch.empty(3, dtype=torch.float32, device=device)
     space = torch.empty(size, dtype=torch.uint8, device=device)
     a.counts = counts.data_ptr()

@@ -11,16 +11,16 @@
 namespace fasgd {
 namespace {
 
-constexpr int kCountThreads = 512;
+constexpr int kCountThreads = 1024;
 constexpr int kCountCluster = 8;        // blocks that count one split together
 constexpr int kThreads = 256;
 
 // Adds the assignments of rows r0 .. r1 to `hist`, and the rows that take part to
 // `rows_valid`, both in shared memory (integers: no order shows).  U entries a
 // thread are asked for before the first is counted.
+template <int U>
 __device__ __forceinline__ void count_rows(const BalanceArgs& a, int64_t r0, int64_t r1, int32_t* hist,
                                            int32_t* rows_valid) {
-    constexpr int U = 8;
     const uint32_t top = (uint32_t)a.top, cols = (uint32_t)a.cols, threads = blockDim.x;
     if (a.valid != nullptr) {
         int32_t v = 0;
@@ -28,14 +28,19 @@ __device__ __forceinline__ void count_rows(const BalanceArgs& a, int64_t r0, int
         v = __reduce_add_sync(0xffffffffu, v);
         if ((threadIdx.x & 31) == 0 && v != 0) atomicAdd(rows_valid, v);
     }
-    const int64_t i1 = r1 * a.top;
-    for (int64_t i = r0 * a.top + threadIdx.x; i < i1; i += (int64_t)threads * U) {
+    const int32_t* chosen = a.chosen + r0 * a.top;
+    const uint8_t* valid = a.valid + r0;
+    const uint32_t count = (uint32_t)((r1 - r0) * a.top);
+    for (uint32_t i = threadIdx.x; i < count; i += threads * U) {
         int32_t e[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t k = i + (int64_t)u * threads;
-            e[u] = k < i1 ? a.chosen[k] : -1;
-            if (a.valid != nullptr && k < i1 && a.valid[(uint32_t)k / top] == 0) e[u] = -1;
+            const uint32_t k = i + u * threads;
+            e[u] = -1;
+            if (k < count) {
+                e[u] = chosen[k];
+                if (a.valid != nullptr && valid[k / top] == 0) e[u] = -1;
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -61,7 +66,7 @@ __global__ void __launch_bounds__(kCountThreads)
         for (int e = threadIdx.x; e <= cols; e += kCountThreads) hist[e] = 0;
         __syncthreads();
         if (a.valid == nullptr && threadIdx.x == 0) hist[cols] = (int32_t)(to - from);
-        count_rows(a, group * a.group_rows + from, group * a.group_rows + to, hist, &hist[cols]);
+        count_rows<16>(a, group * a.group_rows + from, group * a.group_rows + to, hist, &hist[cols]);
         __syncthreads();
         int32_t* out = a.splits > 1 ? a.part_counts + unit * cols : a.counts + group * cols;
         if (blocks == 1) {
@@ -72,40 +77,50 @@ __global__ void __launch_bounds__(kCountThreads)
         }
         cluster_barrier();
         for (int e = rank * kCountThreads + threadIdx.x; e <= cols; e += blocks * kCountThreads) {
-            int32_t s = 0;
-            for (int k = 0; k < blocks; ++k) {
+            int32_t s = 0, v[kCountCluster];
+#pragma unroll
+            for (int k = 0; k < kCountCluster; ++k) {
                 uint32_t there;
-                int32_t v;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
                              : "=r"(there)
                              : "r"((uint32_t)__cvta_generic_to_shared(&hist[e])), "r"(k));
-                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
-                s += v;
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v[k]) : "r"(there) : "memory");
             }
+#pragma unroll
+            for (int k = 0; k < kCountCluster; ++k) s += v[k];
             *(e < cols ? out + e : a.part_valid + unit) = s;
         }
         cluster_barrier();       // before a block's counts are cleared, or it ends
     }
 }
 
-// Sum of one value over the block, every thread ending with it.
-__device__ __forceinline__ float block_sum(float v, float* smem) {
-    v = warp_sum(v);
+// Sums of two values over the block, every thread ending with them.
+__device__ __forceinline__ float2 block_sum2(float2 v, float2* smem) {
+    v.x = warp_sum(v.x);
+    v.y = warp_sum(v.y);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) smem[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = 0.f;
+    v = smem[0];
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) v += smem[w];
+    for (int w = 1; w < kThreads / 32; ++w) v = add2(v, smem[w]);
     return v;
 }
+
+// exp(x) for x <= 0, to a few ulp; 0 where it would be subnormal.
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
 
 // What every block of the pass knows: N and G' (as floats), and the factors made
 // of them.
 struct Totals {
     float rows, live, zscale, up;
 };
-__device__ __forceinline__ Totals totals(const BalanceArgs& a, float* smem) {
+__device__ __forceinline__ Totals totals(const BalanceArgs& a, float2* smem) {
     Totals t;
     t.rows = (float)a.rows;
     t.live = (float)a.groups;
@@ -117,8 +132,9 @@ __device__ __forceinline__ Totals totals(const BalanceArgs& a, float* smem) {
             n += (float)v;
             g1 += v > 0 ? 1.f : 0.f;
         }
-        t.rows = block_sum(n, smem);
-        t.live = block_sum(g1, smem);
+        const float2 s = block_sum2(make_float2(n, g1), smem);
+        t.rows = s.x;
+        t.live = s.y;
     }
     t.up = a.upstream != nullptr ? *a.upstream : 1.f;
     t.zscale = t.rows > 0.f ? 2.f * a.z_scale / t.rows : 0.f;
@@ -155,31 +171,25 @@ __device__ __forceinline__ void store_loss(const BalanceArgs& a, const Totals& t
 }
 // The losses of the blocks' sums: the block that leaves its own last adds them up,
 // in the blocks' order.
-__device__ __forceinline__ void join_loss(const BalanceArgs& a, const Totals& t, float dot, float z, float* smem) {
+__device__ __forceinline__ void join_loss(const BalanceArgs& a, const Totals& t, float dot, float z, float2* smem) {
     __shared__ bool last;
-    dot = block_sum(dot, smem);
-    z = block_sum(z, smem);
+    float2 s = block_sum2(make_float2(dot, z), smem);
     if (gridDim.x == 1) {
-        if (threadIdx.x == 0) store_loss(a, t, dot, z);
+        if (threadIdx.x == 0) store_loss(a, t, s.x, s.y);
         return;
     }
     if (threadIdx.x == 0) {
-        a.part_loss[blockIdx.x] = make_float2(dot, z);
-        __threadfence();
-        last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+        a.part_loss[blockIdx.x] = s;
+        uint32_t before;                // releases this sum, acquires the others'
+        asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.ticket) : "memory");
+        last = before == gridDim.x - 1;
     }
     __syncthreads();
     if (!last) return;
-    __threadfence();
-    dot = z = 0.f;
-    for (int b = threadIdx.x; b < (int)gridDim.x; b += kThreads) {
-        const float2 v = __ldcg(&a.part_loss[b]);
-        dot += v.x;
-        z += v.y;
-    }
-    dot = block_sum(dot, smem);
-    z = block_sum(z, smem);
-    if (threadIdx.x == 0) store_loss(a, t, dot, z);
+    s = f2(0.f);
+    for (int b = threadIdx.x; b < (int)gridDim.x; b += kThreads) s = add2(s, __ldcg(&a.part_loss[b]));
+    s = block_sum2(s, smem);
+    if (threadIdx.x == 0) store_loss(a, t, s.x, s.y);
 }
 
 // Any width, stride and alignment.  A unit is `unit_rows` consecutive rows of one
@@ -188,7 +198,7 @@ template <class T>
 __global__ void __launch_bounds__(kThreads)
     balance_any_kernel(const __grid_constant__ BalanceArgs a, int64_t unit_rows) {
     __shared__ float f[FASGD_EXPERTS_MAX];
-    __shared__ float smem[kThreads / 32];
+    __shared__ float2 smem[kThreads / 32];
     constexpr int kWarps = kThreads / 32;
     pdl_wait();
     pdl_trigger();
@@ -218,7 +228,7 @@ __global__ void __launch_bounds__(kThreads)
             if (top == -INFINITY) top = 0.f;         // no expert is open to this row: sum = 0 (or NaN)
             float sum = 0.f, dot = 0.f;
             for (int e = lane; e < cols; e += 32) {
-                const float p = __expf(to_f32(x[e]) - top);
+                const float p = exp2_of((to_f32(x[e]) - top) * kLog2e);
                 sum += p;
                 dot += f[e] * p;
             }
@@ -231,7 +241,7 @@ __global__ void __launch_bounds__(kThreads)
             const float k = t.up * inv, c = t.zscale * lse - scale * dot;
             if (a.dlogits != nullptr)
                 for (int e = lane; e < cols; e += 32)
-                    d[e] = from_f32<T>(__expf(to_f32(x[e]) - top) * k * fmaf(scale, f[e], c));
+                    d[e] = from_f32<T>(exp2_of((to_f32(x[e]) - top) * kLog2e) * k * fmaf(scale, f[e], c));
         }
         sum_dot += unit_dot * inv_n;
     }
@@ -243,15 +253,54 @@ __global__ void __launch_bounds__(kThreads)
 // next ones' logits asked for before this one's are used.  ONE: a single block,
 // which counts for itself.
 template <class T, int LPR, int NV, bool RAGGED, bool ONE>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, NV > 2 ? 2 : 3)
     balance_rows_kernel(const __grid_constant__ BalanceArgs a, int64_t unit_rows) {
     constexpr int kSlots = kThreads / LPR, kP = kPieces<T>;
-    __shared__ float f[FASGD_EXPERTS_MAX];
-    __shared__ float smem[kThreads / 32];
+    __shared__ __align__(16) float f[FASGD_EXPERTS_MAX];
+    __shared__ float2 smem[kThreads / 32];
     const int slot = threadIdx.x / LPR, lane = threadIdx.x % LPR;
     const int32_t cols = (int32_t)a.cols;
     pdl_wait();
     pdl_trigger();
+    const int64_t units_per_group = (a.group_rows + unit_rows - 1) / unit_rows;
+    // The unit's rows base .. base + rows, and its logits on their way: asked for
+    // before the counts that it takes to use them.
+    int64_t base = 0;
+    int32_t rows = 0;
+    Columns c[NV];
+    uint4 raw[NV][kP];
+    const T* x = nullptr;
+    const int64_t step_x = kSlots * a.ld_logits, step_d = kSlots * a.ld_dlogits;
+    // The matrix's last row may end inside its last octet: that one is read value by value.
+    const auto fetch = [&](int32_t i) {
+        if (i < rows) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if (!c[v].any()) continue;
+                if (!RAGGED || c[v].c0 + kOctet <= cols || base + i < a.rows - 1) {
+                    load_pieces(x + v * (LPR * kOctet), raw[v]);
+                } else {
+                    Oct o = {};
+#pragma unroll
+                    for (int k = 0; k < kOctet; ++k)
+                        if (c[v].in >> k & 1) element(o, k) = to_f32(x[v * (LPR * kOctet) + k]);
+                    pack<T>(o, raw[v]);
+                }
+            }
+        }
+        x += step_x;
+    };
+    const auto begin = [&](int64_t unit) {
+        const int64_t group = unit / units_per_group, part = unit - group * units_per_group;
+        base = group * a.group_rows + part * unit_rows;
+        rows = (int32_t)(a.group_rows - part * unit_rows < unit_rows ? a.group_rows - part * unit_rows : unit_rows);
+        const int shift = RAGGED ? (int)(((base + slot) * a.cols) & 7) : 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) c[v] = Columns(lane + v * LPR, shift, cols);
+        x = static_cast<const T*>(a.logits) + (base + slot) * a.ld_logits + c[0].c0;
+        fetch(slot);
+    };
+    begin(blockIdx.x);
     Totals t;
     if constexpr (ONE) {
         int32_t* hist = reinterpret_cast<int32_t*>(f);
@@ -259,7 +308,7 @@ __global__ void __launch_bounds__(kThreads)
         for (int e = threadIdx.x; e < cols; e += kThreads) hist[e] = 0;
         if (threadIdx.x == 0) rows_valid = a.valid != nullptr ? 0 : (int32_t)a.rows;
         __syncthreads();
-        count_rows(a, 0, a.rows, hist, &rows_valid);
+        count_rows<8>(a, 0, a.rows, hist, &rows_valid);
         __syncthreads();
         for (int e = threadIdx.x; e < cols; e += kThreads) {
             const int32_t c = hist[e];
@@ -274,56 +323,36 @@ __global__ void __launch_bounds__(kThreads)
     } else {
         t = totals(a, smem);
     }
-    const int64_t units_per_group = (a.group_rows + unit_rows - 1) / unit_rows;
     float sum_dot = 0.f, sum_z = 0.f;
     for (int64_t unit = blockIdx.x; unit < a.groups * units_per_group; unit += gridDim.x) {
-        const int64_t group = unit / units_per_group, part = unit - group * units_per_group;
-        const float inv_n = ONE ? (t.rows > 0.f ? 1.f / t.rows : 0.f) : group_shares(a, group, part == 0, f);
+        if (unit != blockIdx.x) begin(unit);
+        const int64_t group = unit / units_per_group;
+        const float inv_n = ONE ? (t.rows > 0.f ? 1.f / t.rows : 0.f)
+                                : group_shares(a, group, unit == group * units_per_group, f);
         const float scale = t.live > 0.f ? a.balance_scale * (float)cols / t.live * inv_n : 0.f;
-        const int64_t base = group * a.group_rows + part * unit_rows;
-        const int64_t rows = a.group_rows - part * unit_rows < unit_rows ? a.group_rows - part * unit_rows : unit_rows;
-        const int shift = RAGGED ? (int)(((base + slot) * a.cols) & 7) : 0;
         Oct share[NV];
-        uint4 raw[NV][kP];
-        const T* x = static_cast<const T*>(a.logits) + (base + slot) * a.ld_logits;
-        T* d = static_cast<T*>(a.dlogits) + (base + slot) * a.ld_dlogits;
-        // The matrix's last row may end inside its last octet: that one is read value by value.
-        const auto fetch = [&](int64_t i) {
+        T* d = static_cast<T*>(a.dlogits) + (base + slot) * a.ld_dlogits + c[0].c0;
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const Columns c(lane + v * LPR, shift, cols);
-                if (i >= rows || !c.any()) continue;
-                if (!RAGGED || c.c0 + kOctet <= cols || base + i < a.rows - 1) {
-                    load_pieces(x + c.c0, raw[v]);
-                } else {
-                    Oct o = {};
-#pragma unroll
-                    for (int k = 0; k < kOctet; ++k)
-                        if (c.in >> k & 1) element(o, k) = to_f32(x[c.c0 + k]);
-                    pack<T>(o, raw[v]);
-                }
-            }
-            x += kSlots * a.ld_logits;
-        };
-        fetch(slot);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) share[v] = load_vector(f, Columns(lane + v * LPR, shift, cols), 0.f);
+        for (int v = 0; v < NV; ++v) share[v] = load_vector(f, c[v], 0.f);
         float unit_dot = 0.f;
         // A warp goes on until the first of its rows is past the end.
-        for (int64_t i = slot, ahead = slot - slot % (32 / LPR); ahead < rows; i += kSlots, ahead += kSlots) {
+        for (int32_t i = slot, ahead = slot - slot % (32 / LPR); ahead < rows; i += kSlots, ahead += kSlots) {
             Oct e[NV];
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const Columns c(lane + v * LPR, shift, cols);
                 e[v] = unpack<T>(raw[v]);
-                if (RAGGED ? !c.whole() : !c.any()) {
+                if (RAGGED ? !c[v].whole() : !c[v].any()) {
 #pragma unroll
                     for (int k = 0; k < kOctet; ++k)
-                        if (!(c.in >> k & 1)) element(e[v], k) = -INFINITY;
+                        if (!(c[v].in >> k & 1)) element(e[v], k) = -INFINITY;
                 }
             }
-            fetch(i + kSlots);
             const bool live = i < rows && (a.valid == nullptr || a.valid[base + i] != 0);
+            fetch(i + kSlots);
+            if (!live) {                             // whatever it holds
+#pragma unroll
+                for (int v = 0; v < NV; ++v) e[v] = Oct{};
+            }
             float top = -INFINITY;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
@@ -334,40 +363,41 @@ __global__ void __launch_bounds__(kThreads)
             if (top == -INFINITY) top = 0.f;         // no expert is open to this row: sum = 0 (or NaN)
             float2 s2 = f2(0.f), d2 = f2(0.f);
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+            for (int v = 0; v < NV; ++v) {
+                const Oct& w = share[v];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     float2& p = e[v].v[k];
-                    p = add2(p, f2(-top));
-                    p = make_float2(__expf(p.x), __expf(p.y));
+                    p = mul2(add2(p, f2(-top)), f2(kLog2e));
+                    p = make_float2(exp2_of(p.x), exp2_of(p.y));
                     s2 = add2(s2, p);
-                    d2 = fma2(share[v].v[k], p, d2);
+                    d2 = fma2(w.v[k], p, d2);
                 }
+            }
             float sum = s2.x + s2.y, dot = d2.x + d2.y;
 #pragma unroll
             for (int off = LPR / 2; off > 0; off >>= 1) {
                 sum += __shfl_xor_sync(0xffffffffu, sum, off);
                 dot += __shfl_xor_sync(0xffffffffu, dot, off);
             }
-            const float inv = sum == 0.f ? 0.f : 1.f / sum, lse = sum == 0.f ? 0.f : top + logf(sum);
-            dot *= inv;
-            if (live) {
-                unit_dot += dot;
-                sum_z += lse * lse;
+            float inv = 0.f, lse = 0.f;
+            if (live && sum != 0.f) {
+                inv = __fdividef(1.f, sum);
+                lse = top + __logf(sum);
             }
+            dot *= inv;
+            unit_dot += dot;
+            sum_z += lse * lse;
             if (a.dlogits != nullptr) {
-                const float k1 = t.up * inv, c1 = t.zscale * lse - scale * dot;
+                const float k = t.up * inv, k1 = k * scale, k0 = k * (t.zscale * lse - scale * dot);
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
-                    const Columns c(lane + v * LPR, shift, cols);
+                    const Oct& w = share[v];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        float2 g = mul2(mul2(e[v].v[k], f2(k1)), fma2(f2(scale), share[v].v[k], f2(c1)));
-                        e[v].v[k] = live ? g : f2(0.f);
-                    }
-                    if (i < rows) store_octet<T, RAGGED>(d + c.c0, c, e[v]);
+                    for (int m = 0; m < 4; ++m) e[v].v[m] = mul2(e[v].v[m], fma2(w.v[m], f2(k1), f2(k0)));
+                    if (i < rows) store_octet<T, RAGGED>(d + v * (LPR * kOctet), c[v], e[v]);
                 }
-                d += kSlots * a.ld_dlogits;
+                d += step_d;
             }
         }
         sum_dot += unit_dot * inv_n;
@@ -400,7 +430,7 @@ cudaError_t launch_rows(const BalanceArgs& a, int num_sms, cudaStream_t stream) 
     constexpr int kSlots = kThreads / LPR;
     if (balance_alone(a, kSlots))
         return launch_pdl(balance_rows_kernel<T, LPR, NV, RAGGED, true>, 1, kThreads, 0, stream, a, a.rows);
-    const int64_t cap = (int64_t)num_sms * (NV > 2 ? 2 : 4);
+    const int64_t cap = (int64_t)num_sms * (NV > 2 ? 2 : 3);      // as many as are resident
     const int64_t unit_rows = rows_of_units(a, cap, kSlots);
     const int64_t units = a.groups * ((a.group_rows + unit_rows - 1) / unit_rows);
     return launch_pdl(balance_rows_kernel<T, LPR, NV, RAGGED, false>, (unsigned)(units < cap ? units : cap), kThreads,
@@ -409,19 +439,18 @@ cudaError_t launch_rows(const BalanceArgs& a, int num_sms, cudaStream_t stream) 
 template <class T, bool RAGGED>
 cudaError_t launch_octets(const BalanceArgs& a, int64_t octets, int num_sms, cudaStream_t stream) {
     if (octets <= 1) return launch_rows<T, 1, 1, RAGGED>(a, num_sms, stream);
-    if (octets <= 2) return launch_rows<T, 1, 2, RAGGED>(a, num_sms, stream);
-    if (octets <= 4) return launch_rows<T, 2, 2, RAGGED>(a, num_sms, stream);
-    if (octets <= 8) return launch_rows<T, 4, 2, RAGGED>(a, num_sms, stream);
-    if (octets <= 16) return launch_rows<T, 8, 2, RAGGED>(a, num_sms, stream);
-    if (octets <= 32) return launch_rows<T, 16, 2, RAGGED>(a, num_sms, stream);
-    if (octets <= 64) return launch_rows<T, 32, 2, RAGGED>(a, num_sms, stream);
+    if (octets <= 4) return launch_rows<T, 1, 4, RAGGED>(a, num_sms, stream);
+    if (octets <= 8) return launch_rows<T, 2, 4, RAGGED>(a, num_sms, stream);
+    if (octets <= 16) return launch_rows<T, 4, 4, RAGGED>(a, num_sms, stream);
+    if (octets <= 32) return launch_rows<T, 8, 4, RAGGED>(a, num_sms, stream);
+    if (octets <= 64) return launch_rows<T, 16, 4, RAGGED>(a, num_sms, stream);
     return launch_rows<T, 32, 4, RAGGED>(a, num_sms, stream);
 }
 constexpr int64_t kOctetsMost = 128;
 
 int lanes_per_row(int64_t octets) {
     int lanes = 1;
-    while (lanes * 2 < octets && lanes < 32) lanes *= 2;
+    while (lanes * 4 < octets && lanes < 32) lanes *= 2;
     return lanes;
 }
 bool in_octets(const BalanceArgs& a, int size) {
@@ -434,10 +463,11 @@ cudaError_t launch(const BalanceArgs& a, int num_sms, cudaStream_t stream) {
     const int64_t octets = row_octets(a.cols);
     const bool fast = in_octets(a, (int)sizeof(T));
     if (!(fast && balance_alone(a, kThreads / lanes_per_row(octets)))) {
-        const int blocks = a.splits > 1 ? kCountCluster : 1;
-        const int64_t units = a.groups * a.splits, cap = (int64_t)num_sms * 4 / blocks;
-        const cudaError_t st = launch_rows_kernel(balance_count_kernel, (units < cap ? units : cap) * blocks,
-                                                  kCountThreads, 0, blocks, stream, a, blocks);
+        // A cluster for more than two entries a thread of a block.
+        const int blocks = a.group_rows / a.splits * a.top > 2 * kCountThreads ? kCountCluster : 1;
+        const int64_t units = a.groups * a.splits, cap = (int64_t)num_sms * 2 / blocks;
+        const cudaError_t st = launch_rows_kernel<balance_count_kernel>((units < cap ? units : cap) * blocks, kCountThreads,
+                                                                        0, blocks, stream, a, blocks);
         if (st != cudaSuccess) return st;
     }
     if (fast)
@@ -452,13 +482,13 @@ cudaError_t launch(const BalanceArgs& a, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
-// Parts of each group in the counting, 16 at most (every block of the pass adds up
-// its group's): one for up to 16,384 assignments, which a block counts, else one
-// for each 131,072, which a cluster does.
+// Splits of each group in the counting, one for each 65,536 assignments, and 19 at
+// most: a cluster of eight blocks each then fills 152 SMs, and every block of the
+// pass adds up its group's.
 int64_t balance_splits(int64_t rows, int64_t groups, int64_t top) {
     if (groups < 1) return 1;
-    const int64_t n = rows / groups * top, s = (n + 131071) / 131072 + 1;
-    return n <= 16384 ? 1 : s > 16 ? 16 : s;
+    const int64_t s = (rows / groups * top + 65535) / 65536;
+    return s < 1 ? 1 : s > 19 ? 19 : s;
 }
 
 cudaError_t launch_balance(const BalanceArgs& a, int dtype, int num_sms, cudaStream_t stream) {

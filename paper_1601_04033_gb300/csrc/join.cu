@@ -257,8 +257,8 @@ cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, int num_sms, cudaS
     if (grid > cap) grid = cap;
     const int64_t rows = grid * s.rows, bytes = rows * (int64_t)sizeof(T);
     const RowSteps steps = {rows, bytes * a.ld_x, bytes * a.ld_y, bytes * a.ld_h, bytes * a.ld_z, rows * a.cols / 8};
-    return launch_rows_kernel(join_rows_kernel<T, TPR, NR, LAYER, RAGGED, DROP>, grid * s.blocks, s.threads, smem,
-                              s.blocks, stream, a, steps, s.blocks);
+    return launch_rows_kernel<join_rows_kernel<T, TPR, NR, LAYER, RAGGED, DROP>>(grid * s.blocks, s.threads, smem, s.blocks,
+                                                                                 stream, a, steps, s.blocks);
 }
 template <class T, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {

@@ -467,8 +467,8 @@ cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, cudaStream_t strea
     const int64_t step = a.splits, bytes = step * (int64_t)sizeof(T);
     const GradSteps steps = {bytes * a.ld_x,  bytes * a.ld_y,  bytes * a.ld_dh, bytes * a.ld_dz,
                              bytes * a.ld_dx, bytes * a.ld_dy, step * 16,       step * a.cols / 8};
-    return launch_rows_kernel(grad_rows_kernel<T, TPR, LAYER, RAGGED, DROP>, a.parts * s.blocks, s.threads, smem,
-                              s.blocks, stream, a, steps, s.blocks);
+    return launch_rows_kernel<grad_rows_kernel<T, TPR, LAYER, RAGGED, DROP>>(a.parts * s.blocks, s.threads, smem, s.blocks,
+                                                                             stream, a, steps, s.blocks);
 }
 template <class T, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {

@@ -9,6 +9,8 @@
 // too, which are loaded, set to zero and not stored.
 #pragma once
 
+#include <atomic>
+
 #include "client.cuh"
 
 namespace fasgd {
@@ -75,6 +77,7 @@ __device__ __forceinline__ float& element(Oct& o, int i) { return (i & 1) ? o.v[
 struct Columns {
     int32_t c0;
     uint32_t in;
+    Columns() = default;
     __device__ Columns(int octet, int shift, int32_t cols) {
         c0 = octet * kOctet - shift;
         in = 0;
@@ -162,17 +165,23 @@ struct CopyLane {
     static constexpr int kPer = 16 / (int)sizeof(T), kStep = W * kPer;
     int32_t col, cols;
     uint32_t in;
-    int place;          // of its piece 0 in shared memory
+    int place;          // the lane
+    CopyLane() = default;
     __device__ CopyLane(const Columns& c, int32_t cols_) : cols(cols_), in(0) {
         const int lane = threadIdx.x & 31, of_row = lane % W;
         col = __shfl_sync(0xffffffffu, c.c0, 0, W) + of_row * kPer;
-        // Its octet's lane owns it; the second pieces lie four places off, so that the
-        // copies of eight neighbours fall into all banks.
-        const int owner = lane - of_row + (of_row >> 1);
-        place = kPieces<T> == 1 ? lane : (of_row & 1) ? kLane + (owner ^ 4) : owner;
+        place = lane;
 #pragma unroll
         for (int k = 0; k < kPieces<T>; ++k)
             if (col + k * kStep + kPer > 0 && col + k * kStep < cols) in |= 1u << k;
+    }
+    // Piece k * W + i of the row (i: this lane of it) belongs to the lane of octet
+    // (k W + i) / 2; second pieces lie four places off, so that the copies of
+    // eight neighbours fall into all banks.
+    __device__ __forceinline__ int place_of(int k) const {
+        if (kPieces<T> == 1) return place;
+        const int i = place % W, piece = k * W + i, owner = place - i + (piece >> 1);
+        return (piece & 1) * kLane + (owner ^ (4 * (piece & 1)));
     }
     // p: the row's first value, `col` on.  clip: the matrix ends with this row, so
     // what lies behind it is not read (zeros).
@@ -180,7 +189,7 @@ struct CopyLane {
 #pragma unroll
         for (int k = 0; k < kPieces<T>; ++k) {
             if (!(in >> k & 1)) continue;
-            uint4* to = slot + (W == 8 ? place ^ (4 * k) : place + k * (W / 2));
+            uint4* to = slot + place_of(k);
             if (!clip) {
                 copy_async16(to, p + k * kStep, 16);
             } else {
@@ -376,13 +385,20 @@ inline int64_t row_octets(int64_t cols) {
     for (int r = 0; r < 8; ++r) most = r * cols % 8 > most ? r * cols % 8 : most;
     return (most + cols + 7) / 8;
 }
-// Programmatic dependent launch (pdl.cuh), of clusters of `cluster` blocks.
-template <class... Args>
-cudaError_t launch_rows_kernel(void (*kernel)(Args...), int64_t grid, int block, size_t smem, int cluster,
-                               cudaStream_t stream, Args... args) {
-    if (smem > 32 * 1024) {          // with the kernel's own, what passes 48 KB is to be asked for
-        const cudaError_t st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+// Programmatic dependent launch (pdl.cuh), of clusters of `cluster` blocks.  With
+// the kernel's own, shared memory beyond 48 KB is to be asked for: once a device.
+template <auto Kernel, class... Args>
+cudaError_t launch_rows_kernel(int64_t grid, int block, size_t smem, int cluster, cudaStream_t stream, Args... args) {
+    if (smem > 32 * 1024) {
+        static std::atomic<uint64_t> most[64];       // bytes asked for, by device
+        int dev = 0;
+        cudaError_t st = cudaGetDevice(&dev);
         if (st != cudaSuccess) return st;
+        if (dev >= 64 || most[dev].load(std::memory_order_relaxed) < smem) {
+            st = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (st != cudaSuccess) return st;
+            if (dev < 64) most[dev].store(smem, std::memory_order_relaxed);
+        }
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
@@ -397,7 +413,7 @@ cudaError_t launch_rows_kernel(void (*kernel)(Args...), int64_t grid, int block,
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
+    return cudaLaunchKernelEx(&cfg, Kernel, args...);
 }
 
 // Whether a matrix (an absent one: yes) can be moved in octets.
