@@ -184,6 +184,22 @@ struct GradSteps {
 };
 template <class T>
 constexpr int kGradStages = sizeof(T) == 4 ? 3 : 4;
+// Vectors held in shared memory: what fits beside the ring of 512 threads.
+template <class T, bool LAYER>
+constexpr int kHeld = !LAYER ? 0 : sizeof(T) == 4 ? 1 : 2;
+__device__ __forceinline__ void hold_octet(float4* p, const Oct& o) {
+    p[0] = make_float4(o.v[0].x, o.v[0].y, o.v[1].x, o.v[1].y);
+    p[kLane] = make_float4(o.v[2].x, o.v[2].y, o.v[3].x, o.v[3].y);
+}
+__device__ __forceinline__ Oct held_octet(const float4* p) {
+    const float4 x = p[0], y = p[kLane];
+    Oct o;
+    o.v[0] = make_float2(x.x, x.y);
+    o.v[1] = make_float2(x.z, x.w);
+    o.v[2] = make_float2(y.x, y.y);
+    o.v[3] = make_float2(y.z, y.w);
+    return o;
+}
 template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
 __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     grad_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ GradSteps s, int blocks) {
@@ -216,14 +232,19 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
 
     const float scale = a.drop.scale;
     // As the forward kernel has them, so that h comes out in the same bits.
-    Oct post = load_vector(a.post, c, 1.f), post_bias, gate;
-    const Oct pre = load_vector(a.pre, c, 0.f);
+    Oct post = load_vector(a.post, c, 1.f), pre = load_vector(a.pre, c, 0.f), post_bias, gate;
     if (LAYER) post_bias = load_vector(a.post_bias, c, 0.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (DROP) post.v[i] = mul2(post.v[i], f2(scale));
         if (DROP && LAYER) post_bias.v[i] = mul2(post_bias.v[i], f2(scale));
     }
+    // With both biases the registers do not hold everything: these lie in shared
+    // memory (a place of each lane's own, as the ring's).
+    float4* const vectors = reinterpret_cast<float4*>(ring + STAGES * (stage_size + kWarpRows * th.warps)) +
+                            (threadIdx.x >> 5) * (kHeld<T, LAYER> * 2 * kLane) + (threadIdx.x & 31);
+    if (kHeld<T, LAYER> > 0) hold_octet(vectors, pre);
+    if (kHeld<T, LAYER> > 1) hold_octet(vectors + 2 * kLane, post_bias);
     // Sums over the rows: those of the norm after the block without `scale`, the
     // gate's without `branch`.
     Oct d_post = {}, d_post_bias = {}, d_gate = {}, d_pre = {}, d_pre_bias = {};
@@ -297,6 +318,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             fetch(stage == 0 ? STAGES - 1 : stage - 1);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
             if (!live) hhat = yhat = w = q = Oct{};      // a row past the end
+            if (kHeld<T, LAYER> > 1) post_bias = held_octet(vectors + 2 * kLane);
             // u; e = what dH is multiplied by in dt / scale.
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -312,6 +334,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
                 hhat.v[i] = LAYER ? mul2(add2(hhat.v[i], f2(-st.z)), f2(st.w)) : mul2(hhat.v[i], f2(st.w));
             }
             if (!has_pre) hhat = Oct{};        // (h may be infinite)
+            if (kHeld<T, LAYER> > 0) pre = held_octet(vectors);
             float2 s2[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) s2[k] = f2(0.f);
@@ -463,7 +486,8 @@ bool in_octets(const JoinArgs& a, int size) {
 
 template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {
-    const size_t smem = (size_t)kGradStages<T> * (4 * kPieces<T> * s.threads + s.threads / 32 * kWarpRows) * 16;
+    const size_t smem = ((size_t)kGradStages<T> * (4 * kPieces<T> * s.threads + s.threads / 32 * kWarpRows) +
+                         (size_t)kHeld<T, LAYER> * 2 * s.threads) * 16;
     const int64_t step = a.splits, bytes = step * (int64_t)sizeof(T);
     const GradSteps steps = {bytes * a.ld_x,  bytes * a.ld_y,  bytes * a.ld_dh, bytes * a.ld_dz,
                              bytes * a.ld_dx, bytes * a.ld_dy, step * 16,       step * a.cols / 8};
@@ -507,6 +531,23 @@ cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
+// Splits of each group's rows for `most` subs: fewest row turns of the busiest
+// sub, a unit costing about four more to begin and to leave its sums.
+static int64_t best_splits(int64_t groups, int64_t rows, int64_t most, int64_t step) {
+    int64_t best = step, least = INT64_MAX;
+    for (int64_t s = step, tried = 0; s <= rows && tried < 64; s += step, ++tried) {
+        // Past one unit for each sub in steps that fill whole rounds of them.
+        if (tried > 0 && groups * s > most) s = ((groups * s + most - 1) / most * most / groups + step - 1) / step * step;
+        if (s > rows) break;
+        const int64_t cost = (groups * s + most - 1) / most * ((rows + s - 1) / s + 4);
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
 JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms) {
     JoinPlan p;
     p.parts = p.splits = p.row_means = 0;
@@ -518,10 +559,7 @@ JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms) {
         if (a.groups == 1) {
             p.splits = at_most(a.rows, most);
         } else {
-            // Four units for each sub, but no fewer than eight rows to a unit: each
-            // leaves a row's worth of fp32 sums.
-            p.splits = at_most((4 * most + a.groups - 1) / a.groups, at_most(a.group_rows / 8, a.group_rows));
-            if (a.cols % 8 != 0) p.splits = (p.splits + 7) / 8 * 8;
+            p.splits = best_splits(a.groups, a.group_rows, most, a.cols % 8 != 0 ? 8 : 1);
         }
         const int64_t units = a.groups * p.splits;
         p.parts = (at_most(units, most) + block_subs - 1) / block_subs;
