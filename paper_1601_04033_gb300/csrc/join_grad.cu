@@ -154,12 +154,12 @@ __host__ __device__ __forceinline__ int64_t gates_left(const JoinArgs& a) {
     return a.out_gate != nullptr && a.groups > 1 && (a.splits > 1 || a.rows == 0) ? a.groups : 0;
 }
 
-// Rows in octets.  TPR threads hold a row, an octet each; every thread keeps its
-// columns' sums over the rows it takes in registers.  One reduction a row is
-// enough: with e = m scale branch gate post (so q2 = e dH) and w = dh + r_h q,
-//   sum q2 yhat = S(e yhat w) - r_h (mean q S(e yhat) + mean(q hhat) S(e yhat hhat)),
-// and the same without yhat for mean q2, so all sums are of what is known before
-// mean q is.  Units as in the plain form, for the threads of one row ("sub") at a
+// Rows in octets.  A row's threads hold an octet of it each; every thread keeps its
+// columns' sums over the rows it takes in registers.  Under rms norms one reduction
+// a row is enough: with e = m scale branch gate post (so q2 = e dH) and w = dh + r_h q,
+//   sum q2 yhat = S(e yhat w) - r_h mean(q hhat) S(e yhat hhat),
+// sums of what is known before mean(q hhat) is.  Under layer norms that takes
+// eight sums, whose registers cost more than a second reduction of two.  Units as in the plain form, for the threads of one row ("sub") at a
 // time; where cols is no multiple of 8 a unit's rows agree modulo 8 (octet.cuh).
 struct Unit {
     int64_t row, step, rows;     // first row, from row to row, one past the last
@@ -186,7 +186,7 @@ template <class T>
 constexpr int kGradStages = sizeof(T) == 4 ? 3 : 4;
 // Vectors held in shared memory: what fits beside the ring of 512 threads.
 template <class T, bool LAYER>
-constexpr int kHeld = !LAYER ? 0 : sizeof(T) == 4 ? 1 : 2;
+constexpr int kHeld = !LAYER ? 0 : sizeof(T) == 4 ? 1 : 3;
 __device__ __forceinline__ void hold_octet(float4* p, const Oct& o) {
     p[0] = make_float4(o.v[0].x, o.v[0].y, o.v[1].x, o.v[1].y);
     p[kLane] = make_float4(o.v[2].x, o.v[2].y, o.v[3].x, o.v[3].y);
@@ -203,7 +203,7 @@ __device__ __forceinline__ Oct held_octet(const float4* p) {
 template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
 __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     grad_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ GradSteps s, int blocks) {
-    constexpr int kP = kPieces<T>, kSums = LAYER ? 8 : 3, STAGES = kGradStages<T>;
+    constexpr int kP = kPieces<T>, kSums = LAYER ? 2 : 3, STAGES = kGradStages<T>;
     extern __shared__ uint4 ring[];                  // [STAGES][warp][x, y, dh, dz][kP][lane], then [STAGES][warp][row of a warp]
     __shared__ __align__(16) float red[RowSums<TPR, kSums>::kPlaces];
     const RowThreads<TPR> th(blocks);
@@ -245,6 +245,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
                             (threadIdx.x >> 5) * (kHeld<T, LAYER> * 2 * kLane) + (threadIdx.x & 31);
     if (kHeld<T, LAYER> > 0) hold_octet(vectors, pre);
     if (kHeld<T, LAYER> > 1) hold_octet(vectors + 2 * kLane, post_bias);
+    if (kHeld<T, LAYER> > 2) hold_octet(vectors + 4 * kLane, post);
     // Sums over the rows: those of the norm after the block without `scale`, the
     // gate's without `branch`.
     Oct d_post = {}, d_post_bias = {}, d_gate = {}, d_pre = {}, d_pre_bias = {};
@@ -319,6 +320,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             stage = stage == STAGES - 1 ? 0 : stage + 1;
             if (!live) hhat = yhat = w = q = Oct{};      // a row past the end
             if (kHeld<T, LAYER> > 1) post_bias = held_octet(vectors + 2 * kLane);
+            if (kHeld<T, LAYER> > 2) post = held_octet(vectors + 4 * kLane);
             // u; e = what dH is multiplied by in dt / scale.
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -335,35 +337,28 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             }
             if (!has_pre) hhat = Oct{};        // (h may be infinite)
             if (kHeld<T, LAYER> > 0) pre = held_octet(vectors);
-            float2 s2[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) s2[k] = f2(0.f);
+            float2 s2[3] = {f2(0.f), f2(0.f), f2(0.f)};
+            float v[kSums];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 d_pre.v[i] = fma2(q.v[i], hhat.v[i], d_pre.v[i]);
                 if (LAYER) d_pre_bias.v[i] = add2(d_pre_bias.v[i], q.v[i]);
                 q.v[i] = mul2(q.v[i], pre.v[i]);
                 w.v[i] = fma2(q.v[i], f2(st.w), w.v[i]);
-                const float2 ep = mul2(e.v[i], post.v[i]), ey = mul2(ep, yhat.v[i]);
                 s2[0] = fma2(q.v[i], hhat.v[i], s2[0]);
-                s2[1] = fma2(ey, w.v[i], s2[1]);
-                s2[2] = fma2(ey, hhat.v[i], s2[2]);
                 if (LAYER) {
-                    s2[3] = add2(s2[3], q.v[i]);
-                    s2[4] = add2(s2[4], ey);
-                    s2[5] = fma2(ep, w.v[i], s2[5]);
-                    s2[6] = fma2(ep, hhat.v[i], s2[6]);
-                    s2[7] = add2(s2[7], ep);
+                    s2[1] = add2(s2[1], q.v[i]);
+                } else {
+                    const float2 ey = mul2(mul2(e.v[i], post.v[i]), yhat.v[i]);
+                    s2[1] = fma2(ey, w.v[i], s2[1]);
+                    s2[2] = fma2(ey, hhat.v[i], s2[2]);
                 }
             }
-            float v[kSums];
 #pragma unroll
             for (int k = 0; k < kSums; ++k) v[k] = s2[k].x + s2[k].y;
             sums(v);
-            // r_h times the means of q hhat and of q; the means of q2 yhat and of q2.
-            const float m1 = v[0] * a.inv_cols * st.w, m0 = LAYER ? v[3] * a.inv_cols * st.w : 0.f;
-            const float k1 = (LAYER ? v[1] - m0 * v[4] - m1 * v[2] : v[1] - m1 * v[2]) * a.inv_cols;
-            const float k0 = LAYER ? (v[5] - m0 * v[7] - m1 * v[6]) * a.inv_cols : 0.f;
+            // r_h times the means of q hhat and (layer norm) of q; then dH.
+            const float m1 = v[0] * a.inv_cols * st.w, m0 = LAYER ? v[1] * a.inv_cols * st.w : 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float2 d = fma2(hhat.v[i], f2(-m1), w.v[i]);
@@ -372,12 +367,36 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
                 d_gate.v[i] = fma2(d, uu.v[i], d_gate.v[i]);
                 w.v[i] = mul2(e.v[i], d);
             }
+            if (live) store_octet<T, RAGGED>(dxp, c, hhat);
             if (has_post) {
+                // The means of q2 yhat and (layer norm) of q2.
+                float k1, k0 = 0.f;
+                if constexpr (LAYER) {
+                    s2[0] = s2[1] = f2(0.f);
+                    if (kHeld<T, LAYER> > 2) post = held_octet(vectors + 4 * kLane);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        d_post.v[i] = fma2(w.v[i], yhat.v[i], d_post.v[i]);
+                        d_post_bias.v[i] = add2(d_post_bias.v[i], w.v[i]);
+                        w.v[i] = mul2(w.v[i], post.v[i]);
+                        s2[0] = fma2(w.v[i], yhat.v[i], s2[0]);
+                        s2[1] = add2(s2[1], w.v[i]);
+                    }
+                    v[0] = s2[0].x + s2[0].y;
+                    v[1] = s2[1].x + s2[1].y;
+                    sums(v);
+                    k1 = v[0] * a.inv_cols;
+                    k0 = v[1] * a.inv_cols;
+                } else {
+                    k1 = (v[1] - m1 * v[2]) * a.inv_cols;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        d_post.v[i] = fma2(w.v[i], yhat.v[i], d_post.v[i]);
+                        w.v[i] = mul2(w.v[i], post.v[i]);
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    d_post.v[i] = fma2(w.v[i], yhat.v[i], d_post.v[i]);
-                    if (LAYER) d_post_bias.v[i] = add2(d_post_bias.v[i], w.v[i]);
-                    w.v[i] = mul2(w.v[i], post.v[i]);
                     if (LAYER) w.v[i] = add2(w.v[i], f2(-k0));
                     w.v[i] = mul2(fma2(yhat.v[i], f2(-k1), w.v[i]), f2(st.y));
                 }
@@ -386,10 +405,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w.v[i] = mul2(w.v[i], f2(scale));
             }
-            if (live) {
-                store_octet<T, RAGGED>(dxp, c, hhat);
-                if (has_y) store_octet<T, RAGGED>(dyp, c, w);
-            }
+            if (live && has_y) store_octet<T, RAGGED>(dyp, c, w);
             dxp = on(dxp, s.dx);
             dyp = on(dyp, s.dy);
         }
