@@ -182,11 +182,11 @@ struct Unit {
 struct GradSteps {
     int64_t x, y, dh, dz, dx, dy, stats, octets;
 };
-template <class T>
-constexpr int kGradStages = sizeof(T) == 4 ? 3 : 4;
+template <class T, bool LAYER>
+constexpr int kGradStages = sizeof(T) == 2 ? 4 : LAYER ? 2 : 3;
 // Vectors held in shared memory: what fits beside the ring of 512 threads.
 template <class T, bool LAYER>
-constexpr int kHeld = !LAYER ? 0 : sizeof(T) == 4 ? 1 : 3;
+constexpr int kHeld = LAYER ? 3 : 0;
 __device__ __forceinline__ void hold_octet(float4* p, const Oct& o) {
     p[0] = make_float4(o.v[0].x, o.v[0].y, o.v[1].x, o.v[1].y);
     p[kLane] = make_float4(o.v[2].x, o.v[2].y, o.v[3].x, o.v[3].y);
@@ -203,7 +203,7 @@ __device__ __forceinline__ Oct held_octet(const float4* p) {
 template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
 __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     grad_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ GradSteps s, int blocks) {
-    constexpr int kP = kPieces<T>, kSums = LAYER ? 2 : 3, STAGES = kGradStages<T>;
+    constexpr int kP = kPieces<T>, kSums = LAYER ? 2 : 3, STAGES = kGradStages<T, LAYER>;
     extern __shared__ uint4 ring[];                  // [STAGES][warp][x, y, dh, dz][kP][lane], then [STAGES][warp][row of a warp]
     __shared__ __align__(16) float red[RowSums<TPR, kSums>::kPlaces];
     const RowThreads<TPR> th(blocks);
@@ -502,7 +502,7 @@ bool in_octets(const JoinArgs& a, int size) {
 
 template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {
-    const size_t smem = ((size_t)kGradStages<T> * (4 * kPieces<T> * s.threads + s.threads / 32 * kWarpRows) +
+    const size_t smem = ((size_t)kGradStages<T, LAYER> * (4 * kPieces<T> * s.threads + s.threads / 32 * kWarpRows) +
                          (size_t)kHeld<T, LAYER> * 2 * s.threads) * 16;
     const int64_t step = a.splits, bytes = step * (int64_t)sizeof(T);
     const GradSteps steps = {bytes * a.ld_x,  bytes * a.ld_y,  bytes * a.ld_dh, bytes * a.ld_dz,
