@@ -82,7 +82,7 @@ struct RowSteps {
 constexpr int kForwardStages = 3;
 constexpr int kForwardThreads = 512;      // of an SM
 template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP>
-__global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : kForwardThreads / 512)
+__global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8 ? 16 : 1)
     join_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ RowSteps s, int blocks) {
     constexpr int kP = kPieces<T>, STAGES = kForwardStages;
     extern __shared__ uint4 ring[];                  // [STAGES][warp][NR][x, y][kP][lane]
@@ -246,14 +246,12 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : kForwardT
     }
 }
 
-constexpr int kForwardRows = 2;      // rows a turn
-template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP>
+template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
-    constexpr int NR = kForwardRows;
     const size_t smem = (size_t)kForwardStages * 2 * NR * kPieces<T> * s.threads * 16;
     int64_t grid = (a.rows + s.rows - 1) / s.rows;
     // Past one row each, they step by a multiple of 8 rows (octet.cuh).
-    const int64_t cap = (int64_t)num_sms * (kForwardThreads / s.threads) / s.blocks / 8 * 8;
+    const int64_t cap = (int64_t)num_sms * (NR == 1 ? 1 : kForwardThreads / s.threads) / s.blocks / 8 * 8;
     if (grid > cap) grid = cap;
     const int64_t rows = grid * s.rows, bytes = rows * (int64_t)sizeof(T);
     const RowSteps steps = {rows, bytes * a.ld_x, bytes * a.ld_y, bytes * a.ld_h, bytes * a.ld_z, rows * a.cols / 8};
@@ -262,8 +260,10 @@ cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, int num_sms, cudaS
 }
 template <class T, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
-    if (s.rows > 1) return launch_rows<T, 8, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
-    return launch_rows<T, 0, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
+    if (s.rows > 1) return launch_rows<T, 8, 2, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
+    // Two rows a turn, but where a row takes more threads than have the registers for it.
+    if (s.threads > 512) return launch_rows<T, 0, 1, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
+    return launch_rows<T, 0, 2, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
 }
 template <class T, bool LAYER>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
@@ -285,7 +285,9 @@ bool in_octets(const JoinArgs& a, int size) {
 
 template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
-    const RowShape s(row_octets(a.cols), 512);
+    // One block where 1,024 threads will do (16384 x 8192 bf16: 291 us; a cluster of two: 376).
+    const int64_t octets = row_octets(a.cols);
+    const RowShape s(octets, octets <= 1024 ? 1024 : 512);
     if (s.fits() && in_octets(a, (int)sizeof(T)))
         return a.layer ? launch_octets<T, true>(a, s, num_sms, stream) : launch_octets<T, false>(a, s, num_sms, stream);
     const int64_t grid = a.rows < (int64_t)num_sms * 8 ? a.rows : (int64_t)num_sms * 8;

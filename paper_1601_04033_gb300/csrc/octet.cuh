@@ -271,7 +271,7 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }
 constexpr int pow2_above(int n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }
-constexpr int kRowWarps = 16;       // of a block, that hold a row; times a cluster's blocks
+constexpr int kRowWarps = 32;       // of a block, that hold a row; times a cluster's blocks
 constexpr int kCluster = 8;
 
 // The threads of a row: a block's (TPR = 0, whole warps), or those of each block
@@ -297,8 +297,8 @@ constexpr int kWarpRows = 4;       // of TPR = 8
 template <int TPR, int N>
 struct RowSums {
     static constexpr int kN = pow2_above(N), kLanes = 32 / kN;     // lanes that end with one value
-    // Floats of shared memory: two places for each warp of a cluster.
-    static constexpr int kPlaces = TPR ? 1 : 2 * kN * kRowWarps * kCluster;
+    // Floats of shared memory: two places for each warp of a cluster's blocks (of 16 at most).
+    static constexpr int kPlaces = TPR ? 1 : 2 * kN * (kRowWarps / 2) * kCluster;
     const RowThreads<TPR>& th;
     float* red;
     int warps, turn;
