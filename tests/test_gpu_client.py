@@ -650,6 +650,49 @@ def test_automatic_differentiation():
     assert torch.equal(torch.cat((loss.detach().reshape(1), parts)), b.loss)
 
 
+def test_both_intakes_agree():
+    """The C module's intake against client.py's own, which serves where Python's
+    headers were missing: the same struct, and the same refusals."""
+    import ctypes
+    import torch
+    from paper_1601_04033_gb300 import fasgd
+    c = _c()
+    if getattr(fasgd._binding, "intake", None) is None:
+        pytest.skip("built without Python's headers")
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")   # noqa: E731
+    w, h = z(24, dtype=torch.float32), z(24, dtype=torch.float16)
+    wide = z(10, 40)
+    cube = z(4, 5, 24)
+    fine = [(z(6, 24), z(6, 24), None, None, w, None, w, w, None), (z(24), None, None, None, None, None, None, w, w),
+            (wide[:, :24], wide[:, 16:], None, None, w, None, z(2, 24), None, None),
+            (cube, cube, cube, None, w, w, z(5, 24, dtype=torch.float32), None, None), (z(1, 24), z(1, 24)) + (None,) * 7,
+            (cube[:, :1], None, None, None, None, None, None, w, None), (cube[:1], None, None, None, None, None, None, w, None),
+            (z(0, 24), z(0, 24)) + (None,) * 7, (z(3, 1)[:, :1], None) + (None,) * 7]
+    bad = [(z(6, 24).t(),) + (None,) * 8, (z(6, 24).cpu(),) + (None,) * 8, (z(6, 24, dtype=torch.float64),) + (None,) * 8,
+           (z(6, 24), z(5, 24)) + (None,) * 7, (z(6, 24), z(6, 24, dtype=torch.float16)) + (None,) * 7,
+           (cube[:, :3], None) + (None,) * 7, (cube.transpose(0, 1), None) + (None,) * 7, (torch.zeros((), device="cuda"),) + (None,) * 8,
+           (z(6, 24), None, None, None, h, None, None, None, None), (z(6, 24), None, None, None, w[:12]) + (None,) * 4,
+           (z(6, 12), None, None, None, w[::2]) + (None,) * 4, (z(6, 24), None, None, None, None, None, z(2, 12), None, None),
+           (z(6, 24), None, None, None, None, None, z(2, 2, 24), None, None), (z(6, 24), None, None, None, None, None, z(4, 24)[::2], None, None),
+           (3,) + (None,) * 8]
+    for tensors in fine + bad:
+        got = []
+        for form in (lambda a, s, *t: fasgd._binding.intake(ctypes.addressof(a), s.words, *t), c._intake):
+            a = fasgd.JoinArgs()
+            try:
+                form(a, c._JOIN, *tensors)
+                got.append(bytes(a))
+            except (ValueError, AttributeError, TypeError):
+                got.append("refused")
+        if any(tensors is f for f in fine):
+            a, b = (fasgd.JoinArgs.from_buffer_copy(g) for g in got)
+            for name, _ in fasgd.JoinArgs._fields_:
+                same = name.startswith("ld_") and a.rows < 2       # not looked at
+                assert same or getattr(a, name) == getattr(b, name), (name, [None if t is None else t.shape for t in tensors])
+        else:
+            assert got == ["refused", "refused"], [None if t is None else getattr(t, "shape", t) for t in tensors]
+
+
 def test_refusals_on_tensors():
     import torch
     from paper_1601_04033_gb300 import fasgd
