@@ -15,7 +15,6 @@
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
-#include <string.h>
 
 #include "fasgd.h"
 
@@ -182,185 +181,6 @@ static PyObject* py_install(PyObject* self, PyObject* space) {
     return out;
 }
 
-/* intake(address, spec, tensors...): the tensors of a client operator into its
- * argument struct at `address`, as client.py's function of the same name does it
- * (which says what the kinds are), at a third of its cost.  spec: bytes, 16-bit
- * little-endian words: the offsets of rows, cols, dtype, groups and gate_dtype
- * (0xffff: the struct has none), then for each tensor its kind, and the offsets
- * of its pointer and its ld. */
-enum { K_FIRST, K_LIKE, K_VECTOR, K_GATE };
-static PyObject* dtypes[3];    /* torch's fp32, bf16, fp16, in the order of enum fasgd_dtype */
-static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_data_ptr, *s_is_contiguous;
-
-static int word(const unsigned char* p, int i) { return p[2 * i] | p[2 * i + 1] << 8; }
-static void put64(char* at, int off, long long v) { memcpy(at + off, &v, 8); }
-static void put32(char* at, int off, int v) { if (off != 0xffff) memcpy(at + off, &v, 4); }
-static int wrong(const char* what) {
-    PyErr_SetString(PyExc_ValueError, what);
-    return -1;
-}
-static long long address_of(PyObject* t) {
-    PyObject* r = PyObject_CallMethodNoArgs(t, s_data_ptr);
-    long long v = r == NULL ? -1 : (long long)PyLong_AsUnsignedLongLong(r);
-    Py_XDECREF(r);
-    return v != 0 ? v : 16;    /* no elements: never followed */
-}
-static int truth(PyObject* r) {
-    int v = r == NULL ? -1 : r == Py_True;
-    Py_XDECREF(r);
-    return v;
-}
-static int dtype_of(PyObject* t) {
-    PyObject* d = PyObject_GetAttr(t, s_dtype);
-    int i;
-    if (d == NULL) return -1;
-    for (i = 0; i < 3 && d != dtypes[i]; ++i) {}
-    Py_DECREF(d);
-    return i < 3 ? i : wrong("activations are fp32, bf16 or fp16");
-}
-/* rows, cols and ld of a matrix [..., cols] whose rows are evenly spaced; its shape. */
-static PyObject* layout(PyObject* t, long long* rows, long long* cols, long long* ld) {
-    PyObject *shape = PyObject_GetAttr(t, s_shape), *stride = NULL;
-    Py_ssize_t n, i;
-    int ok = 0;
-    long long next = 0;
-    if (shape == NULL) return NULL;
-    stride = PyObject_CallMethodNoArgs(t, s_stride);
-    if (stride == NULL || !PyTuple_Check(shape) || !PyTuple_Check(stride)) goto done;
-    n = PyTuple_GET_SIZE(shape);
-    if (n < 1 || PyTuple_GET_SIZE(stride) != n) {
-        wrong("a matrix [..., cols] is expected");
-        goto done;
-    }
-    *cols = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, n - 1));
-    *rows = 1;
-    *ld = *cols;
-    if (PyLong_AsLongLong(PyTuple_GET_ITEM(stride, n - 1)) != 1 && *cols > 1) {
-        wrong("the values of a row must be contiguous");
-        goto done;
-    }
-    for (i = n - 2; i >= 0; --i) {
-        const long long size = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
-        const long long step = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i));
-        if (size != 1) {
-            if (*rows == 1) {
-                *ld = step;
-            } else if (*rows != 0 && size != 0 && step != next) {
-                wrong("the rows must be evenly spaced");
-                goto done;
-            }
-            next = step * size;
-            *rows *= size;
-        }
-    }
-    ok = !PyErr_Occurred();
-done:
-    Py_XDECREF(stride);
-    if (!ok) Py_CLEAR(shape);
-    return shape;
-}
-static int on_gpu(PyObject* t) {
-    const int v = truth(PyObject_GetAttr(t, s_is_cuda));
-    return v == 1 ? 0 : v == 0 ? wrong("CUDA tensors are expected") : -1;
-}
-static int contiguous(PyObject* t) {
-    const int v = truth(PyObject_CallMethodNoArgs(t, s_is_contiguous));
-    return v == 1 ? 0 : v == 0 ? wrong("a contiguous tensor is expected") : -1;
-}
-
-static PyObject* py_intake(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
-    PyObject *first = NULL, *shape = NULL;
-    long long rows = 0, cols = 0, ld, r, c, p;
-    const unsigned char* spec;
-    char* at;
-    int type = 0, bad = 0;
-    (void)self;
-    if (nargs < 2 || !PyLong_Check(args[0]) || !PyBytes_Check(args[1]) ||
-        PyBytes_GET_SIZE(args[1]) != 10 + 6 * (nargs - 2) || dtypes[0] == NULL) {
-        PyErr_SetString(PyExc_TypeError, "intake(address, spec, tensors...)");
-        return NULL;
-    }
-    at = (char*)(uintptr_t)PyLong_AsUnsignedLongLongMask(args[0]);
-    spec = (const unsigned char*)PyBytes_AS_STRING(args[1]);
-    if (word(spec, 3) != 0xffff) put64(at, word(spec, 3), 1);
-    for (Py_ssize_t i = 2; i < nargs && !bad; ++i) {
-        PyObject* t = args[i];
-        const unsigned char* s = spec + 10 + 6 * (i - 2);
-        if (t == Py_None) continue;
-        switch (word(s, 0)) {
-            case K_FIRST:
-                first = layout(t, &rows, &cols, &ld);
-                bad = first == NULL || on_gpu(t) < 0 || (type = dtype_of(t)) < 0;
-                if (bad) break;
-                put64(at, word(spec, 0), rows);
-                put64(at, word(spec, 1), cols);
-                put32(at, word(spec, 2), type);
-                put64(at, word(s, 2), ld);
-                break;
-            case K_LIKE: {
-                int same, ty;
-                shape = layout(t, &r, &c, &ld);
-                bad = shape == NULL || on_gpu(t) < 0 || (ty = dtype_of(t)) < 0;
-                if (!bad && first != NULL) {
-                    same = PyObject_RichCompareBool(shape, first, Py_EQ);
-                    bad = same != 1 || ty != type;
-                    if (bad && same >= 0) wrong("matrices of one shape and type are expected");
-                }
-                Py_XDECREF(shape);
-                if (!bad) put64(at, word(s, 2), ld);
-                break;
-            }
-            case K_VECTOR:
-                shape = layout(t, &r, &c, &ld);
-                bad = shape == NULL || on_gpu(t) < 0 || contiguous(t) < 0;
-                Py_XDECREF(shape);
-                if (!bad && (r * c != cols || dtype_of(t) != 0)) {
-                    PyErr_Clear();
-                    bad = wrong("parameters are contiguous fp32 vectors of cols values");
-                }
-                break;
-            default: {                 /* K_GATE */
-                Py_ssize_t dims = 0;
-                int ty;
-                shape = layout(t, &r, &c, &ld);
-                bad = shape == NULL || on_gpu(t) < 0 || contiguous(t) < 0 || (ty = dtype_of(t)) < 0;
-                if (shape != NULL) dims = PyTuple_GET_SIZE(shape);
-                Py_XDECREF(shape);
-                if (!bad && (dims > 2 || c != cols)) bad = wrong("a gate is contiguous, [cols] or [groups, cols]");
-                if (bad) break;
-                if (dims == 2) put64(at, word(spec, 3), r);
-                put32(at, word(spec, 4), ty);
-            }
-        }
-        if (!bad) {
-            p = address_of(t);
-            bad = p == -1 && PyErr_Occurred();
-            put64(at, word(s, 1), p);
-        }
-    }
-    Py_XDECREF(first);
-    if (bad) {
-        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "intake: not a tensor");
-        return NULL;
-    }
-    Py_RETURN_NONE;
-}
-/* intake_types(fp32, bf16, fp16): torch's types, before the first intake. */
-static PyObject* py_intake_types(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
-    (void)self;
-    if (nargs != 3) {
-        PyErr_SetString(PyExc_TypeError, "intake_types(fp32, bf16, fp16)");
-        return NULL;
-    }
-    for (int i = 0; i < 3; ++i) {
-        PyObject* old = dtypes[i];
-        Py_INCREF(args[i]);
-        dtypes[i] = args[i];
-        Py_XDECREF(old);
-    }
-    Py_RETURN_NONE;
-}
-
 static PyMethodDef methods[] = {
     METHOD(fasgd_push), METHOD(fasgd_push_host), METHOD(fasgd_push_sparse), METHOD(fasgd_apply_pending),
     METHOD(bfasgd_select_compact), METHOD(bfasgd_fetch_compact), METHOD(bfasgd_fetch_apply),
@@ -369,21 +189,9 @@ static PyMethodDef methods[] = {
     METHOD(fasgd_sim_quadratic_grad), METHOD(fasgd_sim_quadratic_loss), METHOD(fasgd_dropout),
     METHOD(fasgd_join), METHOD(fasgd_join_grad), METHOD(fasgd_join_workspace), METHOD(fasgd_balance),
     METHOD(fasgd_balance_workspace),
-    {"install", py_install, METH_O, NULL},
-    {"intake", (PyCFunction)(void (*)(void))py_intake, METH_FASTCALL, NULL},
-    {"intake_types", (PyCFunction)(void (*)(void))py_intake_types, METH_FASTCALL, NULL},
-    {NULL, NULL, 0, NULL}};
+    {"install", py_install, METH_O, NULL}, {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, methods,
                                     NULL, NULL, NULL, NULL};
 
-PyMODINIT_FUNC PyInit__binding(void) {
-    s_shape = PyUnicode_InternFromString("shape");
-    s_stride = PyUnicode_InternFromString("stride");
-    s_dtype = PyUnicode_InternFromString("dtype");
-    s_is_cuda = PyUnicode_InternFromString("is_cuda");
-    s_data_ptr = PyUnicode_InternFromString("data_ptr");
-    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-    if (!s_shape || !s_stride || !s_dtype || !s_is_cuda || !s_data_ptr || !s_is_contiguous) return NULL;
-    return PyModule_Create(&module);
-}
+PyMODINIT_FUNC PyInit__binding(void) { return PyModule_Create(&module); }

@@ -10,10 +10,13 @@ from __future__ import annotations
 
 import concurrent.futures
 import glob
+import importlib.util
 import os
+import re
 import shutil
 import subprocess
 import sysconfig
+import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -57,6 +60,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list | None =
     """Build libfasgd.so (and the binding's module) if needed; returns its path."""
     if not force and up_to_date():
         build_binding()
+        build_client()
         return LIB
     os.makedirs(BUILD, exist_ok=True)
     exe = nvcc()
@@ -84,6 +88,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list | None =
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
     build_binding(force)
+    build_client()
     return LIB
 
 
@@ -115,6 +120,46 @@ def build_binding(force: bool = False) -> str | None:
         raise RuntimeError(f"binding build failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, BINDING)
     return BINDING
+
+
+CLIENT_SRC = os.path.join(PKG, "client_torch.cpp")
+CLIENT = os.path.join(PKG, "_client" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+def torch_home() -> str | None:
+    """torch's folder (without importing it), if its C++ headers are there."""
+    spec = importlib.util.find_spec("torch")
+    home = None if spec is None else next(iter(spec.submodule_search_locations or []), None)
+    header = None if home is None else os.path.join(home, "include", "torch", "csrc", "autograd", "python_variable.h")
+    return home if header is not None and os.path.exists(header) else None
+
+
+def build_client(force: bool = False) -> str | None:
+    """Build the CPython module of the client operators on torch tensors
+    (client_torch.cpp) against libfasgd.so and torch; returns its path, or None,
+    with a warning where it does not compile, where client.py's own code serves."""
+    home, include = torch_home(), sysconfig.get_paths()["include"]
+    if home is None or not os.path.exists(os.path.join(include, "Python.h")):
+        return None
+    newest = max(os.path.getmtime(p) for p in (CLIENT_SRC, os.path.join(INCLUDE, "fasgd.h"),
+                                               os.path.join(home, "version.py")))
+    if not force and os.path.exists(CLIENT) and os.path.getmtime(CLIENT) >= newest:
+        return CLIENT
+    with open(os.path.join(home, "version.py")) as f:
+        version = re.search(r"__version__ = '([^']+)'", f.read()).group(1)
+    tmp = CLIENT + f".tmp{os.getpid()}"
+    lib, cuda = os.path.join(home, "lib"), os.path.dirname(os.path.dirname(nvcc()))
+    cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-Wno-deprecated-declarations", "-shared", "-fPIC",
+           "-fvisibility=hidden", f'-DBUILT_FOR_TORCH="{version}"', CLIENT_SRC, f"-I{include}", f"-I{INCLUDE}",
+           *[f"-isystem{d}" for d in (os.path.join(home, "include"), os.path.join(cuda, "include"))],
+           f"-L{PKG}", "-lfasgd", f"-L{lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+           "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{lib}", "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        warnings.warn(f"the client operators' torch module was not built: {r.stderr[-2000:]}", RuntimeWarning)
+        return None
+    os.replace(tmp, CLIENT)
+    return CLIENT
 
 
 DRIVER_SRC = os.path.join(PKG, "abi_latency.c")

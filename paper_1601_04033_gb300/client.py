@@ -16,6 +16,8 @@ into views of the flat vector that is pushed.
 from __future__ import annotations
 
 import ctypes
+import importlib
+import warnings
 from typing import NamedTuple
 
 import torch
@@ -25,6 +27,24 @@ from . import fasgd as _f
 _DTYPES = {torch.float32: _f.F32, torch.bfloat16: _f.BF16, torch.float16: _f.F16}
 _NORMS = {"rms": _f.RMS_NORM, "layer": _f.LAYER_NORM}
 _NOWHERE = 16      # stands for the address of a tensor without elements: never followed
+
+
+def _module():
+    """client_torch.cpp's module, if it was built for this torch."""
+    try:
+        m = importlib.import_module("._client", __package__)
+    except ImportError as error:
+        if not isinstance(error, ModuleNotFoundError):
+            warnings.warn(f"{error}: the client operators go through ctypes", RuntimeWarning)
+        return None
+    if m.torch_version.split("+")[0] != torch.__version__.split("+")[0]:
+        warnings.warn(f"_client was built for torch {m.torch_version}: the client operators go through ctypes",
+                      RuntimeWarning)
+        return None
+    return m
+
+
+_fast = _module()
 
 
 class Draws(NamedTuple):
@@ -42,6 +62,11 @@ def _check(rc: int):
     return rc
 
 
+def _done(result):
+    """What a call of client_torch.cpp's gave: a negative status, or its tensors."""
+    return _check(result) if type(result) is int else result
+
+
 def _dtype(t) -> int:
     d = _DTYPES.get(t.dtype)
     if d is None:
@@ -49,8 +74,6 @@ def _dtype(t) -> int:
     return d
 
 
-# A small call is bound by the host, so tensors are asked as few questions as
-# will do (each costs 0.06 to 0.2 us, a new tensor 1.4 us).
 def _stream(t) -> int:
     """torch's current stream, which is to be on t's device."""
     if t.get_device() != torch._C._cuda_getDevice():
@@ -85,28 +108,13 @@ def _rows(t):
 _FIRST, _LIKE, _VECTOR, _GATE = range(4)
 
 
-class _Spec:
-    """Where a struct's tensors go: "kind pointer" words in the order of intake's."""
-
-    def __init__(self, struct, **kinds):
-        def off(name):
-            f = getattr(struct, name, None)
-            return 0xFFFF if f is None else f.offset
-        self.fields = [(kind, name) for name, kind in kinds.items()]
-        words = [off("rows"), off("cols"), off("dtype"), off("groups") if struct is _f.JoinArgs else 0xFFFF,
-                 off("gate_dtype")]
-        for kind, name in self.fields:
-            words += [kind, off(name), off("ld_" + name)]
-        self.words = b"".join(w.to_bytes(2, "little") for w in words)
-
-
 def _intake(a, spec, *tensors):
     """Each tensor that is not None into struct a (its pointer, its ld, and what
     the first and the gate fix); ValueError where one is not what its kind says."""
     cols = None
     if hasattr(a, "gate_dtype"):
         a.groups = 1
-    for (kind, name), t in zip(spec.fields, tensors):
+    for (name, kind), t in zip(spec.items(), tensors):
         if t is None:
             continue
         p, rows, width, step = _rows(t)
@@ -130,17 +138,6 @@ def _intake(a, spec, *tensors):
             setattr(a, "ld_" + name, step)
 
 
-if getattr(_f._binding, "intake", None) is not None:
-    _f._binding.intake_types(torch.float32, torch.bfloat16, torch.float16)
-    _fast_intake = _f._binding.intake
-
-    def _take(a, at, spec, *tensors):
-        _fast_intake(at, spec.words, *tensors)
-else:
-    def _take(a, at, spec, *tensors):
-        _intake(a, spec, *tensors)
-
-
 def _new(like):
     """A new matrix of like's shape and type, without gaps."""
     if like.is_contiguous():
@@ -148,17 +145,19 @@ def _new(like):
     return torch.empty(like.shape, dtype=like.dtype, device=like.device)
 
 
-_DROPOUT = _Spec(_f.DropoutArgs, x=_FIRST, out=_LIKE, residual=_LIKE)
+_DROPOUT = dict(x=_FIRST, out=_LIKE, residual=_LIKE)
 
 
 def dropout(x, draws: Draws, *, residual=None, out=None):
     """residual + dropout(x) (fasgd_dropout), in a new tensor or in `out`, which may
     be x or residual.  The gradient of x is dropout(gradient, draws)."""
+    if _fast is not None:
+        return _done(_fast.dropout(x, draws, residual, out))
     a = _f.DropoutArgs()
     at = ctypes.addressof(a)
     if out is None:
         out = _new(x)
-    _take(a, at, _DROPOUT, x, out, residual)
+    _intake(a, _DROPOUT, x, out, residual)
     a.rate, a.seed, a.client, a.n = draws
     _check(_f.fasgd_dropout(at, _stream(x)))
     return out
@@ -170,7 +169,7 @@ class Joined:
     __slots__ = ("h", "z", "args", "x", "y", "parameters", "stats")
 
 
-_JOIN = _Spec(_f.JoinArgs, x=_FIRST, y=_LIKE, h=_LIKE, z=_LIKE, post=_VECTOR, post_bias=_VECTOR, gate=_GATE,
+_JOIN = dict(x=_FIRST, y=_LIKE, h=_LIKE, z=_LIKE, post=_VECTOR, post_bias=_VECTOR, gate=_GATE,
               pre=_VECTOR, pre_bias=_VECTOR)
 
 
@@ -179,16 +178,21 @@ def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=
     """fasgd_join: h = carry x + branch gate dropout(N(y; post)), z = N(h; pre).
     gate: fp32 [cols], or [groups, cols] of fp32 or x's type, groups dividing the
     rows.  h, z: where to write them (new tensors if None)."""
+    j = Joined()
+    j.x, j.y, j.parameters = x, y, (post, post_bias, gate, pre, pre_bias)
+    if _fast is not None:
+        j.h, j.z, j.stats, j.args = _done(_fast.join(x, y, post, post_bias, gate, pre, pre_bias, _NORMS[norm], eps, carry,
+                                                     branch, draws, h, z))
+        return j
     if (h is not None and y is None) or (z is not None and pre is None):
         raise ValueError("h goes with y, z with pre")
     if y is not None and h is None:
         h = _new(x)
     if pre is not None and z is None:
         z = _new(x)
-    j = Joined()
-    a = j.args = _f.JoinArgs()
+    a = _f.JoinArgs()
     at = ctypes.addressof(a)
-    _take(a, at, _JOIN, x, y, h, z, post, post_bias, gate, pre, pre_bias)
+    _intake(a, _JOIN, x, y, h, z, post, post_bias, gate, pre, pre_bias)
     a.norm = _NORMS[norm]
     a.eps = eps
     a.carry = carry
@@ -198,8 +202,7 @@ def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=
     j.stats = torch.empty(4 * a.rows, dtype=torch.float32, device=x.device)
     a.stats = j.stats.data_ptr() or _NOWHERE
     _check(_f.fasgd_join(at, _stream(x)))
-    j.h, j.z, j.x, j.y = h, z, x, y
-    j.parameters = (post, post_bias, gate, pre, pre_bias)
+    j.h, j.z, j.args = h, z, bytes(a)
     return j
 
 
@@ -217,7 +220,10 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
     """fasgd_join_grad: the gradients of ``join``'s x, y and parameters from those
     of its h (None: zero) and z.  x, y, the parameters and the stream's order are
     to be as they were.  into: where to write them (new tensors where None)."""
-    a, x = _f.JoinArgs.from_buffer_copy(j.args), j.x
+    x = j.x
+    if _fast is not None:
+        return JoinGrads(*_done(_fast.join_grad(j.args, x, j.y, dh, dz, j.parameters, into or _NO_GRADS)))
+    a = _f.JoinArgs.from_buffer_copy(j.args)
     at = ctypes.addressof(a)
     dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias = into if into is not None else _NO_GRADS
     post, post_bias, gate, pre, pre_bias = j.parameters
@@ -242,7 +248,7 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
             raise ValueError("the gate's gradient must be as the gate")
         a.dgate = dgate.data_ptr()
     groups = a.groups
-    _take(a, at, _JOIN_GRAD, x, dh, dz, dx, dy, dpost, dpost_bias, dpre, dpre_bias)
+    _intake(a, _JOIN_GRAD, x, dh, dz, dx, dy, dpost, dpost_bias, dpre, dpre_bias)
     a.groups = groups
     size = _check(_f.fasgd_join_workspace(at))
     space = torch.empty(size, dtype=torch.uint8, device=x.device)
@@ -253,7 +259,7 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
 
 
 _NO_GRADS = JoinGrads()
-_JOIN_GRAD = _Spec(_f.JoinArgs, x=_FIRST, dh=_LIKE, dz=_LIKE, dx=_LIKE, dy=_LIKE, dpost=_VECTOR, dpost_bias=_VECTOR,
+_JOIN_GRAD = dict(x=_FIRST, dh=_LIKE, dz=_LIKE, dx=_LIKE, dy=_LIKE, dpost=_VECTOR, dpost_bias=_VECTOR,
                    dpre=_VECTOR, dpre_bias=_VECTOR)
 
 
@@ -263,17 +269,19 @@ class Balance(NamedTuple):
     dlogits: object    # as logits, or None
 
 
-_BALANCE = _Spec(_f.BalanceArgs, logits=_FIRST, dlogits=_LIKE)
+_BALANCE = dict(logits=_FIRST, dlogits=_LIKE)
 
 
 def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstream=None, grad=True) -> Balance:
     """fasgd_balance: a router's balance and z losses, its per-expert counts, and
     (grad) the gradient of the logits, times `upstream` (a device fp32 value) if
     given.  chosen: int32 [..., top]; valid: bool or uint8, one per row."""
+    if _fast is not None:
+        return Balance(*_done(_fast.balance(logits, chosen, balance, z, groups, valid, upstream, bool(grad))))
     a = _f.BalanceArgs()
     at = ctypes.addressof(a)
     dlogits = _new(logits) if grad else None
-    _take(a, at, _BALANCE, logits, dlogits)
+    _intake(a, _BALANCE, logits, dlogits)
     rows = a.rows
     a.groups = groups
     a.top = top = chosen.shape[-1]

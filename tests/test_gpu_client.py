@@ -650,50 +650,71 @@ def test_automatic_differentiation():
     assert torch.equal(torch.cat((loss.detach().reshape(1), parts)), b.loss)
 
 
-def test_both_intakes_agree():
-    """The C module's intake against client.py's own, which serves where Python's
-    headers were missing: the same struct, and the same refusals."""
-    import ctypes
-    import torch
-    from paper_1601_04033_gb300 import fasgd
+@pytest.fixture(params=["module", "python"])
+def form(request, monkeypatch):
+    """Both forms of the marshalling: client_torch.cpp's module, and client.py's own,
+    which serves where torch's headers were missing."""
     c = _c()
-    if getattr(fasgd._binding, "intake", None) is None:
-        pytest.skip("built without Python's headers")
-    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")   # noqa: E731
-    w, h = z(24, dtype=torch.float32), z(24, dtype=torch.float16)
-    wide = z(10, 40)
-    cube = z(4, 5, 24)
-    fine = [(z(6, 24), z(6, 24), None, None, w, None, w, w, None), (z(24), None, None, None, None, None, None, w, w),
-            (wide[:, :24], wide[:, 16:], None, None, w, None, z(2, 24), None, None),
-            (cube, cube, cube, None, w, w, z(5, 24, dtype=torch.float32), None, None), (z(1, 24), z(1, 24)) + (None,) * 7,
-            (cube[:, :1], None, None, None, None, None, None, w, None), (cube[:1], None, None, None, None, None, None, w, None),
-            (z(0, 24), z(0, 24)) + (None,) * 7, (z(3, 1)[:, :1], None) + (None,) * 7]
-    bad = [(z(6, 24).t(),) + (None,) * 8, (z(6, 24).cpu(),) + (None,) * 8, (z(6, 24, dtype=torch.float64),) + (None,) * 8,
-           (z(6, 24), z(5, 24)) + (None,) * 7, (z(6, 24), z(6, 24, dtype=torch.float16)) + (None,) * 7,
-           (cube[:, :3], None) + (None,) * 7, (cube.transpose(0, 1), None) + (None,) * 7, (torch.zeros((), device="cuda"),) + (None,) * 8,
-           (z(6, 24), None, None, None, h, None, None, None, None), (z(6, 24), None, None, None, w[:12]) + (None,) * 4,
-           (z(6, 12), None, None, None, w[::2]) + (None,) * 4, (z(6, 24), None, None, None, None, None, z(2, 12), None, None),
-           (z(6, 24), None, None, None, None, None, z(2, 2, 24), None, None), (z(6, 24), None, None, None, None, None, z(4, 24)[::2], None, None),
-           (3,) + (None,) * 8]
-    for tensors in fine + bad:
-        got = []
-        for form in (lambda a, s, *t: fasgd._binding.intake(ctypes.addressof(a), s.words, *t), c._intake):
-            a = fasgd.JoinArgs()
-            try:
-                form(a, c._JOIN, *tensors)
-                got.append(bytes(a))
-            except (ValueError, AttributeError, TypeError):
-                got.append("refused")
-        if any(tensors is f for f in fine):
-            a, b = (fasgd.JoinArgs.from_buffer_copy(g) for g in got)
-            for name, _ in fasgd.JoinArgs._fields_:
-                same = name.startswith("ld_") and a.rows < 2       # not looked at
-                assert same or getattr(a, name) == getattr(b, name), (name, [None if t is None else t.shape for t in tensors])
-        else:
-            assert got == ["refused", "refused"], [None if t is None else getattr(t, "shape", t) for t in tensors]
+    if request.param == "module":
+        if c._fast is None:
+            pytest.skip("built without torch's headers")
+    else:
+        monkeypatch.setattr(c, "_fast", None)
+    return request.param
 
 
-def test_refusals_on_tensors():
+def test_the_module_is_built():
+    """Here torch's headers are installed."""
+    from paper_1601_04033_gb300 import build
+    assert _c()._fast is not None or build.torch_home() is None
+
+
+def shapes_of_join():
+    """(x, y, post, gate, pre) of every form that a join takes, with its gradients' ends."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(8)
+
+    def z(*s, dtype=torch.bfloat16):
+        return torch.randn(*s, generator=gen, device="cuda").to(dtype)
+    w, wide, cube = z(24, dtype=torch.float32), z(10, 48), z(4, 5, 24)
+    return [(z(6, 24), z(6, 24), w, w, w), (z(24), None, None, None, w), (wide[:, :24], wide[:, 24:], w, z(2, 24), None),
+            (cube, z(4, 5, 24), w, z(5, 24, dtype=torch.float32), w), (z(1, 24), z(1, 24), None, None, None),
+            (cube[:, :1], None, None, None, w), (cube[:1], cube[1:2], None, None, w), (z(0, 24), z(0, 24), w, w, w),
+            (z(3, 1), z(3, 1), None, None, None)]
+
+
+def test_both_forms_agree(monkeypatch):
+    import torch
+    c = _c()
+    if c._fast is None:
+        pytest.skip("built without torch's headers")
+    fast = c._fast
+
+    def both(call):
+        out = []
+        for m in (fast, None):
+            monkeypatch.setattr(c, "_fast", m)
+            out.append(call())
+        for a, b in zip(*out):
+            assert (a is None) == (b is None)
+            if a is not None:
+                assert a.shape == b.shape and a.dtype == b.dtype and a.is_contiguous() == b.is_contiguous()
+                assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+    for x, y, post, gate, pre in shapes_of_join():
+        def step():
+            j = c.join(x, y, post=post, gate=gate, pre=pre, draws=draws(0.3), carry=0.9)
+            return [j.h, j.z, *c.join_grad(j, x, x if pre is not None else None)]
+        both(step)
+        both(lambda: [c.dropout(x, draws(0.3)), c.dropout(x, draws(0.3), residual=y)])
+    for groups, valid in ((1, None), (3, torch.arange(30, device="cuda") % 4 > 0)):
+        logits, chosen, _ = routed(30, 9, 2, "float16")
+        up = torch.full((1,), 2.0, device="cuda")
+        both(lambda: c.balance(logits, chosen, groups=groups, valid=valid, z=0.1, upstream=up))
+        both(lambda: c.balance(logits, chosen, groups=groups, valid=valid, grad=False))
+
+
+def test_refusals_on_tensors(form):
     import torch
     from paper_1601_04033_gb300 import fasgd
     c = _c()
@@ -705,6 +726,14 @@ def test_refusals_on_tensors():
                 lambda: c.join(x, pre=w.half()), lambda: c.join(x, pre=w[:4]), lambda: c.join(x, x, gate=w[:4]),
                 lambda: c.join(x, pre=torch.ones(16, device="cuda")[::2]),
                 lambda: c.balance(x, torch.zeros(4, 2, dtype=torch.int64, device="cuda")),
+                lambda: c.join(x.view(2, 2, 8)[:, :1].expand(2, 2, 8), pre=w), lambda: c.join(x, y=x.clone(), h=x[:2]),
+                lambda: c.join(x, pre=w, h=x.clone()), lambda: c.join(x, x.clone(), gate=torch.ones(2, 2, 8, device="cuda")),
+                lambda: c.dropout(torch.zeros((), device="cuda"), draws(0.5)), lambda: c.join(torch.zeros(4, 4, 8, device="cuda")[:, :3], pre=w),
+                lambda: c.join_grad(c.join(x, x.clone(), pre=w), x, x[:2]), lambda: c.join_grad(c.join(x, pre=w), x, x, into=c.JoinGrads(pre=w[:4])),
+                lambda: c.join_grad(c.join(x, x.clone(), gate=w), x, into=c.JoinGrads(gate=w.half())),
+                lambda: c.balance(x, torch.zeros(4, 2, dtype=torch.int32, device="cuda"), valid=torch.ones(3, device="cuda").bool()),
+                lambda: c.balance(x, torch.zeros(4, 2, dtype=torch.int32, device="cuda"), valid=torch.ones(4, device="cuda")),
+                lambda: c.balance(x, torch.zeros(4, 2, dtype=torch.int32, device="cuda"), upstream=torch.ones(2, device="cuda")),
                 lambda: c.balance(x, torch.zeros(3, 2, dtype=torch.int32, device="cuda"))):
         with pytest.raises(ValueError):
             bad()
