@@ -152,7 +152,7 @@ def build_client(force: bool = False) -> str | None:
     cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-Wno-deprecated-declarations", "-shared", "-fPIC",
            "-fvisibility=hidden", f'-DBUILT_FOR_TORCH="{version}"', CLIENT_SRC, f"-I{include}", f"-I{INCLUDE}",
            *[f"-isystem{d}" for d in (os.path.join(home, "include"), os.path.join(cuda, "include"))],
-           f"-L{PKG}", "-lfasgd", f"-L{lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+           f"-L{PKG}", "-lfasgd", f"-L{lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
            "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{lib}", "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

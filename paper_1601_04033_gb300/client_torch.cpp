@@ -16,7 +16,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -89,8 +89,19 @@ Matrix like(const Tensor& t, const Tensor& first) {
         wrong("matrices of one shape and type are expected");
     return Matrix(t);
 }
-Tensor fresh(const Tensor& like) { return at::empty(like.sizes(), like.options()); }
-Tensor fresh(int64_t n, at::ScalarType type, const Tensor& like) { return at::empty({n}, like.options().dtype(type)); }
+/* New tensors on like's device, without gaps. */
+Tensor fresh(at::IntArrayRef size, at::ScalarType type, const Tensor& like) {
+    return at::detail::empty_cuda(size, type, like.device(), std::nullopt);
+}
+Tensor fresh(const Tensor& like) { return fresh(like.sizes(), like.scalar_type(), like); }
+Tensor fresh(int64_t n, at::ScalarType type, const Tensor& like) { return fresh(at::IntArrayRef(&n, 1), type, like); }
+/* `size` values of `flat` from `offset` on, as a tensor that shares its memory. */
+Tensor part(const Tensor& flat, int64_t offset, at::IntArrayRef size) {
+    Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(flat.storage()), flat.key_set(), flat.dtype());
+    t.unsafeGetTensorImpl()->set_storage_offset(offset);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+    return t;
+}
 
 float* vector(const Tensor* t, int64_t cols) {
     if (t == nullptr) return nullptr;
@@ -310,12 +321,25 @@ PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             matrix(1, a.dy, a.ld_dy);
         else
             out[1] = Py_None;
+        // The parameters' new fp32 gradients share one allocation (one costs 1.4 us).
+        int64_t values = 0;
+        for (int i = 0; i < 5; ++i) {
+            const Tensor* of = tensor(PyTuple_GET_ITEM(args[5], i));
+            if (of != nullptr && into[2 + i] == Py_None && of->scalar_type() == at::kFloat) values += (of->numel() + 3) / 4 * 4;
+        }
+        Tensor flat;
+        if (values > 0) flat = fresh(values, at::kFloat, *x);
+        values = 0;
         void* at[5];
         for (int i = 0; i < 5; ++i) {
             const Tensor *of = tensor(PyTuple_GET_ITEM(args[5], i)), *t = tensor(into[2 + i]);
             at[i] = nullptr;
             if (of == nullptr) {
                 out[2 + i] = Py_None;
+            } else if (t == nullptr && of->scalar_type() == at::kFloat) {
+                made[2 + i] = part(flat, values, of->sizes());
+                values += (of->numel() + 3) / 4 * 4;
+                at[i] = address(*made[2 + i]);
             } else if (t == nullptr) {
                 made[2 + i] = fresh(*of);
                 at[i] = address(*made[2 + i]);
@@ -386,7 +410,8 @@ PyObject* py_balance(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             a.dlogits = address(*dlogits);
             a.ld_dlogits = m.cols;
         }
-        const Tensor counts = at::empty({a.groups, m.cols}, logits->options().dtype(at::kInt));
+        const int64_t shape[2] = {a.groups, m.cols};
+        const Tensor counts = fresh(shape, at::kInt, *logits);
         const Tensor loss = fresh(3, at::kFloat, *logits), space = fresh(size, at::kByte, *logits);
         a.counts = static_cast<int32_t*>(address(counts));
         a.loss = static_cast<float*>(address(loss));
