@@ -11,7 +11,8 @@
 namespace fasgd {
 namespace {
 
-constexpr int kCountThreads = 1024;
+constexpr int kCountThreads = 1024;     // of a block in a cluster; 256 of one alone
+constexpr int64_t kCountAlone = 2048, kSplitsAlone = 16;    // entries a block counts alone, blocks of a group that do
 constexpr int kCountCluster = 8;        // blocks that count one split together
 constexpr int kThreads = 256;
 
@@ -48,8 +49,8 @@ __device__ __forceinline__ void count_rows(const BalanceArgs& a, int64_t r0, int
     }
 }
 
-// Counts of one split of one group's rows: a block's where a group is one split,
-// else a cluster's, whose blocks add up their counts, a share of the experts each.
+// Counts of one split of one group's rows: a block's, or (long splits) a cluster's,
+// whose blocks add up their counts, a share of the experts each.
 __global__ void __launch_bounds__(kCountThreads)
     balance_count_kernel(const __grid_constant__ BalanceArgs a, int blocks) {
     __shared__ int32_t hist[FASGD_EXPERTS_MAX + 1];      // and the rows that take part
@@ -63,20 +64,20 @@ __global__ void __launch_bounds__(kCountThreads)
         const int64_t group = unit / a.splits, piece = (unit - group * a.splits) * blocks + rank;
         const int64_t from = piece * per < a.group_rows ? piece * per : a.group_rows;
         const int64_t to = from + per < a.group_rows ? from + per : a.group_rows;
-        for (int e = threadIdx.x; e <= cols; e += kCountThreads) hist[e] = 0;
+        for (int e = threadIdx.x; e <= cols; e += blockDim.x) hist[e] = 0;
         __syncthreads();
         if (a.valid == nullptr && threadIdx.x == 0) hist[cols] = (int32_t)(to - from);
         count_rows<16>(a, group * a.group_rows + from, group * a.group_rows + to, hist, &hist[cols]);
         __syncthreads();
         int32_t* out = a.splits > 1 ? a.part_counts + unit * cols : a.counts + group * cols;
         if (blocks == 1) {
-            for (int e = threadIdx.x; e <= cols; e += kCountThreads)
+            for (int e = threadIdx.x; e <= cols; e += blockDim.x)
                 *(e < cols ? out + e : a.part_valid + unit) = hist[e];
             __syncthreads();
             continue;
         }
         cluster_barrier();
-        for (int e = rank * kCountThreads + threadIdx.x; e <= cols; e += blocks * kCountThreads) {
+        for (int e = rank * blockDim.x + threadIdx.x; e <= cols; e += blocks * blockDim.x) {
             int32_t s = 0, v[kCountCluster];
 #pragma unroll
             for (int k = 0; k < kCountCluster; ++k) {
@@ -128,6 +129,7 @@ __device__ __forceinline__ Totals totals(const BalanceArgs& a, float2* smem) {
         float n = 0.f, g1 = 0.f;
         for (int64_t g = threadIdx.x; g < a.groups; g += kThreads) {
             int32_t v = 0;
+#pragma unroll 4
             for (int64_t s = 0; s < a.splits; ++s) v += a.part_valid[g * a.splits + s];
             n += (float)v;
             g1 += v > 0 ? 1.f : 0.f;
@@ -144,13 +146,18 @@ __device__ __forceinline__ Totals totals(const BalanceArgs& a, float2* smem) {
 // to add them up and `write` says so); returns 1 / N_g, or 0.
 __device__ __forceinline__ float group_shares(const BalanceArgs& a, int64_t group, bool write, float* f) {
     const int cols = (int)a.cols;
-    int32_t n = 0;
-    for (int64_t s = 0; s < a.splits; ++s) n += a.part_valid[group * a.splits + s];
+    int32_t n = (int32_t)a.group_rows;
+    if (a.valid != nullptr) {
+        n = 0;
+#pragma unroll 4
+        for (int64_t s = 0; s < a.splits; ++s) n += a.part_valid[group * a.splits + s];
+    }
     const float inv_n = n > 0 ? 1.f / (float)n : 0.f;
     __syncthreads();
     for (int e = threadIdx.x; e < cols; e += kThreads) {
         int32_t c = 0;
         if (a.splits > 1) {
+#pragma unroll 8
             for (int64_t s = 0; s < a.splits; ++s) c += a.part_counts[(group * a.splits + s) * cols + e];
             if (write) a.counts[group * cols + e] = c;
         } else {
@@ -463,11 +470,11 @@ cudaError_t launch(const BalanceArgs& a, int num_sms, cudaStream_t stream) {
     const int64_t octets = row_octets(a.cols);
     const bool fast = in_octets(a, (int)sizeof(T));
     if (!(fast && balance_alone(a, kThreads / lanes_per_row(octets)))) {
-        // A cluster for more than two entries a thread of a block.
-        const int blocks = a.group_rows / a.splits * a.top > 2 * kCountThreads ? kCountCluster : 1;
-        const int64_t units = a.groups * a.splits, cap = (int64_t)num_sms * 2 / blocks;
-        const cudaError_t st = launch_rows_kernel<balance_count_kernel>((units < cap ? units : cap) * blocks, kCountThreads,
-                                                                        0, blocks, stream, a, blocks);
+        const bool cluster = a.group_rows * a.top > kCountAlone * kSplitsAlone;
+        const int blocks = cluster ? kCountCluster : 1;
+        const int64_t units = a.groups * a.splits, cap = (int64_t)num_sms * (cluster ? 2 : 8) / blocks;
+        const cudaError_t st = launch_rows_kernel<balance_count_kernel>(
+            (units < cap ? units : cap) * blocks, cluster ? kCountThreads : 256, 0, blocks, stream, a, blocks);
         if (st != cudaSuccess) return st;
     }
     if (fast)
@@ -482,13 +489,18 @@ cudaError_t launch(const BalanceArgs& a, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
-// Splits of each group in the counting, one for each 65,536 assignments, and 19 at
-// most: a cluster of eight blocks each then fills 152 SMs, and every block of the
-// pass adds up its group's.
+// Splits of each group in the counting (every block of the pass adds up its
+// group's): up to 16 blocks of 1,024 assignments or more; past 32,768 a cluster of
+// eight blocks for each 65,536, 19 at most (they fill 152 SMs).
 int64_t balance_splits(int64_t rows, int64_t groups, int64_t top) {
     if (groups < 1) return 1;
-    const int64_t s = (rows / groups * top + 65535) / 65536;
-    return s < 1 ? 1 : s > 19 ? 19 : s;
+    const int64_t n = rows / groups * top;
+    int64_t s = (n + 1023) / 1024;
+    if (n > kCountAlone * kSplitsAlone) {
+        s = (n + 65535) / 65536;
+        return s > 19 ? 19 : s;
+    }
+    return s < 1 ? 1 : s > kSplitsAlone ? kSplitsAlone : s;
 }
 
 cudaError_t launch_balance(const BalanceArgs& a, int dtype, int num_sms, cudaStream_t stream) {
