@@ -81,7 +81,8 @@ struct RowSteps {
 };
 constexpr int kForwardStages = 3;
 constexpr int kForwardThreads = 512;      // of an SM
-template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP>
+// FULL: with y and both norms.
+template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP, bool FULL>
 __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8 ? 16 : 1)
     join_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ RowSteps s, int blocks) {
     constexpr int kP = kPieces<T>, STAGES = kForwardStages;
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
     const int64_t turns = ahead < a.rows ? ((a.rows - ahead + step - 1) / step + NR - 1) / NR : 0;
     const Columns c(th.octet(), RAGGED ? (int)((first * a.cols) & 7) : 0, (int32_t)a.cols);
     RowSums<TPR, NR> sums(th, red);
-    const bool has_y = a.y != nullptr, has_pre = a.pre != nullptr, has_post = a.post != nullptr;
+    const bool has_y = FULL || a.y != nullptr, has_pre = FULL || a.pre != nullptr, has_post = FULL || a.post != nullptr;
     constexpr int kSlots = 2 * NR * kP * kLane;      // of a warp's stage
     uint4* const mine = ring + (threadIdx.x >> 5) * kSlots;
     const int stage_size = kSlots * th.warps;
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
     }
 }
 
-template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP>
+template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP, bool FULL>
 cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
     const size_t smem = (size_t)kForwardStages * 2 * NR * kPieces<T> * s.threads * 16;
     int64_t grid = (a.rows + s.rows - 1) / s.rows;
@@ -255,15 +256,20 @@ cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, int num_sms, cudaS
     if (grid > cap) grid = cap;
     const int64_t rows = grid * s.rows, bytes = rows * (int64_t)sizeof(T);
     const RowSteps steps = {rows, bytes * a.ld_x, bytes * a.ld_y, bytes * a.ld_h, bytes * a.ld_z, rows * a.cols / 8};
-    return launch_rows_kernel<join_rows_kernel<T, TPR, NR, LAYER, RAGGED, DROP>>(grid * s.blocks, s.threads, smem, s.blocks,
-                                                                                 stream, a, steps, s.blocks);
+    return launch_rows_kernel<join_rows_kernel<T, TPR, NR, LAYER, RAGGED, DROP, FULL>>(
+        grid * s.blocks, s.threads, smem, s.blocks, stream, a, steps, s.blocks);
 }
 template <class T, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
-    if (s.rows > 1) return launch_rows<T, 8, 2, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
+    if (s.rows > 1) return launch_rows<T, 8, 2, LAYER, RAGGED, DROP, false>(a, s, num_sms, stream);
     // Two rows a turn, but where a row takes more threads than have the registers for it.
-    if (s.threads > 512) return launch_rows<T, 0, 1, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
-    return launch_rows<T, 0, 2, LAYER, RAGGED, DROP>(a, s, num_sms, stream);
+    if (s.threads > 512) return launch_rows<T, 0, 1, LAYER, RAGGED, DROP, false>(a, s, num_sms, stream);
+    // FULL where it gains (32768 x 4096 bf16 with dropout 181 us, 210 without it) and
+    // not where it costs (32768 x 2048 rms norm, nothing dropped: 91 us, 82 without it).
+    if constexpr (LAYER || DROP)
+        if (a.y != nullptr && a.post != nullptr && a.pre != nullptr)
+            return launch_rows<T, 0, 2, LAYER, RAGGED, DROP, true>(a, s, num_sms, stream);
+    return launch_rows<T, 0, 2, LAYER, RAGGED, DROP, false>(a, s, num_sms, stream);
 }
 template <class T, bool LAYER>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
