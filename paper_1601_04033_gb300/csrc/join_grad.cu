@@ -13,10 +13,9 @@ cudaError_t launch_join_grad_f16(const JoinArgs& a, int num_sms, cudaStream_t st
 // sub, a unit costing about four more to begin and to leave its sums.
 static int64_t best_splits(int64_t groups, int64_t rows, int64_t most, int64_t step) {
     int64_t best = step, least = INT64_MAX;
-    for (int64_t s = step, tried = 0; s <= rows && tried < 64; s += step, ++tried) {
-        // Past one unit for each sub in steps that fill whole rounds of them.
-        if (tried > 0 && groups * s > most) s = ((groups * s + most - 1) / most * most / groups + step - 1) / step * step;
-        if (s > rows) break;
+    for (int64_t rounds = 0; rounds <= 16; ++rounds) {        // the most splits of so many units a sub
+        int64_t s = rounds * most / groups / step * step;
+        s = s < step ? step : s > rows ? rows / step * step : s;
         const int64_t cost = (groups * s + most - 1) / most * ((rows + s - 1) / s + 4);
         if (cost < least) {
             least = cost;

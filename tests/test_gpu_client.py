@@ -92,7 +92,7 @@ def check_join(a, dh, dz, norm="rms", eps=1e-5, carry=0.9, branch=0.7, rate=0.0,
 
 
 WIDTHS = [1, 2, 7, 8, 9, 24, 63, 64, 65, 200, 255, 256, 257, 500, 512, 784, 1000, 1021, 1024, 1031, 2000, 2047,
-          2048, 2056, 4096, 4099, 5000, 8184, 8191, 8192, 8193, 8200, 16384, 20001]
+          2048, 2056, 4096, 4099, 5000, 8184, 8191, 8192, 8193, 8200, 16384, 20001, 32768, 32776, 40001]
 
 
 @pytest.mark.parametrize("D", WIDTHS)
