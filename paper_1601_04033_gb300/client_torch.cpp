@@ -5,8 +5,8 @@
  *
  * Why: a small call is bound by the host.  On a GB300's Arm cores each call from
  * Python into torch costs 1.4 us by itself and up to 3.7 us next to a kernel
- * launch, and a join with its gradients makes eleven new tensors: 50 us from
- * Python, about a third of it here (client.py says what it measured).
+ * launch, and a join with its gradients makes eleven new tensors: 51 us from
+ * Python for 128 rows of 200.
  *
  * client.py holds the same code in Python, which serves where torch's headers were
  * not installed when the library was built; tests compare the two.  Built for
@@ -22,8 +22,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
-#include <optional>
+#include <initializer_list>
 #include <stdexcept>
+#include <type_traits>
 
 #include "fasgd.h"
 
@@ -89,19 +90,63 @@ Matrix like(const Tensor& t, const Tensor& first) {
         wrong("matrices of one shape and type are expected");
     return Matrix(t);
 }
-/* New tensors on like's device, without gaps. */
-Tensor fresh(at::IntArrayRef size, at::ScalarType type, const Tensor& like) {
-    return at::detail::empty_cuda(size, type, like.device(), std::nullopt);
-}
-Tensor fresh(const Tensor& like) { return fresh(like.sizes(), like.scalar_type(), like); }
-Tensor fresh(int64_t n, at::ScalarType type, const Tensor& like) { return fresh(at::IntArrayRef(&n, 1), type, like); }
-/* `size` values of `flat` from `offset` on, as a tensor that shares its memory. */
-Tensor part(const Tensor& flat, int64_t offset, at::IntArrayRef size) {
-    Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(flat.storage()), flat.key_set(), flat.dtype());
-    t.unsafeGetTensorImpl()->set_storage_offset(offset);
-    t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
-    return t;
-}
+/* The new tensors of a call, on one device and without gaps.  Each would cost
+ * 1.4 us of the host, so where all of them are small (1 MiB together) they share
+ * one allocation, and one that outlives the others keeps no more than that. */
+class New {
+  public:
+    explicit New(const Tensor& like) : device_(like.device()) {}
+    /* Announces a tensor, whose address will be in *p after make(). */
+    template <class P>
+    int add(at::IntArrayRef size, at::ScalarType type, P** p) {
+        Item& i = items_[count_];
+        i.size.assign(size.begin(), size.end());
+        i.type = type;
+        i.p = reinterpret_cast<void**>(p);
+        i.bytes = (int64_t)c10::elementSize(type);
+        for (const int64_t s : size) i.bytes *= s;
+        total_ += (i.bytes + 255) / 256 * 256;
+        return count_++;
+    }
+    template <class P>
+    int add(int64_t n, at::ScalarType type, P** p) { return add(at::IntArrayRef(&n, 1), type, p); }
+    template <class P>
+    int add(const Tensor& like, P** p) { return add(like.sizes(), like.scalar_type(), p); }
+    void make() {
+        const bool shared = count_ > 1 && total_ <= kShared;
+        Tensor base;
+        if (shared && total_ > 0) base = at::detail::empty_cuda({total_}, at::kByte, device_, std::nullopt);
+        int64_t at = 0;
+        for (int k = 0; k < count_; ++k) {
+            Item& i = items_[k];
+            if (base.defined() && i.bytes > 0) {
+                i.tensor = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(),
+                                                                    c10::scalarTypeToTypeMeta(i.type));
+                i.tensor.unsafeGetTensorImpl()->set_storage_offset(at / (int64_t)c10::elementSize(i.type));
+                i.tensor.unsafeGetTensorImpl()->set_sizes_contiguous(i.size);
+                at += (i.bytes + 255) / 256 * 256;
+            } else {
+                i.tensor = at::detail::empty_cuda(i.size, i.type, device_, std::nullopt);
+            }
+            *i.p = address(i.tensor);
+        }
+    }
+    PyObject* object(int k) const { return THPVariable_Wrap(items_[k].tensor); }
+
+  private:
+    static constexpr int64_t kShared = 1 << 20;
+    struct Item {
+        c10::SmallVector<int64_t, 5> size;
+        at::ScalarType type;
+        int64_t bytes;
+        void** p;
+        Tensor tensor;
+    };
+    c10::Device device_;
+    Item items_[10];
+    int count_ = 0;
+    int64_t total_ = 0;
+};
 
 float* vector(const Tensor* t, int64_t cols) {
     if (t == nullptr) return nullptr;
@@ -150,10 +195,9 @@ int64_t whole(PyObject* o) {
     return v;
 }
 
-PyObject* object(const Tensor& t) { return THPVariable_Wrap(t); }
-/* The tensor of a call: the caller's own object where there was one. */
-PyObject* object(PyObject* given, const std::optional<Tensor>& made) {
-    if (made) return object(*made);
+/* A result: the caller's own object, or (k >= 0) a new tensor. */
+PyObject* object(const New& made, int k, PyObject* given) {
+    if (k >= 0) return made.object(k);
     Py_INCREF(given);
     return given;
 }
@@ -212,14 +256,20 @@ PyObject* py_dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             a.residual = r.p;
             a.ld_residual = r.ld;
         }
-        std::optional<Tensor> made;
-        if (out == nullptr) made = fresh(*x);
-        const Matrix o = like(made ? *made : *out, *x);
-        a.out = o.p;
-        a.ld_out = o.ld;
+        New made(*x);
+        int k = -1;
+        if (out == nullptr) {
+            k = made.add(*x, &a.out);
+            a.ld_out = m.cols;
+        } else {
+            const Matrix o = like(*out, *x);
+            a.out = o.p;
+            a.ld_out = o.ld;
+        }
         void* s = stream(*x);
+        made.make();
         unlocked([&] { return (int64_t)fasgd_dropout(&a, s); });
-        return object(args[3], made);
+        return object(made, k, args[3]);
     });
 }
 
@@ -240,22 +290,25 @@ PyObject* py_join(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         a.ld_x = m.ld;
         a.dtype = dtype_of(*x);
         a.groups = 1;
-        std::optional<Tensor> made_h, made_z;
+        New made(*x);
+        int at_h = -1, at_z = -1;
+        const auto output = [&](const Tensor* t, void*& p, int64_t& ld) {
+            if (t == nullptr) {
+                ld = m.cols;
+                return made.add(*x, &p);
+            }
+            const Matrix o = like(*t, *x);
+            p = o.p;
+            ld = o.ld;
+            return -1;
+        };
         if (y != nullptr) {
             const Matrix k = like(*y, *x);
             a.y = k.p;
             a.ld_y = k.ld;
-            if (h == nullptr) made_h = fresh(*x);
-            const Matrix o = like(made_h ? *made_h : *h, *x);
-            a.h = o.p;
-            a.ld_h = o.ld;
+            at_h = output(h, a.h, a.ld_h);
         }
-        if (pre != nullptr) {
-            if (z == nullptr) made_z = fresh(*x);
-            const Matrix o = like(made_z ? *made_z : *z, *x);
-            a.z = o.p;
-            a.ld_z = o.ld;
-        }
+        if (pre != nullptr) at_z = output(z, a.z, a.ld_z);
         a.post = vector(tensor(args[2]), m.cols);
         a.post_bias = vector(tensor(args[3]), m.cols);
         a.pre = vector(pre, m.cols);
@@ -273,11 +326,11 @@ PyObject* py_join(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         a.carry = real(args[9]);
         a.branch = real(args[10]);
         draws(args[11], a);
-        const Tensor stats = fresh(4 * m.rows, at::kFloat, *x);
-        a.stats = static_cast<float*>(address(stats));
+        const int at_stats = made.add(4 * m.rows, at::kFloat, &a.stats);
         void* s = stream(*x);
+        made.make();
         unlocked([&] { return (int64_t)fasgd_join(&a, s); });
-        return tuple({object(args[12], made_h), object(args[13], made_z), object(stats),
+        return tuple({object(made, at_h, args[12]), object(made, at_z, args[13]), made.object(at_stats),
                       PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&a), sizeof a)});
     });
 }
@@ -306,65 +359,63 @@ PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             a.ld_dz = m.ld;
         }
         PyObject* const* into = &PyTuple_GET_ITEM(args[6], 0);
-        std::optional<Tensor> made[7];
+        New made(*x);
+        int at[7];
         PyObject* out[7];
-        for (int i = 0; i < 7; ++i) out[i] = into[i];
+        for (int i = 0; i < 7; ++i) {
+            out[i] = into[i];
+            at[i] = -1;
+        }
         const auto matrix = [&](int i, void*& p, int64_t& ld) {
             const Tensor* t = tensor(into[i]);
-            if (t == nullptr) made[i] = fresh(*x);
-            const Matrix m = like(made[i] ? *made[i] : *t, *x);
-            p = m.p;
-            ld = m.ld;
+            if (t == nullptr) {
+                at[i] = made.add(*x, &p);
+                ld = a.cols;
+            } else {
+                const Matrix m = like(*t, *x);
+                p = m.p;
+                ld = m.ld;
+            }
         };
         matrix(0, a.dx, a.ld_dx);
         if (y != nullptr)
             matrix(1, a.dy, a.ld_dy);
         else
             out[1] = Py_None;
-        // The parameters' new fp32 gradients share one allocation (one costs 1.4 us).
-        int64_t values = 0;
-        for (int i = 0; i < 5; ++i) {
-            const Tensor* of = tensor(PyTuple_GET_ITEM(args[5], i));
-            if (of != nullptr && into[2 + i] == Py_None && of->scalar_type() == at::kFloat) values += (of->numel() + 3) / 4 * 4;
-        }
-        Tensor flat;
-        if (values > 0) flat = fresh(values, at::kFloat, *x);
-        values = 0;
-        void* at[5];
-        for (int i = 0; i < 5; ++i) {
-            const Tensor *of = tensor(PyTuple_GET_ITEM(args[5], i)), *t = tensor(into[2 + i]);
-            at[i] = nullptr;
+        const auto parameter = [&](int i, auto*& p) {
+            const Tensor *of = tensor(PyTuple_GET_ITEM(args[5], i - 2)), *t = tensor(into[i]);
             if (of == nullptr) {
-                out[2 + i] = Py_None;
-            } else if (t == nullptr && of->scalar_type() == at::kFloat) {
-                made[2 + i] = part(flat, values, of->sizes());
-                values += (of->numel() + 3) / 4 * 4;
-                at[i] = address(*made[2 + i]);
+                out[i] = Py_None;
             } else if (t == nullptr) {
-                made[2 + i] = fresh(*of);
-                at[i] = address(*made[2 + i]);
-            } else if (i == 2) {
+                at[i] = made.add(*of, &p);
+                // What the workspace depends on: that it is there, and aligned.
+                p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(256);
+            } else if (i == 4) {
                 if (t->sizes() != of->sizes() || t->scalar_type() != of->scalar_type() || !t->is_contiguous() || !t->is_cuda())
                     wrong("the gate's gradient must be as the gate");
-                at[i] = address(*t);
+                p = static_cast<std::remove_reference_t<decltype(p)>>(address(*t));
             } else {
-                at[i] = vector(t, a.cols);
+                p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(vector(t, a.cols));
             }
-        }
-        a.dpost = static_cast<float*>(at[0]);
-        a.dpost_bias = static_cast<float*>(at[1]);
-        a.dgate = at[2];
-        a.dpre = static_cast<float*>(at[3]);
-        a.dpre_bias = static_cast<float*>(at[4]);
+        };
+        parameter(2, a.dpost);
+        parameter(3, a.dpost_bias);
+        parameter(4, a.dgate);
+        parameter(5, a.dpre);
+        parameter(6, a.dpre_bias);
         void* s = stream(*x);
+        // New matrices are aligned as the fast kernels want them, wherever they will lie.
+        if (at[0] >= 0) a.dx = reinterpret_cast<void*>(256);
+        if (at[1] >= 0) a.dy = reinterpret_cast<void*>(256);
         const int64_t size = fasgd_join_workspace(&a);
         if (size < 0) throw Status{size};
-        const Tensor space = fresh(size, at::kByte, *x);
-        a.workspace = space.data_ptr();
+        made.add(size, at::kByte, &a.workspace);
         a.workspace_bytes = size;
+        made.make();
         unlocked([&] { return (int64_t)fasgd_join_grad(&a, s); });
-        return tuple({object(out[0], made[0]), object(out[1], made[1]), object(out[2], made[2]), object(out[3], made[3]),
-                      object(out[4], made[4]), object(out[5], made[5]), object(out[6], made[6])});
+        return tuple({object(made, at[0], out[0]), object(made, at[1], out[1]), object(made, at[2], out[2]),
+                      object(made, at[3], out[3]), object(made, at[4], out[4]), object(made, at[5], out[5]),
+                      object(made, at[6], out[6])});
     });
 }
 
@@ -404,22 +455,20 @@ PyObject* py_balance(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         }
         const int64_t size = fasgd_balance_workspace(&a);
         if (size < 0) throw Status{size};
-        std::optional<Tensor> dlogits;
+        New made(*logits);
+        int at_dlogits = -1;
         if (args[7] == Py_True) {
-            dlogits = fresh(*logits);
-            a.dlogits = address(*dlogits);
+            at_dlogits = made.add(*logits, &a.dlogits);
             a.ld_dlogits = m.cols;
         }
         const int64_t shape[2] = {a.groups, m.cols};
-        const Tensor counts = fresh(shape, at::kInt, *logits);
-        const Tensor loss = fresh(3, at::kFloat, *logits), space = fresh(size, at::kByte, *logits);
-        a.counts = static_cast<int32_t*>(address(counts));
-        a.loss = static_cast<float*>(address(loss));
-        a.workspace = space.data_ptr();
+        const int at_counts = made.add(shape, at::kInt, &a.counts), at_loss = made.add(3, at::kFloat, &a.loss);
+        made.add(size, at::kByte, &a.workspace);
         a.workspace_bytes = size;
         void* s = stream(*logits);
+        made.make();
         unlocked([&] { return (int64_t)fasgd_balance(&a, s); });
-        return tuple({object(loss), object(counts), object(Py_None, dlogits)});
+        return tuple({made.object(at_loss), made.object(at_counts), object(made, at_dlogits, Py_None)});
     });
 }
 
