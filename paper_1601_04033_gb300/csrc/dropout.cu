@@ -44,7 +44,9 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_cons
 
 // Whole octets of rows that begin with one (a matrix without gaps is one row): a
 // block takes kThreads * U of them and each thread U, all asked for before the
-// first is used.
+// first is used.  Bound by memory: 65536 x 4096 bf16 with a residual, 1.6 GB, and
+// its gradient, 1.1 GB: 387 us, 6.94 TB/s; six thousand strided rows of 1,000 in
+// 12 us for both, out of L2.
 struct DropoutRows {
     int64_t octets, row_octets;      // of the matrix, of a row
     int64_t turn_rows, turn_octets;  // kThreads octets on: rows, and octets of a row

@@ -75,6 +75,14 @@ __global__ void __launch_bounds__(kThreads) join_any_kernel(const __grid_constan
 // octet each, so x and y are read once; blocks stay and take NR rows at a time, so
 // that two rows share each barrier, the next STAGES - 1 turns' on their way into
 // shared memory.
+//
+// 8 bytes an element (16-bit types), about 33 instructions with dropout, 20 without.
+// 32768 x 4096 bf16 with dropout: 181 us, 5.9 TB/s, where the issue of the draws and
+// the latency of two reductions a row bound it; 32768 x 2048 without: 82 us, 6.6 TB/s,
+// memory.  Layer norms take four reductions: 32768 x 4096 with dropout 270 us.
+// Joining the warps' moments (Chan) in one barrier instead of two costs more
+// arithmetic than the barrier (143 -> 193 us at 32768 x 2048).  One row a turn at
+// 64 registers and twice the blocks: 246 us against 210 for the kernel of that time.
 // From one of a block's rows to the next: bytes in each matrix, octets of draws.
 struct RowSteps {
     int64_t rows, x, y, h, z, octets;
