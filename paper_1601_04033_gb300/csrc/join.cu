@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) join_any_kernel(const __grid_constan
 // 8 bytes an element (16-bit types), about 33 instructions with dropout, 20 without.
 // 32768 x 4096 bf16 with dropout: 181 us, 5.9 TB/s, where the issue of the draws and
 // the latency of two reductions a row bound it; 32768 x 2048 without: 82 us, 6.6 TB/s,
-// memory.  Layer norms take four reductions: 32768 x 4096 with dropout 270 us.
+// memory.  Layer norms take four reductions: 32768 x 4096 with dropout 262 us.
 // Joining the warps' moments (Chan) in one barrier instead of two costs more
 // arithmetic than the barrier (143 -> 193 us at 32768 x 2048).  One row a turn at
 // 64 registers and twice the blocks: 246 us against 210 for the kernel of that time.
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
             mean[j] = v[j] * a.inv_cols;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[j].v[i] = add2(o[j].v[i], f2(-mean[j]));
-            mask(o[j], c);           // 0 where there is no column
+            if (RAGGED) mask(o[j], c);           // 0 where there is no column
         }
     };
     const auto inverse = [&](const Oct (&o)[NR], float (&rstd)[NR]) {
@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
             const float2 p = fma2(o[j].v[0], o[j].v[0], mul2(o[j].v[1], o[j].v[1]));
             const float2 q = fma2(o[j].v[2], o[j].v[2], mul2(o[j].v[3], o[j].v[3]));
             v[j] = (p.x + q.x) + (p.y + q.y);
+            if (LAYER && !RAGGED && !c.any()) v[j] = 0.f;      // (a mean was taken off)
         }
         sums(v);
 #pragma unroll

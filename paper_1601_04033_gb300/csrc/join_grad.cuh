@@ -166,12 +166,12 @@ __host__ __device__ __forceinline__ int64_t gates_left(const JoinArgs& a) {
 // one row ("sub") at a time; where cols is no multiple of 8 a unit's rows agree
 // modulo 8 (octet.cuh).
 //
-// It moves 12 bytes an element (16-bit types) and issues about 55 instructions for
+// It moves 12 bytes an element (16-bit types) and issues about 50 instructions for
 // each, a fifth of them the draws: instructions bound it, not memory.  32768 x 4096
-// bf16 with dropout: 301 us, 5.3 TB/s; without 5.4 to 6.0 TB/s; layer norm with
-// dropout 398 us, 4.0 TB/s; fp32 4.3 TB/s.  512 threads an SM of 128 registers hold
+// bf16 with dropout: 282 us, 5.7 TB/s; without 5.5 to 5.8 TB/s; layer norm with
+// dropout 381 us, 4.2 TB/s; fp32 4.1 TB/s.  512 threads an SM of 128 registers hold
 // the vectors and sums of 4,096 columns; wider rows take a cluster, whose barrier
-// for every row shows: 16384 x 8192 553 us, 2.9 TB/s.
+// for every row shows: 16384 x 8192 545 us, 3.0 TB/s.
 struct Unit {
     int64_t row, step, rows;     // first row, from row to row, one past the last
     __device__ Unit(const JoinArgs& a, int64_t unit) {
@@ -211,7 +211,7 @@ __device__ __forceinline__ Oct held_octet(const float4* p) {
     o.v[3] = make_float2(y.z, y.w);
     return o;
 }
-// FULL: with y, both norms and dh.
+// FULL: with y, both norms and dh, and one ld for what is read, one for what is written.
 template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP, bool FULL>
 __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     grad_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ GradSteps s, int blocks) {
@@ -268,12 +268,12 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
         const int64_t unit = ahead_unit + th.sub;
         Unit u(a, unit < units ? unit : 0);
         if (unit >= units) u.rows = 0;
-        int64_t turns = u.row < u.rows ? (u.rows - u.row + u.step - 1) / u.step : 0;
-        const int64_t rows = turns;
+        int32_t turns = u.row < u.rows ? (int32_t)((u.rows - u.row + u.step - 1) / u.step) : 0;
+        const int32_t rows = turns;
         if constexpr (TPR == 8) {
 #pragma unroll
             for (int off = 16; off >= 8; off >>= 1) {
-                const int64_t other = __shfl_xor_sync(0xffffffffu, turns, off);
+                const int32_t other = __shfl_xor_sync(0xffffffffu, turns, off);
                 turns = other > turns ? other : turns;
             }
         }
@@ -290,24 +290,30 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
         const T* dh = static_cast<const T*>(a.dh) + r0 * a.ld_dh + lane.col;
         const T* dz = static_cast<const T*>(a.dz) + r0 * a.ld_dz + lane.col;
         const float4* stats = a.stats + r0;
-        int64_t unfetched = rows;
+        // FULL: bytes into the matrices instead, which frees ten registers.
+        int64_t in = (r0 * a.ld_x + lane.col) * (int64_t)sizeof(T), out = (r0 * a.ld_dx + c.c0) * (int64_t)sizeof(T);
+        int32_t unfetched = rows;
         const bool clipped = RAGGED && r0 + (rows - 1) * u.step == a.rows - 1;   // the matrix ends with the last row
         const auto fetch = [&](int stage) {
             uint4* slot = own + stage * stage_size;
             if (unfetched > 0) {
                 const bool clip = clipped && unfetched == 1;
                 if (asks) copy_async16(own_stats + stage * kWarpRows * th.warps, stats, 16);
-                lane.copy(slot, x, clip);
-                if (has_y) lane.copy(slot + kP * kLane, y, clip);
-                if (has_dh) lane.copy(slot + 2 * kP * kLane, dh, clip);
-                if (has_pre) lane.copy(slot + 3 * kP * kLane, dz, clip);
+                lane.copy(slot, FULL ? on(static_cast<const T*>(a.x), in) : x, clip);
+                if (has_y) lane.copy(slot + kP * kLane, FULL ? on(static_cast<const T*>(a.y), in) : y, clip);
+                if (has_dh) lane.copy(slot + 2 * kP * kLane, FULL ? on(static_cast<const T*>(a.dh), in) : dh, clip);
+                if (has_pre) lane.copy(slot + 3 * kP * kLane, FULL ? on(static_cast<const T*>(a.dz), in) : dz, clip);
             }
             copy_commit();
             --unfetched;
-            x = on(x, s.x);
-            y = on(y, s.y);
-            dh = on(dh, s.dh);
-            dz = on(dz, s.dz);
+            if (FULL) {
+                in += s.x;
+            } else {
+                x = on(x, s.x);
+                y = on(y, s.y);
+                dh = on(dh, s.dh);
+                dz = on(dz, s.dz);
+            }
             stats = on(stats, s.stats);
         };
 #pragma unroll
@@ -316,7 +322,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
         T* dyp = static_cast<T*>(a.dy) + r0 * a.ld_dy + c.c0;
         int64_t oct = (r0 * a.cols + c.c0) >> 3;         // the row's octet of draws
         int stage = 0;
-        for (int64_t turn = 0; turn < turns; ++turn) {
+        for (int32_t turn = 0; turn < turns; ++turn) {
             const bool live = TPR != 8 || turn < rows;
             Philox4 draws;
             if (DROP) draws = draw_octet(a.drop, oct);
@@ -380,7 +386,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
                 d_gate.v[i] = fma2(d, uu.v[i], d_gate.v[i]);
                 w.v[i] = mul2(e.v[i], d);
             }
-            if (live) store_octet<T, RAGGED>(dxp, c, hhat);
+            if (live) store_octet<T, RAGGED>(FULL ? on(static_cast<T*>(a.dx), out) : dxp, c, hhat);
             if (has_post) {
                 // The means of q2 yhat and (layer norm) of q2.
                 float k1, k0 = 0.f;
@@ -418,9 +424,13 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w.v[i] = mul2(w.v[i], f2(scale));
             }
-            if (live && has_y) store_octet<T, RAGGED>(dyp, c, w);
-            dxp = on(dxp, s.dx);
-            dyp = on(dyp, s.dy);
+            if (live && has_y) store_octet<T, RAGGED>(FULL ? on(static_cast<T*>(a.dy), out) : dyp, c, w);
+            if (FULL) {
+                out += s.dx;
+            } else {
+                dxp = on(dxp, s.dx);
+                dyp = on(dyp, s.dy);
+            }
         }
         copy_wait<0>();
         if (gates && a.out_gate != nullptr && unit < units) {
@@ -508,6 +518,7 @@ bool in_octets(const JoinArgs& a, int size) {
     const int64_t ld[] = {a.ld_x, a.ld_y, a.ld_dh, a.ld_dz, a.ld_dx, a.ld_dy};
     for (int i = 0; i < 6; ++i)
         if (!octet_matrix(p[i], ld[i], a.rows, a.cols, size)) return false;
+    if (a.rows >> 31) return false;        // 32-bit counters of rows
     // A group's rows fall into eight classes where cols is no multiple of 8: short
     // groups would leave more sums than rows.
     if (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64) return false;
@@ -527,7 +538,8 @@ cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, cudaStream_t strea
 template <class T, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {
     if (s.rows > 1) return launch_rows<T, 8, LAYER, RAGGED, DROP, false>(a, s, stream);
-    if (a.y != nullptr && a.post != nullptr && a.pre != nullptr && a.dh != nullptr)
+    if (a.y != nullptr && a.post != nullptr && a.pre != nullptr && a.dh != nullptr && a.ld_y == a.ld_x &&
+        a.ld_dh == a.ld_x && a.ld_dz == a.ld_x && a.ld_dy == a.ld_dx)
         return launch_rows<T, 0, LAYER, RAGGED, DROP, true>(a, s, stream);
     return launch_rows<T, 0, LAYER, RAGGED, DROP, false>(a, s, stream);
 }
