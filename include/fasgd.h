@@ -518,10 +518,10 @@ FASGD_API int fasgd_sim_quadratic_loss(int64_t P, const float* theta, const floa
  * Arguments come in a struct; set what is not used to zero.  Matrices are rows
  * of `cols` consecutive values, ld values from one row to the next (ld >= cols;
  * not looked at where there are fewer than two rows); base and rows need the
- * alignment of their type only.  Bases aligned to eight values, with rows that
- * follow each other without a gap or with cols and ld multiples of 8, take the
- * fast kernels (fasgd_join: up to 32,768 columns, fasgd_join_grad: 32,768,
- * fasgd_balance: all).  An output must not share memory with another argument, except as
+ * alignment of their type only.  Fastest are bases aligned to eight values, with
+ * rows that follow each other without a gap or with cols and ld multiples of 8;
+ * other joins run at 50 to 80 % of that rate (beyond 32,768 columns far slower),
+ * other dropouts and balance losses at a third.  An output must not share memory with another argument, except as
  * fasgd_dropout says.  Everything computed is held in fp32 and rounded once,
  * where it is stored.  A call with rows = 0 reads nothing and writes zeros to
  * the gradients of parameters.  Limits: rows <= 2^40, cols <= FASGD_COLS_MAX

@@ -9,8 +9,8 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Any width, stride and alignment: a block takes a row at a time and reads it
-// again for every statistic (out of L2, where a row fits).
+// Rows too wide for the rest: a block takes a row at a time and reads it again for
+// every statistic (out of L2, where a row fits).
 template <class T>
 __global__ void __launch_bounds__(kThreads) join_any_kernel(const __grid_constant__ JoinArgs a) {
     __shared__ float smem[kThreads / 32];
@@ -86,11 +86,13 @@ __global__ void __launch_bounds__(kThreads) join_any_kernel(const __grid_constan
 // From one of a block's rows to the next: bytes in each matrix, octets of draws.
 struct RowSteps {
     int64_t rows, x, y, h, z, octets;
+    bool vectors;        // h and z can be written in octets
 };
 constexpr int kForwardStages = 3;
 constexpr int kForwardThreads = 512;      // of an SM
 // FULL: with y and both norms.
-template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP, bool FULL>
+// LOOSE (RAGGED too): matrices of any alignment and step.
+template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP, bool FULL, bool LOOSE>
 __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8 ? 16 : 1)
     join_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ RowSteps s, int blocks) {
     constexpr int kP = kPieces<T>, STAGES = kForwardStages;
@@ -106,27 +108,35 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
     const Columns c(th.octet(), RAGGED ? (int)((first * a.cols) & 7) : 0, (int32_t)a.cols);
     RowSums<TPR, NR> sums(th, red);
     const bool has_y = FULL || a.y != nullptr, has_pre = FULL || a.pre != nullptr, has_post = FULL || a.post != nullptr;
-    constexpr int kSlots = 2 * NR * kP * kLane;      // of a warp's stage
+    constexpr int kPlace = LOOSE ? LooseRow<T>::kPlace : kP * kLane;
+    constexpr int kSlots = 2 * NR * kPlace;          // of a warp's stage
     uint4* const mine = ring + (threadIdx.x >> 5) * kSlots;
     const int stage_size = kSlots * th.warps;
-    if (!c.any())
+    if (!LOOSE && !c.any())
         for (int i = 0; i < STAGES; ++i) clear_octets<T>(mine + i * stage_size, 2 * NR);
     __syncwarp();
     pdl_wait();
     pdl_trigger();
 
     const CopyLane<T, TPR == 8 ? 8 : 32> lane(c, (int32_t)a.cols);
-    const T* x = static_cast<const T*>(a.x) + first * a.ld_x + lane.col;      // of the next row to fetch
-    const T* y = static_cast<const T*>(a.y) + first * a.ld_y + lane.col;
+    const LooseRow<T> loose(c, (int32_t)a.cols);
+    const T* x = static_cast<const T*>(a.x) + first * a.ld_x + (LOOSE ? 0 : lane.col);      // of the next row to fetch
+    const T* y = static_cast<const T*>(a.y) + first * a.ld_y + (LOOSE ? 0 : lane.col);
+    // Where the next row to take begins (LOOSE; the low bits of the address).
+    uint32_t start_x = (uint32_t)reinterpret_cast<uintptr_t>(x + loose.col_lo);
+    uint32_t start_y = (uint32_t)reinterpret_cast<uintptr_t>(y + loose.col_lo);
     int64_t unfetched = rows;
     const bool clipped = RAGGED && first + (rows - 1) * step == a.rows - 1;   // the matrix ends with the last row
     const auto fetch = [&](uint4* slot) {
 #pragma unroll
         for (int j = 0; j < NR; ++j) {
-            if (unfetched > 0) {
+            if (LOOSE && unfetched > 0) {
+                loose.copy(slot + 2 * j * kPlace, x, a.x);
+                if (has_y) loose.copy(slot + (2 * j + 1) * kPlace, y, a.y);
+            } else if (unfetched > 0) {
                 const bool clip = clipped && unfetched == 1;
-                lane.copy(slot + 2 * j * kP * kLane, x, clip);
-                if (has_y) lane.copy(slot + (2 * j + 1) * kP * kLane, y, clip);
+                lane.copy(slot + 2 * j * kPlace, x, clip);
+                if (has_y) lane.copy(slot + (2 * j + 1) * kPlace, y, clip);
             }
             --unfetched;
             x = on(x, s.x);
@@ -193,8 +203,15 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
         Oct h[NR], t[NR];
 #pragma unroll
         for (int j = 0; j < NR; ++j) {
-            h[j] = take_octet<T, RAGGED>(slot + 2 * j * kP * kLane, c);
-            if (has_y) t[j] = take_octet<T, RAGGED>(slot + (2 * j + 1) * kP * kLane, c);
+            if constexpr (LOOSE) {
+                h[j] = loose.take(slot + 2 * j * kPlace, start_x, c);
+                if (has_y) t[j] = loose.take(slot + (2 * j + 1) * kPlace, start_y, c);
+                start_x += (uint32_t)s.x;
+                start_y += (uint32_t)s.y;
+            } else {
+                h[j] = take_octet<T, RAGGED>(slot + 2 * j * kPlace, c);
+                if (has_y) t[j] = take_octet<T, RAGGED>(slot + (2 * j + 1) * kPlace, c);
+            }
         }
         fetch(mine + (stage == 0 ? STAGES - 1 : stage - 1) * stage_size);
         stage = stage == STAGES - 1 ? 0 : stage + 1;
@@ -228,7 +245,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
                     if (DROP) u = keep2(draws[j], i, a.drop.last, u);
                     h[j].v[i] = fma2(gate.v[i], u, mul2(h[j].v[i], f2(a.carry)));
                 }
-                if (left > j) store_octet<T, RAGGED>(hp, c, h[j]);
+                if (left > j) store_octet<T, RAGGED>(hp, c, h[j], !LOOSE || s.vectors);
                 hp = on(hp, s.h);
             }
         }
@@ -242,7 +259,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
                     h[j].v[i] = mul2(h[j].v[i], f2(rstd_h[j]));
                     h[j].v[i] = LAYER ? fma2(h[j].v[i], pre.v[i], pre_bias.v[i]) : mul2(h[j].v[i], pre.v[i]);
                 }
-                if (left > j) store_octet<T, RAGGED>(zp, c, h[j]);
+                if (left > j) store_octet<T, RAGGED>(zp, c, h[j], !LOOSE || s.vectors);
                 zp = on(zp, s.z);
             }
         }
@@ -256,33 +273,42 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
     }
 }
 
-template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP, bool FULL>
+template <class T, int TPR, int NR, bool LAYER, bool RAGGED, bool DROP, bool FULL, bool LOOSE>
 cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
-    const size_t smem = (size_t)kForwardStages * 2 * NR * kPieces<T> * s.threads * 16;
+    const size_t place = LOOSE ? LooseRow<T>::kPlace : kPieces<T> * kLane;
+    const size_t smem = (size_t)kForwardStages * 2 * NR * place * (s.threads / 32) * 16;
     int64_t grid = (a.rows + s.rows - 1) / s.rows;
     // Past one row each, they step by a multiple of 8 rows (octet.cuh).
     const int64_t cap = (int64_t)num_sms * (NR == 1 ? 1 : kForwardThreads / s.threads) / s.blocks / 8 * 8;
     if (grid > cap) grid = cap;
     const int64_t rows = grid * s.rows, bytes = rows * (int64_t)sizeof(T);
-    const RowSteps steps = {rows, bytes * a.ld_x, bytes * a.ld_y, bytes * a.ld_h, bytes * a.ld_z, rows * a.cols / 8};
-    return launch_rows_kernel<join_rows_kernel<T, TPR, NR, LAYER, RAGGED, DROP, FULL>>(
+    const RowSteps steps = {rows, bytes * a.ld_x, bytes * a.ld_y, bytes * a.ld_h, bytes * a.ld_z, rows * a.cols / 8,
+                            octet_matrix(a.h, a.ld_h, a.rows, a.cols, sizeof(T)) && octet_matrix(a.z, a.ld_z, a.rows, a.cols, sizeof(T))};
+    return launch_rows_kernel<join_rows_kernel<T, TPR, NR, LAYER, RAGGED, DROP, FULL, LOOSE>>(
         grid * s.blocks, s.threads, smem, s.blocks, stream, a, steps, s.blocks);
 }
 template <class T, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
-    if (s.rows > 1) return launch_rows<T, 8, 2, LAYER, RAGGED, DROP, false>(a, s, num_sms, stream);
+    if (s.rows > 1) return launch_rows<T, 8, 2, LAYER, RAGGED, DROP, false, false>(a, s, num_sms, stream);
     // Two rows a turn, but where a row takes more threads than have the registers for it.
-    if (s.threads > 512) return launch_rows<T, 0, 1, LAYER, RAGGED, DROP, false>(a, s, num_sms, stream);
+    if (s.threads > 512) return launch_rows<T, 0, 1, LAYER, RAGGED, DROP, false, false>(a, s, num_sms, stream);
     // FULL where it gains (32768 x 4096 bf16 with dropout 181 us, 210 without it) and
     // not where it costs (32768 x 2048 rms norm, nothing dropped: 91 us, 82 without it).
     if constexpr (LAYER || DROP)
         if (a.y != nullptr && a.post != nullptr && a.pre != nullptr)
-            return launch_rows<T, 0, 2, LAYER, RAGGED, DROP, true>(a, s, num_sms, stream);
-    return launch_rows<T, 0, 2, LAYER, RAGGED, DROP, false>(a, s, num_sms, stream);
+            return launch_rows<T, 0, 2, LAYER, RAGGED, DROP, true, false>(a, s, num_sms, stream);
+    return launch_rows<T, 0, 2, LAYER, RAGGED, DROP, false, false>(a, s, num_sms, stream);
+}
+template <class T, bool LAYER, bool DROP>
+cudaError_t launch_loose(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
+    if (s.threads > 512) return launch_rows<T, 0, 1, LAYER, true, DROP, false, true>(a, s, num_sms, stream);
+    return launch_rows<T, 0, 2, LAYER, true, DROP, false, true>(a, s, num_sms, stream);
 }
 template <class T, bool LAYER>
-cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, int num_sms, cudaStream_t stream) {
+cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, bool loose, int num_sms, cudaStream_t stream) {
     const bool drop = a.drop.cut != 0;
+    if (loose)
+        return drop ? launch_loose<T, LAYER, true>(a, s, num_sms, stream) : launch_loose<T, LAYER, false>(a, s, num_sms, stream);
     if (a.cols % 8 == 0)
         return drop ? launch_octets<T, LAYER, false, true>(a, s, num_sms, stream)
                     : launch_octets<T, LAYER, false, false>(a, s, num_sms, stream);
@@ -302,9 +328,11 @@ template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     // One block where 1,024 threads will do (16384 x 8192 bf16: 291 us; a cluster of two: 376).
     const int64_t octets = row_octets(a.cols);
-    const RowShape s(octets, octets <= 1024 ? 1024 : 512);
-    if (s.fits() && in_octets(a, (int)sizeof(T)))
-        return a.layer ? launch_octets<T, true>(a, s, num_sms, stream) : launch_octets<T, false>(a, s, num_sms, stream);
+    const bool loose = !in_octets(a, (int)sizeof(T));
+    const RowShape s(octets, octets <= 1024 ? 1024 : 512, loose);
+    if (s.fits())
+        return a.layer ? launch_octets<T, true>(a, s, loose, num_sms, stream)
+                       : launch_octets<T, false>(a, s, loose, num_sms, stream);
     const int64_t grid = a.rows < (int64_t)num_sms * 8 ? a.rows : (int64_t)num_sms * 8;
     return launch_pdl(join_any_kernel<T>, (unsigned)grid, kThreads, 0, stream, a);
 }

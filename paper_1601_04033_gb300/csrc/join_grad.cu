@@ -29,8 +29,9 @@ JoinPlan join_grad_plan(const JoinArgs& a, int dtype, int num_sms) {
     JoinPlan p;
     p.parts = p.splits = p.row_means = 0;
     if (a.rows == 0) return p;
-    if (in_octets(a, dtype == FASGD_F32 ? 4 : 2)) {
-        const RowShape s(row_octets(a.cols), kGradThreads);
+    const RowForm form = form_of(a, dtype == FASGD_F32 ? 4 : 2);
+    if (form != kValues) {
+        const RowShape s(row_octets(a.cols), kGradThreads, form == kLoose);
         const int64_t block_subs = s.rows, per_sm = kGradThreads / s.threads;
         const int64_t most = (int64_t)num_sms * per_sm / s.blocks / 8 * 8 * block_subs;
         if (a.groups == 1) {

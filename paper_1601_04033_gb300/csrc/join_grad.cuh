@@ -192,6 +192,7 @@ struct Unit {
 // From one of a unit's rows to the next: bytes in each matrix, octets of draws.
 struct GradSteps {
     int64_t x, y, dh, dz, dx, dy, stats, octets;
+    bool vectors;        // dx and dy can be written in octets
 };
 template <class T, bool LAYER>
 constexpr int kGradStages = sizeof(T) == 2 ? 4 : LAYER ? 2 : 3;
@@ -212,7 +213,8 @@ __device__ __forceinline__ Oct held_octet(const float4* p) {
     return o;
 }
 // FULL: with y, both norms and dh, and one ld for what is read, one for what is written.
-template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP, bool FULL>
+// LOOSE (RAGGED too): matrices of any alignment and step.
+template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP, bool FULL, bool LOOSE>
 __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     grad_rows_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ GradSteps s, int blocks) {
     constexpr int kP = kPieces<T>, kSums = LAYER ? 2 : 3, STAGES = kGradStages<T, LAYER>;
@@ -229,16 +231,18 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     // All rows that this sub takes begin at the same place in an octet.
     const Columns c(th.octet(), RAGGED && mine < units ? (int)((Unit(a, mine).row * a.cols) & 7) : 0,
                     (int32_t)a.cols);
-    constexpr int kSlots = 4 * kP * kLane;           // of a warp's stage
+    constexpr int kPlace = LOOSE ? LooseRow<T>::kPlace : kP * kLane;
+    constexpr int kSlots = 4 * kPlace;               // of a warp's stage
     uint4* const own = ring + (threadIdx.x >> 5) * kSlots;
     const int stage_size = kSlots * th.warps;
     // The rows' statistics, copied ahead by one lane of theirs in each warp.
     uint4* const own_stats = ring + STAGES * stage_size + (threadIdx.x >> 5) * kWarpRows + (TPR == 8 ? th.sub : 0);
     const bool asks = (threadIdx.x & (TPR == 8 ? 7 : 31)) == 0;
-    if (!c.any())
+    if (!LOOSE && !c.any())
         for (int i = 0; i < STAGES; ++i) clear_octets<T>(own + i * stage_size, 4);
     __syncwarp();
     const CopyLane<T, TPR == 8 ? 8 : 32> lane(c, (int32_t)a.cols);
+    const LooseRow<T> loose(c, (int32_t)a.cols);
     pdl_wait();
     pdl_trigger();
 
@@ -285,10 +289,16 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
         if (gates) d_gate = Oct{};
 
         const int64_t r0 = u.row;
-        const T* x = static_cast<const T*>(a.x) + r0 * a.ld_x + lane.col;       // of the next row to fetch
-        const T* y = static_cast<const T*>(a.y) + r0 * a.ld_y + lane.col;
-        const T* dh = static_cast<const T*>(a.dh) + r0 * a.ld_dh + lane.col;
-        const T* dz = static_cast<const T*>(a.dz) + r0 * a.ld_dz + lane.col;
+        const int32_t col = LOOSE ? 0 : lane.col;
+        const T* x = static_cast<const T*>(a.x) + r0 * a.ld_x + col;            // of the next row to fetch
+        const T* y = static_cast<const T*>(a.y) + r0 * a.ld_y + col;
+        const T* dh = static_cast<const T*>(a.dh) + r0 * a.ld_dh + col;
+        const T* dz = static_cast<const T*>(a.dz) + r0 * a.ld_dz + col;
+        // Where the next row to take begins (LOOSE; the low bits of the address).
+        uint32_t start[4] = {(uint32_t)reinterpret_cast<uintptr_t>(x + loose.col_lo),
+                             (uint32_t)reinterpret_cast<uintptr_t>(y + loose.col_lo),
+                             (uint32_t)reinterpret_cast<uintptr_t>(dh + loose.col_lo),
+                             (uint32_t)reinterpret_cast<uintptr_t>(dz + loose.col_lo)};
         const float4* stats = a.stats + r0;
         // FULL: bytes into the matrices instead, which frees ten registers.
         int64_t in = (r0 * a.ld_x + lane.col) * (int64_t)sizeof(T), out = (r0 * a.ld_dx + c.c0) * (int64_t)sizeof(T);
@@ -299,10 +309,17 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             if (unfetched > 0) {
                 const bool clip = clipped && unfetched == 1;
                 if (asks) copy_async16(own_stats + stage * kWarpRows * th.warps, stats, 16);
+                if constexpr (LOOSE) {
+                    loose.copy(slot, x, a.x);
+                    if (has_y) loose.copy(slot + kPlace, y, a.y);
+                    if (has_dh) loose.copy(slot + 2 * kPlace, dh, a.dh);
+                    if (has_pre) loose.copy(slot + 3 * kPlace, dz, a.dz);
+                } else {
                 lane.copy(slot, FULL ? on(static_cast<const T*>(a.x), in) : x, clip);
                 if (has_y) lane.copy(slot + kP * kLane, FULL ? on(static_cast<const T*>(a.y), in) : y, clip);
                 if (has_dh) lane.copy(slot + 2 * kP * kLane, FULL ? on(static_cast<const T*>(a.dh), in) : dh, clip);
                 if (has_pre) lane.copy(slot + 3 * kP * kLane, FULL ? on(static_cast<const T*>(a.dz), in) : dz, clip);
+                }
             }
             copy_commit();
             --unfetched;
@@ -331,10 +348,22 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             __syncwarp();
             const float4 st = *reinterpret_cast<const float4*>(own_stats + stage * kWarpRows * th.warps);
             const uint4* slot = own + stage * stage_size;
-            Oct hhat = take_octet<T, RAGGED>(slot, c), yhat = {}, w = {}, q = {}, e, uu;
-            if (has_y) yhat = take_octet<T, RAGGED>(slot + kP * kLane, c);
-            if (has_dh) w = take_octet<T, RAGGED>(slot + 2 * kP * kLane, c);
-            if (has_pre) q = take_octet<T, RAGGED>(slot + 3 * kP * kLane, c);
+            Oct hhat, yhat = {}, w = {}, q = {}, e, uu;
+            if constexpr (LOOSE) {
+                hhat = loose.take(slot, start[0], c);
+                if (has_y) yhat = loose.take(slot + kPlace, start[1], c);
+                if (has_dh) w = loose.take(slot + 2 * kPlace, start[2], c);
+                if (has_pre) q = loose.take(slot + 3 * kPlace, start[3], c);
+                start[0] += (uint32_t)s.x;
+                start[1] += (uint32_t)s.y;
+                start[2] += (uint32_t)s.dh;
+                start[3] += (uint32_t)s.dz;
+            } else {
+                hhat = take_octet<T, RAGGED>(slot, c);
+                if (has_y) yhat = take_octet<T, RAGGED>(slot + kP * kLane, c);
+                if (has_dh) w = take_octet<T, RAGGED>(slot + 2 * kP * kLane, c);
+                if (has_pre) q = take_octet<T, RAGGED>(slot + 3 * kP * kLane, c);
+            }
             fetch(stage == 0 ? STAGES - 1 : stage - 1);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
             if (!live) hhat = yhat = w = q = Oct{};      // a row past the end
@@ -386,7 +415,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
                 d_gate.v[i] = fma2(d, uu.v[i], d_gate.v[i]);
                 w.v[i] = mul2(e.v[i], d);
             }
-            if (live) store_octet<T, RAGGED>(FULL ? on(static_cast<T*>(a.dx), out) : dxp, c, hhat);
+            if (live) store_octet<T, RAGGED>(FULL ? on(static_cast<T*>(a.dx), out) : dxp, c, hhat, !LOOSE || s.vectors);
             if (has_post) {
                 // The means of q2 yhat and (layer norm) of q2.
                 float k1, k0 = 0.f;
@@ -424,7 +453,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w.v[i] = mul2(w.v[i], f2(scale));
             }
-            if (live && has_y) store_octet<T, RAGGED>(FULL ? on(static_cast<T*>(a.dy), out) : dyp, c, w);
+            if (live && has_y) store_octet<T, RAGGED>(FULL ? on(static_cast<T*>(a.dy), out) : dyp, c, w, !LOOSE || s.vectors);
             if (FULL) {
                 out += s.dx;
             } else {
@@ -513,40 +542,46 @@ __global__ void __launch_bounds__(kThreads) grad_finish_kernel(const __grid_cons
 int64_t at_most(int64_t n, int64_t cap) { return n < cap ? (n < 1 ? 1 : n) : cap; }
 
 constexpr int kGradThreads = 512;       // of a row in one block, and in an SM (128 registers each)
-bool in_octets(const JoinArgs& a, int size) {
+RowForm form_of(const JoinArgs& a, int size) {
+    // 32-bit counters of rows; a group's rows fall into eight classes where cols is
+    // no multiple of 8: short groups would leave more sums than rows.
+    if (a.rows >> 31 || (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64)) return kValues;
+    if (!RowShape(row_octets(a.cols), kGradThreads, true).fits()) return kValues;
     const void* p[] = {a.x, a.y, a.dh, a.dz, a.dx, a.dy};
     const int64_t ld[] = {a.ld_x, a.ld_y, a.ld_dh, a.ld_dz, a.ld_dx, a.ld_dy};
     for (int i = 0; i < 6; ++i)
-        if (!octet_matrix(p[i], ld[i], a.rows, a.cols, size)) return false;
-    if (a.rows >> 31) return false;        // 32-bit counters of rows
-    // A group's rows fall into eight classes where cols is no multiple of 8: short
-    // groups would leave more sums than rows.
-    if (a.cols % 8 != 0 && a.groups > 1 && a.group_rows < 64) return false;
-    return RowShape(row_octets(a.cols), kGradThreads).fits();
+        if (!octet_matrix(p[i], ld[i], a.rows, a.cols, size)) return kLoose;
+    return kInOctets;
 }
 
-template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP, bool FULL>
+template <class T, int TPR, bool LAYER, bool RAGGED, bool DROP, bool FULL, bool LOOSE>
 cudaError_t launch_rows(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {
-    const size_t smem = ((size_t)kGradStages<T, LAYER> * (4 * kPieces<T> * s.threads + s.threads / 32 * kWarpRows) +
+    const size_t place = LOOSE ? LooseRow<T>::kPlace : kPieces<T> * kLane, warps = s.threads / 32;
+    const size_t smem = ((size_t)kGradStages<T, LAYER> * (4 * place + kWarpRows) * warps +
                          (size_t)kHeld<T, LAYER> * 2 * s.threads) * 16;
     const int64_t step = a.splits, bytes = step * (int64_t)sizeof(T);
     const GradSteps steps = {bytes * a.ld_x,  bytes * a.ld_y,  bytes * a.ld_dh, bytes * a.ld_dz,
-                             bytes * a.ld_dx, bytes * a.ld_dy, step * 16,       step * a.cols / 8};
-    return launch_rows_kernel<grad_rows_kernel<T, TPR, LAYER, RAGGED, DROP, FULL>>(a.parts * s.blocks, s.threads, smem,
-                                                                                   s.blocks, stream, a, steps, s.blocks);
+                             bytes * a.ld_dx, bytes * a.ld_dy, step * 16,       step * a.cols / 8,
+                             octet_matrix(a.dx, a.ld_dx, a.rows, a.cols, sizeof(T)) &&
+                                 octet_matrix(a.dy, a.ld_dy, a.rows, a.cols, sizeof(T))};
+    return launch_rows_kernel<grad_rows_kernel<T, TPR, LAYER, RAGGED, DROP, FULL, LOOSE>>(
+        a.parts * s.blocks, s.threads, smem, s.blocks, stream, a, steps, s.blocks);
 }
 template <class T, bool LAYER, bool RAGGED, bool DROP>
 cudaError_t launch_octets(const JoinArgs& a, const RowShape& s, cudaStream_t stream) {
-    if (s.rows > 1) return launch_rows<T, 8, LAYER, RAGGED, DROP, false>(a, s, stream);
+    if (s.rows > 1) return launch_rows<T, 8, LAYER, RAGGED, DROP, false, false>(a, s, stream);
     if (a.y != nullptr && a.post != nullptr && a.pre != nullptr && a.dh != nullptr && a.ld_y == a.ld_x &&
         a.ld_dh == a.ld_x && a.ld_dz == a.ld_x && a.ld_dy == a.ld_dx)
-        return launch_rows<T, 0, LAYER, RAGGED, DROP, true>(a, s, stream);
-    return launch_rows<T, 0, LAYER, RAGGED, DROP, false>(a, s, stream);
+        return launch_rows<T, 0, LAYER, RAGGED, DROP, true, false>(a, s, stream);
+    return launch_rows<T, 0, LAYER, RAGGED, DROP, false, false>(a, s, stream);
 }
 template <class T, bool LAYER>
-cudaError_t launch_octets(const JoinArgs& a, cudaStream_t stream) {
-    const RowShape s(row_octets(a.cols), kGradThreads);
+cudaError_t launch_octets(const JoinArgs& a, bool loose, cudaStream_t stream) {
+    const RowShape s(row_octets(a.cols), kGradThreads, loose);
     const bool drop = a.drop.cut != 0;
+    if (loose)
+        return drop ? launch_rows<T, 0, LAYER, true, true, false, true>(a, s, stream)
+                    : launch_rows<T, 0, LAYER, true, false, false, true>(a, s, stream);
     if (a.cols % 8 == 0)
         return drop ? launch_octets<T, LAYER, false, true>(a, s, stream) : launch_octets<T, LAYER, false, false>(a, s, stream);
     return drop ? launch_octets<T, LAYER, true, true>(a, s, stream) : launch_octets<T, LAYER, true, false>(a, s, stream);
@@ -555,8 +590,9 @@ cudaError_t launch_octets(const JoinArgs& a, cudaStream_t stream) {
 template <class T>
 cudaError_t launch(const JoinArgs& a, int num_sms, cudaStream_t stream) {
     cudaError_t st = cudaSuccess;
-    if (a.rows > 0 && in_octets(a, (int)sizeof(T))) {
-        st = a.layer ? launch_octets<T, true>(a, stream) : launch_octets<T, false>(a, stream);
+    const RowForm form = form_of(a, (int)sizeof(T));
+    if (a.rows > 0 && form != kValues) {
+        st = a.layer ? launch_octets<T, true>(a, form == kLoose, stream) : launch_octets<T, false>(a, form == kLoose, stream);
     } else if (a.rows > 0) {
         st = launch_pdl(grad_rows_any_kernel<T>, (unsigned)at_most(a.rows, (int64_t)num_sms * 8), kThreads, 0,
                         stream, a);

@@ -137,7 +137,7 @@ def test_join_gates_of_groups(groups, L, D, gate_f32):
 
 
 @pytest.mark.parametrize("pad, offset", [(0, 1), (0, 3), (1, 0), (3, 0), (8, 0), (16, 8), (8, 4), (5, 2)])
-@pytest.mark.parametrize("D", [200, 203, 1024])
+@pytest.mark.parametrize("D", [1, 6, 40, 200, 203, 1024, 5003])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_join_strides_and_alignments(pad, offset, D, dtype):
     import torch
@@ -160,6 +160,17 @@ def test_join_strides_and_alignments(pad, offset, D, dtype):
         assert torch.equal(o, want)
         o.copy_(was[offset:offset + R * (D + pad)].view(R, D + pad)[:, :D])
         assert torch.equal(o._base.view(torch.uint8), was.view(torch.uint8))
+
+
+@pytest.mark.parametrize("D, pad", [(48, 3), (200, 5), (1021, 16), (2056, 3), (9001, 1)])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_join_many_unaligned_rows(D, pad, norm):
+    """Enough rows for every block to take several, and parts that are absent."""
+    for dtype in ("bfloat16", "float32"):
+        R = 1300 if D < 3000 else 400
+        check_join(*make(R, D, dtype, norm, groups=1, pad=pad, offset=1), norm=norm, rate=0.2)
+        check_join(*make(R, D, dtype, norm, groups=2, post=False, pad=pad), norm=norm, use_dh=False)
+        check_join(*make(R, D, dtype, norm, y=False, pad=pad, offset=3), norm=norm)
 
 
 def test_join_halves_of_one_matrix():
