@@ -520,12 +520,13 @@ FASGD_API int fasgd_sim_quadratic_loss(int64_t P, const float* theta, const floa
  * not looked at where there are fewer than two rows); base and rows need the
  * alignment of their type only.  Fastest are bases aligned to eight values, with
  * rows that follow each other without a gap or with cols and ld multiples of 8;
- * other joins run at 50 to 80 % of that rate (beyond 32,768 columns far slower),
- * other dropouts and balance losses at a third.  An output must not share memory with another argument, except as
- * fasgd_dropout says.  Everything computed is held in fp32 and rounded once,
- * where it is stored.  A call with rows = 0 reads nothing and writes zeros to
- * the gradients of parameters.  Limits: rows <= 2^40, cols <= FASGD_COLS_MAX
- * (fasgd_dropout: 2^40).
+ * other joins ran at 50 to 85 % of that rate, other dropouts at 30 %, other
+ * balance losses at 20 to 70 %.  Joins of more than 32,768 columns are slow in any
+ * layout (0.8 TB/s forward, 0.3 TB/s gradients).  An output must not share memory
+ * with another argument, except as fasgd_dropout says.  Everything computed is
+ * held in fp32 and rounded once, where it is stored.  A call with rows = 0 reads
+ * nothing and writes zeros to the gradients of parameters.  Limits: rows <= 2^40,
+ * cols <= FASGD_COLS_MAX (fasgd_dropout: 2^40).
  * Errors: EINVAL (text via fasgd_last_error(NULL)), ECUDA.
  */
 enum fasgd_dtype { FASGD_F32 = 0, FASGD_BF16 = 1, FASGD_F16 = 2 };

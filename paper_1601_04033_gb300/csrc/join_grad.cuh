@@ -162,14 +162,14 @@ __host__ __device__ __forceinline__ int64_t gates_left(const JoinArgs& a) {
 //   sum q2 yhat = S(e yhat w) - r_h mean(q hhat) S(e yhat hhat),
 // sums of what is known before mean(q hhat) is.  Under layer norms that takes
 // eight sums, whose registers cost more than a second reduction of two
-// (32768 x 4096 bf16: 510 us, 450).  Units as in the plain form, for the threads of
+// (32768 x 4096 bf16, when chosen: 510 us, 450).  Units as in the plain form, for the threads of
 // one row ("sub") at a time; where cols is no multiple of 8 a unit's rows agree
 // modulo 8 (octet.cuh).
 //
 // It moves 12 bytes an element (16-bit types) and issues about 50 instructions for
 // each, a fifth of them the draws: instructions bound it, not memory.  32768 x 4096
-// bf16 with dropout: 282 us, 5.7 TB/s; without 5.5 to 5.8 TB/s; layer norm with
-// dropout 381 us, 4.2 TB/s; fp32 4.1 TB/s.  512 threads an SM of 128 registers hold
+// bf16 with dropout: 281 us, 5.7 TB/s; without 5.3 to 6.3 TB/s; layer norm with
+// dropout 381 us, 4.2 TB/s; fp32 3.8 to 4.1 TB/s.  512 threads an SM of 128 registers hold
 // the vectors and sums of 4,096 columns; wider rows take a cluster, whose barrier
 // for every row shows: 16384 x 8192 545 us, 3.0 TB/s.
 struct Unit {
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
     }
     // With both biases the registers do not hold everything: these lie in shared
     // memory (a place of each lane's own, as the ring's).  Before a third stage of
-    // fp32 rows, too: 16384 x 4096 430 us, 577 with the stage and spills.
+    // fp32 rows, too: 16384 x 4096, when chosen, 430 us, 577 with the stage and spills.
     float4* const vectors = reinterpret_cast<float4*>(ring + STAGES * (stage_size + kWarpRows * th.warps)) +
                             (threadIdx.x >> 5) * (kHeld<T, LAYER> * 2 * kLane) + (threadIdx.x & 31);
     if (kHeld<T, LAYER> > 0) hold_octet(vectors, pre);

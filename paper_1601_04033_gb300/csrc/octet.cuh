@@ -203,7 +203,7 @@ struct CopyLane {
 // that hold its columns of a row, col_lo .. col_hi, and a lane reads its octet at
 // whatever byte it begins.  Two granules lie free before the data, for the values
 // before a row's first that an octet spans.  32768 x 1024 bf16 rows three values
-// apart: 70 us forward, 130 us gradients; without gaps 44 and 74.
+// apart: 70 us forward, 130 us gradients; without gaps 42 and 76.
 template <class T>
 struct LooseRow {
     static constexpr int kPlace = kLane * kPieces<T> + 4;       // 16-byte places of a warp's matrix
