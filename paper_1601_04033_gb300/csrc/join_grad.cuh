@@ -315,10 +315,10 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
                     if (has_dh) loose.copy(slot + 2 * kPlace, dh, a.dh);
                     if (has_pre) loose.copy(slot + 3 * kPlace, dz, a.dz);
                 } else {
-                lane.copy(slot, FULL ? on(static_cast<const T*>(a.x), in) : x, clip);
-                if (has_y) lane.copy(slot + kP * kLane, FULL ? on(static_cast<const T*>(a.y), in) : y, clip);
-                if (has_dh) lane.copy(slot + 2 * kP * kLane, FULL ? on(static_cast<const T*>(a.dh), in) : dh, clip);
-                if (has_pre) lane.copy(slot + 3 * kP * kLane, FULL ? on(static_cast<const T*>(a.dz), in) : dz, clip);
+                    lane.copy(slot, FULL ? on(static_cast<const T*>(a.x), in) : x, clip);
+                    if (has_y) lane.copy(slot + kP * kLane, FULL ? on(static_cast<const T*>(a.y), in) : y, clip);
+                    if (has_dh) lane.copy(slot + 2 * kP * kLane, FULL ? on(static_cast<const T*>(a.dh), in) : dh, clip);
+                    if (has_pre) lane.copy(slot + 3 * kP * kLane, FULL ? on(static_cast<const T*>(a.dz), in) : dz, clip);
                 }
             }
             copy_commit();
