@@ -286,13 +286,14 @@ __global__ void __launch_bounds__(kThreads, NV > 2 ? 2 : 3)
     uint4 raw[NV][kP];
     const T* x = nullptr;
     const int64_t step_x = kSlots * a.ld_logits, step_d = kSlots * a.ld_dlogits;
-    // The matrix's last row may end inside its last octet: that one is read value by value.
+    // The matrix may end inside a last octet: such a one is read value by value.
+    const int64_t followed = rows_followed(a.rows, a.cols);
     const auto fetch = [&](int32_t i) {
         if (i < rows) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 if (!c[v].any()) continue;
-                if (!RAGGED || c[v].c0 + kOctet <= cols || base + i < a.rows - 1) {
+                if (!RAGGED || c[v].c0 + kOctet <= cols || base + i < followed) {
                     load_pieces(x + v * (LPR * kOctet), raw[v]);
                 } else {
                     Oct o = {};

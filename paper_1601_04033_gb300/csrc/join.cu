@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
     uint32_t start_x = (uint32_t)reinterpret_cast<uintptr_t>(x + loose.col_lo);
     uint32_t start_y = (uint32_t)reinterpret_cast<uintptr_t>(y + loose.col_lo);
     int64_t unfetched = rows;
-    const bool clipped = RAGGED && first + (rows - 1) * step == a.rows - 1;   // the matrix ends with the last row
+    const int32_t last_behind = RAGGED ? values_behind(a.rows, a.cols, first + (rows - 1) * step) : -1;
     const auto fetch = [&](uint4* slot) {
 #pragma unroll
         for (int j = 0; j < NR; ++j) {
@@ -134,9 +134,9 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : NR == 1 ? 1024 : 512, TPR == 8
                 loose.copy(slot + 2 * j * kPlace, x, a.x);
                 if (has_y) loose.copy(slot + (2 * j + 1) * kPlace, y, a.y);
             } else if (unfetched > 0) {
-                const bool clip = clipped && unfetched == 1;
-                lane.copy(slot + 2 * j * kPlace, x, clip);
-                if (has_y) lane.copy(slot + (2 * j + 1) * kPlace, y, clip);
+                const int32_t behind = RAGGED && unfetched == 1 ? last_behind : -1;
+                lane.copy(slot + 2 * j * kPlace, x, behind);
+                if (has_y) lane.copy(slot + (2 * j + 1) * kPlace, y, behind);
             }
             --unfetched;
             x = on(x, s.x);

@@ -303,11 +303,11 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
         // FULL: bytes into the matrices instead, which frees ten registers.
         int64_t in = (r0 * a.ld_x + lane.col) * (int64_t)sizeof(T), out = (r0 * a.ld_dx + c.c0) * (int64_t)sizeof(T);
         int32_t unfetched = rows;
-        const bool clipped = RAGGED && r0 + (rows - 1) * u.step == a.rows - 1;   // the matrix ends with the last row
+        const int32_t last_behind = RAGGED ? values_behind(a.rows, a.cols, r0 + (rows - 1) * u.step) : -1;
         const auto fetch = [&](int stage) {
             uint4* slot = own + stage * stage_size;
             if (unfetched > 0) {
-                const bool clip = clipped && unfetched == 1;
+                const int32_t behind = RAGGED && unfetched == 1 ? last_behind : -1;
                 if (asks) copy_async16(own_stats + stage * kWarpRows * th.warps, stats, 16);
                 if constexpr (LOOSE) {
                     loose.copy(slot, x, a.x);
@@ -315,10 +315,10 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
                     if (has_dh) loose.copy(slot + 2 * kPlace, dh, a.dh);
                     if (has_pre) loose.copy(slot + 3 * kPlace, dz, a.dz);
                 } else {
-                    lane.copy(slot, FULL ? on(static_cast<const T*>(a.x), in) : x, clip);
-                    if (has_y) lane.copy(slot + kP * kLane, FULL ? on(static_cast<const T*>(a.y), in) : y, clip);
-                    if (has_dh) lane.copy(slot + 2 * kP * kLane, FULL ? on(static_cast<const T*>(a.dh), in) : dh, clip);
-                    if (has_pre) lane.copy(slot + 3 * kP * kLane, FULL ? on(static_cast<const T*>(a.dz), in) : dz, clip);
+                    lane.copy(slot, FULL ? on(static_cast<const T*>(a.x), in) : x, behind);
+                    if (has_y) lane.copy(slot + kP * kLane, FULL ? on(static_cast<const T*>(a.y), in) : y, behind);
+                    if (has_dh) lane.copy(slot + 2 * kP * kLane, FULL ? on(static_cast<const T*>(a.dh), in) : dh, behind);
+                    if (has_pre) lane.copy(slot + 3 * kP * kLane, FULL ? on(static_cast<const T*>(a.dz), in) : dz, behind);
                 }
             }
             copy_commit();

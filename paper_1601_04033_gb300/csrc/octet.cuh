@@ -12,6 +12,7 @@
 #include <atomic>
 
 #include "client.cuh"
+#include "clip.cuh"
 
 namespace fasgd {
 namespace {
@@ -183,19 +184,14 @@ struct CopyLane {
         const int i = place % W, piece = k * W + i, owner = place - i + (piece >> 1);
         return (piece & 1) * kLane + (owner ^ (4 * (piece & 1)));
     }
-    // p: the row's first value, `col` on.  clip: the matrix ends with this row, so
-    // what lies behind it is not read (zeros).
-    __device__ __forceinline__ void copy(uint4* slot, const T* p, bool clip) const {
+    // p: the row's first value, `col` on.  behind: what the matrix has behind the row
+    // (clip.cuh); past its end nothing is read (zeros).
+    __device__ __forceinline__ void copy(uint4* slot, const T* p, int32_t behind) const {
 #pragma unroll
         for (int k = 0; k < kPieces<T>; ++k) {
             if (!(in >> k & 1)) continue;
             uint4* to = slot + place_of(k);
-            if (!clip) {
-                copy_async16(to, p + k * kStep, 16);
-            } else {
-                const int left = cols - col - k * kStep;
-                copy_async16(to, p + k * kStep, (left < kPer ? left : kPer) * (int)sizeof(T));
-            }
+            copy_async16(to, p + k * kStep, values_there(col + k * kStep, cols, behind, kPer) * (int)sizeof(T));
         }
     }
 };
