@@ -165,7 +165,8 @@ def dropout(x, draws: Draws, *, residual=None, out=None):
 
 class Joined:
     """What ``join`` gives: h (None without y), z (None without pre), and what
-    ``join_grad`` needs: the tensors of the call (kept alive) and its arguments."""
+    ``join_grad`` needs: the tensors of the call (kept alive) and its settings (its
+    argument struct; the addresses in it are not looked at again)."""
     __slots__ = ("h", "z", "args", "x", "y", "parameters", "stats")
 
 
@@ -218,13 +219,17 @@ class JoinGrads(NamedTuple):
 
 def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinGrads:
     """fasgd_join_grad: the gradients of ``join``'s x, y and parameters from those
-    of its h (None: zero) and z.  x, y, the parameters and the stream's order are
-    to be as they were.  into: where to write them (new tensors where None)."""
+    of its h (None: zero) and z.  j's tensors (x, y, parameters, stats) may lie
+    elsewhere by now; their values and the stream's order are to be as they were.
+    into: where to write them (new tensors where None)."""
     x = j.x
     if _fast is not None:
-        return JoinGrads(*_done(_fast.join_grad(j.args, x, j.y, dh, dz, j.parameters, into or _NO_GRADS)))
-    a = _f.JoinArgs.from_buffer_copy(j.args)
+        return JoinGrads(*_done(_fast.join_grad(j.args, x, j.y, dh, dz, j.parameters, into or _NO_GRADS, j.stats)))
+    was = _f.JoinArgs.from_buffer_copy(j.args)
+    a = _f.JoinArgs()
     at = ctypes.addressof(a)
+    for name in _SETTINGS:
+        setattr(a, name, getattr(was, name))
     dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias = into if into is not None else _NO_GRADS
     post, post_bias, gate, pre, pre_bias = j.parameters
     if dx is None:
@@ -247,9 +252,15 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
         elif dgate.shape != gate.shape or dgate.dtype is not gate.dtype or not dgate.is_contiguous():
             raise ValueError("the gate's gradient must be as the gate")
         a.dgate = dgate.data_ptr()
-    groups = a.groups
-    _intake(a, _JOIN_GRAD, x, dh, dz, dx, dy, dpost, dpost_bias, dpre, dpre_bias)
-    a.groups = groups
+    _intake(a, _JOIN_GRAD, x, j.y, post, post_bias, gate, pre, pre_bias, dh, dz, dx, dy, dpost, dpost_bias, dpre,
+            dpre_bias)
+    if (a.rows, a.cols, a.dtype, a.groups) != (was.rows, was.cols, was.dtype, was.groups) or \
+            any((getattr(a, n) is None) != (getattr(was, n) is None) for n in ("y", "post", "pre")):
+        raise ValueError("join_grad: not the join's tensors")
+    if j.stats.dtype is not torch.float32 or j.stats.numel() != 4 * a.rows or not j.stats.is_contiguous() or \
+            not j.stats.is_cuda:
+        raise ValueError("join_grad: not the join's statistics")
+    a.stats = j.stats.data_ptr() or _NOWHERE
     size = _check(_f.fasgd_join_workspace(at))
     space = torch.empty(size, dtype=torch.uint8, device=x.device)
     a.workspace = space.data_ptr()
@@ -259,8 +270,11 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
 
 
 _NO_GRADS = JoinGrads()
-_JOIN_GRAD = dict(x=_FIRST, dh=_LIKE, dz=_LIKE, dx=_LIKE, dy=_LIKE, dpost=_VECTOR, dpost_bias=_VECTOR,
-                   dpre=_VECTOR, dpre_bias=_VECTOR)
+# What join_grad takes of the forward call's struct; addresses are its own tensors'.
+_SETTINGS = ("rate", "seed", "n", "client", "norm", "eps", "carry", "branch")
+_JOIN_GRAD = dict(x=_FIRST, y=_LIKE, post=_VECTOR, post_bias=_VECTOR, gate=_GATE, pre=_VECTOR, pre_bias=_VECTOR,
+                  dh=_LIKE, dz=_LIKE, dx=_LIKE, dy=_LIKE, dpost=_VECTOR, dpost_bias=_VECTOR, dpre=_VECTOR,
+                  dpre_bias=_VECTOR)
 
 
 class Balance(NamedTuple):

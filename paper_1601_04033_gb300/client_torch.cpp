@@ -156,6 +156,35 @@ float* vector(const Tensor* t, int64_t cols) {
     return static_cast<float*>(address(*t));
 }
 
+/* A join's inputs into its struct: the matrices, and the shape and types they fix;
+ * of: (post, post_bias, gate, pre, pre_bias), null where absent. */
+void join_inputs(fasgd_join_args& a, const Tensor& x, const Tensor* y, const Tensor* const (&of)[5]) {
+    const Matrix m(x);
+    a.rows = m.rows;
+    a.cols = m.cols;
+    a.x = m.p;
+    a.ld_x = m.ld;
+    a.dtype = dtype_of(x);
+    a.groups = 1;
+    if (y != nullptr) {
+        const Matrix k = like(*y, x);
+        a.y = k.p;
+        a.ld_y = k.ld;
+    }
+    a.post = vector(of[0], m.cols);
+    a.post_bias = vector(of[1], m.cols);
+    a.pre = vector(of[3], m.cols);
+    a.pre_bias = vector(of[4], m.cols);
+    if (const Tensor* gate = of[2]) {
+        on_gpu(*gate);
+        if (gate->dim() < 1 || gate->dim() > 2 || gate->size(-1) != m.cols || !gate->is_contiguous())
+            wrong("a gate is contiguous, [cols] or [groups, cols]");
+        if (gate->dim() == 2) a.groups = gate->size(0);
+        a.gate = address(*gate);
+        a.gate_dtype = dtype_of(*gate);
+    }
+}
+
 /* torch's current stream, which is to be on t's device. */
 void* stream(const Tensor& t) {
     const auto device = c10::cuda::current_device();
@@ -277,24 +306,18 @@ PyObject* py_dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
  * -> (h, z, stats, the argument struct as bytes) */
 PyObject* py_join(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return entry(nargs, 14, [&]() -> PyObject* {
-        const Tensor *x = tensor(args[0]), *y = tensor(args[1]), *gate = tensor(args[4]), *pre = tensor(args[5]);
-        const Tensor *h = tensor(args[12]), *z = tensor(args[13]);
+        const Tensor *x = tensor(args[0]), *y = tensor(args[1]), *h = tensor(args[12]), *z = tensor(args[13]);
+        const Tensor* const of[5] = {tensor(args[2]), tensor(args[3]), tensor(args[4]), tensor(args[5]), tensor(args[6])};
         if (x == nullptr) wrong("a tensor is expected");
-        if ((h != nullptr && y == nullptr) || (z != nullptr && pre == nullptr)) wrong("h goes with y, z with pre");
+        if ((h != nullptr && y == nullptr) || (z != nullptr && of[3] == nullptr)) wrong("h goes with y, z with pre");
         fasgd_join_args a;
         std::memset(&a, 0, sizeof a);
-        const Matrix m(*x);
-        a.rows = m.rows;
-        a.cols = m.cols;
-        a.x = m.p;
-        a.ld_x = m.ld;
-        a.dtype = dtype_of(*x);
-        a.groups = 1;
+        join_inputs(a, *x, y, of);
         New made(*x);
         int at_h = -1, at_z = -1;
         const auto output = [&](const Tensor* t, void*& p, int64_t& ld) {
             if (t == nullptr) {
-                ld = m.cols;
+                ld = a.cols;
                 return made.add(*x, &p);
             }
             const Matrix o = like(*t, *x);
@@ -302,31 +325,14 @@ PyObject* py_join(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             ld = o.ld;
             return -1;
         };
-        if (y != nullptr) {
-            const Matrix k = like(*y, *x);
-            a.y = k.p;
-            a.ld_y = k.ld;
-            at_h = output(h, a.h, a.ld_h);
-        }
-        if (pre != nullptr) at_z = output(z, a.z, a.ld_z);
-        a.post = vector(tensor(args[2]), m.cols);
-        a.post_bias = vector(tensor(args[3]), m.cols);
-        a.pre = vector(pre, m.cols);
-        a.pre_bias = vector(tensor(args[6]), m.cols);
-        if (gate != nullptr) {
-            on_gpu(*gate);
-            if (gate->dim() < 1 || gate->dim() > 2 || gate->size(-1) != m.cols || !gate->is_contiguous())
-                wrong("a gate is contiguous, [cols] or [groups, cols]");
-            if (gate->dim() == 2) a.groups = gate->size(0);
-            a.gate = address(*gate);
-            a.gate_dtype = dtype_of(*gate);
-        }
+        if (y != nullptr) at_h = output(h, a.h, a.ld_h);
+        if (of[3] != nullptr) at_z = output(z, a.z, a.ld_z);
         a.norm = (int32_t)whole(args[7]);
         a.eps = real(args[8]);
         a.carry = real(args[9]);
         a.branch = real(args[10]);
         draws(args[11], a);
-        const int at_stats = made.add(4 * m.rows, at::kFloat, &a.stats);
+        const int at_stats = made.add(4 * a.rows, at::kFloat, &a.stats);
         void* s = stream(*x);
         made.make();
         unlocked([&] { return (int64_t)fasgd_join(&a, s); });
@@ -336,18 +342,37 @@ PyObject* py_join(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 }
 
 /* join_grad(join's struct, x, y, dh, dz, (post, post_bias, gate, pre, pre_bias),
- * (x, y, post, post_bias, gate, pre, pre_bias)): the parameters, and where their
- * gradients go (None: a new tensor) -> those seven */
+ * (x, y, post, post_bias, gate, pre, pre_bias), stats): the parameters, and where their
+ * gradients go (None: a new tensor) -> those seven.  Of the struct only the settings
+ * are taken: the tensors may have moved since (saved elsewhere, or computed again). */
 PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    return entry(nargs, 7, [&]() -> PyObject* {
-        fasgd_join_args a;
+    return entry(nargs, 8, [&]() -> PyObject* {
+        fasgd_join_args a, was;
         if (!PyBytes_Check(args[0]) || PyBytes_GET_SIZE(args[0]) != (Py_ssize_t)sizeof a ||
             !PyTuple_Check(args[5]) || PyTuple_GET_SIZE(args[5]) != 5 || !PyTuple_Check(args[6]) ||
             PyTuple_GET_SIZE(args[6]) != 7)
             wrong("join_grad: not a join's record");
-        std::memcpy(&a, PyBytes_AS_STRING(args[0]), sizeof a);
         const Tensor *x = tensor(args[1]), *y = tensor(args[2]), *dh = tensor(args[3]), *dz = tensor(args[4]);
-        if (x == nullptr) wrong("a tensor is expected");
+        const Tensor* stats = tensor(args[7]);
+        const Tensor* of[5];
+        for (int i = 0; i < 5; ++i) of[i] = tensor(PyTuple_GET_ITEM(args[5], i));
+        if (x == nullptr || stats == nullptr) wrong("a tensor is expected");
+        std::memcpy(&was, PyBytes_AS_STRING(args[0]), sizeof was);
+        std::memset(&a, 0, sizeof a);
+        a.rate = was.rate;
+        a.seed = was.seed;
+        a.n = was.n;
+        a.client = was.client;
+        a.norm = was.norm;
+        a.eps = was.eps;
+        a.carry = was.carry;
+        a.branch = was.branch;
+        join_inputs(a, *x, y, of);
+        if (a.rows != was.rows || a.cols != was.cols || a.dtype != was.dtype || a.groups != was.groups ||
+            (y != nullptr) != (was.y != nullptr) || (of[0] != nullptr) != (was.post != nullptr) ||
+            (of[3] != nullptr) != (was.pre != nullptr))
+            wrong("join_grad: not the join's tensors");
+        a.stats = vector(stats, 4 * a.rows);
         if (dh != nullptr) {
             const Matrix m = like(*dh, *x);
             a.dh = m.p;
@@ -383,15 +408,15 @@ PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         else
             out[1] = Py_None;
         const auto parameter = [&](int i, auto*& p) {
-            const Tensor *of = tensor(PyTuple_GET_ITEM(args[5], i - 2)), *t = tensor(into[i]);
-            if (of == nullptr) {
+            const Tensor *p_of = of[i - 2], *t = tensor(into[i]);
+            if (p_of == nullptr) {
                 out[i] = Py_None;
             } else if (t == nullptr) {
-                at[i] = made.add(*of, &p);
+                at[i] = made.add(*p_of, &p);
                 // What the workspace depends on: that it is there, and aligned.
                 p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(256);
             } else if (i == 4) {
-                if (t->sizes() != of->sizes() || t->scalar_type() != of->scalar_type() || !t->is_contiguous() || !t->is_cuda())
+                if (t->sizes() != p_of->sizes() || t->scalar_type() != p_of->scalar_type() || !t->is_contiguous() || !t->is_cuda())
                     wrong("the gate's gradient must be as the gate");
                 p = static_cast<std::remove_reference_t<decltype(p)>>(address(*t));
             } else {
