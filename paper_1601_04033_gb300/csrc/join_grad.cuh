@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             oct += s.octets;
             copy_wait<STAGES - 2>();
             __syncwarp();
-            const float4 st = *reinterpret_cast<const float4*>(own_stats + stage * kWarpRows * th.warps);
+            float4 st = *reinterpret_cast<const float4*>(own_stats + stage * kWarpRows * th.warps);
             const uint4* slot = own + stage * stage_size;
             Oct hhat, yhat = {}, w = {}, q = {}, e, uu;
             if constexpr (LOOSE) {
@@ -366,7 +366,10 @@ __global__ void __launch_bounds__(TPR == 8 ? 32 : 512, TPR == 8 ? 16 : 1)
             }
             fetch(stage == 0 ? STAGES - 1 : stage - 1);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
-            if (!live) hhat = yhat = w = q = Oct{};      // a row past the end
+            if (!live) {         // a row past the end: nobody copied its statistics either
+                hhat = yhat = w = q = Oct{};
+                st = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
             if (kHeld<T, LAYER> > 1) post_bias = held_octet(vectors + 2 * kLane);
             if (kHeld<T, LAYER> > 2) post = held_octet(vectors + 4 * kLane);
             // u; e = what dH is multiplied by in dt / scale.
