@@ -9,10 +9,9 @@
 // too, which are loaded, set to zero and not stored.
 #pragma once
 
-#include <atomic>
-
 #include "client.cuh"
 #include "clip.cuh"
+#include "shared_limit.cuh"
 
 namespace fasgd {
 namespace {
@@ -440,20 +439,22 @@ inline int64_t row_octets(int64_t cols) {
     for (int r = 0; r < 8; ++r) most = r * cols % 8 > most ? r * cols % 8 : most;
     return (most + cols + 7) / 8;
 }
+// Dynamic shared memory that any of these kernels can have: 227 KB less their own
+// (4 KB at most); the largest call takes 207 KB.
+constexpr int64_t kSharedMost = 220 * 1024;
 // Programmatic dependent launch (pdl.cuh), of clusters of `cluster` blocks.  With
 // the kernel's own, shared memory beyond 48 KB is to be asked for: once a device.
 template <auto Kernel, class... Args>
 cudaError_t launch_rows_kernel(int64_t grid, int block, size_t smem, int cluster, cudaStream_t stream, Args... args) {
     if (smem > 32 * 1024) {
-        static std::atomic<uint64_t> most[64];       // bytes asked for, by device
+        static SharedLimit limit;
         int dev = 0;
         cudaError_t st = cudaGetDevice(&dev);
         if (st != cudaSuccess) return st;
-        if (dev >= 64 || most[dev].load(std::memory_order_relaxed) < smem) {
-            st = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-            if (st != cudaSuccess) return st;
-            if (dev < 64) most[dev].store(smem, std::memory_order_relaxed);
-        }
+        st = (cudaError_t)limit.ensure(dev, (int64_t)smem, kSharedMost, [](int64_t bytes) {
+            return (int)cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        });
+        if (st != cudaSuccess) return st;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);

@@ -37,3 +37,49 @@ def test_narrow_gradients_whatever_ran_before(D, norm, dtype):
         for name, w, g in zip(want._fields, want, got):
             if w is not None:
                 assert torch.isfinite(g.float()).all() and torch.equal(g, w), (R, groups, name)
+
+
+FIRST_CALLS = r"""
+import sys, threading, torch
+sys.path.insert(0, "tests")
+from test_gpu_client import make
+from paper_1601_04033_gb300 import client as c
+sets = []
+for D in (4096, 264, 2048, 1024, 4088, 520, 8192, 5000):      # what they need of shared memory differs
+    for dtype in ("float32", "bfloat16"):
+        for norm in ("rms", "layer"):
+            sets.append((norm, *make(40, D, dtype, norm, groups=1)))
+            sets.append((norm, *make(40, D, dtype, norm, groups=1, pad=3)))
+torch.cuda.synchronize()
+out, errors, meet = [None] * len(sets), [], threading.Barrier(len(sets))
+
+def call(i):
+    norm, a, dh, dz = sets[i]
+    try:
+        meet.wait(60)
+        j = c.join(**a, norm=norm)
+        out[i] = [j.h, j.z, *c.join_grad(j, dh, dz)]
+    except Exception as e:
+        errors.append((i, e))
+
+threads = [threading.Thread(target=call, args=(i,)) for i in range(len(sets))]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert not errors, errors
+for i, (norm, a, dh, dz) in enumerate(sets):
+    j = c.join(**a, norm=norm)
+    for got, want in zip(out[i], [j.h, j.z, *c.join_grad(j, dh, dz)]):
+        assert got is want is None or torch.equal(got, want), i
+print("same")
+"""
+
+
+def test_first_calls_of_many_threads():
+    """A process whose first joins come on many threads at once, of widths that need
+    more and less shared memory of the same kernels."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.endswith("same\n"), r.stderr[-3000:]
