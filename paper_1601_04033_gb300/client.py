@@ -330,6 +330,24 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
 # ---------------------------------------------------------------------------
 # Inside torch's automatic differentiation
 # ---------------------------------------------------------------------------
+class _Once(torch.autograd.Function):
+    """Gradients as they are, with an error in place of their derivatives."""
+    @staticmethod
+    def forward(ctx, count, *tensors):
+        return tuple(None if t is None else t.detach() for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the join and the balance loss have no second derivatives here")
+
+
+def _once(grads, *of):
+    """What a backward call returns of `grads`, which depend on the tensors `of`.  Where
+    a graph is made of the call, a derivative through it raises: they are plain
+    tensors, whose part would be missing without a word."""
+    return _Once.apply(len(grads), *grads, *of) if torch.is_grad_enabled() else grads
+
+
 class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, draws):
@@ -338,11 +356,12 @@ class _Dropout(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d):
-        return dropout(d.contiguous(), ctx.draws), d if ctx.both else None, None
+        again = dropped if torch.is_grad_enabled() else dropout      # linear: its gradient's gradient is its own
+        return again(d.contiguous(), ctx.draws), d if ctx.both else None, None
 
 
 def dropped(x, draws: Draws, residual=None):
-    """``dropout``, differentiable in x and residual; no mask is kept."""
+    """``dropout``, differentiable in x and residual, any number of times; no mask is kept."""
     return _Dropout.apply(x, residual, draws)
 
 
@@ -359,19 +378,21 @@ class _Join(torch.autograd.Function):
     def backward(ctx, dh, dz):
         if dh is None and dz is None:
             return (None,) * 8
-        x, y, post, post_bias, gate, pre, pre_bias, stats = ctx.saved_tensors
+        *inputs, stats = ctx.saved_tensors
+        x, y, post, post_bias, gate, pre, pre_bias = inputs
         j = Joined()
         j.args, j.x, j.y, j.stats = ctx.args, x, y, stats
         j.parameters = (post, post_bias, gate, pre, pre_bias)
-        if dz is None and pre is not None:
-            dz = torch.zeros_like(x, memory_format=torch.contiguous_format)
-        g = join_grad(j, None if dh is None else dh.contiguous(), None if dz is None else dz.contiguous())
-        return (*g, None)
+        with torch.no_grad():
+            if dz is None and pre is not None:
+                dz = torch.zeros_like(x, memory_format=torch.contiguous_format)
+            g = join_grad(j, None if dh is None else dh.contiguous(), None if dz is None else dz.contiguous())
+        return (*_once(g, dh, dz, *inputs), None)
 
 
 def joined(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=None, **settings):
     """``join``, differentiable in x, y and the parameters: (h, z), None where
-    absent.  settings: norm, eps, carry, branch, draws."""
+    absent.  settings: norm, eps, carry, branch, draws.  A second derivative raises."""
     return _Join.apply(x, y, post, post_bias, gate, pre, pre_bias, settings)
 
 
@@ -387,12 +408,14 @@ class _Balance(torch.autograd.Function):
     @staticmethod
     def backward(ctx, d, _parts, _counts):
         logits, chosen, valid = ctx.saved_tensors
-        b = balance(logits, chosen, valid=valid, upstream=d.reshape(1), **ctx.settings)
-        return b.dlogits, None, None, None
+        with torch.no_grad():
+            b = balance(logits, chosen, valid=valid, upstream=d.reshape(1), **ctx.settings)
+        return (*_once((b.dlogits,), d, logits), None, None, None)
 
 
 def balanced(logits, chosen, *, valid=None, **settings):
     """``balance``, differentiable in logits: (loss, [balance loss, z loss], counts);
-    only the first has a gradient.  settings: balance, z, groups."""
+    only the first has a gradient, and a second derivative of it raises.  settings:
+    balance, z, groups."""
     loss, parts, counts = _Balance.apply(logits, chosen, valid, settings)
     return loss, parts.detach(), counts

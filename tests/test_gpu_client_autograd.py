@@ -106,3 +106,58 @@ def test_rows_that_lay_apart_come_back_without_gaps(client):
         lambda t: t.detach().clone(memory_format=torch.contiguous_format), lambda t: t), True)
     for k, t in want.items():
         torch.testing.assert_close(got[k], t, rtol=1e-3, atol=1e-3)
+
+
+def test_second_derivatives_of_dropout(client):
+    """Inside a graph of the backward call: d2/dx2 of sum (m x + r)^3 + x^2, on the
+    diagonal 6 (m x + r) m^2 + 2; two roundings each way of 2^-24."""
+    import torch
+    a, _, _ = make(9, 203, "float32", post=False)
+    x, r = a["x"].clone().requires_grad_(True), a["y"].clone().requires_grad_(True)
+    d = draws(0.3)
+    (g,) = torch.autograd.grad((client.dropped(x, d, r) ** 3).sum() + (x * x).sum(), x, create_graph=True)
+    gx, gr = torch.autograd.grad(g.sum(), (x, r))
+    m = client.dropout(torch.ones_like(a["x"]), d)
+    u = 6 * (a["x"] * m + a["y"])
+    torch.testing.assert_close(gx, u * m * m + 2, rtol=1e-5, atol=1e-5)
+    torch.testing.assert_close(gr, u * m, rtol=1e-5, atol=1e-5)
+
+
+def test_other_second_derivatives_are_refused(client):
+    """Also where the gradient handed in is a constant; first derivatives made with a
+    graph are as without one, and the other paths' second derivatives stay."""
+    import torch
+    a, dh, dz = make(9, 72, "float32", groups=1)
+
+    def leaves():
+        return {k: t.clone().requires_grad_(True) for k, t in a.items() if t is not None}
+
+    v = leaves()
+    plain = torch.autograd.grad([t for t in client.joined(**v)], list(v.values()), [dh, dz])
+    for power in (1, 2):
+        v = leaves()
+        h, z = client.joined(**v)
+        grads = torch.autograd.grad((h * dh).sum() + (z ** power * dz).sum(), list(v.values()), create_graph=True)
+        if power == 1:
+            assert all(torch.equal(g, w) for g, w in zip(grads, plain))
+        for g in grads:
+            assert g.requires_grad
+            with pytest.raises(RuntimeError, match="second derivatives"):
+                torch.autograd.grad(g.sum(), v["x"], retain_graph=True)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            (sum(g.sum() for g in grads) + (v["x"] ** 3).sum()).backward()
+    logits = torch.randn(12, 8, device="cuda").requires_grad_(True)
+    chosen = torch.zeros(12, 2, dtype=torch.int32, device="cuda")
+    loss, _, _ = client.balanced(logits, chosen, z=0.1)
+    (want,) = torch.autograd.grad(loss, logits, retain_graph=True)
+    (g,) = torch.autograd.grad(loss, logits, create_graph=True)
+    assert torch.equal(g, want)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        (g * g).sum().backward()
+    # A graph of the backward call that is not differentiated through the operators.
+    x = a["x"].clone().requires_grad_(True)
+    w = a["pre"].clone().requires_grad_(True)
+    h, z = client.joined(x.detach(), pre=w)
+    (z.sum() + (x ** 3).sum()).backward(create_graph=True)
+    (second,) = torch.autograd.grad(x.grad.sum(), x)
+    assert torch.equal(second, 6 * a["x"])
