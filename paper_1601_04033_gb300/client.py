@@ -81,6 +81,13 @@ def _stream(t) -> int:
     return _f._current_stream() if _raw_stream is None else _raw_stream(t.get_device())
 
 
+def _one_device(first, *others):
+    """The call's tensors (None: absent) are on one GPU; checked before any address is taken."""
+    at = first.get_device()
+    if any(t is not None and (not t.is_cuda or t.get_device() != at) for t in (first, *others)):
+        raise ValueError("CUDA tensors on one device are expected")
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -97,8 +104,6 @@ def _rows(t):
     step, one = t.stride()
     if one != 1 and cols > 1:
         raise ValueError("the values of a row must be contiguous")
-    if not t.is_cuda:
-        raise ValueError("CUDA tensors are expected")
     return t.data_ptr() or _NOWHERE, rows, cols, step
 
 
@@ -153,6 +158,7 @@ def dropout(x, draws: Draws, *, residual=None, out=None):
     be x or residual.  The gradient of x is dropout(gradient, draws)."""
     if _fast is not None:
         return _done(_fast.dropout(x, draws, residual, out))
+    _one_device(x, residual, out)
     a = _f.DropoutArgs()
     at = ctypes.addressof(a)
     if out is None:
@@ -185,6 +191,7 @@ def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=
         j.h, j.z, j.stats, j.args = _done(_fast.join(x, y, post, post_bias, gate, pre, pre_bias, _NORMS[norm], eps, carry,
                                                      branch, draws, h, z))
         return j
+    _one_device(x, y, *j.parameters, h, z)
     if (h is not None and y is None) or (z is not None and pre is None):
         raise ValueError("h goes with y, z with pre")
     if y is not None and h is None:
@@ -225,6 +232,7 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
     x = j.x
     if _fast is not None:
         return JoinGrads(*_done(_fast.join_grad(j.args, x, j.y, dh, dz, j.parameters, into or _NO_GRADS, j.stats)))
+    _one_device(x, j.y, *j.parameters, j.stats, dh, dz, *(into or _NO_GRADS))
     was = _f.JoinArgs.from_buffer_copy(j.args)
     a = _f.JoinArgs()
     at = ctypes.addressof(a)
@@ -257,8 +265,7 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
     if (a.rows, a.cols, a.dtype, a.groups) != (was.rows, was.cols, was.dtype, was.groups) or \
             any((getattr(a, n) is None) != (getattr(was, n) is None) for n in ("y", "post", "pre")):
         raise ValueError("join_grad: not the join's tensors")
-    if j.stats.dtype is not torch.float32 or j.stats.numel() != 4 * a.rows or not j.stats.is_contiguous() or \
-            not j.stats.is_cuda:
+    if j.stats.dtype is not torch.float32 or j.stats.numel() != 4 * a.rows or not j.stats.is_contiguous():
         raise ValueError("join_grad: not the join's statistics")
     a.stats = j.stats.data_ptr() or _NOWHERE
     size = _check(_f.fasgd_join_workspace(at))
@@ -292,6 +299,7 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
     given.  chosen: int32 [..., top]; valid: bool or uint8, one per row."""
     if _fast is not None:
         return Balance(*_done(_fast.balance(logits, chosen, balance, z, groups, valid, upstream, bool(grad))))
+    _one_device(logits, chosen, valid, upstream)
     a = _f.BalanceArgs()
     at = ctypes.addressof(a)
     dlogits = _new(logits) if grad else None
@@ -301,17 +309,15 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
     a.top = top = chosen.shape[-1]
     a.balance_scale = balance
     a.z_scale = z
-    if chosen.dtype is not torch.int32 or not chosen.is_contiguous() or not chosen.is_cuda or \
-            chosen.numel() != rows * top:
+    if chosen.dtype is not torch.int32 or not chosen.is_contiguous() or chosen.numel() != rows * top:
         raise ValueError("chosen must be contiguous int32 [..., top] on the GPU, a row for each of logits")
     a.chosen = chosen.data_ptr() or _NOWHERE
     if valid is not None:
-        if valid.dtype not in (torch.uint8, torch.bool) or not valid.is_contiguous() or not valid.is_cuda or \
-                valid.numel() != rows:
+        if valid.dtype not in (torch.uint8, torch.bool) or not valid.is_contiguous() or valid.numel() != rows:
             raise ValueError("valid must be contiguous bool or uint8 on the GPU, one for each row")
         a.valid = valid.data_ptr()
     if upstream is not None:
-        if upstream.dtype is not torch.float32 or upstream.numel() != 1 or not upstream.is_cuda:
+        if upstream.dtype is not torch.float32 or upstream.numel() != 1:
             raise ValueError("upstream must be one fp32 value on the GPU")
         a.upstream = upstream.data_ptr()
     size = _check(_f.fasgd_balance_workspace(at))

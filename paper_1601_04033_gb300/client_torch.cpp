@@ -56,8 +56,15 @@ void* address(const Tensor& t) {
     void* p = t.data_ptr();
     return p != nullptr ? p : reinterpret_cast<void*>(16);
 }
-void on_gpu(const Tensor& t) {
-    if (!t.is_cuda()) wrong("CUDA tensors are expected");
+/* A call's tensors (null: absent), the first of which says where they are to be; no
+ * address is taken before. */
+void one_device(std::initializer_list<const Tensor*> tensors) {
+    const Tensor* first = nullptr;
+    for (const Tensor* t : tensors) {
+        if (t == nullptr) continue;
+        if (first == nullptr) first = t;
+        if (!t->is_cuda() || t->device() != first->device()) wrong("CUDA tensors on one device are expected");
+    }
 }
 
 /* A matrix [..., cols] whose rows are evenly spaced. */
@@ -65,7 +72,6 @@ struct Matrix {
     int64_t rows, cols, ld;
     void* p;
     explicit Matrix(const Tensor& t) {
-        on_gpu(t);
         const auto size = t.sizes(), step = t.strides();
         const int64_t n = t.dim();
         if (n < 1) wrong("a matrix [..., cols] is expected");
@@ -150,7 +156,6 @@ class New {
 
 float* vector(const Tensor* t, int64_t cols) {
     if (t == nullptr) return nullptr;
-    on_gpu(*t);
     if (t->scalar_type() != at::kFloat || t->numel() != cols || !t->is_contiguous())
         wrong("parameters are contiguous fp32 vectors of cols values");
     return static_cast<float*>(address(*t));
@@ -176,7 +181,6 @@ void join_inputs(fasgd_join_args& a, const Tensor& x, const Tensor* y, const Ten
     a.pre = vector(of[3], m.cols);
     a.pre_bias = vector(of[4], m.cols);
     if (const Tensor* gate = of[2]) {
-        on_gpu(*gate);
         if (gate->dim() < 1 || gate->dim() > 2 || gate->size(-1) != m.cols || !gate->is_contiguous())
             wrong("a gate is contiguous, [cols] or [groups, cols]");
         if (gate->dim() == 2) a.groups = gate->size(0);
@@ -271,6 +275,7 @@ PyObject* py_dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return entry(nargs, 4, [&]() -> PyObject* {
         const Tensor *x = tensor(args[0]), *residual = tensor(args[2]), *out = tensor(args[3]);
         if (x == nullptr) wrong("a tensor is expected");
+        one_device({x, residual, out});
         fasgd_dropout_args a;
         std::memset(&a, 0, sizeof a);
         const Matrix m(*x);
@@ -309,6 +314,7 @@ PyObject* py_join(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         const Tensor *x = tensor(args[0]), *y = tensor(args[1]), *h = tensor(args[12]), *z = tensor(args[13]);
         const Tensor* const of[5] = {tensor(args[2]), tensor(args[3]), tensor(args[4]), tensor(args[5]), tensor(args[6])};
         if (x == nullptr) wrong("a tensor is expected");
+        one_device({x, y, of[0], of[1], of[2], of[3], of[4], h, z});
         if ((h != nullptr && y == nullptr) || (z != nullptr && of[3] == nullptr)) wrong("h goes with y, z with pre");
         fasgd_join_args a;
         std::memset(&a, 0, sizeof a);
@@ -357,6 +363,9 @@ PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         const Tensor* of[5];
         for (int i = 0; i < 5; ++i) of[i] = tensor(PyTuple_GET_ITEM(args[5], i));
         if (x == nullptr || stats == nullptr) wrong("a tensor is expected");
+        PyObject* const* into = &PyTuple_GET_ITEM(args[6], 0);
+        one_device({x, y, dh, dz, of[0], of[1], of[2], of[3], of[4], stats, tensor(into[0]), tensor(into[1]),
+                    tensor(into[2]), tensor(into[3]), tensor(into[4]), tensor(into[5]), tensor(into[6])});
         std::memcpy(&was, PyBytes_AS_STRING(args[0]), sizeof was);
         std::memset(&a, 0, sizeof a);
         a.rate = was.rate;
@@ -383,7 +392,6 @@ PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             a.dz = m.p;
             a.ld_dz = m.ld;
         }
-        PyObject* const* into = &PyTuple_GET_ITEM(args[6], 0);
         New made(*x);
         int at[7];
         PyObject* out[7];
@@ -416,7 +424,7 @@ PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                 // What the workspace depends on: that it is there, and aligned.
                 p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(256);
             } else if (i == 4) {
-                if (t->sizes() != p_of->sizes() || t->scalar_type() != p_of->scalar_type() || !t->is_contiguous() || !t->is_cuda())
+                if (t->sizes() != p_of->sizes() || t->scalar_type() != p_of->scalar_type() || !t->is_contiguous())
                     wrong("the gate's gradient must be as the gate");
                 p = static_cast<std::remove_reference_t<decltype(p)>>(address(*t));
             } else {
@@ -450,6 +458,7 @@ PyObject* py_balance(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return entry(nargs, 8, [&]() -> PyObject* {
         const Tensor *logits = tensor(args[0]), *chosen = tensor(args[1]), *valid = tensor(args[5]), *up = tensor(args[6]);
         if (logits == nullptr || chosen == nullptr) wrong("a tensor is expected");
+        one_device({logits, chosen, valid, up});
         fasgd_balance_args a;
         std::memset(&a, 0, sizeof a);
         const Matrix m(*logits);
@@ -461,20 +470,17 @@ PyObject* py_balance(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         a.balance_scale = real(args[2]);
         a.z_scale = real(args[3]);
         a.groups = whole(args[4]);
-        on_gpu(*chosen);
         a.top = chosen->dim() > 0 ? chosen->size(-1) : 0;
         if (chosen->scalar_type() != at::kInt || !chosen->is_contiguous() || chosen->numel() != m.rows * a.top)
             wrong("chosen must be contiguous int32 [..., top] on the GPU, a row for each of logits");
         a.chosen = static_cast<int32_t*>(address(*chosen));
         if (valid != nullptr) {
-            on_gpu(*valid);
             if ((valid->scalar_type() != at::kByte && valid->scalar_type() != at::kBool) || !valid->is_contiguous() ||
                 valid->numel() != m.rows)
                 wrong("valid must be contiguous bool or uint8 on the GPU, one for each row");
             a.valid = static_cast<uint8_t*>(address(*valid));
         }
         if (up != nullptr) {
-            on_gpu(*up);
             if (up->scalar_type() != at::kFloat || up->numel() != 1) wrong("upstream must be one fp32 value on the GPU");
             a.upstream = static_cast<float*>(address(*up));
         }
