@@ -58,6 +58,8 @@ def calls(c):
 
 @pytest.mark.parametrize("where", ["cuda:1", "cpu"])
 def test_tensors_of_another_device_are_refused(client, where):
+    if where == "cuda:1" and torch.cuda.device_count() == 1:
+        pytest.skip("torch looks for the second GPU where there is one")
     with FakeTensorMode(allow_non_fake_inputs=True):
         tried = 0
         for name, call, tensors in calls(client):
