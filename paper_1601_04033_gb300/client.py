@@ -49,7 +49,8 @@ _fast = _module()
 
 class Draws(NamedTuple):
     """A dropout call's rate and whose draws it takes: the client's n-th.  n is
-    to be another for every call that is to drop other elements."""
+    to be another for every call that is to drop other elements.  seed counts modulo
+    2^64; a client or n out of fasgd_dropout's range is refused."""
     rate: float
     seed: int = 0
     client: int = 0
@@ -143,6 +144,13 @@ def _intake(a, spec, *tensors):
             setattr(a, "ld_" + name, step)
 
 
+def _draws(a, draws):
+    """Draws into a struct, whose fields would cut a client or n beyond them to another's."""
+    a.rate, a.seed, client, n = draws
+    a.client = client if 0 <= client < 1 << 31 else -1
+    a.n = n if 0 <= n < 1 << 63 else -1
+
+
 def _new(like):
     """A new matrix of like's shape and type, without gaps."""
     if like.is_contiguous():
@@ -164,7 +172,7 @@ def dropout(x, draws: Draws, *, residual=None, out=None):
     if out is None:
         out = _new(x)
     _intake(a, _DROPOUT, x, out, residual)
-    a.rate, a.seed, a.client, a.n = draws
+    _draws(a, draws)
     _check(_f.fasgd_dropout(at, _stream(x)))
     return out
 
@@ -206,7 +214,7 @@ def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=
     a.carry = carry
     a.branch = branch
     if draws is not None:
-        a.rate, a.seed, a.client, a.n = draws
+        _draws(a, draws)
     j.stats = torch.empty(4 * a.rows, dtype=torch.float32, device=x.device)
     a.stats = j.stats.data_ptr() or _NOWHERE
     _check(_f.fasgd_join(at, _stream(x)))
@@ -305,6 +313,8 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
     dlogits = _new(logits) if grad else None
     _intake(a, _BALANCE, logits, dlogits)
     rows = a.rows
+    if not -(1 << 63) <= groups < 1 << 63:
+        raise OverflowError("groups is beyond 64 bits")
     a.groups = groups
     a.top = top = chosen.shape[-1]
     a.balance_scale = balance

@@ -206,16 +206,23 @@ int64_t unlocked(F call) {
     return rc;
 }
 
-/* Draws(rate, seed, client, n), or None. */
+/* Draws(rate, seed, client, n), or None.  A client or n beyond its field becomes one
+ * that the library refuses, not another's draws. */
 template <class Args>
 void draws(PyObject* o, Args& a) {
     if (o == Py_None) return;
     if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) wrong("draws are (rate, seed, client, n)");
     a.rate = PyFloat_AsDouble(PyTuple_GET_ITEM(o, 0));
     a.seed = PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(o, 1));
-    a.client = (int32_t)PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(o, 2));
-    a.n = PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(o, 3));
     if (PyErr_Occurred()) throw Status{0};
+    const auto within = [](PyObject* v, int64_t most) {
+        int beyond = 0;
+        const long long k = PyLong_AsLongLongAndOverflow(v, &beyond);
+        if (PyErr_Occurred()) throw Status{0};
+        return beyond != 0 || k < 0 || k > most ? (int64_t)-1 : (int64_t)k;
+    };
+    a.client = (int32_t)within(PyTuple_GET_ITEM(o, 2), INT32_MAX);
+    a.n = (uint64_t)within(PyTuple_GET_ITEM(o, 3), INT64_MAX);
 }
 float real(PyObject* o) {
     const double v = PyFloat_AsDouble(o);

@@ -1,0 +1,44 @@
+"""Numbers of a client operator's call that are beyond their fields: refused, not cut
+to another client's or another call's."""
+
+import pytest
+
+from test_gpu_client import _c
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=["module", "python"])
+def client(request, monkeypatch):
+    c = _c()
+    if request.param == "module":
+        if c._fast is None:
+            pytest.skip("built without torch's headers")
+    else:
+        monkeypatch.setattr(c, "_fast", None)
+    return c
+
+
+def test_draws_beyond_their_fields(client):
+    import torch
+    from paper_1601_04033_gb300 import fasgd
+    x = torch.ones(4, 256, device="cuda")
+    for who, n in (((1 << 32) + 5, 3), (1 << 31, 3), (1 << 30, 3), (1 << 64, 3), (-1, 3), (5 - (1 << 32), 3),
+                   (5 - (1 << 64), 3), (5, 1 << 48), (5, 1 << 63), (5, (1 << 64) + 3), (5, -1), (5, 3 - (1 << 64)),
+                   (5, 3 - (1 << 70))):
+        d = client.Draws(0.5, 7, who, n)
+        for call in (lambda: client.dropout(x, d), lambda: client.join(x, x.clone(), draws=d)):
+            with pytest.raises(fasgd.FasgdError, match="client|n must") as e:
+                call()
+            assert e.value.code == fasgd.EINVAL
+    for who, n in ((0, 0), ((1 << 30) - 1, (1 << 48) - 1)):
+        assert torch.equal(client.dropout(x, client.Draws(0.5, 7 - (1 << 64), who, n)),
+                           client.dropout(x, client.Draws(0.5, 7, who, n)))
+
+
+def test_groups_beyond_their_field(client):
+    import torch
+    x, ids = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 2, dtype=torch.int32, device="cuda")
+    for groups in ((1 << 64) + 1, 1 - (1 << 64), 1 << 63):
+        with pytest.raises(OverflowError):
+            client.balance(x, ids, groups=groups)
