@@ -405,7 +405,8 @@ __global__ void __launch_bounds__(kThreads, NV > 2 ? 2 : 3)
             unit_dot += dot;
             sum_z += lse * lse;
             if (a.dlogits != nullptr) {
-                const float k = t.up * inv, k1 = k * scale, k0 = k * (t.zscale * lse - scale * dot);
+                const float k = live ? t.up * inv : 0.f;       // (up may be infinite)
+                const float k1 = k * scale, k0 = k * (t.zscale * lse - scale * dot);
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
                     const Oct& w = share[v];

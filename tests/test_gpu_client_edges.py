@@ -1,9 +1,9 @@
-"""Client operators at edges that one call alone does not show: what earlier launches
-left in shared memory."""
+"""Client operators at edges: what earlier launches left in shared memory, first calls
+on many threads, gradients that are not finite."""
 
 import pytest
 
-from test_gpu_client import _c, draws, make
+from test_gpu_client import _c, draws, make, routed
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +83,19 @@ def test_first_calls_of_many_threads():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.endswith("same\n"), r.stderr[-3000:]
+
+
+@pytest.mark.parametrize("E, pad", [(5, 0), (8, 0), (60, 0), (60, 3), (256, 0), (500, 4), (1024, 0)])
+@pytest.mark.parametrize("up", [float("inf"), float("nan")])
+def test_rows_that_take_no_part_have_no_gradient_whatever_it_is_times(E, pad, up):
+    """The gradient of a row that is not valid is 0, not upstream * 0."""
+    import torch
+    for dtype in ("float32", "bfloat16"):
+        for groups in (1, 3):
+            logits, chosen, valid = routed(120, E, 2, dtype, groups=groups, ragged=groups > 1, pad=pad)
+            if valid is None:
+                valid = torch.arange(120, device="cuda") % 3 > 0
+            b = _c().balance(logits, chosen, groups=groups, valid=valid, z=0.1,
+                             upstream=torch.full((1,), up, device="cuda"))
+            assert (b.dlogits[~valid] == 0).all() and not torch.isfinite(b.dlogits[valid]).all()
+            assert torch.isfinite(b.loss).all()
