@@ -63,6 +63,14 @@ def _check(rc: int):
     return rc
 
 
+def _written(*given):
+    """Tensors of the caller's (None: absent) that a call wrote into: their versions, which
+    automatic differentiation looks at before it reads a tensor that it has saved."""
+    for t in given:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _done(result):
     """What a call of client_torch.cpp's gave: a negative status, or its tensors."""
     return _check(result) if type(result) is int else result
@@ -169,11 +177,13 @@ def dropout(x, draws: Draws, *, residual=None, out=None):
     _one_device(x, residual, out)
     a = _f.DropoutArgs()
     at = ctypes.addressof(a)
+    given = out
     if out is None:
         out = _new(x)
     _intake(a, _DROPOUT, x, out, residual)
     _draws(a, draws)
     _check(_f.fasgd_dropout(at, _stream(x)))
+    _written(given)
     return out
 
 
@@ -202,6 +212,7 @@ def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=
     _one_device(x, y, *j.parameters, h, z)
     if (h is not None and y is None) or (z is not None and pre is None):
         raise ValueError("h goes with y, z with pre")
+    given = h, z
     if y is not None and h is None:
         h = _new(x)
     if pre is not None and z is None:
@@ -218,6 +229,7 @@ def join(x, y=None, *, post=None, post_bias=None, gate=None, pre=None, pre_bias=
     j.stats = torch.empty(4 * a.rows, dtype=torch.float32, device=x.device)
     a.stats = j.stats.data_ptr() or _NOWHERE
     _check(_f.fasgd_join(at, _stream(x)))
+    _written(*given)
     j.h, j.z, j.args = h, z, bytes(a)
     return j
 
@@ -246,7 +258,8 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
     at = ctypes.addressof(a)
     for name in _SETTINGS:
         setattr(a, name, getattr(was, name))
-    dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias = into if into is not None else _NO_GRADS
+    given = into if into is not None else _NO_GRADS
+    dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias = given
     post, post_bias, gate, pre, pre_bias = j.parameters
     if dx is None:
         dx = _new(x)
@@ -281,6 +294,7 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
     a.workspace = space.data_ptr()
     a.workspace_bytes = size
     _check(_f.fasgd_join_grad(at, _stream(x)))
+    _written(*given)
     return JoinGrads(dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias)
 
 

@@ -235,9 +235,13 @@ int64_t whole(PyObject* o) {
     return v;
 }
 
-/* A result: the caller's own object, or (k >= 0) a new tensor. */
+/* A result: the caller's own object (or None), or (k >= 0) a new tensor.  What was
+ * written into a tensor of the caller's shows in its version, which automatic
+ * differentiation looks at before it reads a tensor that it has saved. */
 PyObject* object(const New& made, int k, PyObject* given) {
     if (k >= 0) return made.object(k);
+    if (given != Py_None && !THPVariable_Unpack(given).is_inference())
+        THPVariable_Unpack(given).unsafeGetTensorImpl()->bump_version();
     Py_INCREF(given);
     return given;
 }

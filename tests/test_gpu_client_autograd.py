@@ -161,3 +161,34 @@ def test_other_second_derivatives_are_refused(client):
     (z.sum() + (x ** 3).sum()).backward(create_graph=True)
     (second,) = torch.autograd.grad(x.grad.sum(), x)
     assert torch.equal(second, 6 * a["x"])
+
+
+def test_writes_into_saved_tensors_are_noticed(client):
+    """A tensor that an earlier operation saved and a call then writes into: its backward
+    raises, as after any other in-place operation."""
+    import torch
+    a, dh, dz = make(6, 24, "float32", groups=1)
+    w = a["pre"]
+    j = client.join(**a)
+    calls = [lambda t, v: client.dropout(a["x"], draws(0.3), out=t), lambda t, v: client.dropout(t, draws(0.3), out=t),
+             lambda t, v: client.join(**a, h=t), lambda t, v: client.join(**a, z=t)]
+    for name in client.JoinGrads._fields:
+        if name in ("x", "y"):
+            calls.append(lambda t, v, name=name: client.join_grad(j, dh, dz, into=client.JoinGrads(**{name: t})))
+        elif a[name] is not None:
+            calls.append(lambda t, v, name=name: client.join_grad(j, dh, dz, into=client.JoinGrads(**{name: v})))
+    assert len(calls) == 9
+    for call in calls:
+        leaf, vector = a["x"].clone().requires_grad_(True), w.clone().requires_grad_(True)
+        t, v = leaf * 1.0, vector * 1.0
+        out = (t * t).sum() + (v * v).sum()
+        with torch.no_grad():
+            call(t, v)
+        with pytest.raises(RuntimeError, match="inplace"):
+            out.backward()
+    # Inference tensors have no version; new tensors and what is only read keep theirs.
+    with torch.inference_mode():
+        x = a["x"].clone()
+        assert torch.equal(client.dropout(x, draws(0.3), out=x), client.dropout(a["x"], draws(0.3)))
+        client.join(**a, h=x)
+    assert client.join(**a).h._version == 0 and all(t._version <= 1 for t in (a["x"], dh))
