@@ -261,11 +261,11 @@ def join_grad(j: Joined, dh, dz=None, *, into: JoinGrads | None = None) -> JoinG
     given = into if into is not None else _NO_GRADS
     dx, dy, dpost, dpost_bias, dgate, dpre, dpre_bias = given
     post, post_bias, gate, pre, pre_bias = j.parameters
+    if any(t is None and d is not None for t, d in zip((x, j.y, *j.parameters), given)):
+        raise ValueError("the gradient of a tensor that is not there")
     if dx is None:
         dx = _new(x)
-    if j.y is None:
-        dy = None
-    elif dy is None:
+    if j.y is not None and dy is None:
         dy = _new(x)
     if post is not None and dpost is None:
         dpost = torch.empty_like(post)

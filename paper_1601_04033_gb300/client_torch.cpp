@@ -424,12 +424,12 @@ PyObject* py_join_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         matrix(0, a.dx, a.ld_dx);
         if (y != nullptr)
             matrix(1, a.dy, a.ld_dy);
-        else
-            out[1] = Py_None;
+        else if (tensor(into[1]) != nullptr)
+            wrong("the gradient of a tensor that is not there");
         const auto parameter = [&](int i, auto*& p) {
             const Tensor *p_of = of[i - 2], *t = tensor(into[i]);
             if (p_of == nullptr) {
-                out[i] = Py_None;
+                if (t != nullptr) wrong("the gradient of a parameter that is not there");
             } else if (t == nullptr) {
                 at[i] = made.add(*p_of, &p);
                 // What the workspace depends on: that it is there, and aligned.

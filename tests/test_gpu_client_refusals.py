@@ -1,5 +1,5 @@
-"""Numbers of a client operator's call that are beyond their fields: refused, not cut
-to another client's or another call's."""
+"""Arguments of a client operator's call that are refused: numbers beyond their fields, not cut
+to another client's or another call's, and places for gradients of what is not there."""
 
 import pytest
 
@@ -42,3 +42,20 @@ def test_groups_beyond_their_field(client):
     for groups in ((1 << 64) + 1, 1 - (1 << 64), 1 << 63):
         with pytest.raises(OverflowError):
             client.balance(x, ids, groups=groups)
+
+
+def test_gradients_of_absent_tensors_are_refused(client):
+    """`into` for a tensor that the join does not have: no unwritten tensor is handed back."""
+    import torch
+    x, w = torch.ones(4, 8, device="cuda"), torch.ones(8, device="cuda")
+    full = client.join(x, x.clone(), post=w, gate=w, pre=w)
+    for j, absent in ((full, ("post_bias", "pre_bias")), (client.join(x, pre=w), ("y", "post", "post_bias", "gate", "pre_bias")),
+                      (client.join(x, x.clone()), ("post", "post_bias", "gate", "pre", "pre_bias"))):
+        dz = x if j.z is not None else None
+        for name in absent:
+            d = torch.full_like(x if name == "y" else w, 5.0)
+            with pytest.raises(ValueError, match="not there"):
+                client.join_grad(j, x, dz, into=client.JoinGrads(**{name: d}))
+            assert (d == 5.0).all()
+        g = client.join_grad(j, x, dz)
+        assert all(getattr(g, name) is None for name in absent)
