@@ -137,13 +137,15 @@ def torch_home() -> str | None:
 def build_client(force: bool = False) -> str | None:
     """Build the CPython module of the client operators on torch tensors
     (client_torch.cpp) against libfasgd.so and torch; returns its path, or None,
-    with a warning where it does not compile, where client.py's own code serves."""
+    with a warning where it does not compile, where client.py's own code serves.
+    A module of older sources does not stay: its structs may not be the library's."""
     home, include = torch_home(), sysconfig.get_paths()["include"]
+    inputs = [CLIENT_SRC, os.path.join(INCLUDE, "fasgd.h"), *([] if home is None else [os.path.join(home, "version.py")])]
+    if os.path.exists(CLIENT) and (force or os.path.getmtime(CLIENT) < max(map(os.path.getmtime, inputs))):
+        os.remove(CLIENT)
     if home is None or not os.path.exists(os.path.join(include, "Python.h")):
         return None
-    newest = max(os.path.getmtime(p) for p in (CLIENT_SRC, os.path.join(INCLUDE, "fasgd.h"),
-                                               os.path.join(home, "version.py")))
-    if not force and os.path.exists(CLIENT) and os.path.getmtime(CLIENT) >= newest:
+    if os.path.exists(CLIENT):
         return CLIENT
     with open(os.path.join(home, "version.py")) as f:
         version = re.search(r"__version__ = '([^']+)'", f.read()).group(1)
