@@ -575,7 +575,7 @@ FASGD_API int fasgd_dropout(const fasgd_dropout_args* a, void* stream);
  * gate: groups x cols values without gaps, of type gate_dtype (FASGD_F32 or
  * dtype); row r takes gate row r div (rows / groups) -- one learned vector
  * (groups = 1), or one computed for each sequence or token.  groups divides
- * rows, groups >= 1.
+ * rows, 1 <= groups <= 2^40.
  * Without y: post, gate, h and dy are NULL, pre is given (the first norm of a
  * network).  h is written iff y is given, z iff pre is.  stats: fp32[4 rows],
  * 16-byte aligned (mean and 1/sqrt of y, then of h), for the gradient; may be

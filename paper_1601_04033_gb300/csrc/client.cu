@@ -116,8 +116,8 @@ int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 // The checks that fasgd_join and fasgd_join_grad share, and the kernels' view.
 int fill_join(const char* call, const fasgd_join_args& u, fasgd::JoinArgs& a) {
     if (int rc = check_shape(call, u.rows, u.cols, FASGD_COLS_MAX, u.dtype)) return rc;
-    if (u.groups < 1 || u.rows % u.groups != 0)
-        return fail(FASGD_EINVAL, "%s: groups must be at least 1 and divide rows", call);
+    if (u.groups < 1 || u.groups > kRowsMax || u.rows % u.groups != 0)      // (of no rows there may be any number)
+        return fail(FASGD_EINVAL, "%s: groups must be in [1, 2^40] and divide rows", call);
     if (u.norm != FASGD_RMS_NORM && u.norm != FASGD_LAYER_NORM)
         return fail(FASGD_EINVAL, "%s: norm %d is not an fasgd_norm", call, u.norm);
     if (!(u.eps > 0.f) || !std::isfinite(u.eps) || !std::isfinite(u.carry) || !std::isfinite(u.branch))
