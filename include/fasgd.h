@@ -519,12 +519,18 @@ FASGD_API int fasgd_sim_quadratic_loss(int64_t P, const float* theta, const floa
  * of `cols` consecutive values, ld values from one row to the next (ld >= cols;
  * not looked at where there are fewer than two rows); base and rows need the
  * alignment of their type only.  Fastest are bases aligned to eight values, with
- * rows that follow each other without a gap or with cols and ld multiples of 8;
- * other joins ran at 50 to 85 % of that rate, other dropouts at 30 %, other
- * balance losses at 20 to 70 %.  Joins of more than 32,768 columns are slow in any
- * layout (0.8 TB/s forward, 0.3 TB/s gradients).  An output must not share memory
- * with another argument, except as fasgd_dropout says.  Everything computed is
- * held in fp32 and rounded once, where it is stored.  A call with rows = 0 reads
+ * cols and ld multiples of 8 (dropouts: or rows without a gap).  Rows of other
+ * widths that follow each other without a gap ran at 60 to 100 % of that rate in
+ * joins of 200 to 1,021 columns, at 20 to 65 % in joins of 61 and of 8,190, and at
+ * 65 % in a balance loss of 60 experts; rows that lie otherwise at 50 to 85 % in
+ * joins, 30 % in dropouts and 20 to 70 % in balance losses.  Dropouts at rate 0 ran
+ * at 30 % in any layout; joins of more than 32,768 columns are slow in any (0.8 TB/s
+ * forward, 0.3 TB/s gradients).  An output must not share memory with another
+ * argument, except as fasgd_dropout says.  Everything computed is held in fp32 and
+ * rounded once, where it is stored; the fast layouts take the device's approximate
+ * logarithm, quotient and 1/sqrt (a log-sum-exp is then off by up to some 2^-21
+ * near 0), the others its accurate ones, so that layouts may differ in the last bits.
+ * What is read is the matrix's own memory, or between its rows.  A call with rows = 0 reads
  * nothing and writes zeros to the gradients of parameters.  Limits: rows <= 2^40,
  * cols <= FASGD_COLS_MAX (fasgd_dropout: 2^40).
  * Errors: EINVAL (text via fasgd_last_error(NULL)), ECUDA.
@@ -586,7 +592,9 @@ FASGD_API int fasgd_dropout(const fasgd_dropout_args* a, void* stream);
  * stats of the forward call (h is formed again, unrounded) and the same
  * parameters and draws; h and z are not looked at.  dx is written, and dy iff y
  * is given; dpost, dpost_bias, dpre, dpre_bias (fp32[cols]) and dgate (as gate)
- * where not NULL.  Sums over rows are fp32 in a fixed order.  workspace:
+ * where not NULL.  Sums over rows are fp32 in a fixed order.  A gradient that is not
+ * finite makes its place in dx and dy so, dropped or not, and under a norm its row's.
+ * workspace:
  * 16-byte aligned device memory of at least fasgd_join_workspace() bytes.
  *
  * fasgd_join_workspace -- that size, for the rows, cols, groups, dtype and

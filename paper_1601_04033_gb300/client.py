@@ -11,6 +11,11 @@ Activations are fp32, bf16 or fp16 CUDA tensors, [..., cols], rows evenly spaced
 parameters (norm weights and biases, a learned gate) are fp32 -- views into the
 client's flat copy of theta will do, and the gradients may be written straight
 into views of the flat vector that is pushed.
+
+A call's new tensors share one storage where they are small (1 MiB together): each
+is contiguous and its own, but one that is kept keeps the others' memory, and its
+storage must not be resized or freed by hand.  Tensors given as out, h, z or into
+have the storages that they came with.
 """
 
 from __future__ import annotations

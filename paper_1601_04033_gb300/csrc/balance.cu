@@ -199,7 +199,8 @@ __device__ __forceinline__ void join_loss(const BalanceArgs& a, const Totals& t,
     if (threadIdx.x == 0) store_loss(a, t, s.x, s.y);
 }
 
-// Any width, stride and alignment.  A unit is `unit_rows` consecutive rows of one
+// Any width, stride and alignment (and accurate logarithms and quotients, where rows in
+// octets have fast ones: 262144 x 256 bf16 131 us, 53).  A unit is `unit_rows` consecutive rows of one
 // group; a block takes every gridDim-th unit, a warp a row at a time.
 template <class T>
 __global__ void __launch_bounds__(kThreads)

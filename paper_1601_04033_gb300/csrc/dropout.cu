@@ -111,6 +111,8 @@ cudaError_t launch(const DropoutArgs& a, int num_sms, cudaStream_t stream) {
         return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (kOctet * sizeof(T)) == 0 &&
                                 (gapless || (a.cols % kOctet == 0 && ld % kOctet == 0)));
     };
+    // (At cut 0 keep2 would drop draws of 0; the kernel of any layout takes it, 16384 x 4096
+    // bf16 both directions in 354 us, 100 with draws.)
     if (a.drop.cut != 0 && fits(a.x, a.ld_x) && fits(a.residual, a.ld_residual) && fits(a.out, a.ld_out)) {
         DropoutRows m;
         m.octets = count / kOctet;

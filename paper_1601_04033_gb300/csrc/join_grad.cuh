@@ -168,10 +168,11 @@ __host__ __device__ __forceinline__ int64_t gates_left(const JoinArgs& a) {
 //
 // It moves 12 bytes an element (16-bit types) and issues about 50 instructions for
 // each, a fifth of them the draws: instructions bound it, not memory.  32768 x 4096
-// bf16 with dropout: 281 us, 5.7 TB/s; without 5.3 to 6.3 TB/s; layer norm with
-// dropout 381 us, 4.2 TB/s; fp32 3.8 to 4.1 TB/s.  512 threads an SM of 128 registers hold
-// the vectors and sums of 4,096 columns; wider rows take a cluster, whose barrier
-// for every row shows: 16384 x 8192 545 us, 3.0 TB/s.
+// bf16 with dropout: 281 us, 5.7 TB/s; without 5.3 to 6.3 TB/s.  Layer norm with
+// dropout 381 us, 4.2 TB/s, and fp32 3.8 to 4.1 TB/s wait for shared memory (short
+// scoreboard; fp32 for its copies and the memory pipe too).  512 threads an SM of 128
+// registers hold the vectors and sums of 4,096 columns; wider rows take a cluster,
+// whose barrier for every row shows: 16384 x 8192 543 us, 3.0 TB/s.
 struct Unit {
     int64_t row, step, rows;     // first row, from row to row, one past the last
     __device__ Unit(const JoinArgs& a, int64_t unit) {
