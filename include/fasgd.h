@@ -688,6 +688,157 @@ typedef struct fasgd_balance_args {
 FASGD_API int fasgd_balance(const fasgd_balance_args* a, void* stream);
 FASGD_API int64_t fasgd_balance_workspace(const fasgd_balance_args* a);
 
+/*
+ * Routed experts: the way of the rows to their experts and back, and the experts'
+ * matrix products.  Arguments, types, limits and errors as for the operators above,
+ * where nothing else is said; the parameters here may be of the rows' type too.
+ *
+ * fasgd_route -- a router's choices into the experts' order.  chosen: int32[rows x
+ * top], without gaps; entry a = t top + k sends row t to an expert, or, outside
+ * [0, experts), nowhere.  The n = rows top entries that go somewhere have the places
+ * 0, 1, ... by (expert, a):
+ *   offsets[e] = the first place of expert e, offsets[experts] = their number  (int32)
+ *   order[i]   = the entry whose place is i; -1 behind the last                (int32[n])
+ *   place[a]   = the place of entry a; -1: it goes nowhere                     (int32[n])
+ * n < 2^31, experts <= FASGD_EXPERTS_MAX.  workspace: 16-byte aligned device memory of at
+ * least fasgd_route_workspace() bytes, which the shape alone fixes (-1 on a bad one).
+ */
+typedef struct fasgd_route_args {
+    int64_t rows, top, experts;
+    const int32_t* chosen;
+    int32_t* offsets;
+    int32_t* order;
+    int32_t* place;
+    void* workspace;
+    int64_t workspace_bytes;
+} fasgd_route_args;
+FASGD_API int fasgd_route(const fasgd_route_args* a, void* stream);
+FASGD_API int64_t fasgd_route_workspace(const fasgd_route_args* a);
+
+/*
+ * Between rows (a matrix of `rows` rows) and places (one of n = rows top), both of
+ * `cols` columns, by the order and place that fasgd_route gives; weight: fp32[rows x
+ * top], without gaps.  What is outside [0, n) in them stands for "nowhere".
+ *
+ * fasgd_gather -- places[i] = rows[order[i] div top]; 0 where order[i] is nowhere.
+ * fasgd_combine -- row t = sum_k weight[t, k] places[place[t, k]], over the k that have
+ * a place, in k's order and fp32 (weight NULL: 1).
+ * fasgd_combine_grad -- given the gradient of combine's rows (in row_values): that of its
+ * places, dplaces[i] = weight[order[i]] rows[order[i] div top] (0: nowhere), and
+ * dweight[a] = <rows[a div top], places[place[a]]> (0: nowhere; fp32[n]; may be NULL).
+ * The gradient of gather is combine without a weight, and the other way round.
+ * A place that `order` and `place` do not agree on may be written twice or not at all.
+ * cols <= FASGD_COLS_MAX, n < 2^31.
+ */
+typedef struct fasgd_exchange_args {
+    int64_t rows, top, cols;
+    void* row_values;           /* read by gather and combine_grad, written by combine */
+    int64_t ld_rows;
+    void* places;               /* written by gather, read by combine and combine_grad */
+    int64_t ld_places;
+    const int32_t* order;       /* gather, combine_grad */
+    const int32_t* place;       /* all */
+    const float* weight;        /* combine, combine_grad */
+    void* dplaces;              /* combine_grad */
+    int64_t ld_dplaces;
+    float* dweight;             /* combine_grad */
+    int32_t dtype;              /* enum fasgd_dtype */
+    int32_t reserved;           /* 0 */
+} fasgd_exchange_args;
+FASGD_API int fasgd_gather(const fasgd_exchange_args* a, void* stream);
+FASGD_API int fasgd_combine(const fasgd_exchange_args* a, void* stream);
+FASGD_API int fasgd_combine_grad(const fasgd_exchange_args* a, void* stream);
+
+/*
+ * fasgd_multiply -- the experts' products: y[i] = x[i] w[e] for offsets[e] <= i <
+ * offsets[e + 1]; a row that no expert has (before offsets[0], behind the last) is 0.
+ * x: rows x inputs; y: rows x outputs; offsets: int32[experts + 1] on the device, as
+ * fasgd_route gives them (what leaves [0, rows] or falls is cut to it; experts that
+ * share rows leave those rows' values to chance).
+ * w: `experts` matrices, step_w values apart.  Those are inputs x outputs, rows ld_w
+ * apart, or (w_flip) outputs x inputs; of type w_dtype: FASGD_F32 or dtype.  Parameters
+ * of FASGD_F32 take part rounded to dtype.
+ * fasgd_multiply_grad -- given dy: dx[i] = dy[i] w[e]^T (0 where no expert has the row) and
+ * dw[e] = sum_i x[i]^T dy[i] (0 for an expert without rows), of type w_dtype and laid out
+ * by ld_dw, step_dw and dw_flip.  dx or dw may be NULL.  x is read for dw only, w for dx.
+ * Sums are fp32, in an order that the arguments fix.  Rows that no expert has are not
+ * read, whatever they hold.
+ * rows < 2^31; inputs, outputs <= FASGD_COLS_MAX; experts <= FASGD_EXPERTS_MAX.
+ * workspace: 256-byte aligned device memory of at least fasgd_multiply_workspace() bytes
+ * (for fasgd_multiply_grad where dx or dw is given, else for fasgd_multiply), which the
+ * sizes, types, strides and alignments fix (-1 on a bad argument).
+ */
+typedef struct fasgd_multiply_args {
+    int64_t rows, inputs, outputs, experts;
+    const int32_t* offsets;
+    const void* x;
+    int64_t ld_x;
+    const void* w;
+    int64_t ld_w, step_w;
+    void* y;
+    int64_t ld_y;
+    const void* dy;
+    int64_t ld_dy;
+    void* dx;
+    int64_t ld_dx;
+    void* dw;
+    int64_t ld_dw, step_dw;
+    void* workspace;
+    int64_t workspace_bytes;
+    int32_t dtype;              /* enum fasgd_dtype: x, y and their gradients */
+    int32_t w_dtype;            /* FASGD_F32, or dtype: w and dw */
+    int32_t w_flip, dw_flip;    /* 0: inputs x outputs, 1: outputs x inputs */
+} fasgd_multiply_args;
+FASGD_API int fasgd_multiply(const fasgd_multiply_args* a, void* stream);
+FASGD_API int fasgd_multiply_grad(const fasgd_multiply_args* a, void* stream);
+FASGD_API int64_t fasgd_multiply_workspace(const fasgd_multiply_args* a);
+
+/*
+ * fasgd_score -- softmax cross entropy of rows z against classes, from the network's
+ * last product on: s = z w (rows x classes, never kept: it is formed in pieces),
+ *   row_loss[t] = log sum_v exp s[t, v] - s[t, label t]      (fp32; 0 without a label)
+ *   loss        = sum_t row_loss[t] / N, N rows with a label (fp32[1]; 0 for N = 0)
+ *   g[t, v]     = upstream / N (exp(s[t, v] - lse_t) - [v = label t])
+ *   dz = g w^T, dw = z^T g                                   (each may be NULL)
+ * labels: int64[rows]; a row whose label is outside [0, classes) has none: it does not
+ * take part, whatever it holds, and its dz is 0.  z: rows x cols; w and dw: cols x
+ * classes, or (flip) classes x cols.  upstream: device float or NULL (1).
+ * s and its sums are fp32; for 16-bit types g takes part in its two products rounded to
+ * dtype.  rows < 2^31, cols <= FASGD_COLS_MAX, classes <= 2^24.
+ * lse: fp32[rows] (rows without a label: any value) or NULL.  known = 0: it is written.
+ * known = 1: it holds what an earlier call left there for the same z, w and labels; loss
+ * and row_loss are then not looked at, and only dz and dw, one of them at least, are
+ * written, without the first sweep over the classes.
+ * workspace: 256-byte aligned device memory of at least fasgd_score_workspace() bytes (-1 on
+ * a bad argument); it does not grow with rows x classes beyond FASGD_SCORE_PIECE bytes for g
+ * (or 64 classes of it).
+ */
+#define FASGD_CLASSES_MAX ((int64_t)1 << 24)
+#define FASGD_SCORE_PIECE ((int64_t)1 << 29)
+typedef struct fasgd_score_args {
+    int64_t rows, cols, classes;
+    const void* z;
+    int64_t ld_z;
+    const void* w;
+    int64_t ld_w;
+    const int64_t* labels;
+    const float* upstream;
+    float* loss;
+    float* row_loss;
+    float* lse;
+    void* dz;
+    int64_t ld_dz;
+    void* dw;
+    int64_t ld_dw;
+    void* workspace;
+    int64_t workspace_bytes;
+    int32_t dtype;              /* enum fasgd_dtype: z, w and their gradients */
+    int32_t w_flip, dw_flip;    /* 0: cols x classes, 1: classes x cols */
+    int32_t known;              /* 1: lse is read */
+} fasgd_score_args;
+FASGD_API int fasgd_score(const fasgd_score_args* a, void* stream);
+FASGD_API int64_t fasgd_score_workspace(const fasgd_score_args* a);
+
 /* Text of the last failure on h, or, when h is NULL, of the last failed call
  * made without a handle (fasgd_create, bfasgd_fetch_apply, fasgd_sim_*,
  * bfasgd_select_compact_noalloc, the client operators). */

@@ -1,16 +1,20 @@
 """Client operators on torch tensors: what a client computes between a fetch and a
-push, besides its matrix products, when its model is a deep residual network.
+push when its model is a deep residual network with routed experts and a loss over
+classes.
 
-``dropout``, ``join`` / ``join_grad`` and ``balance`` forward to the entry points
-of the same names in include/fasgd.h, which say what they compute; they run on
+``dropout``, ``join`` / ``join_grad``, ``balance``, ``route``, ``gather``, ``combine`` /
+``combine_grad``, ``multiply`` / ``multiply_grad`` and ``score`` forward to the entry
+points of the same names in include/fasgd.h, which say what they compute; they run on
 torch's current stream and allocate their outputs and workspace from torch, on
-that stream.  ``Join`` and ``dropped``, ``joined``, ``balanced`` are the same
-calls inside torch's automatic differentiation.
+that stream.  ``dropped``, ``joined``, ``balanced``, ``gathered``, ``combined``,
+``multiplied`` and ``scored`` are the same calls inside torch's automatic
+differentiation.
 
 Activations are fp32, bf16 or fp16 CUDA tensors, [..., cols], rows evenly spaced;
-parameters (norm weights and biases, a learned gate) are fp32 -- views into the
-client's flat copy of theta will do, and the gradients may be written straight
-into views of the flat vector that is pushed.
+parameters (norm weights and biases, a learned gate, experts' matrices) are fp32 --
+views into the client's flat copy of theta will do, and the gradients may be written
+straight into views of the flat vector that is pushed.  Experts' matrices may be of the
+activations' type too; ``score``'s classes are.
 
 A call's new tensors share one storage where they are small (1 MiB together): each
 is contiguous and its own, but one that is kept keeps the others' memory, and its
@@ -362,6 +366,316 @@ def balance(logits, chosen, *, balance=0.01, z=0.0, groups=1, valid=None, upstre
     return Balance(loss, counts, dlogits)
 
 
+class Route(NamedTuple):
+    """What ``route`` gives: each expert's first place, each place's entry, each entry's place."""
+    offsets: object    # int32 [experts + 1]
+    order: object      # int32 [rows * top]
+    place: object      # int32 [rows, top]
+
+
+def _ints(t, what):
+    if t.dtype is not torch.int32 or not t.is_contiguous():
+        raise ValueError(what + " must be contiguous int32 on the GPU")
+    return t.data_ptr() or _NOWHERE
+
+
+def _space(a, workspace, like):
+    """The workspace of a call, which its struct gets too."""
+    size = _check(workspace(ctypes.addressof(a)))
+    space = torch.empty(size, dtype=torch.uint8, device=like.device)
+    a.workspace = space.data_ptr()
+    a.workspace_bytes = size
+    return space
+
+
+def route(chosen, experts: int) -> Route:
+    """fasgd_route: a router's choices (int32 [..., top]; outside [0, experts): none) into
+    the experts' order."""
+    _one_device(chosen)
+    a = _f.RouteArgs()
+    if chosen.dim() == 0:
+        raise ValueError("chosen must be contiguous int32 on the GPU, [..., top]")
+    a.chosen = _ints(chosen, "chosen")
+    a.top = chosen.shape[-1]
+    a.rows = chosen.numel() // a.top if a.top else 0
+    if not -(1 << 63) <= experts < 1 << 63:
+        raise OverflowError("experts is beyond 64 bits")
+    a.experts = experts
+    space = _space(a, _f.fasgd_route_workspace, chosen)
+    n = chosen.numel()
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=chosen.device)
+    order = torch.empty(n, dtype=torch.int32, device=chosen.device)
+    place = torch.empty_like(chosen)
+    a.offsets = offsets.data_ptr()
+    a.order = order.data_ptr() or _NOWHERE
+    a.place = place.data_ptr() or _NOWHERE
+    _check(_f.fasgd_route(ctypes.addressof(a), _stream(chosen)))
+    del space
+    return Route(offsets, order, place)
+
+
+def _exchange(rows_like, route, weight=None):
+    """A struct of the calls between rows and places, with the route's part."""
+    a = _f.ExchangeArgs()
+    _, order, place = route
+    if place.dim() == 0:
+        raise ValueError("a route's place is [..., top]")
+    a.top = place.shape[-1]
+    a.rows = place.numel() // a.top if a.top else 0
+    a.place = _ints(place, "a route's place")
+    a.order = _ints(order, "a route's order")
+    if order.numel() != place.numel():
+        raise ValueError("a route's order and place have as many entries as each other")
+    a.dtype = _dtype(rows_like)
+    if weight is not None:
+        if weight.dtype is not torch.float32 or weight.numel() != place.numel() or not weight.is_contiguous():
+            raise ValueError("weight must be contiguous fp32, one for each entry")
+        a.weight = weight.data_ptr() or _NOWHERE
+    return a
+
+
+def _at_rows(a, t):
+    a.row_values, rows, cols, a.ld_rows = _rows(t)
+    if rows != a.rows or (a.cols and cols != a.cols):
+        raise ValueError("a matrix with a row for each of the route's is expected, as wide as its places")
+    a.cols = cols
+
+
+def _at_places(a, t):
+    p, rows, cols, ld = _rows(t)
+    if rows != a.rows * a.top or (a.cols and cols != a.cols):
+        raise ValueError("a matrix with a row for each of the route's places is expected, as wide as its rows")
+    a.cols = cols
+    return p, ld
+
+
+def _same_type(t, of):
+    if t.dtype is not of.dtype:
+        raise ValueError("matrices of one type are expected")
+
+
+def gather(x, route: Route, *, out=None):
+    """fasgd_gather: x's rows at their places, [rows * top, cols]; 0 at places that no entry has."""
+    _one_device(x, route.order, route.place, out)
+    a = _exchange(x, route)
+    _at_rows(a, x)
+    given = out
+    if out is None:
+        out = torch.empty((a.rows * a.top, a.cols), dtype=x.dtype, device=x.device)
+    _same_type(out, x)
+    a.places, a.ld_places = _at_places(a, out)
+    _check(_f.fasgd_gather(ctypes.addressof(a), _stream(x)))
+    _written(given)
+    return out
+
+
+def combine(y, route: Route, weight=None, *, out=None):
+    """fasgd_combine: each row's sum over its places in y, times weight (fp32, as the route's
+    place) if given: [..., cols]."""
+    _one_device(y, route.order, route.place, weight, out)
+    a = _exchange(y, route, weight)
+    a.places, a.ld_places = _at_places(a, y)
+    given = out
+    if out is None:
+        out = torch.empty((*route.place.shape[:-1], a.cols), dtype=y.dtype, device=y.device)
+    _same_type(out, y)
+    _at_rows(a, out)
+    _check(_f.fasgd_combine(ctypes.addressof(a), _stream(y)))
+    _written(given)
+    return out
+
+
+class CombineGrads(NamedTuple):
+    y: object = None
+    weight: object = None
+
+
+def combine_grad(y, route: Route, weight, dout, *, into: CombineGrads | None = None) -> CombineGrads:
+    """fasgd_combine_grad: the gradients of ``combine``'s y and weight from that of its result.
+    into: where to write them (new tensors where None)."""
+    dy, dweight = into if into is not None else (None, None)
+    _one_device(y, route.order, route.place, weight, dout, dy, dweight)
+    if weight is None:
+        raise ValueError("the gradient of a combination without weights is gather's")
+    a = _exchange(y, route, weight)
+    a.places, a.ld_places = _at_places(a, y)
+    _same_type(dout, y)
+    _at_rows(a, dout)
+    given = dy, dweight
+    if dy is None:
+        dy = torch.empty((a.rows * a.top, a.cols), dtype=y.dtype, device=y.device)
+    _same_type(dy, y)
+    a.dplaces, a.ld_dplaces = _at_places(a, dy)
+    if dweight is None:
+        dweight = torch.empty_like(weight)
+    elif dweight.dtype is not torch.float32 or dweight.numel() != weight.numel() or not dweight.is_contiguous():
+        raise ValueError("the weights' gradient must be as the weights")
+    a.dweight = dweight.data_ptr() or _NOWHERE
+    _check(_f.fasgd_combine_grad(ctypes.addressof(a), _stream(y)))
+    _written(*given)
+    return CombineGrads(dy, dweight)
+
+
+def _matrices(t, dims):
+    """(address, shape, ld, step, flip) of a matrix, or of several one step apart, whose rows or
+    (flip) columns are consecutive values."""
+    if t.dim() != dims:
+        raise ValueError("a matrix is expected" if dims == 2 else "[experts, inputs, outputs] is expected")
+    rows, cols = t.shape[-2:]
+    down, along = t.stride()[-2:]
+    if along == 1 or cols == 1:
+        flip, ld = 0, down
+    elif down == 1 or rows == 1:
+        flip, ld = 1, along
+    else:
+        raise ValueError("the values of a matrix' rows or columns must be contiguous")
+    return t.data_ptr() or _NOWHERE, t.shape, ld, t.stride(0) if dims == 3 else 0, flip
+
+
+def _products(x, w, offsets):
+    """A struct of the experts' products without their matrices' addresses."""
+    a = _f.MultiplyArgs()
+    a.x, a.rows, a.inputs, a.ld_x = _rows(x)
+    a.dtype = _dtype(x)
+    a.w, (a.experts, inputs, a.outputs), a.ld_w, a.step_w, a.w_flip = _matrices(w, 3)
+    if inputs != a.inputs:
+        raise ValueError("w is [experts, x's columns, outputs]")
+    if w.dtype is not torch.float32 and w.dtype is not x.dtype:
+        raise ValueError("w is of fp32 or of x's type")
+    a.w_dtype = _dtype(w)
+    a.offsets = _ints(offsets, "offsets")
+    if offsets.numel() != a.experts + 1:
+        raise ValueError("offsets has one entry more than there are experts")
+    return a
+
+
+def multiply(x, w, offsets, *, out=None):
+    """fasgd_multiply: rows of x, in their experts' order, times their experts' matrices
+    w[e] ([experts, inputs, outputs], rows or columns contiguous; fp32 or x's type); 0
+    where no expert has the row.  offsets: ``route``'s."""
+    _one_device(x, w, offsets, out)
+    a = _products(x, w, offsets)
+    given = out
+    if out is None:
+        out = torch.empty((*x.shape[:-1], a.outputs), dtype=x.dtype, device=x.device)
+    _same_type(out, x)
+    a.y, rows, cols, a.ld_y = _rows(out)
+    if (rows, cols) != (a.rows, a.outputs):
+        raise ValueError("out is [x's rows, w's outputs]")
+    space = _space(a, _f.fasgd_multiply_workspace, x)
+    _check(_f.fasgd_multiply(ctypes.addressof(a), _stream(x)))
+    del space
+    _written(given)
+    return out
+
+
+class MultiplyGrads(NamedTuple):
+    x: object = None
+    w: object = None
+
+
+def multiply_grad(x, w, offsets, dy, *, grads=(True, True), into: MultiplyGrads | None = None) -> MultiplyGrads:
+    """fasgd_multiply_grad: the gradients of ``multiply``'s x (in x's type) and w (in w's type and
+    layout) from that of its result.  grads: which of them; into: where to write them
+    (new tensors where None)."""
+    dx, dw = into if into is not None else (None, None)
+    _one_device(x, w, offsets, dy, dx, dw)
+    a = _products(x, w, offsets)
+    a.dy, rows, cols, a.ld_dy = _rows(dy)
+    _same_type(dy, x)
+    if (rows, cols) != (a.rows, a.outputs):
+        raise ValueError("dy is [x's rows, w's outputs]")
+    given = dx, dw
+    if (dx is not None and not grads[0]) or (dw is not None and not grads[1]):
+        raise ValueError("a place for a gradient that is not wanted")
+    if grads[0]:
+        if dx is None:
+            dx = _new(x)
+        _same_type(dx, x)
+        a.dx, rows, cols, a.ld_dx = _rows(dx)
+        if (rows, cols) != (a.rows, a.inputs):
+            raise ValueError("x's gradient is as x")
+    if grads[1]:
+        if dw is None:
+            dw = torch.empty_like(w)
+        _same_type(dw, w)
+        a.dw, shape, a.ld_dw, a.step_dw, a.dw_flip = _matrices(dw, 3)
+        if shape != w.shape:
+            raise ValueError("w's gradient is as w")
+    space = _space(a, _f.fasgd_multiply_workspace, x)
+    _check(_f.fasgd_multiply_grad(ctypes.addressof(a), _stream(x)))
+    del space
+    _written(*given)
+    return MultiplyGrads(dx, dw)
+
+
+class Score(NamedTuple):
+    loss: object       # fp32 [1], None with a known lse
+    rows: object       # fp32, as labels: each row's loss, 0 without a label; None with a known lse
+    dz: object         # as z, or None
+    dw: object         # as w, or None
+    lse: object        # fp32, as labels: each row's log-sum-exp (any value without a label)
+
+
+def score(z, w, labels, *, upstream=None, grad=True, grads=(True, True), lse=None, into=None) -> Score:
+    """fasgd_score: softmax cross entropy of z w ([..., cols] x [cols, classes], w of z's type, rows
+    or columns contiguous) against labels (int64, one for each row of z; outside
+    [0, classes): none), the mean over the rows that have one, and (grad) the gradients
+    of z and w that `grads` names, times `upstream` (a device fp32 value) if given.
+    lse: what an earlier call with these z, w and labels gave: only gradients are
+    computed.  into: (dz, dw), where to write them (new tensors where None)."""
+    want = (bool(grad and grads[0]), bool(grad and grads[1]))
+    dz, dw = into if into is not None else (None, None)
+    _one_device(z, w, labels, upstream, lse, dz, dw)
+    a = _f.ScoreArgs()
+    a.z, a.rows, a.cols, a.ld_z = _rows(z)
+    a.dtype = _dtype(z)
+    a.w, (cols, a.classes), a.ld_w, _, a.w_flip = _matrices(w, 2)
+    _same_type(w, z)
+    if cols != a.cols:
+        raise ValueError("w is [z's columns, classes]")
+    if labels.dtype is not torch.int64 or not labels.is_contiguous() or labels.numel() != a.rows:
+        raise ValueError("labels must be contiguous int64 on the GPU, one for each row")
+    a.labels = labels.data_ptr() or _NOWHERE
+    if upstream is not None:
+        if upstream.dtype is not torch.float32 or upstream.numel() != 1:
+            raise ValueError("upstream must be one fp32 value on the GPU")
+        a.upstream = upstream.data_ptr()
+    given = dz, dw
+    if (dz is not None and not want[0]) or (dw is not None and not want[1]):
+        raise ValueError("a place for a gradient that is not wanted")
+    if want[0]:
+        if dz is None:
+            dz = _new(z)
+        _same_type(dz, z)
+        a.dz, rows, cols, a.ld_dz = _rows(dz)
+        if (rows, cols) != (a.rows, a.cols):
+            raise ValueError("z's gradient is as z")
+    if want[1]:
+        if dw is None:
+            dw = torch.empty_like(w)
+        _same_type(dw, w)
+        a.dw, shape, a.ld_dw, _, a.dw_flip = _matrices(dw, 2)
+        if shape != w.shape:
+            raise ValueError("w's gradient is as w")
+    loss = rows = None
+    if lse is None:
+        loss = torch.empty(1, dtype=torch.float32, device=z.device)
+        rows, lse = (torch.empty(labels.shape, dtype=torch.float32, device=z.device) for _ in range(2))
+        a.loss = loss.data_ptr()
+        a.row_loss = rows.data_ptr() or _NOWHERE
+    else:
+        if lse.dtype is not torch.float32 or lse.numel() != a.rows or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous fp32, one for each row")
+        a.known = 1
+    a.lse = lse.data_ptr() or _NOWHERE
+    space = _space(a, _f.fasgd_score_workspace, z)
+    _check(_f.fasgd_score(ctypes.addressof(a), _stream(z)))
+    del space
+    _written(*given)
+    return Score(loss, rows, dz, dw, lse)
+
+
 # ---------------------------------------------------------------------------
 # Inside torch's automatic differentiation
 # ---------------------------------------------------------------------------
@@ -373,7 +687,7 @@ class _Once(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("the join and the balance loss have no second derivatives here")
+        raise RuntimeError("the client operators but dropout, gather and an unweighted combine have no second derivatives here")
 
 
 def _once(grads, *of):
@@ -454,3 +768,89 @@ def balanced(logits, chosen, *, valid=None, **settings):
     balance, z, groups."""
     loss, parts, counts = _Balance.apply(logits, chosen, valid, settings)
     return loss, parts.detach(), counts
+
+
+class _Gather(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, offsets, order, place):
+        ctx.save_for_backward(offsets, order, place)
+        ctx.shape = x.shape
+        return gather(x, Route(offsets, order, place))
+
+    @staticmethod
+    def backward(ctx, d):
+        again = combined if torch.is_grad_enabled() else combine
+        return again(d.contiguous(), Route(*ctx.saved_tensors)).reshape(ctx.shape), None, None, None
+
+
+def gathered(x, route: Route):
+    """``gather``, differentiable in x, any number of times."""
+    return _Gather.apply(x, *route)
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, weight, offsets, order, place):
+        ctx.save_for_backward(None if weight is None else y, weight, offsets, order, place)
+        ctx.shape = y.shape
+        return combine(y, Route(offsets, order, place), weight)
+
+    @staticmethod
+    def backward(ctx, d):
+        y, weight, *route = ctx.saved_tensors
+        d = d.contiguous()
+        if weight is None:
+            again = gathered if torch.is_grad_enabled() else gather
+            return again(d, Route(*route)).reshape(ctx.shape), None, None, None, None
+        with torch.no_grad():
+            g = combine_grad(y, Route(*route), weight, d)
+        dy, dweight = _once((g.y.reshape(ctx.shape), g.weight), d, y, weight)
+        return dy, dweight, None, None, None
+
+
+def combined(y, route: Route, weight=None):
+    """``combine``, differentiable in y and weight; without weights any number of times, with
+    them a second derivative raises."""
+    return _Combine.apply(y, weight, *route)
+
+
+class _Multiply(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, offsets):
+        ctx.save_for_backward(x, w, offsets)
+        return multiply(x, w, offsets)
+
+    @staticmethod
+    def backward(ctx, d):
+        x, w, offsets = ctx.saved_tensors
+        with torch.no_grad():
+            g = multiply_grad(x, w, offsets, d.contiguous(), grads=ctx.needs_input_grad[:2])
+        return (*_once(g, d, x, w), None)
+
+
+def multiplied(x, w, offsets):
+    """``multiply``, differentiable in x and w (an fp32 w has an fp32 gradient); a second
+    derivative raises."""
+    return _Multiply.apply(x, w, offsets)
+
+
+class _Score(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, z, w, labels):
+        s = score(z, w, labels, grad=False)
+        ctx.save_for_backward(z, w, labels, s.lse)
+        ctx.mark_non_differentiable(s.rows)
+        return s.loss.reshape(()), s.rows
+
+    @staticmethod
+    def backward(ctx, d, _rows):
+        z, w, labels, lse = ctx.saved_tensors
+        with torch.no_grad():
+            s = score(z, w, labels, upstream=d.reshape(1), grads=ctx.needs_input_grad[:2], lse=lse)
+        return (*_once((s.dz, s.dw), d, z, w), None)
+
+
+def scored(z, w, labels):
+    """``score``, differentiable in z and w: (loss, each row's); only the first has a gradient,
+    and a second derivative of it raises."""
+    return _Score.apply(z, w, labels)

@@ -3,90 +3,11 @@
 // is allocated and nothing is kept between calls.
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 
+#include "checks.cuh"
 #include "client.cuh"
 
-namespace fasgd {
-void set_handleless_error(const char* msg);  // defined in runtime.cu
-}
-
 namespace {
-
-constexpr int64_t kRowsMax = (int64_t)1 << 40;
-
-int fail(int code, const char* fmt, ...) noexcept {
-    char buf[256];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    try {
-        fasgd::set_handleless_error(buf);
-    } catch (...) {       // out of memory for the text: the code says enough
-    }
-    return code;
-}
-int cuda_status(cudaError_t st, const char* call) {
-    return st == cudaSuccess ? FASGD_OK : fail(FASGD_ECUDA, "%s: %s", call, cudaGetErrorString(st));
-}
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-int64_t dtype_size(int32_t dtype) { return dtype == FASGD_F32 ? 4 : 2; }
-
-// An argument's memory: `rows` rows of `width` bytes, `step` bytes apart.
-struct Region {
-    const char* name;
-    const void* p;
-    int64_t rows, width, step;
-    bool output;
-};
-Region block(const char* name, const void* p, int64_t bytes, bool output) {
-    return {name, p, 1, bytes, bytes, output};
-}
-bool share(const Region& a, const Region& b) {
-    if (a.p == nullptr || b.p == nullptr || a.rows == 0 || b.rows == 0 || a.width == 0 || b.width == 0)
-        return false;
-    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
-    const uintptr_t ea = pa + (uintptr_t)((a.rows - 1) * a.step + a.width);
-    const uintptr_t eb = pb + (uintptr_t)((b.rows - 1) * b.step + b.width);
-    if (ea <= pb || eb <= pa) return false;
-    if (a.rows > 1 && b.rows > 1 && a.step == b.step) {   // columns of one wider matrix
-        const uintptr_t off = (pa < pb ? pb - pa : pa - pb) % (uintptr_t)a.step;
-        const int64_t first = pa < pb ? a.width : b.width, second = pa < pb ? b.width : a.width;
-        if ((int64_t)off >= first && (int64_t)off + second <= a.step) return false;
-    }
-    return true;
-}
-// EINVAL where an output shares memory with another argument.
-int check_shared(const char* call, const Region* r, int n) {
-    for (int i = 0; i < n; ++i)
-        for (int j = 0; j < i; ++j)
-            if ((r[i].output || r[j].output) && share(r[i], r[j]))
-                return fail(FASGD_EINVAL, "%s: %s and %s share memory", call, r[j].name, r[i].name);
-    return FASGD_OK;
-}
-
-int check_shape(const char* call, int64_t rows, int64_t cols, int64_t cols_max, int32_t dtype) {
-    if (rows < 0 || rows > kRowsMax || cols < 1 || cols > cols_max)
-        return fail(FASGD_EINVAL, "%s: rows must be in [0, 2^40], cols in [1, %lld]", call, (long long)cols_max);
-    if (dtype != FASGD_F32 && dtype != FASGD_BF16 && dtype != FASGD_F16)
-        return fail(FASGD_EINVAL, "%s: dtype %d is not an fasgd_dtype", call, dtype);
-    return FASGD_OK;
-}
-// A matrix argument: pointer, alignment of its type, row step.  ld is set to cols
-// where there is no second row to step to.
-int check_matrix(const char* call, const char* name, const void* p, int64_t& ld, int64_t rows, int64_t cols,
-                 int64_t size) {
-    if (p == nullptr) return fail(FASGD_EINVAL, "%s: %s is NULL", call, name);
-    if (!aligned(p, (uintptr_t)size)) return fail(FASGD_EINVAL, "%s: %s is not aligned to its type", call, name);
-    if (rows < 2) ld = cols;
-    if (ld < cols || ld > kRowsMax || (__int128)ld * rows * size > ((__int128)1 << 62))
-        return fail(FASGD_EINVAL, "%s: the rows of %s are %lld values apart, fewer than cols or too many", call,
-                    name, (long long)ld);
-    return FASGD_OK;
-}
 
 int fill_draws(const char* call, fasgd::DropArgs& d, double rate, uint64_t seed, int32_t client, uint64_t n,
                int64_t rows, int64_t cols) {
@@ -104,14 +25,6 @@ int fill_draws(const char* call, fasgd::DropArgs& d, double rate, uint64_t seed,
     d.scale = d.cut < 65536u ? 65536.0f / (float)(65536u - d.cut) : 0.0f;
     return FASGD_OK;
 }
-
-cudaError_t sm_count(int& sms) {
-    int dev = 0;
-    const cudaError_t st = cudaGetDevice(&dev);
-    return st != cudaSuccess ? st : cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-}
-
-int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
 // The checks that fasgd_join and fasgd_join_grad share, and the kernels' view.
 int fill_join(const char* call, const fasgd_join_args& u, fasgd::JoinArgs& a) {

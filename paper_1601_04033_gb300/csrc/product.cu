@@ -1,0 +1,224 @@
+// Matrix products in their simple form: 64 x 64 tiles of D in registers, 16 steps of k
+// through shared memory at a time, fp32 multiply-adds whatever the type.  Right for every
+// layout, alignment and size.
+
+#include <algorithm>
+
+#include "client.cuh"
+#include "product.cuh"
+
+namespace fasgd {
+namespace {
+
+constexpr int kM = 64, kN = kPlainN, kK = 16;
+
+template <class T>
+__device__ __forceinline__ float element(const Side& s, int64_t group, int64_t i, int64_t k) {
+    const T* p = static_cast<const T*>(s.p) + group * s.step;
+    return to_f32(s.across ? p[k * s.ld + i] : p[i * s.ld + k]);
+}
+// Elements [i0, i0 + 64) x [k0, k0 + 16) of a side, 0 beyond [.., i1) and [.., k1).
+template <class T>
+__device__ __forceinline__ void stage(float (&to)[kK][kM + 4], const Side& s, int64_t group, int64_t i0, int64_t i1,
+                                      int64_t k0, int64_t k1) {
+#pragma unroll
+    for (int r = 0; r < kM * kK / 256; ++r) {
+        const int j = threadIdx.x + r * 256;
+        const int i = s.across ? j % kM : j / kK, k = s.across ? j / kM : j % kK;
+        to[k][i] = i0 + i < i1 && k0 + k < k1 ? element<T>(s, group, i0 + i, k0 + k) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ void put(const Product& p, int64_t group, int64_t m, int64_t n, float v) {
+    const int64_t at = group * p.step_out + n * p.ld_out + m;
+    if (p.out_dtype == FASGD_F32) {
+        float* out = static_cast<float*>(p.out) + at;
+        *out = p.add ? *out + v : v;
+    } else if (p.out_dtype == FASGD_BF16) {
+        static_cast<__nv_bfloat16*>(p.out)[at] = from_f32<__nv_bfloat16>(v);
+    } else {
+        static_cast<__half*>(p.out)[at] = from_f32<__half>(v);
+    }
+}
+
+// The group and first n of the block's tile; false: there is no such tile.
+__device__ bool find_tile(const Product& p, int64_t tile, int64_t& group, Bounds& rows) {
+    const int lane = threadIdx.x & 31;
+    int64_t before = 0;
+    for (int g0 = 0; g0 < p.groups; g0 += 32) {
+        Bounds b = {0, 0};
+        if (g0 + lane < p.groups) b = group_bounds(p.offsets, g0 + lane, p.n);
+        const int64_t tiles = (b.hi - b.lo + kN - 1) / kN;
+        int64_t s = tiles;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t o = __shfl_up_sync(0xffffffffu, s, d);
+            if (lane >= d) s += o;
+        }
+        const uint32_t has = __ballot_sync(0xffffffffu, tile < before + s);
+        if (has != 0) {
+            const int first = __ffs(has) - 1;
+            const int64_t begin = before + __shfl_sync(0xffffffffu, s - tiles, first);
+            group = g0 + first;
+            rows = {__shfl_sync(0xffffffffu, b.lo, first) + (tile - begin) * kN, __shfl_sync(0xffffffffu, b.hi, first)};
+            return true;
+        }
+        before += __shfl_sync(0xffffffffu, s, 31);
+    }
+    return false;
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) plain_kernel(Product p) {
+    __shared__ float as[kK][kM + 4], bs[kK][kN + 4];
+    const uint32_t across = (uint32_t)((p.m + kM - 1) / kM), tile = blockIdx.x / across, tiles = gridDim.x / across;
+    const int64_t m0 = (int64_t)(blockIdx.x % across) * kM;
+    int64_t group = blockIdx.z, n0 = (int64_t)tile * kN, n1 = p.n, k0 = 0, k1 = p.k;
+    if (p.ragged == kRaggedN) {
+        // Rows of no group, spread over the blocks; then the block's own tile.
+        const int64_t lo = group_bounds(p.offsets, 0, p.n).lo, hi = group_bounds(p.offsets, p.groups - 1, p.n).hi;
+        for (int64_t r = tile; r < p.n - (hi - lo); r += tiles)
+            for (int64_t m = m0 + threadIdx.x; m < min(m0 + kM, p.m); m += blockDim.x)
+                put(p, 0, m, r < lo ? r : hi + (r - lo), 0.0f);
+        Bounds rows;
+        if (!find_tile(p, tile, group, rows)) return;
+        n0 = rows.lo;
+        n1 = rows.hi;
+    } else if (p.ragged == kRaggedK) {
+        const Bounds b = group_bounds(p.offsets, (int)group, p.k);
+        k0 = b.lo;
+        k1 = b.hi;
+    }
+    const int64_t ga = p.ragged == kRaggedN ? group : 0;
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    float d[4][4] = {};      // [m: tx + 16 i][n: ty * 4 + j]
+    for (int64_t k = k0; k < k1; k += kK) {
+        stage<T>(as, p.a, ga, m0, p.m, k, k1);
+        stage<T>(bs, p.b, 0, n0, n1, k, k1);
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < kK; ++s) {
+            float av[4], bv[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) av[i] = as[s][tx + 16 * i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) bv[j] = bs[s][ty * 4 + j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[i][j] = fmaf(av[i], bv[j], d[i][j]);
+        }
+        __syncthreads();
+    }
+    const int64_t go = p.ragged == kRaggedK ? group : 0;
+    if (p.ending == kStore) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t n = n0 + ty * 4 + j;
+            if (n >= n1) continue;
+            float scale = p.factor;
+            bool zero = false;
+            if (p.scale != nullptr) {
+                const float s = p.scale[p.by_n ? n : 0];
+                zero = p.by_n && s == 0.0f;
+                scale *= s;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t m = m0 + tx + 16 * i;
+                if (m < p.m) put(p, go, m, n, zero ? 0.0f : d[i][j] * scale);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t m = m0 + tx + 16 * i;
+        const int64_t label = m < p.m ? p.labels[m] : -1;
+        const bool has = label >= 0 && label < p.classes;
+        if (p.ending == kResidual) {
+            const float lse = m < p.m ? p.lse[m] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t n = n0 + ty * 4 + j;
+                if (m < p.m && n < n1)
+                    put(p, 0, m, n, has ? p.factor * (p.n0 + n == label ? expm1f(d[i][j] - lse) : expf(d[i][j] - lse)) : 0.0f);
+            }
+            continue;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t n = n0 + ty * 4 + j;
+            if (n < n1) top = fmaxf(top, d[i][j]);
+            if (n < n1 && has && p.n0 + n == label) p.at_label[m] = d[i][j];
+        }
+        as[ty][tx + 16 * i] = top;
+        __syncthreads();
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, as[r][tx + 16 * i]);
+        __syncthreads();
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (n0 + ty * 4 + j < n1) sum += d[i][j] == top ? 1.0f : expf(d[i][j] - top);
+        as[ty][tx + 16 * i] = sum;
+        __syncthreads();
+        if (ty == 0 && m < p.m) {
+            sum = 0.0f;
+            for (int r = 0; r < 16; ++r) sum += as[r][tx + 16 * i];
+            p.parts[(p.n0 / kN + tile) * p.m + m] = make_float2(top, sum);
+        }
+        __syncthreads();
+    }
+}
+
+template <class F, class T>
+__global__ void __launch_bounds__(256) pack_kernel(Pack p) {
+    const int64_t g = blockIdx.z;
+    if (p.offsets != nullptr && p.offsets[g + 1] <= p.offsets[g]) return;
+    for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+        const int64_t label = p.labels != nullptr ? p.labels[r] : 0;
+        const bool has = p.labels == nullptr || (label >= 0 && label < p.classes);
+        const F* from = static_cast<const F*>(p.from) + g * p.step_from + r * p.ld_from;
+        T* to = static_cast<T*>(p.to) + g * p.step_to + r * p.ld_to;
+        for (int64_t c = blockIdx.y * 256 + threadIdx.x; c < p.cols; c += gridDim.y * 256)
+            to[c] = has ? from_f32<T>(to_f32(from[c])) : from_f32<T>(0.0f);
+    }
+}
+template <class F>
+cudaError_t pack(const Pack& p, dim3 grid, cudaStream_t stream) {
+    switch (p.dtype_to) {
+        case FASGD_F32: pack_kernel<F, float><<<grid, 256, 0, stream>>>(p); break;
+        case FASGD_BF16: pack_kernel<F, __nv_bfloat16><<<grid, 256, 0, stream>>>(p); break;
+        default: pack_kernel<F, __half><<<grid, 256, 0, stream>>>(p);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_pack(const Pack& p, cudaStream_t stream) {
+    if (p.rows == 0) return cudaSuccess;
+    const dim3 grid((unsigned)std::min<int64_t>(p.rows, 1 << 20), (unsigned)std::min<int64_t>((p.cols + 255) / 256, 16),
+                    p.groups);
+    switch (p.dtype_from) {
+        case FASGD_F32: return pack<float>(p, grid, stream);
+        case FASGD_BF16: return pack<__nv_bfloat16>(p, grid, stream);
+        default: return pack<__half>(p, grid, stream);
+    }
+}
+
+cudaError_t launch_plain(const Product& p, cudaStream_t stream) {
+    const int64_t tiles = ((p.n + kN - 1) / kN + (p.ragged == kRaggedN ? p.groups : 0)) * ((p.m + kM - 1) / kM);
+    if (tiles == 0) return cudaSuccess;
+    if (tiles >= (int64_t)1 << 31) return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)tiles, 1, p.ragged == kRaggedK ? p.groups : 1);
+    switch (p.dtype) {
+        case FASGD_F32: plain_kernel<float><<<grid, 256, 0, stream>>>(p); break;
+        case FASGD_BF16: plain_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(p); break;
+        default: plain_kernel<__half><<<grid, 256, 0, stream>>>(p);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace fasgd

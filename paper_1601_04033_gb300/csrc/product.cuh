@@ -1,0 +1,92 @@
+// Matrix products of the client operators (experts.cu and score.cu lay them out;
+// product.cu and tile.cu hold the kernels).
+//
+//   D[m, n] = sum_k A[m, k] B[n, k]
+//
+// m is the index that is consecutive where the result is stored, so that the lanes of a
+// warp, which hold consecutive m, write consecutive memory whatever the product.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace fasgd {
+
+// One side of a product.  Element (i, k): i * ld + k, or (across) k * ld + i; group g of
+// several is step values further on.
+struct Side {
+    const void* p;
+    int64_t ld, step;
+    int32_t across;
+};
+
+enum Ragged {
+    kNotRagged,
+    kRaggedN,    // n counts rows of all groups: group g has offsets[g] <= n < offsets[g + 1], B and D go by them, A by groups
+    kRaggedK,    // so does k: A and B go by rows, D by groups
+};
+enum Ending {
+    kStore,      // D, times scale where there is one, into out
+    kStatistics, // of the values s = D over n: each tile's maximum and sum of exp(s - maximum), and s[m, label m]
+    kResidual,   // exp(s - lse m) - [n = label m], 0 where m has no label, times `factor`, into out
+};
+
+struct Product {
+    Side a, b;
+    int64_t m, n, k;
+    int32_t groups;              // ragged products
+    const int32_t* offsets;      // int32[groups + 1] on the device
+    int32_t ragged;              // enum Ragged
+    int32_t dtype;               // of A and B (enum fasgd_dtype)
+    int32_t ending;              // enum Ending
+    // kStore, kResidual: element (m, n) of group g is out[g * step_out + n * ld_out + m]
+    void* out;
+    int64_t ld_out, step_out;
+    int64_t step_split;          // from one part of k's result to the next one's (launch_tiles)
+    int32_t out_dtype;
+    int32_t add;                 // kStore, fp32: out += instead
+    const float* scale;          // kStore: one value, or (by_n) one for each n, whose 0 makes its values 0
+    int32_t by_n;
+    float factor;                // kStore, kResidual: a power of two, on top
+    // kStatistics, kResidual
+    const int64_t* labels;       // [m]
+    float2* parts;               // [n tiles][m]: kStatistics
+    float* at_label;             // [m]: kStatistics
+    const float* lse;            // [m]: kResidual
+    int64_t n0, classes;         // the first n of this piece, and how many there are of all pieces
+};
+
+// Any layout, type and size, fp32 arithmetic on the ordinary cores.  kPlainN: the n of a tile.
+constexpr int kPlainN = 64;
+cudaError_t launch_plain(const Product& p, cudaStream_t stream);
+
+// 16-bit types on the tensor cores, for sides that start and step on 16 bytes.  kTileN: the n of a tile.
+constexpr int kTileN = 256;
+bool tile_side(const Side& s, int64_t groups);
+cudaError_t launch_tiles(const Product& p, cudaStream_t stream);
+
+// A copy of a side with rows that lie as the fast kernels want them: `rows` rows of `cols`
+// values (of group g: p + g * step) to rows ld_to apart, cast to dtype_to.  What it leaves
+// out is not read: groups without rows by offsets (null: none is left out), and rows
+// without a label (labels null: none; its copy is 0).
+struct Pack {
+    const void* from;
+    void* to;
+    int64_t rows, cols, ld_from, step_from, ld_to, step_to;
+    int32_t groups, dtype_from, dtype_to;
+    const int32_t* offsets;
+    const int64_t* labels;
+    int64_t classes;
+};
+cudaError_t launch_pack(const Pack& p, cudaStream_t stream);
+
+// Group g's rows, cut to [0, n).
+struct Bounds {
+    int64_t lo, hi;
+};
+__device__ __forceinline__ Bounds group_bounds(const int32_t* offsets, int g, int64_t n) {
+    const int64_t lo = min(max((int64_t)offsets[g], (int64_t)0), n);
+    return {lo, min(max((int64_t)offsets[g + 1], lo), n)};
+}
+
+}  // namespace fasgd

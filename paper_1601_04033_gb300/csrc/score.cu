@@ -1,0 +1,335 @@
+// fasgd_score: softmax cross entropy of rows against classes from the last product on.
+//
+// s = z w is formed twice and never kept.  The first time its tiles leave, for each row,
+// their maximum m_j and sum_v exp(s - m_j); these give lse = M + log sum_j exp(m_j - M)
+// sum_j.  The second time, a piece of the classes after the other, the tiles leave
+// g = exp(s - lse) - [v = label], from which the piece's part of dz = g w^T and its rows of
+// dw = z^T g follow.  A piece of g lies by classes ([v][row]), which makes it an operand of
+// both products as it stands.  Keeping s in place of forming it again would cost 4 bytes
+// a value written and read, and rounding it to 2 would show in dz and dw.
+//
+// g is held without upstream / N, so that its values are in [-1, 1] and no fp16 value is
+// lost for N's size; for fp16 it is held times 2^14, so that probabilities down to 2^-28
+// keep all their bits.  The products' results are multiplied by upstream / N, in fp32.
+// Rows without a label are copied as zeros before the products that sum over rows.
+
+#include <algorithm>
+
+#include "checks.cuh"
+#include "client.cuh"
+#include "product.cuh"
+
+namespace {
+
+using fasgd::Product;
+
+struct Score {
+    fasgd_score_args u;
+    int64_t size, tile;
+    bool grad;
+    // workspace
+    void* z_copy;                // rows x ld_zc, rows without a label as zeros
+    int64_t ld_zc;
+    float2* parts;               // [tiles][rows]
+    float *at_label, *lse;       // [rows]
+    float* row_scale;            // [rows] upstream / N, 0 without a label
+    float* share;                // [1] upstream / N
+    void* g;                     // [piece][ld_g]
+    int64_t ld_g, piece;
+    float* dz_sum;               // [rows][cols] (several pieces)
+};
+
+// lse and the row's loss from the tiles' parts: 32 rows a block, 8 threads each.
+__global__ void __launch_bounds__(256) lse_kernel(const float2* parts, int64_t tiles, int64_t rows, const int64_t* labels,
+                                                  int64_t classes, const float* at_label, float* lse, float* row_loss) {
+    __shared__ float2 shared[8][32];
+    const int x = threadIdx.x % 32, y = threadIdx.x / 32;
+    const int64_t r = (int64_t)blockIdx.x * 32 + x;
+    float top = -INFINITY, sum = 0.0f;
+    const auto join = [&](float2 p) {
+        const float most = fmaxf(top, p.x);
+        sum = (top == most ? sum : sum * expf(top - most)) + (p.x == most ? p.y : p.y * expf(p.x - most));
+        top = most;
+    };
+    if (r < rows)
+        for (int64_t j = y; j < tiles; j += 8) join(parts[j * rows + r]);
+    shared[y][x] = make_float2(top, sum);
+    __syncthreads();
+    if (y == 0 && r < rows) {
+        for (int i = 1; i < 8; ++i) join(shared[i][x]);
+        const float log_sum = logf(sum);
+        const int64_t label = labels[r];
+        lse[r] = top + log_sum;
+        row_loss[r] = label >= 0 && label < classes ? (top - at_label[r]) + log_sum : 0.0f;
+    }
+}
+
+// The loss, upstream / N, and what each row's gradient is multiplied by: one block.
+__global__ void __launch_bounds__(1024) loss_kernel(int64_t rows, const int64_t* labels, int64_t classes,
+                                                    const float* row_loss, const float* upstream, float* loss,
+                                                    float* share, float* row_scale) {
+    __shared__ float sums[32];
+    __shared__ int64_t counts[32];
+    const auto has = [&](int64_t r) { return labels[r] >= 0 && labels[r] < classes; };
+    float sum = 0.0f;
+    int64_t count = 0;
+    for (int64_t r = threadIdx.x; r < rows; r += 1024)
+        if (has(r)) {
+            if (row_loss != nullptr) sum += row_loss[r];
+            ++count;
+        }
+    sum = fasgd::warp_sum(sum);
+    for (int d = 16; d > 0; d >>= 1) count += __shfl_xor_sync(0xffffffffu, count, d);
+    if (threadIdx.x % 32 == 0) {
+        sums[threadIdx.x / 32] = sum;
+        counts[threadIdx.x / 32] = count;
+    }
+    __syncthreads();
+    sum = 0.0f;
+    count = 0;
+    for (int w = 0; w < 32; ++w) {
+        sum += sums[w];
+        count += counts[w];
+    }
+    const float up = count == 0 ? 0.0f : (upstream != nullptr ? *upstream : 1.0f) / (float)count;
+    if (threadIdx.x == 0) {
+        if (loss != nullptr) *loss = count == 0 ? 0.0f : sum / (float)count;
+        if (share != nullptr) *share = up;
+    }
+    if (row_scale != nullptr)
+        for (int64_t r = threadIdx.x; r < rows; r += 1024) row_scale[r] = has(r) ? up : 0.0f;
+}
+
+// dz from its sums over the pieces.
+template <class T>
+__global__ void __launch_bounds__(256) fold_kernel(const float* sum, const float* row_scale, int64_t rows, int64_t cols,
+                                                   T* dz, int64_t ld, float factor) {
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const float s = row_scale[r];
+        for (int64_t c = threadIdx.x; c < cols; c += 256)
+            dz[r * ld + c] = fasgd::from_f32<T>(s == 0.0f ? 0.0f : sum[r * cols + c] * (s * factor));
+    }
+}
+cudaError_t fold(const Score& s, float factor, cudaStream_t stream) {
+    const unsigned blocks = (unsigned)std::min<int64_t>(s.u.rows, 1 << 20);
+    const auto go = [&](auto* dz) {
+        fold_kernel<<<blocks, 256, 0, stream>>>(s.dz_sum, s.row_scale, s.u.rows, s.u.cols, dz, s.u.ld_dz, factor);
+        return cudaGetLastError();
+    };
+    switch (s.u.dtype) {
+        case FASGD_F32: return go(static_cast<float*>(s.u.dz));
+        case FASGD_BF16: return go(static_cast<__nv_bfloat16*>(s.u.dz));
+        default: return go(static_cast<__half*>(s.u.dz));
+    }
+}
+
+int fill_score(const char* call, const fasgd_score_args& given, Score& s) {
+    s = Score();
+    s.u = given;
+    fasgd_score_args& u = s.u;
+    if (int rc = check_shape(call, u.rows, u.cols, FASGD_COLS_MAX, u.dtype)) return rc;
+    if (u.rows >= (int64_t)1 << 31 || u.classes < 1 || u.classes > FASGD_CLASSES_MAX)
+        return fail(FASGD_EINVAL, "%s: rows must be below 2^31, classes in [1, 2^24]", call);
+    if ((u.w_flip | u.dw_flip) & ~1) return fail(FASGD_EINVAL, "%s: w_flip and dw_flip are 0 or 1", call);
+    s.size = dtype_size(u.dtype);
+    s.grad = u.dz != nullptr || u.dw != nullptr;
+    if (int rc = check_matrix(call, "z", u.z, u.ld_z, u.rows, u.cols, s.size)) return rc;
+    const auto shape = [&](bool flip) { return flip ? u.classes : u.cols; };
+    const auto width = [&](bool flip) { return flip ? u.cols : u.classes; };
+    if (int rc = check_matrix(call, "w", u.w, u.ld_w, shape(u.w_flip), width(u.w_flip), s.size)) return rc;
+    if (u.dz != nullptr)
+        if (int rc = check_matrix(call, "dz", u.dz, u.ld_dz, u.rows, u.cols, s.size)) return rc;
+    if (u.dw != nullptr)
+        if (int rc = check_matrix(call, "dw", u.dw, u.ld_dw, shape(u.dw_flip), width(u.dw_flip), s.size)) return rc;
+    if (u.labels == nullptr || !aligned(u.labels, 8))
+        return fail(FASGD_EINVAL, "%s: labels must not be NULL, and 8-byte aligned", call);
+    if (u.known & ~1) return fail(FASGD_EINVAL, "%s: known is 0 or 1", call);
+    if (u.known ? u.lse == nullptr || !s.grad : u.loss == nullptr || u.row_loss == nullptr)
+        return fail(FASGD_EINVAL, "%s: loss and row_loss must not be NULL, or with a known lse: that, and dz or dw", call);
+    if (u.known) u.loss = u.row_loss = nullptr;
+    if (!aligned(u.loss, 4) || !aligned(u.row_loss, 4) || !aligned(u.lse, 4) || !aligned(u.upstream, 4))
+        return fail(FASGD_EINVAL, "%s: loss, row_loss, lse and upstream must be 4-byte aligned", call);
+    return FASGD_OK;
+}
+
+int64_t lay_out(Score& s, char* base) {
+    const fasgd_score_args& u = s.u;
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        char* p = base + at;
+        at += (bytes + 255) / 256 * 256;
+        return p;
+    };
+    s.tile = fasgd::kPlainN;
+    const int64_t tiles = (u.classes + s.tile - 1) / s.tile;
+    if (!u.known) {
+        s.parts = reinterpret_cast<float2*>(take(8 * tiles * u.rows));
+        s.at_label = reinterpret_cast<float*>(take(4 * u.rows));
+    }
+    s.lse = u.lse != nullptr ? u.lse : reinterpret_cast<float*>(take(4 * u.rows));
+    if (!s.grad) return at;
+    s.share = reinterpret_cast<float*>(take(4));
+    s.row_scale = reinterpret_cast<float*>(take(4 * u.rows));
+    s.ld_zc = (u.cols + 7) / 8 * 8;
+    s.z_copy = take(u.rows * s.ld_zc * s.size);
+    s.ld_g = (u.rows + 7) / 8 * 8;
+    const int64_t most = std::max<int64_t>(64, FASGD_SCORE_PIECE / std::max<int64_t>(1, s.ld_g * s.size));
+    const int64_t pieces = (u.classes + most - 1) / most;
+    s.piece = (u.classes + pieces - 1) / pieces;
+    if (pieces > 1) s.piece = std::min(s.piece / 64 * 64 + 64, most / 64 * 64);
+    s.g = take(s.piece * s.ld_g * s.size);
+    if (u.dz != nullptr && s.piece < u.classes) s.dz_sum = reinterpret_cast<float*>(take(4 * u.rows * u.cols));
+    return at;
+}
+
+// The piece's part of an operand or result by classes.
+const void* at_class(const void* p, int64_t ld, bool flip, int64_t v, int64_t size) {
+    return static_cast<const char*>(p) + (flip ? v * ld : v) * size;
+}
+
+cudaError_t run(const Score& s, cudaStream_t stream) {
+    const fasgd_score_args& u = s.u;
+    cudaError_t st = cudaSuccess;
+    const bool has_z = s.grad;
+    const void* z = has_z ? s.z_copy : u.z;
+    const int64_t ld_z = has_z ? s.ld_zc : u.ld_z;
+    if (has_z) {
+        fasgd::Pack p = {};
+        p.from = u.z;
+        p.to = s.z_copy;
+        p.rows = u.rows;
+        p.cols = u.cols;
+        p.ld_from = u.ld_z;
+        p.ld_to = s.ld_zc;
+        p.groups = 1;
+        p.dtype_from = p.dtype_to = u.dtype;
+        p.labels = u.labels;
+        p.classes = u.classes;
+        st = fasgd::launch_pack(p, stream);
+        if (st != cudaSuccess) return st;
+    }
+    Product p = {};
+    p.a = {z, ld_z, 0, 0};
+    p.b = {u.w, u.ld_w, 0, !u.w_flip};
+    p.m = u.rows;
+    p.n = u.classes;
+    p.k = u.cols;
+    p.dtype = u.dtype;
+    p.ending = fasgd::kStatistics;
+    p.labels = u.labels;
+    p.classes = u.classes;
+    p.parts = s.parts;
+    p.at_label = s.at_label;
+    p.lse = s.lse;
+    if (!u.known && u.rows > 0) {
+        st = fasgd::launch_plain(p, stream);
+        if (st != cudaSuccess) return st;
+        lse_kernel<<<(unsigned)((u.rows + 31) / 32), 256, 0, stream>>>(
+            s.parts, (u.classes + s.tile - 1) / s.tile, u.rows, u.labels, u.classes, s.at_label, s.lse, u.row_loss);
+        if ((st = cudaGetLastError()) != cudaSuccess) return st;
+    }
+    loss_kernel<<<1, 1024, 0, stream>>>(u.rows, u.labels, u.classes, u.row_loss, u.upstream, u.loss, s.share, s.row_scale);
+    if ((st = cudaGetLastError()) != cudaSuccess || !s.grad) return st;
+
+    const float factor = u.dtype == FASGD_F16 ? 16384.0f : 1.0f;
+    for (int64_t v = 0; v < u.classes; v += s.piece) {
+        const int64_t n = std::min(s.piece, u.classes - v);
+        const void* w = at_class(u.w, u.ld_w, u.w_flip, v, s.size);
+        p.b.p = w;
+        p.n = n;
+        p.n0 = v;
+        p.ending = fasgd::kResidual;
+        p.out = s.g;
+        p.ld_out = s.ld_g;
+        p.out_dtype = u.dtype;
+        p.factor = factor;
+        st = fasgd::launch_plain(p, stream);
+        if (st != cudaSuccess) return st;
+        Product q = {};
+        q.dtype = u.dtype;
+        q.ending = fasgd::kStore;
+        q.factor = 1.0f / factor;
+        if (u.dz != nullptr && u.rows > 0) {
+            q.a = {w, u.ld_w, 0, u.w_flip};
+            q.b = {s.g, s.ld_g, 0, 1};
+            q.m = u.cols;
+            q.n = u.rows;
+            q.k = n;
+            if (s.dz_sum != nullptr) {
+                q.out = s.dz_sum;
+                q.ld_out = u.cols;
+                q.out_dtype = FASGD_F32;
+                q.add = v > 0;
+                q.factor = 1.0f;
+            } else {
+                q.out = u.dz;
+                q.ld_out = u.ld_dz;
+                q.out_dtype = u.dtype;
+                q.scale = s.row_scale;
+                q.by_n = 1;
+            }
+            st = fasgd::launch_plain(q, stream);
+            if (st != cudaSuccess) return st;
+        }
+        if (u.dw != nullptr) {
+            const fasgd::Side zs = {s.z_copy, s.ld_zc, 0, 1}, gs = {s.g, s.ld_g, 0, 0};
+            q.a = u.dw_flip ? zs : gs;
+            q.b = u.dw_flip ? gs : zs;
+            q.m = u.dw_flip ? u.cols : n;
+            q.n = u.dw_flip ? n : u.cols;
+            q.k = u.rows;
+            q.out = const_cast<void*>(at_class(u.dw, u.ld_dw, u.dw_flip, v, s.size));
+            q.ld_out = u.ld_dw;
+            q.out_dtype = u.dtype;
+            q.add = 0;
+            q.scale = s.share;
+            q.by_n = 0;
+            q.factor = 1.0f / factor;
+            st = fasgd::launch_plain(q, stream);
+            if (st != cudaSuccess) return st;
+        }
+    }
+    return s.dz_sum != nullptr && u.rows > 0 ? fold(s, 1.0f / factor, stream) : st;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t fasgd_score_workspace(const fasgd_score_args* u) {
+    const char* call = "fasgd_score_workspace";
+    if (u == nullptr) {
+        fail(FASGD_EINVAL, "%s: no arguments", call);
+        return -1;
+    }
+    Score s;
+    if (fill_score(call, *u, s) != FASGD_OK) return -1;
+    return lay_out(s, nullptr);
+}
+
+int fasgd_score(const fasgd_score_args* u, void* stream) {
+    const char* call = "fasgd_score";
+    if (u == nullptr) return fail(FASGD_EINVAL, "%s: no arguments", call);
+    Score s;
+    if (int rc = fill_score(call, *u, s)) return rc;
+    const int64_t need = lay_out(s, static_cast<char*>(u->workspace));
+    if (need > 0 && (u->workspace == nullptr || !aligned(u->workspace, 256) || u->workspace_bytes < need))
+        return fail(FASGD_EINVAL, "%s: workspace must be 256-byte aligned and hold %lld bytes", call, (long long)need);
+    const auto classes = [&](const char* name, const void* p, bool flip, int64_t ld, bool output) {
+        return Region{name, p, flip ? u->classes : u->cols, (flip ? u->cols : u->classes) * s.size, ld * s.size, output};
+    };
+    const Region r[] = {{"z", u->z, u->rows, u->cols * s.size, s.u.ld_z * s.size, false},
+                        classes("w", u->w, u->w_flip, s.u.ld_w, false),
+                        block("labels", u->labels, 8 * u->rows, false),
+                        block("upstream", u->upstream, 4, false),
+                        block("loss", s.u.loss, 4, true),
+                        block("row_loss", s.u.row_loss, 4 * u->rows, true),
+                        block("lse", u->lse, 4 * u->rows, !u->known),
+                        {"dz", u->dz, u->rows, u->cols * s.size, s.u.ld_dz * s.size, true},
+                        classes("dw", u->dw, u->dw_flip, s.u.ld_dw, true),
+                        block("workspace", u->workspace, u->workspace_bytes, true)};
+    if (int rc = check_shared(call, r, sizeof r / sizeof r[0])) return rc;
+    return cuda_status(run(s, static_cast<cudaStream_t>(stream)), call);
+}
+
+}  // extern "C"

@@ -73,12 +73,23 @@ SIGNATURES = {
     "fasgd_join_workspace": (_i64, [_p]),
     "fasgd_balance": (_i32, [_p, _p]),
     "fasgd_balance_workspace": (_i64, [_p]),
+    "fasgd_route": (_i32, [_p, _p]),
+    "fasgd_route_workspace": (_i64, [_p]),
+    "fasgd_gather": (_i32, [_p, _p]),
+    "fasgd_combine": (_i32, [_p, _p]),
+    "fasgd_combine_grad": (_i32, [_p, _p]),
+    "fasgd_multiply": (_i32, [_p, _p]),
+    "fasgd_multiply_grad": (_i32, [_p, _p]),
+    "fasgd_multiply_workspace": (_i64, [_p]),
+    "fasgd_score": (_i32, [_p, _p]),
+    "fasgd_score_workspace": (_i64, [_p]),
     "fasgd_last_error": (ctypes.c_char_p, [_p]),
 }
 
 F32, BF16, F16 = 0, 1, 2
 RMS_NORM, LAYER_NORM = 0, 1
 COLS_MAX, EXPERTS_MAX = 1 << 20, 1024
+CLASSES_MAX, SCORE_PIECE = 1 << 24, 1 << 29
 
 
 def _struct(name, fields):
@@ -99,6 +110,16 @@ JoinArgs = _struct("JoinArgs", "rows:i64 cols:i64 groups:i64 x:p ld_x:i64 y:p ld
 BalanceArgs = _struct("BalanceArgs", "rows:i64 cols:i64 groups:i64 top:i64 logits:p ld_logits:i64 chosen:p "
                       "valid:p upstream:p dlogits:p ld_dlogits:i64 counts:p loss:p workspace:p "
                       "workspace_bytes:i64 balance_scale:f32 z_scale:f32 dtype:i32 reserved:i32")
+RouteArgs = _struct("RouteArgs", "rows:i64 top:i64 experts:i64 chosen:p offsets:p order:p place:p workspace:p "
+                    "workspace_bytes:i64")
+ExchangeArgs = _struct("ExchangeArgs", "rows:i64 top:i64 cols:i64 row_values:p ld_rows:i64 places:p ld_places:i64 "
+                       "order:p place:p weight:p dplaces:p ld_dplaces:i64 dweight:p dtype:i32 reserved:i32")
+MultiplyArgs = _struct("MultiplyArgs", "rows:i64 inputs:i64 outputs:i64 experts:i64 offsets:p x:p ld_x:i64 w:p "
+                       "ld_w:i64 step_w:i64 y:p ld_y:i64 dy:p ld_dy:i64 dx:p ld_dx:i64 dw:p ld_dw:i64 step_dw:i64 "
+                       "workspace:p workspace_bytes:i64 dtype:i32 w_dtype:i32 w_flip:i32 dw_flip:i32")
+ScoreArgs = _struct("ScoreArgs", "rows:i64 cols:i64 classes:i64 z:p ld_z:i64 w:p ld_w:i64 labels:p upstream:p loss:p "
+                    "row_loss:p lse:p dz:p ld_dz:i64 dw:p ld_dw:i64 workspace:p workspace_bytes:i64 dtype:i32 "
+                    "w_flip:i32 dw_flip:i32 known:i32")
 
 NOALLOC_PMAX = 1 << 24
 BFASGD_TMAX = 4096
@@ -304,6 +325,46 @@ def fasgd_balance(a, stream):
 
 def fasgd_balance_workspace(a):
     return LIB.fasgd_balance_workspace(a)
+
+
+def fasgd_route(a, stream):
+    return LIB.fasgd_route(a, stream)
+
+
+def fasgd_route_workspace(a):
+    return LIB.fasgd_route_workspace(a)
+
+
+def fasgd_gather(a, stream):
+    return LIB.fasgd_gather(a, stream)
+
+
+def fasgd_combine(a, stream):
+    return LIB.fasgd_combine(a, stream)
+
+
+def fasgd_combine_grad(a, stream):
+    return LIB.fasgd_combine_grad(a, stream)
+
+
+def fasgd_multiply(a, stream):
+    return LIB.fasgd_multiply(a, stream)
+
+
+def fasgd_multiply_grad(a, stream):
+    return LIB.fasgd_multiply_grad(a, stream)
+
+
+def fasgd_multiply_workspace(a):
+    return LIB.fasgd_multiply_workspace(a)
+
+
+def fasgd_score(a, stream):
+    return LIB.fasgd_score(a, stream)
+
+
+def fasgd_score_workspace(a):
+    return LIB.fasgd_score_workspace(a)
 
 
 def fasgd_last_error(h) -> str:
