@@ -89,9 +89,12 @@ struct Multiply {
     fasgd_multiply_args u;      // with ld and step set where they are not looked at
     bool grad;                  // checked for the gradients
     int64_t size, w_size;
-    // The copies in the workspace (null: the argument itself serves).
-    void *w_copy;
-    int64_t w_ld, w_step;       // of what the products read as w
+    // Copies in the workspace (null: the argument itself serves), and the steps of what is read.
+    void *w_copy, *x_copy, *dy_copy;
+    int64_t w_ld, w_step, x_ld, dy_ld;
+    const void* w() const { return w_copy != nullptr ? w_copy : u.w; }
+    const void* x() const { return x_copy != nullptr ? x_copy : u.x; }
+    const void* dy() const { return dy_copy != nullptr ? dy_copy : u.dy; }
 };
 
 int fill_multiply(const char* call, const fasgd_multiply_args& given, bool grad, Multiply& m) {
@@ -139,12 +142,27 @@ int64_t lay_out(Multiply& m, char* base) {
     };
     m.w_ld = u.ld_w;
     m.w_step = u.step_w;
-    m.w_copy = nullptr;
-    if ((!m.grad || u.dx != nullptr) && u.w_dtype != u.dtype) {
+    m.x_ld = u.ld_x;
+    m.dy_ld = u.ld_dy;
+    m.w_copy = m.x_copy = m.dy_copy = nullptr;
+    // The tensor cores' operands start and step on 16 bytes.
+    const bool tiles = u.dtype != FASGD_F32;
+    const auto fits = [&](const void* p, int64_t ld, int64_t step, int64_t groups) {
+        return !tiles || fasgd::tile_side({p, ld, step, 0}, groups);
+    };
+    if ((!m.grad || u.dx != nullptr) && (u.w_dtype != u.dtype || !fits(u.w, u.ld_w, u.step_w, u.experts))) {
         const int64_t rows = u.w_flip ? u.outputs : u.inputs, cols = u.w_flip ? u.inputs : u.outputs;
         m.w_ld = (cols + 7) / 8 * 8;
         m.w_step = rows * m.w_ld;
         m.w_copy = take(u.experts * m.w_step * m.size);
+    }
+    if ((!m.grad || u.dw != nullptr) && !fits(u.x, u.ld_x, 0, 1)) {
+        m.x_ld = (u.inputs + 7) / 8 * 8;
+        m.x_copy = take(u.rows * m.x_ld * m.size);
+    }
+    if (m.grad && !fits(u.dy, u.ld_dy, 0, 1)) {
+        m.dy_ld = (u.outputs + 7) / 8 * 8;
+        m.dy_copy = take(u.rows * m.dy_ld * m.size);
     }
     return at;
 }
@@ -174,6 +192,21 @@ cudaError_t copy_w(const Multiply& m, cudaStream_t stream) {
     return fasgd::launch_pack(p, stream);
 }
 
+cudaError_t copy_rows(const Multiply& m, const void* from, int64_t ld, int64_t cols, void* to, int64_t ld_to,
+                      cudaStream_t stream) {
+    if (to == nullptr) return cudaSuccess;
+    fasgd::Pack p = {};
+    p.from = from;
+    p.to = to;
+    p.rows = m.u.rows;
+    p.cols = cols;
+    p.ld_from = ld;
+    p.ld_to = ld_to;
+    p.groups = 1;
+    p.dtype_from = p.dtype_to = m.u.dtype;
+    return fasgd::launch_pack(p, stream);
+}
+
 fasgd::Product product(const Multiply& m) {
     fasgd::Product p = {};
     p.groups = (int32_t)m.u.experts;
@@ -188,7 +221,7 @@ fasgd::Product product(const Multiply& m) {
 fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across, const void* x, int64_t ld_x, void* y,
                        int64_t ld_y) {
     fasgd::Product p = product(m);
-    p.a = {m.w_copy != nullptr ? m.w_copy : m.u.w, m.w_ld, m.w_step, across};
+    p.a = {m.w(), m.w_ld, m.w_step, across};
     p.b = {x, ld_x, 0, 0};
     p.m = to;
     p.n = m.u.rows;
@@ -201,7 +234,7 @@ fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across,
 fasgd::Product by_experts(const Multiply& m) {
     const fasgd_multiply_args& u = m.u;
     fasgd::Product p = product(m);
-    const fasgd::Side x = {u.x, u.ld_x, 0, 1}, dy = {u.dy, u.ld_dy, 0, 1};
+    const fasgd::Side x = {m.x(), m.x_ld, 0, 1}, dy = {m.dy(), m.dy_ld, 0, 1};
     p.a = u.dw_flip ? x : dy;
     p.b = u.dw_flip ? dy : x;
     p.m = u.dw_flip ? u.inputs : u.outputs;
@@ -310,8 +343,9 @@ int fasgd_multiply(const fasgd_multiply_args* u, void* stream_) {
     if (int rc = check_multiply_shared(call, m)) return rc;
     if (u->rows == 0) return FASGD_OK;
     cudaError_t st = copy_w(m, stream);
+    if (st == cudaSuccess) st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, stream);
     if (st == cudaSuccess)
-        st = fasgd::launch_plain(by_rows(m, u->inputs, u->outputs, !u->w_flip, m.u.x, m.u.ld_x, m.u.y, m.u.ld_y), stream);
+        st = fasgd::launch_product(by_rows(m, u->inputs, u->outputs, !u->w_flip, m.x(), m.x_ld, m.u.y, m.u.ld_y), stream);
     return cuda_status(st, call);
 }
 
@@ -324,14 +358,20 @@ int fasgd_multiply_grad(const fasgd_multiply_args* u, void* stream_) {
     const int64_t need = lay_out(m, static_cast<char*>(u->workspace));
     if (int rc = check_workspace(call, u->workspace, u->workspace_bytes, need)) return rc;
     if (int rc = check_multiply_shared(call, m)) return rc;
-    cudaError_t st = cudaSuccess;
-    if (u->dx != nullptr && u->rows > 0) {
+    if (u->rows == 0) {      // no rows: no operands to copy or to describe
+        m.u.dtype = FASGD_F32;
+        return cuda_status(u->dw != nullptr ? fasgd::launch_product(by_experts(m), stream) : cudaSuccess, call);
+    }
+    cudaError_t st = copy_rows(m, m.u.dy, m.u.ld_dy, u->outputs, m.dy_copy, m.dy_ld, stream);
+    if (st == cudaSuccess && u->dx != nullptr) {
         st = copy_w(m, stream);
         if (st == cudaSuccess)
-            st = fasgd::launch_plain(by_rows(m, u->outputs, u->inputs, u->w_flip, m.u.dy, m.u.ld_dy, m.u.dx, m.u.ld_dx),
-                                     stream);
+            st = fasgd::launch_product(by_rows(m, u->outputs, u->inputs, u->w_flip, m.dy(), m.dy_ld, m.u.dx, m.u.ld_dx), stream);
     }
-    if (st == cudaSuccess && u->dw != nullptr) st = fasgd::launch_plain(by_experts(m), stream);
+    if (st == cudaSuccess && u->dw != nullptr) {
+        st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, stream);
+        if (st == cudaSuccess) st = fasgd::launch_product(by_experts(m), stream);
+    }
     return cuda_status(st, call);
 }
 

@@ -64,6 +64,10 @@ cudaError_t launch_plain(const Product& p, cudaStream_t stream);
 constexpr int kTileN = 256;
 bool tile_side(const Side& s, int64_t groups);
 cudaError_t launch_tiles(const Product& p, cudaStream_t stream);
+// 16-bit types take the tensor cores (their callers lay the sides out for them), fp32 the plain form.
+inline cudaError_t launch_product(const Product& p, cudaStream_t stream) {
+    return p.dtype == 0 ? launch_plain(p, stream) : launch_tiles(p, stream);
+}
 
 // A copy of a side with rows that lie as the fast kernels want them: `rows` rows of `cols`
 // values (of group g: p + g * step) to rows ld_to apart, cast to dtype_to.  What it leaves

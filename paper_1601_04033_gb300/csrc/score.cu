@@ -28,8 +28,10 @@ struct Score {
     int64_t size, tile;
     bool grad;
     // workspace
-    void* z_copy;                // rows x ld_zc, rows without a label as zeros
+    void* z_copy;                // rows x ld_zc (null: z itself serves)
     int64_t ld_zc;
+    void* w_copy;                // as w, rows ld_wc apart (null: w itself serves)
+    int64_t ld_wc;
     float2* parts;               // [tiles][rows]
     float *at_label, *lse;       // [rows]
     float* row_scale;            // [rows] upstream / N, 0 without a label
@@ -160,18 +162,29 @@ int64_t lay_out(Score& s, char* base) {
         at += (bytes + 255) / 256 * 256;
         return p;
     };
-    s.tile = fasgd::kPlainN;
+    s.tile = u.dtype == FASGD_F32 ? fasgd::kPlainN : fasgd::kTileN;
     const int64_t tiles = (u.classes + s.tile - 1) / s.tile;
     if (!u.known) {
         s.parts = reinterpret_cast<float2*>(take(8 * tiles * u.rows));
         s.at_label = reinterpret_cast<float*>(take(4 * u.rows));
     }
     s.lse = u.lse != nullptr ? u.lse : reinterpret_cast<float*>(take(4 * u.rows));
+    // Gradients' sums over rows need zeros where there is no label; 16-bit products, rows that
+    // start on 16 bytes.
+    s.z_copy = s.w_copy = nullptr;
+    s.ld_zc = u.ld_z;
+    s.ld_wc = u.ld_w;
+    if (s.grad || (u.dtype != FASGD_F32 && !fasgd::tile_side({u.z, u.ld_z, 0, 0}, 1))) {
+        s.ld_zc = (u.cols + 7) / 8 * 8;
+        s.z_copy = take(u.rows * s.ld_zc * s.size);
+    }
+    if (u.dtype != FASGD_F32 && !fasgd::tile_side({u.w, u.ld_w, 0, 0}, 1)) {
+        s.ld_wc = ((u.w_flip ? u.cols : u.classes) + 7) / 8 * 8;
+        s.w_copy = take((u.w_flip ? u.classes : u.cols) * s.ld_wc * s.size);
+    }
     if (!s.grad) return at;
     s.share = reinterpret_cast<float*>(take(4));
     s.row_scale = reinterpret_cast<float*>(take(4 * u.rows));
-    s.ld_zc = (u.cols + 7) / 8 * 8;
-    s.z_copy = take(u.rows * s.ld_zc * s.size);
     s.ld_g = (u.rows + 7) / 8 * 8;
     const int64_t most = std::max<int64_t>(64, FASGD_SCORE_PIECE / std::max<int64_t>(1, s.ld_g * s.size));
     const int64_t pieces = (u.classes + most - 1) / most;
@@ -190,31 +203,42 @@ const void* at_class(const void* p, int64_t ld, bool flip, int64_t v, int64_t si
 cudaError_t run(const Score& s, cudaStream_t stream) {
     const fasgd_score_args& u = s.u;
     cudaError_t st = cudaSuccess;
-    const bool has_z = s.grad;
-    const void* z = has_z ? s.z_copy : u.z;
-    const int64_t ld_z = has_z ? s.ld_zc : u.ld_z;
-    if (has_z) {
-        fasgd::Pack p = {};
-        p.from = u.z;
-        p.to = s.z_copy;
-        p.rows = u.rows;
-        p.cols = u.cols;
-        p.ld_from = u.ld_z;
-        p.ld_to = s.ld_zc;
-        p.groups = 1;
-        p.dtype_from = p.dtype_to = u.dtype;
-        p.labels = u.labels;
-        p.classes = u.classes;
-        st = fasgd::launch_pack(p, stream);
-        if (st != cudaSuccess) return st;
+    const void* z = u.z;
+    const void* w_all = u.w;
+    const int64_t ld_z = s.ld_zc, ld_w = s.ld_wc;
+    fasgd::Pack c = {};
+    c.groups = 1;
+    c.dtype_from = c.dtype_to = u.dtype;
+    if (s.w_copy != nullptr) {
+        c.from = u.w;
+        c.to = s.w_copy;
+        c.rows = u.w_flip ? u.classes : u.cols;
+        c.cols = u.w_flip ? u.cols : u.classes;
+        c.ld_from = u.ld_w;
+        c.ld_to = s.ld_wc;
+        if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
+        w_all = s.w_copy;
+    }
+    if (s.z_copy != nullptr) {
+        c.from = u.z;
+        c.to = s.z_copy;
+        c.rows = u.rows;
+        c.cols = u.cols;
+        c.ld_from = u.ld_z;
+        c.ld_to = s.ld_zc;
+        c.labels = u.labels;
+        c.classes = u.classes;
+        if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
+        z = s.z_copy;
     }
     Product p = {};
     p.a = {z, ld_z, 0, 0};
-    p.b = {u.w, u.ld_w, 0, !u.w_flip};
+    p.b = {w_all, ld_w, 0, !u.w_flip};
     p.m = u.rows;
     p.n = u.classes;
     p.k = u.cols;
-    p.dtype = u.dtype;
+    const int32_t dtype = u.rows > 0 ? u.dtype : FASGD_F32;      // no rows: no operands to describe
+    p.dtype = dtype;
     p.ending = fasgd::kStatistics;
     p.labels = u.labels;
     p.classes = u.classes;
@@ -222,7 +246,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     p.at_label = s.at_label;
     p.lse = s.lse;
     if (!u.known && u.rows > 0) {
-        st = fasgd::launch_plain(p, stream);
+        st = fasgd::launch_product(p, stream);
         if (st != cudaSuccess) return st;
         lse_kernel<<<(unsigned)((u.rows + 31) / 32), 256, 0, stream>>>(
             s.parts, (u.classes + s.tile - 1) / s.tile, u.rows, u.labels, u.classes, s.at_label, s.lse, u.row_loss);
@@ -234,7 +258,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     const float factor = u.dtype == FASGD_F16 ? 16384.0f : 1.0f;
     for (int64_t v = 0; v < u.classes; v += s.piece) {
         const int64_t n = std::min(s.piece, u.classes - v);
-        const void* w = at_class(u.w, u.ld_w, u.w_flip, v, s.size);
+        const void* w = at_class(w_all, ld_w, u.w_flip, v, s.size);
         p.b.p = w;
         p.n = n;
         p.n0 = v;
@@ -243,14 +267,14 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         p.ld_out = s.ld_g;
         p.out_dtype = u.dtype;
         p.factor = factor;
-        st = fasgd::launch_plain(p, stream);
+        st = fasgd::launch_product(p, stream);
         if (st != cudaSuccess) return st;
         Product q = {};
-        q.dtype = u.dtype;
+        q.dtype = dtype;
         q.ending = fasgd::kStore;
         q.factor = 1.0f / factor;
         if (u.dz != nullptr && u.rows > 0) {
-            q.a = {w, u.ld_w, 0, u.w_flip};
+            q.a = {w, ld_w, 0, u.w_flip};
             q.b = {s.g, s.ld_g, 0, 1};
             q.m = u.cols;
             q.n = u.rows;
@@ -268,11 +292,11 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
                 q.scale = s.row_scale;
                 q.by_n = 1;
             }
-            st = fasgd::launch_plain(q, stream);
+            st = fasgd::launch_product(q, stream);
             if (st != cudaSuccess) return st;
         }
         if (u.dw != nullptr) {
-            const fasgd::Side zs = {s.z_copy, s.ld_zc, 0, 1}, gs = {s.g, s.ld_g, 0, 0};
+            const fasgd::Side zs = {z, ld_z, 0, 1}, gs = {s.g, s.ld_g, 0, 0};
             q.a = u.dw_flip ? zs : gs;
             q.b = u.dw_flip ? gs : zs;
             q.m = u.dw_flip ? u.cols : n;
@@ -285,7 +309,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
             q.scale = s.share;
             q.by_n = 0;
             q.factor = 1.0f / factor;
-            st = fasgd::launch_plain(q, stream);
+            st = fasgd::launch_product(q, stream);
             if (st != cudaSuccess) return st;
         }
     }

@@ -1,0 +1,693 @@
+// Matrix products of 16-bit values on the tensor cores (tcgen05), operands by TMA.
+//
+// A block, or a pair of blocks (cluster of 2) that shares its MMAs, computes tiles of
+// 128 (256) m by up to 256 n, one after the other: warp 0 copies 64 steps of k of both
+// sides at a time into a ring of stages in shared memory, warp 1 issues the MMAs into one
+// of two accumulators in tensor memory, warps 2 to 5 empty the other one.  A side is
+// copied as it lies in memory, k or its own index consecutive (128-byte swizzle either way; the
+// MMA's descriptors say which), so no operand is ever transposed by a pass of its own.
+//
+// A pair exists for the copies: a tile of 256 x 256 moves 32 KB per block and 64 steps of
+// k, half as much per MMA as one block's 128 x 128, and less than its 128 x 256 (48 KB,
+// which at the tensor cores' full rate would be 96 bytes a cycle and SM out of L2).
+//
+// Ragged n (rows sorted by expert): a tile's n are one group's; what it copies beyond the
+// group's last row is another's and not stored, and the MMA is only as wide as it needs to be.
+// Ragged k (sums over a group's rows): the last copy's rows beyond the group are set to 0 in
+// shared memory before the MMAs, in both sides, since another group's NaN times 0 is NaN.
+//
+// Every wait is bounded (kWaitLimitNs): a wait that runs out raises the block's flag, every
+// role leaves, and what was not computed is written as NaN.
+
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "client.cuh"
+#include "product.cuh"
+#include "shared_limit.cuh"
+#include "wait.cuh"
+
+namespace fasgd {
+namespace {
+
+constexpr int kK = 64;                              // steps of k in a stage: 128 bytes
+constexpr int kBlockM = 128;                        // m of a block
+constexpr int kThreads = 192;
+constexpr int kSideA = kBlockM * kK * 2;            // bytes of A in a stage
+constexpr int kMaxGroups = FASGD_EXPERTS_MAX;
+constexpr int kColumns = 512;                       // of tensor memory: two accumulators
+
+template <int PAIR>
+struct Shape {
+    static constexpr int kSideB = kTileN / PAIR * kK * 2;
+    static constexpr int kStage = kSideA + kSideB;
+    static constexpr int kStages = PAIR == 2 ? 6 : 4;
+    static constexpr int kBytes = kStages * kStage + 1024;     // and room to align to 1,024
+};
+
+struct TileArgs {
+    CUtensorMap a, b;
+    Product p;
+    int32_t box_a, box_b;      // rows of a copy of a side that is not across
+    int64_t m_tiles, items;    // items: of all groups, unless n is ragged
+    int32_t splits;
+};
+
+// ---- PTX ------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t block_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// The address of a shared variable of the pair's first block.
+__device__ __forceinline__ uint32_t first_block(uint32_t addr) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+template <int PAIR>
+__device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    if (PAIR == 2)
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    return ok != 0;
+}
+// A whole warp waits for a phase; false (and *late): it did not come.
+template <int PAIR>
+__device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, volatile int32_t* late) {
+    const uint32_t bar = smem_addr(barrier);
+    if (__all_sync(0xffffffffu, test<PAIR>(bar, parity))) return true;
+    const uint64_t t0 = global_ns();
+    for (uint32_t i = 0; i < (1u << 26); ++i) {
+        if (__all_sync(0xffffffffu, test<PAIR>(bar, parity))) return true;
+        const bool stop = (i & 63u) == 63u && (global_ns() - t0 > kWaitLimitNs || *late != 0);
+        if (__any_sync(0xffffffffu, stop)) break;
+    }
+    *late = 1;
+    return false;
+}
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(smem_addr(bar))) : "memory");
+}
+__device__ __forceinline__ void arrive_first_expect(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(
+                     first_block(smem_addr(bar))),
+                 "r"(bytes)
+                 : "memory");
+}
+// A box at (x, y, z) to shared memory; bar: an address in this block's or (PAIR 2) its pair's.
+template <int PAIR>
+__device__ __forceinline__ void copy_box(const CUtensorMap* map, uint32_t to, uint32_t bar, int32_t x, int32_t y, int32_t z) {
+    if (PAIR == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, "
+            "%5}], [%2];" ::"r"(to),
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], "
+            "[%2];" ::"r"(to),
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+            : "memory");
+}
+template <int PAIR>
+__device__ __forceinline__ void mma(uint32_t to, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+    if (PAIR == 2)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(to),
+            "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(to),
+            "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+            : "memory");
+}
+// The barrier (of both blocks of a pair) is arrived at once all MMAs before this have ended.
+template <int PAIR>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    if (PAIR == 2)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                smem_addr(bar)),
+            "h"((uint16_t)3)
+            : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+                     : "memory");
+}
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+// 32 columns of the warp's 32 lanes of tensor memory.
+__device__ __forceinline__ void load_columns(uint32_t from, float (&v)[32]) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(from)
+        : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2E = 1.4426950408889634f;
+
+// A shared-memory matrix for the MMA: 128-byte swizzle; k consecutive (8 rows of 128 bytes
+// are 1,024 apart), or across: chunks of 64 values by 64 steps of k, 8,192 bytes apart, whose
+// groups of 8 steps are 1,024 apart.
+__device__ __forceinline__ uint64_t matrix_of(uint32_t addr, bool across) {
+    const uint64_t lead = across ? 8192 >> 4 : 1;
+    return (uint64_t)((addr & 0x3ffff) >> 4) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+// ---- tiles ------------------------------------------------------------------------------
+struct Tile {
+    int64_t m0, n0, n1, k0, k1;
+    int32_t group, split;
+    int64_t n_tile;
+};
+struct Shared {
+    uint64_t full[6], empty[6], ready[2], taken[2], tail;
+    uint32_t tmem;
+    volatile int32_t late;
+    int32_t first[kMaxGroups + 1];      // ragged n: the first n tile of each group
+};
+
+// first[] of the groups, by the first warp.  Offsets that rise and fall may claim more rows than
+// there are: numbers stay within 31 bits all the same.
+__device__ void count_tiles(const Product& p, Shared& s) {
+    if (threadIdx.x < 32) {
+        int64_t before = 0;
+        for (int g = threadIdx.x; g < (p.groups + 31) / 32 * 32; g += 32) {
+            int64_t tiles = 0;
+            if (g < p.groups) {
+                const Bounds b = group_bounds(p.offsets, g, p.n);
+                tiles = (b.hi - b.lo + kTileN - 1) / kTileN;
+            }
+            int64_t sum = tiles;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int64_t o = __shfl_up_sync(0xffffffffu, sum, d);
+                if (threadIdx.x >= d) sum += o;
+            }
+            if (g < p.groups) s.first[g] = (int32_t)min(before + sum - tiles, (int64_t)INT32_MAX);
+            before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (threadIdx.x == 0) s.first[p.groups] = (int32_t)min(before, (int64_t)INT32_MAX);
+    }
+}
+
+// Item i of the product; ragged n: i counts m tiles first, then the groups' n tiles.
+template <int PAIR>
+__device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, int64_t i) {
+    const Product& p = t.p;
+    Tile w;
+    w.split = 0;
+    w.group = 0;
+    w.k0 = 0;
+    w.k1 = p.k;
+    if (t.splits > 1) {
+        w.split = (int32_t)(i % t.splits);
+        i /= t.splits;
+    }
+    if (p.ragged == kRaggedN) {
+        const int64_t j = i / t.m_tiles;
+        w.m0 = (i - j * t.m_tiles) * (kBlockM * PAIR);
+        int lo = 0, hi = p.groups;                  // first[lo] <= j < first[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (s.first[mid] <= j)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        const Bounds b = group_bounds(p.offsets, lo, p.n);
+        w.group = lo;
+        w.n_tile = j;
+        w.n0 = b.lo + (j - s.first[lo]) * kTileN;
+        w.n1 = min(b.hi, w.n0 + kTileN);
+    } else {
+        const int64_t n_tiles = (p.n + kTileN - 1) / kTileN;
+        if (p.ragged == kRaggedK) {
+            w.group = (int32_t)(i / (t.m_tiles * n_tiles));
+            i -= (int64_t)w.group * t.m_tiles * n_tiles;
+            const Bounds b = group_bounds(p.offsets, w.group, p.k);
+            w.k0 = b.lo;
+            w.k1 = b.hi;
+        }
+        // Bands of up to 32 m tiles, by n: what runs at the same time shares its operands in L2.
+        const int64_t band = i / (32 * n_tiles), m_first = band * 32, high = min((int64_t)32, t.m_tiles - m_first);
+        i -= band * 32 * n_tiles;
+        w.n_tile = i / high;
+        w.m0 = (m_first + i - w.n_tile * high) * (kBlockM * PAIR);
+        w.n0 = w.n_tile * kTileN;
+        w.n1 = min(p.n, w.n0 + kTileN);
+    }
+    if (t.splits > 1) {
+        const int64_t blocks = (w.k1 - w.k0 + kK - 1) / kK, k0 = w.k0;
+        w.k0 = k0 + blocks * w.split / t.splits * kK;
+        w.k1 = min(w.k1, k0 + blocks * (w.split + 1) / t.splits * kK);
+    }
+    return w;
+}
+template <int PAIR>
+__device__ __forceinline__ int width_of(const Tile& w) {      // n of the MMA
+    constexpr int step = 16 * PAIR;
+    return (int)(w.n1 - w.n0 + step - 1) / step * step;
+}
+template <int PAIR>
+__device__ __forceinline__ int64_t items_of(const TileArgs& t, const Shared& s) {
+    return t.p.ragged == kRaggedN ? (int64_t)s.first[t.p.groups] * t.m_tiles * t.splits : t.items;
+}
+
+// ---- what becomes of an accumulator -----------------------------------------------------
+template <class T>
+__device__ __forceinline__ void store_columns(const Product& p, T* out, int64_t n, int count, bool live, const float (&v)[32]) {
+    if (!live) return;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < count) {
+            float x = v[j] * p.factor;
+            if (p.scale != nullptr) {
+                const float scale = p.scale[p.by_n ? n + j : 0];
+                x = p.by_n && scale == 0.0f ? 0.0f : x * scale;
+            }
+            out[j * p.ld_out] = from_f32<T>(x);
+        }
+}
+__device__ __forceinline__ void add_columns(const Product& p, float* out, int count, bool live, const float (&v)[32]) {
+    if (!live) return;
+    float old[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) old[j] = j < count ? out[j * p.ld_out] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < count) out[j * p.ld_out] = old[j] + v[j] * p.factor;
+}
+__device__ __forceinline__ void store_any(const Product& p, int64_t at, int64_t n, int count, bool live, const float (&v)[32]) {
+    if (p.out_dtype == FASGD_F32) {
+        if (p.add)
+            add_columns(p, static_cast<float*>(p.out) + at, count, live, v);
+        else
+            store_columns(p, static_cast<float*>(p.out) + at, n, count, live, v);
+    } else if (p.out_dtype == FASGD_BF16) {
+        store_columns(p, static_cast<__nv_bfloat16*>(p.out) + at, n, count, live, v);
+    } else {
+        store_columns(p, static_cast<__half*>(p.out) + at, n, count, live, v);
+    }
+}
+
+// Rows of y or dx that no group has.
+__device__ void clear_rows(const Product& p, int64_t block, int64_t blocks, int thread, int threads) {
+    const int64_t lo = group_bounds(p.offsets, 0, p.n).lo, hi = group_bounds(p.offsets, p.groups - 1, p.n).hi;
+    for (int64_t r = block; r < p.n - (hi - lo); r += blocks) {
+        const int64_t at = (r < lo ? r : hi + (r - lo)) * p.ld_out;
+        for (int64_t m = thread; m < p.m; m += threads) {
+            if (p.out_dtype == FASGD_F32)
+                static_cast<float*>(p.out)[at + m] = 0.0f;
+            else
+                static_cast<uint16_t*>(p.out)[at + m] = 0;
+        }
+    }
+}
+
+template <int PAIR, int ENDING>
+__global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t) {
+    using S = Shape<PAIR>;
+    extern __shared__ char raw[];
+    __shared__ Shared s;
+    char* const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+    const Product& p = t.p;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR == 2 ? block_rank() : 0;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(&s.full[i], PAIR);
+            mbar_init(&s.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.ready[i], 1);
+            mbar_init(&s.taken[i], 4 * PAIR);
+        }
+        mbar_init(&s.tail, 1);
+        s.late = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if (PAIR == 2)
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s.tmem)), "n"(kColumns)
+                         : "memory");
+        else
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s.tmem)), "n"(kColumns)
+                         : "memory");
+    }
+    if (p.ragged == kRaggedN) count_tiles(p, s);
+    fence_before();
+    __syncthreads();
+    if (PAIR == 2) {
+        asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
+    fence_after();
+    const uint32_t tmem = *(volatile uint32_t*)&s.tmem;
+    const int64_t items = items_of<PAIR>(t, s), team = blockIdx.x / PAIR, teams = gridDim.x / PAIR;
+
+    if (warp == 0) {
+        // Copies.
+        uint32_t stage = 0, phase = 0, tails = 0;
+        bool ok = true;
+        for (int64_t i = team; i < items && ok; i += teams) {
+            const Tile w = tile_of<PAIR>(t, s, i);
+            const int rows_b = width_of<PAIR>(w) / PAIR;
+            const int64_t m0 = w.m0 + rank * kBlockM, n0 = w.n0 + (int64_t)rank * rows_b;
+            const int boxes_a = p.a.across ? kBlockM / 64 : 1;
+            const int step_b = p.b.across ? 64 : t.box_b, boxes_b = (rows_b + step_b - 1) / step_b;
+            const uint32_t bytes = kSideA + boxes_b * step_b * kK * 2;
+            const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
+            for (int64_t k = w.k0; k < w.k1; k += kK) {
+                if (!(ok = wait<PAIR>(&s.empty[stage], phase ^ 1, &s.late))) break;
+                const bool tail = p.ragged == kRaggedK && w.k1 - k < kK;
+                char* const at = ring + stage * S::kStage;
+                if (lane == 0) {
+                    uint32_t bar;
+                    if (tail) {
+                        mbar_arrive_expect_tx(&s.tail, bytes);
+                        bar = smem_addr(&s.tail);
+                    } else {
+                        if (PAIR == 2) {
+                            arrive_first_expect(&s.full[stage], bytes);
+                            bar = first_block(smem_addr(&s.full[stage]));
+                        } else {
+                            mbar_arrive_expect_tx(&s.full[stage], bytes);
+                            bar = smem_addr(&s.full[stage]);
+                        }
+                    }
+                    const uint32_t to_a = smem_addr(at), to_b = to_a + kSideA;
+                    for (int j = 0; j < boxes_a; ++j) {
+                        if (p.a.across)
+                            copy_box<PAIR>(&t.a, to_a + j * 8192, bar, (int32_t)m0 + j * 64, (int32_t)k, ga);
+                        else
+                            copy_box<PAIR>(&t.a, to_a, bar, (int32_t)k, (int32_t)m0, ga);
+                    }
+                    for (int j = 0; j < boxes_b; ++j) {
+                        if (p.b.across)
+                            copy_box<PAIR>(&t.b, to_b + j * 8192, bar, (int32_t)n0 + j * 64, (int32_t)k, 0);
+                        else
+                            copy_box<PAIR>(&t.b, to_b + j * step_b * kK * 2, bar, (int32_t)k, (int32_t)n0 + j * step_b, 0);
+                    }
+                }
+                __syncwarp();
+                if (tail) {
+                    // Rows of other groups become 0 (both sides are across: a row is 128 bytes of each chunk).
+                    if (!(ok = wait<1>(&s.tail, tails & 1, &s.late))) break;
+                    ++tails;
+                    const int rows = (int)(w.k1 - k), chunks = boxes_a + boxes_b;
+                    for (int j = lane; j < chunks * (kK - rows) * 8; j += 32) {
+                        const int c = j / ((kK - rows) * 8), r = j % ((kK - rows) * 8);
+                        char* chunk = c < boxes_a ? at + c * 8192 : at + kSideA + (c - boxes_a) * 8192;
+                        *reinterpret_cast<float4*>(chunk + rows * 128 + r * 16) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (PAIR == 2)
+                            arrive_first(&s.full[stage]);
+                        else
+                            mbar_arrive(&s.full[stage]);
+                    }
+                }
+                if (++stage == S::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+        if (!ok) {      // copies in flight end within this
+            const uint64_t t0 = global_ns();
+            for (uint32_t i = 0; i < (1u << 24) && global_ns() - t0 < 2000000; ++i) {
+            }
+        }
+    } else if (warp == 1) {
+        // MMAs: the pair's first block issues them.
+        if (rank == 0) {
+            uint32_t stage = 0, phase = 0, tile = 0;
+            const uint32_t kind = p.dtype == FASGD_BF16 ? 1u << 7 | 1u << 10 : 0u;
+            const uint32_t base = 1u << 4 | kind | (uint32_t)(p.a.across != 0) << 15 | (uint32_t)(p.b.across != 0) << 16 |
+                                  (uint32_t)(kBlockM * PAIR / 16) << 24;
+            const uint32_t next_a = p.a.across ? 2048 >> 4 : 32 >> 4, next_b = p.b.across ? 2048 >> 4 : 32 >> 4;
+            bool ok = true;
+            for (int64_t i = team; i < items && ok; i += teams) {
+                const Tile w = tile_of<PAIR>(t, s, i);
+                if (w.k0 >= w.k1) continue;
+                const uint32_t shape = base | (uint32_t)(width_of<PAIR>(w) / 8) << 17;
+                const uint32_t buffer = tile & 1, to = tmem + buffer * kTileN;
+                if (!(ok = wait<PAIR>(&s.taken[buffer], (tile >> 1 & 1) ^ 1, &s.late))) break;
+                fence_after();
+                for (int64_t k = w.k0; k < w.k1; k += kK) {
+                    if (!(ok = wait<PAIR>(&s.full[stage], phase, &s.late))) break;
+                    fence_after();
+                    if (lane == 0) {
+                        const uint32_t at = smem_addr(ring + stage * S::kStage);
+                        const uint64_t a = matrix_of(at, p.a.across), b = matrix_of(at + kSideA, p.b.across);
+                        const int steps = (int)min((int64_t)(kK / 16), (w.k1 - k + 15) / 16);
+                        for (int j = 0; j < steps; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, shape, k > w.k0 || j > 0);
+                        commit<PAIR>(&s.empty[stage]);
+                        if (k + kK >= w.k1) commit<PAIR>(&s.ready[buffer]);
+                    }
+                    __syncwarp();
+                    if (++stage == S::kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+                ++tile;
+            }
+        }
+    } else {
+        // Results.  The warp's lanes of tensor memory are those of its number modulo 4.
+        const int quarter = warp & 3;
+        if (p.ragged == kRaggedN) clear_rows(p, blockIdx.x, gridDim.x, threadIdx.x - 64, 128);
+        uint32_t tile = 0;
+        bool ok = true;
+        for (int64_t i = team; i < items; i += teams) {
+            const Tile w = tile_of<PAIR>(t, s, i);
+            const bool some = w.k0 < w.k1;
+            const uint32_t buffer = tile & 1;
+            if (some) {
+                ok = ok && wait<PAIR>(&s.ready[buffer], tile >> 1 & 1, &s.late);
+                fence_after();
+                ++tile;
+            }
+            const int64_t m = w.m0 + rank * kBlockM + quarter * 32 + lane;
+            const bool live = m < p.m;
+            const int count = (int)(w.n1 - w.n0);
+            const uint32_t from = tmem + buffer * kTileN + ((uint32_t)(quarter * 32) << 16);
+            float v[32];
+            const auto columns = [&](int c) {
+                if (some && ok) {
+                    load_columns(from + c, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = ok ? 0.0f : NAN;
+                }
+            };
+            if (ENDING == kStore) {
+                const int64_t base = (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * t.p.step_split + w.n0 * p.ld_out + m;
+                for (int c = 0; c < count; c += 32) {
+                    columns(c);
+                    store_any(p, base + c * p.ld_out, w.n0 + c, min(32, count - c), live, v);
+                }
+            } else {
+                const int64_t label = live ? p.labels[m] : -1;
+                const bool has = label >= 0 && label < p.classes;
+                const int64_t in = label - p.n0 - w.n0;      // the label's column of this tile
+                const int at = has && in >= 0 && in < count ? (int)in : -1;
+                if (ENDING == kStatistics) {
+                    float top = -INFINITY, sum = 0.0f;
+                    for (int c = 0; c < count; c += 32) {
+                        columns(c);
+                        if (count - c < 32)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = j < count - c ? v[j] : -INFINITY;
+                        float most = v[0];
+#pragma unroll
+                        for (int j = 1; j < 32; ++j) most = fmaxf(most, v[j]);
+                        most = fmaxf(top, most);
+                        if (__any_sync(0xffffffffu, (uint32_t)(at - c) < 32u)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j == at - c) p.at_label[m] = v[j];
+                        }
+                        const float shift = most == -INFINITY ? 0.0f : most;
+                        float part[4] = {};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[j] - shift) * kLog2E);
+                        sum = sum * exp2_fast((top - shift) * kLog2E) + ((part[0] + part[1]) + (part[2] + part[3]));
+                        top = most;
+                    }
+                    if (live) p.parts[(p.n0 / kTileN + w.n_tile) * p.m + m] = make_float2(top, sum);
+                } else {
+                    const float lse = has ? p.lse[m] : INFINITY;
+                    const float more = log2f(p.factor);
+                    const int64_t base = w.n0 * p.ld_out + m;
+                    for (int c = 0; c < count; c += 32) {
+                        columns(c);
+                        const bool here = (uint32_t)(at - c) < 32u;
+                        float own = 0.0f;
+                        if (__any_sync(0xffffffffu, here)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j == at - c) own = p.factor * expm1f(v[j] - lse);
+                        }
+                        const auto write = [&](auto* out) {
+                            using T = std::remove_reference_t<decltype(*out)>;
+                            if (!live) return;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j < count - c) {
+                                    const float g = exp2_fast(fmaf(v[j] - lse, kLog2E, more));
+                                    out[j * p.ld_out] = from_f32<T>(here && j == at - c ? own : g);
+                                }
+                        };
+                        if (p.out_dtype == FASGD_BF16)
+                            write(static_cast<__nv_bfloat16*>(p.out) + base + c * p.ld_out);
+                        else
+                            write(static_cast<__half*>(p.out) + base + c * p.ld_out);
+                    }
+                }
+            }
+            if (some) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR == 2)
+                        arrive_first(&s.taken[buffer]);
+                    else
+                        mbar_arrive(&s.taken[buffer]);
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (PAIR == 2) {      // no block leaves while its pair may still reach its memory
+        asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
+    if (warp == 1) {
+        fence_after();
+        if (PAIR == 2) {
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kColumns));
+        } else {
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kColumns));
+        }
+    }
+}
+
+// ---- host -------------------------------------------------------------------------------
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {
+    static const Encode f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess)
+            cudaGetLastError();
+        return found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(p) : nullptr;
+    }();
+    return f;
+}
+// How a side lies: `size` values of its index (all groups' rows, where it is ragged), k of the sums.
+bool encode(CUtensorMap* map, const Side& s, int dtype, int64_t size, int64_t k, int64_t groups, int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)(s.across ? size : k), (cuuint64_t)(s.across ? k : size), (cuuint64_t)groups};
+    const cuuint64_t ld = (cuuint64_t)s.ld * 2, step = groups > 1 ? (cuuint64_t)s.step * 2 : ld;
+    const cuuint64_t strides[2] = {ld, step};
+    const cuuint32_t box[3] = {64, (cuuint32_t)(s.across ? kK : box_rows), 1}, one[3] = {1, 1, 1};
+    const Encode f = encoder();
+    return f != nullptr &&
+           f(map, dtype == FASGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+             const_cast<void*>(s.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int PAIR, int ENDING>
+cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStream_t stream) {
+    static SharedLimit limit;
+    const int bytes = Shape<PAIR>::kBytes;
+    const int error = limit.ensure(device, bytes, bytes, [](int64_t n) {
+        return (int)cudaFuncSetAttribute(tile_kernel<PAIR, ENDING>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
+    });
+    if (error != 0) return (cudaError_t)error;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<int64_t>(most, sms / PAIR) * PAIR);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = PAIR;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING>, t);
+}
+template <int PAIR>
+cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
+    const Product& p = t.p;
+    t.m_tiles = (p.m + kBlockM * PAIR - 1) / (kBlockM * PAIR);
+    const int64_t n_tiles = (p.n + kTileN - 1) / kTileN + (p.ragged == kRaggedN ? p.groups : 0);
+    t.items = t.m_tiles * n_tiles * t.splits * (p.ragged == kRaggedK ? p.groups : 1);
+    if (t.items == 0) return cudaSuccess;
+    t.box_b = p.ragged == kRaggedN ? 32 : kTileN / PAIR;
+    if (!encode(&t.a, p.a, p.dtype, p.m, p.k, p.ragged == kRaggedN ? p.groups : 1, kBlockM) ||
+        !encode(&t.b, p.b, p.dtype, p.n, p.k, 1, t.box_b))
+        return cudaErrorInvalidValue;
+    switch (p.ending) {
+        case kStore: return launch<PAIR, kStore>(t, t.items, device, sms, stream);
+        case kStatistics: return launch<PAIR, kStatistics>(t, t.items, device, sms, stream);
+        default: return launch<PAIR, kResidual>(t, t.items, device, sms, stream);
+    }
+}
+
+}  // namespace
+
+bool tile_side(const Side& s, int64_t groups) {
+    return (reinterpret_cast<uintptr_t>(s.p) & 15) == 0 && s.ld % 8 == 0 && (groups < 2 || s.step % s.ld == 0);
+}
+
+cudaError_t launch_tiles(const Product& p, cudaStream_t stream) {
+    int device = 0, sms = 0;
+    cudaError_t st = cudaGetDevice(&device);
+    if (st == cudaSuccess) st = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (st != cudaSuccess) return st;
+    TileArgs t = {};
+    t.p = p;
+    t.splits = 1;
+    return p.m > kBlockM ? launch<2>(t, device, sms, stream) : launch<1>(t, device, sms, stream);
+}
+
+}  // namespace fasgd
