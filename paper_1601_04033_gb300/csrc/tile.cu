@@ -66,10 +66,12 @@ __device__ __forceinline__ uint32_t first_block(uint32_t addr) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
     return r;
 }
-template <int PAIR>
+// CLUSTER: what the pair's other block wrote before it arrived is seen too.  (That, and a release
+// of the same width, cost some 2,000 cycles each: only where a block writes what its pair's MMA reads.)
+template <bool CLUSTER>
 __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    if (PAIR == 2)
+    if (CLUSTER)
         asm volatile(
             "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
             " selp.u32 %0, 1, 0, p;\n}\n"
@@ -85,24 +87,31 @@ __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // A whole warp waits for a phase; false (and *late): it did not come.
-template <int PAIR>
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, volatile int32_t* late) {
     const uint32_t bar = smem_addr(barrier);
-    if (__all_sync(0xffffffffu, test<PAIR>(bar, parity))) return true;
-    const uint64_t t0 = global_ns();
+    uint64_t t0 = 0;       // (reading the timer takes as long as some k of MMAs: not before it is needed)
     for (uint32_t i = 0; i < (1u << 26); ++i) {
-        if (__all_sync(0xffffffffu, test<PAIR>(bar, parity))) return true;
-        const bool stop = (i & 63u) == 63u && (global_ns() - t0 > kWaitLimitNs || *late != 0);
-        if (__any_sync(0xffffffffu, stop)) break;
+        if (__all_sync(0xffffffffu, test<CLUSTER>(bar, parity))) return true;
+        if ((i & 255u) == 255u) {
+            const uint64_t now = global_ns();
+            if (t0 == 0) t0 = now;
+            if (__any_sync(0xffffffffu, now - t0 > kWaitLimitNs || *late != 0)) break;
+        }
     }
     *late = 1;
     return false;
 }
+template <bool CLUSTER = false>
 __device__ __forceinline__ void arrive_first(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(smem_addr(bar))) : "memory");
+    const uint32_t at = first_block(smem_addr(bar));
+    if (CLUSTER)
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
+    else
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
 }
 __device__ __forceinline__ void arrive_first_expect(uint64_t* bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(
+    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(
                      first_block(smem_addr(bar))),
                  "r"(bytes)
                  : "memory");
@@ -386,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const uint32_t bytes = kSideA + boxes_b * step_b * kK * 2;
             const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
             for (int64_t k = w.k0; k < w.k1; k += kK) {
-                if (!(ok = wait<PAIR>(&s.empty[stage], phase ^ 1, &s.late))) break;
+                if (!(ok = wait(&s.empty[stage], phase ^ 1, &s.late))) break;
                 const bool tail = p.ragged == kRaggedK && w.k1 - k < kK;
                 char* const at = ring + stage * S::kStage;
                 if (lane == 0) {
@@ -420,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 __syncwarp();
                 if (tail) {
                     // Rows of other groups become 0 (both sides are across: a row is 128 bytes of each chunk).
-                    if (!(ok = wait<1>(&s.tail, tails & 1, &s.late))) break;
+                    if (!(ok = wait(&s.tail, tails & 1, &s.late))) break;
                     ++tails;
                     const int rows = (int)(w.k1 - k), chunks = boxes_a + boxes_b;
                     for (int j = lane; j < chunks * (kK - rows) * 8; j += 32) {
@@ -432,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     __syncwarp();
                     if (lane == 0) {
                         if (PAIR == 2)
-                            arrive_first(&s.full[stage]);
+                            arrive_first<true>(&s.full[stage]);
                         else
                             mbar_arrive(&s.full[stage]);
                     }
@@ -462,10 +471,11 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 if (w.k0 >= w.k1) continue;
                 const uint32_t shape = base | (uint32_t)(width_of<PAIR>(w) / 8) << 17;
                 const uint32_t buffer = tile & 1, to = tmem + buffer * kTileN;
-                if (!(ok = wait<PAIR>(&s.taken[buffer], (tile >> 1 & 1) ^ 1, &s.late))) break;
+                if (!(ok = wait(&s.taken[buffer], (tile >> 1 & 1) ^ 1, &s.late))) break;
                 fence_after();
                 for (int64_t k = w.k0; k < w.k1; k += kK) {
-                    if (!(ok = wait<PAIR>(&s.full[stage], phase, &s.late))) break;
+                    if (!(ok = p.ragged == kRaggedK && w.k1 - k < kK ? wait<PAIR == 2>(&s.full[stage], phase, &s.late)
+                                                                            : wait(&s.full[stage], phase, &s.late))) break;
                     fence_after();
                     if (lane == 0) {
                         const uint32_t at = smem_addr(ring + stage * S::kStage);
@@ -495,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const bool some = w.k0 < w.k1;
             const uint32_t buffer = tile & 1;
             if (some) {
-                ok = ok && wait<PAIR>(&s.ready[buffer], tile >> 1 & 1, &s.late);
+                ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
                 fence_after();
                 ++tile;
             }
