@@ -290,39 +290,57 @@ __device__ __forceinline__ int64_t items_of(const TileArgs& t, const Shared& s) 
 }
 
 // ---- what becomes of an accumulator -----------------------------------------------------
+// What the stores need, in registers: read again from the kernel's parameters after each of
+// them (which might alias, for all the compiler knows) it made 180 cycles a column.
+struct Target {
+    void* out;
+    int64_t ld;
+    const float* scale;
+    float factor;
+    int32_t by_n, dtype, add;
+};
 template <class T>
-__device__ __forceinline__ void store_columns(const Product& p, T* out, int64_t n, int count, bool live, const float (&v)[32]) {
+__device__ __forceinline__ void store_columns(const Target& g, int64_t at, int64_t n, int count, bool live, const float (&v)[32]) {
     if (!live) return;
+    T* out = static_cast<T*>(g.out) + at;
+    if (g.scale != nullptr && g.by_n) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < count) {
+                const float scale = g.scale[n + j];
+                *out = from_f32<T>(scale == 0.0f ? 0.0f : v[j] * (scale * g.factor));
+                out += g.ld;
+            }
+        return;
+    }
+    const float scale = g.scale != nullptr ? *g.scale * g.factor : g.factor;
 #pragma unroll
     for (int j = 0; j < 32; ++j)
         if (j < count) {
-            float x = v[j] * p.factor;
-            if (p.scale != nullptr) {
-                const float scale = p.scale[p.by_n ? n + j : 0];
-                x = p.by_n && scale == 0.0f ? 0.0f : x * scale;
-            }
-            out[j * p.ld_out] = from_f32<T>(x);
+            *out = from_f32<T>(v[j] * scale);
+            out += g.ld;
         }
 }
-__device__ __forceinline__ void add_columns(const Product& p, float* out, int count, bool live, const float (&v)[32]) {
+__device__ __forceinline__ void add_columns(const Target& g, int64_t at, int count, bool live, const float (&v)[32]) {
     if (!live) return;
+    float* const out = static_cast<float*>(g.out) + at;
     float old[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) old[j] = j < count ? out[j * p.ld_out] : 0.0f;
+    for (int j = 0; j < 32; ++j) old[j] = j < count ? out[j * g.ld] : 0.0f;
 #pragma unroll
     for (int j = 0; j < 32; ++j)
-        if (j < count) out[j * p.ld_out] = old[j] + v[j] * p.factor;
+        if (j < count) out[j * g.ld] = old[j] + v[j] * g.factor;
 }
-__device__ __forceinline__ void store_any(const Product& p, int64_t at, int64_t n, int count, bool live, const float (&v)[32]) {
-    if (p.out_dtype == FASGD_F32) {
-        if (p.add)
-            add_columns(p, static_cast<float*>(p.out) + at, count, live, v);
+__device__ __forceinline__ void store_any(const Target& g, int64_t at, int64_t n, int count, bool live, const float (&v)[32]) {
+    if (g.dtype == FASGD_F32) {
+        if (g.add)
+            add_columns(g, at, count, live, v);
         else
-            store_columns(p, static_cast<float*>(p.out) + at, n, count, live, v);
-    } else if (p.out_dtype == FASGD_BF16) {
-        store_columns(p, static_cast<__nv_bfloat16*>(p.out) + at, n, count, live, v);
+            store_columns<float>(g, at, n, count, live, v);
+    } else if (g.dtype == FASGD_BF16) {
+        store_columns<__nv_bfloat16>(g, at, n, count, live, v);
     } else {
-        store_columns(p, static_cast<__half*>(p.out) + at, n, count, live, v);
+        store_columns<__half>(g, at, n, count, live, v);
     }
 }
 
@@ -497,6 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     } else {
         // Results.  The warp's lanes of tensor memory are those of its number modulo 4.
         const int quarter = warp & 3;
+        const Target target = {p.out, p.ld_out, p.scale, p.factor, p.by_n, p.out_dtype, p.add};
         if (p.ragged == kRaggedN) clear_rows(p, blockIdx.x, gridDim.x, threadIdx.x - 64, 128);
         uint32_t tile = 0;
         bool ok = true;
@@ -526,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 const int64_t base = (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * t.p.step_split + w.n0 * p.ld_out + m;
                 for (int c = 0; c < count; c += 32) {
                     columns(c);
-                    store_any(p, base + c * p.ld_out, w.n0 + c, min(32, count - c), live, v);
+                    store_any(target, base + c * target.ld, w.n0 + c, min(32, count - c), live, v);
                 }
             } else {
                 const int64_t label = live ? p.labels[m] : -1;
@@ -577,13 +596,14 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                             for (int j = 0; j < 32; ++j)
                                 if (j < count - c) {
                                     const float g = exp2_fast(fmaf(v[j] - lse, kLog2E, more));
-                                    out[j * p.ld_out] = from_f32<T>(here && j == at - c ? own : g);
+                                    *out = from_f32<T>(here && j == at - c ? own : g);
+                                    out += target.ld;
                                 }
                         };
-                        if (p.out_dtype == FASGD_BF16)
-                            write(static_cast<__nv_bfloat16*>(p.out) + base + c * p.ld_out);
+                        if (target.dtype == FASGD_BF16)
+                            write(static_cast<__nv_bfloat16*>(target.out) + base + c * target.ld);
                         else
-                            write(static_cast<__half*>(p.out) + base + c * p.ld_out);
+                            write(static_cast<__half*>(target.out) + base + c * target.ld);
                     }
                 }
             }
