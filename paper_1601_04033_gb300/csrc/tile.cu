@@ -35,6 +35,7 @@ constexpr int kK = 64;                              // steps of k in a stage: 12
 constexpr int kBlockM = 128;                        // m of a block
 constexpr int kThreads = 192;
 constexpr int kSideA = kBlockM * kK * 2;            // bytes of A in a stage
+constexpr int kFew = 32;                             // rows of a box of a short tile
 constexpr int kMaxGroups = FASGD_EXPERTS_MAX;
 constexpr int kColumns = 512;                       // of tensor memory: two accumulators
 
@@ -47,9 +48,9 @@ struct Shape {
 };
 
 struct TileArgs {
-    CUtensorMap a, b;
+    CUtensorMap a, b, few;     // few: B in boxes of kFew rows, for groups' short tiles
     Product p;
-    int32_t box_a, box_b;      // rows of a copy of a side that is not across
+    int32_t wide_a, wide_b;    // a side that is across, in boxes of several chunks
     int64_t m_tiles, items;    // items: of all groups, unless n is ragged
     int32_t splits;
 };
@@ -86,21 +87,26 @@ __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
             : "memory");
     return ok != 0;
 }
-// A whole warp waits for a phase; false (and *late): it did not come.
+// One thread waits for a phase; false (and *late): it did not come.  The timer is read only
+// after a while: that takes as long as the MMAs of some k.
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, volatile int32_t* late) {
+__device__ __forceinline__ bool wait_thread(uint64_t* barrier, uint32_t parity, volatile int32_t* late) {
     const uint32_t bar = smem_addr(barrier);
-    uint64_t t0 = 0;       // (reading the timer takes as long as some k of MMAs: not before it is needed)
-    for (uint32_t i = 0; i < (1u << 26); ++i) {
-        if (__all_sync(0xffffffffu, test<CLUSTER>(bar, parity))) return true;
-        if ((i & 255u) == 255u) {
+    uint64_t t0 = 0;
+    for (uint32_t i = 1; i < (1u << 26); ++i) {
+        if (test<CLUSTER>(bar, parity)) return true;
+        if ((i & 255u) == 0) {
             const uint64_t now = global_ns();
             if (t0 == 0) t0 = now;
-            if (__any_sync(0xffffffffu, now - t0 > kWaitLimitNs || *late != 0)) break;
+            if (now - t0 > kWaitLimitNs || *late != 0) break;
         }
     }
     *late = 1;
     return false;
+}
+// A whole warp.
+__device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, volatile int32_t* late) {
+    return __all_sync(0xffffffffu, wait_thread(barrier, parity, late));
 }
 template <bool CLUSTER = false>
 __device__ __forceinline__ void arrive_first(uint64_t* bar) {
@@ -116,20 +122,21 @@ __device__ __forceinline__ void arrive_first_expect(uint64_t* bar, uint32_t byte
                  "r"(bytes)
                  : "memory");
 }
-// A box at (x, y, z) to shared memory; bar: an address in this block's or (PAIR 2) its pair's.
+// A box at (x, y, z, g) to shared memory; bar: an address in this block's or (PAIR 2) its pair's.
 template <int PAIR>
-__device__ __forceinline__ void copy_box(const CUtensorMap* map, uint32_t to, uint32_t bar, int32_t x, int32_t y, int32_t z) {
+__device__ __forceinline__ void copy_box(const CUtensorMap* map, uint32_t to, uint32_t bar, int32_t x, int32_t y, int32_t z,
+                                         int32_t g) {
     if (PAIR == 2)
         asm volatile(
-            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, "
-            "%5}], [%2];" ::"r"(to),
-            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, "
+            "%5, %6}], [%2];" ::"r"(to),
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(g)
             : "memory");
     else
         asm volatile(
-            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], "
+            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], "
             "[%2];" ::"r"(to),
-            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(g)
             : "memory");
 }
 template <int PAIR>
@@ -279,9 +286,10 @@ __device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, int6
     }
     return w;
 }
+// n of the MMA; the halves of a pair's side that is across begin with a chunk.
 template <int PAIR>
-__device__ __forceinline__ int width_of(const Tile& w) {      // n of the MMA
-    constexpr int step = 16 * PAIR;
+__device__ __forceinline__ int width_of(const TileArgs& t, const Tile& w) {
+    const int step = PAIR == 2 && t.p.b.across ? 128 : 16 * PAIR;
     return (int)(w.n1 - w.n0 + step - 1) / step * step;
 }
 template <int PAIR>
@@ -406,10 +414,13 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         bool ok = true;
         for (int64_t i = team; i < items && ok; i += teams) {
             const Tile w = tile_of<PAIR>(t, s, i);
-            const int rows_b = width_of<PAIR>(w) / PAIR;
+            const int rows_b = width_of<PAIR>(t, w) / PAIR;
             const int64_t m0 = w.m0 + rank * kBlockM, n0 = w.n0 + (int64_t)rank * rows_b;
-            const int boxes_a = p.a.across ? kBlockM / 64 : 1;
-            const int step_b = p.b.across ? 64 : t.box_b, boxes_b = (rows_b + step_b - 1) / step_b;
+            const int boxes_a = p.a.across && !t.wide_a ? kBlockM / 64 : 1;
+            // B: one box, or for a short tile of a group and for sides of odd widths several.
+            const bool few = p.ragged == kRaggedN && rows_b <= 64 * (3 - PAIR);
+            const int step_b = few ? kFew : p.b.across && !t.wide_b ? 64 : kTileN / PAIR;
+            const int boxes_b = (rows_b + step_b - 1) / step_b;
             const uint32_t bytes = kSideA + boxes_b * step_b * kK * 2;
             const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
             for (int64_t k = w.k0; k < w.k1; k += kK) {
@@ -431,28 +442,33 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                         }
                     }
                     const uint32_t to_a = smem_addr(at), to_b = to_a + kSideA;
-                    for (int j = 0; j < boxes_a; ++j) {
-                        if (p.a.across)
-                            copy_box<PAIR>(&t.a, to_a + j * 8192, bar, (int32_t)m0 + j * 64, (int32_t)k, ga);
-                        else
-                            copy_box<PAIR>(&t.a, to_a, bar, (int32_t)k, (int32_t)m0, ga);
-                    }
-                    for (int j = 0; j < boxes_b; ++j) {
-                        if (p.b.across)
-                            copy_box<PAIR>(&t.b, to_b + j * 8192, bar, (int32_t)n0 + j * 64, (int32_t)k, 0);
-                        else
-                            copy_box<PAIR>(&t.b, to_b + j * step_b * kK * 2, bar, (int32_t)k, (int32_t)n0 + j * step_b, 0);
-                    }
+                    if (!p.a.across)
+                        copy_box<PAIR>(&t.a, to_a, bar, (int32_t)k, (int32_t)m0, 0, ga);
+                    else if (t.wide_a)
+                        copy_box<PAIR>(&t.a, to_a, bar, 0, (int32_t)k, (int32_t)(m0 / 64), ga);
+                    else
+                        for (int j = 0; j < boxes_a; ++j)
+                            copy_box<PAIR>(&t.a, to_a + j * 8192, bar, (int32_t)m0 + j * 64, (int32_t)k, 0, ga);
+                    if (few)
+                        for (int j = 0; j < boxes_b; ++j)
+                            copy_box<PAIR>(&t.few, to_b + j * kFew * kK * 2, bar, (int32_t)k, (int32_t)n0 + j * kFew, 0, 0);
+                    else if (!p.b.across)
+                        copy_box<PAIR>(&t.b, to_b, bar, (int32_t)k, (int32_t)n0, 0, 0);
+                    else if (t.wide_b)
+                        copy_box<PAIR>(&t.b, to_b, bar, 0, (int32_t)k, (int32_t)(n0 / 64), 0);
+                    else
+                        for (int j = 0; j < boxes_b; ++j)
+                            copy_box<PAIR>(&t.b, to_b + j * 8192, bar, (int32_t)n0 + j * 64, (int32_t)k, 0, 0);
                 }
                 __syncwarp();
                 if (tail) {
                     // Rows of other groups become 0 (both sides are across: a row is 128 bytes of each chunk).
                     if (!(ok = wait(&s.tail, tails & 1, &s.late))) break;
                     ++tails;
-                    const int rows = (int)(w.k1 - k), chunks = boxes_a + boxes_b;
+                    const int rows = (int)(w.k1 - k), chunks = (int)(bytes / 8192);
                     for (int j = lane; j < chunks * (kK - rows) * 8; j += 32) {
                         const int c = j / ((kK - rows) * 8), r = j % ((kK - rows) * 8);
-                        char* chunk = c < boxes_a ? at + c * 8192 : at + kSideA + (c - boxes_a) * 8192;
+                        char* chunk = at + c * 8192;
                         *reinterpret_cast<float4*>(chunk + rows * 128 + r * 16) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -476,42 +492,50 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             }
         }
     } else if (warp == 1) {
-        // MMAs: the pair's first block issues them.
-        if (rank == 0) {
+        // MMAs: one thread of the pair's first block issues them (with the whole warp in the loop
+        // the tensor cores waited for it: 945 cycles for 64 steps of k instead of 700).
+        if (rank == 0 && lane == 0) {
             uint32_t stage = 0, phase = 0, tile = 0;
             const uint32_t kind = p.dtype == FASGD_BF16 ? 1u << 7 | 1u << 10 : 0u;
             const uint32_t base = 1u << 4 | kind | (uint32_t)(p.a.across != 0) << 15 | (uint32_t)(p.b.across != 0) << 16 |
                                   (uint32_t)(kBlockM * PAIR / 16) << 24;
             const uint32_t next_a = p.a.across ? 2048 >> 4 : 32 >> 4, next_b = p.b.across ? 2048 >> 4 : 32 >> 4;
+            const uint64_t a0 = matrix_of(smem_addr(ring), p.a.across), b0 = matrix_of(smem_addr(ring) + kSideA, p.b.across);
+            const bool cut = p.ragged == kRaggedK;
             bool ok = true;
             for (int64_t i = team; i < items && ok; i += teams) {
                 const Tile w = tile_of<PAIR>(t, s, i);
                 if (w.k0 >= w.k1) continue;
-                const uint32_t shape = base | (uint32_t)(width_of<PAIR>(w) / 8) << 17;
+                const uint32_t shape = base | (uint32_t)(width_of<PAIR>(t, w) / 8) << 17;
                 const uint32_t buffer = tile & 1, to = tmem + buffer * kTileN;
-                if (!(ok = wait(&s.taken[buffer], (tile >> 1 & 1) ^ 1, &s.late))) break;
+                if (!(ok = wait_thread(&s.taken[buffer], (tile >> 1 & 1) ^ 1, &s.late))) break;
                 fence_after();
-                for (int64_t k = w.k0; k < w.k1; k += kK) {
-                    if (!(ok = p.ragged == kRaggedK && w.k1 - k < kK ? wait<PAIR == 2>(&s.full[stage], phase, &s.late)
-                                                                            : wait(&s.full[stage], phase, &s.late))) break;
+                const int64_t steps = (w.k1 - w.k0 + 15) / 16;      // of 16 k each; 4 to a stage
+                for (int64_t k = 0; k < steps; k += 4) {
+                    const bool zeroed = cut && w.k1 - w.k0 - k * 16 < kK;
+                    ok = PAIR == 2 && zeroed ? wait_thread<true>(&s.full[stage], phase, &s.late)
+                                             : wait_thread(&s.full[stage], phase, &s.late);
+                    if (!ok) break;
                     fence_after();
-                    if (lane == 0) {
-                        const uint32_t at = smem_addr(ring + stage * S::kStage);
-                        const uint64_t a = matrix_of(at, p.a.across), b = matrix_of(at + kSideA, p.b.across);
-                        const int steps = (int)min((int64_t)(kK / 16), (w.k1 - k + 15) / 16);
-                        for (int j = 0; j < steps; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, shape, k > w.k0 || j > 0);
-                        commit<PAIR>(&s.empty[stage]);
-                        if (k + kK >= w.k1) commit<PAIR>(&s.ready[buffer]);
+                    const uint64_t a = a0 + stage * (S::kStage >> 4), b = b0 + stage * (S::kStage >> 4);
+                    mma<PAIR>(to, a, b, shape, k > 0);
+                    if (k + 4 <= steps) {
+#pragma unroll
+                        for (int j = 1; j < 4; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, shape, true);
+                    } else {
+                        for (int j = 1; j < (int)(steps - k); ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, shape, true);
                     }
-                    __syncwarp();
+                    commit<PAIR>(&s.empty[stage]);
                     if (++stage == S::kStages) {
                         stage = 0;
                         phase ^= 1;
                     }
                 }
+                if (ok) commit<PAIR>(&s.ready[buffer]);
                 ++tile;
             }
         }
+        __syncwarp();
     } else {
         // Results.  The warp's lanes of tensor memory are those of its number modulo 4.
         const int quarter = warp & 3;
@@ -652,15 +676,18 @@ Encode encoder() {
     return f;
 }
 // How a side lies: `size` values of its index (all groups' rows, where it is ragged), k of the sums.
-bool encode(CUtensorMap* map, const Side& s, int dtype, int64_t size, int64_t k, int64_t groups, int box_rows) {
-    const cuuint64_t dims[3] = {(cuuint64_t)(s.across ? size : k), (cuuint64_t)(s.across ? k : size), (cuuint64_t)groups};
-    const cuuint64_t ld = (cuuint64_t)s.ld * 2, step = groups > 1 ? (cuuint64_t)s.step * 2 : ld;
-    const cuuint64_t strides[2] = {ld, step};
-    const cuuint32_t box[3] = {64, (cuuint32_t)(s.across ? kK : box_rows), 1}, one[3] = {1, 1, 1};
+// box: how many of the index a box has; wide (a side that is across): as chunks of 64, which
+// have to be whole ones.
+bool encode(CUtensorMap* map, const Side& s, int dtype, int64_t size, int64_t k, int64_t groups, int box, bool wide) {
+    const auto u = [](int64_t n) { return (cuuint64_t)n; };
+    const cuuint64_t ld = u(s.ld) * 2, step = groups > 1 ? u(s.step) * 2 : ld;
+    const cuuint64_t dims[4] = {u(wide ? 64 : s.across ? size : k), u(s.across ? k : size), u(wide ? size / 64 : 1), u(groups)};
+    const cuuint64_t strides[3] = {ld, wide ? 128 : ld, step};
+    const cuuint32_t boxes[4] = {64, (cuuint32_t)(s.across ? kK : box), wide ? (cuuint32_t)box / 64 : 1, 1}, one[4] = {1, 1, 1, 1};
     const Encode f = encoder();
     return f != nullptr &&
-           f(map, dtype == FASGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-             const_cast<void*>(s.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           f(map, dtype == FASGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+             const_cast<void*>(s.p), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -692,9 +719,11 @@ cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
     const int64_t n_tiles = (p.n + kTileN - 1) / kTileN + (p.ragged == kRaggedN ? p.groups : 0);
     t.items = t.m_tiles * n_tiles * t.splits * (p.ragged == kRaggedK ? p.groups : 1);
     if (t.items == 0) return cudaSuccess;
-    t.box_b = p.ragged == kRaggedN ? 32 : kTileN / PAIR;
-    if (!encode(&t.a, p.a, p.dtype, p.m, p.k, p.ragged == kRaggedN ? p.groups : 1, kBlockM) ||
-        !encode(&t.b, p.b, p.dtype, p.n, p.k, 1, t.box_b))
+    t.wide_a = p.a.across && p.m % 64 == 0;
+    t.wide_b = p.b.across && p.n % 64 == 0;
+    if (!encode(&t.a, p.a, p.dtype, p.m, p.k, p.ragged == kRaggedN ? p.groups : 1, kBlockM, t.wide_a) ||
+        !encode(&t.b, p.b, p.dtype, p.n, p.k, 1, kTileN / PAIR, t.wide_b) ||
+        (p.ragged == kRaggedN && !encode(&t.few, p.b, p.dtype, p.n, p.k, 1, kFew, false)))
         return cudaErrorInvalidValue;
     switch (p.ending) {
         case kStore: return launch<PAIR, kStore>(t, t.items, device, sms, stream);
