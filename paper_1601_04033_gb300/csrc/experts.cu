@@ -245,6 +245,7 @@ fasgd::Product by_experts(const Multiply& m) {
     p.ld_out = u.ld_dw;
     p.step_out = u.step_dw;
     p.out_dtype = u.w_dtype;
+    p.exact = u.w_dtype == FASGD_F32;
     return p;
 }
 

@@ -44,6 +44,7 @@ struct Product {
     int64_t ld_out, step_out;
     int64_t step_split;          // from one part of k's result to the next one's (launch_tiles)
     int32_t out_dtype;
+    int32_t exact;               // sums to fp32's accuracy (launch_tiles: the tensor cores' additions cut bits off)
     int32_t add;                 // kStore, fp32: out += instead
     const float* scale;          // kStore: one value, or (by_n) one for each n, whose 0 makes its values 0
     int32_t by_n;

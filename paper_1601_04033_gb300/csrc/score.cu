@@ -240,6 +240,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     const int32_t dtype = u.rows > 0 ? u.dtype : FASGD_F32;      // no rows: no operands to describe
     p.dtype = dtype;
     p.ending = fasgd::kStatistics;
+    p.exact = 1;
     p.labels = u.labels;
     p.classes = u.classes;
     p.parts = s.parts;
@@ -263,6 +264,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         p.n = n;
         p.n0 = v;
         p.ending = fasgd::kResidual;
+        p.exact = 0;
         p.out = s.g;
         p.ld_out = s.ld_g;
         p.out_dtype = u.dtype;

@@ -3,7 +3,7 @@
 // A block, or a pair of blocks (cluster of 2) that shares its MMAs, computes tiles of
 // 128 (256) m by up to 256 n, one after the other: warp 0 copies 64 steps of k of both
 // sides at a time into a ring of stages in shared memory, warp 1 issues the MMAs into one
-// of two accumulators in tensor memory, warps 2 to 5 empty the other one.  A side is
+// of two accumulators in tensor memory, warps 4 to 11 empty the other one.  A side is
 // copied as it lies in memory, k or its own index consecutive (128-byte swizzle either way; the
 // MMA's descriptors say which), so no operand is ever transposed by a pass of its own.
 //
@@ -33,7 +33,9 @@ namespace {
 
 constexpr int kK = 64;                              // steps of k in a stage: 128 bytes
 constexpr int kBlockM = 128;                        // m of a block
-constexpr int kThreads = 192;
+constexpr int kEnds = 8;                            // warps that take results: two for each 32 lanes
+constexpr int kThreads = 128 + 32 * kEnds;          // warps 0 to 3: copies, MMAs, two at rest
+constexpr int kExact = 256;                         // k of an accumulator where the sums are to be exact ones
 constexpr int kSideA = kBlockM * kK * 2;            // bytes of A in a stage
 constexpr int kFew = 32;                             // rows of a box of a short tile
 constexpr int kMaxGroups = FASGD_EXPERTS_MAX;
@@ -167,13 +169,12 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-// 32 columns of the warp's 32 lanes of tensor memory.
+// 32 columns of the warp's 32 lanes of tensor memory, there after wait_columns().
 __device__ __forceinline__ void load_columns(uint32_t from, float (&v)[32]) {
     uint32_t* r = reinterpret_cast<uint32_t*>(v);
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-        "tcgen05.wait::ld.sync.aligned;"
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
           "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
@@ -181,6 +182,16 @@ __device__ __forceinline__ void load_columns(uint32_t from, float (&v)[32]) {
         : "r"(from)
         : "memory");
 }
+__device__ __forceinline__ void load_half(uint32_t from, float (&v)[16]) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(from)
+        : "memory");
+}
+__device__ __forceinline__ void wait_columns() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -204,6 +215,7 @@ struct Tile {
 };
 struct Shared {
     uint64_t full[6], empty[6], ready[2], taken[2], tail;
+    float2 halves[2][kBlockM];          // statistics of the tile's odd columns' half, by tiles in turn
     uint32_t tmem;
     volatile int32_t late;
     int32_t first[kMaxGroups + 1];      // ragged n: the first n tile of each group
@@ -383,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.ready[i], 1);
-            mbar_init(&s.taken[i], 4 * PAIR);
+            mbar_init(&s.taken[i], kEnds * PAIR);
         }
         mbar_init(&s.tail, 1);
         s.late = 0;
@@ -408,7 +420,10 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     const uint32_t tmem = *(volatile uint32_t*)&s.tmem;
     const int64_t items = items_of<PAIR>(t, s), team = blockIdx.x / PAIR, teams = gridDim.x / PAIR;
 
-    if (warp == 0) {
+    // 384 threads are launched with 168 registers; 128 x 56 + 256 x 216 are fewer.
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 0) {
         // Copies.
         uint32_t stage = 0, phase = 0, tails = 0;
         bool ok = true;
@@ -491,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             for (uint32_t i = 0; i < (1u << 24) && global_ns() - t0 < 2000000; ++i) {
             }
         }
-    } else if (warp == 1) {
+        } else if (warp == 1) {
         // MMAs: one thread of the pair's first block issues them (with the whole warp in the loop
         // the tensor cores waited for it: 945 cycles for 64 steps of k instead of 700).
         if (rank == 0 && lane == 0) {
@@ -507,18 +522,24 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 const Tile w = tile_of<PAIR>(t, s, i);
                 if (w.k0 >= w.k1) continue;
                 const uint32_t shape = base | (uint32_t)(width_of<PAIR>(t, w) / 8) << 17;
-                const uint32_t buffer = tile & 1, to = tmem + buffer * kTileN;
-                if (!(ok = wait_thread(&s.taken[buffer], (tile >> 1 & 1) ^ 1, &s.late))) break;
-                fence_after();
                 const int64_t steps = (w.k1 - w.k0 + 15) / 16;      // of 16 k each; 4 to a stage
-                for (int64_t k = 0; k < steps; k += 4) {
+                const int64_t chunk = p.exact ? kExact / 16 : steps;
+                for (int64_t k = 0, next = 0; k < steps; k += 4) {
+                    const bool first = k == next;
+                    if (first) {
+                        if (k > 0) commit<PAIR>(&s.ready[tile++ & 1]);
+                        if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, &s.late))) break;
+                        fence_after();
+                        next += chunk;
+                    }
+                    const uint32_t to = tmem + (tile & 1) * kTileN;
                     const bool zeroed = cut && w.k1 - w.k0 - k * 16 < kK;
                     ok = PAIR == 2 && zeroed ? wait_thread<true>(&s.full[stage], phase, &s.late)
                                              : wait_thread(&s.full[stage], phase, &s.late);
                     if (!ok) break;
                     fence_after();
                     const uint64_t a = a0 + stage * (S::kStage >> 4), b = b0 + stage * (S::kStage >> 4);
-                    mma<PAIR>(to, a, b, shape, k > 0);
+                    mma<PAIR>(to, a, b, shape, !first);
                     if (k + 4 <= steps) {
 #pragma unroll
                         for (int j = 1; j < 4; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, shape, true);
@@ -531,107 +552,55 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                         phase ^= 1;
                     }
                 }
-                if (ok) commit<PAIR>(&s.ready[buffer]);
+                if (ok) commit<PAIR>(&s.ready[tile & 1]);
                 ++tile;
             }
         }
         __syncwarp();
+        }
     } else {
-        // Results.  The warp's lanes of tensor memory are those of its number modulo 4.
-        const int quarter = warp & 3;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        // Results.  The warp's lanes of tensor memory are those of its number modulo 4; two warps share
+        // them, one with the even 32 columns, one with the odd ones.
+        const int quarter = warp & 3, odd = (warp - 4) >> 2;
         const Target target = {p.out, p.ld_out, p.scale, p.factor, p.by_n, p.out_dtype, p.add};
-        if (p.ragged == kRaggedN) clear_rows(p, blockIdx.x, gridDim.x, threadIdx.x - 64, 128);
-        uint32_t tile = 0;
+        if (p.ragged == kRaggedN) clear_rows(p, blockIdx.x, gridDim.x, threadIdx.x - 128, 32 * kEnds);
+        uint32_t tile = 0, turn = 0;
         bool ok = true;
-        for (int64_t i = team; i < items; i += teams) {
+        for (int64_t i = team; i < items; i += teams, turn ^= 1) {
             const Tile w = tile_of<PAIR>(t, s, i);
-            const bool some = w.k0 < w.k1;
-            const uint32_t buffer = tile & 1;
-            if (some) {
-                ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
-                fence_after();
-                ++tile;
-            }
             const int64_t m = w.m0 + rank * kBlockM + quarter * 32 + lane;
             const bool live = m < p.m;
             const int count = (int)(w.n1 - w.n0);
-            const uint32_t from = tmem + buffer * kTileN + ((uint32_t)(quarter * 32) << 16);
-            float v[32];
-            const auto columns = [&](int c) {
-                if (some && ok) {
-                    load_columns(from + c, v);
+            float v[4][32];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
+            const int64_t step = p.exact ? kExact : w.k1 - w.k0;
+            for (int64_t k = w.k0; k < w.k1; k += step) {
+                const uint32_t buffer = tile & 1;
+                ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
+                ++tile;
+                fence_after();
+                if (!ok) break;
+                const uint32_t from = tmem + buffer * kTileN + ((uint32_t)(quarter * 32) << 16) + odd * 32;
+                if (k == w.k0) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        if (b * 64 + odd * 32 < count) load_columns(from + b * 64, v[b]);
+                    wait_columns();
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = ok ? 0.0f : NAN;
-                }
-            };
-            if (ENDING == kStore) {
-                const int64_t base = (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * t.p.step_split + w.n0 * p.ld_out + m;
-                for (int c = 0; c < count; c += 32) {
-                    columns(c);
-                    store_any(target, base + c * target.ld, w.n0 + c, min(32, count - c), live, v);
-                }
-            } else {
-                const int64_t label = live ? p.labels[m] : -1;
-                const bool has = label >= 0 && label < p.classes;
-                const int64_t in = label - p.n0 - w.n0;      // the label's column of this tile
-                const int at = has && in >= 0 && in < count ? (int)in : -1;
-                if (ENDING == kStatistics) {
-                    float top = -INFINITY, sum = 0.0f;
-                    for (int c = 0; c < count; c += 32) {
-                        columns(c);
-                        if (count - c < 32)
+                    for (int b = 0; b < 8; ++b)
+                        if (b / 2 * 64 + odd * 32 < count) {
+                            float more[16];
+                            load_half(from + b / 2 * 64 + b % 2 * 16, more);
+                            wait_columns();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = j < count - c ? v[j] : -INFINITY;
-                        float most = v[0];
-#pragma unroll
-                        for (int j = 1; j < 32; ++j) most = fmaxf(most, v[j]);
-                        most = fmaxf(top, most);
-                        if (__any_sync(0xffffffffu, (uint32_t)(at - c) < 32u)) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j == at - c) p.at_label[m] = v[j];
+                            for (int j = 0; j < 16; ++j) v[b / 2][b % 2 * 16 + j] += more[j];
                         }
-                        const float shift = most == -INFINITY ? 0.0f : most;
-                        float part[4] = {};
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[j] - shift) * kLog2E);
-                        sum = sum * exp2_fast((top - shift) * kLog2E) + ((part[0] + part[1]) + (part[2] + part[3]));
-                        top = most;
-                    }
-                    if (live) p.parts[(p.n0 / kTileN + w.n_tile) * p.m + m] = make_float2(top, sum);
-                } else {
-                    const float lse = has ? p.lse[m] : INFINITY;
-                    const float more = log2f(p.factor);
-                    const int64_t base = w.n0 * p.ld_out + m;
-                    for (int c = 0; c < count; c += 32) {
-                        columns(c);
-                        const bool here = (uint32_t)(at - c) < 32u;
-                        float own = 0.0f;
-                        if (__any_sync(0xffffffffu, here)) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j == at - c) own = p.factor * expm1f(v[j] - lse);
-                        }
-                        const auto write = [&](auto* out) {
-                            using T = std::remove_reference_t<decltype(*out)>;
-                            if (!live) return;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j < count - c) {
-                                    const float g = exp2_fast(fmaf(v[j] - lse, kLog2E, more));
-                                    *out = from_f32<T>(here && j == at - c ? own : g);
-                                    out += target.ld;
-                                }
-                        };
-                        if (target.dtype == FASGD_BF16)
-                            write(static_cast<__nv_bfloat16*>(target.out) + base + c * target.ld);
-                        else
-                            write(static_cast<__half*>(target.out) + base + c * target.ld);
-                    }
                 }
-            }
-            if (some) {
                 fence_before();
                 __syncwarp();
                 if (lane == 0) {
@@ -639,6 +608,91 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                         arrive_first(&s.taken[buffer]);
                     else
                         mbar_arrive(&s.taken[buffer]);
+                }
+            }
+            if (!ok)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[b][j] = NAN;
+            if (ENDING == kStore) {
+                const int64_t base = (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * p.step_split + w.n0 * target.ld + m;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int c = b * 64 + odd * 32;
+                    if (c < count) store_any(target, base + c * target.ld, w.n0 + c, min(32, count - c), live, v[b]);
+                }
+                continue;
+            }
+            const int64_t label = live ? p.labels[m] : -1;
+            const bool has = label >= 0 && label < p.classes;
+            const int64_t in = label - p.n0 - w.n0;      // the label's column of this tile
+            const int at = has && in >= 0 && in < count ? (int)in : -1;
+            const bool mine = at >= 0 && (at >> 5 & 1) == odd;      // v[at / 64][at % 32] is this thread's
+            if (ENDING == kStatistics) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        if (b * 64 + odd * 32 + j >= count) v[b][j] = -INFINITY;
+                        top = fmaxf(top, v[b][j]);
+                    }
+                if (__any_sync(0xffffffffu, mine)) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (mine && at == b * 64 + odd * 32 + j) p.at_label[m] = v[b][j];
+                }
+                const float shift = top == -INFINITY ? 0.0f : top;
+                float part[4] = {};
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[b][j] - shift) * kLog2E);
+                float sum = (part[0] + part[1]) + (part[2] + part[3]);
+                float2* const other = &s.halves[turn][quarter * 32 + lane];
+                if (odd) *other = make_float2(top, sum);
+                asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
+                if (!odd && live) {
+                    const float2 o = *other;
+                    const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
+                    sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
+                    p.parts[(p.n0 / kTileN + w.n_tile) * p.m + m] = make_float2(most, sum);
+                }
+            } else {
+                const float lse = has ? p.lse[m] : INFINITY;
+                const float more = log2f(target.factor);
+                const int64_t base = w.n0 * target.ld + m;
+                float own = 0.0f;
+                if (__any_sync(0xffffffffu, mine)) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (at == b * 64 + odd * 32 + j) own = target.factor * expm1f(v[b][j] - lse);
+                }
+                const auto write = [&](auto* out, int b) {
+                    using T = std::remove_reference_t<decltype(*out)>;
+                    const int c = b * 64 + odd * 32;
+                    out += base + c * target.ld;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < count - c) {
+                            const float g = exp2_fast(fmaf(v[b][j] - lse, kLog2E, more));
+                            *out = from_f32<T>(mine && at == c + j ? own : g);
+                            out += target.ld;
+                        }
+                };
+                if (live) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        if (target.dtype == FASGD_BF16)
+                            write(static_cast<__nv_bfloat16*>(target.out), b);
+                        else
+                            write(static_cast<__half*>(target.out), b);
+                    }
                 }
             }
         }
