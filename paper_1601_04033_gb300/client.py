@@ -391,6 +391,8 @@ def _space(a, workspace, like):
 def route(chosen, experts: int) -> Route:
     """fasgd_route: a router's choices (int32 [..., top]; outside [0, experts): none) into
     the experts' order."""
+    if _fast is not None:
+        return Route(*_done(_fast.route(chosen, experts)))
     _one_device(chosen)
     a = _f.RouteArgs()
     if chosen.dim() == 0:
@@ -456,6 +458,8 @@ def _same_type(t, of):
 
 def gather(x, route: Route, *, out=None):
     """fasgd_gather: x's rows at their places, [rows * top, cols]; 0 at places that no entry has."""
+    if _fast is not None:
+        return _done(_fast.gather(x, tuple(route), out))
     _one_device(x, route.order, route.place, out)
     a = _exchange(x, route)
     _at_rows(a, x)
@@ -472,6 +476,8 @@ def gather(x, route: Route, *, out=None):
 def combine(y, route: Route, weight=None, *, out=None):
     """fasgd_combine: each row's sum over its places in y, times weight (fp32, as the route's
     place) if given: [..., cols]."""
+    if _fast is not None:
+        return _done(_fast.combine(y, tuple(route), weight, out))
     _one_device(y, route.order, route.place, weight, out)
     a = _exchange(y, route, weight)
     a.places, a.ld_places = _at_places(a, y)
@@ -494,6 +500,8 @@ def combine_grad(y, route: Route, weight, dout, *, into: CombineGrads | None = N
     """fasgd_combine_grad: the gradients of ``combine``'s y and weight from that of its result.
     into: where to write them (new tensors where None)."""
     dy, dweight = into if into is not None else (None, None)
+    if _fast is not None:
+        return CombineGrads(*_done(_fast.combine_grad(y, tuple(route), weight, dout, dy, dweight)))
     _one_device(y, route.order, route.place, weight, dout, dy, dweight)
     if weight is None:
         raise ValueError("the gradient of a combination without weights is gather's")
@@ -553,6 +561,8 @@ def multiply(x, w, offsets, *, out=None):
     """fasgd_multiply: rows of x, in their experts' order, times their experts' matrices
     w[e] ([experts, inputs, outputs], rows or columns contiguous; fp32 or x's type); 0
     where no expert has the row.  offsets: ``route``'s."""
+    if _fast is not None:
+        return _done(_fast.multiply(x, w, offsets, out))
     _one_device(x, w, offsets, out)
     a = _products(x, w, offsets)
     given = out
@@ -579,6 +589,8 @@ def multiply_grad(x, w, offsets, dy, *, grads=(True, True), into: MultiplyGrads 
     layout) from that of its result.  grads: which of them; into: where to write them
     (new tensors where None)."""
     dx, dw = into if into is not None else (None, None)
+    if _fast is not None:
+        return MultiplyGrads(*_done(_fast.multiply_grad(x, w, offsets, dy, bool(grads[0]), bool(grads[1]), dx, dw)))
     _one_device(x, w, offsets, dy, dx, dw)
     a = _products(x, w, offsets)
     a.dy, rows, cols, a.ld_dy = _rows(dy)
@@ -626,6 +638,8 @@ def score(z, w, labels, *, upstream=None, grad=True, grads=(True, True), lse=Non
     computed.  into: (dz, dw), where to write them (new tensors where None)."""
     want = (bool(grad and grads[0]), bool(grad and grads[1]))
     dz, dw = into if into is not None else (None, None)
+    if _fast is not None:
+        return Score(*_done(_fast.score(z, w, labels, upstream, *want, lse, dz, dw)))
     _one_device(z, w, labels, upstream, lse, dz, dw)
     a = _f.ScoreArgs()
     a.z, a.rows, a.cols, a.ld_z = _rows(z)

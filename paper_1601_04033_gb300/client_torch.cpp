@@ -16,6 +16,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty_like.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -514,8 +515,414 @@ PyObject* py_balance(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     });
 }
 
+// ---- routed experts and the score over classes ------------------------------------------
+int32_t* ints(const Tensor& t, const char* what) {
+    if (t.scalar_type() != at::kInt || !t.is_contiguous()) wrong(what);
+    return static_cast<int32_t*>(address(t));
+}
+void same_type(const Tensor& t, const Tensor& of) {
+    if (t.scalar_type() != of.scalar_type()) wrong("matrices of one type are expected");
+}
+
+/* A matrix, or several one step apart, whose rows or (flip) columns are consecutive values. */
+struct Matrices {
+    int64_t first, rows, cols, ld, step;
+    int32_t flip;
+    void* p;
+    Matrices(const Tensor& t, int64_t dims) {
+        if (t.dim() != dims) wrong(dims == 2 ? "a matrix is expected" : "[experts, inputs, outputs] is expected");
+        first = t.size(0);
+        rows = t.size(-2);
+        cols = t.size(-1);
+        const int64_t down = t.stride(-2), along = t.stride(-1);
+        if (along == 1 || cols == 1) {
+            flip = 0;
+            ld = down;
+        } else if (down == 1 || rows == 1) {
+            flip = 1;
+            ld = along;
+        } else {
+            wrong("the values of a matrix' rows or columns must be contiguous");
+        }
+        step = dims == 3 ? t.stride(0) : 0;
+        p = address(t);
+    }
+};
+/* A new tensor like t, in its layout (torch's empty_like): dense ones keep their strides. */
+at::Tensor alike(const Tensor& t) { return at::empty_like(t); }
+
+/* route(chosen, experts) -> (offsets, order, place) */
+PyObject* py_route(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return entry(nargs, 2, [&]() -> PyObject* {
+        const Tensor* chosen = tensor(args[0]);
+        if (chosen == nullptr) wrong("a tensor is expected");
+        one_device({chosen});
+        fasgd_route_args a;
+        std::memset(&a, 0, sizeof a);
+        if (chosen->dim() == 0) wrong("chosen must be contiguous int32 on the GPU, [..., top]");
+        a.chosen = ints(*chosen, "chosen must be contiguous int32 on the GPU");
+        a.top = chosen->size(-1);
+        a.rows = a.top != 0 ? chosen->numel() / a.top : 0;
+        a.experts = whole(args[1]);
+        const int64_t size = fasgd_route_workspace(&a);
+        if (size < 0) throw Status{size};
+        New made(*chosen);
+        const int offsets = made.add(a.experts + 1, at::kInt, &a.offsets), order = made.add(chosen->numel(), at::kInt, &a.order),
+                  place = made.add(*chosen, &a.place);
+        made.add(size, at::kByte, &a.workspace);
+        a.workspace_bytes = size;
+        void* s = stream(*chosen);
+        made.make();
+        unlocked([&] { return (int64_t)fasgd_route(&a, s); });
+        return tuple({made.object(offsets), made.object(order), made.object(place)});
+    });
+}
+
+/* A route (offsets, order, place) into a struct of the calls between rows and places. */
+struct Way {
+    const Tensor *order, *place;
+    explicit Way(PyObject* o) {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) wrong("a route is (offsets, order, place)");
+        order = tensor(PyTuple_GET_ITEM(o, 1));
+        place = tensor(PyTuple_GET_ITEM(o, 2));
+        if (order == nullptr || place == nullptr) wrong("a tensor is expected");
+    }
+    void fill(fasgd_exchange_args& a, const Tensor& of, const Tensor* weight) const {
+        std::memset(&a, 0, sizeof a);
+        if (place->dim() == 0) wrong("a route's place is [..., top]");
+        a.top = place->size(-1);
+        a.rows = a.top != 0 ? place->numel() / a.top : 0;
+        a.place = ints(*place, "a route's place must be contiguous int32 on the GPU");
+        a.order = ints(*order, "a route's order must be contiguous int32 on the GPU");
+        if (order->numel() != place->numel()) wrong("a route's order and place have as many entries as each other");
+        a.dtype = dtype_of(of);
+        if (weight != nullptr) {
+            if (weight->scalar_type() != at::kFloat || weight->numel() != place->numel() || !weight->is_contiguous())
+                wrong("weight must be contiguous fp32, one for each entry");
+            a.weight = static_cast<float*>(address(*weight));
+        }
+    }
+};
+void at_rows(fasgd_exchange_args& a, const Tensor& t) {
+    const Matrix m(t);
+    if (m.rows != a.rows || (a.cols != 0 && m.cols != a.cols))
+        wrong("a matrix with a row for each of the route's is expected, as wide as its places");
+    a.cols = m.cols;
+    a.row_values = m.p;
+    a.ld_rows = m.ld;
+}
+Matrix at_places(fasgd_exchange_args& a, const Tensor& t) {
+    const Matrix m(t);
+    if (m.rows != a.rows * a.top || (a.cols != 0 && m.cols != a.cols))
+        wrong("a matrix with a row for each of the route's places is expected, as wide as its rows");
+    a.cols = m.cols;
+    return m;
+}
+
+/* gather(x, route, out) -> out */
+PyObject* py_gather(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return entry(nargs, 3, [&]() -> PyObject* {
+        const Tensor *x = tensor(args[0]), *out = tensor(args[2]);
+        const Way way(args[1]);
+        if (x == nullptr) wrong("a tensor is expected");
+        one_device({x, way.order, way.place, out});
+        fasgd_exchange_args a;
+        way.fill(a, *x, nullptr);
+        at_rows(a, *x);
+        New made(*x);
+        int k = -1;
+        if (out == nullptr) {
+            const int64_t shape[2] = {a.rows * a.top, a.cols};
+            k = made.add(shape, x->scalar_type(), &a.places);
+            a.ld_places = a.cols;
+        } else {
+            same_type(*out, *x);
+            const Matrix m = at_places(a, *out);
+            a.places = m.p;
+            a.ld_places = m.ld;
+        }
+        void* s = stream(*x);
+        made.make();
+        unlocked([&] { return (int64_t)fasgd_gather(&a, s); });
+        return object(made, k, args[2]);
+    });
+}
+
+/* combine(y, route, weight, out) -> out */
+PyObject* py_combine(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return entry(nargs, 4, [&]() -> PyObject* {
+        const Tensor *y = tensor(args[0]), *weight = tensor(args[2]), *out = tensor(args[3]);
+        const Way way(args[1]);
+        if (y == nullptr) wrong("a tensor is expected");
+        one_device({y, way.order, way.place, weight, out});
+        fasgd_exchange_args a;
+        way.fill(a, *y, weight);
+        const Matrix m = at_places(a, *y);
+        a.places = m.p;
+        a.ld_places = m.ld;
+        New made(*y);
+        int k = -1;
+        if (out == nullptr) {
+            c10::SmallVector<int64_t, 5> shape(way.place->sizes().begin(), way.place->sizes().end());
+            shape.back() = a.cols;
+            k = made.add(shape, y->scalar_type(), &a.row_values);
+            a.ld_rows = a.cols;
+        } else {
+            same_type(*out, *y);
+            at_rows(a, *out);
+        }
+        void* s = stream(*y);
+        made.make();
+        unlocked([&] { return (int64_t)fasgd_combine(&a, s); });
+        return object(made, k, args[3]);
+    });
+}
+
+/* combine_grad(y, route, weight, dout, dy, dweight) -> (dy, dweight) */
+PyObject* py_combine_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return entry(nargs, 6, [&]() -> PyObject* {
+        const Tensor *y = tensor(args[0]), *weight = tensor(args[2]), *dout = tensor(args[3]), *dy = tensor(args[4]),
+                     *dweight = tensor(args[5]);
+        const Way way(args[1]);
+        if (y == nullptr || dout == nullptr) wrong("a tensor is expected");
+        one_device({y, way.order, way.place, weight, dout, dy, dweight});
+        if (weight == nullptr) wrong("the gradient of a combination without weights is gather's");
+        fasgd_exchange_args a;
+        way.fill(a, *y, weight);
+        const Matrix m = at_places(a, *y);
+        a.places = m.p;
+        a.ld_places = m.ld;
+        same_type(*dout, *y);
+        at_rows(a, *dout);
+        New made(*y);
+        int at_dy = -1, at_dweight = -1;
+        if (dy == nullptr) {
+            const int64_t shape[2] = {a.rows * a.top, a.cols};
+            at_dy = made.add(shape, y->scalar_type(), &a.dplaces);
+            a.ld_dplaces = a.cols;
+        } else {
+            same_type(*dy, *y);
+            const Matrix d = at_places(a, *dy);
+            a.dplaces = d.p;
+            a.ld_dplaces = d.ld;
+        }
+        if (dweight == nullptr) {
+            at_dweight = made.add(*weight, &a.dweight);
+        } else {
+            if (dweight->scalar_type() != at::kFloat || dweight->numel() != weight->numel() || !dweight->is_contiguous())
+                wrong("the weights' gradient must be as the weights");
+            a.dweight = static_cast<float*>(address(*dweight));
+        }
+        void* s = stream(*y);
+        made.make();
+        unlocked([&] { return (int64_t)fasgd_combine_grad(&a, s); });
+        return tuple({object(made, at_dy, args[4]), object(made, at_dweight, args[5])});
+    });
+}
+
+/* The struct of the experts' products without results. */
+void products(fasgd_multiply_args& a, const Tensor& x, const Tensor& w, const Tensor& offsets) {
+    std::memset(&a, 0, sizeof a);
+    const Matrix m(x);
+    a.x = m.p;
+    a.rows = m.rows;
+    a.inputs = m.cols;
+    a.ld_x = m.ld;
+    a.dtype = dtype_of(x);
+    const Matrices e(w, 3);
+    a.w = e.p;
+    a.experts = e.first;
+    a.outputs = e.cols;
+    a.ld_w = e.ld;
+    a.step_w = e.step;
+    a.w_flip = e.flip;
+    if (e.rows != a.inputs) wrong("w is [experts, x's columns, outputs]");
+    if (w.scalar_type() != at::kFloat && w.scalar_type() != x.scalar_type()) wrong("w is of fp32 or of x's type");
+    a.w_dtype = dtype_of(w);
+    a.offsets = ints(offsets, "offsets must be contiguous int32 on the GPU");
+    if (offsets.numel() != a.experts + 1) wrong("offsets has one entry more than there are experts");
+}
+
+/* multiply(x, w, offsets, out) -> out */
+PyObject* py_multiply(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return entry(nargs, 4, [&]() -> PyObject* {
+        const Tensor *x = tensor(args[0]), *w = tensor(args[1]), *offsets = tensor(args[2]), *out = tensor(args[3]);
+        if (x == nullptr || w == nullptr || offsets == nullptr) wrong("a tensor is expected");
+        one_device({x, w, offsets, out});
+        fasgd_multiply_args a;
+        products(a, *x, *w, *offsets);
+        New made(*x);
+        int k = -1;
+        if (out == nullptr) {
+            c10::SmallVector<int64_t, 5> shape(x->sizes().begin(), x->sizes().end());
+            shape.back() = a.outputs;
+            k = made.add(shape, x->scalar_type(), &a.y);
+            a.ld_y = a.outputs;
+            a.y = reinterpret_cast<void*>(256);
+        } else {
+            same_type(*out, *x);
+            const Matrix m(*out);
+            if (m.rows != a.rows || m.cols != a.outputs) wrong("out is [x's rows, w's outputs]");
+            a.y = m.p;
+            a.ld_y = m.ld;
+        }
+        void* s = stream(*x);
+        const int64_t size = fasgd_multiply_workspace(&a);
+        if (size < 0) throw Status{size};
+        if (size > 0) made.add(size, at::kByte, &a.workspace);
+        a.workspace_bytes = size;
+        made.make();
+        unlocked([&] { return (int64_t)fasgd_multiply(&a, s); });
+        return object(made, k, args[3]);
+    });
+}
+
+/* A result that is laid out like `of`: the caller's (given), or a new tensor. */
+struct Alike {
+    Tensor own;
+    PyObject* given;
+    const Tensor& take(PyObject* o, const Tensor* t, const Tensor& of, const char* what) {
+        given = o;
+        if (t == nullptr) {
+            own = alike(of);
+            return own;
+        }
+        same_type(*t, of);
+        if (t->sizes() != of.sizes()) wrong(what);
+        return *t;
+    }
+    PyObject* object(const New& made) const { return own.defined() ? THPVariable_Wrap(own) : ::object(made, -1, given); }
+};
+
+/* multiply_grad(x, w, offsets, dy, whether dx, whether dw, dx, dw) -> (dx, dw) */
+PyObject* py_multiply_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return entry(nargs, 8, [&]() -> PyObject* {
+        const Tensor *x = tensor(args[0]), *w = tensor(args[1]), *offsets = tensor(args[2]), *dy = tensor(args[3]),
+                     *dx = tensor(args[6]), *dw = tensor(args[7]);
+        if (x == nullptr || w == nullptr || offsets == nullptr || dy == nullptr) wrong("a tensor is expected");
+        one_device({x, w, offsets, dy, dx, dw});
+        fasgd_multiply_args a;
+        products(a, *x, *w, *offsets);
+        const Matrix d(*dy);
+        same_type(*dy, *x);
+        if (d.rows != a.rows || d.cols != a.outputs) wrong("dy is [x's rows, w's outputs]");
+        a.dy = d.p;
+        a.ld_dy = d.ld;
+        const bool by_x = args[4] == Py_True, by_w = args[5] == Py_True;
+        if ((dx != nullptr && !by_x) || (dw != nullptr && !by_w)) wrong("a place for a gradient that is not wanted");
+        New made(*x);
+        int at_dx = -1;
+        Alike of_w;
+        of_w.given = Py_None;
+        if (by_x && dx == nullptr) {
+            at_dx = made.add(*x, &a.dx);
+            a.ld_dx = a.inputs;
+            a.dx = reinterpret_cast<void*>(256);
+        } else if (by_x) {
+            same_type(*dx, *x);
+            const Matrix m(*dx);
+            if (m.rows != a.rows || m.cols != a.inputs) wrong("x's gradient is as x");
+            a.dx = m.p;
+            a.ld_dx = m.ld;
+        }
+        if (by_w) {
+            const Matrices m(of_w.take(args[7], dw, *w, "w's gradient is as w"), 3);
+            a.dw = m.p;
+            a.ld_dw = m.ld;
+            a.step_dw = m.step;
+            a.dw_flip = m.flip;
+        }
+        void* s = stream(*x);
+        const int64_t size = by_x || by_w ? fasgd_multiply_workspace(&a) : 0;
+        if (size < 0) throw Status{size};
+        if (size > 0) made.add(size, at::kByte, &a.workspace);
+        a.workspace_bytes = size;
+        made.make();
+        unlocked([&] { return (int64_t)fasgd_multiply_grad(&a, s); });
+        return tuple({object(made, at_dx, args[6]), of_w.object(made)});
+    });
+}
+
+/* score(z, w, labels, upstream, whether dz, whether dw, lse, dz, dw) -> (loss, rows, dz, dw, lse) */
+PyObject* py_score(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return entry(nargs, 9, [&]() -> PyObject* {
+        const Tensor *z = tensor(args[0]), *w = tensor(args[1]), *labels = tensor(args[2]), *up = tensor(args[3]),
+                     *lse = tensor(args[6]), *dz = tensor(args[7]), *dw = tensor(args[8]);
+        if (z == nullptr || w == nullptr || labels == nullptr) wrong("a tensor is expected");
+        one_device({z, w, labels, up, lse, dz, dw});
+        fasgd_score_args a;
+        std::memset(&a, 0, sizeof a);
+        const Matrix m(*z);
+        a.z = m.p;
+        a.rows = m.rows;
+        a.cols = m.cols;
+        a.ld_z = m.ld;
+        a.dtype = dtype_of(*z);
+        const Matrices e(*w, 2);
+        a.w = e.p;
+        a.classes = e.cols;
+        a.ld_w = e.ld;
+        a.w_flip = e.flip;
+        same_type(*w, *z);
+        if (e.rows != a.cols) wrong("w is [z's columns, classes]");
+        if (labels->scalar_type() != at::kLong || !labels->is_contiguous() || labels->numel() != a.rows)
+            wrong("labels must be contiguous int64 on the GPU, one for each row");
+        a.labels = static_cast<int64_t*>(address(*labels));
+        if (up != nullptr) {
+            if (up->scalar_type() != at::kFloat || up->numel() != 1) wrong("upstream must be one fp32 value on the GPU");
+            a.upstream = static_cast<float*>(address(*up));
+        }
+        const bool by_z = args[4] == Py_True, by_w = args[5] == Py_True;
+        if ((dz != nullptr && !by_z) || (dw != nullptr && !by_w)) wrong("a place for a gradient that is not wanted");
+        New made(*z);
+        int at_dz = -1, at_loss = -1, at_rows = -1, at_lse = -1;
+        Alike of_w;
+        of_w.given = Py_None;
+        if (by_z && dz == nullptr) {
+            at_dz = made.add(*z, &a.dz);
+            a.ld_dz = a.cols;
+            a.dz = reinterpret_cast<void*>(256);
+        } else if (by_z) {
+            same_type(*dz, *z);
+            const Matrix d(*dz);
+            if (d.rows != a.rows || d.cols != a.cols) wrong("z's gradient is as z");
+            a.dz = d.p;
+            a.ld_dz = d.ld;
+        }
+        if (by_w) {
+            const Matrices d(of_w.take(args[8], dw, *w, "w's gradient is as w"), 2);
+            a.dw = d.p;
+            a.ld_dw = d.ld;
+            a.dw_flip = d.flip;
+        }
+        if (lse == nullptr) {
+            at_loss = made.add(1, at::kFloat, &a.loss);
+            at_rows = made.add(labels->sizes(), at::kFloat, &a.row_loss);
+            at_lse = made.add(labels->sizes(), at::kFloat, &a.lse);
+            a.loss = a.row_loss = a.lse = reinterpret_cast<float*>(256);
+        } else {
+            if (lse->scalar_type() != at::kFloat || lse->numel() != a.rows || !lse->is_contiguous())
+                wrong("lse must be contiguous fp32, one for each row");
+            a.lse = static_cast<float*>(address(*lse));
+            a.known = 1;
+        }
+        void* s = stream(*z);
+        const int64_t size = fasgd_score_workspace(&a);
+        if (size < 0) throw Status{size};
+        made.add(size, at::kByte, &a.workspace);
+        a.workspace_bytes = size;
+        made.make();
+        unlocked([&] { return (int64_t)fasgd_score(&a, s); });
+        PyObject* known = args[6];
+        if (lse != nullptr) Py_INCREF(known);
+        return tuple({object(made, at_loss, Py_None), object(made, at_rows, Py_None), object(made, at_dz, args[7]),
+                      of_w.object(made), lse != nullptr ? known : made.object(at_lse)});
+    });
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(dropout), METHOD(join), METHOD(join_grad), METHOD(balance), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {METHOD(dropout), METHOD(join), METHOD(join_grad), METHOD(balance), METHOD(route), METHOD(gather),
+                         METHOD(combine), METHOD(combine_grad), METHOD(multiply), METHOD(multiply_grad), METHOD(score), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_client", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -34,7 +34,7 @@ namespace {
 constexpr int kK = 64;                              // steps of k in a stage: 128 bytes
 constexpr int kBlockM = 128;                        // m of a block
 constexpr int kEnds = 8;                            // warps that take results: two for each 32 lanes
-constexpr int kThreads = 128 + 32 * kEnds;          // warps 0 to 3: copies, MMAs, two at rest
+constexpr int kThreads = 128 + 32 * kEnds;          // warps 0 to 3: copies, MMAs, groups' last rows, one at rest
 constexpr int kExact = 256;                         // k of an accumulator where the sums are to be exact ones
 constexpr int kSideA = kBlockM * kK * 2;            // bytes of A in a stage
 constexpr int kFew = 32;                             // rows of a box of a short tile
@@ -118,11 +118,8 @@ __device__ __forceinline__ void arrive_first(uint64_t* bar) {
     else
         asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
 }
-__device__ __forceinline__ void arrive_first_expect(uint64_t* bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(
-                     first_block(smem_addr(bar))),
-                 "r"(bytes)
-                 : "memory");
+__device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes) {     // in either block
+    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 // A box at (x, y, z, g) to shared memory; bar: an address in this block's or (PAIR 2) its pair's.
 template <int PAIR>
@@ -142,16 +139,19 @@ __device__ __forceinline__ void copy_box(const CUtensorMap* map, uint32_t to, ui
             : "memory");
 }
 template <int PAIR>
-__device__ __forceinline__ void mma(uint32_t to, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+__device__ __forceinline__ void mma(uint32_t to, uint32_t a_low, uint32_t b_low, uint32_t a_high, uint32_t b_high, uint32_t shape,
+                                    bool add) {
     if (PAIR == 2)
         asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(to),
-            "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+            "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.u32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %6};\n"
+            " tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(to),
+            "r"(a_low), "r"(b_low), "r"(shape), "r"((uint32_t)add), "r"(a_high), "r"(b_high)
             : "memory");
     else
         asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(to),
-            "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+            "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.u32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %6};\n"
+            " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(to),
+            "r"(a_low), "r"(b_low), "r"(shape), "r"((uint32_t)add), "r"(a_high), "r"(b_high)
             : "memory");
 }
 // The barrier (of both blocks of a pair) is arrived at once all MMAs before this have ended.
@@ -191,6 +191,12 @@ __device__ __forceinline__ void load_half(uint32_t from, float (&v)[16]) {
         : "r"(from)
         : "memory");
 }
+// One thread of a converged warp.
+__device__ __forceinline__ bool elected() {
+    uint32_t is;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(is));
+    return is != 0;
+}
 __device__ __forceinline__ void wait_columns() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -214,7 +220,7 @@ struct Tile {
     int64_t n_tile;
 };
 struct Shared {
-    uint64_t full[6], empty[6], ready[2], taken[2], tail;
+    uint64_t full[6], empty[6], tail[6], ready[2], taken[2];
     float2 halves[2][kBlockM];          // statistics of the tile's odd columns' half, by tiles in turn
     uint32_t tmem;
     volatile int32_t late;
@@ -304,6 +310,27 @@ __device__ __forceinline__ int width_of(const TileArgs& t, const Tile& w) {
     const int step = PAIR == 2 && t.p.b.across ? 128 : 16 * PAIR;
     return (int)(w.n1 - w.n0 + step - 1) / step * step;
 }
+// What a block copies of B in a stage: one box, or for a short tile of a group and for sides of
+// odd widths several.
+struct Boxes {
+    int rows_b, boxes_b;
+    bool few;
+    uint32_t bytes;      // of A too
+};
+template <int PAIR>
+__device__ __forceinline__ Boxes boxes_of(const TileArgs& t, const Tile& w) {
+    Boxes x;
+    x.rows_b = width_of<PAIR>(t, w) / PAIR;
+    x.few = t.p.ragged == kRaggedN && x.rows_b <= 64 * (3 - PAIR);
+    const int step = x.few ? kFew : t.p.b.across && !t.wide_b ? 64 : kTileN / PAIR;
+    x.boxes_b = (x.rows_b + step - 1) / step;
+    x.bytes = kSideA + x.boxes_b * step * kK * 2;
+    return x;
+}
+// The copy at k holds rows of the next group.
+__device__ __forceinline__ bool cut(const Product& p, const Tile& w, int64_t k) {
+    return p.ragged == kRaggedK && w.k1 - k < kK;
+}
 template <int PAIR>
 __device__ __forceinline__ int64_t items_of(const TileArgs& t, const Shared& s) {
     return t.p.ragged == kRaggedN ? (int64_t)s.first[t.p.groups] * t.m_tiles * t.splits : t.items;
@@ -392,12 +419,12 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(&s.full[i], PAIR);
             mbar_init(&s.empty[i], 1);
+            mbar_init(&s.tail[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.ready[i], 1);
             mbar_init(&s.taken[i], kEnds * PAIR);
         }
-        mbar_init(&s.tail, 1);
         s.late = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -424,67 +451,73 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 0) {
-        // Copies.
-        uint32_t stage = 0, phase = 0, tails = 0;
-        bool ok = true;
-        for (int64_t i = team; i < items && ok; i += teams) {
-            const Tile w = tile_of<PAIR>(t, s, i);
-            const int rows_b = width_of<PAIR>(t, w) / PAIR;
-            const int64_t m0 = w.m0 + rank * kBlockM, n0 = w.n0 + (int64_t)rank * rows_b;
-            const int boxes_a = p.a.across && !t.wide_a ? kBlockM / 64 : 1;
-            // B: one box, or for a short tile of a group and for sides of odd widths several.
-            const bool few = p.ragged == kRaggedN && rows_b <= 64 * (3 - PAIR);
-            const int step_b = few ? kFew : p.b.across && !t.wide_b ? 64 : kTileN / PAIR;
-            const int boxes_b = (rows_b + step_b - 1) / step_b;
-            const uint32_t bytes = kSideA + boxes_b * step_b * kK * 2;
-            const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
-            for (int64_t k = w.k0; k < w.k1; k += kK) {
-                if (!(ok = wait(&s.empty[stage], phase ^ 1, &s.late))) break;
-                const bool tail = p.ragged == kRaggedK && w.k1 - k < kK;
-                char* const at = ring + stage * S::kStage;
-                if (lane == 0) {
-                    uint32_t bar;
-                    if (tail) {
-                        mbar_arrive_expect_tx(&s.tail, bytes);
-                        bar = smem_addr(&s.tail);
-                    } else {
-                        if (PAIR == 2) {
-                            arrive_first_expect(&s.full[stage], bytes);
-                            bar = first_block(smem_addr(&s.full[stage]));
-                        } else {
-                            mbar_arrive_expect_tx(&s.full[stage], bytes);
-                            bar = smem_addr(&s.full[stage]);
+            // Copies, by one thread.
+            if (elected()) {
+                const uint32_t to = smem_addr(ring);
+                const uint32_t full = PAIR == 2 ? first_block(smem_addr(&s.full[0])) : smem_addr(&s.full[0]);
+                uint32_t stage = 0, phase = 0;
+                bool ok = true;
+                for (int64_t i = team; i < items && ok; i += teams) {
+                    const Tile w = tile_of<PAIR>(t, s, i);
+                    const Boxes x = boxes_of<PAIR>(t, w);
+                    const int32_t m0 = (int32_t)(w.m0 + rank * kBlockM), n0 = (int32_t)(w.n0 + (int64_t)rank * x.rows_b);
+                    const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
+                    for (int64_t k64 = w.k0; k64 < w.k1; k64 += kK) {
+                        const int32_t k = (int32_t)k64;
+                        if (!(ok = wait_thread(&s.empty[stage], phase ^ 1, &s.late))) break;
+                        const uint32_t bar = cut(p, w, k64) ? smem_addr(&s.tail[stage]) : full + 8 * stage;
+                        const uint32_t to_a = to + stage * S::kStage, to_b = to_a + kSideA;
+                        arrive_expect(bar, x.bytes);
+                        if (!p.a.across)
+                            copy_box<PAIR>(&t.a, to_a, bar, k, m0, 0, ga);
+                        else if (t.wide_a)
+                            copy_box<PAIR>(&t.a, to_a, bar, 0, k, m0 / 64, ga);
+                        else
+                            for (int j = 0; j < kBlockM / 64; ++j)
+                                copy_box<PAIR>(&t.a, to_a + j * 8192, bar, m0 + j * 64, k, 0, ga);
+                        if (x.few)
+                            for (int j = 0; j < x.boxes_b; ++j)
+                                copy_box<PAIR>(&t.few, to_b + j * kFew * kK * 2, bar, k, n0 + j * kFew, 0, 0);
+                        else if (!p.b.across)
+                            copy_box<PAIR>(&t.b, to_b, bar, k, n0, 0, 0);
+                        else if (t.wide_b)
+                            copy_box<PAIR>(&t.b, to_b, bar, 0, k, n0 / 64, 0);
+                        else
+                            for (int j = 0; j < x.boxes_b; ++j)
+                                copy_box<PAIR>(&t.b, to_b + j * 8192, bar, n0 + j * 64, k, 0, 0);
+                        if (++stage == S::kStages) {
+                            stage = 0;
+                            phase ^= 1;
                         }
                     }
-                    const uint32_t to_a = smem_addr(at), to_b = to_a + kSideA;
-                    if (!p.a.across)
-                        copy_box<PAIR>(&t.a, to_a, bar, (int32_t)k, (int32_t)m0, 0, ga);
-                    else if (t.wide_a)
-                        copy_box<PAIR>(&t.a, to_a, bar, 0, (int32_t)k, (int32_t)(m0 / 64), ga);
-                    else
-                        for (int j = 0; j < boxes_a; ++j)
-                            copy_box<PAIR>(&t.a, to_a + j * 8192, bar, (int32_t)m0 + j * 64, (int32_t)k, 0, ga);
-                    if (few)
-                        for (int j = 0; j < boxes_b; ++j)
-                            copy_box<PAIR>(&t.few, to_b + j * kFew * kK * 2, bar, (int32_t)k, (int32_t)n0 + j * kFew, 0, 0);
-                    else if (!p.b.across)
-                        copy_box<PAIR>(&t.b, to_b, bar, (int32_t)k, (int32_t)n0, 0, 0);
-                    else if (t.wide_b)
-                        copy_box<PAIR>(&t.b, to_b, bar, 0, (int32_t)k, (int32_t)(n0 / 64), 0);
-                    else
-                        for (int j = 0; j < boxes_b; ++j)
-                            copy_box<PAIR>(&t.b, to_b + j * 8192, bar, (int32_t)n0 + j * 64, (int32_t)k, 0, 0);
                 }
-                __syncwarp();
-                if (tail) {
-                    // Rows of other groups become 0 (both sides are across: a row is 128 bytes of each chunk).
-                    if (!(ok = wait(&s.tail, tails & 1, &s.late))) break;
-                    ++tails;
-                    const int rows = (int)(w.k1 - k), chunks = (int)(bytes / 8192);
+                if (!ok) {      // copies in flight end within this
+                    const uint64_t t0 = global_ns();
+                    for (uint32_t i = 0; i < (1u << 24) && global_ns() - t0 < 2000000; ++i) {
+                    }
+                }
+            }
+            __syncwarp();
+        } else if (warp == 2) {
+            // Ragged k: in a group's last copy, rows of other groups become 0 (both sides are across: a
+            // row is 128 bytes of each chunk).
+            if (p.ragged == kRaggedK) {
+                uint32_t copies = 0, used = 0;
+                bool ok = true;
+                for (int64_t i = team; i < items && ok; i += teams) {
+                    const Tile w = tile_of<PAIR>(t, s, i);
+                    if (w.k0 >= w.k1) continue;
+                    copies += (uint32_t)((w.k1 - w.k0 + kK - 1) / kK);
+                    const int rows = (int)((w.k1 - w.k0) % kK);
+                    if (rows == 0) continue;
+                    const uint32_t stage = (copies - 1) % S::kStages;
+                    if (!(ok = wait(&s.tail[stage], used >> stage & 1, &s.late))) break;
+                    used ^= 1u << stage;
+                    const int chunks = (int)(boxes_of<PAIR>(t, w).bytes / 8192);
+                    char* const at = ring + stage * S::kStage;
                     for (int j = lane; j < chunks * (kK - rows) * 8; j += 32) {
                         const int c = j / ((kK - rows) * 8), r = j % ((kK - rows) * 8);
-                        char* chunk = at + c * 8192;
-                        *reinterpret_cast<float4*>(chunk + rows * 128 + r * 16) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        *reinterpret_cast<float4*>(at + c * 8192 + rows * 128 + r * 16) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -495,65 +528,68 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                             mbar_arrive(&s.full[stage]);
                     }
                 }
-                if (++stage == S::kStages) {
-                    stage = 0;
-                    phase ^= 1;
-                }
             }
-        }
-        if (!ok) {      // copies in flight end within this
-            const uint64_t t0 = global_ns();
-            for (uint32_t i = 0; i < (1u << 24) && global_ns() - t0 < 2000000; ++i) {
-            }
-        }
         } else if (warp == 1) {
-        // MMAs: one thread of the pair's first block issues them (with the whole warp in the loop
-        // the tensor cores waited for it: 945 cycles for 64 steps of k instead of 700).
-        if (rank == 0 && lane == 0) {
+        // MMAs: one thread of the pair's first block issues them.  It is elected, so that the compiler
+        // knows that it is one, and counts in 32 bits: by `lane == 0` and in 64 bits the tensor cores
+        // waited for it (1,530 TFLOP/s for 1,760 at 8,192 of m, n and k).
+        if (rank == 0 && elected()) {
             uint32_t stage = 0, phase = 0, tile = 0;
             const uint32_t kind = p.dtype == FASGD_BF16 ? 1u << 7 | 1u << 10 : 0u;
             const uint32_t base = 1u << 4 | kind | (uint32_t)(p.a.across != 0) << 15 | (uint32_t)(p.b.across != 0) << 16 |
                                   (uint32_t)(kBlockM * PAIR / 16) << 24;
             const uint32_t next_a = p.a.across ? 2048 >> 4 : 32 >> 4, next_b = p.b.across ? 2048 >> 4 : 32 >> 4;
             const uint64_t a0 = matrix_of(smem_addr(ring), p.a.across), b0 = matrix_of(smem_addr(ring) + kSideA, p.b.across);
-            const bool cut = p.ragged == kRaggedK;
-            bool ok = true;
-            for (int64_t i = team; i < items && ok; i += teams) {
-                const Tile w = tile_of<PAIR>(t, s, i);
-                if (w.k0 >= w.k1) continue;
-                const uint32_t shape = base | (uint32_t)(width_of<PAIR>(t, w) / 8) << 17;
-                const int64_t steps = (w.k1 - w.k0 + 15) / 16;      // of 16 k each; 4 to a stage
-                const int64_t chunk = p.exact ? kExact / 16 : steps;
-                for (int64_t k = 0, next = 0; k < steps; k += 4) {
-                    const bool first = k == next;
-                    if (first) {
-                        if (k > 0) commit<PAIR>(&s.ready[tile++ & 1]);
-                        if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, &s.late))) break;
-                        fence_after();
-                        next += chunk;
-                    }
-                    const uint32_t to = tmem + (tile & 1) * kTileN;
-                    const bool zeroed = cut && w.k1 - w.k0 - k * 16 < kK;
-                    ok = PAIR == 2 && zeroed ? wait_thread<true>(&s.full[stage], phase, &s.late)
-                                             : wait_thread(&s.full[stage], phase, &s.late);
-                    if (!ok) break;
-                    fence_after();
-                    const uint64_t a = a0 + stage * (S::kStage >> 4), b = b0 + stage * (S::kStage >> 4);
-                    mma<PAIR>(to, a, b, shape, !first);
-                    if (k + 4 <= steps) {
-#pragma unroll
-                        for (int j = 1; j < 4; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, shape, true);
-                    } else {
-                        for (int j = 1; j < (int)(steps - k); ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, shape, true);
-                    }
-                    commit<PAIR>(&s.empty[stage]);
-                    if (++stage == S::kStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
+            const uint32_t a_high = (uint32_t)(a0 >> 32), b_high = (uint32_t)(b0 >> 32);
+            // The next tile with sums and the next accumulator are looked up while MMAs run.
+            int64_t i = team - teams;
+            int steps = 0;                            // of 16 k each; 4 to a stage
+            uint32_t shape = 0;
+            bool zeroed = false, ok = true;           // zeroed: the tile's last stage holds rows set to 0
+            const auto look = [&] {
+                steps = 0;
+                while (steps == 0 && (i += teams) < items) {
+                    const Tile w = tile_of<PAIR>(t, s, i);
+                    steps = w.k0 < w.k1 ? (int)((w.k1 - w.k0 + 15) / 16) : 0;
+                    shape = base | (uint32_t)(width_of<PAIR>(t, w) / 8) << 17;
+                    zeroed = p.ragged == kRaggedK && (w.k1 - w.k0) % kK != 0;
                 }
-                if (ok) commit<PAIR>(&s.ready[tile & 1]);
-                ++tile;
+            };
+            look();
+            while (steps > 0 && ok) {
+                const int end = steps, chunk = p.exact ? kExact / 16 : end;
+                const uint32_t now = shape;
+                const bool cuts = zeroed;
+                for (int done = 0; done < end && ok; done += chunk) {
+                    const int until = min(done + chunk, end);
+                    if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, &s.late))) break;
+                    fence_after();
+                    const uint32_t to = tmem + (tile & 1) * kTileN;
+                    uint32_t add = 0;
+                    for (int k = done; k < until; k += 4) {
+                        ok = PAIR == 2 && cuts && k + 4 >= end ? wait_thread<true>(&s.full[stage], phase, &s.late)
+                                                               : wait_thread(&s.full[stage], phase, &s.late);
+                        if (!ok) break;
+                        fence_after();
+                        const uint32_t a = (uint32_t)a0 + stage * (S::kStage >> 4), b = (uint32_t)b0 + stage * (S::kStage >> 4);
+                        mma<PAIR>(to, a, b, a_high, b_high, now, add);
+                        add = 1;
+                        if (k + 4 <= until) {
+#pragma unroll
+                            for (int j = 1; j < 4; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
+                        } else {
+                            for (int j = 1; j < until - k; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
+                        }
+                        commit<PAIR>(&s.empty[stage]);
+                        if (++stage == S::kStages) {
+                            stage = 0;
+                            phase ^= 1;
+                        }
+                    }
+                    if (ok) commit<PAIR>(&s.ready[tile & 1]);
+                    ++tile;
+                    if (done == 0) look();
+                }
             }
         }
         __syncwarp();
