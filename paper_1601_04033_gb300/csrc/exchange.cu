@@ -45,10 +45,21 @@ __global__ void __launch_bounds__(256) gather_kernel(ExchangeArgs a) {
     if (!own<N>(a, t, c)) return;
     const Pack<T, N> v = load<T, N>(a.row_values, t * a.ld_rows + c);
     const Pack<T, N> zero = {};
-    for (int64_t k = t * a.top; k < (t + 1) * a.top; ++k) {
-        const int32_t i = a.place[k];
-        if (there(i, a.n)) store(a.places, i * a.ld_places + c, v);
-        if (!there(a.order[k], a.n)) store(a.places, k * a.ld_places + c, zero);
+    // Eight entries at a time, so that their places are read together.
+    for (int64_t k0 = t * a.top; k0 < (t + 1) * a.top; k0 += 8) {
+        const int most = (int)min((int64_t)8, (t + 1) * a.top - k0);
+        int32_t place[8];
+        bool empty[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            place[k] = k < most ? __ldg(a.place + k0 + k) : -1;
+            empty[k] = k < most && !there(__ldg(a.order + k0 + k), a.n);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (there(place[k], a.n)) store(a.places, place[k] * a.ld_places + c, v);
+            if (empty[k]) store(a.places, (k0 + k) * a.ld_places + c, zero);
+        }
     }
 }
 
@@ -65,7 +76,7 @@ __global__ void __launch_bounds__(256) combine_kernel(ExchangeArgs a) {
         bool has[kAtOnce];
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
-            const int32_t i = k < most ? a.place[k0 + k] : -1;
+            const int32_t i = k < most ? __ldg(a.place + k0 + k) : -1;
             has[k] = there(i, a.n);
             if (has[k]) {
                 v[k] = load<T, N>(a.places, i * a.ld_places + c);
@@ -87,7 +98,7 @@ __global__ void __launch_bounds__(256) combine_kernel(ExchangeArgs a) {
 // A team of `TEAM` threads for each row; the dot products of kAtOnce places at a time.
 template <class T, int N, int TEAM>
 __global__ void __launch_bounds__(256) combine_grad_kernel(ExchangeArgs a) {
-    constexpr int kAtOnce = 4, kTeams = 256 / TEAM, kWarps = TEAM / 32;
+    constexpr int kAtOnce = 8, kTeams = 256 / TEAM, kWarps = TEAM / 32;
     __shared__ float part[kTeams][kWarps][kAtOnce];
     const int team = threadIdx.x / TEAM, me = threadIdx.x % TEAM;
     const int64_t t = (int64_t)blockIdx.x * kTeams + team;
@@ -102,10 +113,10 @@ __global__ void __launch_bounds__(256) combine_grad_kernel(ExchangeArgs a) {
         for (int k = 0; k < kAtOnce; ++k) {
             const int64_t e = t * a.top + k0 + k;
             const bool is = live && k0 + k < a.top;
-            at[k] = is ? a.place[e] : -1;
+            at[k] = is ? __ldg(a.place + e) : -1;
             if (!there(at[k], a.n)) at[k] = -1;
-            w[k] = at[k] >= 0 ? a.weight[e] : 0.0f;
-            empty[k] = is && !there(a.order[e], a.n);
+            w[k] = at[k] >= 0 ? __ldg(a.weight + e) : 0.0f;
+            empty[k] = is && !there(__ldg(a.order + e), a.n);
         }
         for (int64_t c = (int64_t)me * N; live && c < a.cols; c += TEAM * N) {
             const Pack<T, N> d = load<T, N>(a.row_values, t * a.ld_rows + c);
@@ -154,7 +165,8 @@ template <class T, int N>
 cudaError_t launch(const ExchangeArgs& a, ExchangeKind kind, cudaStream_t stream) {
     const int64_t packs = (a.cols + N - 1) / N;
     if (kind == kCombineGrad) {
-        if (packs <= 64) {
+        // A warp for each row needs no barriers; few and wide rows want more threads.
+        if (packs <= 64 || a.rows >= 2048) {
             combine_grad_kernel<T, N, 32><<<(unsigned)((a.rows + 7) / 8), 256, 0, stream>>>(a);
         } else {
             combine_grad_kernel<T, N, 256><<<(unsigned)a.rows, 256, 0, stream>>>(a);

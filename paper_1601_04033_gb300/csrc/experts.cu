@@ -92,6 +92,8 @@ struct Multiply {
     // Copies in the workspace (null: the argument itself serves), and the steps of what is read.
     void *w_copy, *x_copy, *dy_copy;
     int64_t w_ld, w_step, x_ld, dy_ld;
+    bool planes;                // fp32 by planes on the tensor cores
+    int64_t w_plane, x_plane, dy_plane;
     const void* w() const { return w_copy != nullptr ? w_copy : u.w; }
     const void* x() const { return x_copy != nullptr ? x_copy : u.x; }
     const void* dy() const { return dy_copy != nullptr ? dy_copy : u.dy; }
@@ -145,24 +147,30 @@ int64_t lay_out(Multiply& m, char* base) {
     m.x_ld = u.ld_x;
     m.dy_ld = u.ld_dy;
     m.w_copy = m.x_copy = m.dy_copy = nullptr;
-    // The tensor cores' operands start and step on 16 bytes.
+    // The tensor cores' operands start and step on 16 bytes; fp32 ones are copied to planes, where
+    // the products are large enough for the copies.
+    m.planes = u.dtype == FASGD_F32 && fasgd::by_planes(u.rows, u.outputs, u.inputs);
     const bool tiles = u.dtype != FASGD_F32;
     const auto fits = [&](const void* p, int64_t ld, int64_t step, int64_t groups) {
-        return !tiles || fasgd::tile_side({p, ld, step, 0}, groups);
+        return !m.planes && (!tiles || fasgd::tile_side({p, ld, step, 0, 0}, groups));
+    };
+    const auto copy = [&](int64_t values, int64_t& plane) {
+        plane = values;
+        return take(m.planes ? 6 * values : values * m.size);
     };
     if ((!m.grad || u.dx != nullptr) && (u.w_dtype != u.dtype || !fits(u.w, u.ld_w, u.step_w, u.experts))) {
         const int64_t rows = u.w_flip ? u.outputs : u.inputs, cols = u.w_flip ? u.inputs : u.outputs;
         m.w_ld = (cols + 7) / 8 * 8;
         m.w_step = rows * m.w_ld;
-        m.w_copy = take(u.experts * m.w_step * m.size);
+        m.w_copy = copy(u.experts * m.w_step, m.w_plane);
     }
     if ((!m.grad || u.dw != nullptr) && !fits(u.x, u.ld_x, 0, 1)) {
         m.x_ld = (u.inputs + 7) / 8 * 8;
-        m.x_copy = take(u.rows * m.x_ld * m.size);
+        m.x_copy = copy(u.rows * m.x_ld, m.x_plane);
     }
     if (m.grad && !fits(u.dy, u.ld_dy, 0, 1)) {
         m.dy_ld = (u.outputs + 7) / 8 * 8;
-        m.dy_copy = take(u.rows * m.dy_ld * m.size);
+        m.dy_copy = copy(u.rows * m.dy_ld, m.dy_plane);
     }
     return at;
 }
@@ -188,11 +196,12 @@ cudaError_t copy_w(const Multiply& m, cudaStream_t stream) {
     p.groups = (int32_t)u.experts;
     p.dtype_from = u.w_dtype;
     p.dtype_to = u.dtype;
+    p.plane = m.planes ? m.w_plane : 0;
     p.offsets = u.offsets;
     return fasgd::launch_pack(p, stream);
 }
 
-cudaError_t copy_rows(const Multiply& m, const void* from, int64_t ld, int64_t cols, void* to, int64_t ld_to,
+cudaError_t copy_rows(const Multiply& m, const void* from, int64_t ld, int64_t cols, void* to, int64_t ld_to, int64_t plane,
                       cudaStream_t stream) {
     if (to == nullptr) return cudaSuccess;
     fasgd::Pack p = {};
@@ -204,6 +213,7 @@ cudaError_t copy_rows(const Multiply& m, const void* from, int64_t ld, int64_t c
     p.ld_to = ld_to;
     p.groups = 1;
     p.dtype_from = p.dtype_to = m.u.dtype;
+    p.plane = m.planes ? plane : 0;
     return fasgd::launch_pack(p, stream);
 }
 
@@ -211,18 +221,18 @@ fasgd::Product product(const Multiply& m) {
     fasgd::Product p = {};
     p.groups = (int32_t)m.u.experts;
     p.offsets = m.u.offsets;
-    p.dtype = m.u.dtype;
+    p.dtype = m.planes ? FASGD_BF16 : m.u.dtype;
+    p.planes = p.exact = m.planes;
     p.ending = fasgd::kStore;
     p.out_dtype = m.u.dtype;
     p.factor = 1.0f;
     return p;
 }
 // y (or dx) by rows: `to` columns from `from`, w's side across or not.
-fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across, const void* x, int64_t ld_x, void* y,
-                       int64_t ld_y) {
+fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across, const fasgd::Side& x, void* y, int64_t ld_y) {
     fasgd::Product p = product(m);
-    p.a = {m.w(), m.w_ld, m.w_step, across};
-    p.b = {x, ld_x, 0, 0};
+    p.a = {m.w(), m.w_ld, m.w_step, across, m.w_plane};
+    p.b = x;
     p.m = to;
     p.n = m.u.rows;
     p.k = from;
@@ -234,7 +244,7 @@ fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across,
 fasgd::Product by_experts(const Multiply& m) {
     const fasgd_multiply_args& u = m.u;
     fasgd::Product p = product(m);
-    const fasgd::Side x = {m.x(), m.x_ld, 0, 1}, dy = {m.dy(), m.dy_ld, 0, 1};
+    const fasgd::Side x = {m.x(), m.x_ld, 0, 1, m.x_plane}, dy = {m.dy(), m.dy_ld, 0, 1, m.dy_plane};
     p.a = u.dw_flip ? x : dy;
     p.b = u.dw_flip ? dy : x;
     p.m = u.dw_flip ? u.inputs : u.outputs;
@@ -245,7 +255,7 @@ fasgd::Product by_experts(const Multiply& m) {
     p.ld_out = u.ld_dw;
     p.step_out = u.step_dw;
     p.out_dtype = u.w_dtype;
-    p.exact = u.w_dtype == FASGD_F32;
+    p.exact = u.w_dtype == FASGD_F32;      // (a sum that is stored in 16 bits loses less than its rounding)
     return p;
 }
 
@@ -344,9 +354,9 @@ int fasgd_multiply(const fasgd_multiply_args* u, void* stream_) {
     if (int rc = check_multiply_shared(call, m)) return rc;
     if (u->rows == 0) return FASGD_OK;
     cudaError_t st = copy_w(m, stream);
-    if (st == cudaSuccess) st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, stream);
+    if (st == cudaSuccess) st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, m.x_plane, stream);
     if (st == cudaSuccess)
-        st = fasgd::launch_product(by_rows(m, u->inputs, u->outputs, !u->w_flip, m.x(), m.x_ld, m.u.y, m.u.ld_y), stream);
+        st = fasgd::launch_product(by_rows(m, u->inputs, u->outputs, !u->w_flip, {m.x(), m.x_ld, 0, 0, m.x_plane}, m.u.y, m.u.ld_y), stream);
     return cuda_status(st, call);
 }
 
@@ -361,16 +371,17 @@ int fasgd_multiply_grad(const fasgd_multiply_args* u, void* stream_) {
     if (int rc = check_multiply_shared(call, m)) return rc;
     if (u->rows == 0) {      // no rows: no operands to copy or to describe
         m.u.dtype = FASGD_F32;
+        m.planes = false;
         return cuda_status(u->dw != nullptr ? fasgd::launch_product(by_experts(m), stream) : cudaSuccess, call);
     }
-    cudaError_t st = copy_rows(m, m.u.dy, m.u.ld_dy, u->outputs, m.dy_copy, m.dy_ld, stream);
+    cudaError_t st = copy_rows(m, m.u.dy, m.u.ld_dy, u->outputs, m.dy_copy, m.dy_ld, m.dy_plane, stream);
     if (st == cudaSuccess && u->dx != nullptr) {
         st = copy_w(m, stream);
         if (st == cudaSuccess)
-            st = fasgd::launch_product(by_rows(m, u->outputs, u->inputs, u->w_flip, m.dy(), m.dy_ld, m.u.dx, m.u.ld_dx), stream);
+            st = fasgd::launch_product(by_rows(m, u->outputs, u->inputs, u->w_flip, {m.dy(), m.dy_ld, 0, 0, m.dy_plane}, m.u.dx, m.u.ld_dx), stream);
     }
     if (st == cudaSuccess && u->dw != nullptr) {
-        st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, stream);
+        st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, m.x_plane, stream);
         if (st == cudaSuccess) st = fasgd::launch_product(by_experts(m), stream);
     }
     return cuda_status(st, call);

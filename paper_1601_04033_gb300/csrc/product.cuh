@@ -7,6 +7,7 @@
 // warp, which hold consecutive m, write consecutive memory whatever the product.
 #pragma once
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -18,6 +19,7 @@ struct Side {
     const void* p;
     int64_t ld, step;
     int32_t across;
+    int64_t plane;      // fp32 values as three bf16 ones: from one of them to the next (launch_tiles)
 };
 
 enum Ragged {
@@ -43,6 +45,8 @@ struct Product {
     void* out;
     int64_t ld_out, step_out;
     int64_t step_split;          // from one part of k's result to the next one's (launch_tiles)
+    int64_t step_plane;          // kResidual of planes: from one to the next
+    int32_t planes;              // the sides are fp32 values as three planes of dtype FASGD_BF16
     int32_t out_dtype;
     int32_t exact;               // sums to fp32's accuracy (launch_tiles: the tensor cores' additions cut bits off)
     int32_t add;                 // kStore, fp32: out += instead
@@ -62,16 +66,31 @@ constexpr int kPlainN = 64;
 cudaError_t launch_plain(const Product& p, cudaStream_t stream);
 
 // 16-bit types on the tensor cores, for sides that start and step on 16 bytes.  kTileN: the n of a tile.
+//
+// fp32 values take part as three bf16 ones each (rounded, then what is left, twice: x = x0 + x1 + x2 to
+// 2^-27), in the six products of them that reach 2^-26:
+// x2 y0, x0 y2, x1 y1, x1 y0, x0 y1, x0 y0.
 constexpr int kTileN = 256;
+constexpr int kPairs = 6;
+constexpr double kPlanesFrom = 1 << 28;
+__host__ __device__ constexpr uint32_t plane_a(uint32_t pair) { return 0x001102u >> 4 * pair & 15u; }
+__host__ __device__ constexpr uint32_t plane_b(uint32_t pair) { return 0x010120u >> 4 * pair & 15u; }
 bool tile_side(const Side& s, int64_t groups);
 cudaError_t launch_tiles(const Product& p, cudaStream_t stream);
-// 16-bit types take the tensor cores (their callers lay the sides out for them), fp32 the plain form.
+// Whether an fp32 product of m x n x k goes by planes: the plain form does some 10 TFLOP/s, the planes
+// some 250, after copies and a launch or two more.
+inline bool by_planes(int64_t m, int64_t n, int64_t k) {
+    return (double)m * (double)n * (double)k >= kPlanesFrom;
+}
+// What is of fp32 still when it gets here takes the plain form; its callers copy sides of large fp32
+// products to planes, and lay out 16-bit ones for the tensor cores.
 inline cudaError_t launch_product(const Product& p, cudaStream_t stream) {
     return p.dtype == 0 ? launch_plain(p, stream) : launch_tiles(p, stream);
 }
 
 // A copy of a side with rows that lie as the fast kernels want them: `rows` rows of `cols`
-// values (of group g: p + g * step) to rows ld_to apart, cast to dtype_to.  What it leaves
+// values (of group g: p + g * step) to rows ld_to apart (a multiple of 8, as step_to and plane; what is
+// between the rows is overwritten), of the same type or rounded from fp32.  What it leaves
 // out is not read: groups without rows by offsets (null: none is left out), and rows
 // without a label (labels null: none; its copy is 0).
 struct Pack {
@@ -79,11 +98,24 @@ struct Pack {
     void* to;
     int64_t rows, cols, ld_from, step_from, ld_to, step_to;
     int32_t groups, dtype_from, dtype_to;
+    int64_t plane;               // fp32 to FASGD_BF16 in three planes this far apart; 0: one value each
     const int32_t* offsets;
     const int64_t* labels;
     int64_t classes;
 };
 cudaError_t launch_pack(const Pack& p, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// The planes of an fp32 value.  A value that would round to infinity in bf16 is cut instead; what is
+// not finite is its first plane alone.
+__device__ __forceinline__ void planes_of(float x, __nv_bfloat16 (&to)[3]) {
+    const bool finite = fabsf(x) <= 3.4028234e38f;
+    to[0] = __float2bfloat16_rn(fabsf(x) < 3.38e38f || !finite ? x : __uint_as_float(__float_as_uint(x) & 0xffff0000u));
+    const float rest = finite ? x - __bfloat162float(to[0]) : 0.0f;
+    to[1] = __float2bfloat16_rn(rest);
+    to[2] = __float2bfloat16_rn(rest - __bfloat162float(to[1]));
+}
+#endif
 
 // Group g's rows, cut to [0, n).
 struct Bounds {

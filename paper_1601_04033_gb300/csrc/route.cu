@@ -8,8 +8,8 @@
 // chunks and earlier warps; a second sweep hands the places out the same way.
 //
 // Short lists (128 rows of a minibatch) take one block and one launch.  Longer ones take
-// two: each block of the second adds up the counters of all chunks itself, at most 256
-// chunks (0.25 MB out of L2), which costs less than a third launch.
+// two: each block of the second adds up the counters of all chunks itself, at most 64
+// chunks (with 256 of them the sums took 40 of 65 us), which costs less than a third launch.
 
 #include <algorithm>
 
@@ -21,8 +21,8 @@ namespace {
 
 constexpr int kManyWarps = 32, kFewWarps = 8;
 constexpr int kManyExperts = 320;        // experts that 32 warps have counters for in 40 KB
-constexpr int64_t kChunk = 2048;         // entries of a block where there are several
-constexpr int kChunks = 256;
+constexpr int64_t kChunk = 4096;         // entries of a block where there are several
+constexpr int kChunks = 64;
 
 int warps_of(int32_t experts) { return experts <= kManyExperts ? kManyWarps : kFewWarps; }
 
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(1024) count_kernel(RouteArgs a) {
 }
 
 __global__ void __launch_bounds__(1024) place_kernel(RouteArgs a) {
-    extern __shared__ int32_t counters[];      // [warps][experts], then [experts] first places
+    extern __shared__ int32_t counters[];      // [warps][experts], then first and before
     __shared__ int32_t total;
     const int warps = blockDim.x / 32;
     int32_t* first = counters + warps * a.experts;
@@ -116,24 +116,29 @@ __global__ void __launch_bounds__(1024) place_kernel(RouteArgs a) {
     count(a.chosen, begin, end, a.experts, mine);
     __syncthreads();
     if (a.chunks > 1) pdl_wait();
-    // first[e]: all entries of e; then where e begins.  before: e's entries of earlier chunks.
+    // first[e]: all entries of e, then where e begins; before[e]: its entries of earlier chunks.
+    int32_t* before = first + a.experts;
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
-        int32_t sum = 0;
+        int32_t sum = 0, mine_before = 0;
         if (a.chunks == 1) {
             for (int w = 0; w < warps; ++w) sum += counters[w * a.experts + e];
         } else {
-#pragma unroll 8
-            for (int c = 0; c < a.chunks; ++c) sum += a.part_counts[(int64_t)c * a.experts + e];
+#pragma unroll 16
+            for (int c = 0; c < a.chunks; ++c) {
+                const int32_t k = a.part_counts[(int64_t)c * a.experts + e];
+                sum += k;
+                mine_before += c < (int)blockIdx.x ? k : 0;
+            }
         }
         first[e] = sum;
+        before[e] = mine_before;
     }
     __syncthreads();
     const int32_t all = scan(first, a.experts, &total);
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
         int32_t at = first[e];
         if (blockIdx.x == 0) a.offsets[e] = at;
-#pragma unroll 8
-        for (int c = 0; c < (int)blockIdx.x; ++c) at += a.part_counts[(int64_t)c * a.experts + e];
+        at += before[e];
         for (int w = 0; w < warps; ++w) {
             const int32_t k = counters[w * a.experts + e];
             counters[w * a.experts + e] = at;
@@ -161,16 +166,16 @@ void route_chunks(int64_t n, int32_t experts, int32_t& chunks, int64_t& chunk) {
 }
 
 cudaError_t launch_route(const RouteArgs& a, cudaStream_t stream) {
-    const int warps = a.chunks > 1 ? kFewWarps : std::max(1, std::min(warps_of(a.experts), (int)((a.n + 31) / 32)));
+    const int warps = std::max(1, (int)std::min<int64_t>(warps_of(a.experts), (a.n + 31) / 32));
     const size_t smem = sizeof(int32_t) * warps * a.experts;
     if (a.chunks == 1) {
-        place_kernel<<<1, warps * 32, smem + sizeof(int32_t) * a.experts, stream>>>(a);
+        place_kernel<<<1, warps * 32, smem + 2 * sizeof(int32_t) * a.experts, stream>>>(a);
         return cudaGetLastError();
     }
     count_kernel<<<a.chunks, warps * 32, smem, stream>>>(a);
     cudaError_t st = cudaGetLastError();
     if (st != cudaSuccess) return st;
-    return launch_pdl(place_kernel, dim3(a.chunks), dim3(warps * 32), smem + sizeof(int32_t) * a.experts, stream, a);
+    return launch_pdl(place_kernel, dim3(a.chunks), dim3(warps * 32), smem + 2 * sizeof(int32_t) * a.experts, stream, a);
 }
 
 }  // namespace fasgd

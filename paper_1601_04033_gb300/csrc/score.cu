@@ -27,6 +27,8 @@ struct Score {
     fasgd_score_args u;
     int64_t size, tile;
     bool grad;
+    bool planes;                 // fp32 by planes on the tensor cores
+    int64_t plane_z, plane_w, plane_g;
     // workspace
     void* z_copy;                // rows x ld_zc (null: z itself serves)
     int64_t ld_zc;
@@ -162,7 +164,8 @@ int64_t lay_out(Score& s, char* base) {
         at += (bytes + 255) / 256 * 256;
         return p;
     };
-    s.tile = u.dtype == FASGD_F32 ? fasgd::kPlainN : fasgd::kTileN;
+    s.planes = u.dtype == FASGD_F32 && fasgd::by_planes(u.rows, u.classes, u.cols);
+    s.tile = u.dtype == FASGD_F32 && !s.planes ? fasgd::kPlainN : fasgd::kTileN;
     const int64_t tiles = (u.classes + s.tile - 1) / s.tile;
     if (!u.known) {
         s.parts = reinterpret_cast<float2*>(take(8 * tiles * u.rows));
@@ -174,23 +177,31 @@ int64_t lay_out(Score& s, char* base) {
     s.z_copy = s.w_copy = nullptr;
     s.ld_zc = u.ld_z;
     s.ld_wc = u.ld_w;
-    if (s.grad || (u.dtype != FASGD_F32 && !fasgd::tile_side({u.z, u.ld_z, 0, 0}, 1))) {
+    const auto fits = [&](const void* p, int64_t ld) {
+        return !s.planes && (u.dtype == FASGD_F32 || fasgd::tile_side({p, ld, 0, 0, 0}, 1));
+    };
+    const auto copy = [&](int64_t values, int64_t& plane) {
+        plane = values;
+        return take(s.planes ? 6 * values : values * s.size);
+    };
+    if (s.grad || !fits(u.z, u.ld_z)) {
         s.ld_zc = (u.cols + 7) / 8 * 8;
-        s.z_copy = take(u.rows * s.ld_zc * s.size);
+        s.z_copy = copy(u.rows * s.ld_zc, s.plane_z);
     }
-    if (u.dtype != FASGD_F32 && !fasgd::tile_side({u.w, u.ld_w, 0, 0}, 1)) {
+    if (!fits(u.w, u.ld_w)) {
         s.ld_wc = ((u.w_flip ? u.cols : u.classes) + 7) / 8 * 8;
-        s.w_copy = take((u.w_flip ? u.classes : u.cols) * s.ld_wc * s.size);
+        s.w_copy = copy((u.w_flip ? u.classes : u.cols) * s.ld_wc, s.plane_w);
     }
     if (!s.grad) return at;
     s.share = reinterpret_cast<float*>(take(4));
     s.row_scale = reinterpret_cast<float*>(take(4 * u.rows));
     s.ld_g = (u.rows + 7) / 8 * 8;
-    const int64_t most = std::max<int64_t>(64, FASGD_SCORE_PIECE / std::max<int64_t>(1, s.ld_g * s.size));
+    const int64_t g_size = s.planes ? 6 : s.size;
+    const int64_t most = std::max<int64_t>(64, FASGD_SCORE_PIECE / std::max<int64_t>(1, s.ld_g * g_size));
     const int64_t pieces = (u.classes + most - 1) / most;
     s.piece = (u.classes + pieces - 1) / pieces;
     if (pieces > 1) s.piece = std::min(s.piece / 64 * 64 + 64, most / 64 * 64);
-    s.g = take(s.piece * s.ld_g * s.size);
+    s.g = copy(s.piece * s.ld_g, s.plane_g);
     if (u.dz != nullptr && s.piece < u.classes) s.dz_sum = reinterpret_cast<float*>(take(4 * u.rows * u.cols));
     return at;
 }
@@ -216,6 +227,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         c.cols = u.w_flip ? u.cols : u.classes;
         c.ld_from = u.ld_w;
         c.ld_to = s.ld_wc;
+        c.plane = s.planes ? s.plane_w : 0;
         if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
         w_all = s.w_copy;
     }
@@ -226,21 +238,23 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         c.cols = u.cols;
         c.ld_from = u.ld_z;
         c.ld_to = s.ld_zc;
+        c.plane = s.planes ? s.plane_z : 0;
         c.labels = u.labels;
         c.classes = u.classes;
         if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
         z = s.z_copy;
     }
     Product p = {};
-    p.a = {z, ld_z, 0, 0};
-    p.b = {w_all, ld_w, 0, !u.w_flip};
+    p.a = {z, ld_z, 0, 0, s.plane_z};
+    p.b = {w_all, ld_w, 0, !u.w_flip, s.plane_w};
     p.m = u.rows;
     p.n = u.classes;
     p.k = u.cols;
-    const int32_t dtype = u.rows > 0 ? u.dtype : FASGD_F32;      // no rows: no operands to describe
+    const int32_t dtype = u.rows > 0 && s.planes ? FASGD_BF16 : u.rows > 0 ? u.dtype : FASGD_F32;      // no rows: no operands to describe
     p.dtype = dtype;
+    p.planes = s.planes;
     p.ending = fasgd::kStatistics;
-    p.exact = 1;
+    p.exact = 1;      // the log-sum-exps and losses are fp32
     p.labels = u.labels;
     p.classes = u.classes;
     p.parts = s.parts;
@@ -259,12 +273,13 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     const float factor = u.dtype == FASGD_F16 ? 16384.0f : 1.0f;
     for (int64_t v = 0; v < u.classes; v += s.piece) {
         const int64_t n = std::min(s.piece, u.classes - v);
-        const void* w = at_class(w_all, ld_w, u.w_flip, v, s.size);
+        const void* w = at_class(w_all, ld_w, u.w_flip, v, s.planes ? 2 : s.size);
         p.b.p = w;
         p.n = n;
         p.n0 = v;
         p.ending = fasgd::kResidual;
-        p.exact = 0;
+        p.exact = s.planes;
+        p.step_plane = s.plane_g;
         p.out = s.g;
         p.ld_out = s.ld_g;
         p.out_dtype = u.dtype;
@@ -273,11 +288,12 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         if (st != cudaSuccess) return st;
         Product q = {};
         q.dtype = dtype;
+        q.planes = q.exact = s.planes;
         q.ending = fasgd::kStore;
         q.factor = 1.0f / factor;
         if (u.dz != nullptr && u.rows > 0) {
-            q.a = {w, ld_w, 0, u.w_flip};
-            q.b = {s.g, s.ld_g, 0, 1};
+            q.a = {w, ld_w, 0, u.w_flip, s.plane_w};
+            q.b = {s.g, s.ld_g, 0, 1, s.plane_g};
             q.m = u.cols;
             q.n = u.rows;
             q.k = n;
@@ -298,7 +314,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
             if (st != cudaSuccess) return st;
         }
         if (u.dw != nullptr) {
-            const fasgd::Side zs = {z, ld_z, 0, 1}, gs = {s.g, s.ld_g, 0, 0};
+            const fasgd::Side zs = {z, ld_z, 0, 1, s.plane_z}, gs = {s.g, s.ld_g, 0, 0, s.plane_g};
             q.a = u.dw_flip ? zs : gs;
             q.b = u.dw_flip ? gs : zs;
             q.m = u.dw_flip ? u.cols : n;

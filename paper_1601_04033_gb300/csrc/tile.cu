@@ -121,21 +121,21 @@ __device__ __forceinline__ void arrive_first(uint64_t* bar) {
 __device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes) {     // in either block
     asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// A box at (x, y, z, g) to shared memory; bar: an address in this block's or (PAIR 2) its pair's.
+// A box at (x, y, z, g) of a plane to shared memory; bar: an address in this block's or (PAIR 2) its pair's.
 template <int PAIR>
 __device__ __forceinline__ void copy_box(const CUtensorMap* map, uint32_t to, uint32_t bar, int32_t x, int32_t y, int32_t z,
-                                         int32_t g) {
+                                         int32_t g, int32_t plane) {
     if (PAIR == 2)
         asm volatile(
-            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, "
-            "%5, %6}], [%2];" ::"r"(to),
-            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(g)
+            "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, "
+            "%5, %6, %7}], [%2];" ::"r"(to),
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(g), "r"(plane)
             : "memory");
     else
         asm volatile(
-            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], "
-            "[%2];" ::"r"(to),
-            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(g)
+            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, "
+            "%7}], [%2];" ::"r"(to),
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(g), "r"(plane)
             : "memory");
 }
 template <int PAIR>
@@ -445,6 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     }
     fence_after();
     const uint32_t tmem = *(volatile uint32_t*)&s.tmem;
+    const uint32_t pairs = p.planes ? kPairs : 1;
     const int64_t items = items_of<PAIR>(t, s), team = blockIdx.x / PAIR, teams = gridDim.x / PAIR;
 
     // 384 threads are launched with 168 registers; 128 x 56 + 256 x 216 are fewer.
@@ -462,32 +463,35 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     const Boxes x = boxes_of<PAIR>(t, w);
                     const int32_t m0 = (int32_t)(w.m0 + rank * kBlockM), n0 = (int32_t)(w.n0 + (int64_t)rank * x.rows_b);
                     const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
-                    for (int64_t k64 = w.k0; k64 < w.k1; k64 += kK) {
-                        const int32_t k = (int32_t)k64;
-                        if (!(ok = wait_thread(&s.empty[stage], phase ^ 1, &s.late))) break;
-                        const uint32_t bar = cut(p, w, k64) ? smem_addr(&s.tail[stage]) : full + 8 * stage;
-                        const uint32_t to_a = to + stage * S::kStage, to_b = to_a + kSideA;
-                        arrive_expect(bar, x.bytes);
-                        if (!p.a.across)
-                            copy_box<PAIR>(&t.a, to_a, bar, k, m0, 0, ga);
-                        else if (t.wide_a)
-                            copy_box<PAIR>(&t.a, to_a, bar, 0, k, m0 / 64, ga);
-                        else
-                            for (int j = 0; j < kBlockM / 64; ++j)
-                                copy_box<PAIR>(&t.a, to_a + j * 8192, bar, m0 + j * 64, k, 0, ga);
-                        if (x.few)
-                            for (int j = 0; j < x.boxes_b; ++j)
-                                copy_box<PAIR>(&t.few, to_b + j * kFew * kK * 2, bar, k, n0 + j * kFew, 0, 0);
-                        else if (!p.b.across)
-                            copy_box<PAIR>(&t.b, to_b, bar, k, n0, 0, 0);
-                        else if (t.wide_b)
-                            copy_box<PAIR>(&t.b, to_b, bar, 0, k, n0 / 64, 0);
-                        else
-                            for (int j = 0; j < x.boxes_b; ++j)
-                                copy_box<PAIR>(&t.b, to_b + j * 8192, bar, n0 + j * 64, k, 0, 0);
-                        if (++stage == S::kStages) {
-                            stage = 0;
-                            phase ^= 1;
+                    for (uint32_t pair = 0; pair < pairs && ok; ++pair) {
+                        const int32_t pa = pairs > 1 ? plane_a(pair) : 0, pb = pairs > 1 ? plane_b(pair) : 0;
+                        for (int64_t k64 = w.k0; k64 < w.k1; k64 += kK) {
+                            const int32_t k = (int32_t)k64;
+                            if (!(ok = wait_thread(&s.empty[stage], phase ^ 1, &s.late))) break;
+                            const uint32_t bar = cut(p, w, k64) ? smem_addr(&s.tail[stage]) : full + 8 * stage;
+                            const uint32_t to_a = to + stage * S::kStage, to_b = to_a + kSideA;
+                            arrive_expect(bar, x.bytes);
+                            if (!p.a.across)
+                                copy_box<PAIR>(&t.a, to_a, bar, k, m0, 0, ga, pa);
+                            else if (t.wide_a)
+                                copy_box<PAIR>(&t.a, to_a, bar, 0, k, m0 / 64, ga, pa);
+                            else
+                                for (int j = 0; j < kBlockM / 64; ++j)
+                                    copy_box<PAIR>(&t.a, to_a + j * 8192, bar, m0 + j * 64, k, 0, ga, pa);
+                            if (x.few)
+                                for (int j = 0; j < x.boxes_b; ++j)
+                                    copy_box<PAIR>(&t.few, to_b + j * kFew * kK * 2, bar, k, n0 + j * kFew, 0, 0, pb);
+                            else if (!p.b.across)
+                                copy_box<PAIR>(&t.b, to_b, bar, k, n0, 0, 0, pb);
+                            else if (t.wide_b)
+                                copy_box<PAIR>(&t.b, to_b, bar, 0, k, n0 / 64, 0, pb);
+                            else
+                                for (int j = 0; j < x.boxes_b; ++j)
+                                    copy_box<PAIR>(&t.b, to_b + j * 8192, bar, n0 + j * 64, k, 0, 0, pb);
+                            if (++stage == S::kStages) {
+                                stage = 0;
+                                phase ^= 1;
+                            }
                         }
                     }
                 }
@@ -502,30 +506,31 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             // Ragged k: in a group's last copy, rows of other groups become 0 (both sides are across: a
             // row is 128 bytes of each chunk).
             if (p.ragged == kRaggedK) {
-                uint32_t copies = 0, used = 0;
+                uint32_t copies = 0, used = 0;      // copies: modulo the stages
                 bool ok = true;
                 for (int64_t i = team; i < items && ok; i += teams) {
                     const Tile w = tile_of<PAIR>(t, s, i);
-                    if (w.k0 >= w.k1) continue;
-                    copies += (uint32_t)((w.k1 - w.k0 + kK - 1) / kK);
                     const int rows = (int)((w.k1 - w.k0) % kK);
-                    if (rows == 0) continue;
-                    const uint32_t stage = (copies - 1) % S::kStages;
-                    if (!(ok = wait(&s.tail[stage], used >> stage & 1, &s.late))) break;
-                    used ^= 1u << stage;
-                    const int chunks = (int)(boxes_of<PAIR>(t, w).bytes / 8192);
-                    char* const at = ring + stage * S::kStage;
-                    for (int j = lane; j < chunks * (kK - rows) * 8; j += 32) {
-                        const int c = j / ((kK - rows) * 8), r = j % ((kK - rows) * 8);
-                        *reinterpret_cast<float4*>(at + c * 8192 + rows * 128 + r * 16) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (PAIR == 2)
-                            arrive_first<true>(&s.full[stage]);
-                        else
-                            mbar_arrive(&s.full[stage]);
+                    for (uint32_t pair = 0; pair < pairs && w.k0 < w.k1 && ok; ++pair) {
+                        copies = (uint32_t)((copies + (w.k1 - w.k0 + kK - 1) / kK) % S::kStages);
+                        if (rows == 0) continue;
+                        const uint32_t stage = (copies + S::kStages - 1) % S::kStages;
+                        if (!(ok = wait(&s.tail[stage], used >> stage & 1, &s.late))) break;
+                        used ^= 1u << stage;
+                        const int chunks = (int)(boxes_of<PAIR>(t, w).bytes / 8192);
+                        char* const at = ring + stage * S::kStage;
+                        for (int j = lane; j < chunks * (kK - rows) * 8; j += 32) {
+                            const int c = j / ((kK - rows) * 8), r = j % ((kK - rows) * 8);
+                            *reinterpret_cast<float4*>(at + c * 8192 + rows * 128 + r * 16) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (PAIR == 2)
+                                arrive_first<true>(&s.full[stage]);
+                            else
+                                mbar_arrive(&s.full[stage]);
+                        }
                     }
                 }
             }
@@ -543,42 +548,47 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const uint32_t a_high = (uint32_t)(a0 >> 32), b_high = (uint32_t)(b0 >> 32);
             // The next tile with sums and the next accumulator are looked up while MMAs run.
             int64_t i = team - teams;
-            int steps = 0;                            // of 16 k each; 4 to a stage
+            int blocks = 0, last = 0;                 // of 64 k each, of every pair of planes; MMAs of the last one
             uint32_t shape = 0;
-            bool zeroed = false, ok = true;           // zeroed: the tile's last stage holds rows set to 0
+            bool zeroed = false, ok = true;           // zeroed: that holds rows set to 0
             const auto look = [&] {
-                steps = 0;
-                while (steps == 0 && (i += teams) < items) {
+                blocks = 0;
+                while (blocks == 0 && (i += teams) < items) {
                     const Tile w = tile_of<PAIR>(t, s, i);
-                    steps = w.k0 < w.k1 ? (int)((w.k1 - w.k0 + 15) / 16) : 0;
+                    if (w.k0 >= w.k1) continue;
+                    blocks = (int)((w.k1 - w.k0 + kK - 1) / kK);
+                    last = (int)((w.k1 - w.k0 + 15) / 16) - (blocks - 1) * (kK / 16);
                     shape = base | (uint32_t)(width_of<PAIR>(t, w) / 8) << 17;
                     zeroed = p.ragged == kRaggedK && (w.k1 - w.k0) % kK != 0;
                 }
             };
             look();
-            while (steps > 0 && ok) {
-                const int end = steps, chunk = p.exact ? kExact / 16 : end;
+            while (blocks > 0 && ok) {
+                const int each = blocks, all = each * (int)pairs, chunk = p.exact ? kExact / kK : all, mmas = last;
                 const uint32_t now = shape;
                 const bool cuts = zeroed;
-                for (int done = 0; done < end && ok; done += chunk) {
-                    const int until = min(done + chunk, end);
+                int in = 0;                           // blocks of this pair of planes
+                for (int done = 0; done < all && ok; done += chunk) {
+                    const int until = min(done + chunk, all);
                     if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, &s.late))) break;
                     fence_after();
                     const uint32_t to = tmem + (tile & 1) * kTileN;
                     uint32_t add = 0;
-                    for (int k = done; k < until; k += 4) {
-                        ok = PAIR == 2 && cuts && k + 4 >= end ? wait_thread<true>(&s.full[stage], phase, &s.late)
-                                                               : wait_thread(&s.full[stage], phase, &s.late);
+                    for (int k = done; k < until; ++k) {
+                        const bool end = ++in == each;
+                        ok = PAIR == 2 && cuts && end ? wait_thread<true>(&s.full[stage], phase, &s.late)
+                                                      : wait_thread(&s.full[stage], phase, &s.late);
                         if (!ok) break;
                         fence_after();
                         const uint32_t a = (uint32_t)a0 + stage * (S::kStage >> 4), b = (uint32_t)b0 + stage * (S::kStage >> 4);
                         mma<PAIR>(to, a, b, a_high, b_high, now, add);
                         add = 1;
-                        if (k + 4 <= until) {
+                        if (!end) {
 #pragma unroll
                             for (int j = 1; j < 4; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
                         } else {
-                            for (int j = 1; j < until - k; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
+                            for (int j = 1; j < mmas; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
+                            in = 0;
                         }
                         commit<PAIR>(&s.empty[stage]);
                         if (++stage == S::kStages) {
@@ -613,15 +623,15 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
-            const int64_t step = p.exact ? kExact : w.k1 - w.k0;
-            for (int64_t k = w.k0; k < w.k1; k += step) {
+            const int64_t blocks = w.k0 < w.k1 ? (w.k1 - w.k0 + kK - 1) / kK * pairs : 0;
+            for (int64_t k = 0; k < blocks; k += p.exact ? kExact / kK : blocks) {
                 const uint32_t buffer = tile & 1;
                 ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
                 ++tile;
                 fence_after();
                 if (!ok) break;
                 const uint32_t from = tmem + buffer * kTileN + ((uint32_t)(quarter * 32) << 16) + odd * 32;
-                if (k == w.k0) {
+                if (k == 0) {
 #pragma unroll
                     for (int b = 0; b < 4; ++b)
                         if (b * 64 + odd * 32 < count) load_columns(from + b * 64, v[b]);
@@ -721,10 +731,25 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                             out += target.ld;
                         }
                 };
+                const auto write_planes = [&](int b) {
+                    const int c = b * 64 + odd * 32;
+                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(target.out) + base + c * target.ld;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < count - c) {
+                            __nv_bfloat16 x[3];
+                            planes_of(mine && at == c + j ? own : exp2_fast(fmaf(v[b][j] - lse, kLog2E, more)), x);
+#pragma unroll
+                            for (int i = 0; i < 3; ++i) out[i * p.step_plane] = x[i];
+                            out += target.ld;
+                        }
+                };
                 if (live) {
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
-                        if (target.dtype == FASGD_BF16)
+                        if (p.planes)
+                            write_planes(b);
+                        else if (target.dtype == FASGD_BF16)
                             write(static_cast<__nv_bfloat16*>(target.out), b);
                         else
                             write(static_cast<__half*>(target.out), b);
@@ -768,15 +793,18 @@ Encode encoder() {
 // How a side lies: `size` values of its index (all groups' rows, where it is ragged), k of the sums.
 // box: how many of the index a box has; wide (a side that is across): as chunks of 64, which
 // have to be whole ones.
-bool encode(CUtensorMap* map, const Side& s, int dtype, int64_t size, int64_t k, int64_t groups, int box, bool wide) {
+bool encode(CUtensorMap* map, const Side& s, const Product& p, int64_t size, int64_t groups, int box, bool wide) {
+    const int64_t k = p.k;
     const auto u = [](int64_t n) { return (cuuint64_t)n; };
     const cuuint64_t ld = u(s.ld) * 2, step = groups > 1 ? u(s.step) * 2 : ld;
-    const cuuint64_t dims[4] = {u(wide ? 64 : s.across ? size : k), u(s.across ? k : size), u(wide ? size / 64 : 1), u(groups)};
-    const cuuint64_t strides[3] = {ld, wide ? 128 : ld, step};
-    const cuuint32_t boxes[4] = {64, (cuuint32_t)(s.across ? kK : box), wide ? (cuuint32_t)box / 64 : 1, 1}, one[4] = {1, 1, 1, 1};
+    const cuuint64_t dims[5] = {u(wide ? 64 : s.across ? size : k), u(s.across ? k : size), u(wide ? size / 64 : 1), u(groups),
+                                p.planes ? 3u : 1u};
+    const cuuint64_t strides[4] = {ld, wide ? 128 : ld, step, p.planes ? u(s.plane) * 2 : ld};
+    const cuuint32_t boxes[5] = {64, (cuuint32_t)(s.across ? kK : box), wide ? (cuuint32_t)box / 64 : 1, 1, 1},
+                     one[5] = {1, 1, 1, 1, 1};
     const Encode f = encoder();
     return f != nullptr &&
-           f(map, dtype == FASGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+           f(map, p.dtype == FASGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
              const_cast<void*>(s.p), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -811,9 +839,9 @@ cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
     if (t.items == 0) return cudaSuccess;
     t.wide_a = p.a.across && p.m % 64 == 0;
     t.wide_b = p.b.across && p.n % 64 == 0;
-    if (!encode(&t.a, p.a, p.dtype, p.m, p.k, p.ragged == kRaggedN ? p.groups : 1, kBlockM, t.wide_a) ||
-        !encode(&t.b, p.b, p.dtype, p.n, p.k, 1, kTileN / PAIR, t.wide_b) ||
-        (p.ragged == kRaggedN && !encode(&t.few, p.b, p.dtype, p.n, p.k, 1, kFew, false)))
+    if (!encode(&t.a, p.a, p, p.m, p.ragged == kRaggedN ? p.groups : 1, kBlockM, t.wide_a) ||
+        !encode(&t.b, p.b, p, p.n, 1, kTileN / PAIR, t.wide_b) ||
+        (p.ragged == kRaggedN && !encode(&t.few, p.b, p, p.n, 1, kFew, false)))
         return cudaErrorInvalidValue;
     switch (p.ending) {
         case kStore: return launch<PAIR, kStore>(t, t.items, device, sms, stream);

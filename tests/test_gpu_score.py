@@ -73,7 +73,7 @@ def check(c, z, w, labels, upstream=None):
 
 
 SIZES = [(1, 1, 2), (1, 64, 1), (1, 4096, 1000), (2, 8, 9), (128, 200, 10), (127, 96, 64), (129, 72, 257), (300, 129, 1021), (64, 1000, 512),
-         (513, 40, 3000), (5, 256, 20000), (1000, 264, 255)]
+         (513, 40, 3000), (5, 256, 20000), (1000, 264, 255), (259, 517, 1555)]
 
 
 @pytest.mark.parametrize("flip", [False, True])
