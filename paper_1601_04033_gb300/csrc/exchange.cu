@@ -78,10 +78,10 @@ __global__ void __launch_bounds__(256) combine_kernel(ExchangeArgs a) {
         for (int k = 0; k < kAtOnce; ++k) {
             const int32_t i = k < most ? __ldg(a.place + k0 + k) : -1;
             has[k] = there(i, a.n);
-            if (has[k]) {
-                v[k] = load<T, N>(a.places, i * a.ld_places + c);
-                w[k] = a.weight != nullptr ? a.weight[k0 + k] : 1.0f;
-            }
+            // (of an absent place the first one's values are read and left out: a load that has a
+            // branch of its own waits for the one before)
+            v[k] = load<T, N>(a.places, (has[k] ? i : 0) * a.ld_places + c);
+            w[k] = a.weight != nullptr ? __ldg(a.weight + (has[k] ? k0 + k : 0)) : 1.0f;
         }
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k)
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(256) combine_grad_kernel(ExchangeArgs a) {
             Pack<T, N> v[kAtOnce];
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k)
-                if (at[k] >= 0 && a.dweight != nullptr) v[k] = load<T, N>(a.places, at[k] * a.ld_places + c);
+                v[k] = load<T, N>(a.places, max(at[k], 0) * a.ld_places + c);
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
                 if (at[k] >= 0) {

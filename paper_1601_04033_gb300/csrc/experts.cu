@@ -2,6 +2,8 @@
 // fasgd_combine_grad, fasgd_multiply, fasgd_multiply_grad): argument checks, workspace
 // layout, launches.  No handle; nothing is allocated and nothing is kept between calls.
 
+#include <algorithm>
+
 #include "checks.cuh"
 #include "product.cuh"
 #include "route.cuh"
@@ -94,6 +96,7 @@ struct Multiply {
     int64_t w_ld, w_step, x_ld, dy_ld;
     bool planes;                // fp32 by planes on the tensor cores
     int64_t w_plane, x_plane, dy_plane;
+    float* parts;               // of sums that are split
     const void* w() const { return w_copy != nullptr ? w_copy : u.w; }
     const void* x() const { return x_copy != nullptr ? x_copy : u.x; }
     const void* dy() const { return dy_copy != nullptr ? dy_copy : u.dy; }
@@ -134,6 +137,54 @@ int fill_multiply(const char* call, const fasgd_multiply_args& given, bool grad,
             return rc;
     return FASGD_OK;
 }
+fasgd::Product product(const Multiply& m) {
+    fasgd::Product p = {};
+    p.groups = (int32_t)m.u.experts;
+    p.offsets = m.u.offsets;
+    p.dtype = m.planes ? FASGD_BF16 : m.u.dtype;
+    p.planes = p.exact = m.planes;
+    p.ending = fasgd::kStore;
+    p.out_dtype = m.u.dtype;
+    p.factor = 1.0f;
+    return p;
+}
+// y (or dx) by rows: `to` columns from `from`, w's side across or not.
+fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across, const fasgd::Side& x, void* y, int64_t ld_y) {
+    fasgd::Product p = product(m);
+    p.a = {m.w(), m.w_ld, m.w_step, across, m.w_plane};
+    p.b = x;
+    p.m = to;
+    p.n = m.u.rows;
+    p.k = from;
+    p.ragged = fasgd::kRaggedN;
+    p.out = y;
+    p.ld_out = ld_y;
+    return p;
+}
+fasgd::Product product_y(const Multiply& m) {
+    return by_rows(m, m.u.inputs, m.u.outputs, !m.u.w_flip, {m.x(), m.x_ld, 0, 0, m.x_plane}, m.u.y, m.u.ld_y);
+}
+fasgd::Product product_dx(const Multiply& m) {
+    return by_rows(m, m.u.outputs, m.u.inputs, m.u.w_flip, {m.dy(), m.dy_ld, 0, 0, m.dy_plane}, m.u.dx, m.u.ld_dx);
+}
+fasgd::Product by_experts(const Multiply& m) {
+    const fasgd_multiply_args& u = m.u;
+    fasgd::Product p = product(m);
+    const fasgd::Side x = {m.x(), m.x_ld, 0, 1, m.x_plane}, dy = {m.dy(), m.dy_ld, 0, 1, m.dy_plane};
+    p.a = u.dw_flip ? x : dy;
+    p.b = u.dw_flip ? dy : x;
+    p.m = u.dw_flip ? u.inputs : u.outputs;
+    p.n = u.dw_flip ? u.outputs : u.inputs;
+    p.k = u.rows;
+    p.ragged = fasgd::kRaggedK;
+    p.out = u.dw;
+    p.ld_out = u.ld_dw;
+    p.step_out = u.step_dw;
+    p.out_dtype = u.w_dtype;
+    p.exact = u.w_dtype == FASGD_F32;      // (a sum that is stored in 16 bits loses less than its rounding)
+    return p;
+}
+
 int64_t lay_out(Multiply& m, char* base) {
     const fasgd_multiply_args& u = m.u;
     int64_t at = 0;
@@ -172,6 +223,14 @@ int64_t lay_out(Multiply& m, char* base) {
         m.dy_ld = (u.outputs + 7) / 8 * 8;
         m.dy_copy = copy(u.rows * m.dy_ld, m.dy_plane);
     }
+    // One product after the other takes the same room.
+    int64_t parts = 0;
+    if (u.rows > 0) {
+        if (!m.grad) parts = fasgd::part_values(product_y(m));
+        if (m.grad && u.dx != nullptr) parts = fasgd::part_values(product_dx(m));
+        if (m.grad && u.dw != nullptr) parts = std::max(parts, fasgd::part_values(by_experts(m)));
+    }
+    m.parts = reinterpret_cast<float*>(take(4 * parts));
     return at;
 }
 
@@ -215,48 +274,6 @@ cudaError_t copy_rows(const Multiply& m, const void* from, int64_t ld, int64_t c
     p.dtype_from = p.dtype_to = m.u.dtype;
     p.plane = m.planes ? plane : 0;
     return fasgd::launch_pack(p, stream);
-}
-
-fasgd::Product product(const Multiply& m) {
-    fasgd::Product p = {};
-    p.groups = (int32_t)m.u.experts;
-    p.offsets = m.u.offsets;
-    p.dtype = m.planes ? FASGD_BF16 : m.u.dtype;
-    p.planes = p.exact = m.planes;
-    p.ending = fasgd::kStore;
-    p.out_dtype = m.u.dtype;
-    p.factor = 1.0f;
-    return p;
-}
-// y (or dx) by rows: `to` columns from `from`, w's side across or not.
-fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across, const fasgd::Side& x, void* y, int64_t ld_y) {
-    fasgd::Product p = product(m);
-    p.a = {m.w(), m.w_ld, m.w_step, across, m.w_plane};
-    p.b = x;
-    p.m = to;
-    p.n = m.u.rows;
-    p.k = from;
-    p.ragged = fasgd::kRaggedN;
-    p.out = y;
-    p.ld_out = ld_y;
-    return p;
-}
-fasgd::Product by_experts(const Multiply& m) {
-    const fasgd_multiply_args& u = m.u;
-    fasgd::Product p = product(m);
-    const fasgd::Side x = {m.x(), m.x_ld, 0, 1, m.x_plane}, dy = {m.dy(), m.dy_ld, 0, 1, m.dy_plane};
-    p.a = u.dw_flip ? x : dy;
-    p.b = u.dw_flip ? dy : x;
-    p.m = u.dw_flip ? u.inputs : u.outputs;
-    p.n = u.dw_flip ? u.outputs : u.inputs;
-    p.k = u.rows;
-    p.ragged = fasgd::kRaggedK;
-    p.out = u.dw;
-    p.ld_out = u.ld_dw;
-    p.step_out = u.step_dw;
-    p.out_dtype = u.w_dtype;
-    p.exact = u.w_dtype == FASGD_F32;      // (a sum that is stored in 16 bits loses less than its rounding)
-    return p;
 }
 
 // The arguments' memory, for check_shared.
@@ -356,7 +373,7 @@ int fasgd_multiply(const fasgd_multiply_args* u, void* stream_) {
     cudaError_t st = copy_w(m, stream);
     if (st == cudaSuccess) st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, m.x_plane, stream);
     if (st == cudaSuccess)
-        st = fasgd::launch_product(by_rows(m, u->inputs, u->outputs, !u->w_flip, {m.x(), m.x_ld, 0, 0, m.x_plane}, m.u.y, m.u.ld_y), stream);
+        st = fasgd::launch_product(product_y(m), m.parts, stream);
     return cuda_status(st, call);
 }
 
@@ -372,17 +389,17 @@ int fasgd_multiply_grad(const fasgd_multiply_args* u, void* stream_) {
     if (u->rows == 0) {      // no rows: no operands to copy or to describe
         m.u.dtype = FASGD_F32;
         m.planes = false;
-        return cuda_status(u->dw != nullptr ? fasgd::launch_product(by_experts(m), stream) : cudaSuccess, call);
+        return cuda_status(u->dw != nullptr ? fasgd::launch_product(by_experts(m), m.parts, stream) : cudaSuccess, call);
     }
     cudaError_t st = copy_rows(m, m.u.dy, m.u.ld_dy, u->outputs, m.dy_copy, m.dy_ld, m.dy_plane, stream);
     if (st == cudaSuccess && u->dx != nullptr) {
         st = copy_w(m, stream);
         if (st == cudaSuccess)
-            st = fasgd::launch_product(by_rows(m, u->outputs, u->inputs, u->w_flip, {m.dy(), m.dy_ld, 0, 0, m.dy_plane}, m.u.dx, m.u.ld_dx), stream);
+            st = fasgd::launch_product(product_dx(m), m.parts, stream);
     }
     if (st == cudaSuccess && u->dw != nullptr) {
         st = copy_rows(m, m.u.x, m.u.ld_x, u->inputs, m.x_copy, m.x_ld, m.x_plane, stream);
-        if (st == cudaSuccess) st = fasgd::launch_product(by_experts(m), stream);
+        if (st == cudaSuccess) st = fasgd::launch_product(by_experts(m), m.parts, stream);
     }
     return cuda_status(st, call);
 }

@@ -1,5 +1,5 @@
-// Matrix products in their simple form: 64 x 64 tiles of D in registers, 16 steps of k
-// through shared memory at a time, fp32 multiply-adds whatever the type.  Right for every
+// Matrix products in their simple form: 64 x 64 tiles of D in registers, 32 steps of k
+// through shared memory at a time, the next 32 read meanwhile, fp32 multiply-adds whatever the type.  Right for every
 // layout, alignment and size.
 
 #include <algorithm>
@@ -10,22 +10,34 @@
 namespace fasgd {
 namespace {
 
-constexpr int kM = 64, kN = kPlainN, kK = 16;
+constexpr int kM = 64, kN = kPlainN, kK = 32;
+constexpr int kEach = kM * kK / 256;     // values of a stage that a thread reads
 
 template <class T>
 __device__ __forceinline__ float element(const Side& s, int64_t group, int64_t i, int64_t k) {
     const T* p = static_cast<const T*>(s.p) + group * s.step;
     return to_f32(s.across ? p[k * s.ld + i] : p[i * s.ld + k]);
 }
-// Elements [i0, i0 + 64) x [k0, k0 + 16) of a side, 0 beyond [.., i1) and [.., k1).
+// Elements [i0, i0 + 64) x [k0, k0 + 32) of a side, 0 beyond [.., i1) and [.., k1): into
+// registers, and from there to shared memory.
 template <class T>
-__device__ __forceinline__ void stage(float (&to)[kK][kM + 4], const Side& s, int64_t group, int64_t i0, int64_t i1,
-                                      int64_t k0, int64_t k1) {
+__device__ __forceinline__ void read(float (&v)[kEach], const Side& s, int64_t group, int64_t i0, int64_t i1, int64_t k0,
+                                     int64_t k1) {
 #pragma unroll
-    for (int r = 0; r < kM * kK / 256; ++r) {
+    for (int r = 0; r < kEach; ++r) {
         const int j = threadIdx.x + r * 256;
         const int i = s.across ? j % kM : j / kK, k = s.across ? j / kM : j % kK;
-        to[k][i] = i0 + i < i1 && k0 + k < k1 ? element<T>(s, group, i0 + i, k0 + k) : 0.0f;
+        v[r] = i0 + i < i1 && k0 + k < k1 ? element<T>(s, group, i0 + i, k0 + k) : 0.0f;
+    }
+}
+__device__ __forceinline__ void stage(float (&to)[kK][kM + 1], const float (&v)[kEach], bool across) {
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) {
+        const int j = threadIdx.x + r * 256;
+        if (across)
+            to[j / kM][j % kM] = v[r];
+        else
+            to[j % kK][j / kK] = v[r];
     }
 }
 
@@ -68,9 +80,31 @@ __device__ bool find_tile(const Product& p, int64_t tile, int64_t& group, Bounds
     return false;
 }
 
+// Parts of k's sums into a product's result.
+__global__ void __launch_bounds__(256) fold_kernel(Product p, const float* parts, int64_t step, int32_t count) {
+    const int64_t g = blockIdx.y;
+    Bounds rows = {0, p.n};
+    if (p.ragged == kRaggedN) rows = {group_bounds(p.offsets, 0, p.n).lo, group_bounds(p.offsets, p.groups - 1, p.n).hi};
+    const float* from = parts + g * p.n * p.m;
+    const float one = p.scale != nullptr && !p.by_n ? *p.scale * p.factor : p.factor;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.n * p.m; i += (int64_t)gridDim.x * 256) {
+        const int64_t n = i / p.m;
+        float v = 0.0f;
+        if (n >= rows.lo && n < rows.hi)
+            for (int s = 0; s < count; ++s) v += from[s * step + i];
+        if (p.by_n) {
+            const float scale = p.scale[n];
+            v = scale == 0.0f ? 0.0f : v * (scale * p.factor);
+        } else {
+            v *= one;
+        }
+        put(p, g, i - n * p.m, n, v);
+    }
+}
+
 template <class T>
 __global__ void __launch_bounds__(256) plain_kernel(Product p) {
-    __shared__ float as[kK][kM + 4], bs[kK][kN + 4];
+    __shared__ float as[kK][kM + 1], bs[kK][kN + 1];
     const uint32_t across = (uint32_t)((p.m + kM - 1) / kM), tile = blockIdx.x / across, tiles = gridDim.x / across;
     const int64_t m0 = (int64_t)(blockIdx.x % across) * kM;
     int64_t group = blockIdx.z, n0 = (int64_t)tile * kN, n1 = p.n, k0 = 0, k1 = p.k;
@@ -91,18 +125,23 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
     }
     const int64_t ga = p.ragged == kRaggedN ? group : 0;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float d[4][4] = {};      // [m: tx + 16 i][n: ty * 4 + j]
+    float d[4][4] = {};      // [m: tx + 16 i][n: ty + 16 j]
+    float a_next[kEach], b_next[kEach];
+    read<T>(a_next, p.a, ga, m0, p.m, k0, k1);
+    read<T>(b_next, p.b, 0, n0, n1, k0, k1);
     for (int64_t k = k0; k < k1; k += kK) {
-        stage<T>(as, p.a, ga, m0, p.m, k, k1);
-        stage<T>(bs, p.b, 0, n0, n1, k, k1);
+        stage(as, a_next, p.a.across);
+        stage(bs, b_next, p.b.across);
         __syncthreads();
+        read<T>(a_next, p.a, ga, m0, p.m, k + kK, k1);
+        read<T>(b_next, p.b, 0, n0, n1, k + kK, k1);
 #pragma unroll
         for (int s = 0; s < kK; ++s) {
             float av[4], bv[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) av[i] = as[s][tx + 16 * i];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) bv[j] = bs[s][ty * 4 + j];
+            for (int j = 0; j < 4; ++j) bv[j] = bs[s][ty + 16 * j];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -114,7 +153,7 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
     if (p.ending == kStore) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int64_t n = n0 + ty * 4 + j;
+            const int64_t n = n0 + ty + 16 * j;
             if (n >= n1) continue;
             float scale = p.factor;
             bool zero = false;
@@ -140,7 +179,7 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
             const float lse = m < p.m ? p.lse[m] : 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int64_t n = n0 + ty * 4 + j;
+                const int64_t n = n0 + ty + 16 * j;
                 if (m < p.m && n < n1)
                     put(p, 0, m, n, has ? p.factor * (p.n0 + n == label ? expm1f(d[i][j] - lse) : expf(d[i][j] - lse)) : 0.0f);
             }
@@ -149,7 +188,7 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int64_t n = n0 + ty * 4 + j;
+            const int64_t n = n0 + ty + 16 * j;
             if (n < n1) top = fmaxf(top, d[i][j]);
             if (n < n1 && has && p.n0 + n == label) p.at_label[m] = d[i][j];
         }
@@ -160,7 +199,7 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (n0 + ty * 4 + j < n1) sum += d[i][j] == top ? 1.0f : expf(d[i][j] - top);
+            if (n0 + ty + 16 * j < n1) sum += d[i][j] == top ? 1.0f : expf(d[i][j] - top);
         as[ty][tx + 16 * i] = sum;
         __syncthreads();
         if (ty == 0 && m < p.m) {
@@ -241,6 +280,13 @@ cudaError_t launch_pack(const Pack& p, cudaStream_t stream) {
         }
     }
     return p.dtype_to == FASGD_BF16 ? pack<float, __nv_bfloat16, false>(p, stream) : pack<float, __half, false>(p, stream);
+}
+
+cudaError_t launch_fold(const Product& p, const float* parts, int64_t step, int32_t count, cudaStream_t stream) {
+    if (p.n * p.m == 0) return cudaSuccess;
+    const dim3 grid((unsigned)std::min<int64_t>((p.n * p.m + 255) / 256, 1 << 14), p.ragged == kRaggedK ? p.groups : 1);
+    fold_kernel<<<grid, 256, 0, stream>>>(p, parts, step, count);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_plain(const Product& p, cudaStream_t stream) {

@@ -44,7 +44,7 @@ struct Product {
     // kStore, kResidual: element (m, n) of group g is out[g * step_out + n * ld_out + m]
     void* out;
     int64_t ld_out, step_out;
-    int64_t step_split;          // from one part of k's result to the next one's (launch_tiles)
+    int64_t step_split;          // launch_tiles: from one part of k's sums to the next
     int64_t step_plane;          // kResidual of planes: from one to the next
     int32_t planes;              // the sides are fp32 values as three planes of dtype FASGD_BF16
     int32_t out_dtype;
@@ -56,6 +56,7 @@ struct Product {
     // kStatistics, kResidual
     const int64_t* labels;       // [m]
     float2* parts;               // [n tiles][m]: kStatistics
+    int32_t narrow;              // kStatistics: tiles of kNarrowN n
     float* at_label;             // [m]: kStatistics
     const float* lse;            // [m]: kResidual
     int64_t n0, classes;         // the first n of this piece, and how many there are of all pieces
@@ -70,13 +71,26 @@ cudaError_t launch_plain(const Product& p, cudaStream_t stream);
 // fp32 values take part as three bf16 ones each (rounded, then what is left, twice: x = x0 + x1 + x2 to
 // 2^-27), in the six products of them that reach 2^-26:
 // x2 y0, x0 y2, x1 y1, x1 y0, x0 y1, x0 y0.
-constexpr int kTileN = 256;
+constexpr int kTileN = 256, kNarrowN = 128;
 constexpr int kPairs = 6;
 constexpr double kPlanesFrom = 1 << 28;
 __host__ __device__ constexpr uint32_t plane_a(uint32_t pair) { return 0x001102u >> 4 * pair & 15u; }
 __host__ __device__ constexpr uint32_t plane_b(uint32_t pair) { return 0x010120u >> 4 * pair & 15u; }
 bool tile_side(const Side& s, int64_t groups);
-cudaError_t launch_tiles(const Product& p, cudaStream_t stream);
+// How a product falls to the SMs: blocks or pairs of them, parts of k's sums, n of a tile.
+struct TilePlan {
+    int32_t pair, splits;
+};
+TilePlan plan_tiles(const Product& p);      // by sizes alone
+cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t stream);
+// out = the sum of `count` parts, `step` values apart, each [groups of ragged k][n][m], as p stores it.
+cudaError_t launch_fold(const Product& p, const float* parts, int64_t step, int32_t count, cudaStream_t stream);
+// The values of the parts that launch_product needs room for.
+inline int64_t part_values(const Product& p) {
+    if (p.dtype == 0 || p.ending != kStore) return 0;
+    const int64_t splits = plan_tiles(p).splits;
+    return splits > 1 ? splits * p.n * p.m * (p.ragged == kRaggedK ? p.groups : 1) : 0;
+}
 // Whether an fp32 product of m x n x k goes by planes: the plain form does some 10 TFLOP/s, the planes
 // some 250, after copies and a launch or two more.
 inline bool by_planes(int64_t m, int64_t n, int64_t k) {
@@ -84,8 +98,22 @@ inline bool by_planes(int64_t m, int64_t n, int64_t k) {
 }
 // What is of fp32 still when it gets here takes the plain form; its callers copy sides of large fp32
 // products to planes, and lay out 16-bit ones for the tensor cores.
-inline cudaError_t launch_product(const Product& p, cudaStream_t stream) {
-    return p.dtype == 0 ? launch_plain(p, stream) : launch_tiles(p, stream);
+// parts: room for part_values().
+inline cudaError_t launch_product(const Product& p, float* parts, cudaStream_t stream) {
+    if (p.dtype == 0) return launch_plain(p, stream);
+    const TilePlan plan = plan_tiles(p);
+    if (part_values(p) == 0) return launch_tiles(p, {plan.pair, 1}, stream);
+    Product q = p;
+    q.out = parts;
+    q.out_dtype = 0;
+    q.ld_out = p.m;
+    q.step_out = p.n * p.m;
+    q.step_split = q.step_out * (p.ragged == kRaggedK ? p.groups : 1);
+    q.scale = nullptr;
+    q.by_n = 0;
+    q.factor = 1.0f;
+    const cudaError_t st = launch_tiles(q, plan, stream);
+    return st != cudaSuccess ? st : launch_fold(p, parts, q.step_split, plan.splits, stream);
 }
 
 // A copy of a side with rows that lie as the fast kernels want them: `rows` rows of `cols`

@@ -28,30 +28,43 @@ int warps_of(int32_t experts) { return experts <= kManyExperts ? kManyWarps : kF
 
 __device__ __forceinline__ bool goes(int32_t e, int32_t experts) { return (uint32_t)e < (uint32_t)experts; }
 
+// Entries of this warp, kAhead steps read together.
+constexpr int kAhead = 8;
+template <class F>
+__device__ __forceinline__ void sweep(const int32_t* chosen, int64_t begin, int64_t end, F step) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t i0 = begin; i0 < end; i0 += 32 * kAhead) {
+        int32_t e[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) e[j] = i0 + 32 * j + lane < end ? __ldg(chosen + i0 + 32 * j + lane) : -1;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (i0 + 32 * j < end) step(i0 + 32 * j + lane, e[j]);
+    }
+}
 // Entries [begin, end) of this warp into its counters.
 __device__ void count(const int32_t* chosen, int64_t begin, int64_t end, int32_t experts, int32_t* mine) {
     const int lane = threadIdx.x & 31;
-    for (int64_t i = begin; i < end; i += 32) {
-        const int32_t e = i + lane < end ? chosen[i + lane] : -1;
+    sweep(chosen, begin, end, [&](int64_t, int32_t e) {
         const uint32_t same = __match_any_sync(0xffffffffu, e);
         if (goes(e, experts) && lane == __ffs(same) - 1) mine[e] += __popc(same);
         __syncwarp();
-    }
+    });
 }
 // The places of this warp's entries; mine: the next place of each expert.
 __device__ void hand_out(const RouteArgs& a, int64_t begin, int64_t end, int32_t* mine) {
     const int lane = threadIdx.x & 31;
-    for (int64_t i = begin; i < end; i += 32) {
-        const int32_t e = i + lane < end ? a.chosen[i + lane] : -1;
+    int32_t *const place = a.place, *const order = a.order;
+    sweep(a.chosen, begin, end, [&](int64_t i, int32_t e) {
         const uint32_t same = __match_any_sync(0xffffffffu, e);
         int32_t at = -1;
         if (goes(e, a.experts)) at = mine[e] + __popc(same & ((1u << lane) - 1u));
         __syncwarp();
         if (at >= 0 && lane == __ffs(same) - 1) mine[e] = at + __popc(same);
         __syncwarp();
-        if (i + lane < end) a.place[i + lane] = at;
-        if (at >= 0) a.order[at] = (int32_t)(i + lane);
-    }
+        if (i < end) place[i] = at;
+        if (at >= 0) order[at] = (int32_t)i;
+    });
 }
 // first[0..experts) from counts to their exclusive sums; the total is returned to all.
 // By warp 0, 32 at a time.

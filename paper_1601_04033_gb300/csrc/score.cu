@@ -28,6 +28,7 @@ struct Score {
     int64_t size, tile;
     bool grad;
     bool planes;                 // fp32 by planes on the tensor cores
+    bool narrow;                 // statistics in tiles of kNarrowN
     int64_t plane_z, plane_w, plane_g;
     // workspace
     void* z_copy;                // rows x ld_zc (null: z itself serves)
@@ -40,15 +41,22 @@ struct Score {
     float* share;                // [1] upstream / N
     void* g;                     // [piece][ld_g]
     int64_t ld_g, piece;
-    float* dz_sum;               // [rows][cols] (several pieces)
+    float* dz_sum;               // [dz_parts][rows][cols] (several pieces)
+    int32_t dz_parts;
+    float* sums;                 // room for the parts of a product's sums
+    float factor;                // what g is held times
+    const void *z, *w;           // what the products read
 };
 
-// lse and the row's loss from the tiles' parts: 32 rows a block, 8 threads each.
+// lse and the row's loss from the tiles' parts: ROWS rows a block, 256 / ROWS threads each, every one
+// four parts at a time (few rows have more threads: one row's 1,024 parts took 8 of them 23 us).
+template <int ROWS>
 __global__ void __launch_bounds__(256) lse_kernel(const float2* parts, int64_t tiles, int64_t rows, const int64_t* labels,
                                                   int64_t classes, const float* at_label, float* lse, float* row_loss) {
-    __shared__ float2 shared[8][32];
-    const int x = threadIdx.x % 32, y = threadIdx.x / 32;
-    const int64_t r = (int64_t)blockIdx.x * 32 + x;
+    constexpr int kEach = 256 / ROWS;
+    __shared__ float2 shared[kEach][ROWS];
+    const int x = threadIdx.x % ROWS, y = threadIdx.x / ROWS;
+    const int64_t r = (int64_t)blockIdx.x * ROWS + x;
     float top = -INFINITY, sum = 0.0f;
     const auto join = [&](float2 p) {
         const float most = fmaxf(top, p.x);
@@ -56,16 +64,35 @@ __global__ void __launch_bounds__(256) lse_kernel(const float2* parts, int64_t t
         top = most;
     };
     if (r < rows)
-        for (int64_t j = y; j < tiles; j += 8) join(parts[j * rows + r]);
+        for (int64_t j = y; j < tiles; j += 4 * kEach) {
+            float2 p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = j + i * kEach < tiles ? parts[(j + i * kEach) * rows + r] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) join(p[i]);
+        }
     shared[y][x] = make_float2(top, sum);
-    __syncthreads();
+#pragma unroll
+    for (int half = kEach / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (y < half) {
+            join(shared[y + half][x]);
+            shared[y][x] = make_float2(top, sum);
+        }
+    }
     if (y == 0 && r < rows) {
-        for (int i = 1; i < 8; ++i) join(shared[i][x]);
         const float log_sum = logf(sum);
         const int64_t label = labels[r];
         lse[r] = top + log_sum;
         row_loss[r] = label >= 0 && label < classes ? (top - at_label[r]) + log_sum : 0.0f;
     }
+}
+template <int ROWS>
+cudaError_t launch_lse(const float2* parts, int64_t tiles, int64_t rows, const int64_t* labels, int64_t classes,
+                       const float* at_label, float* lse, float* row_loss, cudaStream_t stream) {
+    lse_kernel<ROWS><<<(unsigned)((rows + ROWS - 1) / ROWS), 256, 0, stream>>>(parts, tiles, rows, labels, classes, at_label, lse,
+                                                                               row_loss);
+    return cudaGetLastError();
 }
 
 // The loss, upstream / N, and what each row's gradient is multiplied by: one block.
@@ -104,29 +131,6 @@ __global__ void __launch_bounds__(1024) loss_kernel(int64_t rows, const int64_t*
         for (int64_t r = threadIdx.x; r < rows; r += 1024) row_scale[r] = has(r) ? up : 0.0f;
 }
 
-// dz from its sums over the pieces.
-template <class T>
-__global__ void __launch_bounds__(256) fold_kernel(const float* sum, const float* row_scale, int64_t rows, int64_t cols,
-                                                   T* dz, int64_t ld, float factor) {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const float s = row_scale[r];
-        for (int64_t c = threadIdx.x; c < cols; c += 256)
-            dz[r * ld + c] = fasgd::from_f32<T>(s == 0.0f ? 0.0f : sum[r * cols + c] * (s * factor));
-    }
-}
-cudaError_t fold(const Score& s, float factor, cudaStream_t stream) {
-    const unsigned blocks = (unsigned)std::min<int64_t>(s.u.rows, 1 << 20);
-    const auto go = [&](auto* dz) {
-        fold_kernel<<<blocks, 256, 0, stream>>>(s.dz_sum, s.row_scale, s.u.rows, s.u.cols, dz, s.u.ld_dz, factor);
-        return cudaGetLastError();
-    };
-    switch (s.u.dtype) {
-        case FASGD_F32: return go(static_cast<float*>(s.u.dz));
-        case FASGD_BF16: return go(static_cast<__nv_bfloat16*>(s.u.dz));
-        default: return go(static_cast<__half*>(s.u.dz));
-    }
-}
-
 int fill_score(const char* call, const fasgd_score_args& given, Score& s) {
     s = Score();
     s.u = given;
@@ -156,6 +160,53 @@ int fill_score(const char* call, const fasgd_score_args& given, Score& s) {
     return FASGD_OK;
 }
 
+// A piece of n classes' part of dz, and its rows (or columns) of dw; q.a.p or q.out are the piece's.
+Product product_of_g(const Score& s) {
+    Product q = {};
+    q.dtype = s.planes ? FASGD_BF16 : s.u.dtype;
+    q.planes = q.exact = s.planes;
+    q.ending = fasgd::kStore;
+    q.factor = 1.0f / s.factor;
+    q.out_dtype = s.u.dtype;
+    return q;
+}
+Product product_dz(const Score& s, int64_t n) {
+    const fasgd_score_args& u = s.u;
+    Product q = product_of_g(s);
+    q.a = {s.w, s.ld_wc, 0, u.w_flip, s.plane_w};
+    q.b = {s.g, s.ld_g, 0, 1, s.plane_g};
+    q.m = u.cols;
+    q.n = u.rows;
+    q.k = n;
+    if (s.dz_sum != nullptr) {
+        q.out = s.dz_sum;
+        q.ld_out = u.cols;
+        q.step_split = u.rows * u.cols;
+        q.out_dtype = FASGD_F32;
+        q.factor = 1.0f;
+        q.add = 1;      // (a plan for sums that are read again)
+    } else {
+        q.out = u.dz;
+        q.ld_out = u.ld_dz;
+        q.scale = s.row_scale;
+        q.by_n = 1;
+    }
+    return q;
+}
+Product product_dw(const Score& s, int64_t n) {
+    const fasgd_score_args& u = s.u;
+    Product q = product_of_g(s);
+    const fasgd::Side zs = {s.z, s.ld_zc, 0, 1, s.plane_z}, gs = {s.g, s.ld_g, 0, 0, s.plane_g};
+    q.a = u.dw_flip ? zs : gs;
+    q.b = u.dw_flip ? gs : zs;
+    q.m = u.dw_flip ? u.cols : n;
+    q.n = u.dw_flip ? n : u.cols;
+    q.k = u.rows;
+    q.ld_out = u.ld_dw;
+    q.scale = s.share;
+    return q;
+}
+
 int64_t lay_out(Score& s, char* base) {
     const fasgd_score_args& u = s.u;
     int64_t at = 0;
@@ -165,7 +216,10 @@ int64_t lay_out(Score& s, char* base) {
         return p;
     };
     s.planes = u.dtype == FASGD_F32 && fasgd::by_planes(u.rows, u.classes, u.cols);
-    s.tile = u.dtype == FASGD_F32 && !s.planes ? fasgd::kPlainN : fasgd::kTileN;
+    // Few rows: tiles half as wide, which fall more evenly to the SMs (one row of 4,096 against 131,072
+    // classes: 512 tiles are four rounds of 152, 1,024 are seven half ones).
+    s.narrow = u.rows <= 128;
+    s.tile = u.dtype == FASGD_F32 && !s.planes ? fasgd::kPlainN : s.narrow ? fasgd::kNarrowN : fasgd::kTileN;
     const int64_t tiles = (u.classes + s.tile - 1) / s.tile;
     if (!u.known) {
         s.parts = reinterpret_cast<float2*>(take(8 * tiles * u.rows));
@@ -192,6 +246,8 @@ int64_t lay_out(Score& s, char* base) {
         s.ld_wc = ((u.w_flip ? u.cols : u.classes) + 7) / 8 * 8;
         s.w_copy = copy((u.w_flip ? u.classes : u.cols) * s.ld_wc, s.plane_w);
     }
+    s.z = s.z_copy != nullptr ? s.z_copy : u.z;
+    s.w = s.w_copy != nullptr ? s.w_copy : u.w;
     if (!s.grad) return at;
     s.share = reinterpret_cast<float*>(take(4));
     s.row_scale = reinterpret_cast<float*>(take(4 * u.rows));
@@ -202,7 +258,25 @@ int64_t lay_out(Score& s, char* base) {
     s.piece = (u.classes + pieces - 1) / pieces;
     if (pieces > 1) s.piece = std::min(s.piece / 64 * 64 + 64, most / 64 * 64);
     s.g = copy(s.piece * s.ld_g, s.plane_g);
-    if (u.dz != nullptr && s.piece < u.classes) s.dz_sum = reinterpret_cast<float*>(take(4 * u.rows * u.cols));
+    s.factor = u.dtype == FASGD_F16 ? 16384.0f : 1.0f;
+    int64_t parts = 0;
+    s.dz_sum = nullptr;
+    s.dz_parts = 1;
+    if (u.dz != nullptr && u.rows > 0) {
+        if (s.piece < u.classes) {
+            s.dz_sum = reinterpret_cast<float*>(16);      // (that there is one counts)
+            const Product q = product_dz(s, s.piece);
+            if (q.dtype != FASGD_F32) s.dz_parts = fasgd::plan_tiles(q).splits;
+            s.dz_sum = reinterpret_cast<float*>(take(4 * s.dz_parts * u.rows * u.cols));
+        } else {
+            parts = fasgd::part_values(product_dz(s, u.classes));
+        }
+    }
+    // (a last piece may be shorter than the others and split otherwise)
+    if (u.dw != nullptr && u.rows > 0)
+        parts = std::max({parts, fasgd::part_values(product_dw(s, s.piece)),
+                          fasgd::part_values(product_dw(s, u.classes - (u.classes - 1) / s.piece * s.piece))});
+    s.sums = reinterpret_cast<float*>(take(4 * parts));
     return at;
 }
 
@@ -214,8 +288,7 @@ const void* at_class(const void* p, int64_t ld, bool flip, int64_t v, int64_t si
 cudaError_t run(const Score& s, cudaStream_t stream) {
     const fasgd_score_args& u = s.u;
     cudaError_t st = cudaSuccess;
-    const void* z = u.z;
-    const void* w_all = u.w;
+    const void *z = s.z, *w_all = s.w;
     const int64_t ld_z = s.ld_zc, ld_w = s.ld_wc;
     fasgd::Pack c = {};
     c.groups = 1;
@@ -229,7 +302,6 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         c.ld_to = s.ld_wc;
         c.plane = s.planes ? s.plane_w : 0;
         if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
-        w_all = s.w_copy;
     }
     if (s.z_copy != nullptr) {
         c.from = u.z;
@@ -242,7 +314,6 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         c.labels = u.labels;
         c.classes = u.classes;
         if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
-        z = s.z_copy;
     }
     Product p = {};
     p.a = {z, ld_z, 0, 0, s.plane_z};
@@ -258,19 +329,19 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     p.labels = u.labels;
     p.classes = u.classes;
     p.parts = s.parts;
+    p.narrow = s.narrow;
     p.at_label = s.at_label;
     p.lse = s.lse;
     if (!u.known && u.rows > 0) {
-        st = fasgd::launch_product(p, stream);
+        st = fasgd::launch_product(p, nullptr, stream);
         if (st != cudaSuccess) return st;
-        lse_kernel<<<(unsigned)((u.rows + 31) / 32), 256, 0, stream>>>(
-            s.parts, (u.classes + s.tile - 1) / s.tile, u.rows, u.labels, u.classes, s.at_label, s.lse, u.row_loss);
-        if ((st = cudaGetLastError()) != cudaSuccess) return st;
+        const auto launch = u.rows >= 4096 ? launch_lse<32> : u.rows >= 64 ? launch_lse<8> : launch_lse<1>;
+        st = launch(s.parts, (u.classes + s.tile - 1) / s.tile, u.rows, u.labels, u.classes, s.at_label, s.lse, u.row_loss, stream);
+        if (st != cudaSuccess) return st;
     }
     loss_kernel<<<1, 1024, 0, stream>>>(u.rows, u.labels, u.classes, u.row_loss, u.upstream, u.loss, s.share, s.row_scale);
     if ((st = cudaGetLastError()) != cudaSuccess || !s.grad) return st;
 
-    const float factor = u.dtype == FASGD_F16 ? 16384.0f : 1.0f;
     for (int64_t v = 0; v < u.classes; v += s.piece) {
         const int64_t n = std::min(s.piece, u.classes - v);
         const void* w = at_class(w_all, ld_w, u.w_flip, v, s.planes ? 2 : s.size);
@@ -283,55 +354,41 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         p.out = s.g;
         p.ld_out = s.ld_g;
         p.out_dtype = u.dtype;
-        p.factor = factor;
-        st = fasgd::launch_product(p, stream);
+        p.factor = s.factor;
+        st = fasgd::launch_product(p, nullptr, stream);
         if (st != cudaSuccess) return st;
-        Product q = {};
-        q.dtype = dtype;
-        q.planes = q.exact = s.planes;
-        q.ending = fasgd::kStore;
-        q.factor = 1.0f / factor;
         if (u.dz != nullptr && u.rows > 0) {
-            q.a = {w, ld_w, 0, u.w_flip, s.plane_w};
-            q.b = {s.g, s.ld_g, 0, 1, s.plane_g};
-            q.m = u.cols;
-            q.n = u.rows;
-            q.k = n;
-            if (s.dz_sum != nullptr) {
-                q.out = s.dz_sum;
-                q.ld_out = u.cols;
-                q.out_dtype = FASGD_F32;
+            Product q = product_dz(s, n);
+            q.a.p = w;
+            if (s.dz_sum == nullptr) {
+                st = fasgd::launch_product(q, s.sums, stream);
+            } else {      // every piece in as many parts
                 q.add = v > 0;
-                q.factor = 1.0f;
-            } else {
-                q.out = u.dz;
-                q.ld_out = u.ld_dz;
-                q.out_dtype = u.dtype;
-                q.scale = s.row_scale;
-                q.by_n = 1;
+                st = q.dtype == FASGD_F32 ? fasgd::launch_plain(q, stream)
+                                          : fasgd::launch_tiles(q, {fasgd::plan_tiles(q).pair, s.dz_parts}, stream);
             }
-            st = fasgd::launch_product(q, stream);
             if (st != cudaSuccess) return st;
         }
         if (u.dw != nullptr) {
-            const fasgd::Side zs = {z, ld_z, 0, 1, s.plane_z}, gs = {s.g, s.ld_g, 0, 0, s.plane_g};
-            q.a = u.dw_flip ? zs : gs;
-            q.b = u.dw_flip ? gs : zs;
-            q.m = u.dw_flip ? u.cols : n;
-            q.n = u.dw_flip ? n : u.cols;
-            q.k = u.rows;
+            Product q = product_dw(s, n);
+            q.dtype = dtype;
             q.out = const_cast<void*>(at_class(u.dw, u.ld_dw, u.dw_flip, v, s.size));
-            q.ld_out = u.ld_dw;
-            q.out_dtype = u.dtype;
-            q.add = 0;
-            q.scale = s.share;
-            q.by_n = 0;
-            q.factor = 1.0f / factor;
-            st = fasgd::launch_product(q, stream);
+            st = fasgd::launch_product(q, s.sums, stream);
             if (st != cudaSuccess) return st;
         }
     }
-    return s.dz_sum != nullptr && u.rows > 0 ? fold(s, 1.0f / factor, stream) : st;
+    if (s.dz_sum != nullptr && u.rows > 0) {
+        Product q = product_dz(s, s.piece);
+        q.out = u.dz;
+        q.ld_out = u.ld_dz;
+        q.out_dtype = u.dtype;
+        q.add = 0;
+        q.scale = s.row_scale;
+        q.by_n = 1;
+        q.factor = 1.0f / s.factor;
+        st = fasgd::launch_fold(q, s.dz_sum, u.rows * u.cols, s.dz_parts, stream);
+    }
+    return st;
 }
 
 }  // namespace

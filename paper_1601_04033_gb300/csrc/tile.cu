@@ -55,6 +55,7 @@ struct TileArgs {
     int32_t wide_a, wide_b;    // a side that is across, in boxes of several chunks
     int64_t m_tiles, items;    // items: of all groups, unless n is ragged
     int32_t splits;
+    int32_t tile_n;            // of a tile
 };
 
 // ---- PTX ------------------------------------------------------------------------------
@@ -281,7 +282,7 @@ __device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, int6
         w.n0 = b.lo + (j - s.first[lo]) * kTileN;
         w.n1 = min(b.hi, w.n0 + kTileN);
     } else {
-        const int64_t n_tiles = (p.n + kTileN - 1) / kTileN;
+        const int64_t n_tiles = (p.n + t.tile_n - 1) / t.tile_n;
         if (p.ragged == kRaggedK) {
             w.group = (int32_t)(i / (t.m_tiles * n_tiles));
             i -= (int64_t)w.group * t.m_tiles * n_tiles;
@@ -294,8 +295,8 @@ __device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, int6
         i -= band * 32 * n_tiles;
         w.n_tile = i / high;
         w.m0 = (m_first + i - w.n_tile * high) * (kBlockM * PAIR);
-        w.n0 = w.n_tile * kTileN;
-        w.n1 = min(p.n, w.n0 + kTileN);
+        w.n0 = w.n_tile * t.tile_n;
+        w.n1 = min(p.n, w.n0 + t.tile_n);
     }
     if (t.splits > 1) {
         const int64_t blocks = (w.k1 - w.k0 + kK - 1) / kK, k0 = w.k0;
@@ -322,7 +323,7 @@ __device__ __forceinline__ Boxes boxes_of(const TileArgs& t, const Tile& w) {
     Boxes x;
     x.rows_b = width_of<PAIR>(t, w) / PAIR;
     x.few = t.p.ragged == kRaggedN && x.rows_b <= 64 * (3 - PAIR);
-    const int step = x.few ? kFew : t.p.b.across && !t.wide_b ? 64 : kTileN / PAIR;
+    const int step = x.few ? kFew : t.p.b.across && !t.wide_b ? 64 : t.tile_n / PAIR;
     x.boxes_b = (x.rows_b + step - 1) / step;
     x.bytes = kSideA + x.boxes_b * step * kK * 2;
     return x;
@@ -705,7 +706,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     const float2 o = *other;
                     const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
                     sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
-                    p.parts[(p.n0 / kTileN + w.n_tile) * p.m + m] = make_float2(most, sum);
+                    p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
                 }
             } else {
                 const float lse = has ? p.lse[m] : INFINITY;
@@ -834,13 +835,14 @@ template <int PAIR>
 cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
     const Product& p = t.p;
     t.m_tiles = (p.m + kBlockM * PAIR - 1) / (kBlockM * PAIR);
-    const int64_t n_tiles = (p.n + kTileN - 1) / kTileN + (p.ragged == kRaggedN ? p.groups : 0);
+    t.tile_n = p.ending == kStatistics && p.narrow ? kNarrowN : kTileN;
+    const int64_t n_tiles = (p.n + t.tile_n - 1) / t.tile_n + (p.ragged == kRaggedN ? p.groups : 0);
     t.items = t.m_tiles * n_tiles * t.splits * (p.ragged == kRaggedK ? p.groups : 1);
     if (t.items == 0) return cudaSuccess;
     t.wide_a = p.a.across && p.m % 64 == 0;
-    t.wide_b = p.b.across && p.n % 64 == 0;
+    t.wide_b = p.b.across && p.n % 64 == 0 && t.tile_n == kTileN;
     if (!encode(&t.a, p.a, p, p.m, p.ragged == kRaggedN ? p.groups : 1, kBlockM, t.wide_a) ||
-        !encode(&t.b, p.b, p, p.n, 1, kTileN / PAIR, t.wide_b) ||
+        !encode(&t.b, p.b, p, p.n, 1, t.tile_n / PAIR, t.wide_b) ||
         (p.ragged == kRaggedN && !encode(&t.few, p.b, p, p.n, 1, kFew, false)))
         return cudaErrorInvalidValue;
     switch (p.ending) {
@@ -856,15 +858,47 @@ bool tile_side(const Side& s, int64_t groups) {
     return (reinterpret_cast<uintptr_t>(s.p) & 15) == 0 && s.ld % 8 == 0 && (groups < 2 || s.step % s.ld == 0);
 }
 
-cudaError_t launch_tiles(const Product& p, cudaStream_t stream) {
+// The plan that should take the least time, by what was measured on a GB300: 64 k of a tile take a
+// block or a pair 0.27 us times the n of the tile over 256 (a block alone a quarter more), and no less
+// than 80 GB/s and SM copy its sides in; parts of k cost their sums' way through memory and a launch.
+TilePlan plan_tiles(const Product& p) {
+    constexpr int kSms = 152;
+    const bool rows = p.ragged == kRaggedN;
+    const int64_t groups = rows ? std::min<int64_t>(p.groups, p.n) : p.ragged == kRaggedK ? p.groups : 1;
+    const int64_t k = p.ragged == kRaggedK ? (p.k + p.groups - 1) / p.groups : p.k;
+    const int64_t blocks = std::max<int64_t>(1, (k + kK - 1) / kK * (p.planes ? kPairs : 1));
+    const int64_t per = rows ? std::max<int64_t>(1, p.n / std::max<int64_t>(1, groups)) : p.n;
+    const int64_t n_tiles = rows ? std::max<int64_t>(groups, (p.n + kTileN - 1) / kTileN) : (p.n + kTileN - 1) / kTileN;
+    const double width = (double)std::min<int64_t>(per, kTileN);
+    TilePlan best = {p.m > kBlockM ? 2 : 1, 1};
+    double least = 1e300;
+    for (int pair = p.m > kBlockM ? 2 : 1; pair >= 1; --pair) {
+        const int64_t tiles = (p.m + kBlockM * pair - 1) / (kBlockM * pair) * n_tiles * (p.ragged == kRaggedK ? groups : 1);
+        const int teams = kSms / pair;
+        const double each = std::max(0.27 * width / 256.0 * (pair == 1 ? 1.25 : 1.0),
+                                     (kSideA + std::max(width / pair, 32.0) * kK * 2) / 80e3);
+        for (int splits = 1; splits <= 16 && (splits == 1 || (p.ending == kStore && blocks >= 8 * splits)); ++splits) {
+            const double waves = (double)((tiles * splits + teams - 1) / teams);
+            double time = waves * (double)((blocks + splits - 1) / splits) * each;
+            if (splits > 1) time += 4.0 + (double)p.m * (double)p.n * (double)groups * splits * (p.add ? 16.0 : 8.0) / 5e6 / (rows ? (double)groups : 1.0);
+            if (time < least * 0.97) {
+                least = time;
+                best = {pair, splits};
+            }
+        }
+    }
+    return best;
+}
+
+cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t stream) {
     int device = 0, sms = 0;
     cudaError_t st = cudaGetDevice(&device);
     if (st == cudaSuccess) st = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (st != cudaSuccess) return st;
     TileArgs t = {};
     t.p = p;
-    t.splits = 1;
-    return p.m > kBlockM ? launch<2>(t, device, sms, stream) : launch<1>(t, device, sms, stream);
+    t.splits = plan.splits;
+    return plan.pair == 2 ? launch<2>(t, device, sms, stream) : launch<1>(t, device, sms, stream);
 }
 
 }  // namespace fasgd
