@@ -56,7 +56,6 @@ struct Product {
     // kStatistics, kResidual
     const int64_t* labels;       // [m]
     float2* parts;               // [n tiles][m]: kStatistics
-    int32_t narrow;              // kStatistics: tiles of kNarrowN n
     float* at_label;             // [m]: kStatistics
     const float* lse;            // [m]: kResidual
     int64_t n0, classes;         // the first n of this piece, and how many there are of all pieces
@@ -71,12 +70,23 @@ cudaError_t launch_plain(const Product& p, cudaStream_t stream);
 // fp32 values take part as three bf16 ones each (rounded, then what is left, twice: x = x0 + x1 + x2 to
 // 2^-27), in the six products of them that reach 2^-26:
 // x2 y0, x0 y2, x1 y1, x1 y0, x0 y1, x0 y0.
-constexpr int kTileN = 256, kNarrowN = 128;
+constexpr int kTileN = 256;
 constexpr int kPairs = 6;
 constexpr double kPlanesFrom = 1 << 28;
 __host__ __device__ constexpr uint32_t plane_a(uint32_t pair) { return 0x001102u >> 4 * pair & 15u; }
 __host__ __device__ constexpr uint32_t plane_b(uint32_t pair) { return 0x010120u >> 4 * pair & 15u; }
 bool tile_side(const Side& s, int64_t groups);
+// n of a tile of statistics.  A few rows' classes are one tile each of 152 SMs at a time: the width that
+// takes the least rounds times width (131,072 classes: four of 256 or of 224).
+inline int32_t statistics_tile(int64_t m, int64_t n) {
+    int32_t best = kTileN;
+    if (m <= 128)
+        for (int32_t width = kTileN; width >= 192; width -= 16) {
+            const auto cost = [&](int32_t w) { return ((n + w - 1) / w + 151) / 152 * w; };
+            if (cost(width) < cost(best)) best = width;
+        }
+    return best;
+}
 // How a product falls to the SMs: blocks or pairs of them, parts of k's sums, n of a tile.
 struct TilePlan {
     int32_t pair, splits;

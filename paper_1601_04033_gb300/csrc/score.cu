@@ -28,7 +28,6 @@ struct Score {
     int64_t size, tile;
     bool grad;
     bool planes;                 // fp32 by planes on the tensor cores
-    bool narrow;                 // statistics in tiles of kNarrowN
     int64_t plane_z, plane_w, plane_g;
     // workspace
     void* z_copy;                // rows x ld_zc (null: z itself serves)
@@ -216,10 +215,7 @@ int64_t lay_out(Score& s, char* base) {
         return p;
     };
     s.planes = u.dtype == FASGD_F32 && fasgd::by_planes(u.rows, u.classes, u.cols);
-    // Few rows: tiles half as wide, which fall more evenly to the SMs (one row of 4,096 against 131,072
-    // classes: 512 tiles are four rounds of 152, 1,024 are seven half ones).
-    s.narrow = u.rows <= 128;
-    s.tile = u.dtype == FASGD_F32 && !s.planes ? fasgd::kPlainN : s.narrow ? fasgd::kNarrowN : fasgd::kTileN;
+    s.tile = u.dtype == FASGD_F32 && !s.planes ? fasgd::kPlainN : fasgd::statistics_tile(u.rows, u.classes);
     const int64_t tiles = (u.classes + s.tile - 1) / s.tile;
     if (!u.known) {
         s.parts = reinterpret_cast<float2*>(take(8 * tiles * u.rows));
@@ -329,7 +325,6 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     p.labels = u.labels;
     p.classes = u.classes;
     p.parts = s.parts;
-    p.narrow = s.narrow;
     p.at_label = s.at_label;
     p.lse = s.lse;
     if (!u.known && u.rows > 0) {

@@ -406,7 +406,7 @@ __device__ void clear_rows(const Product& p, int64_t block, int64_t blocks, int 
     }
 }
 
-template <int PAIR, int ENDING>
+template <int PAIR, int ENDING, bool EXACT>
 __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t) {
     using S = Shape<PAIR>;
     extern __shared__ char raw[];
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             };
             look();
             while (blocks > 0 && ok) {
-                const int each = blocks, all = each * (int)pairs, chunk = p.exact ? kExact / kK : all, mmas = last;
+                const int each = blocks, all = each * (int)pairs, chunk = EXACT ? kExact / kK : all, mmas = last;
                 const uint32_t now = shape;
                 const bool cuts = zeroed;
                 int in = 0;                           // blocks of this pair of planes
@@ -610,6 +610,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         // Results.  The warp's lanes of tensor memory are those of its number modulo 4; two warps share
         // them, one with the even 32 columns, one with the odd ones.
         const int quarter = warp & 3, odd = (warp - 4) >> 2;
+        const float more = log2f(p.factor);
         const Target target = {p.out, p.ld_out, p.scale, p.factor, p.by_n, p.out_dtype, p.add};
         if (p.ragged == kRaggedN) clear_rows(p, blockIdx.x, gridDim.x, threadIdx.x - 128, 32 * kEnds);
         uint32_t tile = 0, turn = 0;
@@ -619,19 +620,114 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const int64_t m = w.m0 + rank * kBlockM + quarter * 32 + lane;
             const bool live = m < p.m;
             const int count = (int)(w.n1 - w.n0);
+            const int64_t blocks = w.k0 < w.k1 ? (w.k1 - w.k0 + kK - 1) / kK * pairs : 0;
+            const auto taken = [&](uint32_t buffer) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR == 2)
+                        arrive_first(&s.taken[buffer]);
+                    else
+                        mbar_arrive(&s.taken[buffer]);
+                }
+            };
+            const auto columns_of = [&](uint32_t buffer) {
+                return tmem + buffer * kTileN + ((uint32_t)(quarter * 32) << 16) + odd * 32;
+            };
+            // What the endings know of the row m, and of its label's column of this tile.
+            const int64_t label = ENDING != kStore && live ? p.labels[m] : -1;
+            const bool has = label >= 0 && label < p.classes;
+            const int64_t in = label - p.n0 - w.n0;
+            const int at = has && in >= 0 && in < count ? (int)in : -1;
+            const bool mine = at >= 0 && (at >> 5 & 1) == odd;
+            const float lse = ENDING == kResidual && has ? p.lse[m] : INFINITY;
+            const int64_t base = (ENDING == kStore ? (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * p.step_split : 0) +
+                                 w.n0 * target.ld + m;
+            // Columns c ... c + 31 of the tile into out.
+            const auto end_columns = [&](int c, const float (&x)[32]) {
+                if (ENDING == kStore) {
+                    if (EXACT && !target.add)
+                        store_columns<float>(target, base + c * target.ld, w.n0 + c, min(32, count - c), live, x);
+                    else if (EXACT)
+                        add_columns(target, base + c * target.ld, min(32, count - c), live, x);
+                    else
+                        store_any(target, base + c * target.ld, w.n0 + c, min(32, count - c), live, x);
+                    return;
+                }
+                float own = 0.0f;
+                if (__any_sync(0xffffffffu, mine && at >> 5 == c >> 5)) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (at == c + j) own = target.factor * expm1f(x[j] - lse);
+                }
+                if (!live) return;
+                const int own_at = mine ? at - c : -1;
+                if (EXACT) {
+                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(target.out) + base + c * target.ld;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < count - c) {
+                            __nv_bfloat16 y[3];
+                            planes_of(j == own_at ? own : exp2_fast((x[j] - lse) * kLog2E), y);
+#pragma unroll
+                            for (int i = 0; i < 3; ++i) out[i * p.step_plane] = y[i];
+                            out += target.ld;
+                        }
+                    return;
+                }
+                const auto write = [&](auto* out) {
+                    using T = std::remove_reference_t<decltype(*out)>;
+                    out += base + c * target.ld;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < count - c) {
+                            *out = from_f32<T>(exp2_fast(fmaf(x[j] - lse, kLog2E, more)));
+                            out += target.ld;
+                        }
+                    if ((uint32_t)own_at < 32u) out[(own_at - min(32, count - c)) * target.ld] = from_f32<T>(own);
+                };
+                if (target.dtype == FASGD_BF16)
+                    write(static_cast<__nv_bfloat16*>(target.out));
+                else
+                    write(static_cast<__half*>(target.out));
+            };
+            if (!EXACT) {
+                // 32 columns after the other, out of tensor memory and on their way: a loop that stays in the
+                // instruction cache (for all 128 at once the code outgrew it: 38,000 cycles a tile of g).
+                const uint32_t buffer = tile & 1;
+                if (blocks > 0) {
+                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
+                    ++tile;
+                    fence_after();
+                }
+#pragma unroll 1
+                for (int c = odd * 32; c < count; c += 64) {
+                    float x[32];
+                    if (blocks > 0 && ok) {
+                        load_columns(columns_of(buffer) + (c - odd * 32), x);
+                        wait_columns();
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] = ok ? 0.0f : NAN;
+                    }
+                    if (c + 64 >= count && blocks > 0) taken(buffer);
+                    end_columns(c, x);
+                }
+                if (odd * 32 >= count && blocks > 0) taken(buffer);
+                continue;
+            }
             float v[4][32];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
-            const int64_t blocks = w.k0 < w.k1 ? (w.k1 - w.k0 + kK - 1) / kK * pairs : 0;
-            for (int64_t k = 0; k < blocks; k += p.exact ? kExact / kK : blocks) {
+            for (int64_t k = 0; k < blocks; k += kExact / kK) {
                 const uint32_t buffer = tile & 1;
                 ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
                 ++tile;
                 fence_after();
                 if (!ok) break;
-                const uint32_t from = tmem + buffer * kTileN + ((uint32_t)(quarter * 32) << 16) + odd * 32;
+                const uint32_t from = columns_of(buffer);
                 if (k == 0) {
 #pragma unroll
                     for (int b = 0; b < 4; ++b)
@@ -641,121 +737,56 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
 #pragma unroll
                     for (int b = 0; b < 8; ++b)
                         if (b / 2 * 64 + odd * 32 < count) {
-                            float more[16];
-                            load_half(from + b / 2 * 64 + b % 2 * 16, more);
+                            float more_of[16];
+                            load_half(from + b / 2 * 64 + b % 2 * 16, more_of);
                             wait_columns();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[b / 2][b % 2 * 16 + j] += more[j];
+                            for (int j = 0; j < 16; ++j) v[b / 2][b % 2 * 16 + j] += more_of[j];
                         }
                 }
-                fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (PAIR == 2)
-                        arrive_first(&s.taken[buffer]);
-                    else
-                        mbar_arrive(&s.taken[buffer]);
-                }
+                taken(buffer);
             }
             if (!ok)
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[b][j] = NAN;
-            if (ENDING == kStore) {
-                const int64_t base = (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * p.step_split + w.n0 * target.ld + m;
+            if (ENDING != kStatistics) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const int c = b * 64 + odd * 32;
-                    if (c < count) store_any(target, base + c * target.ld, w.n0 + c, min(32, count - c), live, v[b]);
-                }
+                for (int b = 0; b < 4; ++b)
+                    if (b * 64 + odd * 32 < count) end_columns(b * 64 + odd * 32, v[b]);
                 continue;
             }
-            const int64_t label = live ? p.labels[m] : -1;
-            const bool has = label >= 0 && label < p.classes;
-            const int64_t in = label - p.n0 - w.n0;      // the label's column of this tile
-            const int at = has && in >= 0 && in < count ? (int)in : -1;
-            const bool mine = at >= 0 && (at >> 5 & 1) == odd;      // v[at / 64][at % 32] is this thread's
-            if (ENDING == kStatistics) {
-                float top = -INFINITY;
+            float top = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (b * 64 + odd * 32 + j >= count) v[b][j] = -INFINITY;
+                    top = fmaxf(top, v[b][j]);
+                }
+            if (__any_sync(0xffffffffu, mine)) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        if (b * 64 + odd * 32 + j >= count) v[b][j] = -INFINITY;
-                        top = fmaxf(top, v[b][j]);
-                    }
-                if (__any_sync(0xffffffffu, mine)) {
-#pragma unroll
-                    for (int b = 0; b < 4; ++b)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (mine && at == b * 64 + odd * 32 + j) p.at_label[m] = v[b][j];
-                }
-                const float shift = top == -INFINITY ? 0.0f : top;
-                float part[4] = {};
-#pragma unroll
-                for (int b = 0; b < 4; ++b)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[b][j] - shift) * kLog2E);
-                float sum = (part[0] + part[1]) + (part[2] + part[3]);
-                float2* const other = &s.halves[turn][quarter * 32 + lane];
-                if (odd) *other = make_float2(top, sum);
-                asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
-                if (!odd && live) {
-                    const float2 o = *other;
-                    const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
-                    sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
-                    p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
-                }
-            } else {
-                const float lse = has ? p.lse[m] : INFINITY;
-                const float more = log2f(target.factor);
-                const int64_t base = w.n0 * target.ld + m;
-                float own = 0.0f;
-                if (__any_sync(0xffffffffu, mine)) {
-#pragma unroll
-                    for (int b = 0; b < 4; ++b)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (at == b * 64 + odd * 32 + j) own = target.factor * expm1f(v[b][j] - lse);
-                }
-                const auto write = [&](auto* out, int b) {
-                    using T = std::remove_reference_t<decltype(*out)>;
-                    const int c = b * 64 + odd * 32;
-                    out += base + c * target.ld;
-#pragma unroll
                     for (int j = 0; j < 32; ++j)
-                        if (j < count - c) {
-                            const float g = exp2_fast(fmaf(v[b][j] - lse, kLog2E, more));
-                            *out = from_f32<T>(mine && at == c + j ? own : g);
-                            out += target.ld;
-                        }
-                };
-                const auto write_planes = [&](int b) {
-                    const int c = b * 64 + odd * 32;
-                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(target.out) + base + c * target.ld;
+                        if (mine && at == b * 64 + odd * 32 + j) p.at_label[m] = v[b][j];
+            }
+            const float shift = top == -INFINITY ? 0.0f : top;
+            float part[4] = {};
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j < count - c) {
-                            __nv_bfloat16 x[3];
-                            planes_of(mine && at == c + j ? own : exp2_fast(fmaf(v[b][j] - lse, kLog2E, more)), x);
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-                            for (int i = 0; i < 3; ++i) out[i * p.step_plane] = x[i];
-                            out += target.ld;
-                        }
-                };
-                if (live) {
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        if (p.planes)
-                            write_planes(b);
-                        else if (target.dtype == FASGD_BF16)
-                            write(static_cast<__nv_bfloat16*>(target.out), b);
-                        else
-                            write(static_cast<__half*>(target.out), b);
-                    }
-                }
+                for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[b][j] - shift) * kLog2E);
+            float sum = (part[0] + part[1]) + (part[2] + part[3]);
+            float2* const other = &s.halves[turn][quarter * 32 + lane];
+            if (odd) *other = make_float2(top, sum);
+            asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
+            if (!odd && live) {
+                const float2 o = *other;
+                const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
+                sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
+                p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
             }
         }
     }
@@ -810,12 +841,12 @@ bool encode(CUtensorMap* map, const Side& s, const Product& p, int64_t size, int
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int PAIR, int ENDING>
+template <int PAIR, int ENDING, bool EXACT>
 cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStream_t stream) {
     static SharedLimit limit;
     const int bytes = Shape<PAIR>::kBytes;
     const int error = limit.ensure(device, bytes, bytes, [](int64_t n) {
-        return (int)cudaFuncSetAttribute(tile_kernel<PAIR, ENDING>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
+        return (int)cudaFuncSetAttribute(tile_kernel<PAIR, ENDING, EXACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
     });
     if (error != 0) return (cudaError_t)error;
     cudaLaunchConfig_t cfg = {};
@@ -829,13 +860,13 @@ cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStr
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING>, t);
+    return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING, EXACT>, t);
 }
 template <int PAIR>
 cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
     const Product& p = t.p;
     t.m_tiles = (p.m + kBlockM * PAIR - 1) / (kBlockM * PAIR);
-    t.tile_n = p.ending == kStatistics && p.narrow ? kNarrowN : kTileN;
+    t.tile_n = p.ending == kStatistics ? statistics_tile(p.m, p.n) : kTileN;
     const int64_t n_tiles = (p.n + t.tile_n - 1) / t.tile_n + (p.ragged == kRaggedN ? p.groups : 0);
     t.items = t.m_tiles * n_tiles * t.splits * (p.ragged == kRaggedK ? p.groups : 1);
     if (t.items == 0) return cudaSuccess;
@@ -846,9 +877,15 @@ cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
         (p.ragged == kRaggedN && !encode(&t.few, p.b, p, p.n, 1, kFew, false)))
         return cudaErrorInvalidValue;
     switch (p.ending) {
-        case kStore: return launch<PAIR, kStore>(t, t.items, device, sms, stream);
-        case kStatistics: return launch<PAIR, kStatistics>(t, t.items, device, sms, stream);
-        default: return launch<PAIR, kResidual>(t, t.items, device, sms, stream);
+        case kStore: {
+            const bool exact = p.exact && p.out_dtype == FASGD_F32;
+            return exact ? launch<PAIR, kStore, true>(t, t.items, device, sms, stream)
+                         : launch<PAIR, kStore, false>(t, t.items, device, sms, stream);
+        }
+        case kStatistics: return launch<PAIR, kStatistics, true>(t, t.items, device, sms, stream);
+        default:
+            return p.planes ? launch<PAIR, kResidual, true>(t, t.items, device, sms, stream)
+                            : launch<PAIR, kResidual, false>(t, t.items, device, sms, stream);
     }
 }
 
