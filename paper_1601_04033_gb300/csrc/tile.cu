@@ -691,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 else
                     write(static_cast<__half*>(target.out));
             };
-            if (!EXACT) {
+            if constexpr (!EXACT) {
                 // 32 columns after the other, out of tensor memory and on their way: a loop that stays in the
                 // instruction cache (for all 128 at once the code outgrew it: 38,000 cycles a tile of g).
                 const uint32_t buffer = tile & 1;
@@ -714,8 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     end_columns(c, x);
                 }
                 if (odd * 32 >= count && blocks > 0) taken(buffer);
-                continue;
-            }
+            } else {
             float v[4][32];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
@@ -751,42 +750,48 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[b][j] = NAN;
-            if (ENDING != kStatistics) {
+            // The registers' 32 columns after the other, in a loop that moves them down (for the same reason).
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+            for (int c = odd * 32; c < count; c += 64) {
+                if constexpr (ENDING != kStatistics) {
+                    end_columns(c, v[0]);
+                } else {
+                    if (count - c < 32)
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    if (b * 64 + odd * 32 < count) end_columns(b * 64 + odd * 32, v[b]);
-                continue;
-            }
-            float top = -INFINITY;
+                        for (int j = 0; j < 32; ++j) v[0][j] = j < count - c ? v[0][j] : -INFINITY;
+                    float most[4] = {top, v[0][1], v[0][2], v[0][3]};
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+                    for (int j = 0; j < 32; ++j) most[j & 3] = fmaxf(most[j & 3], v[0][j]);
+                    const float next = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+                    if (__any_sync(0xffffffffu, mine && at >> 5 == c >> 5)) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    if (b * 64 + odd * 32 + j >= count) v[b][j] = -INFINITY;
-                    top = fmaxf(top, v[b][j]);
+                        for (int j = 0; j < 32; ++j)
+                            if (mine && at == c + j) p.at_label[m] = v[0][j];
+                    }
+                    const float shift = next == -INFINITY ? 0.0f : next;
+                    float part[4] = {sum * exp2_fast((top - shift) * kLog2E), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[0][j] - shift) * kLog2E);
+                    sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    top = next;
                 }
-            if (__any_sync(0xffffffffu, mine)) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
+                for (int b = 0; b < 3; ++b)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (mine && at == b * 64 + odd * 32 + j) p.at_label[m] = v[b][j];
+                    for (int j = 0; j < 32; ++j) v[b][j] = v[b + 1][j];
             }
-            const float shift = top == -INFINITY ? 0.0f : top;
-            float part[4] = {};
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[b][j] - shift) * kLog2E);
-            float sum = (part[0] + part[1]) + (part[2] + part[3]);
-            float2* const other = &s.halves[turn][quarter * 32 + lane];
-            if (odd) *other = make_float2(top, sum);
-            asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
-            if (!odd && live) {
-                const float2 o = *other;
-                const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
-                sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
-                p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
+            if constexpr (ENDING == kStatistics) {
+                float2* const other = &s.halves[turn][quarter * 32 + lane];
+                if (odd) *other = make_float2(top, sum);
+                asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
+                if (!odd && live) {
+                    const float2 o = *other;
+                    const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
+                    sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
+                    p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
+                }
+            }
             }
         }
     }
