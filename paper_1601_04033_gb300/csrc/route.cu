@@ -42,28 +42,36 @@ __device__ __forceinline__ void sweep(const int32_t* chosen, int64_t begin, int6
             if (i0 + 32 * j < end) step(i0 + 32 * j + lane, e[j]);
     }
 }
-// Entries [begin, end) of this warp into its counters.
+// Entries [begin, end) of this warp into its counters (whose order does not matter).
 __device__ void count(const int32_t* chosen, int64_t begin, int64_t end, int32_t experts, int32_t* mine) {
-    const int lane = threadIdx.x & 31;
     sweep(chosen, begin, end, [&](int64_t, int32_t e) {
-        const uint32_t same = __match_any_sync(0xffffffffu, e);
-        if (goes(e, experts) && lane == __ffs(same) - 1) mine[e] += __popc(same);
-        __syncwarp();
+        if (goes(e, experts)) atomicAdd(mine + e, 1);
     });
+}
+// The lanes whose entries go to the same expert as this one's: a vote for each bit of its number
+// (the warp's own match of values takes a round for each different one, of which there are many).
+__device__ __forceinline__ uint32_t same_as(int32_t e, bool goes_on, int bits) {
+    uint32_t same = __ballot_sync(0xffffffffu, goes_on);
+    for (int b = 0; b < bits; ++b) {
+        const uint32_t ones = __ballot_sync(0xffffffffu, e >> b & 1);
+        same &= e >> b & 1 ? ones : ~ones;
+    }
+    return same;
 }
 // The places of this warp's entries; mine: the next place of each expert.
 __device__ void hand_out(const RouteArgs& a, int64_t begin, int64_t end, int32_t* mine) {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, bits = 32 - __clz(a.experts - 1);
     int32_t *const place = a.place, *const order = a.order;
     sweep(a.chosen, begin, end, [&](int64_t i, int32_t e) {
-        const uint32_t same = __match_any_sync(0xffffffffu, e);
+        const bool on = goes(e, a.experts);
+        const uint32_t same = same_as(e, on, bits);
         int32_t at = -1;
-        if (goes(e, a.experts)) at = mine[e] + __popc(same & ((1u << lane) - 1u));
+        if (on) at = mine[e] + __popc(same & ((1u << lane) - 1u));
         __syncwarp();
-        if (at >= 0 && lane == __ffs(same) - 1) mine[e] = at + __popc(same);
+        if (on && lane == __ffs(same) - 1) mine[e] = at + __popc(same);
         __syncwarp();
         if (i < end) place[i] = at;
-        if (at >= 0) order[at] = (int32_t)i;
+        if (on) order[at] = (int32_t)i;
     });
 }
 // first[0..experts) from counts to their exclusive sums; the total is returned to all.

@@ -18,6 +18,7 @@
 #include "checks.cuh"
 #include "client.cuh"
 #include "product.cuh"
+#include "shared_limit.cuh"
 
 namespace {
 
@@ -27,6 +28,9 @@ struct Score {
     fasgd_score_args u;
     int64_t size, tile;
     bool grad;
+    bool few;                    // few classes: no products
+    float2* few_sums;
+    float* few_dw;
     bool planes;                 // fp32 by planes on the tensor cores
     int64_t plane_z, plane_w, plane_g;
     // workspace
@@ -130,6 +134,178 @@ __global__ void __launch_bounds__(1024) loss_kernel(int64_t rows, const int64_t*
         for (int64_t r = threadIdx.x; r < rows; r += 1024) row_scale[r] = has(r) ? up : 0.0f;
 }
 
+// ---- few classes ------------------------------------------------------------------------------
+// A client's last product with, say, 10 classes: everything in one pass over the rows, fp32 on the
+// ordinary cores, and a second launch for the sums over the rows.  w lies in shared memory as
+// [class][col]; a warp takes a row: its lanes go along the columns and keep a sum for each class, so that
+// every value of z and w is read once a row.  Blocks take the rows by turns and keep their share of dw in
+// shared memory too, each thread its own columns of it; the shares are added up in the blocks' order.
+// The bound is latency: 128 x 200 x 10 took seven launches of the products' general forms (68 us).
+constexpr int kFewClasses = 32, kFewBlocks = 152;
+constexpr int64_t kFewValues = 12 << 10;           // of w: 48 KB, and dw as much again
+constexpr int kFewWarps = 8;
+
+bool few_classes(const fasgd_score_args& u) {
+    return u.classes <= kFewClasses && u.cols * u.classes <= kFewValues;
+}
+int64_t few_blocks(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(kFewBlocks, (rows + kFewWarps - 1) / kFewWarps)); }
+
+struct FewArgs {
+    fasgd_score_args u;
+    float2* sums;       // [blocks] loss, (unused)
+    float* dw;          // [blocks][classes][cols]
+};
+template <class T>
+__global__ void __launch_bounds__(32 * kFewWarps) few_kernel(FewArgs a) {
+    extern __shared__ float shared[];              // w, then dw, then g [warps][classes], then sums [warps]
+    const fasgd_score_args& u = a.u;
+    const int V = (int)u.classes, D = (int)u.cols, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    float *const w = shared, *const dw = w + V * D, *const g = dw + (u.dw != nullptr ? V * D : 0), *const part = g + kFewWarps * V;
+    __shared__ long long total;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    // N, by every block for itself.
+    if (u.dz != nullptr) {
+        long long n = 0;
+        for (int64_t r = threadIdx.x; r < u.rows; r += blockDim.x) n += u.labels[r] >= 0 && u.labels[r] < V;
+        for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+        if (lane == 0) atomicAdd(reinterpret_cast<unsigned long long*>(&total), (unsigned long long)n);
+    }
+    const T* from = static_cast<const T*>(u.w);
+    for (int i = threadIdx.x; i < V * D; i += blockDim.x) {
+        const int v = u.w_flip ? i / D : i % V, d = u.w_flip ? i % D : i / V;
+        w[v * D + d] = fasgd::to_f32(from[u.w_flip ? v * u.ld_w + d : d * u.ld_w + v]);
+        if (u.dw != nullptr) dw[i] = 0.0f;
+    }
+    __syncthreads();
+    const float share = total == 0 ? 0.0f : (u.upstream != nullptr ? *u.upstream : 1.0f) / (float)total;
+    float loss = 0.0f;
+    for (int64_t r0 = (int64_t)blockIdx.x * kFewWarps; r0 < u.rows; r0 += (int64_t)gridDim.x * kFewWarps) {
+        const int64_t r = r0 + warp;
+        const int64_t label = r < u.rows ? u.labels[r] : -1;
+        const bool has = label >= 0 && label < V;
+        const T* z = static_cast<const T*>(u.z) + r * u.ld_z;
+        float p = 0.0f;                            // lane v: g of class v
+        if (has) {
+            float s = -INFINITY;                   // lane v: the value of class v
+            for (int v0 = 0; v0 < V; v0 += 8) {
+                float sum[8] = {};
+                for (int d = lane; d < D; d += 32) {
+                    const float x = fasgd::to_f32(z[d]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (v0 + j < V) sum[j] = fmaf(x, w[(v0 + j) * D + d], sum[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float all = fasgd::warp_sum(sum[j]);
+                    if (lane == v0 + j && v0 + j < V) s = all;
+                }
+            }
+            float top = s;
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float log_sum = logf(fasgd::warp_sum(lane < V ? (s == top ? 1.0f : expf(s - top)) : 0.0f));
+            const float own = __shfl_sync(0xffffffffu, s, (int)label), row_loss = (top - own) + log_sum;
+            const float lse = u.known ? u.lse[r] : top + log_sum;
+            loss += row_loss;
+            if (lane == 0 && !u.known) {
+                u.row_loss[r] = row_loss;
+                if (u.lse != nullptr) u.lse[r] = lse;
+            }
+            p = lane >= V ? 0.0f : lane == label ? expm1f(s - lse) : expf(s - lse);
+        } else if (r < u.rows && lane == 0 && !u.known) {
+            u.row_loss[r] = 0.0f;
+            if (u.lse != nullptr) u.lse[r] = 0.0f;
+        }
+        if (u.dz == nullptr && u.dw == nullptr) continue;
+        if (lane < V) g[warp * V + lane] = p;
+        __syncwarp();
+        if (u.dz != nullptr && r < u.rows) {
+            T* dz = static_cast<T*>(u.dz) + r * u.ld_dz;
+            for (int d = lane; d < D; d += 32) {
+                float sum = 0.0f;
+                for (int v = 0; has && v < V; ++v) sum = fmaf(g[warp * V + v], w[v * D + d], sum);
+                dz[d] = fasgd::from_f32<T>(has ? sum * share : 0.0f);
+            }
+        }
+        if (u.dw != nullptr) {
+            __syncthreads();                       // the rows of all warps
+            const int rows = (int)min((int64_t)kFewWarps, u.rows - r0);
+            for (int d = threadIdx.x; d < D; d += blockDim.x) {
+                float x[kFewWarps];
+#pragma unroll
+                for (int i = 0; i < kFewWarps; ++i) {
+                    const int64_t l = i < rows ? u.labels[r0 + i] : -1;
+                    x[i] = l >= 0 && l < V ? fasgd::to_f32(static_cast<const T*>(u.z)[(r0 + i) * u.ld_z + d]) : 0.0f;
+                }
+                for (int v = 0; v < V; ++v) {
+                    float sum = dw[v * D + d];
+#pragma unroll
+                    for (int i = 0; i < kFewWarps; ++i) sum = fmaf(g[i * V + v], x[i], sum);
+                    dw[v * D + d] = sum;
+                }
+            }
+            __syncthreads();
+        }
+    }
+    if (lane == 0) part[warp] = loss;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float sum = 0.0f;
+        for (int i = 0; i < kFewWarps; ++i) sum += part[i];
+        a.sums[blockIdx.x] = make_float2(sum, 0.0f);
+    }
+    if (u.dw != nullptr)
+        for (int i = threadIdx.x; i < V * D; i += blockDim.x) a.dw[(int64_t)blockIdx.x * V * D + i] = dw[i];
+}
+// The blocks' shares of dw and of the loss.
+template <class T>
+__global__ void __launch_bounds__(256) few_sum_kernel(FewArgs a, int32_t blocks) {
+    const fasgd_score_args& u = a.u;
+    __shared__ unsigned long long total;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    unsigned long long n = 0;
+    for (int64_t r = threadIdx.x; r < u.rows; r += 256) n += u.labels[r] >= 0 && u.labels[r] < u.classes;
+    for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+    if ((threadIdx.x & 31) == 0) atomicAdd(&total, n);
+    __syncthreads();
+    const float count = (float)total;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && u.loss != nullptr) {
+        float sum = 0.0f;
+        for (int b = 0; b < blocks; ++b) sum += a.sums[b].x;
+        *u.loss = total == 0 ? 0.0f : sum / count;
+    }
+    if (u.dw == nullptr) return;
+    const float share = total == 0 ? 0.0f : (u.upstream != nullptr ? *u.upstream : 1.0f) / count;
+    const int64_t values = u.classes * u.cols, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= values) return;
+    float sum = 0.0f;
+#pragma unroll 8
+    for (int b = 0; b < blocks; ++b) sum += a.dw[b * values + i];
+    const int64_t v = i / u.cols, d = i % u.cols;
+    static_cast<T*>(u.dw)[u.dw_flip ? v * u.ld_dw + d : d * u.ld_dw + v] = fasgd::from_f32<T>(total == 0 ? 0.0f : sum * share);
+}
+template <class T>
+cudaError_t run_few(const FewArgs& a, cudaStream_t stream) {
+    static fasgd::SharedLimit limit;
+    const fasgd_score_args& u = a.u;
+    const int64_t blocks = few_blocks(u.rows), values = u.cols * u.classes;
+    const int64_t bytes = 4 * (values * (u.dw != nullptr ? 2 : 1) + kFewWarps * u.classes + kFewWarps);
+    int device = 0;
+    cudaError_t st = cudaGetDevice(&device);
+    if (st != cudaSuccess) return st;
+    const int error = limit.ensure(device, bytes, 4 * (2 * kFewValues + kFewWarps * kFewClasses + kFewWarps), [](int64_t n) {
+        return (int)cudaFuncSetAttribute(few_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
+    });
+    if (error != 0) return (cudaError_t)error;
+    few_kernel<T><<<(unsigned)blocks, 32 * kFewWarps, bytes, stream>>>(a);
+    if ((st = cudaGetLastError()) != cudaSuccess) return st;
+    const int64_t grid = u.dw != nullptr ? (values + 255) / 256 : 1;
+    few_sum_kernel<T><<<(unsigned)grid, 256, 0, stream>>>(a, (int32_t)blocks);
+    return cudaGetLastError();
+}
+
 int fill_score(const char* call, const fasgd_score_args& given, Score& s) {
     s = Score();
     s.u = given;
@@ -214,6 +390,12 @@ int64_t lay_out(Score& s, char* base) {
         at += (bytes + 255) / 256 * 256;
         return p;
     };
+    s.few = few_classes(u);
+    if (s.few) {
+        s.few_sums = reinterpret_cast<float2*>(take(8 * few_blocks(u.rows)));
+        s.few_dw = reinterpret_cast<float*>(take(u.dw != nullptr ? 4 * few_blocks(u.rows) * u.classes * u.cols : 0));
+        return at;
+    }
     s.planes = u.dtype == FASGD_F32 && fasgd::by_planes(u.rows, u.classes, u.cols);
     s.tile = u.dtype == FASGD_F32 && !s.planes ? fasgd::kPlainN : fasgd::statistics_tile(u.rows, u.classes);
     const int64_t tiles = (u.classes + s.tile - 1) / s.tile;
@@ -284,6 +466,11 @@ const void* at_class(const void* p, int64_t ld, bool flip, int64_t v, int64_t si
 cudaError_t run(const Score& s, cudaStream_t stream) {
     const fasgd_score_args& u = s.u;
     cudaError_t st = cudaSuccess;
+    if (s.few) {
+        FewArgs a = {u, s.few_sums, s.few_dw};
+        return u.dtype == FASGD_F32 ? run_few<float>(a, stream)
+               : u.dtype == FASGD_BF16 ? run_few<__nv_bfloat16>(a, stream) : run_few<__half>(a, stream);
+    }
     const void *z = s.z, *w_all = s.w;
     const int64_t ld_z = s.ld_zc, ld_w = s.ld_wc;
     fasgd::Pack c = {};
