@@ -806,8 +806,8 @@ FASGD_API int64_t fasgd_multiply_workspace(const fasgd_multiply_args* a);
  * s and its sums are fp32; for 16-bit types g takes part in its two products rounded to
  * dtype.  rows < 2^31, cols <= FASGD_COLS_MAX, classes <= 2^24.
  * lse: fp32[rows] (rows without a label: any value) or NULL.  known = 0: it is written.
- * known = 1: it holds what an earlier call left there for the same z, w and labels; loss
- * and row_loss are then not looked at, and only dz and dw, one of them at least, are
+ * known = 1: it and row_loss hold what an earlier call left there for the same z, w and
+ * labels; loss is then not looked at, and only dz and dw, one of them at least, are
  * written, without the first sweep over the classes.
  * workspace: 256-byte aligned device memory of at least fasgd_score_workspace() bytes (-1 on
  * a bad argument); it does not grow with rows x classes beyond FASGD_SCORE_PIECE bytes for g
@@ -834,7 +834,7 @@ typedef struct fasgd_score_args {
     int64_t workspace_bytes;
     int32_t dtype;              /* enum fasgd_dtype: z, w and their gradients */
     int32_t w_flip, dw_flip;    /* 0: cols x classes, 1: classes x cols */
-    int32_t known;              /* 1: lse is read */
+    int32_t known;              /* 1: lse and row_loss are read */
 } fasgd_score_args;
 FASGD_API int fasgd_score(const fasgd_score_args* a, void* stream);
 FASGD_API int64_t fasgd_score_workspace(const fasgd_score_args* a);

@@ -622,25 +622,26 @@ def multiply_grad(x, w, offsets, dy, *, grads=(True, True), into: MultiplyGrads 
 
 
 class Score(NamedTuple):
-    loss: object       # fp32 [1], None with a known lse
-    rows: object       # fp32, as labels: each row's loss, 0 without a label; None with a known lse
+    loss: object       # fp32 [1]
+    rows: object       # fp32, as labels: each row's loss, 0 without a label
     dz: object         # as z, or None
     dw: object         # as w, or None
     lse: object        # fp32, as labels: each row's log-sum-exp (any value without a label)
 
 
-def score(z, w, labels, *, upstream=None, grad=True, grads=(True, True), lse=None, into=None) -> Score:
+def score(z, w, labels, *, upstream=None, grad=True, grads=(True, True), known: Score | None = None, into=None) -> Score:
     """fasgd_score: softmax cross entropy of z w ([..., cols] x [cols, classes], w of z's type, rows
     or columns contiguous) against labels (int64, one for each row of z; outside
     [0, classes): none), the mean over the rows that have one, and (grad) the gradients
     of z and w that `grads` names, times `upstream` (a device fp32 value) if given.
-    lse: what an earlier call with these z, w and labels gave: only gradients are
+    known: what an earlier call with these z, w and labels gave: only gradients are
     computed.  into: (dz, dw), where to write them (new tensors where None)."""
+    loss, rows, *_, lse = known if known is not None else (None,) * 5
     want = (bool(grad and grads[0]), bool(grad and grads[1]))
     dz, dw = into if into is not None else (None, None)
     if _fast is not None:
-        return Score(*_done(_fast.score(z, w, labels, upstream, *want, lse, dz, dw)))
-    _one_device(z, w, labels, upstream, lse, dz, dw)
+        return Score(*_done(_fast.score(z, w, labels, upstream, *want, loss, rows, lse, dz, dw)))
+    _one_device(z, w, labels, upstream, loss, rows, lse, dz, dw)
     a = _f.ScoreArgs()
     a.z, a.rows, a.cols, a.ld_z = _rows(z)
     a.dtype = _dtype(z)
@@ -662,8 +663,8 @@ def score(z, w, labels, *, upstream=None, grad=True, grads=(True, True), lse=Non
         if dz is None:
             dz = _new(z)
         _same_type(dz, z)
-        a.dz, rows, cols, a.ld_dz = _rows(dz)
-        if (rows, cols) != (a.rows, a.cols):
+        a.dz, *shape, a.ld_dz = _rows(dz)
+        if shape != [a.rows, a.cols]:
             raise ValueError("z's gradient is as z")
     if want[1]:
         if dw is None:
@@ -672,16 +673,15 @@ def score(z, w, labels, *, upstream=None, grad=True, grads=(True, True), lse=Non
         a.dw, shape, a.ld_dw, _, a.dw_flip = _matrices(dw, 2)
         if shape != w.shape:
             raise ValueError("w's gradient is as w")
-    loss = rows = None
-    if lse is None:
+    if known is None:
         loss = torch.empty(1, dtype=torch.float32, device=z.device)
         rows, lse = (torch.empty(labels.shape, dtype=torch.float32, device=z.device) for _ in range(2))
         a.loss = loss.data_ptr()
-        a.row_loss = rows.data_ptr() or _NOWHERE
     else:
-        if lse.dtype is not torch.float32 or lse.numel() != a.rows or not lse.is_contiguous():
-            raise ValueError("lse must be contiguous fp32, one for each row")
+        if any(t.dtype is not torch.float32 or t.numel() != a.rows or not t.is_contiguous() for t in (rows, lse)):
+            raise ValueError("known rows and lse must be contiguous fp32, one for each row")
         a.known = 1
+    a.row_loss = rows.data_ptr() or _NOWHERE
     a.lse = lse.data_ptr() or _NOWHERE
     space = _space(a, _f.fasgd_score_workspace, z)
     _check(_f.fasgd_score(ctypes.addressof(a), _stream(z)))
@@ -852,15 +852,17 @@ class _Score(torch.autograd.Function):
     @staticmethod
     def forward(ctx, z, w, labels):
         s = score(z, w, labels, grad=False)
-        ctx.save_for_backward(z, w, labels, s.lse)
-        ctx.mark_non_differentiable(s.rows)
-        return s.loss.reshape(()), s.rows
+        rows = s.rows.clone()        # the caller's, who may write into it
+        ctx.save_for_backward(z, w, labels, s.rows, s.lse)
+        ctx.mark_non_differentiable(rows)
+        return s.loss.reshape(()), rows
 
     @staticmethod
     def backward(ctx, d, _rows):
-        z, w, labels, lse = ctx.saved_tensors
+        z, w, labels, rows, lse = ctx.saved_tensors
         with torch.no_grad():
-            s = score(z, w, labels, upstream=d.reshape(1), grads=ctx.needs_input_grad[:2], lse=lse)
+            s = score(z, w, labels, upstream=d.reshape(1), grads=ctx.needs_input_grad[:2],
+                      known=Score(None, rows, None, None, lse))
         return (*_once((s.dz, s.dw), d, z, w), None)
 
 

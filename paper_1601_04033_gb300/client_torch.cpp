@@ -843,13 +843,15 @@ PyObject* py_multiply_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     });
 }
 
-/* score(z, w, labels, upstream, whether dz, whether dw, lse, dz, dw) -> (loss, rows, dz, dw, lse) */
+/* score(z, w, labels, upstream, whether dz, whether dw, known loss, rows and lse (or Nones), dz, dw)
+ * -> (loss, rows, dz, dw, lse) */
 PyObject* py_score(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    return entry(nargs, 9, [&]() -> PyObject* {
+    return entry(nargs, 11, [&]() -> PyObject* {
         const Tensor *z = tensor(args[0]), *w = tensor(args[1]), *labels = tensor(args[2]), *up = tensor(args[3]),
-                     *lse = tensor(args[6]), *dz = tensor(args[7]), *dw = tensor(args[8]);
+                     *loss = tensor(args[6]), *rows = tensor(args[7]), *lse = tensor(args[8]), *dz = tensor(args[9]),
+                     *dw = tensor(args[10]);
         if (z == nullptr || w == nullptr || labels == nullptr) wrong("a tensor is expected");
-        one_device({z, w, labels, up, lse, dz, dw});
+        one_device({z, w, labels, up, loss, rows, lse, dz, dw});
         fasgd_score_args a;
         std::memset(&a, 0, sizeof a);
         const Matrix m(*z);
@@ -890,19 +892,21 @@ PyObject* py_score(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             a.ld_dz = d.ld;
         }
         if (by_w) {
-            const Matrices d(of_w.take(args[8], dw, *w, "w's gradient is as w"), 2);
+            const Matrices d(of_w.take(args[10], dw, *w, "w's gradient is as w"), 2);
             a.dw = d.p;
             a.ld_dw = d.ld;
             a.dw_flip = d.flip;
         }
-        if (lse == nullptr) {
+        if (rows == nullptr || lse == nullptr) {
             at_loss = made.add(1, at::kFloat, &a.loss);
             at_rows = made.add(labels->sizes(), at::kFloat, &a.row_loss);
             at_lse = made.add(labels->sizes(), at::kFloat, &a.lse);
             a.loss = a.row_loss = a.lse = reinterpret_cast<float*>(256);
         } else {
-            if (lse->scalar_type() != at::kFloat || lse->numel() != a.rows || !lse->is_contiguous())
-                wrong("lse must be contiguous fp32, one for each row");
+            for (const Tensor* t : {rows, lse})
+                if (t->scalar_type() != at::kFloat || t->numel() != a.rows || !t->is_contiguous())
+                    wrong("known rows and lse must be contiguous fp32, one for each row");
+            a.row_loss = static_cast<float*>(address(*rows));
             a.lse = static_cast<float*>(address(*lse));
             a.known = 1;
         }
@@ -913,10 +917,13 @@ PyObject* py_score(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         a.workspace_bytes = size;
         made.make();
         unlocked([&] { return (int64_t)fasgd_score(&a, s); });
-        PyObject* known = args[6];
-        if (lse != nullptr) Py_INCREF(known);
-        return tuple({object(made, at_loss, Py_None), object(made, at_rows, Py_None), object(made, at_dz, args[7]),
-                      of_w.object(made), lse != nullptr ? known : made.object(at_lse)});
+        const auto kept = [&](int k, PyObject* given) {      // what was known is not written into
+            if (k >= 0) return made.object(k);
+            Py_INCREF(given);
+            return given;
+        };
+        return tuple({kept(at_loss, args[6]), kept(at_rows, args[7]), object(made, at_dz, args[9]), of_w.object(made),
+                      kept(at_lse, args[8])});
     });
 }
 

@@ -176,12 +176,12 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
         const int64_t label = m < p.m ? p.labels[m] : -1;
         const bool has = label >= 0 && label < p.classes;
         if (p.ending == kResidual) {
-            const float lse = m < p.m ? p.lse[m] : 0.0f;
+            const float lse = has ? p.lse[m] : 0.0f, own = has ? expm1f(-p.row_loss[m]) : 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int64_t n = n0 + ty + 16 * j;
                 if (m < p.m && n < n1)
-                    put(p, 0, m, n, has ? p.factor * (p.n0 + n == label ? expm1f(d[i][j] - lse) : expf(d[i][j] - lse)) : 0.0f);
+                    put(p, 0, m, n, has ? p.factor * (p.n0 + n == label ? own : expf(d[i][j] - lse)) : 0.0f);
             }
             continue;
         }

@@ -30,7 +30,7 @@ enum Ragged {
 enum Ending {
     kStore,      // D, times scale where there is one, into out
     kStatistics, // of the values s = D over n: each tile's maximum and sum of exp(s - maximum), and s[m, label m]
-    kResidual,   // exp(s - lse m) - [n = label m], 0 where m has no label, times `factor`, into out
+    kResidual,   // exp(s - lse m), for n = label m exp(-row_loss m) - 1, 0 where m has no label, times `factor`, into out
 };
 
 struct Product {
@@ -57,7 +57,7 @@ struct Product {
     const int64_t* labels;       // [m]
     float2* parts;               // [n tiles][m]: kStatistics
     float* at_label;             // [m]: kStatistics
-    const float* lse;            // [m]: kResidual
+    const float *lse, *row_loss; // [m]: kResidual
     int64_t n0, classes;         // the first n of this piece, and how many there are of all pieces
 };
 

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(1024) loss_kernel(int64_t rows, const int64_t*
     int64_t count = 0;
     for (int64_t r = threadIdx.x; r < rows; r += 1024)
         if (has(r)) {
-            if (row_loss != nullptr) sum += row_loss[r];
+            sum += row_loss[r];
             ++count;
         }
     sum = fasgd::warp_sum(sum);
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(FewArgs a) {
                 u.row_loss[r] = row_loss;
                 if (u.lse != nullptr) u.lse[r] = lse;
             }
-            p = lane >= V ? 0.0f : lane == label ? expm1f(s - lse) : expf(s - lse);
+            p = lane >= V ? 0.0f : lane == label ? expm1f(u.known ? -u.row_loss[r] : -row_loss) : expf(s - lse);
         } else if (r < u.rows && lane == 0 && !u.known) {
             u.row_loss[r] = 0.0f;
             if (u.lse != nullptr) u.lse[r] = 0.0f;
@@ -327,9 +327,9 @@ int fill_score(const char* call, const fasgd_score_args& given, Score& s) {
     if (u.labels == nullptr || !aligned(u.labels, 8))
         return fail(FASGD_EINVAL, "%s: labels must not be NULL, and 8-byte aligned", call);
     if (u.known & ~1) return fail(FASGD_EINVAL, "%s: known is 0 or 1", call);
-    if (u.known ? u.lse == nullptr || !s.grad : u.loss == nullptr || u.row_loss == nullptr)
-        return fail(FASGD_EINVAL, "%s: loss and row_loss must not be NULL, or with a known lse: that, and dz or dw", call);
-    if (u.known) u.loss = u.row_loss = nullptr;
+    if (u.row_loss == nullptr || (u.known ? u.lse == nullptr || !s.grad : u.loss == nullptr))
+        return fail(FASGD_EINVAL, "%s: loss and row_loss must not be NULL; what is known: row_loss, lse, and dz or dw", call);
+    if (u.known) u.loss = nullptr;
     if (!aligned(u.loss, 4) || !aligned(u.row_loss, 4) || !aligned(u.lse, 4) || !aligned(u.upstream, 4))
         return fail(FASGD_EINVAL, "%s: loss, row_loss, lse and upstream must be 4-byte aligned", call);
     return FASGD_OK;
@@ -508,12 +508,16 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     p.dtype = dtype;
     p.planes = s.planes;
     p.ending = fasgd::kStatistics;
-    p.exact = 1;      // the log-sum-exps and losses are fp32
+    // The log-sum-exps and losses are fp32.  A row's own g, which for a row that is nearly sure of its
+    // label is a small difference, is taken from its loss, exp(-row_loss) - 1; in the others an s that is
+    // off by 2^-17 of itself is lost in g's rounding.
+    p.exact = 1;
     p.labels = u.labels;
     p.classes = u.classes;
     p.parts = s.parts;
     p.at_label = s.at_label;
     p.lse = s.lse;
+    p.row_loss = u.row_loss;
     if (!u.known && u.rows > 0) {
         st = fasgd::launch_product(p, nullptr, stream);
         if (st != cudaSuccess) return st;
@@ -531,7 +535,6 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         p.n = n;
         p.n0 = v;
         p.ending = fasgd::kResidual;
-        p.exact = s.planes;
         p.step_plane = s.plane_g;
         p.out = s.g;
         p.ld_out = s.ld_g;
@@ -604,7 +607,7 @@ int fasgd_score(const fasgd_score_args* u, void* stream) {
                         block("labels", u->labels, 8 * u->rows, false),
                         block("upstream", u->upstream, 4, false),
                         block("loss", s.u.loss, 4, true),
-                        block("row_loss", s.u.row_loss, 4 * u->rows, true),
+                        block("row_loss", u->row_loss, 4 * u->rows, !u->known),
                         block("lse", u->lse, 4 * u->rows, !u->known),
                         {"dz", u->dz, u->rows, u->cols * s.size, s.u.ld_dz * s.size, true},
                         classes("dw", u->dw, u->dw_flip, s.u.ld_dw, true),

@@ -641,6 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const int at = has && in >= 0 && in < count ? (int)in : -1;
             const bool mine = at >= 0 && (at >> 5 & 1) == odd;
             const float lse = ENDING == kResidual && has ? p.lse[m] : INFINITY;
+            const float own = ENDING == kResidual && mine ? target.factor * expm1f(-p.row_loss[m]) : 0.0f;
             const int64_t base = (ENDING == kStore ? (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * p.step_split : 0) +
                                  w.n0 * target.ld + m;
             // Columns c ... c + 31 of the tile into out.
@@ -653,12 +654,6 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     else
                         store_any(target, base + c * target.ld, w.n0 + c, min(32, count - c), live, x);
                     return;
-                }
-                float own = 0.0f;
-                if (__any_sync(0xffffffffu, mine && at >> 5 == c >> 5)) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (at == c + j) own = target.factor * expm1f(x[j] - lse);
                 }
                 if (!live) return;
                 const int own_at = mine ? at - c : -1;
@@ -897,7 +892,9 @@ cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
 }  // namespace
 
 bool tile_side(const Side& s, int64_t groups) {
-    return (reinterpret_cast<uintptr_t>(s.p) & 15) == 0 && s.ld % 8 == 0 && (groups < 2 || s.step % s.ld == 0);
+    constexpr int64_t kFar = (int64_t)1 << 38;      // values that a copy's steps can be apart, and more
+    return (reinterpret_cast<uintptr_t>(s.p) & 15) == 0 && s.ld % 8 == 0 && s.ld < kFar &&
+           (groups < 2 || (s.step % s.ld == 0 && s.step < kFar));
 }
 
 // The plan that should take the least time, by what was measured on a GB300: 64 k of a tile take a

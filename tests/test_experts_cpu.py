@@ -86,7 +86,7 @@ def test_score_refusals(f):  # noqa: F811
              dict(dtype=3), dict(z=None), dict(z=A + 1), dict(ld_z=39), dict(w=None), dict(w=B + 1), dict(ld_w=23), dict(w_flip=1), dict(w_flip=2),
              dict(dw_flip=1), dict(labels=None), dict(labels=C + 4), dict(loss=None), dict(row_loss=None), dict(loss=D + 2),
              dict(row_loss=D + 4097), dict(lse=D + 8193), dict(upstream=D + 1), dict(dz=E + 1), dict(ld_dz=1), dict(dw=F + 1), dict(ld_dw=23),
-             dict(known=2), dict(known=1, lse=None), dict(known=1, dz=None, dw=None)]
+             dict(known=2), dict(known=1, lse=None), dict(known=1, row_loss=None), dict(known=1, dz=None, dw=None)]
     refused(f, f.fasgd_score, good, every + [
         dict(workspace=None), dict(workspace=G + 128), dict(workspace_bytes=512), dict(dz=A), dict(dw=B + 48), dict(row_loss=C), dict(loss=D + 4096),
         dict(lse=D + 4000), dict(upstream=D), dict(workspace=F), dict(dw=E + 8)])
@@ -142,8 +142,9 @@ def calls(c):
     yield lambda v: c.multiply(v["x"], v["w"], v["offsets"], out=v["out"]), dict(x=new(12, 8), w=new(3, 8, 16), offsets=ints(4), out=new(12, 16))
     yield lambda v: c.multiply_grad(v["x"], v["w"], v["offsets"], v["dy"], into=c.MultiplyGrads(v["dx"], v["dw"])), \
         dict(x=new(12, 8), w=new(3, 8, 16), offsets=ints(4), dy=new(12, 16), dx=new(12, 8), dw=new(3, 8, 16))
-    yield lambda v: c.score(v["z"], v["w"], v["labels"], upstream=v["upstream"], lse=v["lse"], into=(v["dz"], v["dw"])), \
-        dict(z=new(6, 8), w=new(8, 16), labels=new(6, dtype=torch.int64), upstream=new(1), lse=new(6), dz=new(6, 8), dw=new(8, 16))
+    yield lambda v: c.score(v["z"], v["w"], v["labels"], upstream=v["upstream"], known=c.Score(None, v["rows"], None, None, v["lse"]),
+                            into=(v["dz"], v["dw"])), \
+        dict(z=new(6, 8), w=new(8, 16), labels=new(6, dtype=torch.int64), upstream=new(1), rows=new(6), lse=new(6), dz=new(6, 8), dw=new(8, 16))
 
 
 @pytest.mark.parametrize("where", ["cuda:1", "cpu"])
@@ -158,4 +159,4 @@ def test_tensors_of_another_device_are_refused(client, where):
                 with pytest.raises(ValueError, match="one device"):
                     call(v)
                 tried += 1
-    assert tried == (where == "cpu") + 4 + 5 + 7 + 4 + 6 + 7
+    assert tried == (where == "cpu") + 4 + 5 + 7 + 4 + 6 + 8

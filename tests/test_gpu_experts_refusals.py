@@ -23,6 +23,7 @@ def test_wrong_tensors_are_refused(client):  # noqa: F811
         "dweight": [new(5, 2), new(6, 2, dtype=torch.float16)],
         "upstream": [new(2), new(1, dtype=torch.float64)],
         "lse": [new(5), new(6, dtype=torch.float64)],
+        "rows": [new(7), new(12)[::2]],
     }
     tried = 0
     for call, tensors in calls(client):

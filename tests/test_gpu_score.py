@@ -116,8 +116,8 @@ def test_in_two_steps(dtype):
     # Rows without a label are copied as zeros before gradients, and their log-sum-exp is any value.
     kept = labels >= 0
     assert torch.equal(loss.lse[kept], s.lse[kept])
-    t = c.score(z, w, labels, lse=loss.lse)
-    assert t.loss is None and t.rows is None and torch.equal(t.dz, s.dz) and torch.equal(t.dw, s.dw)
+    t = c.score(z, w, labels, known=loss)
+    assert t.loss is loss.loss and t.rows is loss.rows and torch.equal(t.dz, s.dz) and torch.equal(t.dw, s.dw)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -163,6 +163,33 @@ def test_sure_and_hopeless_rows(dtype):
     third = torch.tensor([0.0, 16.0, 16.0], device="cuda") / 3
     assert torch.equal(s.dz[:, 5].float(), third.to(dtype).float())
     assert float(s.dz[1, 6]) == float(torch.tensor(-16.0 / 3).to(dtype)) and not s.dz[0].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_of_sure_rows(dtype):
+    """Rows that are nearly certain of their class, 1 - p of some 1e-4: their gradients are made of s - lse,
+    whose error is the fp32 sums' and not that of a rounded or cut one.  With |s| near 24 that is 512 2^-23
+    sum |z| |w| in the worst case; the sums of the formula's random signs stay below 2^-17 of it in all."""
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(7)
+    R, D, V = 256, 2048, 1024
+    w = (torch.randn(V, D, generator=g, device="cuda") * D ** -0.5).to(dtype)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda")
+    z = (torch.randn(R, D, generator=g, device="cuda") * 0.5 + 17.0 * w[labels].float()).to(dtype)
+    logits = z.double() @ w.double().t()
+    p = torch.softmax(logits, 1)
+    sure = 1.0 - p.gather(1, labels[:, None])[:, 0]
+    assert 1e-6 < float(sure.median()) < 1e-2
+    p[torch.arange(R, device="cuda"), labels] -= 1.0
+    # s - lse is off by some 2^-17: as much of 1 - p relative to 1 - p itself, which is 1e-4 or so, would be
+    # 8 %; the sums' actual errors are a few 2^-24 of 17.  fp16 values this small (1e-8) lie between
+    # multiples of 2^-24, off by up to half of it each, unless the loss is scaled up as it is for fp16.
+    for scale in (1.0, 65536.0):
+        s = c.score(z, w.t(), labels, upstream=torch.tensor([scale], device="cuda"))
+        dz = p @ w.double() / R * scale
+        off = (s.dz.double() - dz).norm() / dz.norm()
+        steps = TINY[dtype] / 2 * dz.numel() ** 0.5 / float(dz.norm())
+        assert float(off) <= 2 * UNIT[dtype] + 64 * 2.0 ** -24 * 17 / float(sure.square().mean().sqrt()) + steps
 
 
 def test_pieces(monkeypatch):
