@@ -88,10 +88,10 @@ __global__ void __launch_bounds__(256) fold_kernel(Product p, const float* parts
     const float* from = parts + g * p.n * p.m;
     const float one = p.scale != nullptr && !p.by_n ? *p.scale * p.factor : p.factor;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.n * p.m; i += (int64_t)gridDim.x * 256) {
-        const int64_t n = i / p.m;
+        const int64_t n = i / p.m, at = p.row_of != nullptr ? i + (p.row_of[n] - n) * p.m : i;
         float v = 0.0f;
         if (n >= rows.lo && n < rows.hi)
-            for (int s = 0; s < count; ++s) v += from[s * step + i];
+            for (int s = 0; s < count; ++s) v += from[s * step + at];
         if (p.by_n) {
             const float scale = p.scale[n];
             v = scale == 0.0f ? 0.0f : v * (scale * p.factor);
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(256) pack_kernel(Pack p) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = j < most ? from[j] : from_f32<F>(0.0f);
         }
-        T* to = static_cast<T*>(p.to) + g * p.step_to + r * p.ld_to + c;
+        T* to = static_cast<T*>(p.to) + g * p.step_to + (p.to_row != nullptr ? p.to_row[r] : r) * p.ld_to + c;
         alignas(16) T out[PLANES ? 3 : 1][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

@@ -27,6 +27,7 @@ enum Ragged {
     kRaggedN,    // n counts rows of all groups: group g has offsets[g] <= n < offsets[g + 1], B and D go by them, A by groups
     kRaggedK,    // so does k: A and B go by rows, D by groups
 };
+enum Live { kLiveM, kLiveN, kLiveK };
 enum Ending {
     kStore,      // D, times scale where there is one, into out
     kStatistics, // of the values s = D over n: each tile's maximum and sum of exp(s - maximum), and s[m, label m]
@@ -53,6 +54,11 @@ struct Product {
     const float* scale;          // kStore: one value, or (by_n) one for each n, whose 0 makes its values 0
     int32_t by_n;
     float factor;                // kStore, kResidual: a power of two, on top
+    // Where not all of m, n or k take part, how many do is known on the device (null: all).  What lies
+    // behind them in the sides is 0 as far as a stage reaches.
+    const int32_t* live;
+    int32_t live_of;             // enum Live
+    const int32_t* row_of;       // launch_fold: n's sums are those of row_of[n] (null: of n)
     // kStatistics, kResidual
     const int64_t* labels;       // [m]
     float2* parts;               // [n tiles][m]: kStatistics
@@ -140,6 +146,7 @@ struct Pack {
     const int32_t* offsets;
     const int64_t* labels;
     int64_t classes;
+    const int32_t* to_row;       // row r goes to row to_row[r] (null: r)
 };
 cudaError_t launch_pack(const Pack& p, cudaStream_t stream);
 

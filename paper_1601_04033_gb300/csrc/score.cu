@@ -33,6 +33,11 @@ struct Score {
     float* few_dw;
     bool planes;                 // fp32 by planes on the tensor cores
     int64_t plane_z, plane_w, plane_g;
+    // Rows that have labels first, where the tensor cores take many rows: what has none costs nothing.
+    bool first;
+    int32_t *to_row, *row_at, *live;     // [rows] each row's place and back, [1] how many have labels
+    int64_t* labels;                     // [rows] by place
+    float* loss_at;                      // [rows] by place (lse too)
     // workspace
     void* z_copy;                // rows x ld_zc (null: z itself serves)
     int64_t ld_zc;
@@ -54,10 +59,10 @@ struct Score {
 // lse and the row's loss from the tiles' parts: ROWS rows a block, 256 / ROWS threads each, every one
 // four parts at a time (few rows have more threads: one row's 1,024 parts took 8 of them 23 us).
 template <int ROWS>
-__global__ void __launch_bounds__(256) lse_kernel(const float2* parts, int64_t tiles, int64_t rows, const int64_t* labels,
-                                                  int64_t classes, const float* at_label, float* lse, float* row_loss) {
+__global__ void __launch_bounds__(256) lse_kernel(Score s) {
     constexpr int kEach = 256 / ROWS;
     __shared__ float2 shared[kEach][ROWS];
+    const int64_t rows = s.u.rows, tiles = (s.u.classes + s.tile - 1) / s.tile, live = s.first ? *s.live : rows;
     const int x = threadIdx.x % ROWS, y = threadIdx.x / ROWS;
     const int64_t r = (int64_t)blockIdx.x * ROWS + x;
     float top = -INFINITY, sum = 0.0f;
@@ -66,11 +71,12 @@ __global__ void __launch_bounds__(256) lse_kernel(const float2* parts, int64_t t
         sum = (top == most ? sum : sum * expf(top - most)) + (p.x == most ? p.y : p.y * expf(p.x - most));
         top = most;
     };
-    if (r < rows)
+    if (r < live)
         for (int64_t j = y; j < tiles; j += 4 * kEach) {
             float2 p[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = j + i * kEach < tiles ? parts[(j + i * kEach) * rows + r] : make_float2(-INFINITY, 0.0f);
+            for (int i = 0; i < 4; ++i)
+                p[i] = j + i * kEach < tiles ? s.parts[(j + i * kEach) * rows + r] : make_float2(-INFINITY, 0.0f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) join(p[i]);
         }
@@ -83,19 +89,69 @@ __global__ void __launch_bounds__(256) lse_kernel(const float2* parts, int64_t t
             shared[y][x] = make_float2(top, sum);
         }
     }
-    if (y == 0 && r < rows) {
-        const float log_sum = logf(sum);
-        const int64_t label = labels[r];
-        lse[r] = top + log_sum;
-        row_loss[r] = label >= 0 && label < classes ? (top - at_label[r]) + log_sum : 0.0f;
+    if (y == 0 && r < live) {
+        const float log_sum = logf(sum), lse = top + log_sum;
+        const int64_t label = (s.first ? s.labels : s.u.labels)[r];
+        const float loss = label >= 0 && label < s.u.classes ? (top - s.at_label[r]) + log_sum : 0.0f;
+        s.lse[r] = lse;
+        if (s.first) {
+            const int64_t at = s.row_at[r];
+            s.loss_at[r] = loss;
+            s.u.row_loss[at] = loss;
+            if (s.u.lse != nullptr) s.u.lse[at] = lse;
+        } else {
+            s.u.row_loss[r] = loss;
+        }
     }
 }
 template <int ROWS>
-cudaError_t launch_lse(const float2* parts, int64_t tiles, int64_t rows, const int64_t* labels, int64_t classes,
-                       const float* at_label, float* lse, float* row_loss, cudaStream_t stream) {
-    lse_kernel<ROWS><<<(unsigned)((rows + ROWS - 1) / ROWS), 256, 0, stream>>>(parts, tiles, rows, labels, classes, at_label, lse,
-                                                                               row_loss);
+cudaError_t launch_lse(const Score& s, cudaStream_t stream) {
+    lse_kernel<ROWS><<<(unsigned)((s.u.rows + ROWS - 1) / ROWS), 256, 0, stream>>>(s);
     return cudaGetLastError();
+}
+
+// The rows' places, those that have labels first, in their order: one block.  What rows without one
+// leave behind is written here, and what is known of the others goes to their places.
+__global__ void __launch_bounds__(1024) first_kernel(fasgd_score_args u, Score s) {
+    __shared__ int32_t counts[32];
+    __shared__ int32_t total;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const auto has = [&](int64_t r) { return r < u.rows && u.labels[r] >= 0 && u.labels[r] < u.classes; };
+    int32_t n = 0;
+    for (int64_t r = threadIdx.x; r < u.rows; r += 1024) n += has(r);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) counts[warp] = n;
+    __syncthreads();
+    if (warp == 0) {
+        n = __reduce_add_sync(0xffffffffu, counts[lane]);
+        if (lane == 0) *s.live = total = n;
+    }
+    int32_t before = 0;                              // labels in earlier rounds
+    for (int64_t r0 = 0; r0 < u.rows; r0 += 1024) {
+        const int64_t r = r0 + threadIdx.x;
+        const bool is = has(r);
+        const uint32_t votes = __ballot_sync(0xffffffffu, is);
+        __syncthreads();
+        if (lane == 0) counts[warp] = __popc(votes);
+        __syncthreads();
+        const int32_t of = counts[lane];             // this round's warps
+        const int32_t earlier = __reduce_add_sync(0xffffffffu, lane < warp ? of : 0), all = __reduce_add_sync(0xffffffffu, of);
+        if (r < u.rows) {
+            const int32_t rank = before + earlier + __popc(votes & ((1u << lane) - 1u));
+            const int32_t to = is ? rank : total + (int32_t)(r - rank);
+            s.to_row[r] = to;
+            s.row_at[to] = (int32_t)r;
+            s.labels[to] = is ? u.labels[r] : -1;
+            if (u.known) {
+                s.lse[to] = is ? u.lse[r] : 0.0f;
+                s.loss_at[to] = is ? u.row_loss[r] : 0.0f;
+            } else if (!is) {
+                u.row_loss[r] = 0.0f;
+                if (u.lse != nullptr) u.lse[r] = 0.0f;
+            }
+        }
+        before += all;
+    }
 }
 
 // The loss, upstream / N, and what each row's gradient is multiplied by: one block.
@@ -357,6 +413,8 @@ Product product_dz(const Score& s, int64_t n) {
         q.out = s.dz_sum;
         q.ld_out = u.cols;
         q.step_split = u.rows * u.cols;
+        q.live = s.first ? s.live : nullptr;
+        q.live_of = fasgd::kLiveN;
         q.out_dtype = FASGD_F32;
         q.factor = 1.0f;
         q.add = 1;      // (a plan for sums that are read again)
@@ -377,6 +435,8 @@ Product product_dw(const Score& s, int64_t n) {
     q.m = u.dw_flip ? u.cols : n;
     q.n = u.dw_flip ? n : u.cols;
     q.k = u.rows;
+    q.live = s.first ? s.live : nullptr;
+    q.live_of = fasgd::kLiveK;
     q.ld_out = u.ld_dw;
     q.scale = s.share;
     return q;
@@ -399,11 +459,20 @@ int64_t lay_out(Score& s, char* base) {
     s.planes = u.dtype == FASGD_F32 && fasgd::by_planes(u.rows, u.classes, u.cols);
     s.tile = u.dtype == FASGD_F32 && !s.planes ? fasgd::kPlainN : fasgd::statistics_tile(u.rows, u.classes);
     const int64_t tiles = (u.classes + s.tile - 1) / s.tile;
+    // (512 rows are two tiles; of fewer none would be saved)
+    s.first = (u.dtype != FASGD_F32 || s.planes) && u.rows > 512;
+    if (s.first) {
+        s.to_row = reinterpret_cast<int32_t*>(take(4 * u.rows));
+        s.row_at = reinterpret_cast<int32_t*>(take(4 * u.rows));
+        s.live = reinterpret_cast<int32_t*>(take(4));
+        s.labels = reinterpret_cast<int64_t*>(take(8 * u.rows));
+        s.loss_at = reinterpret_cast<float*>(take(4 * u.rows));
+    }
     if (!u.known) {
         s.parts = reinterpret_cast<float2*>(take(8 * tiles * u.rows));
         s.at_label = reinterpret_cast<float*>(take(4 * u.rows));
     }
-    s.lse = u.lse != nullptr ? u.lse : reinterpret_cast<float*>(take(4 * u.rows));
+    s.lse = u.lse != nullptr && !s.first ? u.lse : reinterpret_cast<float*>(take(4 * u.rows));
     // Gradients' sums over rows need zeros where there is no label; 16-bit products, rows that
     // start on 16 bytes.
     s.z_copy = s.w_copy = nullptr;
@@ -416,7 +485,7 @@ int64_t lay_out(Score& s, char* base) {
         plane = values;
         return take(s.planes ? 6 * values : values * s.size);
     };
-    if (s.grad || !fits(u.z, u.ld_z)) {
+    if (s.grad || s.first || !fits(u.z, u.ld_z)) {
         s.ld_zc = (u.cols + 7) / 8 * 8;
         s.z_copy = copy(u.rows * s.ld_zc, s.plane_z);
     }
@@ -429,7 +498,7 @@ int64_t lay_out(Score& s, char* base) {
     if (!s.grad) return at;
     s.share = reinterpret_cast<float*>(take(4));
     s.row_scale = reinterpret_cast<float*>(take(4 * u.rows));
-    s.ld_g = (u.rows + 7) / 8 * 8;
+    s.ld_g = (u.rows + 63) / 64 * 64;      // (a stage of rows)
     const int64_t g_size = s.planes ? 6 : s.size;
     const int64_t most = std::max<int64_t>(64, FASGD_SCORE_PIECE / std::max<int64_t>(1, s.ld_g * g_size));
     const int64_t pieces = (u.classes + most - 1) / most;
@@ -441,7 +510,7 @@ int64_t lay_out(Score& s, char* base) {
     s.dz_sum = nullptr;
     s.dz_parts = 1;
     if (u.dz != nullptr && u.rows > 0) {
-        if (s.piece < u.classes) {
+        if (s.piece < u.classes || s.first) {
             s.dz_sum = reinterpret_cast<float*>(16);      // (that there is one counts)
             const Product q = product_dz(s, s.piece);
             if (q.dtype != FASGD_F32) s.dz_parts = fasgd::plan_tiles(q).splits;
@@ -471,6 +540,10 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         return u.dtype == FASGD_F32 ? run_few<float>(a, stream)
                : u.dtype == FASGD_BF16 ? run_few<__nv_bfloat16>(a, stream) : run_few<__half>(a, stream);
     }
+    if (s.first) {
+        first_kernel<<<1, 1024, 0, stream>>>(s.u, s);
+        if ((st = cudaGetLastError()) != cudaSuccess) return st;
+    }
     const void *z = s.z, *w_all = s.w;
     const int64_t ld_z = s.ld_zc, ld_w = s.ld_wc;
     fasgd::Pack c = {};
@@ -496,6 +569,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         c.plane = s.planes ? s.plane_z : 0;
         c.labels = u.labels;
         c.classes = u.classes;
+        c.to_row = s.first ? s.to_row : nullptr;
         if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
     }
     Product p = {};
@@ -512,17 +586,19 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
     // label is a small difference, is taken from its loss, exp(-row_loss) - 1; in the others an s that is
     // off by 2^-17 of itself is lost in g's rounding.
     p.exact = 1;
-    p.labels = u.labels;
+    p.live = s.first ? s.live : nullptr;
+    p.live_of = fasgd::kLiveM;
+    p.labels = s.first ? s.labels : u.labels;
     p.classes = u.classes;
     p.parts = s.parts;
     p.at_label = s.at_label;
     p.lse = s.lse;
-    p.row_loss = u.row_loss;
+    p.row_loss = s.first ? s.loss_at : u.row_loss;
     if (!u.known && u.rows > 0) {
         st = fasgd::launch_product(p, nullptr, stream);
         if (st != cudaSuccess) return st;
         const auto launch = u.rows >= 4096 ? launch_lse<32> : u.rows >= 64 ? launch_lse<8> : launch_lse<1>;
-        st = launch(s.parts, (u.classes + s.tile - 1) / s.tile, u.rows, u.labels, u.classes, s.at_label, s.lse, u.row_loss, stream);
+        st = launch(s, stream);
         if (st != cudaSuccess) return st;
     }
     loss_kernel<<<1, 1024, 0, stream>>>(u.rows, u.labels, u.classes, u.row_loss, u.upstream, u.loss, s.share, s.row_scale);
@@ -571,6 +647,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         q.scale = s.row_scale;
         q.by_n = 1;
         q.factor = 1.0f / s.factor;
+        q.row_of = s.first ? s.to_row : nullptr;
         st = fasgd::launch_fold(q, s.dz_sum, u.rows * u.cols, s.dz_parts, stream);
     }
     return st;

@@ -252,15 +252,33 @@ __device__ void count_tiles(const Product& p, Shared& s) {
     }
 }
 
+// What takes part of n and k, and the tiles of it.
+struct Sizes {
+    int64_t n, k, m_tiles, items;
+};
+template <int PAIR>
+__device__ __forceinline__ Sizes sizes_of(const TileArgs& t, const Shared& s) {
+    const Product& p = t.p;
+    Sizes z = {p.n, p.k, t.m_tiles, t.items};
+    if (p.live != nullptr) {
+        const int64_t live = *p.live;
+        if (p.live_of == kLiveM) z.m_tiles = (min(p.m, live) + kBlockM * PAIR - 1) / (kBlockM * PAIR);
+        if (p.live_of == kLiveN) z.n = min(p.n, live);
+        if (p.live_of == kLiveK) z.k = min(p.k, live);
+        z.items = z.m_tiles * ((z.n + t.tile_n - 1) / t.tile_n) * t.splits;
+    }
+    if (p.ragged == kRaggedN) z.items = (int64_t)s.first[p.groups] * t.m_tiles * t.splits;
+    return z;
+}
 // Item i of the product; ragged n: i counts m tiles first, then the groups' n tiles.
 template <int PAIR>
-__device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, int64_t i) {
+__device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, const Sizes& z, int64_t i) {
     const Product& p = t.p;
     Tile w;
     w.split = 0;
     w.group = 0;
     w.k0 = 0;
-    w.k1 = p.k;
+    w.k1 = z.k;
     if (t.splits > 1) {
         w.split = (int32_t)(i % t.splits);
         i /= t.splits;
@@ -282,7 +300,7 @@ __device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, int6
         w.n0 = b.lo + (j - s.first[lo]) * kTileN;
         w.n1 = min(b.hi, w.n0 + kTileN);
     } else {
-        const int64_t n_tiles = (p.n + t.tile_n - 1) / t.tile_n;
+        const int64_t n_tiles = (z.n + t.tile_n - 1) / t.tile_n;
         if (p.ragged == kRaggedK) {
             w.group = (int32_t)(i / (t.m_tiles * n_tiles));
             i -= (int64_t)w.group * t.m_tiles * n_tiles;
@@ -291,12 +309,12 @@ __device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, int6
             w.k1 = b.hi;
         }
         // Bands of up to 32 m tiles, by n: what runs at the same time shares its operands in L2.
-        const int64_t band = i / (32 * n_tiles), m_first = band * 32, high = min((int64_t)32, t.m_tiles - m_first);
+        const int64_t band = i / (32 * n_tiles), m_first = band * 32, high = min((int64_t)32, z.m_tiles - m_first);
         i -= band * 32 * n_tiles;
         w.n_tile = i / high;
         w.m0 = (m_first + i - w.n_tile * high) * (kBlockM * PAIR);
         w.n0 = w.n_tile * t.tile_n;
-        w.n1 = min(p.n, w.n0 + t.tile_n);
+        w.n1 = min(z.n, w.n0 + t.tile_n);
     }
     if (t.splits > 1) {
         const int64_t blocks = (w.k1 - w.k0 + kK - 1) / kK, k0 = w.k0;
@@ -332,11 +350,6 @@ __device__ __forceinline__ Boxes boxes_of(const TileArgs& t, const Tile& w) {
 __device__ __forceinline__ bool cut(const Product& p, const Tile& w, int64_t k) {
     return p.ragged == kRaggedK && w.k1 - k < kK;
 }
-template <int PAIR>
-__device__ __forceinline__ int64_t items_of(const TileArgs& t, const Shared& s) {
-    return t.p.ragged == kRaggedN ? (int64_t)s.first[t.p.groups] * t.m_tiles * t.splits : t.items;
-}
-
 // ---- what becomes of an accumulator -----------------------------------------------------
 // What the stores need, in registers: read again from the kernel's parameters after each of
 // them (which might alias, for all the compiler knows) it made 180 cycles a column.
@@ -447,7 +460,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     fence_after();
     const uint32_t tmem = *(volatile uint32_t*)&s.tmem;
     const uint32_t pairs = p.planes ? kPairs : 1;
-    const int64_t items = items_of<PAIR>(t, s), team = blockIdx.x / PAIR, teams = gridDim.x / PAIR;
+    const Sizes sizes = sizes_of<PAIR>(t, s);
+    const int64_t items = sizes.items, team = blockIdx.x / PAIR, teams = gridDim.x / PAIR;
 
     // 384 threads are launched with 168 registers; 128 x 56 + 256 x 216 are fewer.
     if (warp < 4) {
@@ -460,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 uint32_t stage = 0, phase = 0;
                 bool ok = true;
                 for (int64_t i = team; i < items && ok; i += teams) {
-                    const Tile w = tile_of<PAIR>(t, s, i);
+                    const Tile w = tile_of<PAIR>(t, s, sizes, i);
                     const Boxes x = boxes_of<PAIR>(t, w);
                     const int32_t m0 = (int32_t)(w.m0 + rank * kBlockM), n0 = (int32_t)(w.n0 + (int64_t)rank * x.rows_b);
                     const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
@@ -510,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 uint32_t copies = 0, used = 0;      // copies: modulo the stages
                 bool ok = true;
                 for (int64_t i = team; i < items && ok; i += teams) {
-                    const Tile w = tile_of<PAIR>(t, s, i);
+                    const Tile w = tile_of<PAIR>(t, s, sizes, i);
                     const int rows = (int)((w.k1 - w.k0) % kK);
                     for (uint32_t pair = 0; pair < pairs && w.k0 < w.k1 && ok; ++pair) {
                         copies = (uint32_t)((copies + (w.k1 - w.k0 + kK - 1) / kK) % S::kStages);
@@ -555,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const auto look = [&] {
                 blocks = 0;
                 while (blocks == 0 && (i += teams) < items) {
-                    const Tile w = tile_of<PAIR>(t, s, i);
+                    const Tile w = tile_of<PAIR>(t, s, sizes, i);
                     if (w.k0 >= w.k1) continue;
                     blocks = (int)((w.k1 - w.k0 + kK - 1) / kK);
                     last = (int)((w.k1 - w.k0 + 15) / 16) - (blocks - 1) * (kK / 16);
@@ -616,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         uint32_t tile = 0, turn = 0;
         bool ok = true;
         for (int64_t i = team; i < items; i += teams, turn ^= 1) {
-            const Tile w = tile_of<PAIR>(t, s, i);
+            const Tile w = tile_of<PAIR>(t, s, sizes, i);
             const int64_t m = w.m0 + rank * kBlockM + quarter * 32 + lane;
             const bool live = m < p.m;
             const int count = (int)(w.n1 - w.n0);

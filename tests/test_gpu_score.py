@@ -50,6 +50,7 @@ def check(c, z, w, labels, upstream=None):
     assert not rows[~kept].any()
     assert bool(((rows[k] - want).abs() <= off).all()), float(((rows[k] - want).abs() - off).max())
     assert bool(((s.lse.double()[k] - lse).abs() <= off).all())
+    assert s.dz.isfinite().all() and s.dw.isfinite().all()
     n = max(1, k.numel())
     assert abs(float(s.loss) - float(want.sum() / n)) <= float(off.sum() / n + 2.0 ** -20 * (want.abs().sum() / n)) + 1e-30
     # gradients
@@ -138,6 +139,28 @@ def test_rows_without_labels(dtype):
     assert torch.equal(e.loss, s.loss) and torch.equal(e.rows, s.rows)
     t = c.score(z, w, torch.full_like(labels, -1))
     assert float(t.loss) == 0.0 and not t.rows.any() and not t.dz.any() and not t.dw.any()
+
+
+@pytest.mark.parametrize("kept", [0, 1, 63, 64, 256, 512, 700, 1299])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_without_labels(dtype, kept):
+    """Any number of many rows that have labels, anywhere among NaNs: their results, zeros elsewhere, and
+    the same from what is known of them."""
+    c = _c()
+    z, w, labels = case(1299, 264, 1000, dtype, True, 8, drop=0.0)
+    out = torch.randperm(1299, generator=torch.Generator().manual_seed(kept))[kept:].cuda()
+    labels[out] = torch.where(out % 2 == 0, -1, 1 << 33)
+    zeroed = z.clone()
+    zeroed[out] = 0.0
+    s = check(c, zeroed, w, labels)
+    z[out] = float("nan")
+    t = c.score(z, w, labels)
+    on = labels.lt(1000) & labels.ge(0)
+    assert all(torch.equal(p, q) for p, q in zip(s[:4], t[:4])) and torch.equal(s.lse[on], t.lse[on])
+    e = c.score(z, w, labels, grad=False)
+    assert torch.equal(e.loss, s.loss) and torch.equal(e.rows, s.rows)
+    again = c.score(z, w, labels, known=e)
+    assert torch.equal(again.dz, s.dz) and torch.equal(again.dw, s.dw)
 
 
 def test_no_rows():
