@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "client.cuh"
+#include "pdl.cuh"
 #include "product.cuh"
 
 namespace fasgd {
@@ -83,6 +84,8 @@ __device__ bool find_tile(const Product& p, int64_t tile, int64_t& group, Bounds
 // Parts of k's sums into a product's result.
 __global__ void __launch_bounds__(256) fold_kernel(Product p, const float* parts, int64_t step, int32_t count) {
     const int64_t g = blockIdx.y;
+    pdl_wait();
+    pdl_trigger();
     Bounds rows = {0, p.n};
     if (p.ragged == kRaggedN) rows = {group_bounds(p.offsets, 0, p.n).lo, group_bounds(p.offsets, p.groups - 1, p.n).hi};
     const float* from = parts + g * p.n * p.m;
@@ -216,6 +219,8 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
 template <class F, class T, bool WIDE, bool PLANES>
 __global__ void __launch_bounds__(256) pack_kernel(Pack p) {
     const int64_t g = blockIdx.y, octets = (p.cols + 7) / 8, all = p.rows * octets;
+    pdl_wait();
+    pdl_trigger();
     if (p.offsets != nullptr && p.offsets[g + 1] <= p.offsets[g]) return;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const int64_t r = all >> 31 ? i / octets : (int64_t)((uint32_t)i / (uint32_t)octets), c = (i - r * octets) * 8;
@@ -260,11 +265,7 @@ cudaError_t pack(const Pack& p, cudaStream_t stream) {
     const bool wide = (reinterpret_cast<uintptr_t>(p.from) & 15) == 0 && p.ld_from % kStep == 0 &&
                       (p.groups < 2 || p.step_from % kStep == 0);
     const dim3 grid((unsigned)blocks, (unsigned)p.groups);
-    if (wide)
-        pack_kernel<F, T, true, PLANES><<<grid, 256, 0, stream>>>(p);
-    else
-        pack_kernel<F, T, false, PLANES><<<grid, 256, 0, stream>>>(p);
-    return cudaGetLastError();
+    return launch_pdl(wide ? pack_kernel<F, T, true, PLANES> : pack_kernel<F, T, false, PLANES>, grid, dim3(256), 0, stream, p);
 }
 
 }  // namespace
@@ -285,8 +286,7 @@ cudaError_t launch_pack(const Pack& p, cudaStream_t stream) {
 cudaError_t launch_fold(const Product& p, const float* parts, int64_t step, int32_t count, cudaStream_t stream) {
     if (p.n * p.m == 0) return cudaSuccess;
     const dim3 grid((unsigned)std::min<int64_t>((p.n * p.m + 255) / 256, 1 << 14), p.ragged == kRaggedK ? p.groups : 1);
-    fold_kernel<<<grid, 256, 0, stream>>>(p, parts, step, count);
-    return cudaGetLastError();
+    return launch_pdl(fold_kernel, grid, dim3(256), 0, stream, p, parts, step, count);
 }
 
 cudaError_t launch_plain(const Product& p, cudaStream_t stream) {

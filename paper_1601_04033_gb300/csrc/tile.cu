@@ -24,6 +24,7 @@
 #include <algorithm>
 
 #include "client.cuh"
+#include "pdl.cuh"
 #include "product.cuh"
 #include "shared_limit.cuh"
 #include "wait.cuh"
@@ -226,9 +227,10 @@ struct Shared {
     uint32_t tmem;
     volatile int32_t late;
     int32_t first[kMaxGroups + 1];      // ragged n: the first n tile of each group
+    int32_t lo[kMaxGroups], hi[kMaxGroups];      // ragged products: the groups' rows
 };
 
-// first[] of the groups, by the first warp.  Offsets that rise and fall may claim more rows than
+// lo, hi and first[] of the groups, by the first warp.  Offsets that rise and fall may claim more rows than
 // there are: numbers stay within 31 bits all the same.
 __device__ void count_tiles(const Product& p, Shared& s) {
     if (threadIdx.x < 32) {
@@ -236,7 +238,9 @@ __device__ void count_tiles(const Product& p, Shared& s) {
         for (int g = threadIdx.x; g < (p.groups + 31) / 32 * 32; g += 32) {
             int64_t tiles = 0;
             if (g < p.groups) {
-                const Bounds b = group_bounds(p.offsets, g, p.n);
+                const Bounds b = group_bounds(p.offsets, g, p.ragged == kRaggedN ? p.n : p.k);
+                s.lo[g] = (int32_t)b.lo;
+                s.hi[g] = (int32_t)b.hi;
                 tiles = (b.hi - b.lo + kTileN - 1) / kTileN;
             }
             int64_t sum = tiles;
@@ -294,19 +298,17 @@ __device__ __forceinline__ Tile tile_of(const TileArgs& t, const Shared& s, cons
             else
                 hi = mid;
         }
-        const Bounds b = group_bounds(p.offsets, lo, p.n);
         w.group = lo;
         w.n_tile = j;
-        w.n0 = b.lo + (j - s.first[lo]) * kTileN;
-        w.n1 = min(b.hi, w.n0 + kTileN);
+        w.n0 = s.lo[lo] + (j - s.first[lo]) * kTileN;
+        w.n1 = min((int64_t)s.hi[lo], w.n0 + kTileN);
     } else {
         const int64_t n_tiles = (z.n + t.tile_n - 1) / t.tile_n;
         if (p.ragged == kRaggedK) {
             w.group = (int32_t)(i / (t.m_tiles * n_tiles));
             i -= (int64_t)w.group * t.m_tiles * n_tiles;
-            const Bounds b = group_bounds(p.offsets, w.group, p.k);
-            w.k0 = b.lo;
-            w.k1 = b.hi;
+            w.k0 = s.lo[w.group];
+            w.k1 = s.hi[w.group];
         }
         // Bands of up to 32 m tiles, by n: what runs at the same time shares its operands in L2.
         const int64_t band = i / (32 * n_tiles), m_first = band * 32, high = min((int64_t)32, z.m_tiles - m_first);
@@ -406,8 +408,8 @@ __device__ __forceinline__ void store_any(const Target& g, int64_t at, int64_t n
 }
 
 // Rows of y or dx that no group has.
-__device__ void clear_rows(const Product& p, int64_t block, int64_t blocks, int thread, int threads) {
-    const int64_t lo = group_bounds(p.offsets, 0, p.n).lo, hi = group_bounds(p.offsets, p.groups - 1, p.n).hi;
+__device__ void clear_rows(const Product& p, const Shared& s, int64_t block, int64_t blocks, int thread, int threads) {
+    const int64_t lo = s.lo[0], hi = s.hi[p.groups - 1];
     for (int64_t r = block; r < p.n - (hi - lo); r += blocks) {
         const int64_t at = (r < lo ? r : hi + (r - lo)) * p.ld_out;
         for (int64_t m = thread; m < p.m; m += threads) {
@@ -430,6 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     const uint32_t rank = PAIR == 2 ? block_rank() : 0;
 
     if (threadIdx.x == 0) {
+        for (const CUtensorMap* map : {&t.a, &t.b, &t.few}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(&s.full[i], PAIR);
             mbar_init(&s.empty[i], 1);
@@ -450,7 +453,10 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s.tmem)), "n"(kColumns)
                          : "memory");
     }
-    if (p.ragged == kRaggedN) count_tiles(p, s);
+    // Nothing in global memory is touched before the kernels before this one have ended.
+    pdl_wait();
+    pdl_trigger();
+    if (p.ragged != kNotRagged) count_tiles(p, s);
     fence_before();
     __syncthreads();
     if (PAIR == 2) {
@@ -626,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
         const int quarter = warp & 3, odd = (warp - 4) >> 2;
         const float more = log2f(p.factor);
         const Target target = {p.out, p.ld_out, p.scale, p.factor, p.by_n, p.out_dtype, p.add};
-        if (p.ragged == kRaggedN) clear_rows(p, blockIdx.x, gridDim.x, threadIdx.x - 128, 32 * kEnds);
+        if (p.ragged == kRaggedN) clear_rows(p, s, blockIdx.x, gridDim.x, threadIdx.x - 128, 32 * kEnds);
         uint32_t tile = 0, turn = 0;
         bool ok = true;
         for (int64_t i = team; i < items; i += teams, turn ^= 1) {
@@ -868,12 +874,14 @@ cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStr
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = PAIR;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING, EXACT>, t);
 }
 template <int PAIR>
@@ -913,7 +921,7 @@ bool tile_side(const Side& s, int64_t groups) {
 
 // The plan that should take the least time, by what was measured on a GB300: 64 k of a tile take a
 // block or a pair 0.27 us times the n of the tile over 256 (a block alone a quarter more), and no less
-// than 80 GB/s and SM copy its sides in; parts of k cost their sums' way through memory and a launch.
+// than 50 GB/s and SM copy its sides in; parts of k cost their sums' way through memory and a launch.
 TilePlan plan_tiles(const Product& p) {
     constexpr int kSms = 152;
     const bool rows = p.ragged == kRaggedN;
@@ -929,7 +937,7 @@ TilePlan plan_tiles(const Product& p) {
         const int64_t tiles = (p.m + kBlockM * pair - 1) / (kBlockM * pair) * n_tiles * (p.ragged == kRaggedK ? groups : 1);
         const int teams = kSms / pair;
         const double each = std::max(0.27 * width / 256.0 * (pair == 1 ? 1.25 : 1.0),
-                                     (kSideA + std::max(width / pair, 32.0) * kK * 2) / 80e3);
+                                     (kSideA + std::max(width / pair, 32.0) * kK * 2) / 50e3);
         for (int splits = 1; splits <= 16 && (splits == 1 || (p.ending == kStore && blocks >= 8 * splits)); ++splits) {
             const double waves = (double)((tiles * splits + teams - 1) / teams);
             double time = waves * (double)((blocks + splits - 1) / splits) * each;
