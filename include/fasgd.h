@@ -764,6 +764,8 @@ FASGD_API int fasgd_combine_grad(const fasgd_exchange_args* a, void* stream);
  * Sums are fp32, in an order that the arguments fix.  Rows that no expert has are not
  * read, whatever they hold.
  * rows < 2^31; inputs, outputs <= FASGD_COLS_MAX; experts <= FASGD_EXPERTS_MAX.
+ * Fastest are bases and ld of multiples of 16 bytes: 16-bit matrices that lie otherwise are copied
+ * first, as are fp32 ones of large products (times 1.5).
  * workspace: 256-byte aligned device memory of at least fasgd_multiply_workspace() bytes
  * (for fasgd_multiply_grad where dx or dw is given, else for fasgd_multiply), which the
  * sizes, types, strides and alignments fix (-1 on a bad argument).
@@ -810,8 +812,10 @@ FASGD_API int64_t fasgd_multiply_workspace(const fasgd_multiply_args* a);
  * labels; loss is then not looked at, and only dz and dw, one of them at least, are
  * written, without the first sweep over the classes.
  * workspace: 256-byte aligned device memory of at least fasgd_score_workspace() bytes (-1 on
- * a bad argument); it does not grow with rows x classes beyond FASGD_SCORE_PIECE bytes for g
- * (or 64 classes of it).
+ * a bad argument): what grows with rows x classes in it are FASGD_SCORE_PIECE bytes for g
+ * (or 64 classes of it) at most and 8 bytes for each row and 192 classes (64 for small fp32
+ * products); besides, copies of z, and of w where it is not aligned to 16 bytes or of fp32 (times 1.5), and
+ * fp32 sums of dz.
  */
 #define FASGD_CLASSES_MAX ((int64_t)1 << 24)
 #define FASGD_SCORE_PIECE ((int64_t)1 << 29)

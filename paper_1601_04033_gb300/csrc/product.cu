@@ -1,6 +1,11 @@
-// Matrix products in their simple form: 64 x 64 tiles of D in registers, 32 steps of k
-// through shared memory at a time, the next 32 read meanwhile, fp32 multiply-adds whatever the type.  Right for every
-// layout, alignment and size.
+// Matrix products of fp32 values in their simple form: 64 x 64 tiles of D in registers, 32
+// steps of k through shared memory at a time, the next 32 read meanwhile.  Right for every layout,
+// alignment and size; for products too small for planes (by_planes) also the fastest here: 12 us for
+// 128 x 128 x 128, where planes take 20, and 35 us for 1,024 rows of 512 x 512 in 4 experts, where they
+// take 39; at 1,024 x 1,024 x 1,024 it is 92 us (23 TFLOP/s) to 54.  It is bound by its shared-memory
+// reads, 8 of them for 16 multiply-adds.
+//
+// Also here: the copies that lay sides out for the tensor cores, and the sums of parts of k.
 
 #include <algorithm>
 
@@ -14,21 +19,19 @@ namespace {
 constexpr int kM = 64, kN = kPlainN, kK = 32;
 constexpr int kEach = kM * kK / 256;     // values of a stage that a thread reads
 
-template <class T>
 __device__ __forceinline__ float element(const Side& s, int64_t group, int64_t i, int64_t k) {
-    const T* p = static_cast<const T*>(s.p) + group * s.step;
-    return to_f32(s.across ? p[k * s.ld + i] : p[i * s.ld + k]);
+    const float* p = static_cast<const float*>(s.p) + group * s.step;
+    return s.across ? p[k * s.ld + i] : p[i * s.ld + k];
 }
 // Elements [i0, i0 + 64) x [k0, k0 + 32) of a side, 0 beyond [.., i1) and [.., k1): into
 // registers, and from there to shared memory.
-template <class T>
 __device__ __forceinline__ void read(float (&v)[kEach], const Side& s, int64_t group, int64_t i0, int64_t i1, int64_t k0,
                                      int64_t k1) {
 #pragma unroll
     for (int r = 0; r < kEach; ++r) {
         const int j = threadIdx.x + r * 256;
         const int i = s.across ? j % kM : j / kK, k = s.across ? j / kM : j % kK;
-        v[r] = i0 + i < i1 && k0 + k < k1 ? element<T>(s, group, i0 + i, k0 + k) : 0.0f;
+        v[r] = i0 + i < i1 && k0 + k < k1 ? element(s, group, i0 + i, k0 + k) : 0.0f;
     }
 }
 __device__ __forceinline__ void stage(float (&to)[kK][kM + 1], const float (&v)[kEach], bool across) {
@@ -105,16 +108,17 @@ __global__ void __launch_bounds__(256) fold_kernel(Product p, const float* parts
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(256) plain_kernel(Product p) {
+// splits: parts of k, each to its own result.
+__global__ void __launch_bounds__(256) plain_kernel(Product p, int32_t splits) {
     __shared__ float as[kK][kM + 1], bs[kK][kN + 1];
     const uint32_t across = (uint32_t)((p.m + kM - 1) / kM), tile = blockIdx.x / across, tiles = gridDim.x / across;
     const int64_t m0 = (int64_t)(blockIdx.x % across) * kM;
-    int64_t group = blockIdx.z, n0 = (int64_t)tile * kN, n1 = p.n, k0 = 0, k1 = p.k;
+    int64_t group = blockIdx.z / splits, n0 = (int64_t)tile * kN, n1 = p.n, k0 = 0, k1 = p.k;
+    const int32_t split = blockIdx.z % splits;
     if (p.ragged == kRaggedN) {
         // Rows of no group, spread over the blocks; then the block's own tile.
         const int64_t lo = group_bounds(p.offsets, 0, p.n).lo, hi = group_bounds(p.offsets, p.groups - 1, p.n).hi;
-        for (int64_t r = tile; r < p.n - (hi - lo); r += tiles)
+        for (int64_t r = tile; splits == 1 && r < p.n - (hi - lo); r += tiles)      // (else the fold does)
             for (int64_t m = m0 + threadIdx.x; m < min(m0 + kM, p.m); m += blockDim.x)
                 put(p, 0, m, r < lo ? r : hi + (r - lo), 0.0f);
         Bounds rows;
@@ -126,18 +130,23 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
         k0 = b.lo;
         k1 = b.hi;
     }
+    if (splits > 1) {
+        const int64_t stages = (k1 - k0 + kK - 1) / kK, first = k0;
+        k0 = first + stages * split / splits * kK;
+        k1 = min(k1, first + stages * (split + 1) / splits * kK);
+    }
     const int64_t ga = p.ragged == kRaggedN ? group : 0;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
     float d[4][4] = {};      // [m: tx + 16 i][n: ty + 16 j]
     float a_next[kEach], b_next[kEach];
-    read<T>(a_next, p.a, ga, m0, p.m, k0, k1);
-    read<T>(b_next, p.b, 0, n0, n1, k0, k1);
+    read(a_next, p.a, ga, m0, p.m, k0, k1);
+    read(b_next, p.b, 0, n0, n1, k0, k1);
     for (int64_t k = k0; k < k1; k += kK) {
         stage(as, a_next, p.a.across);
         stage(bs, b_next, p.b.across);
         __syncthreads();
-        read<T>(a_next, p.a, ga, m0, p.m, k + kK, k1);
-        read<T>(b_next, p.b, 0, n0, n1, k + kK, k1);
+        read(a_next, p.a, ga, m0, p.m, k + kK, k1);
+        read(b_next, p.b, 0, n0, n1, k + kK, k1);
 #pragma unroll
         for (int s = 0; s < kK; ++s) {
             float av[4], bv[4];
@@ -153,6 +162,7 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p) {
         __syncthreads();
     }
     const int64_t go = p.ragged == kRaggedK ? group : 0;
+    p.out = static_cast<char*>(p.out) + 4 * split * p.step_split;
     if (p.ending == kStore) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -289,16 +299,20 @@ cudaError_t launch_fold(const Product& p, const float* parts, int64_t step, int3
     return launch_pdl(fold_kernel, grid, dim3(256), 0, stream, p, parts, step, count);
 }
 
-cudaError_t launch_plain(const Product& p, cudaStream_t stream) {
+int32_t plain_splits(const Product& p) {
+    const bool rows = p.ragged == kRaggedN;
+    const int64_t tiles = ((p.m + kM - 1) / kM) * ((p.n + kN - 1) / kN + (rows ? std::min<int64_t>(p.groups, p.n) : 0)) *
+                          (p.ragged == kRaggedK ? p.groups : 1);
+    const int64_t k = p.ragged == kRaggedK ? p.k / p.groups : p.k;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({16, 304 / std::max<int64_t>(1, tiles), k / 128}));
+}
+
+cudaError_t launch_plain(const Product& p, int32_t splits, cudaStream_t stream) {
     const int64_t tiles = ((p.n + kN - 1) / kN + (p.ragged == kRaggedN ? p.groups : 0)) * ((p.m + kM - 1) / kM);
     if (tiles == 0) return cudaSuccess;
     if (tiles >= (int64_t)1 << 31) return cudaErrorInvalidConfiguration;
-    const dim3 grid((unsigned)tiles, 1, p.ragged == kRaggedK ? p.groups : 1);
-    switch (p.dtype) {
-        case FASGD_F32: plain_kernel<float><<<grid, 256, 0, stream>>>(p); break;
-        case FASGD_BF16: plain_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(p); break;
-        default: plain_kernel<__half><<<grid, 256, 0, stream>>>(p);
-    }
+    const dim3 grid((unsigned)tiles, 1, (p.ragged == kRaggedK ? p.groups : 1) * splits);
+    plain_kernel<<<grid, 256, 0, stream>>>(p, splits);
     return cudaGetLastError();
 }
 

@@ -67,9 +67,12 @@ struct Product {
     int64_t n0, classes;         // the first n of this piece, and how many there are of all pieces
 };
 
-// Any layout, type and size, fp32 arithmetic on the ordinary cores.  kPlainN: the n of a tile.
+// fp32 of any layout and size on the ordinary cores.  kPlainN: the n of a tile.
 constexpr int kPlainN = 64;
-cudaError_t launch_plain(const Product& p, cudaStream_t stream);
+cudaError_t launch_plain(const Product& p, int32_t splits, cudaStream_t stream);
+// Parts of k that fill the SMs where there are few tiles: a stage of 32 k takes a block alone some 1.5 us
+// of latency, however little there is to do (12 rows by 2,036 x 34: 100 us in one part).
+int32_t plain_splits(const Product& p);
 
 // 16-bit types on the tensor cores, for sides that start and step on 16 bytes.  kTileN: the n of a tile.
 //
@@ -103,12 +106,13 @@ cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t st
 cudaError_t launch_fold(const Product& p, const float* parts, int64_t step, int32_t count, cudaStream_t stream);
 // The values of the parts that launch_product needs room for.
 inline int64_t part_values(const Product& p) {
-    if (p.dtype == 0 || p.ending != kStore) return 0;
-    const int64_t splits = plan_tiles(p).splits;
+    if (p.ending != kStore) return 0;
+    const int64_t splits = p.dtype == 0 ? plain_splits(p) : plan_tiles(p).splits;
     return splits > 1 ? splits * p.n * p.m * (p.ragged == kRaggedK ? p.groups : 1) : 0;
 }
-// Whether an fp32 product of m x n x k goes by planes: the plain form does some 10 TFLOP/s, the planes
-// some 250, after copies and a launch or two more.
+// Whether an fp32 product of m x n x k goes by planes: from where copies and launches of theirs are made
+// up for.  Measured on both sides: y of 1,024 rows by 512 x 512 in 4 experts (2^28) 35 us plain and 39 by
+// planes; a score's gradients of 512 x 512 x 2,048 (2^29) 243 and 161; y of 1,024 x 1,024 x 1,024 92 and 54.
 inline bool by_planes(int64_t m, int64_t n, int64_t k) {
     return (double)m * (double)n * (double)k >= kPlanesFrom;
 }
@@ -116,9 +120,10 @@ inline bool by_planes(int64_t m, int64_t n, int64_t k) {
 // products to planes, and lay out 16-bit ones for the tensor cores.
 // parts: room for part_values().
 inline cudaError_t launch_product(const Product& p, float* parts, cudaStream_t stream) {
-    if (p.dtype == 0) return launch_plain(p, stream);
-    const TilePlan plan = plan_tiles(p);
-    if (part_values(p) == 0) return launch_tiles(p, {plan.pair, 1}, stream);
+    const bool plain = p.dtype == 0;
+    const TilePlan plan = plain ? TilePlan{1, plain_splits(p)} : plan_tiles(p);
+    if (part_values(p) == 0)
+        return plain ? launch_plain(p, 1, stream) : launch_tiles(p, {plan.pair, 1}, stream);
     Product q = p;
     q.out = parts;
     q.out_dtype = 0;
@@ -128,7 +133,7 @@ inline cudaError_t launch_product(const Product& p, float* parts, cudaStream_t s
     q.scale = nullptr;
     q.by_n = 0;
     q.factor = 1.0f;
-    const cudaError_t st = launch_tiles(q, plan, stream);
+    const cudaError_t st = plain ? launch_plain(q, plan.splits, stream) : launch_tiles(q, plan, stream);
     return st != cudaSuccess ? st : launch_fold(p, parts, q.step_split, plan.splits, stream);
 }
 

@@ -10,6 +10,8 @@
 // Short lists (128 rows of a minibatch) take one block and one launch.  Longer ones take
 // two: each block of the second adds up the counters of all chunks itself, at most 64
 // chunks (with 256 of them the sums took 40 of 65 us), which costs less than a third launch.
+//
+// Bound by latency: 524,288 entries of 256 experts take 15 us (6.3 MB would be 1), 256 entries 5 with the host.
 
 #include <algorithm>
 

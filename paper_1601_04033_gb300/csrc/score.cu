@@ -11,7 +11,10 @@
 // g is held without upstream / N, so that its values are in [-1, 1] and no fp16 value is
 // lost for N's size; for fp16 it is held times 2^14, so that probabilities down to 2^-28
 // keep all their bits.  The products' results are multiplied by upstream / N, in fp32.
-// Rows without a label are copied as zeros before the products that sum over rows.
+// Rows without a label are copied as zeros, behind the others where there are many, and have no tiles.
+//
+// 8,192 x 2,048 x 131,072 bf16, a tenth without labels: 9.8 ms, 2.2 of them the first sweep; all products
+// together 1,620 TFLOP/s of the work that rows with labels need.
 
 #include <algorithm>
 
@@ -196,7 +199,8 @@ __global__ void __launch_bounds__(1024) loss_kernel(int64_t rows, const int64_t*
 // [class][col]; a warp takes a row: its lanes go along the columns and keep a sum for each class, so that
 // every value of z and w is read once a row.  Blocks take the rows by turns and keep their share of dw in
 // shared memory too, each thread its own columns of it; the shares are added up in the blocks' order.
-// The bound is latency: 128 x 200 x 10 took seven launches of the products' general forms (68 us).
+// The bound is latency: 128 x 200 x 10 takes 17 us with the host; seven launches of the products' general
+// forms took 68.
 constexpr int kFewClasses = 32, kFewBlocks = 152;
 constexpr int64_t kFewValues = 12 << 10;           // of w: 48 KB, and dw as much again
 constexpr int kFewWarps = 8;
@@ -394,7 +398,7 @@ int fill_score(const char* call, const fasgd_score_args& given, Score& s) {
 // A piece of n classes' part of dz, and its rows (or columns) of dw; q.a.p or q.out are the piece's.
 Product product_of_g(const Score& s) {
     Product q = {};
-    q.dtype = s.planes ? FASGD_BF16 : s.u.dtype;
+    q.dtype = s.u.rows == 0 ? FASGD_F32 : s.planes ? FASGD_BF16 : s.u.dtype;      // no rows: no operands to describe
     q.planes = q.exact = s.planes;
     q.ending = fasgd::kStore;
     q.factor = 1.0f / s.factor;
@@ -625,7 +629,7 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
                 st = fasgd::launch_product(q, s.sums, stream);
             } else {      // every piece in as many parts
                 q.add = v > 0;
-                st = q.dtype == FASGD_F32 ? fasgd::launch_plain(q, stream)
+                st = q.dtype == FASGD_F32 ? fasgd::launch_plain(q, 1, stream)
                                           : fasgd::launch_tiles(q, {fasgd::plan_tiles(q).pair, s.dz_parts}, stream);
             }
             if (st != cudaSuccess) return st;

@@ -4,7 +4,9 @@ gradients in place of sim.py's quadratic, against the same server.
 lambda clients hold copies of the flat parameter vector.  A dispatched client runs
 one minibatch through the network on its (stale) copy -- residual blocks of routed
 experts, with the client operators (``client.joined``, ``client.balanced``,
-``client.dropped``) between the matrix products, which are torch's -- and pushes
+``client.dropped``) between the matrix products, which are torch's, or (``sparse``) with
+rows that go to their experts alone (``client.route``, ``gathered``, ``multiplied``,
+``combined``) and the loss from the rows before the last product (``scored``) -- and pushes
 the gradient of the whole vector; the server applies the batch and the client
 fetches fresh parameters (the protocol of the paper's Sec. 2.1 and 3).  Draws of
 dropout are keyed by (seed, client, the client's count of gradients and the place
@@ -27,12 +29,14 @@ from . import client, fasgd, streams
 class RoutedNetwork:
     """blocks x [norm, top-k routed experts, join], a last norm, dropout, classes.
     The parameters are views of one fp32 vector, in the order of `shapes`; each is
-    a tensor of its own to the server's per-tensor rules (`sizes`)."""
+    a tensor of its own to the server's per-tensor rules (`sizes`).  sparse: every row
+    goes through its own experts only, as fp32 parameters rounded to dtype, not through
+    every expert with a weight."""
 
     def __init__(self, inputs=64, width=96, hidden=64, classes=10, blocks=3, experts=4, top=2, norm="rms",
-                 rate=0.1, dtype=torch.bfloat16, seed=0):
+                 rate=0.1, dtype=torch.bfloat16, seed=0, sparse=False):
         self.width, self.classes, self.blocks, self.experts, self.top = width, classes, blocks, experts, top
-        self.norm, self.rate, self.dtype, self.seed = norm, rate, dtype, seed
+        self.norm, self.rate, self.dtype, self.seed, self.sparse = norm, rate, dtype, seed, sparse
         self.shapes = {"in": (inputs, width), "pre0": (width,)}
         for b in range(blocks):
             self.shapes.update({f"router{b}": (width, experts), f"up{b}": (experts, width, hidden),
@@ -58,6 +62,11 @@ class RoutedNetwork:
         """Class scores, the sum of the blocks' balance losses, and each block's
         per-expert counts.  draws: (client, n) of a training pass; None: nothing
         is dropped."""
+        z, out, balance, counts = self._rows(theta, x, draws)
+        return z @ out, balance, counts
+
+    def _rows(self, theta, x, draws):
+        """forward's rows before the last product, fp32, and its matrix."""
         p = {k: t.view(s) for (k, s), t in zip(self.shapes.items(), torch.split(theta, self.sizes))}
         cast = self.dtype
 
@@ -76,20 +85,27 @@ class RoutedNetwork:
             counts.append(count)
             open_ = (chosen[:, :, None] == torch.arange(self.experts, device="cuda")).any(1)
             weight = torch.softmax(scores.masked_fill(~open_, float("-inf")), 1).to(cast)
-            # Every expert on every row, weighted: an example's way to route.
-            u = torch.relu(torch.einsum("rd,edh->erh", z, p[f"up{b}"].to(cast)))
-            y = torch.einsum("erh,ehd,re->rd", u, p[f"down{b}"].to(cast), weight)
+            if self.sparse:
+                way = client.route(chosen, self.experts)
+                u = torch.relu(client.multiplied(client.gathered(z, way), p[f"up{b}"], way.offsets))
+                y = client.combined(client.multiplied(u, p[f"down{b}"], way.offsets), way,
+                                    weight.float().gather(1, chosen.long()))
+            else:
+                # Every expert on every row, weighted: an example's way to route.
+                u = torch.relu(torch.einsum("rd,edh->erh", z, p[f"up{b}"].to(cast)))
+                y = torch.einsum("erh,ehd,re->rd", u, p[f"down{b}"].to(cast), weight)
             h, z = client.joined(h, y, post=p[f"post{b}"], gate=p[f"gate{b}"], pre=p[f"pre{b + 1}"], norm=self.norm,
                                  draws=at(b))
         if draws is not None:
             z = client.dropped(z, at(self.blocks))
-        return z.float() @ p["out"], balance, counts
+        return z.float(), p["out"], balance, counts
 
     def gradient(self, theta, x, labels, draws):
         """(loss, its gradient as one vector) of a minibatch at theta."""
         leaf = theta.detach().requires_grad_(True)
-        scores, balance, _ = self.forward(leaf, x, draws)
-        loss = torch.nn.functional.cross_entropy(scores, labels) + balance
+        z, out, balance, _ = self._rows(leaf, x, draws)
+        loss = client.scored(z, out, labels)[0] if self.sparse else torch.nn.functional.cross_entropy(z @ out, labels)
+        loss = loss + balance
         loss.backward()
         return loss.detach(), leaf.grad
 
@@ -155,12 +171,13 @@ def main():
     ap.add_argument("--K", type=int, default=2)
     ap.add_argument("--norm", choices=["rms", "layer"], default="rms")
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--sparse", action="store_true", help="rows go to their own experts only")
     args = ap.parse_args()
     out = {}
     # Gradients' spreads are near 1e-3 here, so v nears its largest, eps^-1/2 = 100, and
     # FASGD's alpha / v is a fiftieth.
     for name, variant, alpha in (("sasgd", fasgd.SASGD, 0.04), ("fasgd", fasgd.FASGD, 2.0)):
-        net = RoutedNetwork(norm=args.norm, seed=args.seed)
+        net = RoutedNetwork(norm=args.norm, seed=args.seed, sparse=args.sparse)
         losses, _ = train(net, lam=args.lam, batches=args.batches, K=args.K, alpha=alpha, variant=variant)
         out[name] = {"alpha": alpha, "held_out_losses": losses}
     print(json.dumps({"parameters": net.P, "lambda": args.lam, "batches": args.batches, "K": args.K, **out}))

@@ -82,7 +82,8 @@ def matrix(g, R, D, dtype, pad=0, scale=1.0):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,top,E,D,pad", [(128, 2, 4, 96, 0), (1, 8, 16, 2048, 0), (1, 1, 1, 1, 0), (37, 3, 5, 61, 0), (200, 9, 13, 264, 8),
-                                           (500, 2, 7, 1021, 3), (64, 17, 40, 8192, 0), (0, 2, 3, 40, 0)])
+                                           (500, 2, 7, 1021, 3), (64, 17, 40, 8192, 0), (0, 2, 3, 40, 0),
+                                           (41, 3, 4, 1030, 0), (30, 9, 11, 260, 6), (2100, 2, 3, 515, 1)])
 def test_rows_to_places_and_back(dtype, T, top, E, D, pad):
     c = _c()
     g = torch.Generator(device="cuda").manual_seed(D)

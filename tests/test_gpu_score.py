@@ -169,6 +169,10 @@ def test_no_rows():
         s = c.score(torch.empty(0, 40, dtype=dtype, device="cuda"), torch.ones(40, 24, dtype=dtype, device="cuda"),
                     torch.empty(0, dtype=torch.int64, device="cuda"))
         assert float(s.loss) == 0.0 and s.dz.shape == (0, 40) and not s.dw.any()
+        for flip in (False, True):
+            w = torch.ones(1000, 300, dtype=dtype, device="cuda").t() if flip else torch.ones(300, 1000, dtype=dtype, device="cuda")
+            s = c.score(torch.empty(0, 300, dtype=dtype, device="cuda"), w, torch.empty(0, dtype=torch.int64, device="cuda"))
+            assert float(s.loss) == 0.0 and s.dz.shape == (0, 300) and not s.dw.any()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
