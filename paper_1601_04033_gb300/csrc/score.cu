@@ -121,6 +121,7 @@ __global__ void __launch_bounds__(1024) first_kernel(fasgd_score_args u, Score s
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const auto has = [&](int64_t r) { return r < u.rows && u.labels[r] >= 0 && u.labels[r] < u.classes; };
     int32_t n = 0;
+#pragma unroll 8
     for (int64_t r = threadIdx.x; r < u.rows; r += 1024) n += has(r);
     n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) counts[warp] = n;
@@ -130,9 +131,11 @@ __global__ void __launch_bounds__(1024) first_kernel(fasgd_score_args u, Score s
         if (lane == 0) *s.live = total = n;
     }
     int32_t before = 0;                              // labels in earlier rounds
+    int64_t next = threadIdx.x < u.rows ? u.labels[threadIdx.x] : -1;
     for (int64_t r0 = 0; r0 < u.rows; r0 += 1024) {
-        const int64_t r = r0 + threadIdx.x;
-        const bool is = has(r);
+        const int64_t r = r0 + threadIdx.x, label = next;
+        next = r + 1024 < u.rows ? u.labels[r + 1024] : -1;      // (read ahead of this round's barriers)
+        const bool is = label >= 0 && label < u.classes;
         const uint32_t votes = __ballot_sync(0xffffffffu, is);
         __syncthreads();
         if (lane == 0) counts[warp] = __popc(votes);
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(1024) first_kernel(fasgd_score_args u, Score s
             const int32_t to = is ? rank : total + (int32_t)(r - rank);
             s.to_row[r] = to;
             s.row_at[to] = (int32_t)r;
-            s.labels[to] = is ? u.labels[r] : -1;
+            s.labels[to] = is ? label : -1;
             if (u.known) {
                 s.lse[to] = is ? u.lse[r] : 0.0f;
                 s.loss_at[to] = is ? u.row_loss[r] : 0.0f;
@@ -166,11 +169,14 @@ __global__ void __launch_bounds__(1024) loss_kernel(int64_t rows, const int64_t*
     const auto has = [&](int64_t r) { return labels[r] >= 0 && labels[r] < classes; };
     float sum = 0.0f;
     int64_t count = 0;
-    for (int64_t r = threadIdx.x; r < rows; r += 1024)
+#pragma unroll 8
+    for (int64_t r = threadIdx.x; r < rows; r += 1024) {
+        const float loss_of = row_loss[r];
         if (has(r)) {
-            sum += row_loss[r];
+            sum += loss_of;
             ++count;
         }
+    }
     sum = fasgd::warp_sum(sum);
     for (int d = 16; d > 0; d >>= 1) count += __shfl_xor_sync(0xffffffffu, count, d);
     if (threadIdx.x % 32 == 0) {

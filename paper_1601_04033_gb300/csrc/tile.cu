@@ -925,7 +925,8 @@ bool tile_side(const Side& s, int64_t groups) {
 
 // The plan that should take the least time, by what was measured on a GB300: 64 k of a tile take a
 // block or a pair 0.27 us times the n of the tile over 256 (a block alone a quarter more), and no less
-// than 50 GB/s and SM copy its sides in; parts of k cost their sums' way through memory and a launch.
+// than 50 GB/s and SM copy its sides in; a group's last rows take a pair 1.2 us a tile (a release that its other block sees),
+// a block alone 0.4; parts of k cost their sums' way through memory and a launch.
 TilePlan plan_tiles(const Product& p) {
     constexpr int kSms = 152;
     const bool rows = p.ragged == kRaggedN;
@@ -944,7 +945,8 @@ TilePlan plan_tiles(const Product& p) {
                                      (kSideA + std::max(width / pair, 32.0) * kK * 2) / 50e3);
         for (int splits = 1; splits <= 16 && (splits == 1 || (p.ending == kStore && blocks >= 8 * splits)); ++splits) {
             const double waves = (double)((tiles * splits + teams - 1) / teams);
-            double time = waves * (double)((blocks + splits - 1) / splits) * each;
+            const double cut = p.ragged != kRaggedK ? 0.0 : pair == 2 ? 1.2 : 0.4;
+            double time = waves * ((double)((blocks + splits - 1) / splits) * each + cut);
             if (splits > 1) time += 4.0 + (double)p.m * (double)p.n * (double)groups * splits * (p.add ? 16.0 : 8.0) / 5e6 / (rows ? (double)groups : 1.0);
             if (time < least * 0.97) {
                 least = time;
