@@ -98,23 +98,23 @@ __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
 // One thread waits for a phase; false (and *late): it did not come.  The timer is read only
 // after a while: that takes as long as the MMAs of some k.
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool wait_thread(uint64_t* barrier, uint32_t parity, volatile int32_t* late) {
+__device__ __forceinline__ bool wait_thread(uint64_t* barrier, uint32_t parity, volatile int32_t* late, uint64_t more = 0) {
     const uint32_t bar = smem_addr(barrier);
     uint64_t t0 = 0;
-    for (uint32_t i = 1; i < (1u << 26); ++i) {
+    for (uint32_t i = 1; i < (1u << 30); ++i) {
         if (test<CLUSTER>(bar, parity)) return true;
         if ((i & 255u) == 0) {
             const uint64_t now = global_ns();
             if (t0 == 0) t0 = now;
-            if (now - t0 > kWaitLimitNs || *late != 0) break;
+            if (now - t0 > kWaitLimitNs + more || *late != 0) break;
         }
     }
     *late = 1;
     return false;
 }
 // A whole warp.
-__device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, volatile int32_t* late) {
-    return __all_sync(0xffffffffu, wait_thread(barrier, parity, late));
+__device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, volatile int32_t* late, uint64_t more = 0) {
+    return __all_sync(0xffffffffu, wait_thread(barrier, parity, late, more));
 }
 template <bool CLUSTER = false>
 __device__ __forceinline__ void arrive_first(uint64_t* bar) {
@@ -715,7 +715,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 // instruction cache (for all 128 at once the code outgrew it: 38,000 cycles a tile of g).
                 const uint32_t buffer = tile & 1;
                 if (blocks > 0) {
-                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
+                    // (of hundreds of millions of k the sums alone take a second)
+                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late, (uint64_t)blocks * 4000);
                     ++tile;
                     fence_after();
                 }

@@ -378,6 +378,40 @@ def test_gathers_differentiate_twice():
     assert torch.equal(again, c.combine(torch.ones(6, 8, device="cuda"), r))
 
 
+def test_many_experts():
+    """As many as there may be, most with two rows, one with many, some with none."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    sizes = [2] * 1024
+    sizes[17], sizes[500], sizes[1023] = 700, 0, 0
+    for dtype in (torch.bfloat16, torch.float32):
+        check_products(_c(), *product_case(g, sizes, 0, 3, 24, 40, dtype, dtype, False))
+
+
+def test_rows_far_apart():
+    """Offsets beyond 2^31 values: rows of a wide buffer, read, written and exchanged."""
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(4)
+    R, D, far = 60000, 64, 40000
+    wide = torch.empty(2, R, far, dtype=torch.bfloat16, device="cuda")
+    x, out = wide[0][:, 8:8 + D], wide[1][:, 16:16 + D]
+    x.copy_(torch.randn(R, D, generator=g, device="cuda"))
+    w = torch.randn(3, D, D, generator=g, device="cuda").to(torch.bfloat16)
+    offsets = torch.tensor([0, 20000, 59000, 59990], dtype=torch.int32, device="cuda")
+    near_by = x.contiguous()
+    want = c.multiply(near_by, w, offsets)
+    assert torch.equal(c.multiply(x, w, offsets, out=out), want) and torch.equal(out, want)
+    for p, q in zip(c.multiply_grad(x, w, offsets, out), c.multiply_grad(near_by, w, offsets, want)):
+        assert torch.equal(p, q)
+    r = c.route(choices(g, R, 1, 7), 7)
+    assert torch.equal(c.gather(x, r, out=out), c.gather(near_by, r))
+    weight = torch.rand(R, 1, generator=g, device="cuda")
+    assert torch.equal(c.combine(out, r, weight), c.combine(out.contiguous(), r, weight))
+    labels = torch.randint(0, 900, (R,), generator=g, device="cuda")
+    classes = torch.randn(D, 900, generator=g, device="cuda").to(torch.bfloat16)
+    for p, q in zip(c.score(x, classes, labels), c.score(near_by, classes, labels)):
+        assert torch.equal(p, q)
+
+
 def test_random_products():
     """Sizes drawn over the range of small ones, all layouts."""
     c = _c()
