@@ -32,7 +32,7 @@ struct Score {
     int64_t size, tile;
     bool grad;
     bool few;                    // few classes: no products
-    float2* few_sums;
+    float* few_sums;
     float* few_dw;
     bool planes;                 // fp32 by planes on the tensor cores
     int64_t plane_z, plane_w, plane_g;
@@ -218,7 +218,7 @@ int64_t few_blocks(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>
 
 struct FewArgs {
     fasgd_score_args u;
-    float2* sums;       // [blocks] loss, (unused)
+    float* sums;        // [blocks] of the rows' losses
     float* dw;          // [blocks][classes][cols]
 };
 template <class T>
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(FewArgs a) {
     if (threadIdx.x == 0) {
         float sum = 0.0f;
         for (int i = 0; i < kFewWarps; ++i) sum += part[i];
-        a.sums[blockIdx.x] = make_float2(sum, 0.0f);
+        a.sums[blockIdx.x] = sum;
     }
     if (u.dw != nullptr)
         for (int i = threadIdx.x; i < V * D; i += blockDim.x) a.dw[(int64_t)blockIdx.x * V * D + i] = dw[i];
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(FewArgs a, int32_t blocks)
     const float count = (float)total;
     if (blockIdx.x == 0 && threadIdx.x == 0 && u.loss != nullptr) {
         float sum = 0.0f;
-        for (int b = 0; b < blocks; ++b) sum += a.sums[b].x;
+        for (int b = 0; b < blocks; ++b) sum += a.sums[b];
         *u.loss = total == 0 ? 0.0f : sum / count;
     }
     if (u.dw == nullptr) return;
@@ -462,7 +462,7 @@ int64_t lay_out(Score& s, char* base) {
     };
     s.few = few_classes(u);
     if (s.few) {
-        s.few_sums = reinterpret_cast<float2*>(take(8 * few_blocks(u.rows)));
+        s.few_sums = reinterpret_cast<float*>(take(4 * few_blocks(u.rows)));
         s.few_dw = reinterpret_cast<float*>(take(u.dw != nullptr ? 4 * few_blocks(u.rows) * u.classes * u.cols : 0));
         return at;
     }

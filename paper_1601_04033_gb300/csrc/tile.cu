@@ -436,7 +436,9 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     const uint32_t rank = PAIR == 2 ? block_rank() : 0;
 
     if (threadIdx.x == 0) {
-        for (const CUtensorMap* map : {&t.a, &t.b, &t.few}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&t.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&t.b) : "memory");
+        if (p.ragged == kRaggedN) asm volatile("prefetch.tensormap [%0];" ::"l"(&t.few) : "memory");
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(&s.full[i], PAIR);
             mbar_init(&s.empty[i], 1);
@@ -560,74 +562,74 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 }
             }
         } else if (warp == 1) {
-        // MMAs: one thread of the pair's first block issues them.  It is elected, so that the compiler
-        // knows that it is one, and counts in 32 bits: by `lane == 0` and in 64 bits the tensor cores
-        // waited for it (1,530 TFLOP/s for 1,760 at 8,192 of m, n and k).
-        if (rank == 0 && elected()) {
-            uint32_t stage = 0, phase = 0, tile = 0;
-            const uint32_t kind = p.dtype == FASGD_BF16 ? 1u << 7 | 1u << 10 : 0u;
-            const uint32_t base = 1u << 4 | kind | (uint32_t)(p.a.across != 0) << 15 | (uint32_t)(p.b.across != 0) << 16 |
-                                  (uint32_t)(kBlockM * PAIR / 16) << 24;
-            const uint32_t next_a = p.a.across ? 2048 >> 4 : 32 >> 4, next_b = p.b.across ? 2048 >> 4 : 32 >> 4;
-            const uint64_t a0 = matrix_of(smem_addr(ring), p.a.across), b0 = matrix_of(smem_addr(ring) + kSideA, p.b.across);
-            const uint32_t a_high = (uint32_t)(a0 >> 32), b_high = (uint32_t)(b0 >> 32);
-            // The next tile with sums and the next accumulator are looked up while MMAs run.
-            int64_t i = team - teams;
-            int blocks = 0, last = 0;                 // of 64 k each, of every pair of planes; MMAs of the last one
-            uint32_t shape = 0;
-            bool zeroed = false, ok = true;           // zeroed: that holds rows set to 0
-            const auto look = [&] {
-                blocks = 0;
-                while (blocks == 0 && (i += teams) < items) {
-                    const Tile w = tile_of<PAIR>(t, s, sizes, i);
-                    if (w.k0 >= w.k1) continue;
-                    blocks = (int)((w.k1 - w.k0 + kK - 1) / kK);
-                    last = (int)((w.k1 - w.k0 + 15) / 16) - (blocks - 1) * (kK / 16);
-                    shape = base | (uint32_t)(width_of<PAIR>(t, w) / 8) << 17;
-                    zeroed = p.ragged == kRaggedK && (w.k1 - w.k0) % kK != 0;
-                }
-            };
-            look();
-            while (blocks > 0 && ok) {
-                const int each = blocks, all = each * (int)pairs, chunk = EXACT ? kExact / kK : all, mmas = last;
-                const uint32_t now = shape;
-                const bool cuts = zeroed;
-                int in = 0;                           // blocks of this pair of planes
-                for (int done = 0; done < all && ok; done += chunk) {
-                    const int until = min(done + chunk, all);
-                    if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, &s.late))) break;
-                    fence_after();
-                    const uint32_t to = tmem + (tile & 1) * kTileN;
-                    uint32_t add = 0;
-                    for (int k = done; k < until; ++k) {
-                        const bool end = ++in == each;
-                        ok = PAIR == 2 && cuts && end ? wait_thread<true>(&s.full[stage], phase, &s.late)
-                                                      : wait_thread(&s.full[stage], phase, &s.late);
-                        if (!ok) break;
-                        fence_after();
-                        const uint32_t a = (uint32_t)a0 + stage * (S::kStage >> 4), b = (uint32_t)b0 + stage * (S::kStage >> 4);
-                        mma<PAIR>(to, a, b, a_high, b_high, now, add);
-                        add = 1;
-                        if (!end) {
-#pragma unroll
-                            for (int j = 1; j < 4; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
-                        } else {
-                            for (int j = 1; j < mmas; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
-                            in = 0;
-                        }
-                        commit<PAIR>(&s.empty[stage]);
-                        if (++stage == S::kStages) {
-                            stage = 0;
-                            phase ^= 1;
-                        }
+            // MMAs: one thread of the pair's first block issues them.  It is elected, so that the compiler
+            // knows that it is one, and counts in 32 bits: by `lane == 0` and in 64 bits the tensor cores
+            // waited for it (1,530 TFLOP/s for 1,760 at 8,192 of m, n and k).
+            if (rank == 0 && elected()) {
+                uint32_t stage = 0, phase = 0, tile = 0;
+                const uint32_t kind = p.dtype == FASGD_BF16 ? 1u << 7 | 1u << 10 : 0u;
+                const uint32_t base = 1u << 4 | kind | (uint32_t)(p.a.across != 0) << 15 | (uint32_t)(p.b.across != 0) << 16 |
+                                      (uint32_t)(kBlockM * PAIR / 16) << 24;
+                const uint32_t next_a = p.a.across ? 2048 >> 4 : 32 >> 4, next_b = p.b.across ? 2048 >> 4 : 32 >> 4;
+                const uint64_t a0 = matrix_of(smem_addr(ring), p.a.across), b0 = matrix_of(smem_addr(ring) + kSideA, p.b.across);
+                const uint32_t a_high = (uint32_t)(a0 >> 32), b_high = (uint32_t)(b0 >> 32);
+                // The next tile with sums and the next accumulator are looked up while MMAs run.
+                int64_t i = team - teams;
+                int blocks = 0, last = 0;                 // of 64 k each, of every pair of planes; MMAs of the last one
+                uint32_t shape = 0;
+                bool zeroed = false, ok = true;           // zeroed: that holds rows set to 0
+                const auto look = [&] {
+                    blocks = 0;
+                    while (blocks == 0 && (i += teams) < items) {
+                        const Tile w = tile_of<PAIR>(t, s, sizes, i);
+                        if (w.k0 >= w.k1) continue;
+                        blocks = (int)((w.k1 - w.k0 + kK - 1) / kK);
+                        last = (int)((w.k1 - w.k0 + 15) / 16) - (blocks - 1) * (kK / 16);
+                        shape = base | (uint32_t)(width_of<PAIR>(t, w) / 8) << 17;
+                        zeroed = p.ragged == kRaggedK && (w.k1 - w.k0) % kK != 0;
                     }
-                    if (ok) commit<PAIR>(&s.ready[tile & 1]);
-                    ++tile;
-                    if (done == 0) look();
+                };
+                look();
+                while (blocks > 0 && ok) {
+                    const int each = blocks, all = each * (int)pairs, chunk = EXACT ? kExact / kK : all, mmas = last;
+                    const uint32_t now = shape;
+                    const bool cuts = zeroed;
+                    int in = 0;                           // blocks of this pair of planes
+                    for (int done = 0; done < all && ok; done += chunk) {
+                        const int until = min(done + chunk, all);
+                        if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, &s.late))) break;
+                        fence_after();
+                        const uint32_t to = tmem + (tile & 1) * kTileN;
+                        uint32_t add = 0;
+                        for (int k = done; k < until; ++k) {
+                            const bool end = ++in == each;
+                            ok = PAIR == 2 && cuts && end ? wait_thread<true>(&s.full[stage], phase, &s.late)
+                                                          : wait_thread(&s.full[stage], phase, &s.late);
+                            if (!ok) break;
+                            fence_after();
+                            const uint32_t a = (uint32_t)a0 + stage * (S::kStage >> 4), b = (uint32_t)b0 + stage * (S::kStage >> 4);
+                            mma<PAIR>(to, a, b, a_high, b_high, now, add);
+                            add = 1;
+                            if (!end) {
+#pragma unroll
+                                for (int j = 1; j < 4; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
+                            } else {
+                                for (int j = 1; j < mmas; ++j) mma<PAIR>(to, a + j * next_a, b + j * next_b, a_high, b_high, now, true);
+                                in = 0;
+                            }
+                            commit<PAIR>(&s.empty[stage]);
+                            if (++stage == S::kStages) {
+                                stage = 0;
+                                phase ^= 1;
+                            }
+                        }
+                        if (ok) commit<PAIR>(&s.ready[tile & 1]);
+                        ++tile;
+                        if (done == 0) look();
+                    }
                 }
             }
-        }
-        __syncwarp();
+            __syncwarp();
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -735,83 +737,83 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 }
                 if (odd * 32 >= count && blocks > 0) taken(buffer);
             } else {
-            float v[4][32];
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
-            for (int64_t k = 0; k < blocks; k += kExact / kK) {
-                const uint32_t buffer = tile & 1;
-                ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
-                ++tile;
-                fence_after();
-                if (!ok) break;
-                const uint32_t from = columns_of(buffer);
-                if (k == 0) {
-#pragma unroll
-                    for (int b = 0; b < 4; ++b)
-                        if (b * 64 + odd * 32 < count) load_columns(from + b * 64, v[b]);
-                    wait_columns();
-                } else {
-#pragma unroll
-                    for (int b = 0; b < 8; ++b)
-                        if (b / 2 * 64 + odd * 32 < count) {
-                            float more_of[16];
-                            load_half(from + b / 2 * 64 + b % 2 * 16, more_of);
-                            wait_columns();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) v[b / 2][b % 2 * 16 + j] += more_of[j];
-                        }
-                }
-                taken(buffer);
-            }
-            if (!ok)
+                float v[4][32];
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[b][j] = NAN;
-            // The registers' 32 columns after the other, in a loop that moves them down (for the same reason).
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll 1
-            for (int c = odd * 32; c < count; c += 64) {
-                if constexpr (ENDING != kStatistics) {
-                    end_columns(c, v[0]);
-                } else {
-                    if (count - c < 32)
+                    for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
+                for (int64_t k = 0; k < blocks; k += kExact / kK) {
+                    const uint32_t buffer = tile & 1;
+                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
+                    ++tile;
+                    fence_after();
+                    if (!ok) break;
+                    const uint32_t from = columns_of(buffer);
+                    if (k == 0) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[0][j] = j < count - c ? v[0][j] : -INFINITY;
-                    float most[4] = {top, v[0][1], v[0][2], v[0][3]};
+                        for (int b = 0; b < 4; ++b)
+                            if (b * 64 + odd * 32 < count) load_columns(from + b * 64, v[b]);
+                        wait_columns();
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) most[j & 3] = fmaxf(most[j & 3], v[0][j]);
-                    const float next = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-                    if (__any_sync(0xffffffffu, mine && at >> 5 == c >> 5)) {
+                        for (int b = 0; b < 8; ++b)
+                            if (b / 2 * 64 + odd * 32 < count) {
+                                float more_of[16];
+                                load_half(from + b / 2 * 64 + b % 2 * 16, more_of);
+                                wait_columns();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (mine && at == c + j) p.at_label[m] = v[0][j];
+                                for (int j = 0; j < 16; ++j) v[b / 2][b % 2 * 16 + j] += more_of[j];
+                            }
                     }
-                    const float shift = next == -INFINITY ? 0.0f : next;
-                    float part[4] = {sum * exp2_fast((top - shift) * kLog2E), 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[0][j] - shift) * kLog2E);
-                    sum = (part[0] + part[1]) + (part[2] + part[3]);
-                    top = next;
+                    taken(buffer);
                 }
+                if (!ok)
 #pragma unroll
-                for (int b = 0; b < 3; ++b)
+                    for (int b = 0; b < 4; ++b)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[b][j] = v[b + 1][j];
-            }
-            if constexpr (ENDING == kStatistics) {
-                float2* const other = &s.halves[turn][quarter * 32 + lane];
-                if (odd) *other = make_float2(top, sum);
-                asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
-                if (!odd && live) {
-                    const float2 o = *other;
-                    const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
-                    sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
-                    p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
+                        for (int j = 0; j < 32; ++j) v[b][j] = NAN;
+                // The registers' 32 columns after the other, in a loop that moves them down (for the same reason).
+                float top = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+                for (int c = odd * 32; c < count; c += 64) {
+                    if constexpr (ENDING != kStatistics) {
+                        end_columns(c, v[0]);
+                    } else {
+                        if (count - c < 32)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[0][j] = j < count - c ? v[0][j] : -INFINITY;
+                        float most[4] = {top, v[0][1], v[0][2], v[0][3]};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) most[j & 3] = fmaxf(most[j & 3], v[0][j]);
+                        const float next = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+                        if (__any_sync(0xffffffffu, mine && at >> 5 == c >> 5)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (mine && at == c + j) p.at_label[m] = v[0][j];
+                        }
+                        const float shift = next == -INFINITY ? 0.0f : next;
+                        float part[4] = {sum * exp2_fast((top - shift) * kLog2E), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[0][j] - shift) * kLog2E);
+                        sum = (part[0] + part[1]) + (part[2] + part[3]);
+                        top = next;
+                    }
+#pragma unroll
+                    for (int b = 0; b < 3; ++b)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[b][j] = v[b + 1][j];
                 }
-            }
+                if constexpr (ENDING == kStatistics) {
+                    float2* const other = &s.halves[turn][quarter * 32 + lane];
+                    if (odd) *other = make_float2(top, sum);
+                    asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
+                    if (!odd && live) {
+                        const float2 o = *other;
+                        const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
+                        sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
+                        p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
+                    }
+                }
             }
         }
     }
