@@ -293,6 +293,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(FewArgs a) {
                 for (int v = 0; has && v < V; ++v) sum = fmaf(g[warp * V + v], w[v * D + d], sum);
                 dz[d] = fasgd::from_f32<T>(has ? sum * share : 0.0f);
             }
+            __syncwarp();                          // a next row without a label writes g at once
         }
         if (u.dw != nullptr) {
             __syncthreads();                       // the rows of all warps
