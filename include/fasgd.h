@@ -843,6 +843,15 @@ typedef struct fasgd_score_args {
 FASGD_API int fasgd_score(const fasgd_score_args* a, void* stream);
 FASGD_API int64_t fasgd_score_workspace(const fasgd_score_args* a);
 
+/*
+ * fasgd_selftest_product_limit -- the products of fasgd_multiply(_grad) and fasgd_score on the
+ * tensor cores wait inside their kernels for copies, products and stores.  Such a wait
+ * gives up where the block has not issued a copy for a second; results that are not there
+ * then are NaN.  This sets that time, of launches from now on, for tests: ns in
+ * [10^6, 10^9], which is the ordinary one.  Errors: EINVAL.
+ */
+FASGD_API int fasgd_selftest_product_limit(int64_t ns);
+
 /* Text of the last failure on h, or, when h is NULL, of the last failed call
  * made without a handle (fasgd_create, bfasgd_fetch_apply, fasgd_sim_*,
  * bfasgd_select_compact_noalloc, the client operators). */

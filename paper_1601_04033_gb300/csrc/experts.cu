@@ -349,6 +349,12 @@ int fasgd_combine_grad(const fasgd_exchange_args* u, void* stream) {
     return exchange("fasgd_combine_grad", u, fasgd::kCombineGrad, stream);
 }
 
+int fasgd_selftest_product_limit(int64_t ns) {
+    if (ns < 1000000 || ns > 1000000000) return fail(FASGD_EINVAL, "fasgd_selftest_product_limit: ns must be in [10^6, 10^9]");
+    fasgd::set_wait_limit((uint64_t)ns);
+    return FASGD_OK;
+}
+
 int64_t fasgd_multiply_workspace(const fasgd_multiply_args* u) {
     const char* call = "fasgd_multiply_workspace";
     if (u == nullptr) {

@@ -102,6 +102,8 @@ struct TilePlan {
 };
 TilePlan plan_tiles(const Product& p);      // by sizes alone
 cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t stream);
+// ns without a copy after which a launch's waits give up, of launches from now on (10^9 before the first call).
+void set_wait_limit(uint64_t ns);
 // out = the sum of `count` parts, `step` values apart, each [groups of ragged k][n][m], as p stores it.
 cudaError_t launch_fold(const Product& p, const float* parts, int64_t step, int32_t count, cudaStream_t stream);
 // The values of the parts that launch_product needs room for.

@@ -20,12 +20,13 @@
 // limit leaves: 1,550 to 1,930 TFLOP/s (bf16, 8,192 rows; 1,800 for 32,768 rows in 32 experts of 4,096 x
 // 2,048).  Short products are bound by a launch's latency (6 us) and 0.3 us for each 64 of k.
 //
-// Every wait is bounded (kWaitLimitNs): a wait that runs out raises the block's flag, every
+// Every wait is bounded (wait_thread): one that runs out raises the block's flag, every
 // role leaves, and what was not computed is written as NaN.
 
 #include <cuda.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "client.cuh"
 #include "pdl.cuh"
@@ -61,6 +62,7 @@ struct TileArgs {
     int64_t m_tiles, items;    // items: of all groups, unless n is ragged
     int32_t splits;
     int32_t tile_n;            // of a tile
+    uint64_t limit;            // ns: see wait_thread
 };
 
 // ---- PTX ------------------------------------------------------------------------------
@@ -94,27 +96,6 @@ __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
             : "r"(bar), "r"(parity)
             : "memory");
     return ok != 0;
-}
-// One thread waits for a phase; false (and *late): it did not come.  The timer is read only
-// after a while: that takes as long as the MMAs of some k.
-template <bool CLUSTER = false>
-__device__ __forceinline__ bool wait_thread(uint64_t* barrier, uint32_t parity, volatile int32_t* late, uint64_t more = 0) {
-    const uint32_t bar = smem_addr(barrier);
-    uint64_t t0 = 0;
-    for (uint32_t i = 1; i < (1u << 30); ++i) {
-        if (test<CLUSTER>(bar, parity)) return true;
-        if ((i & 255u) == 0) {
-            const uint64_t now = global_ns();
-            if (t0 == 0) t0 = now;
-            if (now - t0 > kWaitLimitNs + more || *late != 0) break;
-        }
-    }
-    *late = 1;
-    return false;
-}
-// A whole warp.
-__device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, volatile int32_t* late, uint64_t more = 0) {
-    return __all_sync(0xffffffffu, wait_thread(barrier, parity, late, more));
 }
 template <bool CLUSTER = false>
 __device__ __forceinline__ void arrive_first(uint64_t* bar) {
@@ -230,9 +211,44 @@ struct Shared {
     float2 halves[2][kBlockM];          // statistics of the tile's odd columns' half, by tiles in turn
     uint32_t tmem;
     volatile int32_t late;
+    volatile uint32_t copies;           // stages that the block has issued copies of
+    uint64_t limit;                     // ns without one after which a wait gives up
     int32_t first[kMaxGroups + 1];      // ragged n: the first n tile of each group
     int32_t lo[kMaxGroups], hi[kMaxGroups];      // ragged products: the groups' rows
 };
+
+// One thread waits for a phase; false (and s.late): it did not come.  It gives up where the block has issued no
+// copy for s.limit ns, however long its launch takes: a wait for a group's last rows lasts through all tiles
+// before them.  The barrier is then tested for a while more, so that time in which the GPU is another
+// context's does not count.  The timer is read only after a while: that takes as long as the MMAs of some k.
+constexpr uint32_t kAgain = 64;                     // times 256 tests
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool wait_thread(uint64_t* barrier, uint32_t parity, Shared& s) {
+    const uint32_t bar = smem_addr(barrier);
+    uint64_t since = 0;
+    uint32_t seen = 0, again = 0;
+    for (uint32_t i = 1; i < (1u << 30); ++i) {
+        if (test<CLUSTER>(bar, parity)) return true;
+        if ((i & 255u) == 0) {
+            const uint64_t now = global_ns();
+            const uint32_t copies = s.copies;
+            if (s.late != 0) break;
+            if (since == 0 || copies != seen) {
+                since = now;
+                seen = copies;
+                again = i = 0;
+            } else if (now - since > s.limit && ++again > kAgain) {
+                break;
+            }
+        }
+    }
+    s.late = 1;
+    return false;
+}
+// A whole warp.
+__device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, Shared& s) {
+    return __all_sync(0xffffffffu, wait_thread(barrier, parity, s));
+}
 
 // lo, hi and first[] of the groups, by the first warp.  Offsets that rise and fall may claim more rows than
 // there are: numbers stay within 31 bits all the same.
@@ -449,6 +465,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             mbar_init(&s.taken[i], kEnds * PAIR);
         }
         s.late = 0;
+        s.copies = 0;
+        s.limit = t.limit;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -483,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             if (elected()) {
                 const uint32_t to = smem_addr(ring);
                 const uint32_t full = PAIR == 2 ? first_block(smem_addr(&s.full[0])) : smem_addr(&s.full[0]);
-                uint32_t stage = 0, phase = 0;
+                uint32_t stage = 0, phase = 0, copies = 0;
                 bool ok = true;
                 for (int64_t i = team; i < items && ok; i += teams) {
                     const Tile w = tile_of<PAIR>(t, s, sizes, i);
@@ -494,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                         const int32_t pa = pairs > 1 ? plane_a(pair) : 0, pb = pairs > 1 ? plane_b(pair) : 0;
                         for (int64_t k64 = w.k0; k64 < w.k1; k64 += kK) {
                             const int32_t k = (int32_t)k64;
-                            if (!(ok = wait_thread(&s.empty[stage], phase ^ 1, &s.late))) break;
+                            if (!(ok = wait_thread(&s.empty[stage], phase ^ 1, s))) break;
                             const uint32_t bar = cut(p, w, k64) ? smem_addr(&s.tail[stage]) : full + 8 * stage;
                             const uint32_t to_a = to + stage * S::kStage, to_b = to_a + kSideA;
                             arrive_expect(bar, x.bytes);
@@ -515,6 +533,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                             else
                                 for (int j = 0; j < x.boxes_b; ++j)
                                     copy_box<PAIR>(&t.b, to_b + j * 8192, bar, n0 + j * 64, k, 0, 0, pb);
+                            s.copies = ++copies;
                             if (++stage == S::kStages) {
                                 stage = 0;
                                 phase ^= 1;
@@ -542,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                         copies = (uint32_t)((copies + (w.k1 - w.k0 + kK - 1) / kK) % S::kStages);
                         if (rows == 0) continue;
                         const uint32_t stage = (copies + S::kStages - 1) % S::kStages;
-                        if (!(ok = wait(&s.tail[stage], used >> stage & 1, &s.late))) break;
+                        if (!(ok = wait(&s.tail[stage], used >> stage & 1, s))) break;
                         used ^= 1u << stage;
                         const int chunks = (int)(boxes_of<PAIR>(t, w).bytes / 8192);
                         char* const at = ring + stage * S::kStage;
@@ -597,14 +616,14 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     int in = 0;                           // blocks of this pair of planes
                     for (int done = 0; done < all && ok; done += chunk) {
                         const int until = min(done + chunk, all);
-                        if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, &s.late))) break;
+                        if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, s))) break;
                         fence_after();
                         const uint32_t to = tmem + (tile & 1) * kTileN;
                         uint32_t add = 0;
                         for (int k = done; k < until; ++k) {
                             const bool end = ++in == each;
-                            ok = PAIR == 2 && cuts && end ? wait_thread<true>(&s.full[stage], phase, &s.late)
-                                                          : wait_thread(&s.full[stage], phase, &s.late);
+                            ok = PAIR == 2 && cuts && end ? wait_thread<true>(&s.full[stage], phase, s)
+                                                          : wait_thread(&s.full[stage], phase, s);
                             if (!ok) break;
                             fence_after();
                             const uint32_t a = (uint32_t)a0 + stage * (S::kStage >> 4), b = (uint32_t)b0 + stage * (S::kStage >> 4);
@@ -717,8 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 // instruction cache (for all 128 at once the code outgrew it: 38,000 cycles a tile of g).
                 const uint32_t buffer = tile & 1;
                 if (blocks > 0) {
-                    // (of hundreds of millions of k the sums alone take a second)
-                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late, (uint64_t)blocks * 4000);
+                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, s);
                     ++tile;
                     fence_after();
                 }
@@ -744,7 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
                 for (int64_t k = 0; k < blocks; k += kExact / kK) {
                     const uint32_t buffer = tile & 1;
-                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, &s.late);
+                    ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, s);
                     ++tile;
                     fence_after();
                     if (!ok) break;
@@ -836,6 +854,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
 }
 
 // ---- host -------------------------------------------------------------------------------
+std::atomic<uint64_t> wait_limit{kWaitLimitNs};
+
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -960,6 +980,8 @@ TilePlan plan_tiles(const Product& p) {
     return best;
 }
 
+void set_wait_limit(uint64_t ns) { wait_limit.store(ns, std::memory_order_relaxed); }
+
 cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t stream) {
     int device = 0, sms = 0;
     cudaError_t st = cudaGetDevice(&device);
@@ -968,6 +990,7 @@ cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t st
     TileArgs t = {};
     t.p = p;
     t.splits = plan.splits;
+    t.limit = wait_limit.load(std::memory_order_relaxed);
     return plan.pair == 2 ? launch<2>(t, device, sms, stream) : launch<1>(t, device, sms, stream);
 }
 

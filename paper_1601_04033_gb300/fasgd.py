@@ -83,6 +83,7 @@ SIGNATURES = {
     "fasgd_multiply_workspace": (_i64, [_p]),
     "fasgd_score": (_i32, [_p, _p]),
     "fasgd_score_workspace": (_i64, [_p]),
+    "fasgd_selftest_product_limit": (_i32, [_i64]),
     "fasgd_last_error": (ctypes.c_char_p, [_p]),
 }
 
@@ -365,6 +366,10 @@ def fasgd_score(a, stream):
 
 def fasgd_score_workspace(a):
     return LIB.fasgd_score_workspace(a)
+
+
+def fasgd_selftest_product_limit(ns):
+    return LIB.fasgd_selftest_product_limit(ns)
 
 
 def fasgd_last_error(h) -> str:

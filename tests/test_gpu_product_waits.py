@@ -1,0 +1,47 @@
+"""The bounded waits inside the products on the tensor cores."""
+
+import pytest
+
+from test_gpu_client import _c
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture
+def limit():
+    """Sets the time without a copy after which waits give up."""
+    from paper_1601_04033_gb300 import fasgd
+
+    def set_limit(ns):
+        assert fasgd.fasgd_selftest_product_limit(ns) == 0
+
+    yield set_limit
+    set_limit(1_000_000_000)
+
+
+@pytest.mark.parametrize("rows, width, dtype", [(1 << 16, 4096, torch.float32), (1 << 17, 8192, torch.bfloat16)])
+def test_a_groups_last_rows_may_come_late(limit, rows, width, dtype):
+    """Groups of whole copies (multiples of 64 rows), which keep the tensor cores for ten milliseconds, before
+    one whose last copy is cut: the wait for that begins with the launch.  Copies go on all the while, so that
+    it lasts longer than a limit of one millisecond."""
+    c = _c()
+    limit(1_000_000)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    n = rows + 67
+    x, dy = (torch.randn(n, width, generator=g, device="cuda", dtype=dtype) for _ in range(2))
+    offsets = torch.tensor([0, rows, n], dtype=torch.int32, device="cuda")
+    w = torch.empty(2, width, width, dtype=dtype, device="cuda")
+    before, after = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    before.record()
+    dw = c.multiply_grad(x, w, offsets, dy, grads=(False, True)).w
+    after.record()
+    assert dw.isfinite().all()
+    assert before.elapsed_time(after) > 5.0
+    cols = slice(width // 2, width // 2 + 32)
+    for e, (a, b) in enumerate(((0, rows), (rows, n))):
+        want = x[a:b, cols].double().t() @ dy[a:b].double()
+        size = x[a:b, cols].double().abs().t() @ dy[a:b].double().abs()
+        # (a sum of b - a products in fp32, as elsewhere; roundings to 16 bits)
+        u = torch.finfo(dtype).eps / 2
+        assert bool(((dw[e, cols].double() - want).abs() <= (b - a) * 2.0 ** -23 * size * 33 / 32 + u * want.abs() * (1 + 2.0 ** -8)).all())
