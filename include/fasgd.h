@@ -844,13 +844,26 @@ FASGD_API int fasgd_score(const fasgd_score_args* a, void* stream);
 FASGD_API int64_t fasgd_score_workspace(const fasgd_score_args* a);
 
 /*
- * fasgd_selftest_product_limit -- the products of fasgd_multiply(_grad) and fasgd_score on the
- * tensor cores wait inside their kernels for copies, products and stores.  Such a wait
- * gives up where the block has not issued a copy for a second; results that are not there
- * then are NaN.  This sets that time, of launches from now on, for tests: ns in
- * [10^6, 10^9], which is the ordinary one.  Errors: EINVAL.
+ * fasgd_client_sync -- wait until `stream` is idle; *late = 1 if a wait inside a product ran
+ * out in a call on the current device since this was last asked, else 0.  The products of
+ * fasgd_multiply(_grad) and fasgd_score on the tensor cores wait inside their kernels for
+ * copies, MMAs and stores; such a wait gives up where its block has not issued a copy for
+ * a second, rather than hang, and results that are not there then are NaN.  The calls
+ * have returned FASGD_OK by then: a caller that needs to tell this from NaN in its data
+ * asks here, once a step or as often as it reads results.  (Calls on other streams may
+ * not have ended.)  Not while the stream is being captured.  Errors: EINVAL, ECUDA.
+ */
+FASGD_API int fasgd_client_sync(int32_t* late, void* stream);
+
+/*
+ * fasgd_selftest_product_limit -- that time without a copy, of launches of this process from
+ * now on, for tests: ns in [10^6, 10^9], which is the ordinary one.  Errors: EINVAL.
+ * fasgd_selftest_product_wait -- sets it and enqueues one small kernel in which one thread
+ * and one warp wait, by the products' own code, for a barrier that nobody arrives at: the next
+ * fasgd_client_sync finds it.  Errors: EINVAL, ECUDA.
  */
 FASGD_API int fasgd_selftest_product_limit(int64_t ns);
+FASGD_API int fasgd_selftest_product_wait(int64_t ns, void* stream);
 
 /* Text of the last failure on h, or, when h is NULL, of the last failed call
  * made without a handle (fasgd_create, bfasgd_fetch_apply, fasgd_sim_*,

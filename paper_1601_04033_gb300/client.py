@@ -8,7 +8,7 @@ points of the same names in include/fasgd.h, which say what they compute; they r
 torch's current stream and allocate their outputs and workspace from torch, on
 that stream.  ``dropped``, ``joined``, ``balanced``, ``gathered``, ``combined``,
 ``multiplied`` and ``scored`` are the same calls inside torch's automatic
-differentiation.
+differentiation.  ``sync`` waits for them and raises where a product gave up.
 
 Activations are fp32, bf16 or fp16 CUDA tensors, [..., cols], rows evenly spaced;
 parameters (norm weights and biases, a learned gate, experts' matrices) are fp32 --
@@ -688,6 +688,16 @@ def score(z, w, labels, *, upstream=None, grad=True, grads=(True, True), known: 
     del space
     _written(*given)
     return Score(loss, rows, dz, dw, lse)
+
+
+def sync():
+    """fasgd_client_sync: waits for torch's current stream, and raises where a wait inside a
+    product has run out on this device since the last call, so that its results are NaN."""
+    late = ctypes.c_int32()
+    device = torch._C._cuda_getDevice()
+    _check(_f.fasgd_client_sync(ctypes.byref(late), _f._current_stream() if _raw_stream is None else _raw_stream(device)))
+    if late.value:
+        raise _f.FasgdError(_f.EDEVICE, "a wait inside a product on the tensor cores ran out: its results are NaN")
 
 
 # ---------------------------------------------------------------------------

@@ -349,6 +349,22 @@ int fasgd_combine_grad(const fasgd_exchange_args* u, void* stream) {
     return exchange("fasgd_combine_grad", u, fasgd::kCombineGrad, stream);
 }
 
+int fasgd_client_sync(int32_t* late, void* stream_) {
+    const char* call = "fasgd_client_sync";
+    const auto stream = static_cast<cudaStream_t>(stream_);
+    if (late == nullptr) return fail(FASGD_EINVAL, "%s: late is NULL", call);
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    const cudaError_t st = cudaStreamIsCapturing(stream, &capture);
+    if (st != cudaSuccess) return cuda_status(st, call);
+    if (capture != cudaStreamCaptureStatusNone) return fail(FASGD_EINVAL, "%s: the stream is being captured", call);
+    return cuda_status(fasgd::read_late(late, stream), call);
+}
+
+int fasgd_selftest_product_wait(int64_t ns, void* stream) {
+    const int rc = fasgd_selftest_product_limit(ns);
+    return rc != FASGD_OK ? rc : cuda_status(fasgd::launch_expiry(static_cast<cudaStream_t>(stream)), "fasgd_selftest_product_wait");
+}
+
 int fasgd_selftest_product_limit(int64_t ns) {
     if (ns < 1000000 || ns > 1000000000) return fail(FASGD_EINVAL, "fasgd_selftest_product_limit: ns must be in [10^6, 10^9]");
     fasgd::set_wait_limit((uint64_t)ns);

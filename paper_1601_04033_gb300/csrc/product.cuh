@@ -104,6 +104,9 @@ TilePlan plan_tiles(const Product& p);      // by sizes alone
 cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t stream);
 // ns without a copy after which a launch's waits give up, of launches from now on (10^9 before the first call).
 void set_wait_limit(uint64_t ns);
+// Waits for the stream; whether a launch's wait ran out on this device since the last call.
+cudaError_t read_late(int32_t* late, cudaStream_t stream);
+cudaError_t launch_expiry(cudaStream_t stream);      // a kernel whose waits run out
 // out = the sum of `count` parts, `step` values apart, each [groups of ragged k][n][m], as p stores it.
 cudaError_t launch_fold(const Product& p, const float* parts, int64_t step, int32_t count, cudaStream_t stream);
 // The values of the parts that launch_product needs room for.

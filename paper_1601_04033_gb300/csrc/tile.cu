@@ -250,6 +250,9 @@ __device__ __forceinline__ bool wait(uint64_t* barrier, uint32_t parity, Shared&
     return __all_sync(0xffffffffu, wait_thread(barrier, parity, s));
 }
 
+// Whether a wait of a launch on this device ran out since the host last asked (read_late).
+__device__ int32_t waits_ran_out;
+
 // lo, hi and first[] of the groups, by the first warp.  Offsets that rise and fall may claim more rows than
 // there are: numbers stay within 31 bits all the same.
 __device__ void count_tiles(const Product& p, Shared& s) {
@@ -837,6 +840,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     }
     fence_before();
     __syncthreads();
+    if (threadIdx.x == 0 && s.late != 0) waits_ran_out = 1;
     if (PAIR == 2) {      // no block leaves while its pair may still reach its memory
         asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
@@ -851,6 +855,23 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kColumns));
         }
     }
+}
+
+// One thread's and a warp's wait for a barrier that nobody arrives at.
+__global__ void __launch_bounds__(64) expiry_kernel(uint64_t limit) {
+    __shared__ Shared s;
+    if (threadIdx.x == 0) {
+        mbar_init(&s.full[0], 1);
+        s.late = 0;
+        s.copies = 0;
+        s.limit = limit;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) wait_thread(&s.full[0], 0, s);
+    if (threadIdx.x >= 32) wait(&s.full[0], 0, s);
+    __syncthreads();
+    if (threadIdx.x == 0 && s.late != 0) waits_ran_out = 1;
 }
 
 // ---- host -------------------------------------------------------------------------------
@@ -981,6 +1002,24 @@ TilePlan plan_tiles(const Product& p) {
 }
 
 void set_wait_limit(uint64_t ns) { wait_limit.store(ns, std::memory_order_relaxed); }
+
+cudaError_t launch_expiry(cudaStream_t stream) {
+    expiry_kernel<<<1, 64, 0, stream>>>(wait_limit.load(std::memory_order_relaxed));
+    return cudaGetLastError();
+}
+
+cudaError_t read_late(int32_t* late, cudaStream_t stream) {
+    int32_t is = 0;
+    const int32_t none = 0;
+    cudaError_t st = cudaMemcpyFromSymbolAsync(&is, waits_ran_out, sizeof is, 0, cudaMemcpyDeviceToHost, stream);
+    if (st == cudaSuccess) st = cudaStreamSynchronize(stream);
+    if (st == cudaSuccess && is != 0) {
+        st = cudaMemcpyToSymbolAsync(waits_ran_out, &none, sizeof none, 0, cudaMemcpyHostToDevice, stream);
+        if (st == cudaSuccess) st = cudaStreamSynchronize(stream);
+    }
+    if (st == cudaSuccess) *late = is;
+    return st;
+}
 
 cudaError_t launch_tiles(const Product& p, const TilePlan& plan, cudaStream_t stream) {
     int device = 0, sms = 0;

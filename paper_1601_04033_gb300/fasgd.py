@@ -83,7 +83,9 @@ SIGNATURES = {
     "fasgd_multiply_workspace": (_i64, [_p]),
     "fasgd_score": (_i32, [_p, _p]),
     "fasgd_score_workspace": (_i64, [_p]),
+    "fasgd_client_sync": (_i32, [_p, _p]),
     "fasgd_selftest_product_limit": (_i32, [_i64]),
+    "fasgd_selftest_product_wait": (_i32, [_i64, _p]),
     "fasgd_last_error": (ctypes.c_char_p, [_p]),
 }
 
@@ -368,8 +370,16 @@ def fasgd_score_workspace(a):
     return LIB.fasgd_score_workspace(a)
 
 
+def fasgd_client_sync(late, stream):
+    return LIB.fasgd_client_sync(late, stream)
+
+
 def fasgd_selftest_product_limit(ns):
     return LIB.fasgd_selftest_product_limit(ns)
+
+
+def fasgd_selftest_product_wait(ns, stream):
+    return LIB.fasgd_selftest_product_wait(ns, stream)
 
 
 def fasgd_last_error(h) -> str:

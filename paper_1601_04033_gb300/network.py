@@ -144,7 +144,9 @@ def train(net: RoutedNetwork, *, lam=8, batches=200, K=2, alpha=2.0, variant=fas
         srv.pull(theta)
         with torch.no_grad():
             scores, balance, _ = net.forward(theta, held[0])
-            return float(torch.nn.functional.cross_entropy(scores, held[1]) + balance)
+            loss = float(torch.nn.functional.cross_entropy(scores, held[1]) + balance)
+        client.sync()       # no gradient since the last time is NaN for a wait that ran out
+        return loss
 
     losses = [held_out()]
     for b, batch in enumerate(streams.dispatch_schedule(net.seed, lam, batches, K)):

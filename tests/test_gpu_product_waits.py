@@ -45,3 +45,38 @@ def test_a_groups_last_rows_may_come_late(limit, rows, width, dtype):
         # (a sum of b - a products in fp32, as elsewhere; roundings to 16 bits)
         u = torch.finfo(dtype).eps / 2
         assert bool(((dw[e, cols].double() - want).abs() <= (b - a) * 2.0 ** -23 * size * 33 / 32 + u * want.abs() * (1 + 2.0 ** -8)).all())
+
+
+def test_a_wait_that_runs_out_is_reported(limit):
+    """Failure detection without a fault: a kernel whose barrier nobody arrives at gives up after the limit
+    and returns; the next sync says so, once, and products are as before."""
+    from paper_1601_04033_gb300 import fasgd
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, w = torch.randn(300, 64, generator=g, device="cuda").bfloat16(), torch.randn(1, 64, 40, generator=g, device="cuda").bfloat16()
+    offsets = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+    y = c.multiply(x, w, offsets)
+    c.sync()
+    for stream in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(stream):
+            assert fasgd.fasgd_selftest_product_wait(5_000_000, stream.cuda_stream) == 0
+            with pytest.raises(fasgd.FasgdError, match="ran out") as e:
+                c.sync()
+            assert e.value.code == fasgd.EDEVICE
+            c.sync()
+            assert torch.equal(c.multiply(x, w, offsets), y)
+            c.sync()
+
+
+def test_sync_is_refused_in_a_capture():
+    from paper_1601_04033_gb300 import fasgd
+    c = _c()
+    graph = torch.cuda.CUDAGraph()
+    t = torch.zeros(4, device="cuda")
+    with torch.cuda.graph(graph):
+        t.add_(1.0)
+        with pytest.raises(fasgd.FasgdError, match="captured"):
+            c.sync()
+    graph.replay()
+    assert t.sum() == 4.0
+    c.sync()
