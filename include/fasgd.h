@@ -761,11 +761,13 @@ FASGD_API int fasgd_combine_grad(const fasgd_exchange_args* a, void* stream);
  * fasgd_multiply_grad -- given dy: dx[i] = dy[i] w[e]^T (0 where no expert has the row) and
  * dw[e] = sum_i x[i]^T dy[i] (0 for an expert without rows), of type w_dtype and laid out
  * by ld_dw, step_dw and dw_flip.  dx or dw may be NULL.  x is read for dw only, w for dx.
- * Sums are fp32, in an order that the arguments fix.  Rows that no expert has are not
- * read, whatever they hold.
+ * Sums are fp32, in an order that the arguments fix, and values that are not finite make
+ * results as fp32 products and sums do; but in large products of FASGD_F32 (from rows x inputs x
+ * outputs = 2^28 on) a product of two finite values beyond fp32's range may make NaN of
+ * an infinite result.  Rows that no expert has are not read, whatever they hold.
  * rows < 2^31; inputs, outputs <= FASGD_COLS_MAX; experts <= FASGD_EXPERTS_MAX.
  * Fastest are bases and ld of multiples of 16 bytes: 16-bit matrices that lie otherwise are copied
- * first, as are fp32 ones of large products (times 1.5).
+ * first, as are fp32 ones of large products (times 2).
  * workspace: 256-byte aligned device memory of at least fasgd_multiply_workspace() bytes
  * (for fasgd_multiply_grad where dx or dw is given, else for fasgd_multiply), which the
  * sizes, types, strides and alignments fix (-1 on a bad argument).
@@ -814,7 +816,7 @@ FASGD_API int64_t fasgd_multiply_workspace(const fasgd_multiply_args* a);
  * workspace: 256-byte aligned device memory of at least fasgd_score_workspace() bytes (-1 on
  * a bad argument): what grows with rows x classes in it are FASGD_SCORE_PIECE bytes for g
  * (or 64 classes of it) at most and 8 bytes for each row and 192 classes (64 for small fp32
- * products); besides, copies of z, and of w where it is not aligned to 16 bytes or of fp32 (times 1.5), and
+ * products); besides, copies of z, and of w where it is not aligned to 16 bytes or of fp32 (times 2), and
  * fp32 sums of dz.
  */
 #define FASGD_CLASSES_MAX ((int64_t)1 << 24)

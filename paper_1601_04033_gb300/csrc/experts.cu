@@ -151,7 +151,7 @@ fasgd::Product product(const Multiply& m) {
 // y (or dx) by rows: `to` columns from `from`, w's side across or not.
 fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across, const fasgd::Side& x, void* y, int64_t ld_y) {
     fasgd::Product p = product(m);
-    p.a = {m.w(), m.w_ld, m.w_step, across, m.w_plane};
+    p.a = {m.w(), m.w_ld, m.w_step, across, m.w_plane, m.planes ? 4 : 0};
     p.b = x;
     p.m = to;
     p.n = m.u.rows;
@@ -162,15 +162,15 @@ fasgd::Product by_rows(const Multiply& m, int64_t from, int64_t to, bool across,
     return p;
 }
 fasgd::Product product_y(const Multiply& m) {
-    return by_rows(m, m.u.inputs, m.u.outputs, !m.u.w_flip, {m.x(), m.x_ld, 0, 0, m.x_plane}, m.u.y, m.u.ld_y);
+    return by_rows(m, m.u.inputs, m.u.outputs, !m.u.w_flip, {m.x(), m.x_ld, 0, 0, m.x_plane, m.planes ? 4 : 0}, m.u.y, m.u.ld_y);
 }
 fasgd::Product product_dx(const Multiply& m) {
-    return by_rows(m, m.u.outputs, m.u.inputs, m.u.w_flip, {m.dy(), m.dy_ld, 0, 0, m.dy_plane}, m.u.dx, m.u.ld_dx);
+    return by_rows(m, m.u.outputs, m.u.inputs, m.u.w_flip, {m.dy(), m.dy_ld, 0, 0, m.dy_plane, m.planes ? 4 : 0}, m.u.dx, m.u.ld_dx);
 }
 fasgd::Product by_experts(const Multiply& m) {
     const fasgd_multiply_args& u = m.u;
     fasgd::Product p = product(m);
-    const fasgd::Side x = {m.x(), m.x_ld, 0, 1, m.x_plane}, dy = {m.dy(), m.dy_ld, 0, 1, m.dy_plane};
+    const fasgd::Side x = {m.x(), m.x_ld, 0, 1, m.x_plane, m.planes ? 4 : 0}, dy = {m.dy(), m.dy_ld, 0, 1, m.dy_plane, m.planes ? 4 : 0};
     p.a = u.dw_flip ? x : dy;
     p.b = u.dw_flip ? dy : x;
     p.m = u.dw_flip ? u.inputs : u.outputs;
@@ -203,11 +203,11 @@ int64_t lay_out(Multiply& m, char* base) {
     m.planes = u.dtype == FASGD_F32 && fasgd::by_planes(u.rows, u.outputs, u.inputs);
     const bool tiles = u.dtype != FASGD_F32;
     const auto fits = [&](const void* p, int64_t ld, int64_t step, int64_t groups) {
-        return !m.planes && (!tiles || fasgd::tile_side({p, ld, step, 0, 0}, groups));
+        return !m.planes && (!tiles || fasgd::tile_side({p, ld, step, 0, 0, 0}, groups));
     };
     const auto copy = [&](int64_t values, int64_t& plane) {
         plane = values;
-        return take(m.planes ? 6 * values : values * m.size);
+        return take(m.planes ? 8 * values : values * m.size);
     };
     if ((!m.grad || u.dx != nullptr) && (u.w_dtype != u.dtype || !fits(u.w, u.ld_w, u.step_w, u.experts))) {
         const int64_t rows = u.w_flip ? u.outputs : u.inputs, cols = u.w_flip ? u.inputs : u.outputs;

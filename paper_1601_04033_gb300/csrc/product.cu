@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(256) plain_kernel(Product p, int32_t splits) {
 }
 
 // Copies of a side, eight values a thread: 16-byte stores, and 16-byte loads where the side has them.
-// PLANES: fp32 to three bf16 planes.
+// PLANES: fp32 to four bf16 planes.
 template <class F, class T, bool WIDE, bool PLANES>
 __global__ void __launch_bounds__(256) pack_kernel(Pack p) {
     const int64_t g = blockIdx.y, octets = (p.cols + 7) / 8, all = p.rows * octets;
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(256) pack_kernel(Pack p) {
             for (int j = 0; j < 8; ++j) v[j] = j < most ? from[j] : from_f32<F>(0.0f);
         }
         T* to = static_cast<T*>(p.to) + g * p.step_to + (p.to_row != nullptr ? p.to_row[r] : r) * p.ld_to + c;
-        alignas(16) T out[PLANES ? 3 : 1][8];
+        alignas(16) T out[PLANES ? 4 : 1][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float x = has ? to_f32(v[j]) : 0.0f;
@@ -290,12 +290,13 @@ __global__ void __launch_bounds__(256) pack_kernel(Pack p) {
                 planes_of(x, y);
 #pragma unroll
                 for (int k = 0; k < 3; ++k) out[k][j] = y[k];
+                out[3][j] = isfinite(x) ? y[0] : from_f32<T>(0.0f);
             } else {
                 out[0][j] = from_f32<T>(x);
             }
         }
 #pragma unroll
-        for (int k = 0; k < (PLANES ? 3 : 1); ++k)
+        for (int k = 0; k < (PLANES ? 4 : 1); ++k)
 #pragma unroll
             for (int j = 0; j < (int)sizeof(T) / 2; ++j)
                 reinterpret_cast<uint4*>(to + k * p.plane)[j] = reinterpret_cast<const uint4*>(out[k])[j];

@@ -19,7 +19,8 @@ struct Side {
     const void* p;
     int64_t ld, step;
     int32_t across;
-    int64_t plane;      // fp32 values as three bf16 ones: from one of them to the next (launch_tiles)
+    int64_t plane;      // fp32 values in bf16 planes: from one of them to the next (launch_tiles)
+    int32_t planes;     // how many: 4, or 3 of values that are finite or reach only results that are NaN
 };
 
 enum Ragged {
@@ -47,7 +48,7 @@ struct Product {
     int64_t ld_out, step_out;
     int64_t step_split;          // launch_tiles: from one part of k's sums to the next
     int64_t step_plane;          // kResidual of planes: from one to the next
-    int32_t planes;              // the sides are fp32 values as three planes of dtype FASGD_BF16
+    int32_t planes;              // the sides are fp32 values in planes of dtype FASGD_BF16
     int32_t out_dtype;
     int32_t exact;               // sums to fp32's accuracy (launch_tiles: the tensor cores' additions cut bits off)
     int32_t add;                 // kStore, fp32: out += instead
@@ -79,11 +80,15 @@ int32_t plain_splits(const Product& p);
 // fp32 values take part as three bf16 ones each (rounded, then what is left, twice: x = x0 + x1 + x2 to
 // 2^-27), in the six products of them that reach 2^-26:
 // x2 y0, x0 y2, x1 y1, x1 y0, x0 y1, x0 y0.
+// An infinity is x0 alone, and may meet the other's largest part only: with the others, which are 0 or of either
+// sign, it would make NaN of an infinite result.  So there is a fourth plane, x0 where it is finite and else 0,
+// for the products with smaller parts.  (It is copied like the others, 8 bytes a value and not 6.)
 constexpr int kTileN = 256;
 constexpr int kPairs = 6;
 constexpr double kPlanesFrom = 1 << 28;
-__host__ __device__ constexpr uint32_t plane_a(uint32_t pair) { return 0x001102u >> 4 * pair & 15u; }
-__host__ __device__ constexpr uint32_t plane_b(uint32_t pair) { return 0x010120u >> 4 * pair & 15u; }
+// The planes of each pair, 4 bits a pair from the lowest on.
+constexpr uint32_t planes_a(int32_t planes) { return planes == 4 ? 0x031132u : 0x001102u; }
+constexpr uint32_t planes_b(int32_t planes) { return planes == 4 ? 0x013123u : 0x010120u; }
 bool tile_side(const Side& s, int64_t groups);
 // n of a tile of statistics.  A few rows' classes are one tile each of 152 SMs at a time: the width that
 // takes the least rounds times width (131,072 classes: four of 256 or of 224).
@@ -152,7 +157,7 @@ struct Pack {
     void* to;
     int64_t rows, cols, ld_from, step_from, ld_to, step_to;
     int32_t groups, dtype_from, dtype_to;
-    int64_t plane;               // fp32 to FASGD_BF16 in three planes this far apart; 0: one value each
+    int64_t plane;               // fp32 to FASGD_BF16 in four planes this far apart; 0: one value each
     const int32_t* offsets;
     const int64_t* labels;
     int64_t classes;
@@ -161,8 +166,8 @@ struct Pack {
 cudaError_t launch_pack(const Pack& p, cudaStream_t stream);
 
 #ifdef __CUDACC__
-// The planes of an fp32 value.  A value that would round to infinity in bf16 is cut instead; what is
-// not finite is its first plane alone.
+// The three parts of an fp32 value.  A value that would round to infinity in bf16 is cut instead; what is
+// not finite is its first part alone.
 __device__ __forceinline__ void planes_of(float x, __nv_bfloat16 (&to)[3]) {
     const bool finite = fabsf(x) <= 3.4028234e38f;
     to[0] = __float2bfloat16_rn(fabsf(x) < 3.38e38f || !finite ? x : __uint_as_float(__float_as_uint(x) & 0xffff0000u));

@@ -415,8 +415,8 @@ Product product_of_g(const Score& s) {
 Product product_dz(const Score& s, int64_t n) {
     const fasgd_score_args& u = s.u;
     Product q = product_of_g(s);
-    q.a = {s.w, s.ld_wc, 0, u.w_flip, s.plane_w};
-    q.b = {s.g, s.ld_g, 0, 1, s.plane_g};
+    q.a = {s.w, s.ld_wc, 0, u.w_flip, s.plane_w, 4};
+    q.b = {s.g, s.ld_g, 0, 1, s.plane_g, 3};
     q.m = u.cols;
     q.n = u.rows;
     q.k = n;
@@ -440,7 +440,7 @@ Product product_dz(const Score& s, int64_t n) {
 Product product_dw(const Score& s, int64_t n) {
     const fasgd_score_args& u = s.u;
     Product q = product_of_g(s);
-    const fasgd::Side zs = {s.z, s.ld_zc, 0, 1, s.plane_z}, gs = {s.g, s.ld_g, 0, 0, s.plane_g};
+    const fasgd::Side zs = {s.z, s.ld_zc, 0, 1, s.plane_z, 4}, gs = {s.g, s.ld_g, 0, 0, s.plane_g, 3};
     q.a = u.dw_flip ? zs : gs;
     q.b = u.dw_flip ? gs : zs;
     q.m = u.dw_flip ? u.cols : n;
@@ -490,11 +490,11 @@ int64_t lay_out(Score& s, char* base) {
     s.ld_zc = u.ld_z;
     s.ld_wc = u.ld_w;
     const auto fits = [&](const void* p, int64_t ld) {
-        return !s.planes && (u.dtype == FASGD_F32 || fasgd::tile_side({p, ld, 0, 0, 0}, 1));
+        return !s.planes && (u.dtype == FASGD_F32 || fasgd::tile_side({p, ld, 0, 0, 0, 0}, 1));
     };
     const auto copy = [&](int64_t values, int64_t& plane) {
         plane = values;
-        return take(s.planes ? 6 * values : values * s.size);
+        return take(s.planes ? 8 * values : values * s.size);
     };
     if (s.grad || s.first || !fits(u.z, u.ld_z)) {
         s.ld_zc = (u.cols + 7) / 8 * 8;
@@ -515,7 +515,8 @@ int64_t lay_out(Score& s, char* base) {
     const int64_t pieces = (u.classes + most - 1) / most;
     s.piece = (u.classes + pieces - 1) / pieces;
     if (pieces > 1) s.piece = std::min(s.piece / 64 * 64 + 64, most / 64 * 64);
-    s.g = copy(s.piece * s.ld_g, s.plane_g);
+    s.plane_g = s.piece * s.ld_g;
+    s.g = take(g_size * s.plane_g);
     s.factor = u.dtype == FASGD_F16 ? 16384.0f : 1.0f;
     int64_t parts = 0;
     s.dz_sum = nullptr;
@@ -584,8 +585,8 @@ cudaError_t run(const Score& s, cudaStream_t stream) {
         if ((st = fasgd::launch_pack(c, stream)) != cudaSuccess) return st;
     }
     Product p = {};
-    p.a = {z, ld_z, 0, 0, s.plane_z};
-    p.b = {w_all, ld_w, 0, !u.w_flip, s.plane_w};
+    p.a = {z, ld_z, 0, 0, s.plane_z, 4};
+    p.b = {w_all, ld_w, 0, !u.w_flip, s.plane_w, 4};
     p.m = u.rows;
     p.n = u.classes;
     p.k = u.cols;

@@ -63,6 +63,7 @@ struct TileArgs {
     int32_t splits;
     int32_t tile_n;            // of a tile
     uint64_t limit;            // ns: see wait_thread
+    uint32_t planes_a, planes_b;      // the pairs'
 };
 
 // ---- PTX ------------------------------------------------------------------------------
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     const int32_t m0 = (int32_t)(w.m0 + rank * kBlockM), n0 = (int32_t)(w.n0 + (int64_t)rank * x.rows_b);
                     const int32_t ga = p.ragged == kRaggedN ? w.group : 0;
                     for (uint32_t pair = 0; pair < pairs && ok; ++pair) {
-                        const int32_t pa = pairs > 1 ? plane_a(pair) : 0, pb = pairs > 1 ? plane_b(pair) : 0;
+                        const int32_t pa = t.planes_a >> 4 * pair & 15u, pb = t.planes_b >> 4 * pair & 15u;      // (one pair: 0)
                         for (int64_t k64 = w.k0; k64 < w.k1; k64 += kK) {
                             const int32_t k = (int32_t)k64;
                             if (!(ok = wait_thread(&s.empty[stage], phase ^ 1, s))) break;
@@ -898,7 +899,7 @@ bool encode(CUtensorMap* map, const Side& s, const Product& p, int64_t size, int
     const auto u = [](int64_t n) { return (cuuint64_t)n; };
     const cuuint64_t ld = u(s.ld) * 2, step = groups > 1 ? u(s.step) * 2 : ld;
     const cuuint64_t dims[5] = {u(wide ? 64 : s.across ? size : k), u(s.across ? k : size), u(wide ? size / 64 : 1), u(groups),
-                                p.planes ? 3u : 1u};
+                                p.planes ? (cuuint64_t)s.planes : 1u};
     const cuuint64_t strides[4] = {ld, wide ? 128 : ld, step, p.planes ? u(s.plane) * 2 : ld};
     const cuuint32_t boxes[5] = {64, (cuuint32_t)(s.across ? kK : box), wide ? (cuuint32_t)box / 64 : 1, 1, 1},
                      one[5] = {1, 1, 1, 1, 1};
@@ -940,6 +941,8 @@ cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
     const int64_t n_tiles = (p.n + t.tile_n - 1) / t.tile_n + (p.ragged == kRaggedN ? p.groups : 0);
     t.items = t.m_tiles * n_tiles * t.splits * (p.ragged == kRaggedK ? p.groups : 1);
     if (t.items == 0) return cudaSuccess;
+    t.planes_a = p.planes ? planes_a(p.a.planes) : 0;
+    t.planes_b = p.planes ? planes_b(p.b.planes) : 0;
     t.wide_a = p.a.across && p.m % 64 == 0;
     t.wide_b = p.b.across && p.n % 64 == 0 && t.tile_n == kTileN;
     if (!encode(&t.a, p.a, p, p.m, p.ragged == kRaggedN ? p.groups : 1, kBlockM, t.wide_a) ||
