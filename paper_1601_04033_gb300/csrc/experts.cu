@@ -181,7 +181,7 @@ fasgd::Product by_experts(const Multiply& m) {
     p.ld_out = u.ld_dw;
     p.step_out = u.step_dw;
     p.out_dtype = u.w_dtype;
-    p.exact = u.w_dtype == FASGD_F32;      // (a sum that is stored in 16 bits loses less than its rounding)
+    p.exact = u.w_dtype == FASGD_F32;      // (one that is stored in 16 bits loses less than its rounding: launch_tiles sees to that)
     return p;
 }
 

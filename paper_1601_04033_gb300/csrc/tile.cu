@@ -42,6 +42,12 @@ constexpr int kBlockM = 128;                        // m of a block
 constexpr int kEnds = 8;                            // warps that take results: two for each 32 lanes
 constexpr int kThreads = 128 + 32 * kEnds;          // warps 0 to 3: copies, MMAs, groups' last rows, one at rest
 constexpr int kExact = 256;                         // k of an accumulator where the sums are to be exact ones
+// An accumulator's additions cut bits off, always toward zero: each of n terms of one sign up to 2^-24 of what is
+// there, n / 2 2^-24 of the sum; measured is a quarter of that (16,384: 1.1e-4).  Up to kLongFrom that is at most the
+// 2^-11 by which rounding to fp16 is off; where sums are longer they leave the accumulator every kLong k and
+// go on in registers, 6e-5 at most (1.4e-5).  Going on like that from 2,048 on cost dw of 12,279 rows by 1,021 x 509
+// in 7 experts 5 us (a kernel more to fetch), and 8,192 x 2,048 x 131,072's score 2 %.
+constexpr int kLong = 2048, kLongFrom = 16384;
 constexpr int kSideA = kBlockM * kK * 2;            // bytes of A in a stage
 constexpr int kFew = 32;                             // rows of a box of a short tile
 constexpr int kMaxGroups = FASGD_EXPERTS_MAX;
@@ -445,9 +451,13 @@ __device__ void clear_rows(const Product& p, const Shared& s, int64_t block, int
     }
 }
 
-template <int PAIR, int ENDING, bool EXACT>
+// SUMS: kOne accumulator for all of k, or parts of k that are added up in registers: of kExact or kLong each.
+enum Sums { kOne, kExactParts, kLongParts };
+template <int PAIR, int ENDING, int SUMS>
 __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t) {
     using S = Shape<PAIR>;
+    constexpr bool EXACT = SUMS == kExactParts;
+    constexpr int kPart = SUMS == kLongParts ? kLong : kExact;
     extern __shared__ char raw[];
     __shared__ Shared s;
     char* const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
@@ -614,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 };
                 look();
                 while (blocks > 0 && ok) {
-                    const int each = blocks, all = each * (int)pairs, chunk = EXACT ? kExact / kK : all, mmas = last;
+                    const int each = blocks, all = each * (int)pairs, chunk = SUMS == kOne ? all : kPart / kK, mmas = last;
                     const uint32_t now = shape;
                     const bool cuts = zeroed;
                     int in = 0;                           // blocks of this pair of planes
@@ -735,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 else
                     write(static_cast<__half*>(target.out));
             };
-            if constexpr (!EXACT) {
+            if constexpr (SUMS == kOne) {
                 // 32 columns after the other, out of tensor memory and on their way: a loop that stays in the
                 // instruction cache (for all 128 at once the code outgrew it: 38,000 cycles a tile of g).
                 const uint32_t buffer = tile & 1;
@@ -764,7 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
-                for (int64_t k = 0; k < blocks; k += kExact / kK) {
+                for (int64_t k = 0; k < blocks; k += kPart / kK) {
                     const uint32_t buffer = tile & 1;
                     ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, s);
                     ++tile;
@@ -910,12 +920,12 @@ bool encode(CUtensorMap* map, const Side& s, const Product& p, int64_t size, int
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int PAIR, int ENDING, bool EXACT>
+template <int PAIR, int ENDING, int SUMS>
 cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStream_t stream) {
     static SharedLimit limit;
     const int bytes = Shape<PAIR>::kBytes;
     const int error = limit.ensure(device, bytes, bytes, [](int64_t n) {
-        return (int)cudaFuncSetAttribute(tile_kernel<PAIR, ENDING, EXACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
+        return (int)cudaFuncSetAttribute(tile_kernel<PAIR, ENDING, SUMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
     });
     if (error != 0) return (cudaError_t)error;
     cudaLaunchConfig_t cfg = {};
@@ -931,7 +941,7 @@ cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStr
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING, EXACT>, t);
+    return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING, SUMS>, t);
 }
 template <int PAIR>
 cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
@@ -952,13 +962,15 @@ cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
     switch (p.ending) {
         case kStore: {
             const bool exact = p.exact && p.out_dtype == FASGD_F32;
-            return exact ? launch<PAIR, kStore, true>(t, t.items, device, sms, stream)
-                         : launch<PAIR, kStore, false>(t, t.items, device, sms, stream);
+            // (of ragged k one group may have all)
+            return exact                                 ? launch<PAIR, kStore, kExactParts>(t, t.items, device, sms, stream)
+                   : p.k > (int64_t)kLongFrom * t.splits ? launch<PAIR, kStore, kLongParts>(t, t.items, device, sms, stream)
+                                                         : launch<PAIR, kStore, kOne>(t, t.items, device, sms, stream);
         }
-        case kStatistics: return launch<PAIR, kStatistics, true>(t, t.items, device, sms, stream);
+        case kStatistics: return launch<PAIR, kStatistics, kExactParts>(t, t.items, device, sms, stream);
         default:
-            return p.planes ? launch<PAIR, kResidual, true>(t, t.items, device, sms, stream)
-                            : launch<PAIR, kResidual, false>(t, t.items, device, sms, stream);
+            return p.planes ? launch<PAIR, kResidual, kExactParts>(t, t.items, device, sms, stream)
+                            : launch<PAIR, kResidual, kOne>(t, t.items, device, sms, stream);
     }
 }
 
