@@ -218,14 +218,14 @@ struct Shared {
     float2 halves[2][kBlockM];          // statistics of the tile's odd columns' half, by tiles in turn
     uint32_t tmem;
     volatile int32_t late;
-    volatile uint32_t copies;           // stages that the block has issued copies of
+    volatile uint32_t rounds;           // of the ring that the block has issued copies of
     uint64_t limit;                     // ns without one after which a wait gives up
     int32_t first[kMaxGroups + 1];      // ragged n: the first n tile of each group
     int32_t lo[kMaxGroups], hi[kMaxGroups];      // ragged products: the groups' rows
 };
 
 // One thread waits for a phase; false (and s.late): it did not come.  It gives up where the block has issued no
-// copy for s.limit ns, however long its launch takes: a wait for a group's last rows lasts through all tiles
+// copies for s.limit ns, however long its launch takes: a wait for a group's last rows lasts through all tiles
 // before them.  The barrier is then tested for a while more, so that time in which the GPU is another
 // context's does not count.  The timer is read only after a while: that takes as long as the MMAs of some k.
 constexpr uint32_t kAgain = 64;                     // times 256 tests
@@ -234,18 +234,23 @@ __device__ __forceinline__ bool wait_thread(uint64_t* barrier, uint32_t parity, 
     const uint32_t bar = smem_addr(barrier);
     uint64_t since = 0;
     uint32_t seen = 0, again = 0;
+#pragma unroll 1
     for (uint32_t i = 1; i < (1u << 30); ++i) {
         if (test<CLUSTER>(bar, parity)) return true;
         if ((i & 255u) == 0) {
             const uint64_t now = global_ns();
-            const uint32_t copies = s.copies;
-            if (s.late != 0) break;
-            if (since == 0 || copies != seen) {
+            if (since == 0) {
                 since = now;
-                seen = copies;
-                again = i = 0;
-            } else if (now - since > s.limit && ++again > kAgain) {
-                break;
+                seen = s.rounds;
+            }
+            if (now - since > s.limit || s.late != 0) {
+                const uint32_t rounds = s.rounds;
+                if (s.late != 0 || (rounds == seen && ++again > kAgain)) break;
+                if (rounds != seen) {
+                    since = now;
+                    seen = rounds;
+                    again = i = 0;
+                }
             }
         }
     }
@@ -479,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             mbar_init(&s.taken[i], kEnds * PAIR);
         }
         s.late = 0;
-        s.copies = 0;
+        s.rounds = 0;
         s.limit = t.limit;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -515,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             if (elected()) {
                 const uint32_t to = smem_addr(ring);
                 const uint32_t full = PAIR == 2 ? first_block(smem_addr(&s.full[0])) : smem_addr(&s.full[0]);
-                uint32_t stage = 0, phase = 0, copies = 0;
+                uint32_t stage = 0, phase = 0, rounds = 0;
                 bool ok = true;
                 for (int64_t i = team; i < items && ok; i += teams) {
                     const Tile w = tile_of<PAIR>(t, s, sizes, i);
@@ -547,10 +552,10 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                             else
                                 for (int j = 0; j < x.boxes_b; ++j)
                                     copy_box<PAIR>(&t.b, to_b + j * 8192, bar, n0 + j * 64, k, 0, 0, pb);
-                            s.copies = ++copies;
                             if (++stage == S::kStages) {
                                 stage = 0;
                                 phase ^= 1;
+                                s.rounds = ++rounds;      // (with every stage it cost 1 %)
                             }
                         }
                     }
@@ -874,7 +879,7 @@ __global__ void __launch_bounds__(64) expiry_kernel(uint64_t limit) {
     if (threadIdx.x == 0) {
         mbar_init(&s.full[0], 1);
         s.late = 0;
-        s.copies = 0;
+        s.rounds = 0;
         s.limit = limit;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
