@@ -457,12 +457,15 @@ __device__ void clear_rows(const Product& p, const Shared& s, int64_t block, int
 }
 
 // SUMS: kOne accumulator for all of k, or parts of k that are added up in registers: of kExact or kLong each.
+// PLANES: results of kResidual are the planes of fp32 values.
 enum Sums { kOne, kExactParts, kLongParts };
-template <int PAIR, int ENDING, int SUMS>
+template <int PAIR, int ENDING, int SUMS, bool PLANES = false>
 __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ TileArgs t) {
     using S = Shape<PAIR>;
     constexpr bool EXACT = SUMS == kExactParts;
-    constexpr int kPart = SUMS == kLongParts ? kLong : kExact;
+    // k of the parts, and of a tile's first one: for the residuals as long as the MMAs need to go on while the results of
+    // the tile before leave (with 256 they waited, and a score of 4,096 x 4,096 x 32,768 took 8 % longer).
+    constexpr int kPart = SUMS == kLongParts ? kLong : kExact, kFirst = ENDING == kResidual && !PLANES ? kLong : kPart;
     extern __shared__ char raw[];
     __shared__ Shared s;
     char* const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
@@ -633,8 +636,9 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     const uint32_t now = shape;
                     const bool cuts = zeroed;
                     int in = 0;                           // blocks of this pair of planes
-                    for (int done = 0; done < all && ok; done += chunk) {
-                        const int until = min(done + chunk, all);
+                    const auto part = [&](int done) { return SUMS != kOne && kFirst != kPart && done == 0 ? kFirst / kK : chunk; };
+                    for (int done = 0; done < all && ok; done += part(done)) {
+                        const int until = min(done + part(done), all);
                         if (!(ok = wait_thread(&s.taken[tile & 1], (tile >> 1 & 1) ^ 1, s))) break;
                         fence_after();
                         const uint32_t to = tmem + (tile & 1) * kTileN;
@@ -721,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 }
                 if (!live) return;
                 const int own_at = mine ? at - c : -1;
-                if (EXACT) {
+                if (PLANES) {
                     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(target.out) + base + c * target.ld;
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
@@ -779,7 +783,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[b][j] = 0.0f;
-                for (int64_t k = 0; k < blocks; k += kPart / kK) {
+                for (int64_t k = 0; k < blocks; k += (k == 0 ? kFirst : kPart) / kK) {
                     const uint32_t buffer = tile & 1;
                     ok = ok && wait(&s.ready[buffer], tile >> 1 & 1, s);
                     ++tile;
@@ -925,12 +929,12 @@ bool encode(CUtensorMap* map, const Side& s, const Product& p, int64_t size, int
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int PAIR, int ENDING, int SUMS>
+template <int PAIR, int ENDING, int SUMS, bool PLANES = false>
 cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStream_t stream) {
     static SharedLimit limit;
     const int bytes = Shape<PAIR>::kBytes;
     const int error = limit.ensure(device, bytes, bytes, [](int64_t n) {
-        return (int)cudaFuncSetAttribute(tile_kernel<PAIR, ENDING, SUMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
+        return (int)cudaFuncSetAttribute(tile_kernel<PAIR, ENDING, SUMS, PLANES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)n);
     });
     if (error != 0) return (cudaError_t)error;
     cudaLaunchConfig_t cfg = {};
@@ -946,7 +950,7 @@ cudaError_t launch(const TileArgs& t, int64_t most, int device, int sms, cudaStr
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING, SUMS>, t);
+    return cudaLaunchKernelEx(&cfg, tile_kernel<PAIR, ENDING, SUMS, PLANES>, t);
 }
 template <int PAIR>
 cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
@@ -974,8 +978,12 @@ cudaError_t launch(TileArgs& t, int device, int sms, cudaStream_t stream) {
         }
         case kStatistics: return launch<PAIR, kStatistics, kExactParts>(t, t.items, device, sms, stream);
         default:
-            return p.planes ? launch<PAIR, kResidual, kExactParts>(t, t.items, device, sms, stream)
-                            : launch<PAIR, kResidual, kOne>(t, t.items, device, sms, stream);
+            // What one accumulator cuts of s (kLong: 6e-5 of it at most, 1.4e-5 as a rule) is a relative error of exp(s - lse)
+            // as large as s times that: below rounding to 16 bits for |s| of some 30 (bf16: 100).  Longer rows' sums go on
+            // in exact parts, so that they lose no more.
+            return p.planes      ? launch<PAIR, kResidual, kExactParts, true>(t, t.items, device, sms, stream)
+                   : p.k > kLong ? launch<PAIR, kResidual, kExactParts>(t, t.items, device, sms, stream)
+                                 : launch<PAIR, kResidual, kOne>(t, t.items, device, sms, stream);
     }
 }
 

@@ -38,3 +38,24 @@ def test_long_sums_in_16_bits(dtype):
     # As long a sum in y: the same rows as columns.
     y = c.multiply(x.t().contiguous(), dy[None], torch.tensor([0, K], dtype=torch.int32, device="cuda"))
     assert bias(y[:64, :64], x[:, :64].double().t() @ dy[:, :64].double()) <= most
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_probabilities_of_long_rows(dtype):
+    """524,288 columns, every s near 20: one accumulator would make s 2e-2 and with it every
+    probability 2 % too small.  Off by 8 2^-23 20 for s and as much for the log-sum-exp, 2^-20 for exp, what
+    holding and storing gradients rounds, and the roundings of 2,048 parts' sum, each up to 2^-20 to either
+    side: six times 2,048^1/2 2^-20 / 3^1/2."""
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    R, D, V = 256, 1 << 19, 2048
+    z, w = positive(g, R, D, dtype=dtype, scale=2.0 ** -8), positive(g, V, D, dtype=dtype, scale=20.0 * 2.0 ** -11)
+    labels = torch.zeros(R, dtype=torch.int64, device="cuda")
+    s = c.score(z, w.t(), labels, upstream=torch.tensor([4096.0], device="cuda"))
+    step = 1 << 16
+    logits = sum(z[:, a:a + step].double() @ w[:, a:a + step].double().t() for a in range(0, D, step))
+    p = torch.softmax(logits, 1)
+    off = 2 * 8 * 2.0 ** -23 * 21 + 6 * (2048 / 3) ** 0.5 * 2.0 ** -20
+    assert float((s.rows.double() + torch.log(p[:, 0])).abs().max()) <= off + 2.0 ** -18
+    want = z[:, :512].double().t() @ p[:, 1:] * (4096.0 / R)
+    assert bias(s.dw[:512, 1:], want) <= off + 2.0 ** -20 + 2 * UNIT[dtype] / 64
