@@ -832,7 +832,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                             for (int j = 0; j < 32; ++j)
                                 if (mine && at == c + j) p.at_label[m] = v[0][j];
                         }
-                        const float shift = next == -INFINITY ? 0.0f : next;
+                        const float shift = fabsf(next) == INFINITY ? 0.0f : next;      // (of an infinite one the sum is)
                         float part[4] = {sum * exp2_fast((top - shift) * kLog2E), 0.0f, 0.0f, 0.0f};
 #pragma unroll
                         for (int j = 0; j < 32; ++j) part[j & 3] += exp2_fast((v[0][j] - shift) * kLog2E);
@@ -850,7 +850,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory");
                     if (!odd && live) {
                         const float2 o = *other;
-                        const float most = fmaxf(top, o.x), zero = most == -INFINITY ? 0.0f : most;
+                        const float most = fmaxf(top, o.x), zero = fabsf(most) == INFINITY ? 0.0f : most;
                         sum = sum * exp2_fast((top - zero) * kLog2E) + o.y * exp2_fast((o.x - zero) * kLog2E);
                         p.parts[w.n_tile * p.m + m] = make_float2(most, sum);
                     }

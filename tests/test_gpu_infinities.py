@@ -79,3 +79,31 @@ def test_classes_that_are_shut(rows, dtype, flip):
     u = 2 * torch.finfo(dtype).eps / 2 + 1e-5
     assert not s.dw[:, shut].any() and off(s.dw[:, open_], dw) <= u
     assert s.dz[:, 5].isnan().all() and off(s.dz[:, rest], dz[:, rest]) <= u
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows, cols, classes", [(40, 24, 10), (64, 128, 520), (700, 128, 3100), (4096, 128, 520)])
+def test_losses_of_infinite_values(rows, cols, classes, dtype):
+    """A class of infinite value: the loss of another one is infinite, its own is no number, and rows that it
+    shuts or leaves alone have theirs; whichever kernels the size takes."""
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(9)
+    w = (torch.randn(cols, classes, generator=g, device="cuda") * cols ** -0.5).to(dtype)
+    z = torch.randn(rows, cols, generator=g, device="cuda").to(dtype)
+    w[5, 7], w[5, 8:] = float("inf"), 0.0
+    z[:, 5] = torch.tensor([1.0, -1.0], device="cuda").repeat(rows // 2).to(dtype)
+    w[5, :7] = 0.0
+    labels = torch.randint(0, 7, (rows,), generator=g, device="cuda")
+    labels[:8] = 7
+    labels[8:12] = classes - 1
+    s = c.score(z, w, labels, grad=False)
+    logits = z.double() @ w.double()
+    want = torch.logsumexp(logits, 1) - logits.gather(1, labels[:, None])[:, 0]
+    assert torch.equal(signs(s.rows), signs(want))
+    assert want[0].isnan() and want[1].isposinf() and want[8].isposinf() and want[9].isfinite()
+    on = want.isfinite()
+    rest = torch.arange(cols, device="cuda") != 5
+    size = z[:, rest].double().abs() @ w[rest].double().abs()
+    bound = 2 * cols * U23 * size.max(1).values + 2.0 ** -20 * (1 + want.abs())
+    assert bool(((s.rows.double() - want).abs() <= bound)[on].all()) and bool(on.any())
+    assert s.loss.isnan().all()
