@@ -708,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
             const int64_t in = label - p.n0 - w.n0;
             const int at = has && in >= 0 && in < count ? (int)in : -1;
             const bool mine = at >= 0 && (at >> 5 & 1) == odd;
-            const float lse = ENDING == kResidual && has ? p.lse[m] : INFINITY;
+            const float lse = ENDING == kResidual && has ? p.lse[m] : 0.0f;
             const float own = ENDING == kResidual && mine ? target.factor * expm1f(-p.row_loss[m]) : 0.0f;
             const int64_t base = (ENDING == kStore ? (p.ragged == kRaggedK ? w.group * p.step_out : 0) + w.split * p.step_split : 0) +
                                  w.n0 * target.ld + m;
@@ -731,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                     for (int j = 0; j < 32; ++j)
                         if (j < count - c) {
                             __nv_bfloat16 y[3];
-                            planes_of(j == own_at ? own : exp2_fast((x[j] - lse) * kLog2E), y);
+                            planes_of(j == own_at ? own : has ? exp2_fast((x[j] - lse) * kLog2E) : 0.0f, y);
 #pragma unroll
                             for (int i = 0; i < 3; ++i) out[i * p.step_plane] = y[i];
                             out += target.ld;
@@ -744,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
                         if (j < count - c) {
-                            *out = from_f32<T>(exp2_fast(fmaf(x[j] - lse, kLog2E, more)));
+                            *out = from_f32<T>(has ? exp2_fast(fmaf(x[j] - lse, kLog2E, more)) : 0.0f);
                             out += target.ld;
                         }
                     if ((uint32_t)own_at < 32u) out[(own_at - min(32, count - c)) * target.ld] = from_f32<T>(own);

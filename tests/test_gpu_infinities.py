@@ -107,3 +107,32 @@ def test_losses_of_infinite_values(rows, cols, classes, dtype):
     bound = 2 * cols * U23 * size.max(1).values + 2.0 ** -20 * (1 + want.abs())
     assert bool(((s.rows.double() - want).abs() <= bound)[on].all()) and bool(on.any())
     assert s.loss.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows, classes", [(40, 10), (64, 520), (500, 4200), (700, 3100), (4096, 520)])
+def test_shut_classes_and_rows_without_labels(rows, classes, dtype):
+    """Rows without a label take no part where classes are shut either: the gradients are those of the
+    others' alone, and zeros in their place."""
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(10)
+    cols = 128
+    w = (torch.randn(cols, classes, generator=g, device="cuda") * cols ** -0.5).to(dtype)
+    z = torch.randn(rows, cols, generator=g, device="cuda").to(dtype)
+    z[:, 5] = 1.0
+    shut = torch.arange(classes, device="cuda") % 3 == 1
+    w[5, shut] = -float("inf")
+    labels = torch.randint(0, (classes - 1) // 3, (rows,), generator=g, device="cuda") * 3
+    labels[torch.rand(rows, generator=g, device="cuda") < 0.3] = -1
+    on = labels >= 0
+    s = c.score(z, w, labels)
+    logits = z[on].double() @ w[:, ~shut].double()
+    p = torch.softmax(logits, 1)
+    at = torch.cumsum(~shut, 0)[labels[on]] - 1
+    p[torch.arange(p.shape[0], device="cuda"), at] -= 1.0
+    n, rest = p.shape[0], torch.arange(cols, device="cuda") != 5
+    # g's and the results' roundings, in the 2-norm.
+    u = 2 * torch.finfo(dtype).eps / 2 + 1e-5
+    assert s.rows.isfinite().all() and not s.rows[~on].any()
+    assert not s.dw[:, shut].any() and off(s.dw[:, ~shut], z[on].double().t() @ p / n) <= u
+    assert not s.dz[~on].any() and off(s.dz[on][:, rest], (p @ w[:, ~shut].double().t() / n)[:, rest]) <= u
