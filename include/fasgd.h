@@ -761,8 +761,9 @@ FASGD_API int fasgd_combine_grad(const fasgd_exchange_args* a, void* stream);
  * fasgd_multiply_grad -- given dy: dx[i] = dy[i] w[e]^T (0 where no expert has the row) and
  * dw[e] = sum_i x[i]^T dy[i] (0 for an expert without rows), of type w_dtype and laid out
  * by ld_dw, step_dw and dw_flip.  dx or dw may be NULL.  x is read for dw only, w for dx.
- * Sums are fp32, in an order that the arguments fix, and values that are not finite make
- * results as fp32 products and sums do; but in large products of FASGD_F32 (from rows x inputs x
+ * Sums are fp32, in an order that the arguments fix; before it is rounded, one that is stored
+ * in 16 bits may be off by 2^-11 of its terms' size (2^-13 as a rule; of more than 16,384 terms by
+ * 2^-14).  Values that are not finite make results as fp32 products and sums do; but in large products of FASGD_F32 (from rows x inputs x
  * outputs = 2^28 on) a product of two finite values beyond fp32's range may make NaN of
  * an infinite result.  Rows that no expert has are not read, whatever they hold.
  * rows < 2^31; inputs, outputs <= FASGD_COLS_MAX; experts <= FASGD_EXPERTS_MAX.
@@ -808,7 +809,8 @@ FASGD_API int64_t fasgd_multiply_workspace(const fasgd_multiply_args* a);
  * take part, whatever it holds, and its dz is 0.  z: rows x cols; w and dw: cols x
  * classes, or (flip) classes x cols.  upstream: device float or NULL (1).
  * s and its sums are fp32; for 16-bit types g takes part in its two products rounded to
- * dtype.  rows < 2^31, cols <= FASGD_COLS_MAX, classes <= 2^24.
+ * dtype, formed of an s that may be off by 2^-14 of its terms' size (2^-16 as a rule).
+ * rows < 2^31, cols <= FASGD_COLS_MAX, classes <= 2^24.
  * lse: fp32[rows] (rows without a label: any value) or NULL.  known = 0: it is written.
  * known = 1: it and row_loss hold what an earlier call left there for the same z, w and
  * labels; loss is then not looked at, and only dz and dw, one of them at least, are

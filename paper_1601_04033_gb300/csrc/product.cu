@@ -1,9 +1,8 @@
 // Matrix products of fp32 values in their simple form: 64 x 64 tiles of D in registers, 32
 // steps of k through shared memory at a time, the next 32 read meanwhile.  Right for every layout,
-// alignment and size; for products too small for planes (by_planes) also the fastest here: 12 us for
-// 128 x 128 x 128, where planes take 20, and 35 us for 1,024 rows of 512 x 512 in 4 experts, where they
-// take 39; at 1,024 x 1,024 x 1,024 it is 92 us (23 TFLOP/s) to 54.  It is bound by its shared-memory
-// reads, 8 of them for 16 multiply-adds.
+// alignment and size; for products too small for planes (by_planes) also the fastest here: 11 us for
+// 128 x 128 x 128, where planes take 13; at 1,024 x 1,024 x 1,024 it is 104 us (21 TFLOP/s) to 29.  At 229 registers
+// a thread one block fits on an SM, whose eight warps leave its loads' latency exposed at every stage.
 //
 // Also here: the copies that lay sides out for the tensor cores, and the sums of parts of k.
 

@@ -101,7 +101,7 @@ inline int32_t statistics_tile(int64_t m, int64_t n) {
         }
     return best;
 }
-// How a product falls to the SMs: blocks or pairs of them, parts of k's sums, n of a tile.
+// How a product falls to the SMs: blocks or pairs of them, parts of k's sums.
 struct TilePlan {
     int32_t pair, splits;
 };
@@ -121,8 +121,10 @@ inline int64_t part_values(const Product& p) {
     return splits > 1 ? splits * p.n * p.m * (p.ragged == kRaggedK ? p.groups : 1) : 0;
 }
 // Whether an fp32 product of m x n x k goes by planes: from where copies and launches of theirs are made
-// up for.  Measured on both sides: y of 1,024 rows by 512 x 512 in 4 experts (2^28) 35 us plain and 39 by
-// planes; a score's gradients of 512 x 512 x 2,048 (2^29) 243 and 161; y of 1,024 x 1,024 x 1,024 92 and 54.
+// up for.  Measured on both sides: y of 128 x 128 x 128 11 us plain and 13 by planes; of 1,024 rows by 512 x 512 in 4
+// experts (2^28) 31 and 25, of 1,024 x 1,024 x 1,024 104 and 29, of 512 rows by 1,024 x 1,024 in 128 experts, where the
+// copies are of 134 million values for 2^29 multiply-adds, 692 and 472; a score of 512 x 512 x 2,048 with gradients
+// 244 and 110.
 inline bool by_planes(int64_t m, int64_t n, int64_t k) {
     return (double)m * (double)n * (double)k >= kPlanesFrom;
 }
@@ -149,9 +151,9 @@ inline cudaError_t launch_product(const Product& p, float* parts, cudaStream_t s
 
 // A copy of a side with rows that lie as the fast kernels want them: `rows` rows of `cols`
 // values (of group g: p + g * step) to rows ld_to apart (a multiple of 8, as step_to and plane; what is
-// between the rows is overwritten), of the same type or rounded from fp32.  What it leaves
-// out is not read: groups without rows by offsets (null: none is left out), and rows
-// without a label (labels null: none; its copy is 0).
+// between the rows is overwritten), of the same type or rounded from fp32.  Groups without rows by
+// offsets (null: there are none) are not read or written; the copy of a row without a label (labels
+// null: all have one) is 0 whatever the row holds.
 struct Pack {
     const void* from;
     void* to;

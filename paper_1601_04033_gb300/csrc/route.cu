@@ -2,10 +2,11 @@
 //
 // The entries fall into chunks of consecutive ones, a block each, and a chunk into
 // one piece for each of its warps, so (chunk, warp, step, lane) is the entries' own
-// order.  A warp counts its piece 32 entries at a time: lanes of one expert find each
-// other (match), and the first of them adds their number to the warp's counter of that
-// expert in shared memory.  Counters become first places by sums over experts, earlier
-// chunks and earlier warps; a second sweep hands the places out the same way.
+// order.  A warp counts its piece 32 entries at a time, each lane adding one to the warp's
+// counter of its entry's expert in shared memory.  Counters become first places by sums over
+// experts, earlier chunks and earlier warps.  A second sweep hands the places out: lanes of one
+// expert find each other by votes over the bits of its number, take the places behind its
+// counter in their order, and the first of them moves the counter on.
 //
 // Short lists (128 rows of a minibatch) take one block and one launch.  Longer ones take
 // two: each block of the second adds up the counters of all chunks itself, at most 64

@@ -21,7 +21,9 @@
 // 2,048).  Short products are bound by a launch's latency (6 us) and 0.3 us for each 64 of k.
 //
 // Every wait is bounded (wait_thread): one that runs out raises the block's flag, every
-// role leaves, and what was not computed is written as NaN.
+// role leaves, what was not computed is written as NaN, and the host learns of it (read_late).
+//
+// Kernels that add sums up in registers (Sums) spill 36 to 44 bytes at 216 of them.
 
 #include <cuda.h>
 
