@@ -59,3 +59,33 @@ def test_probabilities_of_long_rows(dtype):
     assert float((s.rows.double() + torch.log(p[:, 0])).abs().max()) <= off + 2.0 ** -18
     want = z[:, :512].double().t() @ p[:, 1:] * (4096.0 / R)
     assert bias(s.dw[:512, 1:], want) <= off + 2.0 ** -20 + 2 * UNIT[dtype] / 64
+
+
+def test_small_products_in_fp32():
+    """Sums of 4,000 terms of either sign on the ordinary cores, in parts of 256.  An addition rounds by 2^-24 of
+    what is there at most, a half of that in the root of the mean square; after i terms that is i^1/2 terms, in all
+    (n / 2)^1/2 2^-25 of a part of n and as much of the 16 parts: 4.2e-7 (one after the other: 1.3e-6)."""
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    E, K, N = 40, 4000, 256
+    x, w = torch.randn(4 * E, K, generator=g, device="cuda"), torch.randn(E, K, N, generator=g, device="cuda")
+    y = c.multiply(x, w, torch.arange(0, 4 * E + 1, 4, dtype=torch.int32, device="cuda"))
+    want = torch.bmm(x.double().reshape(E, 4, K), w.double()).reshape(4 * E, N)
+    assert float((y.double() - want).norm() / want.norm()) <= ((256 / 2) ** 0.5 + (16 / 2) ** 0.5) * 2.0 ** -25
+
+
+def test_gradients_of_few_rows_in_fp32():
+    """g is -1 for one class and some 1e-5 for each of the others: whatever is added after that one's part rounds by
+    2^-24 of it at most.  256 such roundings to either side are 16 / 3^1/2 2^-24, the parts' sum (54 in each of 16)
+    less than as much again, and g itself is off by some 2^-22."""
+    c = _c()
+    g = torch.Generator(device="cuda").manual_seed(4)
+    R, D, V = 3, 24, 220561
+    w = torch.randn(D, V, generator=g, device="cuda") * 0.3
+    z = torch.randn(R, D, generator=g, device="cuda")
+    labels = torch.tensor([3, 100000, 220560], device="cuda")
+    s = c.score(z, w, labels)
+    p = torch.softmax(z.double() @ w.double(), 1)
+    p[torch.arange(R), labels] -= 1.0
+    want = p @ w.double().t() / R
+    assert float((s.dz.double() - want).norm() / want.norm()) <= 2 * 16 / 3 ** 0.5 * 2.0 ** -24 + 2.0 ** -22
